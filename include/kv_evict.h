@@ -71,7 +71,8 @@ typedef enum {
   KVE_EINVAL = 1,   /* invalid argument or unsupported shape (host check)     */
   KVE_ECUDA = 2,    /* a CUDA runtime/driver call failed                      */
   KVE_ETIMEOUT = 3, /* a device-side bounded wait ran out (kv_evict_status)   */
-  KVE_ENOMEM = 4    /* host allocation failed                                 */
+  KVE_ENOMEM = 4,   /* host allocation failed                                 */
+  KVE_EPAGES = 5    /* too few free pages (kv_evict_cache_status)             */
 } kve_status;
 
 typedef struct {
@@ -316,6 +317,136 @@ kve_status kv_evict_profile(int32_t kind, const float* c, int32_t num_layers,
  * unless B >= 1, num_layers >= 1 and 0 < last_ratio <= 1. */
 kve_status kv_evict_budget_pyramid(int32_t budget, int32_t num_layers,
                                    float last_ratio, int32_t* budgets_out);
+
+/* ------------------------------------------------------------------------------------
+ * The paged 8-bit cache: what a serving program decodes from after an eviction.
+ *
+ * A sequence's compact cache is kept in 8 bits, in pages of P tokens that a block table
+ * names, and grows as the model answers. Four calls work on it:
+ *   kv_evict_cache_pages   pages taken and released, and the slots of new tokens, from
+ *                          the sequences' old and new lengths (on the GPU);
+ *   kv_evict_cache_gather  step 4 into the cache: the kept and the window rows;
+ *   kv_evict_cache_store   new tokens' key and value rows, written by slot;
+ *   kv_evict_cache_attend  attention of new tokens' queries over one layer's sequences.
+ *
+ *  * H = num_kv_heads is the number of heads whose rows the cache holds: the KV heads,
+ *    or the query heads for a KVE_PLAN_PER_QUERY_HEAD plan (then num_q_heads = H).
+ *    Query head hq reads cache head hq / G, G = num_q_heads / H. S = max_seqs.
+ *  * Pages:  k, v [num_pages][H][P][d] uint8, e4m3 codes (1 sign, 4 exponent, 3 fraction
+ *    bits, largest 448, no infinities); k_scale, v_scale [num_pages][H] fp32. A cached
+ *    value is its code's value times the scale of its page and head. The pages are shared
+ *    by all layers.
+ *  * Scales are powers of two: need(a) is the smallest 2^e, e >= -126, with a <= 448 * 2^e
+ *    for the largest finite magnitude a of the rows that share it. A code is the value
+ *    divided by the scale, rounded to the nearest (ties to even); infinities become the
+ *    largest code of their sign, NaN stays NaN. A power of two loses at most one of the 18
+ *    binades that a code spans and none of its fraction bits, and a page whose scale grows
+ *    keeps its older codes exactly, but for those that become subnormal.
+ *  * table [N_L][S][max_pages] int32: page j of a sequence holds its tokens j*P ..
+ *    j*P + P - 1. Entries at and behind ceil(len / P) are not read. Position i of a
+ *    sequence is slot table[i / P] * P + i % P.
+ *  * lens [N_L][S] int32: tokens in the cache, 0 .. max_pages * P; budgets may differ by
+ *    layer, so lengths do.
+ *  * The workspace ws (256-byte aligned) belongs to one cache and is cleared once by
+ *    kv_evict_cache_reset; calls that use it must not overlap on the GPU. Page numbers and
+ *    slots outside the pool are never followed: the call leaves those tokens out and
+ *    reports KVE_ECUDA through kv_evict_cache_status.
+ *  * The handle holds the addresses of k, v, k_scale and v_scale; it is immutable. A call
+ *    made while another device than theirs is current returns KVE_EINVAL.
+ * ---------------------------------------------------------------------------------- */
+typedef struct {
+  int32_t num_layers;       /* N_L, 1 .. 256                                   */
+  int32_t num_q_heads;      /* a multiple of num_kv_heads, G <= 128            */
+  int32_t num_kv_heads;     /* H, 1 .. 1024                                    */
+  int32_t head_dim;         /* d; this build supports d = 128                  */
+  int32_t page_tokens;      /* P: 16, 32, 64 or 128                            */
+  int32_t num_pages;        /* pages in the pool, num_pages * H * P < 2^31     */
+  int32_t max_pages;        /* pages of one sequence, 1 .. num_pages           */
+  int32_t max_seqs;         /* S, 1 .. 1024                                    */
+} kve_cache_config;
+
+typedef struct kve_cache kve_cache;
+
+/* A cache of cfg over device buffers that the caller owns (k and v 128-byte, the scales
+ * 16-byte aligned; nothing is written). The handle owns host memory only.
+ * *workspace_bytes receives the size of ws. */
+kve_status kv_evict_cache_create(const kve_cache_config* cfg, uint8_t* k, uint8_t* v,
+                                 float* k_scale, float* v_scale, kve_cache** cache_out,
+                                 size_t* workspace_bytes);
+
+void kv_evict_cache_destroy(kve_cache* cache);
+
+/* Clears ws, and where free_pages and ring are given makes every page free:
+ * free_pages [num_pages] = 0, 1, .., ring [2] = {0, num_pages}. Both or neither. */
+kve_status kv_evict_cache_reset(const kve_cache* cache, int32_t* free_pages, int32_t* ring,
+                                void* ws, void* stream);
+
+/* Pages and slots of every sequence, from lens_from to lens_to (each [N_L][S], device
+ * memory). free_pages [num_pages] is a ring of page numbers, ring_in = {head, count}: the
+ * free pages are entries head .. head + count - 1 modulo num_pages. In the order (layer,
+ * sequence, page), a sequence that grows takes ceil(to / P) - ceil(from / P) pages from the
+ * ring's head into its table row, one that shrinks gives its last pages to the ring's tail
+ * (their table entries stay as they were). ring_out and lens_out (= lens_to) receive the
+ * state after the call. Pages released here can be taken from the next call on.
+ * slots (or NULL) [N_L][slot_stride] receives per layer the slots of the new tokens
+ * (positions from .. to - 1 where to > from), packed in sequence order, -1 behind them: the
+ * slots argument of kv_evict_cache_store for that layer.
+ * All or nothing: if the free pages do not suffice (KVE_EPAGES), or a length or the ring is
+ * out of range, or a layer has more than slot_stride new tokens (KVE_ECUDA), no page moves,
+ * lens_out = lens_from, ring_out = ring_in, every slot is -1, and kv_evict_cache_status
+ * tells. ring_out may be ring_in, and lens_out may be lens_from or lens_to, so that one
+ * captured graph can advance its own state. Tables are int32 throughout and the call
+ * neither synchronises nor allocates. */
+kve_status kv_evict_cache_pages(const kve_cache* cache, const int32_t* lens_from,
+                                const int32_t* lens_to, int32_t* table, int32_t* free_pages,
+                                const int32_t* ring_in, int32_t* ring_out, int32_t* lens_out,
+                                int32_t* slots, int64_t slot_stride, void* ws, void* stream);
+
+/* Step 4 into the cache: the rows that kv_evict_gather would copy for the plan's request r,
+ * in its order (kept candidates ascending, then the window rows), become positions 0 ..
+ * m + W - 1 of sequence first_seq + r of every layer, in 8 bits. The table rows of those
+ * sequences hold the pages (kv_evict_cache_pages with lens_to = m + W). Rows of the last
+ * page behind the sequence are left as they were. k, v and indices as for kv_evict_gather
+ * (pinned host memory too); the plan and the cache have the same layers and heads. */
+kve_status kv_evict_cache_gather(const kve_cache* cache, const kve_plan* plan,
+                                 const uint16_t* k, const uint16_t* v, const int32_t* indices,
+                                 int32_t first_seq, const int32_t* table, void* ws,
+                                 void* stream);
+
+/* Key and value rows of n_tokens new tokens of one layer, written by slot: token t's rows
+ * go to slots[t]; a negative slot (a padded batch) writes nothing. k_new, v_new [n_tokens]
+ * [H][d] bf16, 16-byte aligned, with element strides {token, head} (multiples of 8, not
+ * negative; NULL is dense). Tokens of one page that the call writes stand together in
+ * ascending order (as kv_evict_cache_pages packs them); a page written from two places of
+ * the call gets undefined codes. A run of tokens that starts at row 0 of a page sets its scale to
+ * need of its rows; one that starts later keeps the larger of need and the page's scale,
+ * and where that grows, the page's older rows are rounded to it once more. Making the same
+ * call again changes nothing. n_tokens < 2^20. */
+kve_status kv_evict_cache_store(const kve_cache* cache, const uint16_t* k_new,
+                                const uint16_t* v_new, const int64_t* k_strides,
+                                const int64_t* v_strides, const int32_t* slots,
+                                int64_t n_tokens, void* ws, void* stream);
+
+/* Attention of layer `layer`: q_tokens (T >= 1, G * T <= 128) queries of each of the
+ * sequences 0 .. n_seq - 1, whose keys and values are in the cache already. Query t of a
+ * sequence of length len stands at position len - T + t and sees the positions up to its
+ * own:  out = sum_i softmax(q . k_i / sqrt(d)) v_i.  A query that sees nothing (len < T - t, an
+ * empty sequence) gets zeros and lse = -inf. Rows of sequences behind n_seq are left as
+ * they were. q, out [n_seq * T][Hq][d] bf16, 16-byte aligned, element strides {token, head}
+ * (multiples of 8, not negative; NULL is dense; out's rows must not overlap). lse (or NULL)
+ * [n_seq * T][Hq] fp32: ln sum_i exp(q . k_i / sqrt(d)). The table and lens of every layer
+ * are passed; layer picks. What the pages hold behind a sequence, NaN codes included, has
+ * no part in its rows. A query row with an infinity or a NaN gives NaN. */
+kve_status kv_evict_cache_attend(const kve_cache* cache, int32_t layer, int32_t n_seq,
+                                 int32_t q_tokens, const uint16_t* q, const int64_t* q_strides,
+                                 const int32_t* table, const int32_t* lens, uint16_t* out,
+                                 const int64_t* out_strides, float* lse, void* ws,
+                                 void* stream);
+
+/* Synchronise the stream, read the error word of ws and clear it: KVE_OK, KVE_EPAGES (too
+ * few free pages), KVE_ETIMEOUT (a bounded wait ran out) or KVE_ECUDA (a length, page, slot
+ * or ring entry out of range, or a CUDA call failed). */
+kve_status kv_evict_cache_status(const kve_cache* cache, void* ws, void* stream);
 
 const char* kv_evict_strerror(kve_status status);
 

@@ -1,0 +1,710 @@
+// The paged 8-bit cache: its C entry points, and the kernels that keep its tables and write its
+// pages (the attention that reads them is in kve_attend.cu).
+//
+// A page holds P tokens of every cache head: e4m3 codes and one power-of-two scale per (page, head).
+// For the rows that share a scale and their largest finite magnitude a,
+//   need(a) = 2^e, the smallest e >= -126 with a <= 448 * 2^e,   code = RN_e4m3(x / scale).
+// Division by a power of two is exact, so a code is rounded once, and a page whose scale grows by 2^k
+// keeps RN(x / 2^e) / 2^k = RN(x / 2^(e+k)) for every code that stays normal.
+#include <algorithm>
+#include <cmath>
+#include <cstring>
+#include <new>
+
+#include "kve_internal.h"
+#include "kve_ptx.cuh"
+
+namespace kve {
+namespace {
+
+// ---------------------------------------------------------------- tables and slots
+
+constexpr int kPagesThreads = 256;
+constexpr int kPagesWarps = kPagesThreads / 32;
+
+__device__ __forceinline__ long long warp_sum(long long x) {
+#pragma unroll
+  for (int o = 16; o > 0; o >>= 1) x += __shfl_xor_sync(0xffffffffu, x, o);
+  return x;
+}
+
+__device__ __forceinline__ int ring_at(int head, long long i, int n) {
+  // head < n and i <= n (checked before any use)
+  long long p = head + i;
+  if (p >= n) p -= n;
+  if (p >= n) p -= n;
+  return static_cast<int>(p);
+}
+
+// Every CTA sums the pages that all sequences take and give (so all agree whether the call can be
+// done, before one of them writes) and those of the sequences in front of its own eight, a warp each;
+// blockIdx.y deals a sequence's pages and slots to more than one warp where they are long. What the
+// call changes in place (lens_out, ring_out may be inputs) is written by the CTA that finishes
+// reading last.
+//
+// Nothing here is bound by bandwidth at a decode step: it is the latency of the sums, one pass over
+// 8 bytes a sequence from L2, and of the chain length -> ring entry -> table.
+__global__ void __launch_bounds__(kPagesThreads) cache_pages_kernel(const __grid_constant__ PagesParams P) {
+  wait_previous_kernel();
+  __shared__ long long sum[4][kPagesWarps];        // taken, given: of all, of those in front
+  __shared__ unsigned long long layer_new[kMaxLayers];
+  __shared__ uint32_t bad_word;
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+  const int S = P.c.max_seqs, n = P.c.num_layers * S, shift = P.c.page_shift, page_mask = P.c.page - 1;
+  const int cap = P.c.max_pages << shift;
+  const int first = blockIdx.x * kPagesWarps;
+  for (int i = threadIdx.x; i < P.c.num_layers; i += kPagesThreads) layer_new[i] = 0;
+  if (threadIdx.x == 0) bad_word = 0;
+  __syncthreads();
+  long long taken = 0, given = 0, taken_front = 0, given_front = 0;
+  bool bad = false;
+  int run_layer = -1;
+  unsigned long long run = 0;
+  for (int i = threadIdx.x; i < n; i += kPagesThreads) {
+    const int a = __ldg(P.from + i), b = __ldg(P.to + i);
+    bad |= a < 0 || b < 0 || a > cap || b > cap;
+    const int d = ((b + page_mask) >> shift) - ((a + page_mask) >> shift);
+    taken += max(d, 0);
+    given += max(-d, 0);
+    if (i < first) {
+      taken_front += max(d, 0);
+      given_front += max(-d, 0);
+    }
+    if (P.slots && b > a) {
+      const int l = i / S;
+      if (l != run_layer) {
+        if (run) atomicAdd(&layer_new[run_layer], run);
+        run_layer = l;
+        run = 0;
+      }
+      run += static_cast<unsigned>(b - a);
+    }
+  }
+  if (run) atomicAdd(&layer_new[run_layer], run);
+  if (bad) bad_word = 1;
+  taken = warp_sum(taken);
+  given = warp_sum(given);
+  taken_front = warp_sum(taken_front);
+  given_front = warp_sum(given_front);
+  if (lane == 0) {
+    sum[0][warp] = taken;
+    sum[1][warp] = given;
+    sum[2][warp] = taken_front;
+    sum[3][warp] = given_front;
+  }
+  const int head = __ldg(P.ring_in), count = __ldg(P.ring_in + 1), np = P.c.num_pages;
+  __syncthreads();
+  taken = given = taken_front = given_front = 0;
+#pragma unroll
+  for (int w = 0; w < kPagesWarps; ++w) {
+    taken += sum[0][w];
+    given += sum[1][w];
+    taken_front += sum[2][w];
+    given_front += sum[3][w];
+  }
+  bad = bad_word || head < 0 || head >= np || count < 0 || count > np || count + given > np;
+  if (P.slots)
+    for (int l = 0; l < P.c.num_layers; ++l)
+      bad |= layer_new[l] > static_cast<unsigned long long>(P.slot_stride);
+  const bool ok = !bad && taken <= count;
+  const int seq = first + warp;
+  if (seq < n) {
+    const int layer = seq / S, r = seq - layer * S;
+    const int step = 32 * gridDim.y, start = lane + 32 * blockIdx.y;
+    // pages of this CTA's earlier sequences, and the new tokens of this layer's
+    long long at = 0, back = 0, tok = 0;
+    if (lane < warp) {
+      const int a = __ldg(P.from + first + lane), b = __ldg(P.to + first + lane);
+      const int d = ((b + page_mask) >> shift) - ((a + page_mask) >> shift);
+      at = max(d, 0);
+      back = max(-d, 0);
+    }
+    at = taken_front + warp_sum(at);
+    back = given_front + warp_sum(back);
+    if (P.slots) {
+      for (int i = lane; i < r; i += 32)
+        tok += max(__ldg(P.to + layer * S + i) - __ldg(P.from + layer * S + i), 0);
+      tok = warp_sum(tok);
+    }
+    const int a = __ldg(P.from + seq), b = __ldg(P.to + seq);
+    int32_t* row = P.table + static_cast<int64_t>(seq) * P.c.max_pages;
+    if (ok) {
+      const int have = (a + page_mask) >> shift, need = (b + page_mask) >> shift;
+      for (int j = have + start; j < need; j += step) row[j] = P.free_pages[ring_at(head, at + (j - have), np)];
+      for (int j = need + start; j < have; j += step)
+        P.free_pages[ring_at(head, count + back + (j - need), np)] = row[j];
+      if (P.slots) {
+        int32_t* out = P.slots + layer * P.slot_stride + tok;
+#pragma unroll 4
+        for (int i = start; i < b - a; i += step) {
+          const int pos = a + i, j = pos >> shift;
+          const int page = j < have ? row[j] : P.free_pages[ring_at(head, at + (j - have), np)];
+          out[i] = page >= 0 && page < np ? (page << shift) + (pos & page_mask) : -1;
+        }
+      }
+    }
+    if (P.slots && r == S - 1) {
+      // behind the layer's new tokens (from its start where nothing was done)
+      const int64_t end = ok ? static_cast<int64_t>(layer_new[layer]) : 0;
+      int32_t* out = P.slots + layer * P.slot_stride;
+      for (int64_t i = end + start; i < P.slot_stride; i += step) out[i] = -1;
+    }
+  }
+  // the last CTA moves the state on
+  __syncthreads();
+  if (threadIdx.x == 0) {
+    __threadfence();
+    bad_word = atomicInc(P.done, gridDim.x * gridDim.y - 1) == gridDim.x * gridDim.y - 1;
+  }
+  __syncthreads();
+  if (!bad_word) return;
+  __threadfence();
+  const int32_t* now = ok ? P.to : P.from;
+  if (P.lens_out != now)
+    for (int i = threadIdx.x; i < n; i += kPagesThreads) P.lens_out[i] = now[i];
+  if (threadIdx.x == 0) {
+    P.ring_out[0] = ok ? ring_at(head, taken, np) : head;
+    P.ring_out[1] = ok ? static_cast<int>(count - taken + given) : count;
+    if (!ok) atomicOr(P.err, bad ? kErrCheck : kErrPages);
+  }
+}
+
+__global__ void cache_reset_kernel(int32_t* free_pages, int32_t* ring, int n) {
+  wait_previous_kernel();
+  for (int i = blockIdx.x * blockDim.x + threadIdx.x; i < n; i += gridDim.x * blockDim.x) free_pages[i] = i;
+  if (blockIdx.x == 0 && threadIdx.x == 0) {
+    ring[0] = 0;
+    ring[1] = n;
+  }
+}
+
+// ---------------------------------------------------------------- rows in 8 bits
+
+// A run (new rows of one page and head, of keys or of values) is written by a team of P / 16 groups of 16
+// lanes; group g holds page rows 16 g .. 16 g + 15 in registers, 8 elements of each row a lane, from
+// the load of a row to the store of its codes: bf16 is read once and codes are written once, whatever
+// P. 64 registers of rows a thread leave three CTAs an SM, 192 KB of loads in flight.
+constexpr int kRowThreads = 256;
+constexpr int kGroupRows = 16;
+
+__device__ __forceinline__ uint32_t max_u16x2(uint32_t a, uint32_t b) {
+  uint32_t d;
+  asm("max.u16x2 %0, %1, %2;" : "=r"(d) : "r"(a), "r"(b));
+  return d;
+}
+
+// The largest finite magnitude of the bf16 pair x, or'ed into the pair m of magnitudes.
+__device__ __forceinline__ uint32_t max_finite(uint32_t m, uint32_t x) {
+  x &= 0x7fff7fffu;
+  if ((x & 0xffffu) >= 0x7f80u) x &= 0xffff0000u;
+  if (x >= 0x7f800000u) x &= 0x0000ffffu;
+  return max_u16x2(m, x);
+}
+
+// need(a) as fp32 bits for the magnitude with bf16 bits a (finite): a = (1 + f/128) 2^(x-127), and
+// 448 = 1.75 * 2^8, so e = x - 127 - 8, one more where the fraction passes 1.75 (f > 96).
+__device__ __forceinline__ uint32_t need_bits(uint32_t a) {
+  const int e = static_cast<int>(a >> 7) - 8 + ((a & 0x7fu) > 96u ? 1 : 0);
+  return static_cast<uint32_t>(max(e, 1)) << 23;
+}
+
+// Two fp32 values as e4m3 codes (lo in the low byte), rounded to the nearest, ties to even.
+__device__ __forceinline__ uint32_t e4m3x2(float lo, float hi) {
+  uint16_t d;
+  asm("cvt.rn.satfinite.e4m3x2.f32 %0, %1, %2;" : "=h"(d) : "f"(hi), "f"(lo));
+  return d;
+}
+
+__device__ __forceinline__ uint2 row_codes(const uint4& x, float inv) {
+  const auto two = [&](uint32_t p) {
+    return e4m3x2(__uint_as_float(p << 16) * inv, __uint_as_float(p & 0xffff0000u) * inv);
+  };
+  return make_uint2(two(x.x) | two(x.y) << 16, two(x.z) | two(x.w) << 16);
+}
+
+// Two e4m3 codes times f, as e4m3 codes again.
+__device__ __forceinline__ uint32_t scaled_codes(uint32_t two, float f) {
+  uint32_t h;
+  asm("cvt.rn.f16x2.e4m3x2 %0, %1;" : "=r"(h) : "h"(static_cast<uint16_t>(two)));
+  float lo, hi;
+  asm("{\n .reg .b16 a, b;\n mov.b32 {a, b}, %2;\n cvt.f32.f16 %0, a;\n cvt.f32.f16 %1, b;\n}"
+      : "=f"(lo), "=f"(hi)
+      : "r"(h));
+  return e4m3x2(lo * f, hi * f);
+}
+
+// Waits for the other groups of this thread's team (teams of one warp or less are together).
+template <int kPage>
+__device__ __forceinline__ void team_sync() {
+  constexpr int kTeam = kPage;   // threads of a team: P / 16 groups of 16
+  if constexpr (kTeam > 32)
+    named_bar_sync(1 + threadIdx.x / kTeam, kTeam);
+  else
+    __syncwarp(kTeam == 32 ? 0xffffffffu : (threadIdx.x & 16 ? 0xffff0000u : 0x0000ffffu));
+}
+
+// Writes rows [off, off + n) of a page (codes and scale of one head); x[i] holds this lane's 8
+// elements of page row 16 g + i, zero outside the run. Every thread of the team comes here.
+template <int kPage>
+__device__ __forceinline__ void write_run(const uint4 (&x)[kGroupRows], int off, int n, uint8_t* codes, float* scale,
+                                          uint32_t* team_max) {
+  constexpr int kGroups = kPage / kGroupRows;
+  const int lane = threadIdx.x & 15, g = (threadIdx.x / 16) % kGroups;
+  const uint32_t lanes = threadIdx.x & 16 ? 0xffff0000u : 0x0000ffffu;
+  uint32_t m = 0;
+#pragma unroll
+  for (int i = 0; i < kGroupRows; ++i)
+    m = max_u16x2(max_u16x2(max_u16x2(m, x[i].x & 0x7fff7fffu), max_u16x2(x[i].y & 0x7fff7fffu, x[i].z & 0x7fff7fffu)),
+                  x[i].w & 0x7fff7fffu);
+  if ((m & 0xffffu) >= 0x7f80u || m >= 0x7f800000u) {
+    // an infinity or a NaN among them (rare): the finite ones alone
+    m = 0;
+#pragma unroll
+    for (int i = 0; i < kGroupRows; ++i)
+      m = max_finite(max_finite(max_finite(max_finite(m, x[i].x), x[i].y), x[i].z), x[i].w);
+  }
+  m = max(m & 0xffffu, m >> 16);
+#pragma unroll
+  for (int o = 8; o > 0; o >>= 1) m = max(m, __shfl_xor_sync(lanes, m, o));
+  // the page's scale is read before it is written: every group reads, then all meet
+  const float held = off > 0 ? *scale : 0.f;
+  if constexpr (kGroups > 1) {
+    if (lane == 0) team_max[g] = m;
+    team_sync<kPage>();
+#pragma unroll
+    for (int i = 0; i < kGroups; ++i) m = max(m, team_max[i]);
+  } else {
+    __syncwarp(lanes);
+  }
+  const float s = fmaxf(held, __uint_as_float(need_bits(m)));
+  const float inv = __frcp_rn(s);   // exact: a power of two
+  if (s > held && off > 0) {
+    // older rows to the larger scale (their rounding again only where they become subnormal)
+    const float f = held * inv;
+    for (int i = 0; i < kGroupRows; ++i) {
+      const int row = g * kGroupRows + i;
+      if (row >= off) break;
+      uint2* at = reinterpret_cast<uint2*>(codes + row * kHeadDim) + lane;
+      uint2 c = *at;
+      c.x = scaled_codes(c.x & 0xffffu, f) | scaled_codes(c.x >> 16, f) << 16;
+      c.y = scaled_codes(c.y & 0xffffu, f) | scaled_codes(c.y >> 16, f) << 16;
+      *at = c;
+    }
+  }
+#pragma unroll
+  for (int i = 0; i < kGroupRows; ++i) {
+    const int row = g * kGroupRows + i;
+    if (row >= off && row < off + n) reinterpret_cast<uint2*>(codes + row * kHeadDim)[lane] = row_codes(x[i], inv);
+  }
+  if (g == 0 && lane == 0) *scale = s;
+}
+
+// Step 4 into the cache. A team takes page j of a unit, keys or values (the two alternate).
+template <int kPage>
+__global__ void __launch_bounds__(kRowThreads) cache_gather_kernel(const __grid_constant__ CacheGatherParams P) {
+  wait_previous_kernel();   // the indices come from the selection launched before
+  constexpr int kGroups = kPage / kGroupRows, kTeams = kRowThreads / kPage;
+  __shared__ uint32_t team_max[kTeams][kGroups];
+  const int team = threadIdx.x / kPage, lane = threadIdx.x & 15, g = (threadIdx.x / 16) % kGroups;
+  const int64_t item = static_cast<int64_t>(blockIdx.x) * kTeams + team;
+  const int64_t pages = item >> 1;
+  const int64_t unit = pages / P.unit_pages;
+  if (unit >= P.g.g.n_units) return;   // the whole team
+  const bool values = item & 1;
+  const int j = static_cast<int>(pages - unit * P.unit_pages);
+  const UnitInfo u = unit_info(P.g.g, unit);
+  const int W = P.g.g.window, Lc = u.L - W;
+  const int m = min(P.g.layer_budget[u.layer], Lc);
+  const int n = min(m + W - j * kPage, kPage);
+  if (n <= 0) return;
+  const int64_t seq = static_cast<int64_t>(u.layer) * P.c.max_seqs + P.first_seq + u.r;
+  const int page = __ldg(P.table + seq * P.c.max_pages + j);
+  // the positions of this group's rows: lane i looks row i's up
+  const int row = j * kPage + g * kGroupRows + lane;
+  int src = -1;
+  if (row < m) {
+    src = __ldg(P.g.indices + unit * P.g.budget + row);
+    if (src >= Lc) src = -1;   // never read outside the unit
+  } else if (row < m + W) {
+    src = Lc + (row - m);
+  }
+  if (page < 0 || page >= P.c.num_pages) {
+    if (g == 0 && lane == 0) atomicOr(P.err, kErrCheck);
+    return;
+  }
+  const uint16_t* from = values ? P.g.v + u.v_off : P.g.k + u.k_off;
+  const int64_t st = values ? P.g.g.v_st : P.g.g.k_st;
+  const uint32_t lanes = threadIdx.x & 16 ? 0xffff0000u : 0x0000ffffu;
+  uint4 x[kGroupRows];
+#pragma unroll
+  for (int i = 0; i < kGroupRows; ++i) {
+    const int s = __shfl_sync(lanes, src, i, 16);
+    x[i] = make_uint4(0, 0, 0, 0);
+    if (s >= 0) x[i] = __ldcs(reinterpret_cast<const uint4*>(from + s * st) + lane);
+  }
+  const int64_t block = static_cast<int64_t>(page) * P.c.heads + u.h;
+  write_run<kPage>(x, 0, n, (values ? P.c.v : P.c.k) + block * (kPage * kHeadDim),
+                   (values ? P.c.v_scale : P.c.k_scale) + block, team_max[team]);
+}
+
+// New tokens by slot. A team takes `block` consecutive tokens of one head, keys or values, and writes
+// the runs that start among them one after the other: 1 where the calls of a decode step have a token a
+// sequence, P where whole prompts have a run every P tokens.
+template <int kPage>
+__global__ void __launch_bounds__(kRowThreads) cache_store_kernel(const __grid_constant__ CacheStoreParams P) {
+  wait_previous_kernel();
+  constexpr int kGroups = kPage / kGroupRows, kTeams = kRowThreads / kPage;
+  __shared__ uint32_t team_max[kTeams][kGroups];
+  const int team = threadIdx.x / kPage, lane = threadIdx.x & 15, g = (threadIdx.x / 16) % kGroups;
+  const int64_t item = static_cast<int64_t>(blockIdx.x) * kTeams + team;
+  const int H = P.c.heads;
+  const int64_t first = item / (2 * H) * P.block;
+  if (first >= P.n_tokens) return;   // the whole team
+  const int hv = static_cast<int>(item % (2 * H)), h = hv >> 1;
+  const bool values = hv & 1;
+  const uint16_t* from = (values ? P.v + h * P.v_sh : P.k + h * P.k_sh);
+  const int64_t st = values ? P.v_st : P.k_st;
+  const uint32_t lanes = threadIdx.x & 16 ? 0xffff0000u : 0x0000ffffu;
+  const int64_t limit = static_cast<int64_t>(P.c.num_pages) * kPage;
+  const int64_t last = min(first + P.block, P.n_tokens);
+  int prev = first > 0 ? __ldg(P.slots + first - 1) : -1;
+  for (int64_t t = first; t < last;) {
+    const int slot = __ldg(P.slots + t);
+    const bool starts = slot >= 0 && (prev < 0 || slot != prev + 1 || slot % kPage == 0);
+    prev = slot;
+    if (!starts) {
+      ++t;
+      continue;
+    }
+    if (slot >= limit) {
+      if (g == 0 && lane == 0) atomicOr(P.err, kErrCheck);
+      ++t;
+      continue;
+    }
+    // the run's length: the first token that is not the next slot of this page
+    const int page = slot / kPage, off = slot % kPage;
+    int n = kPage - off;
+#pragma unroll
+    for (int c = 0; c < kGroups; ++c) {
+      const int i = c * 16 + lane;
+      const bool breaks = i < n && (t + i >= P.n_tokens || __ldg(P.slots + t + i) != slot + i);
+      const uint32_t who = (__ballot_sync(lanes, breaks) >> (threadIdx.x & 16)) & 0xffffu;
+      if (who) n = min(n, c * 16 + __ffs(who) - 1);
+    }
+    uint4 x[kGroupRows];
+#pragma unroll
+    for (int i = 0; i < kGroupRows; ++i) {
+      const int row = g * kGroupRows + i - off;
+      x[i] = make_uint4(0, 0, 0, 0);
+      if (row >= 0 && row < n) x[i] = __ldcs(reinterpret_cast<const uint4*>(from + (t + row) * st) + lane);
+    }
+    const int64_t block = static_cast<int64_t>(page) * H + h;
+    write_run<kPage>(x, off, n, (values ? P.c.v : P.c.k) + block * (kPage * kHeadDim),
+                     (values ? P.c.v_scale : P.c.k_scale) + block, team_max[team]);
+    if constexpr (kGroups > 1) team_sync<kPage>();   // team_max and the scale before the next run
+    t += n;
+    prev = slot + n - 1;
+  }
+}
+
+// Slots and table entries that one warp of kv_evict_cache_pages goes through before a sequence is
+// dealt to more warps.
+constexpr int64_t kPagesPerWarp = 512;
+// Tokens of a call from which a team takes P tokens instead of one (measured at the kernel's launcher).
+constexpr int64_t kStoreBlockTokens = 4096;
+
+template <int kPage>
+cudaError_t store_paged(const CacheStoreParams& p, cudaStream_t stream) {
+  constexpr int kTeams = kRowThreads / kPage;
+  const int64_t items = (p.n_tokens + p.block - 1) / p.block * 2 * p.c.heads;
+  return launch_after_previous(cache_store_kernel<kPage>, dim3(static_cast<unsigned>((items + kTeams - 1) / kTeams)),
+                               dim3(kRowThreads), 0, stream, p);
+}
+
+template <int kPage>
+cudaError_t gather_paged(const CacheGatherParams& p, cudaStream_t stream) {
+  constexpr int kTeams = kRowThreads / kPage;
+  const int64_t items = p.g.g.n_units * p.unit_pages * 2;
+  return launch_after_previous(cache_gather_kernel<kPage>, dim3(static_cast<unsigned>((items + kTeams - 1) / kTeams)),
+                               dim3(kRowThreads), 0, stream, p);
+}
+
+}  // namespace
+
+cudaError_t launch_cache_pages(const PagesParams& p, cudaStream_t stream) {
+  const int n = p.c.num_layers * p.c.max_seqs;
+  const int64_t x = (n + kPagesWarps - 1) / kPagesWarps;
+  // warps a sequence: what its slots ask for on average, within a few waves of CTAs
+  const int64_t per_seq = p.slots ? (p.slot_stride + p.c.max_seqs - 1) / p.c.max_seqs : p.c.max_pages / 8;
+  int64_t y = (per_seq + kPagesPerWarp - 1) / kPagesPerWarp;
+  const int64_t most = x < 2048 ? 2048 / x : 1;
+  y = y > most ? most : y;
+  return launch_after_previous(cache_pages_kernel, dim3(static_cast<unsigned>(x), static_cast<unsigned>(y < 1 ? 1 : y)),
+                               dim3(kPagesThreads), 0, stream, p);
+}
+
+cudaError_t launch_cache_reset(const kve_cache& c, int32_t* free_pages, int32_t* ring, cudaStream_t stream) {
+  const int blocks = (c.geo.num_pages + 255) / 256;
+  return launch_after_previous(cache_reset_kernel, dim3(blocks < 304 ? blocks : 304), dim3(256), 0, stream,
+                               free_pages, ring, c.geo.num_pages);
+}
+
+cudaError_t launch_cache_gather(const CacheGatherParams& p, cudaStream_t stream) {
+  switch (p.c.page) {
+    case 16: return gather_paged<16>(p, stream);
+    case 32: return gather_paged<32>(p, stream);
+    case 64: return gather_paged<64>(p, stream);
+    default: return gather_paged<128>(p, stream);
+  }
+}
+
+cudaError_t launch_cache_store(const CacheStoreParams& params, cudaStream_t stream) {
+  CacheStoreParams p = params;
+  p.block = p.n_tokens > kStoreBlockTokens ? p.c.page : 1;
+  switch (p.c.page) {
+    case 16: return store_paged<16>(p, stream);
+    case 32: return store_paged<32>(p, stream);
+    case 64: return store_paged<64>(p, stream);
+    default: return store_paged<128>(p, stream);
+  }
+}
+
+}  // namespace kve
+
+namespace {
+
+using kve::kHeadDim;
+
+size_t align_up(size_t x, size_t a) { return (x + a - 1) / a * a; }
+
+bool aligned(const void* p, uintptr_t a) { return (reinterpret_cast<uintptr_t>(p) % a) == 0; }
+
+// {token, head} strides of a [tokens][heads][d] operand: the given ones, or dense. False if they
+// cannot be used (16-byte accesses; below 2^37 elements).
+bool row_strides(const int64_t* given, int64_t heads, int64_t* token, int64_t* head) {
+  *token = given ? given[0] : heads * kHeadDim;
+  *head = given ? given[1] : kHeadDim;
+  for (const int64_t s : {*token, *head})
+    if (s < 0 || s % 8 != 0 || s >= (int64_t(1) << 37)) return false;
+  return true;
+}
+
+// The call's device is the buffers' device.
+bool on_device(const kve_cache* c) {
+  if (c->device < 0) return true;
+  int dev = -1;
+  return cudaGetDevice(&dev) == cudaSuccess && dev == c->device;
+}
+
+uint32_t* word(void* ws, size_t at) { return reinterpret_cast<uint32_t*>(static_cast<uint8_t*>(ws) + at); }
+
+}  // namespace
+
+extern "C" {
+
+kve_status kv_evict_cache_create(const kve_cache_config* cfg, uint8_t* k, uint8_t* v, float* k_scale,
+                                 float* v_scale, kve_cache** cache_out, size_t* workspace_bytes) {
+  if (!cfg || !k || !v || !k_scale || !v_scale || !cache_out) return KVE_EINVAL;
+  *cache_out = nullptr;
+  const kve_cache_config& c = *cfg;
+  if (c.num_layers < 1 || c.num_layers > kve::kMaxLayers || c.head_dim != kHeadDim) return KVE_EINVAL;
+  if (c.num_kv_heads < 1 || c.num_kv_heads > kve::kMaxCacheHeads || c.num_q_heads < c.num_kv_heads ||
+      c.num_q_heads % c.num_kv_heads || c.num_q_heads / c.num_kv_heads > kve::kMaxRows)
+    return KVE_EINVAL;
+  if (c.page_tokens != 16 && c.page_tokens != 32 && c.page_tokens != 64 && c.page_tokens != 128) return KVE_EINVAL;
+  if (c.num_pages < 1 || c.max_pages < 1 || c.max_pages > c.num_pages || c.max_seqs < 1 ||
+      c.max_seqs > kve::kMaxCacheSeqs)
+    return KVE_EINVAL;
+  // rows of the pool are 32-bit TMA coordinates
+  if (static_cast<int64_t>(c.num_pages) * c.page_tokens >= (int64_t(1) << 31) / c.num_kv_heads) return KVE_EINVAL;
+  if (!aligned(k, 128) || !aligned(v, 128) || !aligned(k_scale, 16) || !aligned(v_scale, 16)) return KVE_EINVAL;
+  kve_cache* h = new (std::nothrow) kve_cache;
+  if (!h) return KVE_ENOMEM;
+  std::memset(h, 0, sizeof(*h));
+  kve::CacheGeometry& g = h->geo;
+  g.num_layers = c.num_layers;
+  g.hq = c.num_q_heads;
+  g.heads = c.num_kv_heads;
+  g.group = c.num_q_heads / c.num_kv_heads;
+  g.page = c.page_tokens;
+  for (g.page_shift = 0; (1 << g.page_shift) < g.page;) ++g.page_shift;
+  g.num_pages = c.num_pages;
+  g.max_pages = c.max_pages;
+  g.max_seqs = c.max_seqs;
+  g.k = k;
+  g.v = v;
+  g.k_scale = k_scale;
+  g.v_scale = v_scale;
+  cudaPointerAttributes at;
+  h->device = -1;
+  if (cudaPointerGetAttributes(&at, k) == cudaSuccess && at.type == cudaMemoryTypeDevice) h->device = at.device;
+  cudaGetLastError();
+  int dev = h->device, sms = 0;
+  if ((dev < 0 && cudaGetDevice(&dev) != cudaSuccess) ||
+      cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, dev) != cudaSuccess) {
+    cudaGetLastError();
+    sms = 152;   // no device visible: size for a full GB300
+  }
+  h->sms = sms;
+  kve::CacheWsLayout& w = h->ws;
+  w.err = 0;
+  w.pages_done = 64;
+  w.arrive = 256;
+  w.clear_end = align_up(w.arrive + sizeof(uint32_t), 256);
+  w.partial = w.clear_end;
+  w.total = w.partial;
+  if (workspace_bytes) *workspace_bytes = w.total;
+  *cache_out = h;
+  return KVE_OK;
+}
+
+void kv_evict_cache_destroy(kve_cache* cache) { delete cache; }
+
+kve_status kv_evict_cache_reset(const kve_cache* cache, int32_t* free_pages, int32_t* ring, void* ws, void* stream) {
+  if (!cache || !ws || !aligned(ws, 256) || !free_pages != !ring) return KVE_EINVAL;
+  if (free_pages && (!aligned(free_pages, 4) || !aligned(ring, 4))) return KVE_EINVAL;
+  if (!on_device(cache)) return KVE_EINVAL;
+  cudaStream_t st = static_cast<cudaStream_t>(stream);
+  if (cudaMemsetAsync(ws, 0, cache->ws.clear_end, st) != cudaSuccess) return KVE_ECUDA;
+  if (free_pages && kve::launch_cache_reset(*cache, free_pages, ring, st) != cudaSuccess) return KVE_ECUDA;
+  return KVE_OK;
+}
+
+kve_status kv_evict_cache_pages(const kve_cache* cache, const int32_t* lens_from, const int32_t* lens_to,
+                                int32_t* table, int32_t* free_pages, const int32_t* ring_in, int32_t* ring_out,
+                                int32_t* lens_out, int32_t* slots, int64_t slot_stride, void* ws, void* stream) {
+  if (!cache || !lens_from || !lens_to || !table || !free_pages || !ring_in || !ring_out || !lens_out || !ws)
+    return KVE_EINVAL;
+  for (const void* p : {static_cast<const void*>(lens_from), static_cast<const void*>(lens_to),
+                        static_cast<const void*>(table), static_cast<const void*>(free_pages),
+                        static_cast<const void*>(ring_in), static_cast<const void*>(ring_out),
+                        static_cast<const void*>(lens_out), static_cast<const void*>(slots)})
+    if (!aligned(p, 4)) return KVE_EINVAL;
+  if (!aligned(ws, 256) || slot_stride < 0 || (slots && slot_stride > INT32_MAX)) return KVE_EINVAL;
+  if (!on_device(cache)) return KVE_EINVAL;
+  kve::PagesParams p;
+  std::memset(&p, 0, sizeof(p));
+  p.c = cache->geo;
+  p.from = lens_from;
+  p.to = lens_to;
+  p.table = table;
+  p.free_pages = free_pages;
+  p.ring_in = ring_in;
+  p.ring_out = ring_out;
+  p.lens_out = lens_out;
+  p.slots = slots;
+  p.slot_stride = slot_stride;
+  p.err = word(ws, cache->ws.err);
+  p.done = word(ws, cache->ws.pages_done);
+  return kve::launch_cache_pages(p, static_cast<cudaStream_t>(stream)) == cudaSuccess ? KVE_OK : KVE_ECUDA;
+}
+
+kve_status kv_evict_cache_gather(const kve_cache* cache, const kve_plan* plan, const uint16_t* k, const uint16_t* v,
+                                 const int32_t* indices, int32_t first_seq, const int32_t* table, void* ws,
+                                 void* stream) {
+  if (!cache || !plan || !k || !v || !indices || !table || !ws) return KVE_EINVAL;
+  const kve::Geometry& g = plan->geo;
+  const kve::CacheGeometry& c = cache->geo;
+  if (g.num_layers != c.num_layers || g.uheads != c.heads || first_seq < 0 || first_seq > c.max_seqs - g.n_req)
+    return KVE_EINVAL;
+  // the most rows that a unit of this plan keeps
+  int64_t rows = 0;
+  for (int l = 0; l < g.num_layers; ++l)
+    for (int r = 0; r < g.n_req; ++r)
+      rows = std::max<int64_t>(rows, std::min(plan->layer_budget[l], g.req_len[r] - g.window) + g.window);
+  const int64_t pages = (rows + c.page - 1) / c.page;
+  if (pages > c.max_pages) return KVE_EINVAL;
+  if (!aligned(k, 16) || !aligned(v, 16) || !aligned(indices, 4) || !aligned(table, 4) || !aligned(ws, 256))
+    return KVE_EINVAL;
+  // teams of one launch
+  if (g.n_units * pages * 2 >= (int64_t(1) << 31)) return KVE_EINVAL;
+  if (!kve::readable_source(k) || !kve::readable_source(v) || !on_device(cache)) return KVE_EINVAL;
+  kve::CacheGatherParams p;
+  std::memset(&p, 0, sizeof(p));
+  p.g.g = g;
+  p.g.budget = plan->cfg.budget;
+  for (int l = 0; l < g.num_layers; ++l) p.g.layer_budget[l] = plan->layer_budget[l];
+  p.g.k = k;
+  p.g.v = v;
+  p.g.indices = indices;
+  p.c = c;
+  p.table = table;
+  p.first_seq = first_seq;
+  p.unit_pages = static_cast<int32_t>(pages);
+  p.err = word(ws, cache->ws.err);
+  return kve::launch_cache_gather(p, static_cast<cudaStream_t>(stream)) == cudaSuccess ? KVE_OK : KVE_ECUDA;
+}
+
+kve_status kv_evict_cache_store(const kve_cache* cache, const uint16_t* k_new, const uint16_t* v_new,
+                                const int64_t* k_strides, const int64_t* v_strides, const int32_t* slots,
+                                int64_t n_tokens, void* ws, void* stream) {
+  if (!cache || n_tokens < 0 || n_tokens > INT32_MAX / (2 * kve::kMaxCacheHeads) || !ws || !aligned(ws, 256))
+    return KVE_EINVAL;
+  if (!k_new || !v_new || !slots || !aligned(k_new, 16) || !aligned(v_new, 16) || !aligned(slots, 4)) return KVE_EINVAL;
+  kve::CacheStoreParams p;
+  std::memset(&p, 0, sizeof(p));
+  p.c = cache->geo;
+  if (!row_strides(k_strides, p.c.heads, &p.k_st, &p.k_sh) || !row_strides(v_strides, p.c.heads, &p.v_st, &p.v_sh))
+    return KVE_EINVAL;
+  if (!on_device(cache)) return KVE_EINVAL;
+  if (n_tokens == 0) return KVE_OK;
+  p.k = k_new;
+  p.v = v_new;
+  p.slots = slots;
+  p.n_tokens = n_tokens;
+  p.err = word(ws, cache->ws.err);
+  return kve::launch_cache_store(p, static_cast<cudaStream_t>(stream)) == cudaSuccess ? KVE_OK : KVE_ECUDA;
+}
+
+kve_status kv_evict_cache_attend(const kve_cache* cache, int32_t layer, int32_t n_seq, int32_t q_tokens,
+                                 const uint16_t* q, const int64_t* q_strides, const int32_t* table,
+                                 const int32_t* lens, uint16_t* out, const int64_t* out_strides, float* lse,
+                                 void* ws, void* stream) {
+  if (!cache || !q || !table || !lens || !out || !ws || !aligned(ws, 256)) return KVE_EINVAL;
+  const kve::CacheGeometry& c = cache->geo;
+  if (layer < 0 || layer >= c.num_layers || n_seq < 0 || n_seq > c.max_seqs || q_tokens < 1 ||
+      static_cast<int64_t>(q_tokens) * c.group > kve::kMaxRows)
+    return KVE_EINVAL;
+  if (!aligned(q, 16) || !aligned(out, 16) || !aligned(table, 4) || !aligned(lens, 4) || !aligned(lse, 4))
+    return KVE_EINVAL;
+  kve::AttendParams p;
+  std::memset(&p, 0, sizeof(p));
+  if (!row_strides(q_strides, c.hq, &p.q_st, &p.q_sh) || !row_strides(out_strides, c.hq, &p.o_st, &p.o_sh))
+    return KVE_EINVAL;
+  // rows of out lie apart: tokens outside heads, or heads outside tokens
+  const int64_t tokens = static_cast<int64_t>(n_seq) * q_tokens;
+  const auto apart = [](int64_t inner, int64_t count, int64_t outer, int64_t outer_count) {
+    return (count <= 1 || inner >= kHeadDim) &&
+           (outer_count <= 1 || outer >= (count > 0 ? (count - 1) * inner : 0) + kHeadDim);
+  };
+  if (!apart(p.o_sh, c.hq, p.o_st, tokens) && !apart(p.o_st, tokens, p.o_sh, c.hq)) return KVE_EINVAL;
+  if (!on_device(cache)) return KVE_EINVAL;
+  if (n_seq == 0) return KVE_OK;
+  p.c = c;
+  p.n_seq = n_seq;
+  p.q_tokens = q_tokens;
+  p.alpha = static_cast<float>(1.4426950408889634 / std::sqrt(static_cast<double>(kHeadDim)));
+  p.q = q;
+  p.out = out;
+  p.lse = lse;
+  p.table = table + static_cast<int64_t>(layer) * c.max_seqs * c.max_pages;
+  p.lens = lens + static_cast<int64_t>(layer) * c.max_seqs;
+  p.partial = reinterpret_cast<float*>(static_cast<uint8_t*>(ws) + cache->ws.partial);
+  p.arrive = word(ws, cache->ws.arrive);
+  p.err = word(ws, cache->ws.err);
+  return kve::launch_cache_attend(*cache, p, static_cast<cudaStream_t>(stream)) == cudaSuccess ? KVE_OK : KVE_ECUDA;
+}
+
+kve_status kv_evict_cache_status(const kve_cache* cache, void* ws, void* stream) {
+  if (!cache || !ws || !aligned(ws, 256) || !on_device(cache)) return KVE_EINVAL;
+  if (cudaStreamSynchronize(static_cast<cudaStream_t>(stream)) != cudaSuccess) return KVE_ECUDA;
+  uint32_t err = 0;
+  if (cudaMemcpy(&err, word(ws, cache->ws.err), sizeof(err), cudaMemcpyDeviceToHost) != cudaSuccess) return KVE_ECUDA;
+  if (err == 0) return KVE_OK;
+  // the arrival counters too: a call that gave up may not have counted all of its parts
+  if (cudaMemset(ws, 0, cache->ws.clear_end) != cudaSuccess) return KVE_ECUDA;
+  if (err & kve::kErrCheck) return KVE_ECUDA;
+  return err & kve::kErrWait ? KVE_ETIMEOUT : KVE_EPAGES;
+}
+
+}  // extern "C"

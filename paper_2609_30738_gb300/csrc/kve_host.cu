@@ -447,6 +447,17 @@ kve_status kv_evict_score_attn_workspace(const kve_plan* plan, size_t* bytes) {
 
 namespace kve {
 
+// Sources of the compact cache may be pinned host memory (read in place under unified
+// addressing); host memory the CUDA runtime does not know is refused.
+bool readable_source(const void* src) {
+  cudaPointerAttributes at;
+  if (cudaPointerGetAttributes(&at, src) != cudaSuccess) {
+    cudaGetLastError();
+    return false;
+  }
+  return at.type != cudaMemoryTypeUnregistered;
+}
+
 kve_status select_params(const kve_plan* plan, const float* mu, const float* sigma, const uint16_t* k,
                          const float* lambda1, const float* lambda2, int32_t* indices, int32_t* order,
                          float* margins, SelectParams* p) {
@@ -476,6 +487,7 @@ kve_status select_params(const kve_plan* plan, const float* mu, const float* sig
 
 namespace {
 
+using kve::readable_source;
 using kve::select_params;
 
 // Bytes in front of the multi-profile scratch that hold its error word.
@@ -492,17 +504,6 @@ int64_t profile_keys_words(const kve_plan* plan) {
 // Profiles one launch can carry in its parameter table.
 int32_t profiles_per_launch(const kve_plan* plan) {
   return kve::kProfileLambdas / (2 * plan->geo.num_layers);
-}
-
-// Sources of the compact cache may be pinned host memory (read in place under unified
-// addressing); host memory the CUDA runtime does not know is refused.
-bool readable_source(const void* src) {
-  cudaPointerAttributes at;
-  if (cudaPointerGetAttributes(&at, src) != cudaSuccess) {
-    cudaGetLastError();
-    return false;
-  }
-  return at.type != cudaMemoryTypeUnregistered;
 }
 
 }  // namespace
@@ -693,6 +694,7 @@ const char* kv_evict_strerror(kve_status s) {
     case KVE_ECUDA: return "CUDA call failed";
     case KVE_ETIMEOUT: return "device-side wait timed out";
     case KVE_ENOMEM: return "host allocation failed";
+    case KVE_EPAGES: return "too few free pages";
   }
   return "unknown status";
 }

@@ -24,6 +24,10 @@ constexpr int kMaxAllBudget = 1024;// admissions of the every-candidate selector
 // Bits of the workspace error word (kv_evict_status).
 constexpr uint32_t kErrWait = 1u;    // a bounded wait ran out
 constexpr uint32_t kErrCheck = 2u;   // a device-side consistency check failed
+constexpr uint32_t kErrPages = 4u;   // too few free pages for the lengths asked for
+// The paged 8-bit cache
+constexpr int kMaxCacheSeqs = 1024;  // sequences per layer
+constexpr int kMaxCacheHeads = 1024; // cache heads
 
 // Request table and derived counts, identical on host and device.
 struct Geometry {
@@ -223,7 +227,87 @@ struct GatherParams {
   uint16_t* v_out;
 };
 
+// Sizes of a paged 8-bit cache and its buffers, identical on host and device.
+struct CacheGeometry {
+  int32_t num_layers, hq, heads, group;   // heads: those whose rows the cache holds
+  int32_t page, page_shift;               // P = 1 << page_shift
+  int32_t num_pages, max_pages, max_seqs;
+  uint8_t* k;
+  uint8_t* v;
+  float* k_scale;
+  float* v_scale;
+};
+
+// Workspace of a cache (byte offsets): a header that kv_evict_cache_reset clears, then the
+// attention's partial outputs.
+struct CacheWsLayout {
+  size_t err;        // uint32 error word
+  size_t pages_done; // uint32 CTAs of a kv_evict_cache_pages call that have finished reading
+  size_t arrive;     // uint32 [S * H * row blocks] split arrivals of the attention
+  size_t clear_end;  // bytes cleared by kv_evict_cache_reset
+  size_t partial;    // fp32 partial rows of the attention
+  size_t total;
+};
+
+struct PagesParams {
+  CacheGeometry c;
+  const int32_t* from;
+  const int32_t* to;
+  int32_t* table;
+  int32_t* free_pages;
+  const int32_t* ring_in;
+  int32_t* ring_out;
+  int32_t* lens_out;
+  int32_t* slots;        // or null
+  int64_t slot_stride;
+  uint32_t* err;
+  uint32_t* done;
+};
+
+struct CacheGatherParams {
+  GatherParams g;        // k_out and v_out null
+  CacheGeometry c;
+  const int32_t* table;
+  int32_t first_seq;
+  int32_t unit_pages;    // pages of a unit of B + W rows
+  uint32_t* err;
+};
+
+struct CacheStoreParams {
+  CacheGeometry c;
+  const uint16_t* k;
+  const uint16_t* v;
+  int64_t k_st, k_sh, v_st, v_sh;   // element strides of tokens and heads
+  const int32_t* slots;
+  int64_t n_tokens;
+  int32_t block;         // consecutive tokens whose runs one team writes
+  uint32_t* err;
+};
+
+struct AttendParams {
+  CacheGeometry c;
+  int32_t n_seq, q_tokens;
+  float alpha;           // log2(e) / sqrt(d)
+  const uint16_t* q;
+  int64_t q_st, q_sh;    // element strides of tokens and heads
+  uint16_t* out;
+  int64_t o_st, o_sh;
+  float* lse;            // or null
+  const int32_t* table;  // this layer's [S][max_pages]
+  const int32_t* lens;   // this layer's [S]
+  float* partial;
+  uint32_t* arrive;
+  uint32_t* err;
+};
+
 }  // namespace kve
+
+struct kve_cache {
+  kve::CacheGeometry geo;
+  kve::CacheWsLayout ws;
+  int32_t device;        // of k, or -1 where the runtime does not know the pointer
+  int32_t sms;           // SMs the workspace was sized for
+};
 
 struct kve_plan {
   kve_config cfg;
@@ -281,6 +365,13 @@ cudaError_t launch_select_all(const kve_plan& plan, const SelectParams& p, cudaS
 cudaError_t launch_select_profiles(const kve_plan& plan, const SelectParams& p, const ProfileTable& table,
                                    int profiles, cudaStream_t stream);
 cudaError_t launch_gather(const kve_plan& plan, const GatherParams& p, cudaStream_t stream);
+cudaError_t launch_cache_pages(const PagesParams& p, cudaStream_t stream);
+cudaError_t launch_cache_gather(const CacheGatherParams& p, cudaStream_t stream);
+cudaError_t launch_cache_store(const CacheStoreParams& p, cudaStream_t stream);
+cudaError_t launch_cache_reset(const kve_cache& c, int32_t* free_pages, int32_t* ring, cudaStream_t stream);
+cudaError_t launch_cache_attend(const kve_cache& c, const AttendParams& p, cudaStream_t stream);
+// Host memory the CUDA runtime does not know is refused as a row source (kve_host.cu).
+bool readable_source(const void* src);
 
 // The select kernel's parameters common to every selection entry point (host code,
 // kve_host.cu); lambda1 / lambda2 (HOST [N_L]) may be NULL when a profile table

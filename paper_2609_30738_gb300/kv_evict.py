@@ -15,7 +15,7 @@ import numpy as np
 _HERE = os.path.dirname(os.path.abspath(__file__))
 LIB_PATH = os.path.join(_HERE, "libkvevict.so")
 
-KVE_OK, KVE_EINVAL, KVE_ECUDA, KVE_ETIMEOUT, KVE_ENOMEM = range(5)
+KVE_OK, KVE_EINVAL, KVE_ECUDA, KVE_ETIMEOUT, KVE_ENOMEM, KVE_EPAGES = range(6)
 
 # Names declared in include/kv_evict.h.
 EXPORTS = ("kv_evict_plan", "kv_evict_plan_layered", "kv_evict_plan_ex", "kv_evict_plan_destroy",
@@ -23,7 +23,9 @@ EXPORTS = ("kv_evict_plan", "kv_evict_plan_layered", "kv_evict_plan_ex", "kv_evi
            "kv_evict_score", "kv_evict_score_lse", "kv_evict_score_attn", "kv_evict_score_attn_workspace",
            "kv_evict_select", "kv_evict_select_noalloc", "kv_evict_select_profiles",
            "kv_evict_select_profiles_workspace", "kv_evict_gather", "kv_evict_select_gather",
-           "kv_evict_status", "kv_evict_profile", "kv_evict_budget_pyramid", "kv_evict_strerror")
+           "kv_evict_status", "kv_evict_profile", "kv_evict_budget_pyramid", "kv_evict_strerror",
+           "kv_evict_cache_create", "kv_evict_cache_destroy", "kv_evict_cache_reset", "kv_evict_cache_pages",
+           "kv_evict_cache_gather", "kv_evict_cache_store", "kv_evict_cache_attend", "kv_evict_cache_status")
 
 
 class KvEvictError(RuntimeError):
@@ -38,6 +40,13 @@ class Config(ctypes.Structure):
                 ("window", ctypes.c_int32), ("budget", ctypes.c_int32),
                 ("pool_kernel", ctypes.c_int32), ("candidate_factor", ctypes.c_int32),
                 ("norm_eps", ctypes.c_float)]
+
+
+class CacheConfig(ctypes.Structure):
+    _fields_ = [("num_layers", ctypes.c_int32), ("num_q_heads", ctypes.c_int32),
+                ("num_kv_heads", ctypes.c_int32), ("head_dim", ctypes.c_int32),
+                ("page_tokens", ctypes.c_int32), ("num_pages", ctypes.c_int32),
+                ("max_pages", ctypes.c_int32), ("max_seqs", ctypes.c_int32)]
 
 
 _LIB = None
@@ -74,6 +83,15 @@ def _lib():
         lib.kv_evict_select_gather.argtypes = [vp] * 14
         lib.kv_evict_status.argtypes = [vp, vp, vp]
         lib.kv_evict_profile.argtypes = [i32, vp, i32, vp, vp]
+        lib.kv_evict_cache_create.argtypes = [vp] * 7
+        lib.kv_evict_cache_destroy.argtypes = [vp]
+        lib.kv_evict_cache_destroy.restype = None
+        lib.kv_evict_cache_reset.argtypes = [vp] * 5
+        lib.kv_evict_cache_pages.argtypes = [vp] * 9 + [i64, vp, vp]
+        lib.kv_evict_cache_gather.argtypes = [vp] * 5 + [i32, vp, vp, vp]
+        lib.kv_evict_cache_store.argtypes = [vp] * 6 + [i64, vp, vp]
+        lib.kv_evict_cache_attend.argtypes = [vp, i32, i32, i32] + [vp] * 9
+        lib.kv_evict_cache_status.argtypes = [vp, vp, vp]
         lib.kv_evict_strerror.argtypes = [ctypes.c_int]
         lib.kv_evict_strerror.restype = ctypes.c_char_p
         for name in ("kv_evict_plan", "kv_evict_plan_layered", "kv_evict_plan_ex", "kv_evict_plan_set_debug",
@@ -82,7 +100,9 @@ def _lib():
                      "kv_evict_select", "kv_evict_select_noalloc",
                      "kv_evict_select_profiles", "kv_evict_select_profiles_workspace", "kv_evict_gather",
                      "kv_evict_select_gather", "kv_evict_status", "kv_evict_profile",
-                     "kv_evict_budget_pyramid"):
+                     "kv_evict_budget_pyramid", "kv_evict_cache_create", "kv_evict_cache_reset",
+                     "kv_evict_cache_pages", "kv_evict_cache_gather", "kv_evict_cache_store",
+                     "kv_evict_cache_attend", "kv_evict_cache_status"):
             getattr(lib, name).restype = ctypes.c_int
         _LIB = lib
     return _LIB
@@ -180,6 +200,16 @@ class Plan:
     @property
     def score_elems(self) -> int:
         return self.spec["num_layers"] * self.unit_heads * sum(self.seq_lens)
+
+    def kept_lens(self, lens, first_seq: int = 0):
+        """lens (int32 [N_L, max_seqs]) with the sequences first_seq .. of this plan's requests at the rows that
+        the plan keeps, min(B_l, Lc_r) + W."""
+        import torch
+        w = self.spec["window"]
+        kept = [[min(b, n - w) + w for n in self.seq_lens] for b in self.layer_budgets]
+        out = lens.clone()
+        out[:, first_seq:first_seq + len(self.seq_lens)] = torch.tensor(kept, dtype=lens.dtype, device=lens.device)
+        return out
 
     def set_kv_strides(self, k_strides=None, v_strides=None):
         """kv_evict_plan_set_kv_strides: element strides (layer, KV head, token) of k
@@ -346,3 +376,139 @@ def run_step(plan: Plan, bufs: Buffers, q_win, k, v, lambda1, lambda2, stream=No
     plan.select(bufs.mu, bufs.sigma, k, lambda1, lambda2, bufs.indices, bufs.ws, bufs.order,
                 bufs.margins, stream)
     plan.gather(k, v, bufs.indices, bufs.k_out, bufs.v_out, stream)
+
+
+def _row_strides(t, heads: int, name: str):
+    """The {token, head} element strides of a bf16 tensor [..., heads, d] as a host array, or None where it
+    is dense. The dimensions in front of the heads must be one run of tokens."""
+    import torch
+    if t.dtype != torch.bfloat16 or t.shape[-2] != heads or t.stride(-1) != 1:
+        raise ValueError(f"{name}: expected bf16 [..., {heads}, d] with contiguous rows")
+    for i in range(t.dim() - 3):
+        if t.shape[i] > 1 and t.stride(i) != t.stride(i + 1) * t.shape[i + 1]:
+            raise ValueError(f"{name}: its tokens are not one run")
+    if t.is_contiguous():
+        return None
+    return (ctypes.c_int64 * 2)(t.stride(-3), t.stride(-2))
+
+
+class Cache8:
+    """kv_evict_cache_create: the paged 8-bit cache of a configuration (num_layers, num_q_heads,
+    num_kv_heads, head_dim of spec; per_query_head: the query heads are the cache's heads). Its pages
+    k, v [num_pages, H, P, d] uint8 (e4m3 codes) and k_scale, v_scale [num_pages, H] fp32 are the given
+    tensors, or allocated here, with the workspace ws. Tables, lengths, the free ring and slots are the
+    caller's int32 tensors (state() makes them)."""
+
+    def __init__(self, spec: dict, max_seqs: int, num_pages: int, max_pages: int, page_tokens: int = 64,
+                 device="cuda", per_query_head: bool = False, k=None, v=None, k_scale=None, v_scale=None):
+        import torch
+        self.heads = spec["num_q_heads"] if per_query_head else spec["num_kv_heads"]
+        self.num_layers, self.num_q_heads, self.head_dim = spec["num_layers"], spec["num_q_heads"], spec["head_dim"]
+        self.max_seqs, self.num_pages, self.max_pages, self.page_tokens = max_seqs, num_pages, max_pages, page_tokens
+        shape = (num_pages, self.heads, page_tokens, self.head_dim)
+        self.k, self.v = (self._buffer(t, shape, torch.uint8, device) for t in (k, v))
+        self.k_scale, self.v_scale = (self._buffer(t, shape[:2], torch.float32, device) for t in (k_scale, v_scale))
+        self._h = None
+        cfg = CacheConfig(self.num_layers, self.num_q_heads, self.heads, self.head_dim, page_tokens, num_pages,
+                          max_pages, max_seqs)
+        handle, size = ctypes.c_void_p(), ctypes.c_size_t()
+        _check(_lib().kv_evict_cache_create(ctypes.byref(cfg), _ptr(self.k), _ptr(self.v), _ptr(self.k_scale),
+                                            _ptr(self.v_scale), ctypes.byref(handle), ctypes.byref(size)),
+               "kv_evict_cache_create")
+        self._h = handle
+        self.ws = torch.empty(size.value, dtype=torch.uint8, device=self.k.device)
+        self.reset()
+
+    @staticmethod
+    def _buffer(t, shape, dtype, device):
+        import torch
+        if t is None:
+            return torch.empty(shape, dtype=dtype, device=device)
+        if tuple(t.shape) != tuple(shape) or t.dtype != dtype or not t.is_contiguous():
+            raise ValueError(f"expected a contiguous {dtype} tensor of shape {tuple(shape)}")
+        return t
+
+    def __del__(self):
+        h = getattr(self, "_h", None)
+        if h is not None and h.value and _LIB is not None:
+            _LIB.kv_evict_cache_destroy(h)
+            self._h = None
+
+    def state(self):
+        """(table, lens, free_pages, ring) of an empty cache: every page free."""
+        import torch
+        i32 = dict(dtype=torch.int32, device=self.k.device)
+        table = torch.full((self.num_layers, self.max_seqs, self.max_pages), -1, **i32)
+        lens = torch.zeros((self.num_layers, self.max_seqs), **i32)
+        free, ring = torch.empty(self.num_pages, **i32), torch.empty(2, **i32)
+        self.reset(free, ring)
+        return table, lens, free, ring
+
+    def reset(self, free_pages=None, ring=None, stream=None):
+        """kv_evict_cache_reset: clear the workspace, and make every page free where the ring is given."""
+        _check(_lib().kv_evict_cache_reset(self._h, _ptr(free_pages), _ptr(ring), _ptr(self.ws),
+                                           _stream_ptr(stream)), "kv_evict_cache_reset")
+
+    def pages(self, lens_from, lens_to, table, free_pages, ring_in, ring_out, lens_out, slots=None, stream=None):
+        """kv_evict_cache_pages. slots: int32 [N_L, n] or None."""
+        stride = 0
+        if slots is not None:
+            if slots.dim() != 2 or slots.shape[0] != self.num_layers or not slots.is_contiguous():
+                raise ValueError("slots: expected a contiguous [num_layers, n] tensor")
+            stride = slots.shape[1]
+        for name, t, n in (("lens_from", lens_from, self.num_layers * self.max_seqs),
+                           ("lens_to", lens_to, self.num_layers * self.max_seqs),
+                           ("lens_out", lens_out, self.num_layers * self.max_seqs),
+                           ("table", table, self.num_layers * self.max_seqs * self.max_pages),
+                           ("free_pages", free_pages, self.num_pages), ("ring_in", ring_in, 2), ("ring_out", ring_out, 2)):
+            if t.numel() != n or not t.is_contiguous():
+                raise ValueError(f"{name}: expected {n} contiguous values")
+        _check(_lib().kv_evict_cache_pages(self._h, _ptr(lens_from), _ptr(lens_to), _ptr(table), _ptr(free_pages),
+                                           _ptr(ring_in), _ptr(ring_out), _ptr(lens_out), _ptr(slots), stride,
+                                           _ptr(self.ws), _stream_ptr(stream)), "kv_evict_cache_pages")
+
+    def gather(self, plan: Plan, k, v, indices, table, first_seq: int = 0, stream=None):
+        """kv_evict_cache_gather: the kept and the window rows of plan's requests as sequences first_seq ..;
+        k and v as for Plan.gather."""
+        for name, t in (("k", k), ("v", v)):
+            dev = getattr(t, "device", None)
+            if dev is not None and getattr(dev, "type", None) == "cpu" and not t.is_pinned():
+                raise ValueError(f"gather: {name} is a pageable CPU tensor; pin it or move it to the GPU")
+        _check(_lib().kv_evict_cache_gather(self._h, plan._h, _ptr(k), _ptr(v), _ptr(indices), int(first_seq),
+                                            _ptr(table), _ptr(self.ws), _stream_ptr(stream)), "kv_evict_cache_gather")
+
+    def store(self, k_new, v_new, slots, stream=None):
+        """kv_evict_cache_store: k_new, v_new bf16 [tokens, H, d] (slices of a projection's output too), slots
+        int32 [tokens]."""
+        n = slots.numel()
+        if k_new.numel() != n * self.heads * self.head_dim or v_new.numel() != k_new.numel() or not slots.is_contiguous():
+            raise ValueError("store: k_new and v_new hold a row of every head for each slot")
+        _check(_lib().kv_evict_cache_store(self._h, _ptr(k_new), _ptr(v_new), _row_strides(k_new, self.heads, "k_new"),
+                                           _row_strides(v_new, self.heads, "v_new"), _ptr(slots), n, _ptr(self.ws),
+                                           _stream_ptr(stream)), "kv_evict_cache_store")
+
+    def attend(self, q, table, lens, layer: int, out, lse=None, stream=None):
+        """kv_evict_cache_attend: q, out bf16 [n_seq, q_tokens, Hq, d], lse fp32 [n_seq, q_tokens, Hq] or
+        None; table and lens of all layers."""
+        if q.dim() != 4 or out.shape != q.shape or (lse is not None and
+                                                    (lse.shape != q.shape[:3] or not lse.is_contiguous())):
+            raise ValueError("attend: q and out are [n_seq, q_tokens, Hq, d], lse [n_seq, q_tokens, Hq]")
+        _check(_lib().kv_evict_cache_attend(self._h, int(layer), q.shape[0], q.shape[1], _ptr(q),
+                                            _row_strides(q, self.num_q_heads, "q"), _ptr(table), _ptr(lens), _ptr(out),
+                                            _row_strides(out, self.num_q_heads, "out"), _ptr(lse), _ptr(self.ws),
+                                            _stream_ptr(stream)), "kv_evict_cache_attend")
+
+    def status(self, stream=None) -> int:
+        """Synchronise, return the device status of the calls so far and clear it."""
+        return int(_lib().kv_evict_cache_status(self._h, _ptr(self.ws), _stream_ptr(stream)))
+
+
+def run_step_cache8(plan: Plan, bufs: Buffers, cache: Cache8, q_win, k, v, lambda1, lambda2, table, lens, free_pages,
+                    ring, first_seq: int = 0, stream=None):
+    """The eviction step whose compact cache is the paged 8-bit one: score, select, pages for the plan's
+    requests (their sequences first_seq .. must be empty), and the kept and window rows written into them.
+    lens and ring are advanced in place."""
+    plan.score(q_win, k, bufs.mu, bufs.sigma, bufs.ws, stream)
+    plan.select(bufs.mu, bufs.sigma, k, lambda1, lambda2, bufs.indices, bufs.ws, bufs.order, bufs.margins, stream)
+    cache.pages(lens, plan.kept_lens(lens, first_seq), table, free_pages, ring, ring, lens, None, stream)
+    cache.gather(plan, k, v, bufs.indices, table, first_seq, stream)
