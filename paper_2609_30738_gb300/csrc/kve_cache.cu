@@ -475,6 +475,8 @@ namespace {
 
 using kve::kHeadDim;
 
+constexpr uint64_t kWaitNs = 2000000000ull;   // every device-side wait, 2 s
+
 size_t align_up(size_t x, size_t a) { return (x + a - 1) / a * a; }
 
 bool aligned(const void* p, uintptr_t a) { return (reinterpret_cast<uintptr_t>(p) % a) == 0; }
@@ -550,9 +552,11 @@ kve_status kv_evict_cache_create(const kve_cache_config* cfg, uint8_t* k, uint8_
   w.err = 0;
   w.pages_done = 64;
   w.arrive = 256;
-  w.clear_end = align_up(w.arrive + sizeof(uint32_t), 256);
+  const size_t workers = static_cast<size_t>(kve::kAttendCtas) * sms;
+  w.clear_end = align_up(w.arrive + sizeof(uint32_t) * workers, 256);
   w.partial = w.clear_end;
-  w.total = w.partial;
+  w.total = align_up(w.partial + workers * 2 * kve::kAttendPartWords * sizeof(float), 256);
+  h->maps = kve::encode_pages(&h->tm_k, k, g) && kve::encode_pages(&h->tm_v, v, g);
   if (workspace_bytes) *workspace_bytes = w.total;
   *cache_out = h;
   return KVE_OK;
@@ -680,7 +684,9 @@ kve_status kv_evict_cache_attend(const kve_cache* cache, int32_t layer, int32_t 
   if (!apart(p.o_sh, c.hq, p.o_st, tokens) && !apart(p.o_st, tokens, p.o_sh, c.hq)) return KVE_EINVAL;
   if (!on_device(cache)) return KVE_EINVAL;
   if (n_seq == 0) return KVE_OK;
+  if (!cache->maps) return KVE_ECUDA;
   p.c = c;
+  p.wait_limit_ns = kWaitNs;
   p.n_seq = n_seq;
   p.q_tokens = q_tokens;
   p.alpha = static_cast<float>(1.4426950408889634 / std::sqrt(static_cast<double>(kHeadDim)));

@@ -447,6 +447,19 @@ kve_status kv_evict_score_attn_workspace(const kve_plan* plan, size_t* bytes) {
 
 namespace kve {
 
+bool encode_pages(CUtensorMap* map, const void* base, const CacheGeometry& c) {
+  auto fn = encode_fn();
+  if (!fn) return false;
+  cuuint64_t dims[2] = {static_cast<cuuint64_t>(kHeadDim),
+                        static_cast<cuuint64_t>(c.num_pages) * c.heads * c.page};
+  cuuint64_t strides[1] = {static_cast<cuuint64_t>(kHeadDim)};
+  cuuint32_t box[2] = {kHeadDim, static_cast<cuuint32_t>(c.page)};
+  cuuint32_t estr[2] = {1, 1};
+  return fn(map, CU_TENSOR_MAP_DATA_TYPE_UINT8, 2, const_cast<void*>(base), dims, strides, box, estr,
+            CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B,
+            CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+
 // Sources of the compact cache may be pinned host memory (read in place under unified
 // addressing); host memory the CUDA runtime does not know is refused.
 bool readable_source(const void* src) {

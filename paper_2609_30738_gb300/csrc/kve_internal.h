@@ -28,6 +28,9 @@ constexpr uint32_t kErrPages = 4u;   // too few free pages for the lengths asked
 // The paged 8-bit cache
 constexpr int kMaxCacheSeqs = 1024;  // sequences per layer
 constexpr int kMaxCacheHeads = 1024; // cache heads
+constexpr int kAttendCtas = 2;       // attention CTAs an SM
+constexpr int kAttendRows = 16;      // most query rows of one attention row block
+constexpr int kAttendPartWords = kAttendRows * (kHeadDim + 2);   // a part: rows, their maxima and sums
 
 // Request table and derived counts, identical on host and device.
 struct Geometry {
@@ -243,9 +246,9 @@ struct CacheGeometry {
 struct CacheWsLayout {
   size_t err;        // uint32 error word
   size_t pages_done; // uint32 CTAs of a kv_evict_cache_pages call that have finished reading
-  size_t arrive;     // uint32 [S * H * row blocks] split arrivals of the attention
+  size_t arrive;     // uint32 [kAttendCtas * SMs] arrivals of the parts of a split row block
   size_t clear_end;  // bytes cleared by kv_evict_cache_reset
-  size_t partial;    // fp32 partial rows of the attention
+  size_t partial;    // fp32 [kAttendCtas * SMs][2][kAttendPartWords] partial rows of the attention
   size_t total;
 };
 
@@ -295,6 +298,7 @@ struct AttendParams {
   float* lse;            // or null
   const int32_t* table;  // this layer's [S][max_pages]
   const int32_t* lens;   // this layer's [S]
+  uint64_t wait_limit_ns;
   float* partial;
   uint32_t* arrive;
   uint32_t* err;
@@ -307,6 +311,8 @@ struct kve_cache {
   kve::CacheWsLayout ws;
   int32_t device;        // of k, or -1 where the runtime does not know the pointer
   int32_t sms;           // SMs the workspace was sized for
+  bool maps;             // the TMA maps are encoded (no driver, none)
+  CUtensorMap tm_k, tm_v;
 };
 
 struct kve_plan {
@@ -370,6 +376,9 @@ cudaError_t launch_cache_gather(const CacheGatherParams& p, cudaStream_t stream)
 cudaError_t launch_cache_store(const CacheStoreParams& p, cudaStream_t stream);
 cudaError_t launch_cache_reset(const kve_cache& c, int32_t* free_pages, int32_t* ring, cudaStream_t stream);
 cudaError_t launch_cache_attend(const kve_cache& c, const AttendParams& p, cudaStream_t stream);
+// The TMA map of a cache's codes, [pages * H * P][d] bytes in boxes of a page's rows with the 128-byte
+// swizzle; false without a driver (kve_host.cu).
+bool encode_pages(CUtensorMap* map, const void* base, const CacheGeometry& c);
 // Host memory the CUDA runtime does not know is refused as a row source (kve_host.cu).
 bool readable_source(const void* src);
 
