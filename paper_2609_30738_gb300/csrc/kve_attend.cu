@@ -27,78 +27,84 @@
 namespace kve {
 namespace {
 
-constexpr int kAttendThreads = 192;   // 4 softmax warps, TMA producer, MMA issuer
-constexpr int kStages = 3;            // K and V tiles in flight: 96 KB a CTA, 192 KB an SM
+constexpr int kKStages = 2, kVStages = 4;   // 96 KB of tiles a CTA; a K tile is done with two tiles before its V
 constexpr int kTileBytes = kTileKeys * kHeadDim;
 constexpr int kMostTilePages = kTileKeys / 16;
 
+constexpr int kNoNan = 255;   // of positions 0 .. 126
+
 constexpr int up16(int x) { return (x + 15) / 16 * 16; }
 
-template <int R>
+// R rows of a block; each of H groups of four softmax warps has R / H of them.
+template <int R, int H>
 struct ACfg {
+  static constexpr int kRows = R / H;
+  static constexpr int kThreads = 128 * (1 + H);    // producer, MMA issuer, query loader and one more; softmax
   static constexpr int kNs = up16(2 * R);           // columns of S^T: q's hi rows, then its lo rows
   static constexpr int kNp = up16(3 * R);           // columns of O^T: p's hi, mid and lo rows
-  static constexpr int kOCol = kNs;
-  static constexpr int kTmemCols = kNs + kNp <= 32 ? 32 : kNs + kNp <= 64 ? 64 : 128;
+  static constexpr int kOCol = 2 * kNs;             // two S^T, one O^T
+  static constexpr int kTmemCols = 2 * kNs + kNp <= 64 ? 64 : 128;
   static constexpr uint32_t kIdescS = idesc_e4m3_f32(128, kNs, false);
   static constexpr uint32_t kIdescO = idesc_e4m3_f32(128, kNp, true);
-  static constexpr size_t kQ = size_t(kStages) * 2 * kTileBytes;
-  static constexpr size_t kP = kQ + kNs * kHeadDim;
+  static constexpr size_t kV = size_t(kKStages) * kTileBytes;
+  static constexpr size_t kQ = kV + size_t(kVStages) * kTileBytes;
+  static constexpr size_t kQBytes = kNs * kHeadDim;  // by part parity
+  static constexpr size_t kP = kQ + 2 * kQBytes;
   static constexpr size_t kCtl = kP + kNp * kTileKeys;
 };
 
-template <int R>
-struct ACtl {
-  uint64_t full[kStages], empty[kStages];
-  uint64_t s_full, p_full, o_full, q_full, meet, drain;
-  float ks[kStages][kMostTilePages], vs[kStages][kMostTilePages];
-  uint32_t pages[kStages];          // bit j: page j of the tile holds tokens
-  float red[2][4][R];               // row maxima of the warps, by tile parity (and row sums of a part)
-  float qs[2][R];                   // log2(e) / sqrt(d) / the power of two in the q pieces, by part parity
-  unsigned long long sums[kAttendThreads / 32];
-  long long base;                   // tiles in front of the first part's sequence
-  int first_r, last;
-  uint32_t tmem_base;
-  int abort, never;   // never: stays 0 (waits that a given-up call still has to make)
+// A (sequence, head, row block): the rows of one row block over one sequence's tiles, `first` their first in
+// the line of all tiles.
+struct Block {
+  int r, h, rb, len, tiles, first;
 };
 
-template <int R>
+template <int R, int H>
+struct ACtl {
+  uint64_t k_full[kKStages], k_empty[kKStages], v_full[kVStages], v_empty[kVStages];
+  uint64_t m_full[kVStages];                   // the scales beside a V stage
+  uint64_t s_full[2], q_full[2], q_empty[2];   // by tile parity, by part parity
+  uint64_t p_full, o_full, meet[H], drain;
+  float ks[kVStages][kMostTilePages], vs[kVStages][kMostTilePages];
+  uint32_t pages[kVStages];                    // bit j: page j of the tile holds tokens
+  float red[2][4][R];                          // row maxima of the warps, by tile parity
+  float sum[4][R];                             // row sums of the warps, at the end of a part
+  // of a part's rows, by part parity: log2(e) / sqrt(d) / the power of two in the q pieces; tokens that the
+  // row sees; where its output goes (elements of out, of lse), -1 for no row
+  float qs[2][R];
+  int seen[2][R];
+  long long out_at[2][R];
+  int lse_at[2][R];
+  uint8_t nan_from[2][kHeadDim];               // by part parity: see there
+  Block split[2 * H];                          // parts left for the join, by half
+  int last[2 * H];
+  Block first;                                 // the first part's block
+  unsigned long long sums[ACfg<R, H>::kThreads / 32];
+  uint32_t tmem_base;
+  int abort, never;                            // never: stays 0 (waits that a given-up call still has to make)
+};
+
+template <int R, int H>
 constexpr size_t attend_smem() {
-  return ACfg<R>::kCtl + sizeof(ACtl<R>) + 1024;   // the tiles start on 1024 bytes
+  return ACfg<R, H>::kCtl + sizeof(ACtl<R, H>);
 }
 
-// Walks a CTA's share of the line of tiles, part by part: (sequence, head, row block)s in this order.
-struct Walk {
-  int r, h, rb, tiles, len;
-  long long first;   // the block's first tile in the line
+__device__ __forceinline__ int seq_len(const AttendParams& P, int r) {
+  return min(max(__ldg(P.lens + r), 0), P.c.max_pages << P.c.page_shift);
+}
 
-  __device__ __forceinline__ static int length(const AttendParams& P, int r) {
-    const int len = __ldg(P.lens + r);
-    return min(max(len, 0), P.c.max_pages << P.c.page_shift);
-  }
-  __device__ __forceinline__ void enter(const AttendParams& P, int seq) {
-    r = seq;
-    len = length(P, r);
-    tiles = (len + kTileKeys - 1) / kTileKeys;
-  }
-  // The block that holds tile x, for x at or behind the first tile of sequence seq (base).
-  __device__ __forceinline__ void seek(const AttendParams& P, int blocks, int seq, long long base, long long x) {
-    enter(P, seq);
-    const long long at = (x - base) / tiles;
-    h = static_cast<int>(at / blocks);
-    rb = static_cast<int>(at - static_cast<long long>(h) * blocks);
-    first = base + at * tiles;
-  }
-  __device__ __forceinline__ void next(const AttendParams& P, int blocks) {
-    first += tiles;
-    if (++rb < blocks) return;
-    rb = 0;
-    if (++h < P.c.heads) return;
-    h = 0;
-    do enter(P, r + 1);
-    while (tiles == 0);   // a tile follows, so a sequence that is not empty does
-  }
-};
+// The block behind b in the line; a tile follows, so a sequence that is not empty does.
+__device__ __forceinline__ void next_block(const AttendParams& P, int blocks, Block& b) {
+  b.first += b.tiles;
+  if (++b.rb < blocks) return;
+  b.rb = 0;
+  if (++b.h < P.c.heads) return;
+  b.h = 0;
+  do {
+    b.len = seq_len(P, ++b.r);
+    b.tiles = (b.len + kTileKeys - 1) / kTileKeys;
+  } while (b.tiles == 0);
+}
 
 // The power of two that brings the largest magnitude (bf16 bits a, finite) into [128, 256), as fp32 bits.
 __device__ __forceinline__ uint32_t piece_scale(uint32_t a) {
@@ -128,27 +134,40 @@ __device__ __forceinline__ uint16_t to_bf16(float x) {
   return d;
 }
 
-template <int R>
-__global__ void __launch_bounds__(kAttendThreads, kAttendCtas)
+// ln of a row's sum given its maximum in log2 units (no token seen: -inf; a NaN sum is not 0, its row is NaN).
+__device__ __forceinline__ float log_sum(float top, float sum) {
+  return sum == 0.f ? -INFINITY : ((top == -INFINITY ? 0.f : top) + lg2(sum)) * 0.69314718056f;
+}
+
+template <int R, int H>
+__global__ void __launch_bounds__(ACfg<R, H>::kThreads, kAttendCtas)
 cache_attend_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constant__ CUtensorMap tm_v,
                     const __grid_constant__ AttendParams P) {
-  using C = ACfg<R>;
-  extern __shared__ uint8_t smem_raw[];
-  uint8_t* smem = smem_raw + ((1024u - (smem_u32(smem_raw) & 1023u)) & 1023u);
-  ACtl<R>& ctl = *reinterpret_cast<ACtl<R>*>(smem + C::kCtl);
-  const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+  using C = ACfg<R, H>;
+  constexpr int N = C::kRows, kThreads = C::kThreads;
+  extern __shared__ __align__(1024) uint8_t smem[];   // the tiles' swizzle counts from 1024 bytes
+  ACtl<R, H>& ctl = *reinterpret_cast<ACtl<R, H>*>(smem + C::kCtl);
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
   const int rows = P.q_tokens * P.c.group;
   const int blocks = (rows + R - 1) / R;
-  if (tid == 0) {
-    for (int i = 0; i < kStages; ++i) {
-      mbar_init(&ctl.full[i], 2);    // the bytes, and the scales beside them
-      mbar_init(&ctl.empty[i], 1);
+  if (threadIdx.x == 0) {
+    for (int i = 0; i < kKStages; ++i) {
+      mbar_init(&ctl.k_full[i], 1);
+      mbar_init(&ctl.k_empty[i], 1);
     }
-    mbar_init(&ctl.s_full, 1);
-    mbar_init(&ctl.p_full, 4);
+    for (int i = 0; i < kVStages; ++i) {
+      mbar_init(&ctl.v_full[i], 1);
+      mbar_init(&ctl.v_empty[i], 1);
+      mbar_init(&ctl.m_full[i], 1);
+    }
+    for (int i = 0; i < 2; ++i) {
+      mbar_init(&ctl.s_full[i], 1);
+      mbar_init(&ctl.q_full[i], 1);
+      mbar_init(&ctl.q_empty[i], 4 * H + 1);   // the softmax warps, and the last scores
+    }
+    for (int i = 0; i < H; ++i) mbar_init(&ctl.meet[i], 4);
+    mbar_init(&ctl.p_full, 4 * H);
     mbar_init(&ctl.o_full, 1);
-    mbar_init(&ctl.q_full, 4);
-    mbar_init(&ctl.meet, 4);
     mbar_init(&ctl.drain, 1);
     ctl.abort = ctl.never = 0;
     fence_mbar_init();
@@ -156,14 +175,10 @@ cache_attend_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_const
     prefetch_tensormap(&tm_v);
   }
   wait_previous_kernel();
-  if (warp == 5) {
-    tmem_alloc(&ctl.tmem_base, C::kTmemCols);
-    tmem_relinquish();
-  }
-  // The line's length, and the sequence in which this CTA's share starts: a run of sequences a thread
+  // The line's length, and the block in which this CTA's share starts: a run of sequences a thread
   const int cap = P.c.max_pages << P.c.page_shift;
-  const int per = (P.n_seq + kAttendThreads - 1) / kAttendThreads;
-  const int s0 = min(tid * per, P.n_seq), s1 = min(s0 + per, P.n_seq);
+  const int per = (P.n_seq + kThreads - 1) / kThreads;
+  const int s0 = min(static_cast<int>(threadIdx.x) * per, P.n_seq), s1 = min(s0 + per, P.n_seq);
   long long mine = 0;
   bool bad = false;
   for (int r = s0; r < s1; ++r) {
@@ -171,8 +186,12 @@ cache_attend_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_const
     bad |= len < 0 || len > cap;
     mine += (min(max(len, 0), cap) + kTileKeys - 1) / kTileKeys;
   }
-  if (bad && blockIdx.x == 0) atomicOr(P.err, kErrCheck);
-  const long long own = mine * (static_cast<long long>(P.c.heads) * blocks);
+  if (warp == 1) {
+    tmem_alloc(&ctl.tmem_base, C::kTmemCols);
+    tmem_relinquish();
+  }
+  const int per_tile = P.c.heads * blocks;
+  const long long own = mine * per_tile;
   long long front = own;   // tiles up to and with this thread's sequences
 #pragma unroll
   for (int o = 1; o < 32; o <<= 1) {
@@ -183,27 +202,32 @@ cache_attend_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_const
   tc_fence_before();
   __syncthreads();
   tc_fence_after();
-  long long total = 0;
+  long long all_tiles = 0;
 #pragma unroll
-  for (int w = 0; w < kAttendThreads / 32; ++w) {
+  for (int w = 0; w < kThreads / 32; ++w) {
     if (w < warp) front += static_cast<long long>(ctl.sums[w]);
-    total += static_cast<long long>(ctl.sums[w]);
+    all_tiles += static_cast<long long>(ctl.sums[w]);
   }
   front -= own;
-  const int ctas = static_cast<int>(min(total, static_cast<long long>(gridDim.x)));   // those that have a share
+  // (tiles of 32 KB each: a line of 2^31 of them is no call that ends)
+  bad |= all_tiles >= (1ll << 31);
+  if (bad && blockIdx.x == 0) atomicOr(P.err, kErrCheck);
+  const int total = all_tiles >= (1ll << 31) ? 0 : static_cast<int>(all_tiles);
+  const int ctas = min(total, static_cast<int>(gridDim.x));   // those that have a share
   const bool works = static_cast<int>(blockIdx.x) < ctas;
-  const auto share = [&](long long w) { return total * w / ctas; };                    // first tile of CTA w
-  const long long x0 = works ? share(blockIdx.x) : 0, x1 = works ? share(blockIdx.x + 1) : 0;
+  const int each = works ? total / ctas : 0, rest = total - each * ctas;
+  const auto share = [&](int w) { return each * w + rest * w / ctas; };   // first tile of CTA w: floor(total w / ctas)
+  const int x0 = works ? share(blockIdx.x) : 0, x1 = works ? share(blockIdx.x + 1) : 0;
   if (works && own > 0 && x0 >= front && x0 < front + own) {
-    long long at = front;
+    int at = static_cast<int>(front);
     for (int r = s0; r < s1; ++r) {
-      const long long n = (Walk::length(P, r) + kTileKeys - 1) / kTileKeys * (static_cast<long long>(P.c.heads) * blocks);
-      if (x0 < at + n) {
-        ctl.first_r = r;
-        ctl.base = at;
+      const int len = seq_len(P, r), tiles = (len + kTileKeys - 1) / kTileKeys;
+      if (x0 < at + tiles * per_tile) {
+        const int b = (x0 - at) / tiles, h = b / blocks;
+        ctl.first = {r, h, b - h * blocks, len, tiles, at + b * tiles};
         break;
       }
-      at += n;
+      at += tiles * per_tile;
     }
   }
   __syncthreads();
@@ -213,110 +237,129 @@ cache_attend_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_const
     atomicOr(P.err, kErrWait);
   };
 
-  if (warp == 4) {
+  if (warp == 0) {
     // ------------------------------------------------------------ producer: lane j the tile's page j
     if (works) {
       const int tile_pages = kTileKeys >> P.c.page_shift, page_bytes = P.c.page * kHeadDim;
-      Walk at;
-      at.seek(P, blocks, ctl.first_r, ctl.base, x0);
-      long long x = x0;
-      // the page of this lane in tile x (-1: none), and its scales
-      const auto page_of = [&](const Walk& w, long long tile) {
-        const int j = static_cast<int>(tile - w.first) * tile_pages + lane;
-        const bool has = lane < tile_pages && (j << P.c.page_shift) < w.len;
-        return has ? __ldg(P.table + static_cast<int64_t>(w.r) * P.c.max_pages + j) : -1;
+      // pages run two tiles ahead and scales one: neither is waited for in the loop
+      struct Ahead {
+        Block b;
+        int x, id;
+        bool has;   // this lane's page holds tokens
+      };
+      const auto step = [&](Ahead a) {
+        ++a.x;
+        if (a.x < x1 && a.x == a.b.first + a.b.tiles) next_block(P, blocks, a.b);
+        const int j = (a.x - a.b.first) * tile_pages + lane;
+        a.id = -1;
+        a.has = a.x < x1 && lane < tile_pages && (j << P.c.page_shift) < a.b.len;
+        if (a.has) a.id = __ldg(P.table + static_cast<int64_t>(a.b.r) * P.c.max_pages + j);
+        return a;
       };
       const auto valid = [&](int id) { return id >= 0 && id < P.c.num_pages; };
-      int id = page_of(at, x);
-      bool more = true;
-      int it = 0;
-      for (; more; ++it) {
-        const int st = it % kStages;
-        const bool has = lane < tile_pages && ((static_cast<int>(x - at.first) * tile_pages + lane) << P.c.page_shift) < at.len;
-        const bool ok = valid(id);
-        if (has && !ok) atomicOr(P.err, kErrCheck);
-        const int64_t block = static_cast<int64_t>(ok ? id : 0) * P.c.heads + at.h;
-        float ks = 0.f, vs = 0.f;
-        if (ok) {
-          ks = __ldg(P.c.k_scale + block);
-          vs = __ldg(P.c.v_scale + block);
+      const auto scales = [&](const Ahead& a) {
+        float2 f = make_float2(0.f, 0.f);
+        if (valid(a.id)) {
+          const int64_t block = static_cast<int64_t>(a.id) * P.c.heads + a.b.h;
+          f.x = __ldg(P.c.k_scale + block);
+          f.y = __ldg(P.c.v_scale + block);
         }
-        // the next tile's page while this one waits
-        Walk then = at;
-        more = x + 1 < x1;
-        if (more && x + 1 == then.first + then.tiles) then.next(P, blocks);
-        const int next_id = more ? page_of(then, x + 1) : -1;
-        if (!warp_wait(&ctl.empty[st], ((it / kStages) & 1) ^ 1, P.wait_limit_ns, &ctl.abort)) {
+        return f;
+      };
+      Ahead now = step({ctl.first, x0 - 1, 0, false});
+      Ahead then = step(now);
+      float2 sc = scales(now);
+      const int n = x1 - x0;
+      int it = 0;
+      for (; it < n; ++it) {
+        const int ks_at = it % kKStages, st = it % kVStages;
+        const bool ok = valid(now.id);
+        if (!ok && now.has) atomicOr(P.err, kErrCheck);
+        const Ahead after = step(then);
+        const float2 next_sc = scales(then);
+        if (!warp_wait(&ctl.k_empty[ks_at], ((it / kKStages) & 1) ^ 1, P.wait_limit_ns, &ctl.abort) ||
+            !warp_wait(&ctl.v_empty[st], ((it / kVStages) & 1) ^ 1, P.wait_limit_ns, &ctl.abort)) {
           if (lane == 0) fail();
           break;
         }
         const uint32_t mask = __ballot_sync(0xffffffffu, ok);
-        if (lane == 0) mbar_arrive_expect_tx(&ctl.full[st], __popc(mask) * 2 * page_bytes);
+        if (lane == 0) {
+          mbar_arrive_expect_tx(&ctl.k_full[ks_at], __popc(mask) * page_bytes);
+          mbar_arrive_expect_tx(&ctl.v_full[st], __popc(mask) * page_bytes);
+          ctl.pages[st] = mask;
+        }
         __syncwarp();
         if (ok) {
-          uint8_t* kdst = smem + static_cast<size_t>(st) * 2 * kTileBytes + lane * page_bytes;
-          const int row = static_cast<int>(block << P.c.page_shift);
-          tma_load_2d(kdst, &tm_k, 0, row, &ctl.full[st]);
-          tma_load_2d(kdst + kTileBytes, &tm_v, 0, row, &ctl.full[st]);
+          const int row = (now.id * P.c.heads + now.b.h) << P.c.page_shift;
+          tma_load_2d(smem + ks_at * kTileBytes + lane * page_bytes, &tm_k, 0, row, &ctl.k_full[ks_at]);
+          tma_load_2d(smem + C::kV + st * kTileBytes + lane * page_bytes, &tm_v, 0, row, &ctl.v_full[st]);
         }
         if (lane < kMostTilePages) {
-          ctl.ks[st][lane] = ks;
-          ctl.vs[st][lane] = vs;
+          ctl.ks[st][lane] = sc.x;
+          ctl.vs[st][lane] = sc.y;
         }
-        if (lane == 0) ctl.pages[st] = mask;
         __syncwarp();
-        if (lane == 0) mbar_arrive(&ctl.full[st]);
-        id = next_id;
-        at = then;
-        ++x;
+        if (lane == 0) mbar_arrive(&ctl.m_full[st]);
+        now = then;
+        then = after;
+        sc = next_sc;
       }
       // after a wait that ran out: the copies in flight end before the shared memory does
       if (ctl.abort && lane == 0) {
-        for (int k = max(it - kStages, 0); k < it; ++k)
-          mbar_wait(&ctl.full[k % kStages], (k / kStages) & 1, P.wait_limit_ns, &ctl.never);
+        for (int k = max(it - kKStages, 0); k < it; ++k)
+          mbar_wait(&ctl.k_full[k % kKStages], (k / kKStages) & 1, P.wait_limit_ns, &ctl.never);
+        for (int k = max(it - kVStages, 0); k < it; ++k)
+          mbar_wait(&ctl.v_full[k % kVStages], (k / kVStages) & 1, P.wait_limit_ns, &ctl.never);
       }
     }
-  } else if (warp == 5) {
+  } else if (warp == 1) {
     // ------------------------------------------------------------ MMA issuer
     if (works && lane == 0) {
       const uint32_t kaddr = smem_u32(smem), qaddr = kaddr + static_cast<uint32_t>(C::kQ);
       const uint32_t paddr = kaddr + static_cast<uint32_t>(C::kP);
-      Walk at;
-      at.seek(P, blocks, ctl.first_r, ctl.base, x0);
-      const int n = static_cast<int>(x1 - x0);
+      Block at = ctl.first;
+      const int n = x1 - x0;
       int part = 0;
-      long long x = x0;
-      const auto scores = [&](int it, bool new_q) -> bool {
-        if (new_q && !mbar_wait(&ctl.q_full, part++ & 1, P.wait_limit_ns, &ctl.abort)) return false;
-        if (!mbar_wait(&ctl.full[it % kStages], (it / kStages) & 1, P.wait_limit_ns, &ctl.abort)) return false;
+      // S^T of tile `it`; it runs two tiles ahead of the probabilities
+      const auto scores = [&](int it) -> bool {
+        const int x = x0 + it, st = it % kKStages;
+        const bool fresh = x == at.first + at.tiles;
+        if (fresh) {
+          next_block(P, blocks, at);
+          ++part;
+        }
+        if ((it == 0 || fresh) &&
+            !mbar_wait(&ctl.q_full[part & 1], (part >> 1) & 1, P.wait_limit_ns, &ctl.abort)) return false;
+        if (!mbar_wait(&ctl.k_full[st], (it / kKStages) & 1, P.wait_limit_ns, &ctl.abort)) return false;
         tc_fence_after();
-        const uint64_t a = sw128_desc(kaddr + (it % kStages) * 2 * kTileBytes), b = sw128_desc(qaddr);
+        const uint64_t a = sw128_desc(kaddr + st * kTileBytes);
+        const uint64_t b = sw128_desc(qaddr + (part & 1) * static_cast<uint32_t>(C::kQBytes));
+        const uint32_t d = tmem + (it & 1) * C::kNs;
 #pragma unroll
         for (int j = 0; j < kHeadDim / 32; ++j)   // 32 elements of d a step: 32 bytes of a row
-          tc_mma_e4m3(tmem, a + 2 * j, b + 2 * j, C::kIdescS, j > 0);
-        tc_commit(&ctl.s_full);
+          tc_mma_e4m3(d, a + 2 * j, b + 2 * j, C::kIdescS, j > 0);
+        tc_commit(&ctl.k_empty[st]);
+        tc_commit(&ctl.s_full[it & 1]);
+        if (x + 1 == x1 || x + 1 == at.first + at.tiles) tc_commit(&ctl.q_empty[part & 1]);
         return true;
       };
-      bool ok = scores(0, true);
+      bool ok = scores(0) && (n == 1 || scores(1));
       for (int it = 0; ok && it < n; ++it) {
-        if (!mbar_wait(&ctl.p_full, it & 1, P.wait_limit_ns, &ctl.abort)) {
+        const int st = it % kVStages;
+        if (!mbar_wait(&ctl.v_full[st], (it / kVStages) & 1, P.wait_limit_ns, &ctl.abort) ||
+            !mbar_wait(&ctl.p_full, it & 1, P.wait_limit_ns, &ctl.abort)) {
           ok = false;
           break;
         }
         tc_fence_after();
-        const uint32_t vaddr = kaddr + (it % kStages) * 2 * kTileBytes + kTileBytes;
+        const uint32_t vaddr = kaddr + static_cast<uint32_t>(C::kV) + st * kTileBytes;
 #pragma unroll
         for (int j = 0; j < kTileKeys / 32; ++j)   // 32 tokens a step: four 8-row groups of V, of P
           tc_mma_e4m3(tmem + C::kOCol, sw128_mn_desc(vaddr + 4096u * j, kTileBytes, 1024),
                       plain_mn_desc(paddr + 512u * j, 128, 16 * kTileKeys), C::kIdescO, j > 0);
-        tc_commit(&ctl.empty[it % kStages]);
+        tc_commit(&ctl.v_empty[st]);
         tc_commit(&ctl.o_full);
-        if (it + 1 < n) {
-          ++x;
-          const bool fresh = x == at.first + at.tiles;
-          if (fresh) at.next(P, blocks);
-          ok = scores(it + 1, fresh);
-        }
+        if (it + 2 < n) ok = scores(it + 2);
       }
       if (!ok) {
         fail();
@@ -324,370 +367,447 @@ cache_attend_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_const
         mbar_wait(&ctl.drain, 0, P.wait_limit_ns, &ctl.never);
       }
     }
-  } else {
-    // ------------------------------------------------------------ softmax: a token, then a column, a thread
-    // sequences without a token: their rows are zeros
+  } else if (warp == 2) {
+    // ------------------------------------------------------------ query rows, a block ahead
+    // Two e4m3 pieces, K-major with the 128-byte swizzle: 4 elements a lane and row.
+    if (works) {
+      uint8_t* qbuf = smem + C::kQ;
+      if constexpr (2 * R < C::kNs)   // columns behind the pieces: zeros, once
+        for (int i = lane; i < (C::kNs - 2 * R) * kHeadDim / 4; i += 32)
+          for (int k = 0; k < 2; ++k) reinterpret_cast<uint32_t*>(qbuf + k * C::kQBytes + 2 * R * kHeadDim)[i] = 0;
+      Block at = ctl.first;
+      for (int part = 0;; ++part) {
+        const int parity = part & 1;
+        if (part >= 2 && !warp_wait(&ctl.q_empty[parity], ((part >> 1) & 1) ^ 1, P.wait_limit_ns, &ctl.abort)) {
+          if (lane == 0) fail();
+          break;
+        }
+        long long src = -1;   // lane i: row i's
+        if (lane < R) {
+          const int row = at.rb * R + lane;
+          long long out_at = -1;
+          int lse_at = 0;
+          if (row < rows) {
+            const int t = row / P.c.group, hq = at.h * P.c.group + row - t * P.c.group;
+            const long long tok = static_cast<long long>(at.r) * P.q_tokens + t;
+            src = tok * P.q_st + hq * P.q_sh;
+            out_at = tok * P.o_st + hq * P.o_sh;
+            lse_at = static_cast<int>(tok * P.c.hq) + hq;
+            ctl.seen[parity][lane] = at.len - P.q_tokens + t + 1;
+          } else {
+            ctl.seen[parity][lane] = 0;
+          }
+          ctl.out_at[parity][lane] = out_at;
+          ctl.lse_at[parity][lane] = lse_at;
+        }
+        constexpr int kBatch = R < 8 ? R : 8;
+#pragma unroll 1
+        for (int i0 = 0; i0 < R; i0 += kBatch) {
+          uint2 x[kBatch];
+#pragma unroll
+          for (int i = 0; i < kBatch; ++i) {
+            const long long from = __shfl_sync(0xffffffffu, src, i0 + i);
+            x[i] = make_uint2(0, 0);
+            if (from >= 0) x[i] = __ldg(reinterpret_cast<const uint2*>(P.q + from) + lane);
+          }
+#pragma unroll
+          for (int i = 0; i < kBatch; ++i) {
+            const uint32_t two = x[i].x & 0x7fff7fffu, two2 = x[i].y & 0x7fff7fffu;
+            const uint32_t m = __reduce_max_sync(
+                0xffffffffu, max(max(two & 0xffffu, two >> 16), max(two2 & 0xffffu, two2 >> 16)));
+            const bool finite = m < 0x7f80u;
+            const float scale = __uint_as_float(piece_scale(m));
+            const float a = __uint_as_float(x[i].x << 16) * scale, b = __uint_as_float(x[i].x & 0xffff0000u) * scale;
+            const float c = __uint_as_float(x[i].y << 16) * scale, d = __uint_as_float(x[i].y & 0xffff0000u) * scale;
+            const uint32_t ab = e4m3x2(a, b), cd = e4m3x2(c, d);
+            const float2 fab = e4m3x2_values(ab), fcd = e4m3x2_values(cd);
+            const uint32_t lo = e4m3x2((a - fab.x) * 16.f, (b - fab.y) * 16.f) |
+                                e4m3x2((c - fcd.x) * 16.f, (d - fcd.y) * 16.f) << 16;
+            const auto put = [&](int n, uint32_t v) {
+              *reinterpret_cast<uint32_t*>(qbuf + parity * C::kQBytes + n * kHeadDim + (((lane >> 2) ^ (n & 7)) << 4) +
+                                           ((lane & 3) << 2)) = v;
+            };
+            put(i0 + i, finite ? ab | cd << 16 : 0u);
+            put(R + i0 + i, finite ? lo : 0u);
+            // a row with an infinity or a NaN: every logit NaN
+            if (lane == 0)
+              ctl.qs[parity][i0 + i] = finite ? P.alpha * __frcp_rn(scale) : __uint_as_float(0x7fc00000u);
+          }
+        }
+        fence_proxy_async_smem();
+        __syncwarp();
+        if (lane == 0) mbar_arrive(&ctl.q_full[parity]);
+        if (at.first + at.tiles >= x1) break;
+        next_block(P, blocks, at);
+      }
+    }
+  } else if (warp == 3) {
+    // ------------------------------------------------------------ sequences without a token: their rows are zeros
     for (int r = blockIdx.x; r < P.n_seq; r += gridDim.x)
-      if (Walk::length(P, r) == 0)
+      if (seq_len(P, r) == 0)
         for (int i = 0; i < P.q_tokens * P.c.hq; ++i) {
           const int64_t tok = static_cast<int64_t>(r) * P.q_tokens + i / P.c.hq;
-          P.out[tok * P.o_st + (i % P.c.hq) * P.o_sh + tid] = 0;
-          if (P.lse && tid == 0) P.lse[tok * P.c.hq + i % P.c.hq] = -INFINITY;
+          reinterpret_cast<uint2*>(P.out + tok * P.o_st + (i % P.c.hq) * P.o_sh)[lane] = make_uint2(0, 0);
+          if (P.lse && lane == 0) P.lse[tok * P.c.hq + i % P.c.hq] = -INFINITY;
         }
-    if (works) {
-      const uint32_t quad = static_cast<uint32_t>(warp) << 21;   // this warp's TMEM lanes
-      uint8_t* qbuf = smem + C::kQ;
-      uint8_t* pbuf = smem + C::kP;
-      uint32_t met = 0;
-      // all 128 threads; what each wrote to shared memory before is seen behind it
-      const auto meet = [&]() -> bool {
-        __syncwarp();
-        if (lane == 0) mbar_arrive(&ctl.meet);
-        return warp_wait(&ctl.meet, met++ & 1u, P.wait_limit_ns, &ctl.abort);
-      };
-      // Query rows of a block as two e4m3 pieces, K-major with the 128-byte swizzle. 128 / R threads a
-      // row, R elements each.
-      const auto load_q = [&](const Walk& w, int parity) {
-        constexpr int kPer = R, kLanes = 128 / R;
-        const int i = tid / kLanes, c = tid % kLanes * kPer, row = w.rb * R + i;
-        uint32_t x[kPer / 2];
+  } else if (works) {
+    // ------------------------------------------------------------ softmax: a token, then a column, a thread
+    const int half = H == 1 ? 0 : (warp >> 2) - 1, quad = warp & 3;
+    const int tid = quad * 32 + lane, i0 = half * N;     // this thread's rows are i0 .. i0 + N - 1 of the block
+    const uint32_t my_lanes = static_cast<uint32_t>(quad) << 21;
+    uint8_t* pbuf = smem + C::kP;
+    uint32_t met = 0;
+    // the 128 threads of these rows; what each wrote to shared memory before is seen behind it
+    const auto meet_arrive = [&]() {
+      __syncwarp();
+      if (lane == 0) mbar_arrive(&ctl.meet[half]);
+    };
+    const auto meet_wait = [&]() -> bool {
+      return warp_wait(&ctl.meet[half], met++ & 1u, P.wait_limit_ns, &ctl.abort);
+    };
+    Block at = ctl.first;
+    const int n = x1 - x0;
+    int part = 0, part0 = x0, splits = 0;
+    bool ok = true;
+    float m[N], l[N], acc[N], keep[N];   // keep: exp(old maximum - new) of the last tile
+    float back = 0.f;                    // the last tile's scale of O^T
+    // adds tile `it`'s O^T
+    const auto take = [&](int it) -> bool {
+      if (!warp_wait(&ctl.o_full, it & 1, P.wait_limit_ns, &ctl.abort)) return false;
+      tc_fence_after();
+      float o[N == 4 ? 16 : 3 * N];
+      if constexpr (H == 1 && N == 4) {
+        tmem_ld16(tmem + C::kOCol + my_lanes, o);
+      } else {
+        static_assert(N == 8, "three loads of 8 columns");
 #pragma unroll
-        for (int j = 0; j < kPer / 2; ++j) x[j] = 0;
-        if (row < rows) {
-          const int64_t tok = static_cast<int64_t>(w.r) * P.q_tokens + row / P.c.group;
-          const uint16_t* src = P.q + tok * P.q_st + (w.h * P.c.group + row % P.c.group) * P.q_sh + c;
-          if constexpr (kPer == 4) {
-            const uint2 y = __ldg(reinterpret_cast<const uint2*>(src));
-            x[0] = y.x, x[1] = y.y;
-          } else {
+        for (int k = 0; k < 3; ++k) tmem_ld8(tmem + C::kOCol + k * R + i0 + my_lanes, o + k * N);
+      }
+      tmem_wait_ld(o);
 #pragma unroll
-            for (int j = 0; j < kPer / 8; ++j) {
-              const uint4 y = __ldg(reinterpret_cast<const uint4*>(src) + j);
-              x[4 * j] = y.x, x[4 * j + 1] = y.y, x[4 * j + 2] = y.z, x[4 * j + 3] = y.w;
-            }
-          }
+      for (int i = 0; i < N; ++i) {
+        const float y = fmaf(fmaf(o[2 * N + i], 0.0625f, o[N + i]), 0.0625f, o[i]);
+        acc[i] = fmaf(y, back, acc[i] * keep[i]);
+      }
+      return true;
+    };
+    const auto begin = [&]() -> bool {
+#pragma unroll
+      for (int i = 0; i < N; ++i) {
+        m[i] = -INFINITY;
+        l[i] = acc[i] = 0.f;
+      }
+      if (half == 0) ctl.nan_from[part & 1][tid] = kNoNan;
+      return warp_wait(&ctl.q_full[part & 1], (part >> 1) & 1, P.wait_limit_ns, &ctl.abort);
+    };
+    ok = begin();
+    bool pending = false;   // the tile before is of this part and not added yet
+    for (int it = 0; ok && it < n; ++it) {
+      const int x = x0 + it, st = it % kVStages;
+      const int pos = (x - at.first) * kTileKeys + tid;
+      if (!warp_wait(&ctl.m_full[st], (it / kVStages) & 1, P.wait_limit_ns, &ctl.abort)) {
+        ok = false;
+        break;
+      }
+      const int pg = tid >> P.c.page_shift;
+      const uint32_t have = ctl.pages[st];
+      const bool held = (have >> pg & 1u) && pos < at.len;
+      const float ks = ctl.ks[st][pg];
+      float vtop = 0.f;
+#pragma unroll
+      for (int j = 0; j < kMostTilePages; ++j) vtop = fmaxf(vtop, ctl.vs[st][j]);
+      // the largest scale of the tile's values comes out of the sums; a token keeps the rest (at most 1)
+      const float vrest = held && vtop > 0.f ? ctl.vs[st][pg] * __frcp_rn(vtop) * 256.f : 0.f;
+      if (!warp_wait(&ctl.s_full[it & 1], (it >> 1) & 1, P.wait_limit_ns, &ctl.abort)) {
+        ok = false;
+        break;
+      }
+      tc_fence_after();
+      float w[N];
+      {
+        float s[2 * N];
+        const uint32_t from = tmem + (it & 1) * C::kNs + my_lanes;
+        if constexpr (H == 1 && N == 4) {
+          tmem_ld8(from, s);
+        } else {
+          tmem_ld8(from + i0, s);
+          tmem_ld8(from + R + i0, s + N);
         }
-        uint32_t m = 0;
-#pragma unroll
-        for (int j = 0; j < kPer / 2; ++j) m = max(m, max(x[j] & 0x7fffu, (x[j] >> 16) & 0x7fffu));
-#pragma unroll
-        for (int o = kLanes / 2; o > 0; o >>= 1) m = max(m, __shfl_xor_sync(0xffffffffu, m, o));
-        const bool finite = m < 0x7f80u;
-        const float scale = __uint_as_float(finite ? piece_scale(m) : 0u);
-        uint32_t hi[kPer / 4], lo[kPer / 4];
-#pragma unroll
-        for (int j = 0; j < kPer / 2; ++j) {
-          const float a = finite ? __uint_as_float(x[j] << 16) * scale : 0.f;
-          const float b = finite ? __uint_as_float(x[j] & 0xffff0000u) * scale : 0.f;
-          const uint32_t two = e4m3x2(a, b);
-          const float2 f = e4m3x2_values(two);
-          const uint32_t rest = e4m3x2((a - f.x) * 16.f, (b - f.y) * 16.f);
-          hi[j / 2] = j % 2 ? hi[j / 2] | two << 16 : two;
-          lo[j / 2] = j % 2 ? lo[j / 2] | rest << 16 : rest;
-        }
-        const auto put = [&](int n, const uint32_t* v) {
-          uint8_t* dst = qbuf + n * kHeadDim + (((c >> 4) ^ (n & 7)) << 4) + (c & 15);
-          if constexpr (kPer == 4) {
-            *reinterpret_cast<uint32_t*>(dst) = v[0];
-          } else if constexpr (kPer == 8) {
-            *reinterpret_cast<uint2*>(dst) = make_uint2(v[0], v[1]);
-          } else {
-            *reinterpret_cast<uint4*>(dst) = make_uint4(v[0], v[1], v[2], v[3]);
-          }
-        };
-        put(i, hi);
-        put(R + i, lo);
-        // a row with an infinity or a NaN: every logit NaN
-        if (tid % kLanes == 0) ctl.qs[parity][i] = finite ? P.alpha * __frcp_rn(scale) : __uint_as_float(0x7fc00000u);
-        fence_proxy_async();
-        __syncwarp();
-        if (lane == 0) mbar_arrive(&ctl.q_full);
-      };
-
-      Walk at;
-      at.seek(P, blocks, ctl.first_r, ctl.base, x0);
-      if constexpr (2 * R < C::kNs)   // columns behind the pieces: zeros, once
-        for (int i = tid; i < (C::kNs - 2 * R) * kHeadDim / 4; i += 128)
-          reinterpret_cast<uint32_t*>(qbuf + 2 * R * kHeadDim)[i] = 0;
-      int part = 0;
-      load_q(at, 0);
-      bool ok = meet();
-      float m[R], l[R], acc[R];
-      int seen[R];   // tokens that the row sees
-      int nan_from = INT32_MAX;   // the first position with a NaN in this column, among those not all rows see
-      const auto begin = [&]() {
-#pragma unroll
-        for (int i = 0; i < R; ++i) {
-          m[i] = -INFINITY;
-          l[i] = acc[i] = 0.f;
-          const int row = at.rb * R + i;
-          seen[i] = row < rows ? at.len - P.q_tokens + row / P.c.group + 1 : 0;
-        }
-        nan_from = INT32_MAX;
-      };
-      if (ok) begin();
-      long long x = x0, part0 = x0;
-      const int n = static_cast<int>(x1 - x0);
-      for (int it = 0; ok && it < n; ++it, ++x) {
-        const int st = it % kStages;
-        const int pos = static_cast<int>(x - at.first) * kTileKeys + tid;
-        if (!warp_wait(&ctl.full[st], (it / kStages) & 1, P.wait_limit_ns, &ctl.abort)) {
-          ok = false;
-          break;
-        }
-        const int pg = tid >> P.c.page_shift;
-        const uint32_t have = ctl.pages[st];
-        const bool held = (have >> pg & 1u) && pos < at.len;
-        const float ks = ctl.ks[st][pg];
-        float vtop = 0.f;
-#pragma unroll
-        for (int j = 0; j < kMostTilePages; ++j) vtop = fmaxf(vtop, ctl.vs[st][j]);
-        // the largest scale of the tile's values comes out of the sums; a token keeps the rest (at most 1)
-        const float vrest = held && vtop > 0.f ? ctl.vs[st][pg] * __frcp_rn(vtop) * 256.f : 0.f;
-        if (!warp_wait(&ctl.s_full, it & 1, P.wait_limit_ns, &ctl.abort)) {
-          ok = false;
-          break;
-        }
-        tc_fence_after();
-        float s[C::kNs];
-        if constexpr (C::kNs == 16) tmem_ld16(tmem + quad, s);
-        else tmem_ld32(tmem + quad, s);
         tmem_wait_ld(s);
-        float w[R];
 #pragma unroll
-        for (int i = 0; i < R; ++i) {
-          const float y = fmaf(s[R + i], 0.0625f, s[i]) * ctl.qs[part & 1][i] * ks;
-          w[i] = held && pos < seen[i] ? y : -INFINITY;
+        for (int i = 0; i < N; ++i) {
+          const float y = fmaf(s[N + i], 0.0625f, s[i]) * ctl.qs[part & 1][i0 + i] * ks;
+          w[i] = held && pos < ctl.seen[part & 1][i0 + i] ? y : -INFINITY;
         }
-        float* red = &ctl.red[it & 1][warp][0];
+      }
+      float* red = &ctl.red[it & 1][quad][i0];
 #pragma unroll
-        for (int i = 0; i < R; ++i) {
-          const float top = warp_max(w[i]);
-          if (lane == i) red[i] = top;
-        }
-        if (!meet()) {
-          ok = false;
-          break;
-        }
-        float keep[R];   // exp(old maximum - new)
+      for (int i = 0; i < N; ++i) {
+        const float top = warp_max(w[i]);
+        if (lane == i) red[i] = top;
+      }
+      meet_arrive();
+      // the tile before while the others arrive; its probabilities' buffer is free behind it
+      if (pending && !take(it - 1)) {
+        ok = false;
+        break;
+      }
+      if (!meet_wait()) {
+        ok = false;
+        break;
+      }
+      back = vtop * (1.f / 256.f);
 #pragma unroll
-        for (int i = 0; i < R; ++i) {
-          const float top = fmaxf(fmaxf(ctl.red[it & 1][0][i], ctl.red[it & 1][1][i]),
-                                  fmaxf(ctl.red[it & 1][2][i], ctl.red[it & 1][3][i]));
-          const float mn = fmaxf(m[i], top), ref = mn == -INFINITY ? 0.f : mn;
-          keep[i] = ex2(m[i] - ref);
-          m[i] = mn;
-          const float p = ex2(w[i] - ref);
-          l[i] = fmaf(l[i], keep[i], p);
-          w[i] = w[i] == -INFINITY ? 0.f : p * vrest;
-        }
-        // three e4m3 pieces of each probability: column k R + i of the token's row
-        uint32_t out[C::kNp / 4];
+      for (int i = 0; i < N; ++i) {
+        const float top = fmaxf(fmaxf(ctl.red[it & 1][0][i0 + i], ctl.red[it & 1][1][i0 + i]),
+                                fmaxf(ctl.red[it & 1][2][i0 + i], ctl.red[it & 1][3][i0 + i]));
+        const float mn = fmaxf(m[i], top), ref = mn == -INFINITY ? 0.f : mn;
+        keep[i] = ex2(m[i] - ref);
+        m[i] = mn;
+        const float p = ex2(w[i] - ref);
+        l[i] = fmaf(l[i], keep[i], p);
+        w[i] = w[i] == -INFINITY ? 0.f : p * vrest;
+      }
+      // three e4m3 pieces of each probability: column k R + i of the token's row
+      uint32_t out[up16(3 * N) / 4];
 #pragma unroll
-        for (int i = 0; i < C::kNp / 4; ++i) out[i] = 0;
+      for (int i = 0; i < up16(3 * N) / 4; ++i) out[i] = 0;
 #pragma unroll
-        for (int i = 0; i < R; i += 2) {
-          float a = w[i], b = w[i + 1];
+      for (int i = 0; i < N; i += 2) {
+        float a = w[i], b = w[i + 1];
 #pragma unroll
-          for (int k = 0; k < 3; ++k) {
-            const uint32_t two = e4m3x2(a, b);
-            out[(k * R + i) / 4] |= two << (8 * ((k * R + i) % 4));
-            if (k < 2) {
-              const float2 f = e4m3x2_values(two);
-              a = (a - f.x) * 16.f;
-              b = (b - f.y) * 16.f;
-            }
+        for (int k = 0; k < 3; ++k) {
+          const uint32_t two = e4m3x2(a, b);
+          out[(k * N + i) / 4] |= two << (8 * ((k * N + i) % 4));
+          if (k < 2) {
+            const float2 f = e4m3x2_values(two);
+            a = (a - f.x) * 16.f;
+            b = (b - f.y) * 16.f;
           }
         }
+      }
+      if constexpr (H == 1) {
 #pragma unroll
         for (int c = 0; c < C::kNp / 16; ++c)
           *reinterpret_cast<uint4*>(pbuf + c * (16 * kTileKeys) + tid * 16) =
               make_uint4(out[4 * c], out[4 * c + 1], out[4 * c + 2], out[4 * c + 3]);
-        const int tile_end = pos - tid + kTileKeys;
-        const bool all = have == (0xffu >> (kMostTilePages - (kTileKeys >> P.c.page_shift))) && tile_end <= at.len;
-        const bool some = P.q_tokens > 1 && tile_end > at.len - P.q_tokens + 1;
-        if (!all || some) {
-          uint8_t* v = smem + static_cast<size_t>(st) * 2 * kTileBytes + kTileBytes;
-          if (!held) {
-            // a probability of 0 does not undo a NaN: rows without a token are zeros
+      } else {
+        static_assert(H == 1 || (R == 16 && N == 8), "a piece of 16 rows is 16 bytes, 8 a half");
 #pragma unroll
-            for (int j = 0; j < kHeadDim / 16; ++j) reinterpret_cast<uint4*>(v + tid * kHeadDim)[j] = make_uint4(0, 0, 0, 0);
-          }
-          if (some) {
-            // nor may a NaN value that later rows see reach the earlier ones: it is taken out here, and
-            // given to the rows that see it when the part ends
-            const int t0 = max(at.len - P.q_tokens + 1 - (pos - tid), 0), t1 = min(at.len - (pos - tid), kTileKeys);
-            for (int t = t0; t < t1; ++t) {
-              uint8_t* at8 = v + t * kHeadDim + (((tid >> 4) ^ (t & 7)) << 4) + (tid & 15);
-              if ((have >> (t >> P.c.page_shift) & 1u) && (*at8 & 0x7f) == 0x7f) {
-                nan_from = min(nan_from, pos - tid + t);
-                *at8 = 0;
-              }
-            }
-          }
-        }
-        fence_proxy_async();
-        tc_fence_before();
-        __syncwarp();
-        if (lane == 0) mbar_arrive(&ctl.p_full);
-        const bool part_ends = x + 1 == x1 || x + 1 == at.first + at.tiles;
-        Walk then = at;
-        if (part_ends && x + 1 < x1) {
-          // the next block's rows while the tensor cores work (the scores of this one are done)
-          then.next(P, blocks);
-          load_q(then, (part + 1) & 1);
-        }
-        if (!warp_wait(&ctl.o_full, it & 1, P.wait_limit_ns, &ctl.abort)) {
+        for (int k = 0; k < 3; ++k)
+          *reinterpret_cast<uint2*>(pbuf + k * (16 * kTileKeys) + tid * 16 + half * 8) =
+              make_uint2(out[2 * k], out[2 * k + 1]);
+      }
+      const int tile0 = pos - tid, tile_end = tile0 + kTileKeys;
+      const bool whole = have == (0xffu >> (kMostTilePages - (kTileKeys >> P.c.page_shift))) && tile_end <= at.len;
+      const bool some = P.q_tokens > 1 && tile_end > at.len - P.q_tokens + 1;
+      if (half == 0 && (!whole || some)) {
+        if (!warp_wait(&ctl.v_full[st], (it / kVStages) & 1, P.wait_limit_ns, &ctl.abort)) {
           ok = false;
           break;
         }
-        tc_fence_after();
-        float o[C::kNp];
-        if constexpr (C::kNp == 16) {
-          tmem_ld16(tmem + C::kOCol + quad, o);
-        } else {
-          tmem_ld32(tmem + C::kOCol + quad, o);
-          if constexpr (C::kNp == 48) tmem_ld16(tmem + C::kOCol + 32 + quad, o + 32);
+        uint8_t* v = smem + C::kV + st * kTileBytes;
+        if (!held) {
+          // a probability of 0 does not undo a NaN: rows without a token are zeros
+#pragma unroll
+          for (int j = 0; j < kHeadDim / 16; ++j) reinterpret_cast<uint4*>(v + tid * kHeadDim)[j] = make_uint4(0, 0, 0, 0);
         }
-        tmem_wait_ld(o);
-        tc_fence_before();
-        const float back = vtop * (1.f / 256.f);
-#pragma unroll
-        for (int i = 0; i < R; ++i) {
-          const float y = fmaf(fmaf(o[2 * R + i], 0.0625f, o[R + i]), 0.0625f, o[i]);
-          acc[i] = fmaf(y, back, acc[i] * keep[i]);
-        }
-        if (!part_ends) continue;
-
-        // ---------------------------------------------------------- the end of a part
-#pragma unroll
-        for (int i = 0; i < R; ++i)
-          if (seen[i] > nan_from) acc[i] = __uint_as_float(0x7fc00000u);
-        // row sums over the tokens' threads
-#pragma unroll
-        for (int i = 0; i < R; ++i) {
-#pragma unroll
-          for (int o2 = 16; o2 > 0; o2 >>= 1) l[i] += __shfl_xor_sync(0xffffffffu, l[i], o2);
-          if (lane == i) ctl.red[(it + 1) & 1][warp][i] = l[i];   // (the next tile writes there behind a meet)
-        }
-        if (!meet()) {
-          ok = false;
-          break;
-        }
-#pragma unroll
-        for (int i = 0; i < R; ++i) {
-          const float(*red4)[R] = ctl.red[(it + 1) & 1];
-          l[i] = (red4[0][i] + red4[1][i]) + (red4[2][i] + red4[3][i]);
-        }
-        bool write = true;
-        const long long end = at.first + at.tiles;
-        if (part0 != at.first || x + 1 != end) {
-          // one of several parts: leave it for the CTA that finishes last
-          const int w0 = static_cast<int>(((at.first + 1) * ctas + total - 1) / total) - 1;
-          const int w1 = static_cast<int>((end * ctas + total - 1) / total) - 1;
-          const auto slot = [&](int w) {   // a part that starts where the CTA does, or a later one
-            return P.partial + (static_cast<int64_t>(w) * 2 + (w == w0 && share(w) != at.first ? 1 : 0)) * kAttendPartWords;
-          };
-          float* dst = slot(blockIdx.x);
-#pragma unroll
-          for (int i = 0; i < R; ++i) {
-            __stcg(dst + i * kHeadDim + tid, acc[i]);
-            if (tid == i) {
-              __stcg(dst + R * kHeadDim + i, m[i]);
-              __stcg(dst + R * kHeadDim + R + i, l[i]);
+        if (some) {
+          // nor may a NaN value that later rows see reach the earlier ones: it is taken out here, and given to
+          // the rows that see it when the part ends. nan_from: the first position with a NaN in this
+          // column, counted from the first one that not every row sees
+          const int first = at.len - P.q_tokens + 1 - tile0, t0 = max(first, 0), t1 = min(at.len - tile0, kTileKeys);
+          for (int t = t0; t < t1; ++t) {
+            uint8_t* at8 = v + t * kHeadDim + (((tid >> 4) ^ (t & 7)) << 4) + (tid & 15);
+            if ((have >> (t >> P.c.page_shift) & 1u) && (*at8 & 0x7f) == 0x7f) {
+              const int f = t - first;
+              if (f < ctl.nan_from[part & 1][tid]) ctl.nan_from[part & 1][tid] = static_cast<uint8_t>(f);
+              *at8 = 0;
             }
           }
-          __threadfence();
-          if (!meet()) {
-            ok = false;
-            break;
-          }
-          if (tid == 0) ctl.last = atomicInc(P.arrive + w0, static_cast<unsigned>(w1 - w0)) == static_cast<unsigned>(w1 - w0);
-          if (!meet()) {
-            ok = false;
-            break;
-          }
-          write = ctl.last != 0;
-          if (write) {
-            __threadfence();
-#pragma unroll
-            for (int i = 0; i < R; ++i) {
-              m[i] = -INFINITY;
-              l[i] = acc[i] = 0.f;
-            }
-            for (int wk = w0; wk <= w1; ++wk) {
-              const float* src = slot(wk);
-#pragma unroll
-              for (int i = 0; i < R; ++i) {
-                const float pm = __ldcg(src + R * kHeadDim + i), pl = __ldcg(src + R * kHeadDim + R + i);
-                const float po = __ldcg(src + i * kHeadDim + tid);
-                const float mn = fmaxf(m[i], pm), ref = mn == -INFINITY ? 0.f : mn;
-                const float f = ex2(m[i] - ref), g = ex2(pm - ref);
-                l[i] = l[i] * f + pl * g;
-                acc[i] = acc[i] * f + po * g;
-                m[i] = mn;
-              }
-            }
-          }
-        }
-        if (write) {
-#pragma unroll
-          for (int i = 0; i < R; ++i) {
-            const int row = at.rb * R + i;
-            if (row < rows) {
-              const int64_t tok = static_cast<int64_t>(at.r) * P.q_tokens + row / P.c.group;
-              const int hq = at.h * P.c.group + row % P.c.group;
-              const bool none = l[i] == 0.f;   // (a NaN sum is not: its row is NaN)
-              P.out[tok * P.o_st + hq * P.o_sh + tid] = none ? 0 : to_bf16(acc[i] / l[i]);
-              if (P.lse && tid == 0)
-                P.lse[tok * P.c.hq + hq] = none ? -INFINITY : (m[i] == -INFINITY ? 0.f : m[i]) * 0.69314718056f +
-                                                                   lg2(l[i]) * 0.69314718056f;
-            }
-          }
-        }
-        if (x + 1 < x1) {
-          at = then;
-          ++part;
-          part0 = x + 1;
-          begin();
-          ok = meet();   // the next block's scales are there, and this one's sums have been read
         }
       }
-      if (!ok && lane == 0) fail();
+      fence_proxy_async_smem();
+      tc_fence_before();
+      __syncwarp();
+      if (lane == 0) mbar_arrive(&ctl.p_full);
+      pending = !(x + 1 == x1 || x + 1 == at.first + at.tiles);
+      if (pending) continue;
+
+      // ---------------------------------------------------------- the end of a part
+      if (!take(it)) {
+        ok = false;
+        break;
+      }
+      if (P.q_tokens > 1) {
+        const int found = ctl.nan_from[part & 1][tid];
+        const int from = found == kNoNan ? INT32_MAX : at.len - P.q_tokens + 1 + found;
+#pragma unroll
+        for (int i = 0; i < N; ++i)
+          if (ctl.seen[part & 1][i0 + i] > from) acc[i] = __uint_as_float(0x7fc00000u);
+      }
+      // row sums over the tokens' threads
+#pragma unroll
+      for (int i = 0; i < N; ++i) {
+#pragma unroll
+        for (int o = 16; o > 0; o >>= 1) l[i] += __shfl_xor_sync(0xffffffffu, l[i], o);
+        if (lane == i) ctl.sum[quad][i0 + i] = l[i];
+      }
+      meet_arrive();
+      if (!meet_wait()) {
+        ok = false;
+        break;
+      }
+#pragma unroll
+      for (int i = 0; i < N; ++i)
+        l[i] = (ctl.sum[0][i0 + i] + ctl.sum[1][i0 + i]) + (ctl.sum[2][i0 + i] + ctl.sum[3][i0 + i]);
+      if (part0 == at.first && x + 1 == at.first + at.tiles) {
+#pragma unroll
+        for (int i = 0; i < N; ++i) {
+          const long long to = ctl.out_at[part & 1][i0 + i];
+          if (to < 0) continue;
+          P.out[to + tid] = l[i] == 0.f ? 0 : to_bf16(acc[i] * __frcp_rn(l[i]));
+          if (P.lse && tid == i) P.lse[ctl.lse_at[part & 1][i0 + i]] = log_sum(m[i], l[i]);
+        }
+      } else {
+        // one of several parts of the block: left for the join. Slot 0 is a part that starts where its CTA
+        // does, slot 1 a later one
+        float* dst = P.partial + (static_cast<int64_t>(blockIdx.x) * 2 + (part0 != x0)) * kAttendPartWords;
+#pragma unroll
+        for (int i = 0; i < N; ++i) {
+          __stcg(dst + (i0 + i) * kHeadDim + tid, acc[i]);
+          if (tid == i) {
+            __stcg(dst + R * kHeadDim + i0 + i, m[i]);
+            __stcg(dst + R * kHeadDim + R + i0 + i, l[i]);
+          }
+        }
+        if (tid == 0) ctl.split[2 * half + splits] = at;
+        ++splits;
+      }
+      __syncwarp();
+      if (lane == 0) mbar_arrive(&ctl.q_empty[part & 1]);
+      if (x + 1 < x1) {
+        next_block(P, blocks, at);
+        ++part;
+        part0 = x + 1;
+        ok = begin();
+      }
     }
+
+    // ------------------------------------------------------------ the join of blocks that several CTAs had parts of
+    // Counted once this CTA's share is done (a fence under the loads of a running share takes 5 us), by the
+    // first CTA that has a part of the block; the CTA that counts last joins.
+    if (ok && splits > 0) {
+      const auto cta_of = [&](int tile) {   // whose share tile is in
+        int w = min(static_cast<int>(static_cast<float>(tile) * static_cast<float>(ctas) / static_cast<float>(total)),
+                    ctas - 1);
+        while (w > 0 && share(w) > tile) --w;
+        while (w + 1 < ctas && share(w + 1) <= tile) ++w;
+        return w;
+      };
+      __threadfence();
+      meet_arrive();
+      ok = meet_wait();
+      if (ok && tid < splits) {
+        const Block b = ctl.split[2 * half + tid];
+        const int w0 = cta_of(b.first), parts = cta_of(b.first + b.tiles - 1) - w0;
+        __threadfence();
+        ctl.last[2 * half + tid] = atomicInc(P.arrive + w0 * H + half, static_cast<unsigned>(parts)) == static_cast<unsigned>(parts);
+      }
+      if (ok) {
+        meet_arrive();
+        ok = meet_wait();
+      }
+      for (int k = 0; ok && k < splits; ++k) {
+        if (!ctl.last[2 * half + k]) continue;
+        __threadfence();
+        const Block b = ctl.split[2 * half + k];
+        const int w0 = cta_of(b.first), w1 = cta_of(b.first + b.tiles - 1);
+        const int w0_slot = share(w0) != b.first;
+        const auto slot = [&](int w) {
+          return P.partial + (static_cast<int64_t>(w) * 2 + (w == w0 ? w0_slot : 0)) * kAttendPartWords;
+        };
+        // a warp a row, four columns a lane, kJoin parts in flight; every sum in the order of the tokens
+        constexpr int kJoin = 8;
+        for (int i = i0 + quad; i < i0 + N; i += 4) {
+          const int row = b.rb * R + i;
+          if (row >= rows) break;
+          float top = -INFINITY, sum = 0.f;
+          float4 a4 = make_float4(0.f, 0.f, 0.f, 0.f);
+          for (int wb = w0; wb <= w1; wb += kJoin) {
+            float4 o[kJoin];
+            float pm = -INFINITY, pl = 0.f;
+            if (lane < kJoin && wb + lane <= w1) {
+              const float* src = slot(wb + lane) + R * kHeadDim + i;
+              pm = __ldcg(src);
+              pl = __ldcg(src + R);
+            }
+#pragma unroll
+            for (int j = 0; j < kJoin; ++j)
+              if (wb + j <= w1) o[j] = __ldcg(reinterpret_cast<const float4*>(slot(wb + j) + i * kHeadDim) + lane);
+            const float mn = fmaxf(top, warp_max(pm)), ref = mn == -INFINITY ? 0.f : mn;
+            const float f0 = ex2(top - ref), f = ex2(pm - ref);
+            top = mn;
+            sum *= f0;
+            a4.x *= f0, a4.y *= f0, a4.z *= f0, a4.w *= f0;
+            pl *= f;
+#pragma unroll
+            for (int j = 0; j < kJoin; ++j) {
+              const float g = __shfl_sync(0xffffffffu, f, j), s = __shfl_sync(0xffffffffu, pl, j);
+              if (wb + j <= w1) {
+                sum += s;
+                a4.x = fmaf(o[j].x, g, a4.x);
+                a4.y = fmaf(o[j].y, g, a4.y);
+                a4.z = fmaf(o[j].z, g, a4.z);
+                a4.w = fmaf(o[j].w, g, a4.w);
+              }
+            }
+          }
+          const int t = row / P.c.group, hq = b.h * P.c.group + row - t * P.c.group;
+          const int64_t tok = static_cast<int64_t>(b.r) * P.q_tokens + t;
+          const float inv = sum == 0.f ? 0.f : __frcp_rn(sum);
+          uint2 v;
+          v.x = to_bf16(a4.x * inv) | static_cast<uint32_t>(to_bf16(a4.y * inv)) << 16;
+          v.y = to_bf16(a4.z * inv) | static_cast<uint32_t>(to_bf16(a4.w * inv)) << 16;
+          reinterpret_cast<uint2*>(P.out + tok * P.o_st + hq * P.o_sh)[lane] = v;
+          if (P.lse && lane == 0) P.lse[tok * P.c.hq + hq] = log_sum(top, sum);
+        }
+      }
+    }
+    if (!ok && lane == 0) fail();
   }
 
   tc_fence_before();
   __syncthreads();
-  if (warp == 5) {
+  if (warp == 1) {
     tc_fence_after();
     tmem_dealloc(tmem, C::kTmemCols);
   }
 }
 
-template <int R>
+template <int R, int H>
 cudaError_t attend_rows(const kve_cache& c, const AttendParams& p, cudaStream_t stream) {
-  constexpr size_t smem = attend_smem<R>();
+  constexpr size_t smem = attend_smem<R, H>();
   static_assert(smem <= 113 * 1024, "two CTAs an SM");
-  cudaError_t e = cudaFuncSetAttribute(cache_attend_kernel<R>, cudaFuncAttributeMaxDynamicSharedMemorySize,
-                                       static_cast<int>(smem));
+  auto* fn = cache_attend_kernel<R, H>;
+  cudaError_t e = cudaFuncSetAttribute(fn, cudaFuncAttributeMaxDynamicSharedMemorySize, static_cast<int>(smem));
   if (e != cudaSuccess) return e;
   // no more CTAs than there can be tiles
   const int64_t blocks = (p.q_tokens * p.c.group + R - 1) / R;
   const int64_t tiles = ((static_cast<int64_t>(p.c.max_pages) << p.c.page_shift) + kTileKeys - 1) / kTileKeys;
   const int64_t most = static_cast<int64_t>(kAttendCtas) * c.sms;
   const int64_t want = tiles >= most ? most : tiles * p.n_seq * p.c.heads * blocks;
-  return launch_after_previous(cache_attend_kernel<R>, dim3(static_cast<unsigned>(want < most ? want : most)),
-                               dim3(kAttendThreads), smem, stream, c.tm_k, c.tm_v, p);
+  return launch_after_previous(fn, dim3(static_cast<unsigned>(want < most ? want : most)), dim3(ACfg<R, H>::kThreads),
+                               smem, stream, c.tm_k, c.tm_v, p);
 }
 
 }  // namespace
 
 cudaError_t launch_cache_attend(const kve_cache& c, const AttendParams& p, cudaStream_t stream) {
   const int rows = p.q_tokens * p.c.group;
-  if (rows <= 4) return attend_rows<4>(c, p, stream);
-  if (rows <= 8) return attend_rows<8>(c, p, stream);
-  return attend_rows<16>(c, p, stream);
+  if (rows <= 4) return attend_rows<4, 1>(c, p, stream);
+  if (rows <= 8) return attend_rows<8, 1>(c, p, stream);
+  return attend_rows<16, 2>(c, p, stream);
 }
 
 }  // namespace kve

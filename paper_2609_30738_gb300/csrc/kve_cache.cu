@@ -553,7 +553,7 @@ kve_status kv_evict_cache_create(const kve_cache_config* cfg, uint8_t* k, uint8_
   w.pages_done = 64;
   w.arrive = 256;
   const size_t workers = static_cast<size_t>(kve::kAttendCtas) * sms;
-  w.clear_end = align_up(w.arrive + sizeof(uint32_t) * workers, 256);
+  w.clear_end = align_up(w.arrive + sizeof(uint32_t) * 2 * workers, 256);
   w.partial = w.clear_end;
   w.total = align_up(w.partial + workers * 2 * kve::kAttendPartWords * sizeof(float), 256);
   h->maps = kve::encode_pages(&h->tm_k, k, g) && kve::encode_pages(&h->tm_v, v, g);

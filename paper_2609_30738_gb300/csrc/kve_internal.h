@@ -246,7 +246,7 @@ struct CacheGeometry {
 struct CacheWsLayout {
   size_t err;        // uint32 error word
   size_t pages_done; // uint32 CTAs of a kv_evict_cache_pages call that have finished reading
-  size_t arrive;     // uint32 [kAttendCtas * SMs] arrivals of the parts of a split row block
+  size_t arrive;     // uint32 [kAttendCtas * SMs][2] parts of a split row block that are written
   size_t clear_end;  // bytes cleared by kv_evict_cache_reset
   size_t partial;    // fp32 [kAttendCtas * SMs][2][kAttendPartWords] partial rows of the attention
   size_t total;
