@@ -57,6 +57,7 @@ struct ACfg {
 // the line of all tiles.
 struct Block {
   int r, h, rb, len, tiles, first;
+  int index;   // its number among all blocks that have tiles
 };
 
 template <int R, int H>
@@ -64,7 +65,7 @@ struct ACtl {
   uint64_t k_full[kKStages], k_empty[kKStages], v_full[kVStages], v_empty[kVStages];
   uint64_t m_full[kVStages];                   // the scales beside a V stage
   uint64_t s_full[2], q_full[2], q_empty[2];   // by tile parity, by part parity
-  uint64_t p_full, o_full, meet[H], drain;
+  uint64_t p_full, o_full, meet[H], joined[H], drain;
   float ks[kVStages][kMostTilePages], vs[kVStages][kMostTilePages];
   uint32_t pages[kVStages];                    // bit j: page j of the tile holds tokens
   float red[2][4][R];                          // row maxima of the warps, by tile parity
@@ -77,9 +78,10 @@ struct ACtl {
   int lse_at[2][R];
   uint8_t nan_from[2][kHeadDim];               // by part parity: see there
   Block split[2 * H];                          // parts left for the join, by half
-  int last[2 * H];
+  int last[2 * H], split_cta[2 * H];           // its parts, if they are all written; the CTA of the first
   Block first;                                 // the first part's block
-  unsigned long long sums[ACfg<R, H>::kThreads / 32];
+  int ends[2];                                 // this CTA's tiles of the line
+  unsigned long long sums[ACfg<R, H>::kThreads / 32][2];
   uint32_t tmem_base;
   int abort, never;                            // never: stays 0 (waits that a given-up call still has to make)
 };
@@ -96,6 +98,7 @@ __device__ __forceinline__ int seq_len(const AttendParams& P, int r) {
 // The block behind b in the line; a tile follows, so a sequence that is not empty does.
 __device__ __forceinline__ void next_block(const AttendParams& P, int blocks, Block& b) {
   b.first += b.tiles;
+  ++b.index;
   if (++b.rb < blocks) return;
   b.rb = 0;
   if (++b.h < P.c.heads) return;
@@ -105,6 +108,42 @@ __device__ __forceinline__ void next_block(const AttendParams& P, int blocks, Bl
     b.tiles = (b.len + kTileKeys - 1) / kTileKeys;
   } while (b.tiles == 0);
 }
+
+// How the line is cut. A part costs about kPartTiles tiles besides its own (its query rows, the tensor
+// cores' latency at its two ends, its output), so a block counts as its tiles and kPartTiles more units, and
+// the units are dealt evenly: CTA w's raw cut is floor(units * w / ctas). A cut that would leave fewer than
+// kLeastTiles tiles of a block on one of its sides moves to that end of the block: a join costs more than
+// those tiles do.
+// No more CTAs take part than have kLeastUnits each, or a block.
+constexpr int kPartTiles = 2, kLeastTiles = 4, kLeastUnits = 4;
+
+struct Cuts {
+  int each, rest, ctas, units;
+  uint32_t inverse;   // of ctas, 2^32 / ctas rounded up: exact for the products below ctas^2 that it divides
+  __device__ __forceinline__ void set(int n, int w) {
+    units = n;
+    ctas = w;
+    each = n / w;
+    rest = n - each * w;
+    inverse = 0xffffffffu / static_cast<uint32_t>(w) + 1u;   // (for one CTA 0, and rest is 0)
+  }
+  __device__ __forceinline__ int raw(int w) const {
+    return each * w + static_cast<int>(__umulhi(static_cast<uint32_t>(rest * w), inverse));
+  }
+  // the first w with raw(w) >= u
+  __device__ __forceinline__ int from(int u) const {
+    int w = min(max(static_cast<int>(static_cast<float>(u) * static_cast<float>(ctas) / static_cast<float>(units)), 0), ctas);
+    while (w > 0 && raw(w - 1) >= u) --w;
+    while (w < ctas && raw(w) < u) ++w;
+    return w;
+  }
+  // CTAs [*w0, *w1] have the parts of block b
+  __device__ __forceinline__ void parts(const Block& b, int* w0, int* w1) const {
+    const int a = b.first + (b.index + 1) * kPartTiles;   // its tile 0 in units
+    *w0 = from(a + kLeastTiles) - 1;
+    *w1 = from(a + b.tiles - kLeastTiles + 1) - 1;
+  }
+};
 
 // The power of two that brings the largest magnitude (bf16 bits a, finite) into [128, 256), as fp32 bits.
 __device__ __forceinline__ uint32_t piece_scale(uint32_t a) {
@@ -162,10 +201,13 @@ cache_attend_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_const
     }
     for (int i = 0; i < 2; ++i) {
       mbar_init(&ctl.s_full[i], 1);
-      mbar_init(&ctl.q_full[i], 1);
+      mbar_init(&ctl.q_full[i], 2);
       mbar_init(&ctl.q_empty[i], 4 * H + 1);   // the softmax warps, and the last scores
     }
-    for (int i = 0; i < H; ++i) mbar_init(&ctl.meet[i], 4);
+    for (int i = 0; i < H; ++i) {
+      mbar_init(&ctl.meet[i], 4);
+      mbar_init(&ctl.joined[i], 1);
+    }
     mbar_init(&ctl.p_full, 4 * H);
     mbar_init(&ctl.o_full, 1);
     mbar_init(&ctl.drain, 1);
@@ -180,57 +222,112 @@ cache_attend_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_const
   const int per = (P.n_seq + kThreads - 1) / kThreads;
   const int s0 = min(static_cast<int>(threadIdx.x) * per, P.n_seq), s1 = min(s0 + per, P.n_seq);
   long long mine = 0;
+  int filled = 0;
   bool bad = false;
   for (int r = s0; r < s1; ++r) {
     const int len = __ldg(P.lens + r);
     bad |= len < 0 || len > cap;
     mine += (min(max(len, 0), cap) + kTileKeys - 1) / kTileKeys;
+    filled += len > 0;
   }
   if (warp == 1) {
     tmem_alloc(&ctl.tmem_base, C::kTmemCols);
     tmem_relinquish();
   }
-  const int per_tile = P.c.heads * blocks;
-  const long long own = mine * per_tile;
-  long long front = own;   // tiles up to and with this thread's sequences
+  const int per_seq = P.c.heads * blocks;   // blocks of a sequence
+  long long front = mine;   // tiles of one block each, up to and with this thread's sequences; those sequences
+  int front_filled = filled;
 #pragma unroll
   for (int o = 1; o < 32; o <<= 1) {
     const long long x = __shfl_up_sync(0xffffffffu, front, o);
-    if (lane >= o) front += x;
+    const int y = __shfl_up_sync(0xffffffffu, front_filled, o);
+    if (lane >= o) {
+      front += x;
+      front_filled += y;
+    }
   }
-  if (lane == 31) ctl.sums[warp] = static_cast<unsigned long long>(front);
+  if (lane == 31) {
+    ctl.sums[warp][0] = static_cast<unsigned long long>(front);
+    ctl.sums[warp][1] = static_cast<unsigned long long>(front_filled);
+  }
   tc_fence_before();
   __syncthreads();
   tc_fence_after();
   long long all_tiles = 0;
+  int all_filled = 0;
 #pragma unroll
   for (int w = 0; w < kThreads / 32; ++w) {
-    if (w < warp) front += static_cast<long long>(ctl.sums[w]);
-    all_tiles += static_cast<long long>(ctl.sums[w]);
+    const long long x = static_cast<long long>(ctl.sums[w][0]);
+    const int y = static_cast<int>(ctl.sums[w][1]);
+    if (w < warp) {
+      front += x;
+      front_filled += y;
+    }
+    all_tiles += x;
+    all_filled += y;
   }
-  front -= own;
+  front -= mine;
+  front_filled -= filled;
+  const long long all_units = (all_tiles + static_cast<long long>(all_filled) * kPartTiles) * per_seq;
   // (tiles of 32 KB each: a line of 2^31 of them is no call that ends)
-  bad |= all_tiles >= (1ll << 31);
-  if (bad && blockIdx.x == 0) atomicOr(P.err, kErrCheck);
-  const int total = all_tiles >= (1ll << 31) ? 0 : static_cast<int>(all_tiles);
-  const int ctas = min(total, static_cast<int>(gridDim.x));   // those that have a share
-  const bool works = static_cast<int>(blockIdx.x) < ctas;
-  const int each = works ? total / ctas : 0, rest = total - each * ctas;
-  const auto share = [&](int w) { return each * w + rest * w / ctas; };   // first tile of CTA w: floor(total w / ctas)
-  const int x0 = works ? share(blockIdx.x) : 0, x1 = works ? share(blockIdx.x + 1) : 0;
-  if (works && own > 0 && x0 >= front && x0 < front + own) {
-    int at = static_cast<int>(front);
+  const bool too_long = all_units >= (1ll << 31);
+  if ((bad || too_long) && blockIdx.x == 0) atomicOr(P.err, kErrCheck);
+  Cuts cuts;
+  const int units = too_long ? 0 : static_cast<int>(all_units);
+  cuts.set(units, max(min(max(units / kLeastUnits, all_filled * per_seq), static_cast<int>(gridDim.x)), 1));
+  if (cuts.units > 0 && static_cast<int>(blockIdx.x) < cuts.ctas) {
+    // the thread that holds a cut's sequence says which tile of the line it is
+    const int c0 = cuts.raw(blockIdx.x), c1 = cuts.raw(blockIdx.x + 1);
+    int at = static_cast<int>(front) * per_seq, index = front_filled * per_seq;   // tiles, blocks in front
+    if (threadIdx.x == 0 && c1 == cuts.units) ctl.ends[1] = static_cast<int>(all_tiles) * per_seq;
     for (int r = s0; r < s1; ++r) {
       const int len = seq_len(P, r), tiles = (len + kTileKeys - 1) / kTileKeys;
-      if (x0 < at + tiles * per_tile) {
-        const int b = (x0 - at) / tiles, h = b / blocks;
-        ctl.first = {r, h, b - h * blocks, len, tiles, at + b * tiles};
-        break;
+      if (tiles == 0) continue;
+      const int unit = at + index * kPartTiles, size = tiles + kPartTiles;
+#pragma unroll
+      for (int e = 0; e < 2; ++e) {
+        const int c = (e ? c1 : c0) - unit;
+        if (c < 0 || c >= size * per_seq) continue;
+        int b = c / size, j = c - b * size - kPartTiles;   // block of the sequence, tiles in front of the cut
+        if (j < kLeastTiles) {
+          j = 0;
+        } else if (tiles - j < kLeastTiles) {
+          j = 0;
+          ++b;   // (a block's end is the next one's start)
+        }
+        ctl.ends[e] = at + b * tiles + j;
+        if (e == 0) {
+          Block f = {r, b / blocks, 0, len, tiles, at + b * tiles, index + b};
+          f.rb = b - f.h * blocks;
+          if (b == per_seq) {   // behind the sequence: the next one that is not empty, if there is one
+            f.r = -1 - r;
+          }
+          ctl.first = f;
+        }
       }
-      at += tiles * per_tile;
+      at += tiles * per_seq;
+      index += per_seq;
     }
+  } else if (threadIdx.x == 0) {
+    ctl.ends[0] = ctl.ends[1] = 0;
   }
   __syncthreads();
+  const int x0 = ctl.ends[0], x1 = ctl.ends[1];
+  const bool works = x0 < x1;
+  if (works && ctl.first.r < 0) {   // (for all threads)
+    __syncthreads();
+    if (threadIdx.x == 0) {
+      Block f = ctl.first;
+      f.r = -1 - f.r;
+      f.h = f.rb = 0;
+      do {
+        f.len = seq_len(P, ++f.r);
+        f.tiles = (f.len + kTileKeys - 1) / kTileKeys;
+      } while (f.tiles == 0);
+      ctl.first = f;
+    }
+    __syncthreads();
+  }
   const uint32_t tmem = ctl.tmem_base;
   const auto fail = [&]() {
     ctl.abort = 1;
@@ -367,14 +464,16 @@ cache_attend_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_const
         mbar_wait(&ctl.drain, 0, P.wait_limit_ns, &ctl.never);
       }
     }
-  } else if (warp == 2) {
+  } else if (warp < 4) {
     // ------------------------------------------------------------ query rows, a block ahead
-    // Two e4m3 pieces, K-major with the 128-byte swizzle: 4 elements a lane and row.
+    // Two e4m3 pieces, K-major with the 128-byte swizzle: 16 lanes a row, 8 elements each; four rows at once.
     if (works) {
       uint8_t* qbuf = smem + C::kQ;
-      if constexpr (2 * R < C::kNs)   // columns behind the pieces: zeros, once
-        for (int i = lane; i < (C::kNs - 2 * R) * kHeadDim / 4; i += 32)
+      const int sub = lane & 15, first_row = (warp - 2) * 2 + (lane >> 4);
+      if constexpr (2 * R < C::kNs) {   // columns behind the pieces: zeros, once
+        for (int i = threadIdx.x - 64; i < (C::kNs - 2 * R) * kHeadDim / 4; i += 64)
           for (int k = 0; k < 2; ++k) reinterpret_cast<uint32_t*>(qbuf + k * C::kQBytes + 2 * R * kHeadDim)[i] = 0;
+      }
       Block at = ctl.first;
       for (int part = 0;; ++part) {
         const int parity = part & 1;
@@ -382,57 +481,48 @@ cache_attend_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_const
           if (lane == 0) fail();
           break;
         }
-        long long src = -1;   // lane i: row i's
-        if (lane < R) {
-          const int row = at.rb * R + lane;
-          long long out_at = -1;
-          int lse_at = 0;
-          if (row < rows) {
-            const int t = row / P.c.group, hq = at.h * P.c.group + row - t * P.c.group;
-            const long long tok = static_cast<long long>(at.r) * P.q_tokens + t;
-            src = tok * P.q_st + hq * P.q_sh;
-            out_at = tok * P.o_st + hq * P.o_sh;
-            lse_at = static_cast<int>(tok * P.c.hq) + hq;
-            ctl.seen[parity][lane] = at.len - P.q_tokens + t + 1;
-          } else {
-            ctl.seen[parity][lane] = 0;
+        uint4 x[R / 4];
+#pragma unroll
+        for (int k = 0; k < R / 4; ++k) {
+          const int i = first_row + 4 * k, row = at.rb * R + i;
+          const int t = row / P.c.group, hq = at.h * P.c.group + row - t * P.c.group;
+          const long long tok = static_cast<long long>(at.r) * P.q_tokens + t;
+          x[k] = make_uint4(0, 0, 0, 0);
+          if (row < rows) x[k] = __ldg(reinterpret_cast<const uint4*>(P.q + tok * P.q_st + hq * P.q_sh) + sub);
+          if (sub == 0) {
+            ctl.seen[parity][i] = row < rows ? at.len - P.q_tokens + t + 1 : 0;
+            ctl.out_at[parity][i] = row < rows ? tok * P.o_st + hq * P.o_sh : -1;
+            ctl.lse_at[parity][i] = static_cast<int>(tok * P.c.hq) + hq;
           }
-          ctl.out_at[parity][lane] = out_at;
-          ctl.lse_at[parity][lane] = lse_at;
         }
-        constexpr int kBatch = R < 8 ? R : 8;
-#pragma unroll 1
-        for (int i0 = 0; i0 < R; i0 += kBatch) {
-          uint2 x[kBatch];
 #pragma unroll
-          for (int i = 0; i < kBatch; ++i) {
-            const long long from = __shfl_sync(0xffffffffu, src, i0 + i);
-            x[i] = make_uint2(0, 0);
-            if (from >= 0) x[i] = __ldg(reinterpret_cast<const uint2*>(P.q + from) + lane);
-          }
+        for (int k = 0; k < R / 4; ++k) {
+          const int i = first_row + 4 * k;
+          const uint32_t word[4] = {x[k].x, x[k].y, x[k].z, x[k].w};
+          uint32_t m = 0;
 #pragma unroll
-          for (int i = 0; i < kBatch; ++i) {
-            const uint32_t two = x[i].x & 0x7fff7fffu, two2 = x[i].y & 0x7fff7fffu;
-            const uint32_t m = __reduce_max_sync(
-                0xffffffffu, max(max(two & 0xffffu, two >> 16), max(two2 & 0xffffu, two2 >> 16)));
-            const bool finite = m < 0x7f80u;
-            const float scale = __uint_as_float(piece_scale(m));
-            const float a = __uint_as_float(x[i].x << 16) * scale, b = __uint_as_float(x[i].x & 0xffff0000u) * scale;
-            const float c = __uint_as_float(x[i].y << 16) * scale, d = __uint_as_float(x[i].y & 0xffff0000u) * scale;
-            const uint32_t ab = e4m3x2(a, b), cd = e4m3x2(c, d);
-            const float2 fab = e4m3x2_values(ab), fcd = e4m3x2_values(cd);
-            const uint32_t lo = e4m3x2((a - fab.x) * 16.f, (b - fab.y) * 16.f) |
-                                e4m3x2((c - fcd.x) * 16.f, (d - fcd.y) * 16.f) << 16;
-            const auto put = [&](int n, uint32_t v) {
-              *reinterpret_cast<uint32_t*>(qbuf + parity * C::kQBytes + n * kHeadDim + (((lane >> 2) ^ (n & 7)) << 4) +
-                                           ((lane & 3) << 2)) = v;
-            };
-            put(i0 + i, finite ? ab | cd << 16 : 0u);
-            put(R + i0 + i, finite ? lo : 0u);
-            // a row with an infinity or a NaN: every logit NaN
-            if (lane == 0)
-              ctl.qs[parity][i0 + i] = finite ? P.alpha * __frcp_rn(scale) : __uint_as_float(0x7fc00000u);
+          for (int j = 0; j < 4; ++j) m = max(m, max(word[j] & 0x7fffu, (word[j] >> 16) & 0x7fffu));
+#pragma unroll
+          for (int o = 8; o > 0; o >>= 1) m = max(m, __shfl_xor_sync(0xffffffffu, m, o));
+          const bool finite = m < 0x7f80u;
+          const float scale = __uint_as_float(piece_scale(m));
+          uint32_t hi[2] = {0, 0}, lo[2] = {0, 0};
+#pragma unroll
+          for (int j = 0; j < 4; ++j) {
+            const float a = __uint_as_float(word[j] << 16) * scale, b = __uint_as_float(word[j] & 0xffff0000u) * scale;
+            const uint32_t two = e4m3x2(a, b);
+            const float2 f = e4m3x2_values(two);
+            hi[j / 2] |= two << (16 * (j & 1));
+            lo[j / 2] |= e4m3x2((a - f.x) * 16.f, (b - f.y) * 16.f) << (16 * (j & 1));
           }
+          const auto put = [&](int n, const uint32_t* v) {
+            *reinterpret_cast<uint2*>(qbuf + parity * C::kQBytes + n * kHeadDim + (((sub >> 1) ^ (n & 7)) << 4) +
+                                      ((sub & 1) << 3)) = finite ? make_uint2(v[0], v[1]) : make_uint2(0, 0);
+          };
+          put(i, hi);
+          put(R + i, lo);
+          // a row with an infinity or a NaN: every logit NaN
+          if (sub == 0) ctl.qs[parity][i] = finite ? P.alpha * __frcp_rn(scale) : __uint_as_float(0x7fc00000u);
         }
         fence_proxy_async_smem();
         __syncwarp();
@@ -441,9 +531,8 @@ cache_attend_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_const
         next_block(P, blocks, at);
       }
     }
-  } else if (warp == 3) {
-    // ------------------------------------------------------------ sequences without a token: their rows are zeros
-    for (int r = blockIdx.x; r < P.n_seq; r += gridDim.x)
+    // sequences without a token: their rows are zeros
+    for (int r = blockIdx.x * 2 + warp - 2; r < P.n_seq; r += 2 * gridDim.x)
       if (seq_len(P, r) == 0)
         for (int i = 0; i < P.q_tokens * P.c.hq; ++i) {
           const int64_t tok = static_cast<int64_t>(r) * P.q_tokens + i / P.c.hq;
@@ -454,6 +543,7 @@ cache_attend_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_const
     // ------------------------------------------------------------ softmax: a token, then a column, a thread
     const int half = H == 1 ? 0 : (warp >> 2) - 1, quad = warp & 3;
     const int tid = quad * 32 + lane, i0 = half * N;     // this thread's rows are i0 .. i0 + N - 1 of the block
+    constexpr int kPartWords = N * (kHeadDim + 2);       // of a part: these rows, their maxima and sums
     const uint32_t my_lanes = static_cast<uint32_t>(quad) << 21;
     uint8_t* pbuf = smem + C::kP;
     uint32_t met = 0;
@@ -670,15 +760,16 @@ cache_attend_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_const
           if (P.lse && tid == i) P.lse[ctl.lse_at[part & 1][i0 + i]] = log_sum(m[i], l[i]);
         }
       } else {
-        // one of several parts of the block: left for the join. Slot 0 is a part that starts where its CTA
-        // does, slot 1 a later one
-        float* dst = P.partial + (static_cast<int64_t>(blockIdx.x) * 2 + (part0 != x0)) * kAttendPartWords;
+        // one of several parts of the block: left for the join. Slot 1 of the CTA is for a block's first part
+        // (its own last one), slot 0 for a later one (its own first)
+        float* dst = P.partial + (static_cast<int64_t>(blockIdx.x) * 2 + (part0 == at.first)) * kAttendPartWords +
+                     half * kPartWords;
 #pragma unroll
         for (int i = 0; i < N; ++i) {
-          __stcg(dst + (i0 + i) * kHeadDim + tid, acc[i]);
+          __stcg(dst + i * kHeadDim + tid, acc[i]);
           if (tid == i) {
-            __stcg(dst + R * kHeadDim + i0 + i, m[i]);
-            __stcg(dst + R * kHeadDim + R + i0 + i, l[i]);
+            __stcg(dst + N * kHeadDim + i, m[i]);
+            __stcg(dst + N * kHeadDim + N + i, l[i]);
           }
         }
         if (tid == 0) ctl.split[2 * half + splits] = at;
@@ -697,80 +788,95 @@ cache_attend_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_const
     // ------------------------------------------------------------ the join of blocks that several CTAs had parts of
     // Counted once this CTA's share is done (a fence under the loads of a running share takes 5 us), by the
     // first CTA that has a part of the block; the CTA that counts last joins.
+    allow_next_kernel();
     if (ok && splits > 0) {
-      const auto cta_of = [&](int tile) {   // whose share tile is in
-        int w = min(static_cast<int>(static_cast<float>(tile) * static_cast<float>(ctas) / static_cast<float>(total)),
-                    ctas - 1);
-        while (w > 0 && share(w) > tile) --w;
-        while (w + 1 < ctas && share(w + 1) <= tile) ++w;
-        return w;
-      };
-      __threadfence();
+      int w0 = 0, w1 = 0;
+      if (tid < splits) cuts.parts(ctl.split[2 * half + tid], &w0, &w1);
       meet_arrive();
       ok = meet_wait();
-      if (ok && tid < splits) {
-        const Block b = ctl.split[2 * half + tid];
-        const int w0 = cta_of(b.first), parts = cta_of(b.first + b.tiles - 1) - w0;
-        __threadfence();
-        ctl.last[2 * half + tid] = atomicInc(P.arrive + w0 * H + half, static_cast<unsigned>(parts)) == static_cast<unsigned>(parts);
-      }
+      if (ok && tid < splits)
+        ctl.last[2 * half + tid] =
+            inc_acq_rel_gpu(P.arrive + w0 * H + half, static_cast<unsigned>(w1 - w0)) == static_cast<unsigned>(w1 - w0)
+                ? w1 - w0 + 1 : 0;
+      if (tid < splits) ctl.split_cta[2 * half + tid] = w0;
       if (ok) {
         meet_arrive();
         ok = meet_wait();
       }
+      // The parts are brought into the tiles' memory (nothing else uses it now: this CTA's tiles are done),
+      // kBatch at a time; then a warp a row, four columns a lane, every sum in the order of the tokens.
+      constexpr int kBatch = C::kQ / H / (kPartWords * 4);
+      float* buf = reinterpret_cast<float*>(smem) + half * (C::kQ / H / 4);
+      uint32_t copied = 0;
       for (int k = 0; ok && k < splits; ++k) {
-        if (!ctl.last[2 * half + k]) continue;
-        __threadfence();
+        const int parts = ctl.last[2 * half + k];
+        if (parts == 0) continue;
         const Block b = ctl.split[2 * half + k];
-        const int w0 = cta_of(b.first), w1 = cta_of(b.first + b.tiles - 1);
-        const int w0_slot = share(w0) != b.first;
-        const auto slot = [&](int w) {
-          return P.partial + (static_cast<int64_t>(w) * 2 + (w == w0 ? w0_slot : 0)) * kAttendPartWords;
-        };
-        // a warp a row, four columns a lane, kJoin parts in flight; every sum in the order of the tokens
-        constexpr int kJoin = 8;
-        for (int i = i0 + quad; i < i0 + N; i += 4) {
-          const int row = b.rb * R + i;
-          if (row >= rows) break;
-          float top = -INFINITY, sum = 0.f;
-          float4 a4 = make_float4(0.f, 0.f, 0.f, 0.f);
-          for (int wb = w0; wb <= w1; wb += kJoin) {
-            float4 o[kJoin];
-            float pm = -INFINITY, pl = 0.f;
-            if (lane < kJoin && wb + lane <= w1) {
-              const float* src = slot(wb + lane) + R * kHeadDim + i;
-              pm = __ldcg(src);
-              pl = __ldcg(src + R);
-            }
+        const int first = ctl.split_cta[2 * half + k];
+        float top[N / 4], sum[N / 4];
+        float4 a4[N / 4];
 #pragma unroll
-            for (int j = 0; j < kJoin; ++j)
-              if (wb + j <= w1) o[j] = __ldcg(reinterpret_cast<const float4*>(slot(wb + j) + i * kHeadDim) + lane);
-            const float mn = fmaxf(top, warp_max(pm)), ref = mn == -INFINITY ? 0.f : mn;
-            const float f0 = ex2(top - ref), f = ex2(pm - ref);
-            top = mn;
-            sum *= f0;
-            a4.x *= f0, a4.y *= f0, a4.z *= f0, a4.w *= f0;
-            pl *= f;
+        for (int i = 0; i < N / 4; ++i) {
+          top[i] = -INFINITY;
+          sum[i] = 0.f;
+          a4[i] = make_float4(0.f, 0.f, 0.f, 0.f);
+        }
+        for (int p0 = 0; ok && p0 < parts; p0 += kBatch) {
+          const int count = min(parts - p0, kBatch);
+          if (quad == 0) {
+            fence_proxy_async();   // the others' stores, and our reads of the batch before, then the copies
+            if (lane == 0) mbar_arrive_expect_tx(&ctl.joined[half], count * (kPartWords * 4));
+            __syncwarp();
+            for (int j = lane; j < count; j += 32)   // part p: slot 0 of CTA first + p, of the first one slot 1
+              bulk_load(buf + j * kPartWords,
+                        P.partial + (static_cast<int64_t>(first + p0 + j) * 2 + (p0 + j == 0)) * kAttendPartWords +
+                            half * kPartWords,
+                        kPartWords * 4, &ctl.joined[half]);
+          }
+          ok = warp_wait(&ctl.joined[half], copied & 1u, P.wait_limit_ns, &ctl.abort);
+          if (!ok) {
+            if (lane == 0) mbar_wait(&ctl.joined[half], copied & 1u, P.wait_limit_ns, &ctl.never);   // (in flight)
+            break;
+          }
+          ++copied;
 #pragma unroll
-            for (int j = 0; j < kJoin; ++j) {
-              const float g = __shfl_sync(0xffffffffu, f, j), s = __shfl_sync(0xffffffffu, pl, j);
-              if (wb + j <= w1) {
-                sum += s;
-                a4.x = fmaf(o[j].x, g, a4.x);
-                a4.y = fmaf(o[j].y, g, a4.y);
-                a4.z = fmaf(o[j].z, g, a4.z);
-                a4.w = fmaf(o[j].w, g, a4.w);
-              }
+          for (int i = 0; i < N / 4; ++i) {
+            const float* row = buf + (quad + 4 * i) * kHeadDim;
+            const float* stats = buf + N * kHeadDim + quad + 4 * i;
+            float mn = top[i];
+            for (int j = lane; j < count; j += 32) mn = fmaxf(mn, stats[j * kPartWords]);
+            mn = warp_max(mn);
+            const float ref = mn == -INFINITY ? 0.f : mn, f0 = ex2(top[i] - ref);
+            top[i] = mn;
+            sum[i] *= f0;
+            a4[i].x *= f0, a4[i].y *= f0, a4[i].z *= f0, a4[i].w *= f0;
+#pragma unroll 4
+            for (int j = 0; j < count; ++j) {
+              const float g = ex2(stats[j * kPartWords] - ref);
+              const float4 o = reinterpret_cast<const float4*>(row + j * kPartWords)[lane];
+              sum[i] = fmaf(stats[j * kPartWords + N], g, sum[i]);
+              a4[i].x = fmaf(o.x, g, a4[i].x);
+              a4[i].y = fmaf(o.y, g, a4[i].y);
+              a4[i].z = fmaf(o.z, g, a4[i].z);
+              a4[i].w = fmaf(o.w, g, a4[i].w);
             }
           }
+          meet_arrive();
+          ok = meet_wait();   // the batch has been read
+        }
+        if (!ok) break;
+#pragma unroll
+        for (int i = 0; i < N / 4; ++i) {
+          const int row = b.rb * R + i0 + quad + 4 * i;
+          if (row >= rows) break;
           const int t = row / P.c.group, hq = b.h * P.c.group + row - t * P.c.group;
           const int64_t tok = static_cast<int64_t>(b.r) * P.q_tokens + t;
-          const float inv = sum == 0.f ? 0.f : __frcp_rn(sum);
+          const float inv = sum[i] == 0.f ? 0.f : __frcp_rn(sum[i]);
           uint2 v;
-          v.x = to_bf16(a4.x * inv) | static_cast<uint32_t>(to_bf16(a4.y * inv)) << 16;
-          v.y = to_bf16(a4.z * inv) | static_cast<uint32_t>(to_bf16(a4.w * inv)) << 16;
+          v.x = to_bf16(a4[i].x * inv) | static_cast<uint32_t>(to_bf16(a4[i].y * inv)) << 16;
+          v.y = to_bf16(a4[i].z * inv) | static_cast<uint32_t>(to_bf16(a4[i].w * inv)) << 16;
           reinterpret_cast<uint2*>(P.out + tok * P.o_st + hq * P.o_sh)[lane] = v;
-          if (P.lse && lane == 0) P.lse[tok * P.c.hq + hq] = log_sum(top, sum);
+          if (P.lse && lane == 0) P.lse[tok * P.c.hq + hq] = log_sum(top[i], sum[i]);
         }
       }
     }

@@ -339,6 +339,12 @@ __device__ __forceinline__ void wait_previous_kernel() {
   asm volatile("griddepcontrol.wait;" ::: "memory");
 }
 
+// Lets the next launch on the stream be scheduled from here on, once every CTA has come here or ended
+// (it still waits for this kernel's end in wait_previous_kernel).
+__device__ __forceinline__ void allow_next_kernel() {
+  asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
+}
+
 // Launch `fn` on `stream` after the previous kernel of the stream, overlapping its
 // launch with that kernel's tail (programmatic stream serialization).
 template <class... KArgs, class... Args>
