@@ -68,12 +68,13 @@ struct ACtl {
   uint64_t p_full, o_full, meet[H], joined[H], drain;
   float ks[kVStages][kMostTilePages], vs[kVStages][kMostTilePages];
   uint32_t pages[kVStages];                    // bit j: page j of the tile holds tokens
-  float red[2][4][R];                          // row maxima of the warps, by tile parity
-  float sum[4][R];                             // row sums of the warps, at the end of a part
+  alignas(16) float red[2][4][R];              // row maxima of the warps, by tile parity
+  // of each warp's rows: the maximum, exp(old maximum - new); at the end of a part (x) the warp's row sums
+  alignas(16) float2 ref[4 * H][R / H];
   // of a part's rows, by part parity: log2(e) / sqrt(d) / the power of two in the q pieces; tokens that the
   // row sees; where its output goes (elements of out, of lse), -1 for no row
-  float qs[2][R];
-  int seen[2][R];
+  alignas(16) float qs[2][R];
+  alignas(16) int seen[2][R];
   long long out_at[2][R];
   int lse_at[2][R];
   uint8_t nan_from[2][kHeadDim];               // by part parity: see there
@@ -112,19 +113,21 @@ __device__ __forceinline__ void next_block(const AttendParams& P, int blocks, Bl
 // How the line is cut. A part costs about kPartTiles tiles besides its own (its query rows, the tensor
 // cores' latency at its two ends, its output), so a block counts as its tiles and kPartTiles more units, and
 // the units are dealt evenly: CTA w's raw cut is floor(units * w / ctas). A cut that would leave fewer than
-// kLeastTiles tiles of a block on one of its sides moves to that end of the block: a join costs more than
-// those tiles do.
-// No more CTAs take part than have kLeastUnits each, or a block.
-constexpr int kPartTiles = 2, kLeastTiles = 4, kLeastUnits = 4;
+// `least` tiles of a block on one of its sides moves to that end of the block: a join costs more than those
+// tiles do. That is 4 tiles where a share is 8 units at most and 2 where it is longer and evenness counts
+// for more: 16 sequences of 96 to 700 tokens take 9.0 us with 4 against 10.0 with 2 and 11.3 with 1, 24 of
+// 500 to 8192 with 4 drafts each (share 16) 40.1 with 4 against 37.1 with 2 and with 1. No more CTAs take part than have kLeastUnits each, or a block.
+constexpr int kPartTiles = 2, kLeastUnits = 4;
 
 struct Cuts {
-  int each, rest, ctas, units;
+  int each, rest, ctas, units, least;
   uint32_t inverse;   // of ctas, 2^32 / ctas rounded up: exact for the products below ctas^2 that it divides
   __device__ __forceinline__ void set(int n, int w) {
     units = n;
     ctas = w;
     each = n / w;
     rest = n - each * w;
+    least = each <= 8 ? 4 : 2;
     inverse = 0xffffffffu / static_cast<uint32_t>(w) + 1u;   // (for one CTA 0, and rest is 0)
   }
   __device__ __forceinline__ int raw(int w) const {
@@ -140,8 +143,8 @@ struct Cuts {
   // CTAs [*w0, *w1] have the parts of block b
   __device__ __forceinline__ void parts(const Block& b, int* w0, int* w1) const {
     const int a = b.first + (b.index + 1) * kPartTiles;   // its tile 0 in units
-    *w0 = from(a + kLeastTiles) - 1;
-    *w1 = from(a + b.tiles - kLeastTiles + 1) - 1;
+    *w0 = from(a + least) - 1;
+    *w1 = from(a + b.tiles - least + 1) - 1;
   }
 };
 
@@ -167,6 +170,26 @@ __device__ __forceinline__ float2 e4m3x2_values(uint32_t two) {
   return f;
 }
 
+// Three e4m3 pieces of two values of at most 256: x = hi + mid / 16 + lo / 256, each pair in 16 bits. The
+// values are rounded to f16 first (2^-12 of them; below 2^-14 an absolute 2^-25), whose 11 bits three
+// pieces of 4 hold, so that the rest is exact in packed f16.
+__device__ __forceinline__ void e4m3_pieces(float lo, float hi, uint32_t (&piece)[3]) {
+  uint32_t x;
+  asm("cvt.rn.f16x2.f32 %0, %1, %2;" : "=r"(x) : "f"(hi), "f"(lo));
+#pragma unroll
+  for (int k = 0; k < 3; ++k) {
+    uint16_t c;
+    asm("cvt.rn.satfinite.e4m3x2.f16x2 %0, %1;" : "=h"(c) : "r"(x));
+    piece[k] = c;
+    if (k == 2) break;
+    uint32_t v;
+    asm("cvt.rn.f16x2.e4m3x2 %0, %1;" : "=r"(v) : "h"(c));
+    asm("{\n .reg .b32 d;\n sub.rn.f16x2 d, %1, %2;\n mul.rn.f16x2 %0, d, %3;\n}"
+        : "=r"(x)
+        : "r"(x), "r"(v), "r"(0x4c004c00u));   // 16
+  }
+}
+
 __device__ __forceinline__ uint16_t to_bf16(float x) {
   uint16_t d;
   asm("cvt.rn.bf16.f32 %0, %1;" : "=h"(d) : "f"(x));
@@ -177,6 +200,8 @@ __device__ __forceinline__ uint16_t to_bf16(float x) {
 __device__ __forceinline__ float log_sum(float top, float sum) {
   return sum == 0.f ? -INFINITY : ((top == -INFINITY ? 0.f : top) + lg2(sum)) * 0.69314718056f;
 }
+
+static_assert(attend_smem<16, 2>() <= 113 * 1024 && attend_smem<8, 1>() <= 113 * 1024, "two CTAs an SM");
 
 template <int R, int H>
 __global__ void __launch_bounds__(ACfg<R, H>::kThreads, kAttendCtas)
@@ -289,9 +314,9 @@ cache_attend_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_const
         const int c = (e ? c1 : c0) - unit;
         if (c < 0 || c >= size * per_seq) continue;
         int b = c / size, j = c - b * size - kPartTiles;   // block of the sequence, tiles in front of the cut
-        if (j < kLeastTiles) {
+        if (j < cuts.least) {
           j = 0;
-        } else if (tiles - j < kLeastTiles) {
+        } else if (tiles - j < cuts.least) {
           j = 0;
           ++b;   // (a block's end is the next one's start)
         }
@@ -559,7 +584,8 @@ cache_attend_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_const
     const int n = x1 - x0;
     int part = 0, part0 = x0, splits = 0;
     bool ok = true;
-    float m[N], l[N], acc[N], keep[N];   // keep: exp(old maximum - new) of the last tile
+    float m = -INFINITY;                 // lane i: row i's maximum so far
+    float l[N], acc[N], keep[N];         // keep: exp(old maximum - new) of the last tile
     float back = 0.f;                    // the last tile's scale of O^T
     // adds tile `it`'s O^T
     const auto take = [&](int it) -> bool {
@@ -583,10 +609,8 @@ cache_attend_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_const
     };
     const auto begin = [&]() -> bool {
 #pragma unroll
-      for (int i = 0; i < N; ++i) {
-        m[i] = -INFINITY;
-        l[i] = acc[i] = 0.f;
-      }
+      for (int i = 0; i < N; ++i) l[i] = acc[i] = 0.f;
+      m = -INFINITY;
       if (half == 0) ctl.nan_from[part & 1][tid] = kNoNan;
       return warp_wait(&ctl.q_full[part & 1], (part >> 1) & 1, P.wait_limit_ns, &ctl.abort);
     };
@@ -625,10 +649,15 @@ cache_attend_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_const
         }
         tmem_wait_ld(s);
 #pragma unroll
-        for (int i = 0; i < N; ++i) {
-          const float y = fmaf(s[N + i], 0.0625f, s[i]) * ctl.qs[part & 1][i0 + i] * ks;
-          w[i] = held && pos < ctl.seen[part & 1][i0 + i] ? y : -INFINITY;
-        }
+        for (int i = 0; i < N; ++i) w[i] = fmaf(s[N + i], 0.0625f, s[i]) * ctl.qs[part & 1][i0 + i] * ks;
+      }
+      const int tile0 = pos - tid, tile_end = tile0 + kTileKeys;
+      const bool whole = have == (0xffu >> (kMostTilePages - (kTileKeys >> P.c.page_shift))) && tile_end <= at.len;
+      const bool some = P.q_tokens > 1 && tile_end > at.len - P.q_tokens + 1;   // tokens that not all rows see
+      if (!whole || some) {
+#pragma unroll
+        for (int i = 0; i < N; ++i)
+          if (!held || pos >= ctl.seen[part & 1][i0 + i]) w[i] = -INFINITY;
       }
       float* red = &ctl.red[it & 1][quad][i0];
 #pragma unroll
@@ -647,34 +676,38 @@ cache_attend_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_const
         break;
       }
       back = vtop * (1.f / 256.f);
+      if (lane < N) {   // lane i: row i's maximum
+        const float top = fmaxf(fmaxf(ctl.red[it & 1][0][i0 + lane], ctl.red[it & 1][1][i0 + lane]),
+                                fmaxf(ctl.red[it & 1][2][i0 + lane], ctl.red[it & 1][3][i0 + lane]));
+        const float mn = fmaxf(m, top), ref = mn == -INFINITY ? 0.f : mn;
+        ctl.ref[half * 4 + quad][lane] = make_float2(ref, ex2(m - ref));
+        m = mn;
+      }
+      __syncwarp();
 #pragma unroll
       for (int i = 0; i < N; ++i) {
-        const float top = fmaxf(fmaxf(ctl.red[it & 1][0][i0 + i], ctl.red[it & 1][1][i0 + i]),
-                                fmaxf(ctl.red[it & 1][2][i0 + i], ctl.red[it & 1][3][i0 + i]));
-        const float mn = fmaxf(m[i], top), ref = mn == -INFINITY ? 0.f : mn;
-        keep[i] = ex2(m[i] - ref);
-        m[i] = mn;
-        const float p = ex2(w[i] - ref);
-        l[i] = fmaf(l[i], keep[i], p);
-        w[i] = w[i] == -INFINITY ? 0.f : p * vrest;
+        const float2 r = ctl.ref[half * 4 + quad][i];
+        const float p = ex2(w[i] - r.x);
+        keep[i] = r.y;
+        l[i] = fmaf(l[i], r.y, p);
+        w[i] = p * vrest;
+      }
+      if (!whole || some) {   // (a scale that is NaN, of tokens that a row does not see)
+#pragma unroll
+        for (int i = 0; i < N; ++i)
+          if (!held || pos >= ctl.seen[part & 1][i0 + i]) w[i] = 0.f;
       }
       // three e4m3 pieces of each probability: column k R + i of the token's row
       uint32_t out[up16(3 * N) / 4];
 #pragma unroll
       for (int i = 0; i < up16(3 * N) / 4; ++i) out[i] = 0;
 #pragma unroll
-      for (int i = 0; i < N; i += 2) {
-        float a = w[i], b = w[i + 1];
+      for (int i = 0; i < N; i += 4) {
+        uint32_t a[3], b[3];
+        e4m3_pieces(w[i], w[i + 1], a);
+        e4m3_pieces(w[i + 2], w[i + 3], b);
 #pragma unroll
-        for (int k = 0; k < 3; ++k) {
-          const uint32_t two = e4m3x2(a, b);
-          out[(k * N + i) / 4] |= two << (8 * ((k * N + i) % 4));
-          if (k < 2) {
-            const float2 f = e4m3x2_values(two);
-            a = (a - f.x) * 16.f;
-            b = (b - f.y) * 16.f;
-          }
-        }
+        for (int k = 0; k < 3; ++k) out[(k * N + i) / 4] = __byte_perm(a[k], b[k], 0x5410);
       }
       if constexpr (H == 1) {
 #pragma unroll
@@ -688,9 +721,6 @@ cache_attend_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_const
           *reinterpret_cast<uint2*>(pbuf + k * (16 * kTileKeys) + tid * 16 + half * 8) =
               make_uint2(out[2 * k], out[2 * k + 1]);
       }
-      const int tile0 = pos - tid, tile_end = tile0 + kTileKeys;
-      const bool whole = have == (0xffu >> (kMostTilePages - (kTileKeys >> P.c.page_shift))) && tile_end <= at.len;
-      const bool some = P.q_tokens > 1 && tile_end > at.len - P.q_tokens + 1;
       if (half == 0 && (!whole || some)) {
         if (!warp_wait(&ctl.v_full[st], (it / kVStages) & 1, P.wait_limit_ns, &ctl.abort)) {
           ok = false;
@@ -736,41 +766,54 @@ cache_attend_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_const
         for (int i = 0; i < N; ++i)
           if (ctl.seen[part & 1][i0 + i] > from) acc[i] = __uint_as_float(0x7fc00000u);
       }
-      // row sums over the tokens' threads
+      // row sums over the tokens' threads: each step halves the rows that a lane has, then the lanes
+      {
+        int row = 0;
 #pragma unroll
-      for (int i = 0; i < N; ++i) {
+        for (int o = 16, c = N / 2; o > 0; o >>= 1, c >>= 1) {
+          const bool up = lane & o;
+          if (c > 0) {
 #pragma unroll
-        for (int o = 16; o > 0; o >>= 1) l[i] += __shfl_xor_sync(0xffffffffu, l[i], o);
-        if (lane == i) ctl.sum[quad][i0 + i] = l[i];
+            for (int i = 0; i < c; ++i) {
+              const float other = __shfl_xor_sync(0xffffffffu, up ? l[i] : l[i + c], o);
+              l[i] = (up ? l[i + c] : l[i]) + other;
+            }
+            row += up ? c : 0;
+          } else {
+            l[0] += __shfl_xor_sync(0xffffffffu, l[0], o);
+          }
+        }
+        if (lane % (32 / N) == 0) ctl.ref[half * 4 + quad][row].x = l[0];
       }
       meet_arrive();
       if (!meet_wait()) {
         ok = false;
         break;
       }
-#pragma unroll
-      for (int i = 0; i < N; ++i)
-        l[i] = (ctl.sum[0][i0 + i] + ctl.sum[1][i0 + i]) + (ctl.sum[2][i0 + i] + ctl.sum[3][i0 + i]);
+      float sum = 0.f;   // lane i: row i's
+      if (lane < N)
+        sum = (ctl.ref[half * 4][lane].x + ctl.ref[half * 4 + 1][lane].x) +
+              (ctl.ref[half * 4 + 2][lane].x + ctl.ref[half * 4 + 3][lane].x);
       if (part0 == at.first && x + 1 == at.first + at.tiles) {
+        const float inv = sum == 0.f ? 0.f : __frcp_rn(sum);
 #pragma unroll
         for (int i = 0; i < N; ++i) {
           const long long to = ctl.out_at[part & 1][i0 + i];
-          if (to < 0) continue;
-          P.out[to + tid] = l[i] == 0.f ? 0 : to_bf16(acc[i] * __frcp_rn(l[i]));
-          if (P.lse && tid == i) P.lse[ctl.lse_at[part & 1][i0 + i]] = log_sum(m[i], l[i]);
+          const float f = __shfl_sync(0xffffffffu, inv, i);
+          if (to >= 0) P.out[to + tid] = to_bf16(acc[i] * f);
         }
+        if (P.lse && quad == 0 && lane < N && ctl.out_at[part & 1][i0 + lane] >= 0)
+          P.lse[ctl.lse_at[part & 1][i0 + lane]] = log_sum(m, sum);
       } else {
         // one of several parts of the block: left for the join. Slot 1 of the CTA is for a block's first part
         // (its own last one), slot 0 for a later one (its own first)
         float* dst = P.partial + (static_cast<int64_t>(blockIdx.x) * 2 + (part0 == at.first)) * kAttendPartWords +
                      half * kPartWords;
 #pragma unroll
-        for (int i = 0; i < N; ++i) {
-          __stcg(dst + i * kHeadDim + tid, acc[i]);
-          if (tid == i) {
-            __stcg(dst + N * kHeadDim + i, m[i]);
-            __stcg(dst + N * kHeadDim + N + i, l[i]);
-          }
+        for (int i = 0; i < N; ++i) __stcg(dst + i * kHeadDim + tid, acc[i]);
+        if (quad == 0 && lane < N) {
+          __stcg(dst + N * kHeadDim + lane, m);
+          __stcg(dst + N * kHeadDim + N + lane, sum);
         }
         if (tid == 0) ctl.split[2 * half + splits] = at;
         ++splits;
@@ -894,7 +937,6 @@ cache_attend_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_const
 template <int R, int H>
 cudaError_t attend_rows(const kve_cache& c, const AttendParams& p, cudaStream_t stream) {
   constexpr size_t smem = attend_smem<R, H>();
-  static_assert(smem <= 113 * 1024, "two CTAs an SM");
   auto* fn = cache_attend_kernel<R, H>;
   cudaError_t e = cudaFuncSetAttribute(fn, cudaFuncAttributeMaxDynamicSharedMemorySize, static_cast<int>(smem));
   if (e != cudaSuccess) return e;
