@@ -82,7 +82,7 @@ struct ACtl {
   int last[2 * H], split_cta[2 * H];           // its parts, if they are all written; the CTA of the first
   Block first;                                 // the first part's block
   int ends[2];                                 // this CTA's tiles of the line
-  unsigned long long sums[ACfg<R, H>::kThreads / 32][2];
+  int2 sums[ACfg<R, H>::kThreads / 32];        // tiles, sequences that have some
   uint32_t tmem_base;
   int abort, never;                            // never: stays 0 (waits that a given-up call still has to make)
 };
@@ -212,6 +212,10 @@ cache_attend_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_const
   extern __shared__ __align__(1024) uint8_t smem[];   // the tiles' swizzle counts from 1024 bytes
   ACtl<R, H>& ctl = *reinterpret_cast<ACtl<R, H>*>(smem + C::kCtl);
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+  // row / group, for groups that are no power of two as for those that are
+  const auto row_token = [&](int row) {
+    return P.group_inverse ? static_cast<int>(__umulhi(static_cast<uint32_t>(row), P.group_inverse)) : row;
+  };
   const int rows = P.q_tokens * P.c.group;
   const int blocks = (rows + R - 1) / R;
   if (threadIdx.x == 0) {
@@ -246,13 +250,12 @@ cache_attend_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_const
   const int cap = P.c.max_pages << P.c.page_shift;
   const int per = (P.n_seq + kThreads - 1) / kThreads;
   const int s0 = min(static_cast<int>(threadIdx.x) * per, P.n_seq), s1 = min(s0 + per, P.n_seq);
-  long long mine = 0;
-  int filled = 0;
+  int mine = 0, filled = 0;   // tiles of one block each (2^30: too many), sequences that have some
   bool bad = false;
   for (int r = s0; r < s1; ++r) {
     const int len = __ldg(P.lens + r);
     bad |= len < 0 || len > cap;
-    mine += (min(max(len, 0), cap) + kTileKeys - 1) / kTileKeys;
+    mine = min(mine + (min(max(len, 0), cap) + kTileKeys - 1) / kTileKeys, 1 << 30);
     filled += len > 0;
   }
   if (warp == 1) {
@@ -260,42 +263,35 @@ cache_attend_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_const
     tmem_relinquish();
   }
   const int per_seq = P.c.heads * blocks;   // blocks of a sequence
-  long long front = mine;   // tiles of one block each, up to and with this thread's sequences; those sequences
-  int front_filled = filled;
+  int front = mine, front_filled = filled;  // up to and with this thread's sequences
 #pragma unroll
   for (int o = 1; o < 32; o <<= 1) {
-    const long long x = __shfl_up_sync(0xffffffffu, front, o);
-    const int y = __shfl_up_sync(0xffffffffu, front_filled, o);
+    const int x = __shfl_up_sync(0xffffffffu, front, o), y = __shfl_up_sync(0xffffffffu, front_filled, o);
     if (lane >= o) {
-      front += x;
+      front = min(front + x, 1 << 30);
       front_filled += y;
     }
   }
-  if (lane == 31) {
-    ctl.sums[warp][0] = static_cast<unsigned long long>(front);
-    ctl.sums[warp][1] = static_cast<unsigned long long>(front_filled);
-  }
+  if (lane == 31) ctl.sums[warp] = make_int2(front, front_filled);
   tc_fence_before();
   __syncthreads();
   tc_fence_after();
-  long long all_tiles = 0;
-  int all_filled = 0;
+  int all_tiles = 0, all_filled = 0;
 #pragma unroll
   for (int w = 0; w < kThreads / 32; ++w) {
-    const long long x = static_cast<long long>(ctl.sums[w][0]);
-    const int y = static_cast<int>(ctl.sums[w][1]);
+    const int2 x = ctl.sums[w];
     if (w < warp) {
-      front += x;
-      front_filled += y;
+      front = min(front + x.x, 1 << 30);
+      front_filled += x.y;
     }
-    all_tiles += x;
-    all_filled += y;
+    all_tiles = min(all_tiles + x.x, 1 << 30);
+    all_filled += x.y;
   }
   front -= mine;
   front_filled -= filled;
-  const long long all_units = (all_tiles + static_cast<long long>(all_filled) * kPartTiles) * per_seq;
-  // (tiles of 32 KB each: a line of 2^31 of them is no call that ends)
-  const bool too_long = all_units >= (1ll << 31);
+  // (tiles of 32 KB each: a line of 2^30 of them is no call that ends)
+  const long long all_units = (static_cast<long long>(all_tiles) + all_filled * kPartTiles) * per_seq;
+  const bool too_long = all_tiles >= 1 << 30 || all_units >= 1 << 30;
   if ((bad || too_long) && blockIdx.x == 0) atomicOr(P.err, kErrCheck);
   Cuts cuts;
   const int units = too_long ? 0 : static_cast<int>(all_units);
@@ -303,8 +299,8 @@ cache_attend_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_const
   if (cuts.units > 0 && static_cast<int>(blockIdx.x) < cuts.ctas) {
     // the thread that holds a cut's sequence says which tile of the line it is
     const int c0 = cuts.raw(blockIdx.x), c1 = cuts.raw(blockIdx.x + 1);
-    int at = static_cast<int>(front) * per_seq, index = front_filled * per_seq;   // tiles, blocks in front
-    if (threadIdx.x == 0 && c1 == cuts.units) ctl.ends[1] = static_cast<int>(all_tiles) * per_seq;
+    int at = front * per_seq, index = front_filled * per_seq;   // tiles, blocks in front
+    if (threadIdx.x == 0 && c1 == cuts.units) ctl.ends[1] = all_tiles * per_seq;
     for (int r = s0; r < s1; ++r) {
       const int len = seq_len(P, r), tiles = (len + kTileKeys - 1) / kTileKeys;
       if (tiles == 0) continue;
@@ -510,7 +506,7 @@ cache_attend_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_const
 #pragma unroll
         for (int k = 0; k < R / 4; ++k) {
           const int i = first_row + 4 * k, row = at.rb * R + i;
-          const int t = row / P.c.group, hq = at.h * P.c.group + row - t * P.c.group;
+          const int t = row_token(row), hq = at.h * P.c.group + row - t * P.c.group;
           const long long tok = static_cast<long long>(at.r) * P.q_tokens + t;
           x[k] = make_uint4(0, 0, 0, 0);
           if (row < rows) x[k] = __ldg(reinterpret_cast<const uint4*>(P.q + tok * P.q_st + hq * P.q_sh) + sub);
@@ -912,7 +908,7 @@ cache_attend_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_const
         for (int i = 0; i < N / 4; ++i) {
           const int row = b.rb * R + i0 + quad + 4 * i;
           if (row >= rows) break;
-          const int t = row / P.c.group, hq = b.h * P.c.group + row - t * P.c.group;
+          const int t = row_token(row), hq = b.h * P.c.group + row - t * P.c.group;
           const int64_t tok = static_cast<int64_t>(b.r) * P.q_tokens + t;
           const float inv = sum[i] == 0.f ? 0.f : __frcp_rn(sum[i]);
           uint2 v;

@@ -690,6 +690,7 @@ kve_status kv_evict_cache_attend(const kve_cache* cache, int32_t layer, int32_t 
   p.n_seq = n_seq;
   p.q_tokens = q_tokens;
   p.alpha = static_cast<float>(1.4426950408889634 / std::sqrt(static_cast<double>(kHeadDim)));
+  p.group_inverse = 0xffffffffu / static_cast<uint32_t>(c.group) + 1u;
   p.q = q;
   p.out = out;
   p.lse = lse;

@@ -291,6 +291,7 @@ struct AttendParams {
   CacheGeometry c;
   int32_t n_seq, q_tokens;
   float alpha;           // log2(e) / sqrt(d)
+  uint32_t group_inverse;  // 2^32 / group rounded up (0 for 1): row / group by a product, rows < 2^16
   const uint16_t* q;
   int64_t q_st, q_sh;    // element strides of tokens and heads
   uint16_t* out;
