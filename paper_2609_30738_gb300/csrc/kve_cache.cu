@@ -36,129 +36,119 @@ __device__ __forceinline__ int ring_at(int head, long long i, int n) {
   return static_cast<int>(p);
 }
 
-// Every CTA sums the pages that all sequences take and give (so all agree whether the call can be
-// done, before one of them writes) and those of the sequences in front of its own eight, a warp each;
-// blockIdx.y deals a sequence's pages and slots to more than one warp where they are long. What the
-// call changes in place (lens_out, ring_out may be inputs) is written by the CTA that finishes
-// reading last.
+// A warp takes a sequence, in chunks of 32 pages (a lane a page) that blockIdx.y deals to more than one
+// warp where sequences are long; a chunk's pages are read in one access, and 32 slots at a time leave from
+// registers, so new pages cost their 8 bytes and slots their 4. Every CTA first sums the pages and tokens that
+// each layer takes and gives (a warp a layer): all agree whether the call can be done before one of them
+// writes, and every warp finds its place in the ring and in its layer's slots. What the call changes in
+// place (lens_out, ring_out may be inputs) is written by the CTA that finishes reading last.
 //
-// Nothing here is bound by bandwidth at a decode step: it is the latency of the sums, one pass over
-// 8 bytes a sequence from L2, and of the chain length -> ring entry -> table.
+// A decode step (512 sequences, one new token each) is bound by latency: two reads of 8 bytes a sequence from
+// L2 and the chain length -> ring entry -> table.
 __global__ void __launch_bounds__(kPagesThreads) cache_pages_kernel(const __grid_constant__ PagesParams P) {
   wait_previous_kernel();
-  __shared__ long long sum[4][kPagesWarps];        // taken, given: of all, of those in front
-  __shared__ unsigned long long layer_new[kMaxLayers];
-  __shared__ uint32_t bad_word;
+  __shared__ long long layer_sum[3][kMaxLayers];   // pages taken, pages given, new tokens
+  __shared__ uint32_t bad_word, last_word;
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-  const int S = P.c.max_seqs, n = P.c.num_layers * S, shift = P.c.page_shift, page_mask = P.c.page - 1;
+  const int S = P.c.max_seqs, layers = P.c.num_layers, n = layers * S;
+  const int shift = P.c.page_shift, page_mask = P.c.page - 1;
   const int cap = P.c.max_pages << shift;
-  const int first = blockIdx.x * kPagesWarps;
-  for (int i = threadIdx.x; i < P.c.num_layers; i += kPagesThreads) layer_new[i] = 0;
+  const int head = __ldg(P.ring_in), count = __ldg(P.ring_in + 1), np = P.c.num_pages;
   if (threadIdx.x == 0) bad_word = 0;
   __syncthreads();
-  long long taken = 0, given = 0, taken_front = 0, given_front = 0;
   bool bad = false;
-  int run_layer = -1;
-  unsigned long long run = 0;
-  for (int i = threadIdx.x; i < n; i += kPagesThreads) {
-    const int a = __ldg(P.from + i), b = __ldg(P.to + i);
-    bad |= a < 0 || b < 0 || a > cap || b > cap;
-    const int d = ((b + page_mask) >> shift) - ((a + page_mask) >> shift);
-    taken += max(d, 0);
-    given += max(-d, 0);
-    if (i < first) {
-      taken_front += max(d, 0);
-      given_front += max(-d, 0);
+  const auto sum_of = [&](const int32_t* from, const int32_t* to, int m, long long (&sum)[3]) {
+    uint32_t taken = 0, given = 0;   // (below 2^27 pages a sequence, 32 of them a lane)
+    long long tokens = 0;
+    for (int i = lane; i < m; i += 32) {
+      const int a = __ldg(from + i), b = __ldg(to + i);
+      bad |= a < 0 || b < 0 || a > cap || b > cap;
+      const int d = ((b + page_mask) >> shift) - ((a + page_mask) >> shift);
+      taken += max(d, 0);
+      given += max(-d, 0);
+      tokens += max(b - a, 0);
     }
-    if (P.slots && b > a) {
-      const int l = i / S;
-      if (l != run_layer) {
-        if (run) atomicAdd(&layer_new[run_layer], run);
-        run_layer = l;
-        run = 0;
-      }
-      run += static_cast<unsigned>(b - a);
-    }
+    sum[0] = warp_sum(taken);
+    sum[1] = warp_sum(given);
+    sum[2] = P.slots ? warp_sum(tokens) : 0;
+  };
+#pragma unroll 4
+  for (int l = warp; l < layers; l += kPagesWarps) {
+    long long sum[3];
+    sum_of(P.from + l * S, P.to + l * S, S, sum);
+    if (lane < 3) layer_sum[lane][l] = lane == 0 ? sum[0] : lane == 1 ? sum[1] : sum[2];
   }
-  if (run) atomicAdd(&layer_new[run_layer], run);
   if (bad) bad_word = 1;
+  __syncthreads();
+  const int seq = blockIdx.x * kPagesWarps + warp;
+  const int layer = seq < n ? seq / S : layers - 1, r = seq - layer * S;
+  long long taken = 0, given = 0, at = 0, back = 0;
+  bool too_many = false;
+  for (int l = lane; l < layers; l += 32) {
+    const long long x = layer_sum[0][l], y = layer_sum[1][l];
+    taken += x;
+    given += y;
+    at += l < layer ? x : 0;
+    back += l < layer ? y : 0;
+    too_many |= P.slots && layer_sum[2][l] > P.slot_stride;
+  }
   taken = warp_sum(taken);
   given = warp_sum(given);
-  taken_front = warp_sum(taken_front);
-  given_front = warp_sum(given_front);
-  if (lane == 0) {
-    sum[0][warp] = taken;
-    sum[1][warp] = given;
-    sum[2][warp] = taken_front;
-    sum[3][warp] = given_front;
-  }
-  const int head = __ldg(P.ring_in), count = __ldg(P.ring_in + 1), np = P.c.num_pages;
-  __syncthreads();
-  taken = given = taken_front = given_front = 0;
-#pragma unroll
-  for (int w = 0; w < kPagesWarps; ++w) {
-    taken += sum[0][w];
-    given += sum[1][w];
-    taken_front += sum[2][w];
-    given_front += sum[3][w];
-  }
-  bad = bad_word || head < 0 || head >= np || count < 0 || count > np || count + given > np;
-  if (P.slots)
-    for (int l = 0; l < P.c.num_layers; ++l)
-      bad |= layer_new[l] > static_cast<unsigned long long>(P.slot_stride);
+  bad = bad_word || __any_sync(0xffffffffu, too_many) || head < 0 || head >= np || count < 0 || count > np ||
+        count + given > np;
   const bool ok = !bad && taken <= count;
-  const int seq = first + warp;
   if (seq < n) {
-    const int layer = seq / S, r = seq - layer * S;
-    const int step = 32 * gridDim.y, start = lane + 32 * blockIdx.y;
-    // pages of this CTA's earlier sequences, and the new tokens of this layer's
-    long long at = 0, back = 0, tok = 0;
-    if (lane < warp) {
-      const int a = __ldg(P.from + first + lane), b = __ldg(P.to + first + lane);
-      const int d = ((b + page_mask) >> shift) - ((a + page_mask) >> shift);
-      at = max(d, 0);
-      back = max(-d, 0);
-    }
-    at = taken_front + warp_sum(at);
-    back = given_front + warp_sum(back);
-    if (P.slots) {
-      for (int i = lane; i < r; i += 32)
-        tok += max(__ldg(P.to + layer * S + i) - __ldg(P.from + layer * S + i), 0);
-      tok = warp_sum(tok);
-    }
     const int a = __ldg(P.from + seq), b = __ldg(P.to + seq);
     int32_t* row = P.table + static_cast<int64_t>(seq) * P.c.max_pages;
-    if (ok) {
+    if (ok && a != b) {
+      long long before[3];
+      sum_of(P.from + layer * S, P.to + layer * S, r, before);
+      at = warp_sum(at) + before[0];
+      back = warp_sum(back) + before[1];
       const int have = (a + page_mask) >> shift, need = (b + page_mask) >> shift;
-      for (int j = have + start; j < need; j += step) row[j] = P.free_pages[ring_at(head, at + (j - have), np)];
-      for (int j = need + start; j < have; j += step)
-        P.free_pages[ring_at(head, count + back + (j - need), np)] = row[j];
-      if (P.slots) {
-        int32_t* out = P.slots + layer * P.slot_stride + tok;
+      if (b > a) {
+        int32_t* out = P.slots ? P.slots + layer * P.slot_stride + before[2] : nullptr;
+        const int taken_at = ring_at(head, at, np);
+        // chunks of 32 pages, from the one that holds the first new token
+        for (int j0 = (a >> shift) + 32 * blockIdx.y; j0 < need; j0 += 32 * gridDim.y) {
+          const int j = j0 + lane;
+          int page = -1;
+          if (j < have) {
+            if (out) page = row[j];
+          } else if (j < need) {
+            page = P.free_pages[ring_at(taken_at, j - have, np)];
+            row[j] = page;
+          }
+          if (!out) continue;
+          const int base = page >= 0 && page < np ? page << shift : -1;
+          const int end = min(b, (j0 + 32) << shift);
 #pragma unroll 4
-        for (int i = start; i < b - a; i += step) {
-          const int pos = a + i, j = pos >> shift;
-          const int page = j < have ? row[j] : P.free_pages[ring_at(head, at + (j - have), np)];
-          out[i] = page >= 0 && page < np ? (page << shift) + (pos & page_mask) : -1;
+          for (int pos = j0 << shift; pos < end; pos += 32) {
+            const int mine = pos + lane;
+            const int from = __shfl_sync(0xffffffffu, base, (mine >> shift) - j0);
+            if (mine >= a && mine < end) out[mine - a] = from < 0 ? -1 : from + (mine & page_mask);
+          }
         }
+      } else {
+        const int given_at = ring_at(head, count + back, np);
+        for (int j = need + lane + 32 * blockIdx.y; j < have; j += 32 * gridDim.y)
+          P.free_pages[ring_at(given_at, j - need, np)] = row[j];
       }
     }
     if (P.slots && r == S - 1) {
       // behind the layer's new tokens (from its start where nothing was done)
-      const int64_t end = ok ? static_cast<int64_t>(layer_new[layer]) : 0;
       int32_t* out = P.slots + layer * P.slot_stride;
-      for (int64_t i = end + start; i < P.slot_stride; i += step) out[i] = -1;
+      for (int64_t i = (ok ? layer_sum[2][layer] : 0) + lane + 32 * blockIdx.y; i < P.slot_stride; i += 32 * gridDim.y)
+        out[i] = -1;
     }
   }
   // the last CTA moves the state on
   __syncthreads();
-  if (threadIdx.x == 0) {
-    __threadfence();
-    bad_word = atomicInc(P.done, gridDim.x * gridDim.y - 1) == gridDim.x * gridDim.y - 1;
-  }
+  const uint32_t ctas = gridDim.x * gridDim.y;
+  if (threadIdx.x == 0) last_word = inc_acq_rel_gpu(P.done, ctas - 1) == ctas - 1;
   __syncthreads();
-  if (!bad_word) return;
-  __threadfence();
+  allow_next_kernel();
+  if (!last_word) return;
   const int32_t* now = ok ? P.to : P.from;
   if (P.lens_out != now)
     for (int i = threadIdx.x; i < n; i += kPagesThreads) P.lens_out[i] = now[i];
@@ -180,12 +170,13 @@ __global__ void cache_reset_kernel(int32_t* free_pages, int32_t* ring, int n) {
 
 // ---------------------------------------------------------------- rows in 8 bits
 
-// A run (new rows of one page and head, of keys or of values) is written by a team of P / 16 groups of 16
-// lanes; group g holds page rows 16 g .. 16 g + 15 in registers, 8 elements of each row a lane, from
-// the load of a row to the store of its codes: bf16 is read once and codes are written once, whatever
-// P. 64 registers of rows a thread leave three CTAs an SM, 192 KB of loads in flight.
+// A run (new rows of one page and head, of keys or of values) is written by a team of P / kGroupRows groups
+// of 16 lanes; group g holds page rows kGroupRows g .. in registers, 8 elements of each row a lane, from the
+// load of a row to the store of its codes: bf16 is read once and codes are written once, whatever P.
 constexpr int kRowThreads = 256;
-constexpr int kGroupRows = 16;
+constexpr int kGroupRows = 8;
+template <int kPage>
+constexpr int kTeamThreads = kPage / kGroupRows * 16;   // a warp at least
 
 __device__ __forceinline__ uint32_t max_u16x2(uint32_t a, uint32_t b) {
   uint32_t d;
@@ -233,14 +224,16 @@ __device__ __forceinline__ uint32_t scaled_codes(uint32_t two, float f) {
   return e4m3x2(lo * f, hi * f);
 }
 
-// Waits for the other groups of this thread's team (teams of one warp or less are together).
+// Waits for the other groups of this thread's team.
 template <int kPage>
 __device__ __forceinline__ void team_sync() {
-  constexpr int kTeam = kPage;   // threads of a team: P / 16 groups of 16
-  if constexpr (kTeam > 32)
+  constexpr int kTeam = kTeamThreads<kPage>;
+  if constexpr (kTeam == kRowThreads)
+    __syncthreads();
+  else if constexpr (kTeam > 32)
     named_bar_sync(1 + threadIdx.x / kTeam, kTeam);
   else
-    __syncwarp(kTeam == 32 ? 0xffffffffu : (threadIdx.x & 16 ? 0xffff0000u : 0x0000ffffu));
+    __syncwarp();
 }
 
 // Writes rows [off, off + n) of a page (codes and scale of one head); x[i] holds this lane's 8
@@ -268,14 +261,10 @@ __device__ __forceinline__ void write_run(const uint4 (&x)[kGroupRows], int off,
   for (int o = 8; o > 0; o >>= 1) m = max(m, __shfl_xor_sync(lanes, m, o));
   // the page's scale is read before it is written: every group reads, then all meet
   const float held = off > 0 ? *scale : 0.f;
-  if constexpr (kGroups > 1) {
-    if (lane == 0) team_max[g] = m;
-    team_sync<kPage>();
+  if (lane == 0) team_max[g] = m;
+  team_sync<kPage>();
 #pragma unroll
-    for (int i = 0; i < kGroups; ++i) m = max(m, team_max[i]);
-  } else {
-    __syncwarp(lanes);
-  }
+  for (int i = 0; i < kGroups; ++i) m = max(m, team_max[i]);
   const float s = fmaxf(held, __uint_as_float(need_bits(m)));
   const float inv = __frcp_rn(s);   // exact: a power of two
   if (s > held && off > 0) {
@@ -303,12 +292,11 @@ __device__ __forceinline__ void write_run(const uint4 (&x)[kGroupRows], int off,
 template <int kPage>
 __global__ void __launch_bounds__(kRowThreads) cache_gather_kernel(const __grid_constant__ CacheGatherParams P) {
   wait_previous_kernel();   // the indices come from the selection launched before
-  constexpr int kGroups = kPage / kGroupRows, kTeams = kRowThreads / kPage;
+  constexpr int kTeam = kTeamThreads<kPage>, kGroups = kPage / kGroupRows, kTeams = kRowThreads / kTeam;
   __shared__ uint32_t team_max[kTeams][kGroups];
-  const int team = threadIdx.x / kPage, lane = threadIdx.x & 15, g = (threadIdx.x / 16) % kGroups;
-  const int64_t item = static_cast<int64_t>(blockIdx.x) * kTeams + team;
-  const int64_t pages = item >> 1;
-  const int64_t unit = pages / P.unit_pages;
+  const int team = threadIdx.x / kTeam, lane = threadIdx.x & 15, g = (threadIdx.x / 16) % kGroups;
+  const uint32_t item = blockIdx.x * kTeams + team;   // (below 2^31)
+  const uint32_t pages = item >> 1, unit = pages / P.unit_pages;
   if (unit >= P.g.g.n_units) return;   // the whole team
   const bool values = item & 1;
   const int j = static_cast<int>(pages - unit * P.unit_pages);
@@ -317,13 +305,13 @@ __global__ void __launch_bounds__(kRowThreads) cache_gather_kernel(const __grid_
   const int m = min(P.g.layer_budget[u.layer], Lc);
   const int n = min(m + W - j * kPage, kPage);
   if (n <= 0) return;
-  const int64_t seq = static_cast<int64_t>(u.layer) * P.c.max_seqs + P.first_seq + u.r;
-  const int page = __ldg(P.table + seq * P.c.max_pages + j);
+  const int seq = u.layer * P.c.max_seqs + P.first_seq + u.r;
+  const int page = __ldg(P.table + static_cast<int64_t>(seq) * P.c.max_pages + j);
   // the positions of this group's rows: lane i looks row i's up
-  const int row = j * kPage + g * kGroupRows + lane;
+  const int row = j * kPage + g * kGroupRows + (lane & (kGroupRows - 1));
   int src = -1;
   if (row < m) {
-    src = __ldg(P.g.indices + unit * P.g.budget + row);
+    src = __ldg(P.g.indices + static_cast<int64_t>(unit) * P.g.budget + row);
     if (src >= Lc) src = -1;   // never read outside the unit
   } else if (row < m + W) {
     src = Lc + (row - m);
@@ -345,6 +333,7 @@ __global__ void __launch_bounds__(kRowThreads) cache_gather_kernel(const __grid_
   const int64_t block = static_cast<int64_t>(page) * P.c.heads + u.h;
   write_run<kPage>(x, 0, n, (values ? P.c.v : P.c.k) + block * (kPage * kHeadDim),
                    (values ? P.c.v_scale : P.c.k_scale) + block, team_max[team]);
+  allow_next_kernel();
 }
 
 // New tokens by slot. A team takes `block` consecutive tokens of one head, keys or values, and writes
@@ -353,9 +342,9 @@ __global__ void __launch_bounds__(kRowThreads) cache_gather_kernel(const __grid_
 template <int kPage>
 __global__ void __launch_bounds__(kRowThreads) cache_store_kernel(const __grid_constant__ CacheStoreParams P) {
   wait_previous_kernel();
-  constexpr int kGroups = kPage / kGroupRows, kTeams = kRowThreads / kPage;
+  constexpr int kTeam = kTeamThreads<kPage>, kGroups = kPage / kGroupRows, kTeams = kRowThreads / kTeam;
   __shared__ uint32_t team_max[kTeams][kGroups];
-  const int team = threadIdx.x / kPage, lane = threadIdx.x & 15, g = (threadIdx.x / 16) % kGroups;
+  const int team = threadIdx.x / kTeam, lane = threadIdx.x & 15, g = (threadIdx.x / 16) % kGroups;
   const int64_t item = static_cast<int64_t>(blockIdx.x) * kTeams + team;
   const int H = P.c.heads;
   const int64_t first = item / (2 * H) * P.block;
@@ -385,7 +374,7 @@ __global__ void __launch_bounds__(kRowThreads) cache_store_kernel(const __grid_c
     const int page = slot / kPage, off = slot % kPage;
     int n = kPage - off;
 #pragma unroll
-    for (int c = 0; c < kGroups; ++c) {
+    for (int c = 0; c < kPage / 16; ++c) {
       const int i = c * 16 + lane;
       const bool breaks = i < n && (t + i >= P.n_tokens || __ldg(P.slots + t + i) != slot + i);
       const uint32_t who = (__ballot_sync(lanes, breaks) >> (threadIdx.x & 16)) & 0xffffu;
@@ -401,21 +390,19 @@ __global__ void __launch_bounds__(kRowThreads) cache_store_kernel(const __grid_c
     const int64_t block = static_cast<int64_t>(page) * H + h;
     write_run<kPage>(x, off, n, (values ? P.c.v : P.c.k) + block * (kPage * kHeadDim),
                      (values ? P.c.v_scale : P.c.k_scale) + block, team_max[team]);
-    if constexpr (kGroups > 1) team_sync<kPage>();   // team_max and the scale before the next run
+    team_sync<kPage>();   // team_max and the scale before the next run
     t += n;
     prev = slot + n - 1;
   }
+  allow_next_kernel();
 }
 
-// Slots and table entries that one warp of kv_evict_cache_pages goes through before a sequence is
-// dealt to more warps.
-constexpr int64_t kPagesPerWarp = 512;
 // Tokens of a call from which a team takes P tokens instead of one (measured at the kernel's launcher).
 constexpr int64_t kStoreBlockTokens = 4096;
 
 template <int kPage>
 cudaError_t store_paged(const CacheStoreParams& p, cudaStream_t stream) {
-  constexpr int kTeams = kRowThreads / kPage;
+  constexpr int kTeams = kRowThreads / kTeamThreads<kPage>;
   const int64_t items = (p.n_tokens + p.block - 1) / p.block * 2 * p.c.heads;
   return launch_after_previous(cache_store_kernel<kPage>, dim3(static_cast<unsigned>((items + kTeams - 1) / kTeams)),
                                dim3(kRowThreads), 0, stream, p);
@@ -423,7 +410,7 @@ cudaError_t store_paged(const CacheStoreParams& p, cudaStream_t stream) {
 
 template <int kPage>
 cudaError_t gather_paged(const CacheGatherParams& p, cudaStream_t stream) {
-  constexpr int kTeams = kRowThreads / kPage;
+  constexpr int kTeams = kRowThreads / kTeamThreads<kPage>;
   const int64_t items = p.g.g.n_units * p.unit_pages * 2;
   return launch_after_previous(cache_gather_kernel<kPage>, dim3(static_cast<unsigned>((items + kTeams - 1) / kTeams)),
                                dim3(kRowThreads), 0, stream, p);
@@ -434,10 +421,10 @@ cudaError_t gather_paged(const CacheGatherParams& p, cudaStream_t stream) {
 cudaError_t launch_cache_pages(const PagesParams& p, cudaStream_t stream) {
   const int n = p.c.num_layers * p.c.max_seqs;
   const int64_t x = (n + kPagesWarps - 1) / kPagesWarps;
-  // warps a sequence: what its slots ask for on average, within a few waves of CTAs
-  const int64_t per_seq = p.slots ? (p.slot_stride + p.c.max_seqs - 1) / p.c.max_seqs : p.c.max_pages / 8;
-  int64_t y = (per_seq + kPagesPerWarp - 1) / kPagesPerWarp;
-  const int64_t most = x < 2048 ? 2048 / x : 1;
+  // warps a sequence: what its slots (or its table row) ask for, within a few waves of CTAs
+  const int64_t tokens = p.slots ? (p.slot_stride + p.c.max_seqs - 1) / p.c.max_seqs : int64_t(p.c.max_pages) << p.c.page_shift;
+  int64_t y = (tokens >> p.c.page_shift) / 32;
+  const int64_t most = x < 1216 ? 1216 / x : 1;
   y = y > most ? most : y;
   return launch_after_previous(cache_pages_kernel, dim3(static_cast<unsigned>(x), static_cast<unsigned>(y < 1 ? 1 : y)),
                                dim3(kPagesThreads), 0, stream, p);

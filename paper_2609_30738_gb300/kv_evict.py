@@ -378,18 +378,34 @@ def run_step(plan: Plan, bufs: Buffers, q_win, k, v, lambda1, lambda2, stream=No
     plan.gather(k, v, bufs.indices, bufs.k_out, bufs.v_out, stream)
 
 
+_Pair = ctypes.c_int64 * 2
+
+
 def _row_strides(t, heads: int, name: str):
     """The {token, head} element strides of a bf16 tensor [..., heads, d] as a host array, or None where it
     is dense. The dimensions in front of the heads must be one run of tokens."""
-    import torch
-    if t.dtype != torch.bfloat16 or t.shape[-2] != heads or t.stride(-1) != 1:
+    shape, st = t.shape, t.stride()
+    if t.dtype != _bf16() or len(shape) < 3 or shape[-2] != heads or st[-1] != 1:
         raise ValueError(f"{name}: expected bf16 [..., {heads}, d] with contiguous rows")
-    for i in range(t.dim() - 3):
-        if t.shape[i] > 1 and t.stride(i) != t.stride(i + 1) * t.shape[i + 1]:
-            raise ValueError(f"{name}: its tokens are not one run")
-    if t.is_contiguous():
+    dense = heads * shape[-1]
+    token = span = None
+    for n, step in zip(shape[-3::-1], st[-3::-1]):
+        if n != 1:
+            if span is None:
+                token = step
+            elif step != span:
+                raise ValueError(f"{name}: its tokens are not one run")
+            span = step * n
+    if token is None:
+        token = dense
+    if token == dense and (heads == 1 or st[-2] == shape[-1]):
         return None
-    return (ctypes.c_int64 * 2)(t.stride(-3), t.stride(-2))
+    return _Pair(token, st[-2])
+
+
+def _bf16():
+    import torch
+    return torch.bfloat16
 
 
 class Cache8:
@@ -415,9 +431,17 @@ class Cache8:
         _check(_lib().kv_evict_cache_create(ctypes.byref(cfg), _ptr(self.k), _ptr(self.v), _ptr(self.k_scale),
                                             _ptr(self.v_scale), ctypes.byref(handle), ctypes.byref(size)),
                "kv_evict_cache_create")
-        self._h = handle
+        self._h, self._lib = handle, _lib()
         self.ws = torch.empty(size.value, dtype=torch.uint8, device=self.k.device)
+        self._ws = self.ws.data_ptr()
         self.reset()
+
+    def _stream(self, stream):
+        """The stream's address; None is the current stream of the cache's device."""
+        if stream is None:
+            import torch
+            return torch.cuda.current_stream(self.k.device).cuda_stream
+        return _stream_ptr(stream)
 
     @staticmethod
     def _buffer(t, shape, dtype, device):
@@ -446,26 +470,27 @@ class Cache8:
 
     def reset(self, free_pages=None, ring=None, stream=None):
         """kv_evict_cache_reset: clear the workspace, and make every page free where the ring is given."""
-        _check(_lib().kv_evict_cache_reset(self._h, _ptr(free_pages), _ptr(ring), _ptr(self.ws),
-                                           _stream_ptr(stream)), "kv_evict_cache_reset")
+        _check(self._lib.kv_evict_cache_reset(self._h, _ptr(free_pages), _ptr(ring), self._ws,
+                                              self._stream(stream)), "kv_evict_cache_reset")
 
     def pages(self, lens_from, lens_to, table, free_pages, ring_in, ring_out, lens_out, slots=None, stream=None):
         """kv_evict_cache_pages. slots: int32 [N_L, n] or None."""
         stride = 0
         if slots is not None:
-            if slots.dim() != 2 or slots.shape[0] != self.num_layers or not slots.is_contiguous():
+            shape = slots.shape
+            if len(shape) != 2 or shape[0] != self.num_layers or not slots.is_contiguous():
                 raise ValueError("slots: expected a contiguous [num_layers, n] tensor")
-            stride = slots.shape[1]
-        for name, t, n in (("lens_from", lens_from, self.num_layers * self.max_seqs),
-                           ("lens_to", lens_to, self.num_layers * self.max_seqs),
-                           ("lens_out", lens_out, self.num_layers * self.max_seqs),
-                           ("table", table, self.num_layers * self.max_seqs * self.max_pages),
-                           ("free_pages", free_pages, self.num_pages), ("ring_in", ring_in, 2), ("ring_out", ring_out, 2)):
+            stride = shape[1]
+        seqs = self.num_layers * self.max_seqs
+        for name, t, n in (("lens_from", lens_from, seqs), ("lens_to", lens_to, seqs), ("lens_out", lens_out, seqs),
+                           ("table", table, seqs * self.max_pages), ("free_pages", free_pages, self.num_pages),
+                           ("ring_in", ring_in, 2), ("ring_out", ring_out, 2)):
             if t.numel() != n or not t.is_contiguous():
                 raise ValueError(f"{name}: expected {n} contiguous values")
-        _check(_lib().kv_evict_cache_pages(self._h, _ptr(lens_from), _ptr(lens_to), _ptr(table), _ptr(free_pages),
-                                           _ptr(ring_in), _ptr(ring_out), _ptr(lens_out), _ptr(slots), stride,
-                                           _ptr(self.ws), _stream_ptr(stream)), "kv_evict_cache_pages")
+        _check(self._lib.kv_evict_cache_pages(
+            self._h, lens_from.data_ptr(), lens_to.data_ptr(), table.data_ptr(), free_pages.data_ptr(),
+            ring_in.data_ptr(), ring_out.data_ptr(), lens_out.data_ptr(), _ptr(slots), stride, self._ws,
+            self._stream(stream)), "kv_evict_cache_pages")
 
     def gather(self, plan: Plan, k, v, indices, table, first_seq: int = 0, stream=None):
         """kv_evict_cache_gather: the kept and the window rows of plan's requests as sequences first_seq ..;
@@ -474,33 +499,37 @@ class Cache8:
             dev = getattr(t, "device", None)
             if dev is not None and getattr(dev, "type", None) == "cpu" and not t.is_pinned():
                 raise ValueError(f"gather: {name} is a pageable CPU tensor; pin it or move it to the GPU")
-        _check(_lib().kv_evict_cache_gather(self._h, plan._h, _ptr(k), _ptr(v), _ptr(indices), int(first_seq),
-                                            _ptr(table), _ptr(self.ws), _stream_ptr(stream)), "kv_evict_cache_gather")
+        _check(self._lib.kv_evict_cache_gather(self._h, plan._h, k.data_ptr(), v.data_ptr(), indices.data_ptr(),
+                                               first_seq, table.data_ptr(), self._ws, self._stream(stream)),
+               "kv_evict_cache_gather")
 
     def store(self, k_new, v_new, slots, stream=None):
         """kv_evict_cache_store: k_new, v_new bf16 [tokens, H, d] (slices of a projection's output too), slots
         int32 [tokens]."""
         n = slots.numel()
-        if k_new.numel() != n * self.heads * self.head_dim or v_new.numel() != k_new.numel() or not slots.is_contiguous():
+        rows = n * self.heads * self.head_dim
+        if k_new.numel() != rows or v_new.numel() != rows or not slots.is_contiguous():
             raise ValueError("store: k_new and v_new hold a row of every head for each slot")
-        _check(_lib().kv_evict_cache_store(self._h, _ptr(k_new), _ptr(v_new), _row_strides(k_new, self.heads, "k_new"),
-                                           _row_strides(v_new, self.heads, "v_new"), _ptr(slots), n, _ptr(self.ws),
-                                           _stream_ptr(stream)), "kv_evict_cache_store")
+        _check(self._lib.kv_evict_cache_store(
+            self._h, k_new.data_ptr(), v_new.data_ptr(), _row_strides(k_new, self.heads, "k_new"),
+            _row_strides(v_new, self.heads, "v_new"), slots.data_ptr(), n, self._ws, self._stream(stream)),
+            "kv_evict_cache_store")
 
     def attend(self, q, table, lens, layer: int, out, lse=None, stream=None):
         """kv_evict_cache_attend: q, out bf16 [n_seq, q_tokens, Hq, d], lse fp32 [n_seq, q_tokens, Hq] or
         None; table and lens of all layers."""
-        if q.dim() != 4 or out.shape != q.shape or (lse is not None and
-                                                    (lse.shape != q.shape[:3] or not lse.is_contiguous())):
+        shape = q.shape
+        if len(shape) != 4 or out.shape != shape or (lse is not None and
+                                                     (lse.shape != shape[:3] or not lse.is_contiguous())):
             raise ValueError("attend: q and out are [n_seq, q_tokens, Hq, d], lse [n_seq, q_tokens, Hq]")
-        _check(_lib().kv_evict_cache_attend(self._h, int(layer), q.shape[0], q.shape[1], _ptr(q),
-                                            _row_strides(q, self.num_q_heads, "q"), _ptr(table), _ptr(lens), _ptr(out),
-                                            _row_strides(out, self.num_q_heads, "out"), _ptr(lse), _ptr(self.ws),
-                                            _stream_ptr(stream)), "kv_evict_cache_attend")
+        _check(self._lib.kv_evict_cache_attend(
+            self._h, layer, shape[0], shape[1], q.data_ptr(), _row_strides(q, self.num_q_heads, "q"),
+            table.data_ptr(), lens.data_ptr(), out.data_ptr(), _row_strides(out, self.num_q_heads, "out"), _ptr(lse),
+            self._ws, self._stream(stream)), "kv_evict_cache_attend")
 
     def status(self, stream=None) -> int:
         """Synchronise, return the device status of the calls so far and clear it."""
-        return int(_lib().kv_evict_cache_status(self._h, _ptr(self.ws), _stream_ptr(stream)))
+        return int(self._lib.kv_evict_cache_status(self._h, self._ws, self._stream(stream)))
 
 
 def run_step_cache8(plan: Plan, bufs: Buffers, cache: Cache8, q_win, k, v, lambda1, lambda2, table, lens, free_pages,
