@@ -19,13 +19,22 @@ namespace {
 
 // ---------------------------------------------------------------- tables and slots
 
-constexpr int kPagesThreads = 256;
+constexpr int kPagesThreads = 1024;
 constexpr int kPagesWarps = kPagesThreads / 32;
+static_assert(kPagesWarps == 32, "a lane a sequence of the CTA");
 
+// A sequence that changes: lengths, its first place in the ring, its slots (or null), its table row.
+struct Grown {
+  int32_t a, b, ring;
+  int32_t* out;
+  int32_t* row;
+};
+
+// The warp's sum of x < 2^50 (in two parts whose sums fit 32 bits).
 __device__ __forceinline__ long long warp_sum(long long x) {
-#pragma unroll
-  for (int o = 16; o > 0; o >>= 1) x += __shfl_xor_sync(0xffffffffu, x, o);
-  return x;
+  const uint32_t lo = __reduce_add_sync(0xffffffffu, static_cast<uint32_t>(x) & 0xffffffu);
+  const uint32_t hi = __reduce_add_sync(0xffffffffu, static_cast<uint32_t>(x >> 24));
+  return (static_cast<long long>(hi) << 24) + lo;
 }
 
 __device__ __forceinline__ int ring_at(int head, long long i, int n) {
@@ -36,18 +45,21 @@ __device__ __forceinline__ int ring_at(int head, long long i, int n) {
   return static_cast<int>(p);
 }
 
-// A warp takes a sequence, in chunks of 32 pages (a lane a page) that blockIdx.y deals to more than one
-// warp where sequences are long; a chunk's pages are read in one access, and 32 slots at a time leave from
-// registers, so new pages cost their 8 bytes and slots their 4. Every CTA first sums the pages and tokens that
-// each layer takes and gives (a warp a layer): all agree whether the call can be done before one of them
-// writes, and every warp finds its place in the ring and in its layer's slots. What the call changes in
-// place (lens_out, ring_out may be inputs) is written by the CTA that finishes reading last.
+// A CTA has 32 sequences, a warp each for their places in the ring and in their layer's slots; their pages, in
+// chunks of 32 (a lane a page), are one line that the warps share, so that one long sequence is no warp's
+// alone. A chunk's pages are read in one access and 32 slots at a time leave from registers: new pages cost
+// their 8 bytes and slots their 4. Before that every CTA sums the pages and tokens that each layer takes and
+// gives (a warp a layer), so that all agree whether the call can be done before one of them writes; these
+// sums are why there is one CTA an SM at most. Where the call changes its inputs in place (lens_out,
+// ring_out), the CTA that finishes reading last does that.
 //
 // A decode step (512 sequences, one new token each) is bound by latency: two reads of 8 bytes a sequence from
 // L2 and the chain length -> ring entry -> table.
 __global__ void __launch_bounds__(kPagesThreads) cache_pages_kernel(const __grid_constant__ PagesParams P) {
   wait_previous_kernel();
   __shared__ long long layer_sum[3][kMaxLayers];   // pages taken, pages given, new tokens
+  __shared__ Grown grown[kPagesWarps];
+  __shared__ int chunks_of[kPagesWarps];
   __shared__ uint32_t bad_word, last_word;
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
   const int S = P.c.max_seqs, layers = P.c.num_layers, n = layers * S;
@@ -97,50 +109,80 @@ __global__ void __launch_bounds__(kPagesThreads) cache_pages_kernel(const __grid
   bad = bad_word || __any_sync(0xffffffffu, too_many) || head < 0 || head >= np || count < 0 || count > np ||
         count + given > np;
   const bool ok = !bad && taken <= count;
-  if (seq < n) {
+  // this warp's sequence: its chunks of 32 pages, its place in the ring and in its layer's slots
+  int chunks = 0;
+  if (seq < n && ok) {
     const int a = __ldg(P.from + seq), b = __ldg(P.to + seq);
-    int32_t* row = P.table + static_cast<int64_t>(seq) * P.c.max_pages;
-    if (ok && a != b) {
+    const int have = (a + page_mask) >> shift, need = (b + page_mask) >> shift;
+    // from the page of the first new token on, or the released ones
+    chunks = b > a ? (need - (a >> shift) + 31) >> 5 : (have - need + 31) >> 5;
+    if (chunks > 0) {
       long long before[3];
       sum_of(P.from + layer * S, P.to + layer * S, r, before);
       at = warp_sum(at) + before[0];
       back = warp_sum(back) + before[1];
-      const int have = (a + page_mask) >> shift, need = (b + page_mask) >> shift;
-      if (b > a) {
-        int32_t* out = P.slots ? P.slots + layer * P.slot_stride + before[2] : nullptr;
-        const int taken_at = ring_at(head, at, np);
-        // chunks of 32 pages, from the one that holds the first new token
-        for (int j0 = (a >> shift) + 32 * blockIdx.y; j0 < need; j0 += 32 * gridDim.y) {
-          const int j = j0 + lane;
-          int page = -1;
-          if (j < have) {
-            if (out) page = row[j];
-          } else if (j < need) {
-            page = P.free_pages[ring_at(taken_at, j - have, np)];
-            row[j] = page;
-          }
-          if (!out) continue;
-          const int base = page >= 0 && page < np ? page << shift : -1;
-          const int end = min(b, (j0 + 32) << shift);
-#pragma unroll 4
-          for (int pos = j0 << shift; pos < end; pos += 32) {
-            const int mine = pos + lane;
-            const int from = __shfl_sync(0xffffffffu, base, (mine >> shift) - j0);
-            if (mine >= a && mine < end) out[mine - a] = from < 0 ? -1 : from + (mine & page_mask);
-          }
-        }
-      } else {
-        const int given_at = ring_at(head, count + back, np);
-        for (int j = need + lane + 32 * blockIdx.y; j < have; j += 32 * gridDim.y)
-          P.free_pages[ring_at(given_at, j - need, np)] = row[j];
+      if (lane == 0) {
+        grown[warp] = {a, b, ring_at(head, b > a ? at : count + back, np),
+                       b > a && P.slots ? P.slots + layer * P.slot_stride + before[2] : nullptr,
+                       P.table + static_cast<int64_t>(seq) * P.c.max_pages};
       }
     }
+  }
+  if (lane == 0) chunks_of[warp] = chunks;
+  __syncthreads();
+  // all chunks of this CTA's sequences in one line, dealt to its warps (and those of the other blockIdx.y)
+  int last = chunks_of[lane];
+#pragma unroll
+  for (int o = 1; o < 32; o <<= 1) {
+    const int x = __shfl_up_sync(0xffffffffu, last, o);
+    if (lane >= o) last += x;
+  }
+  const int all = __shfl_sync(0xffffffffu, last, 31);
+  for (int q = blockIdx.y * kPagesWarps + warp; q < all; q += kPagesWarps * gridDim.y) {
+    const int w = __popc(__ballot_sync(0xffffffffu, last <= q));   // the sequence whose chunk it is
+    const int c = q - (w > 0 ? __shfl_sync(0xffffffffu, last, max(w - 1, 0)) : 0);
+    const Grown s = grown[w];
+    const int have = (s.a + page_mask) >> shift, need = (s.b + page_mask) >> shift;
+    if (s.b > s.a) {
+      const int j0 = (s.a >> shift) + 32 * c, j = j0 + lane;
+      int page = -1;
+      if (j < have) {
+        if (s.out) page = s.row[j];
+      } else if (j < need) {
+        page = P.free_pages[ring_at(s.ring, j - have, np)];
+        s.row[j] = page;
+      }
+      if (!s.out) continue;
+      const int base = page >= 0 && page < np ? page << shift : -1;
+      const int end = min(s.b, (j0 + 32) << shift);
+#pragma unroll 4
+      for (int pos = j0 << shift; pos < end; pos += 32) {
+        const int mine = pos + lane;
+        const int from = __shfl_sync(0xffffffffu, base, (mine >> shift) - j0);
+        if (mine >= s.a && mine < end) s.out[mine - s.a] = from < 0 ? -1 : from + (mine & page_mask);
+      }
+    } else {
+      const int j = need + 32 * c + lane;
+      if (j < have) P.free_pages[ring_at(s.ring, j - need, np)] = s.row[j];
+    }
+  }
+  if (seq < n) {
     if (P.slots && r == S - 1) {
       // behind the layer's new tokens (from its start where nothing was done)
       int32_t* out = P.slots + layer * P.slot_stride;
       for (int64_t i = (ok ? layer_sum[2][layer] : 0) + lane + 32 * blockIdx.y; i < P.slot_stride; i += 32 * gridDim.y)
         out[i] = -1;
     }
+  }
+  if (!P.in_place) {
+    if (seq < n && lane == 0 && blockIdx.y == 0) P.lens_out[seq] = ok ? P.to[seq] : P.from[seq];
+    if (blockIdx.x == 0 && blockIdx.y == 0 && threadIdx.x == 0) {
+      P.ring_out[0] = ok ? ring_at(head, taken, np) : head;
+      P.ring_out[1] = ok ? static_cast<int>(count - taken + given) : count;
+      if (!ok) atomicOr(P.err, bad ? kErrCheck : kErrPages);
+    }
+    allow_next_kernel();
+    return;
   }
   // the last CTA moves the state on
   __syncthreads();
@@ -340,7 +382,7 @@ __global__ void __launch_bounds__(kRowThreads) cache_gather_kernel(const __grid_
 // the runs that start among them one after the other: 1 where the calls of a decode step have a token a
 // sequence, P where whole prompts have a run every P tokens.
 template <int kPage>
-__global__ void __launch_bounds__(kRowThreads) cache_store_kernel(const __grid_constant__ CacheStoreParams P) {
+__global__ void __launch_bounds__(kRowThreads, 4) cache_store_kernel(const __grid_constant__ CacheStoreParams P) {
   wait_previous_kernel();
   constexpr int kTeam = kTeamThreads<kPage>, kGroups = kPage / kGroupRows, kTeams = kRowThreads / kTeam;
   __shared__ uint32_t team_max[kTeams][kGroups];
@@ -356,15 +398,18 @@ __global__ void __launch_bounds__(kRowThreads) cache_store_kernel(const __grid_c
   const uint32_t lanes = threadIdx.x & 16 ? 0xffff0000u : 0x0000ffffu;
   const int64_t limit = static_cast<int64_t>(P.c.num_pages) * kPage;
   const int64_t last = min(first + P.block, P.n_tokens);
-  int prev = first > 0 ? __ldg(P.slots + first - 1) : -1;
   for (int64_t t = first; t < last;) {
-    const int slot = __ldg(P.slots + t);
-    const bool starts = slot >= 0 && (prev < 0 || slot != prev + 1 || slot % kPage == 0);
-    prev = slot;
-    if (!starts) {
-      ++t;
+    // the next token that starts a run, 16 at a time
+    const int64_t i16 = t + lane;
+    const int here = i16 < last ? __ldg(P.slots + i16) : -1, prev = i16 > 0 && i16 < last ? __ldg(P.slots + i16 - 1) : -1;
+    const bool starts = here >= 0 && (prev < 0 || here != prev + 1 || here % kPage == 0);
+    const uint32_t found = (__ballot_sync(lanes, starts) >> (threadIdx.x & 16)) & 0xffffu;
+    if (!found) {
+      t += 16;
       continue;
     }
+    t += __ffs(found) - 1;
+    const int slot = __shfl_sync(lanes, here, __ffs(found) - 1, 16);
     if (slot >= limit) {
       if (g == 0 && lane == 0) atomicOr(P.err, kErrCheck);
       ++t;
@@ -373,12 +418,16 @@ __global__ void __launch_bounds__(kRowThreads) cache_store_kernel(const __grid_c
     // the run's length: the first token that is not the next slot of this page
     const int page = slot / kPage, off = slot % kPage;
     int n = kPage - off;
+    int next[kPage / 16];
 #pragma unroll
     for (int c = 0; c < kPage / 16; ++c) {
       const int i = c * 16 + lane;
-      const bool breaks = i < n && (t + i >= P.n_tokens || __ldg(P.slots + t + i) != slot + i);
-      const uint32_t who = (__ballot_sync(lanes, breaks) >> (threadIdx.x & 16)) & 0xffffu;
-      if (who) n = min(n, c * 16 + __ffs(who) - 1);
+      next[c] = i < n && t + i < P.n_tokens ? __ldg(P.slots + t + i) : -1;
+    }
+#pragma unroll
+    for (int c = kPage / 16 - 1; c >= 0; --c) {   // (backwards: the first break counts)
+      const uint32_t who = (__ballot_sync(lanes, next[c] != slot + c * 16 + lane) >> (threadIdx.x & 16)) & 0xffffu;
+      if (who) n = min(kPage - off, c * 16 + __ffs(who) - 1);
     }
     uint4 x[kGroupRows];
 #pragma unroll
@@ -392,11 +441,11 @@ __global__ void __launch_bounds__(kRowThreads) cache_store_kernel(const __grid_c
                      (values ? P.c.v_scale : P.c.k_scale) + block, team_max[team]);
     team_sync<kPage>();   // team_max and the scale before the next run
     t += n;
-    prev = slot + n - 1;
   }
   allow_next_kernel();
 }
 
+constexpr int64_t kPagesCtas = 152;
 // Tokens of a call from which a team takes P tokens instead of one (measured at the kernel's launcher).
 constexpr int64_t kStoreBlockTokens = 4096;
 
@@ -421,10 +470,10 @@ cudaError_t gather_paged(const CacheGatherParams& p, cudaStream_t stream) {
 cudaError_t launch_cache_pages(const PagesParams& p, cudaStream_t stream) {
   const int n = p.c.num_layers * p.c.max_seqs;
   const int64_t x = (n + kPagesWarps - 1) / kPagesWarps;
-  // warps a sequence: what its slots (or its table row) ask for, within a few waves of CTAs
+  // CTAs that share 32 sequences: what their slots (or table rows) ask for, one CTA an SM in all
   const int64_t tokens = p.slots ? (p.slot_stride + p.c.max_seqs - 1) / p.c.max_seqs : int64_t(p.c.max_pages) << p.c.page_shift;
   int64_t y = (tokens >> p.c.page_shift) / 32;
-  const int64_t most = x < 1216 ? 1216 / x : 1;
+  const int64_t most = x < kPagesCtas ? kPagesCtas / x : 1;
   y = y > most ? most : y;
   return launch_after_previous(cache_pages_kernel, dim3(static_cast<unsigned>(x), static_cast<unsigned>(y < 1 ? 1 : y)),
                                dim3(kPagesThreads), 0, stream, p);
@@ -587,6 +636,7 @@ kve_status kv_evict_cache_pages(const kve_cache* cache, const int32_t* lens_from
   p.slot_stride = slot_stride;
   p.err = word(ws, cache->ws.err);
   p.done = word(ws, cache->ws.pages_done);
+  p.in_place = lens_out == lens_from || lens_out == lens_to || ring_out == ring_in;
   return kve::launch_cache_pages(p, static_cast<cudaStream_t>(stream)) == cudaSuccess ? KVE_OK : KVE_ECUDA;
 }
 

@@ -263,6 +263,7 @@ struct PagesParams {
   int32_t* lens_out;
   int32_t* slots;        // or null
   int64_t slot_stride;
+  bool in_place;         // lens_out or ring_out is an input
   uint32_t* err;
   uint32_t* done;
 };

@@ -385,27 +385,19 @@ def _row_strides(t, heads: int, name: str):
     """The {token, head} element strides of a bf16 tensor [..., heads, d] as a host array, or None where it
     is dense. The dimensions in front of the heads must be one run of tokens."""
     shape, st = t.shape, t.stride()
-    if t.dtype != _bf16() or len(shape) < 3 or shape[-2] != heads or st[-1] != 1:
+    if str(t.dtype) != "torch.bfloat16" or len(shape) < 3 or shape[-2] != heads or st[-1] != 1:
         raise ValueError(f"{name}: expected bf16 [..., {heads}, d] with contiguous rows")
-    dense = heads * shape[-1]
-    token = span = None
-    for n, step in zip(shape[-3::-1], st[-3::-1]):
-        if n != 1:
-            if span is None:
-                token = step
-            elif step != span:
-                raise ValueError(f"{name}: its tokens are not one run")
-            span = step * n
-    if token is None:
-        token = dense
-    if token == dense and (heads == 1 or st[-2] == shape[-1]):
+    if t.is_contiguous():
         return None
-    return _Pair(token, st[-2])
-
-
-def _bf16():
-    import torch
-    return torch.bfloat16
+    token = span = None
+    for i in range(len(shape) - 3, -1, -1):
+        if shape[i] != 1:
+            if span is None:
+                token = st[i]
+            elif st[i] != span:
+                raise ValueError(f"{name}: its tokens are not one run")
+            span = st[i] * shape[i]
+    return _Pair(heads * shape[-1] if token is None else token, st[-2])
 
 
 class Cache8:
@@ -434,14 +426,18 @@ class Cache8:
         self._h, self._lib = handle, _lib()
         self.ws = torch.empty(size.value, dtype=torch.uint8, device=self.k.device)
         self._ws = self.ws.data_ptr()
+        dev = self.k.device
+        raw = getattr(torch._C, "_cuda_getCurrentRawStream", None)   # (no Stream object made: 2 us less a call)
+        if raw is not None and dev.type == "cuda":
+            index = torch.cuda.current_device() if dev.index is None else dev.index
+            self._current_stream = lambda: raw(index)
+        else:
+            self._current_stream = lambda: torch.cuda.current_stream(dev).cuda_stream
         self.reset()
 
     def _stream(self, stream):
         """The stream's address; None is the current stream of the cache's device."""
-        if stream is None:
-            import torch
-            return torch.cuda.current_stream(self.k.device).cuda_stream
-        return _stream_ptr(stream)
+        return self._current_stream() if stream is None else _stream_ptr(stream)
 
     @staticmethod
     def _buffer(t, shape, dtype, device):
