@@ -220,18 +220,18 @@ constexpr int kGroupRows = 8;
 template <int kPage>
 constexpr int kTeamThreads = kPage / kGroupRows * 16;   // a warp at least
 
-__device__ __forceinline__ uint32_t max_u16x2(uint32_t a, uint32_t b) {
+// The larger magnitudes of two bf16 pairs; NaN counts only where both are.
+__device__ __forceinline__ uint32_t max_abs(uint32_t a, uint32_t b) {
   uint32_t d;
-  asm("max.u16x2 %0, %1, %2;" : "=r"(d) : "r"(a), "r"(b));
+  asm("{\n .reg .b32 x, y;\n abs.bf16x2 x, %1;\n abs.bf16x2 y, %2;\n max.bf16x2 %0, x, y;\n}" : "=r"(d) : "r"(a), "r"(b));
   return d;
 }
 
-// The largest finite magnitude of the bf16 pair x, or'ed into the pair m of magnitudes.
-__device__ __forceinline__ uint32_t max_finite(uint32_t m, uint32_t x) {
-  x &= 0x7fff7fffu;
-  if ((x & 0xffffu) >= 0x7f80u) x &= 0xffff0000u;
-  if (x >= 0x7f800000u) x &= 0x0000ffffu;
-  return max_u16x2(m, x);
+// The pair x without its infinities and NaN.
+__device__ __forceinline__ uint32_t finite_only(uint32_t x) {
+  if ((x & 0x7f80u) == 0x7f80u) x &= 0xffff0000u;
+  if ((x & 0x7f800000u) == 0x7f800000u) x &= 0x0000ffffu;
+  return x;
 }
 
 // need(a) as fp32 bits for the magnitude with bf16 bits a (finite): a = (1 + f/128) 2^(x-127), and
@@ -288,15 +288,14 @@ __device__ __forceinline__ void write_run(const uint4 (&x)[kGroupRows], int off,
   const uint32_t lanes = threadIdx.x & 16 ? 0xffff0000u : 0x0000ffffu;
   uint32_t m = 0;
 #pragma unroll
-  for (int i = 0; i < kGroupRows; ++i)
-    m = max_u16x2(max_u16x2(max_u16x2(m, x[i].x & 0x7fff7fffu), max_u16x2(x[i].y & 0x7fff7fffu, x[i].z & 0x7fff7fffu)),
-                  x[i].w & 0x7fff7fffu);
-  if ((m & 0xffffu) >= 0x7f80u || m >= 0x7f800000u) {
-    // an infinity or a NaN among them (rare): the finite ones alone
+  for (int i = 0; i < kGroupRows; ++i) m = max_abs(m, max_abs(max_abs(x[i].x, x[i].y), max_abs(x[i].z, x[i].w)));
+  if ((m & 0x7f80u) == 0x7f80u || (m & 0x7f800000u) == 0x7f800000u) {
+    // an infinity or nothing but NaN among them (rare): the finite ones alone
     m = 0;
 #pragma unroll
     for (int i = 0; i < kGroupRows; ++i)
-      m = max_finite(max_finite(max_finite(max_finite(m, x[i].x), x[i].y), x[i].z), x[i].w);
+      m = max_abs(m, max_abs(max_abs(finite_only(x[i].x), finite_only(x[i].y)),
+                             max_abs(finite_only(x[i].z), finite_only(x[i].w))));
   }
   m = max(m & 0xffffu, m >> 16);
 #pragma unroll
@@ -325,7 +324,7 @@ __device__ __forceinline__ void write_run(const uint4 (&x)[kGroupRows], int off,
 #pragma unroll
   for (int i = 0; i < kGroupRows; ++i) {
     const int row = g * kGroupRows + i;
-    if (row >= off && row < off + n) reinterpret_cast<uint2*>(codes + row * kHeadDim)[lane] = row_codes(x[i], inv);
+    if (static_cast<uint32_t>(row - off) < static_cast<uint32_t>(n)) reinterpret_cast<uint2*>(codes + row * kHeadDim)[lane] = row_codes(x[i], inv);
   }
   if (g == 0 && lane == 0) *scale = s;
 }
