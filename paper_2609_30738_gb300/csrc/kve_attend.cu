@@ -27,7 +27,7 @@
 namespace kve {
 namespace {
 
-constexpr int kKStages = 2, kVStages = 4;   // 96 KB of tiles a CTA; a K tile is done with two tiles before its V
+constexpr uint32_t kKStages = 2, kVStages = 4;   // 96 KB of tiles a CTA; a K tile is done with two tiles before its V
 constexpr int kTileBytes = kTileKeys * kHeadDim;
 constexpr int kMostTilePages = kTileKeys / 16;
 
@@ -66,7 +66,9 @@ struct ACtl {
   uint64_t m_full[kVStages];                   // the scales beside a V stage
   uint64_t s_full[2], q_full[2], q_empty[2];   // by tile parity, by part parity
   uint64_t p_full, o_full, meet[H], joined[H], drain;
+  // of a tile's pages: the keys' scale, and the values' as 256 times a share of the tile's largest one
   float ks[kVStages][kMostTilePages], vs[kVStages][kMostTilePages];
+  float vtop[kVStages];                        // that largest one / 256
   uint32_t pages[kVStages];                    // bit j: page j of the tile holds tokens
   alignas(16) float red[2][4][R];              // row maxima of the warps, by tile parity
   // of each warp's rows: the maximum, exp(old maximum - new); at the end of a part (x) the warp's row sums
@@ -384,13 +386,13 @@ cache_attend_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_const
         }
         return f;
       };
-      Ahead now = step({ctl.first, x0 - 1, 0, false});
+      Ahead now = step({ctl.first, x0 - 1, -1, false});
       Ahead then = step(now);
       float2 sc = scales(now);
-      const int n = x1 - x0;
-      int it = 0;
+      const uint32_t n = x1 - x0;
+      uint32_t it = 0;
       for (; it < n; ++it) {
-        const int ks_at = it % kKStages, st = it % kVStages;
+        const uint32_t ks_at = it % kKStages, st = it % kVStages;
         const bool ok = valid(now.id);
         if (!ok && now.has) atomicOr(P.err, kErrCheck);
         const Ahead after = step(then);
@@ -412,10 +414,13 @@ cache_attend_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_const
           tma_load_2d(smem + ks_at * kTileBytes + lane * page_bytes, &tm_k, 0, row, &ctl.k_full[ks_at]);
           tma_load_2d(smem + C::kV + st * kTileBytes + lane * page_bytes, &tm_v, 0, row, &ctl.v_full[st]);
         }
+        // the largest scale of the tile's values comes out of the sums; a token keeps the rest (at most 1)
+        const float top = warp_max(sc.y);
         if (lane < kMostTilePages) {
           ctl.ks[st][lane] = sc.x;
-          ctl.vs[st][lane] = sc.y;
+          ctl.vs[st][lane] = top > 0.f ? sc.y * rcp(top) * 256.f : 0.f;
         }
+        if (lane == 0) ctl.vtop[st] = top * (1.f / 256.f);
         __syncwarp();
         if (lane == 0) mbar_arrive(&ctl.m_full[st]);
         now = then;
@@ -424,9 +429,9 @@ cache_attend_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_const
       }
       // after a wait that ran out: the copies in flight end before the shared memory does
       if (ctl.abort && lane == 0) {
-        for (int k = max(it - kKStages, 0); k < it; ++k)
+        for (uint32_t k = it > kKStages ? it - kKStages : 0; k < it; ++k)
           mbar_wait(&ctl.k_full[k % kKStages], (k / kKStages) & 1, P.wait_limit_ns, &ctl.never);
-        for (int k = max(it - kVStages, 0); k < it; ++k)
+        for (uint32_t k = it > kVStages ? it - kVStages : 0; k < it; ++k)
           mbar_wait(&ctl.v_full[k % kVStages], (k / kVStages) & 1, P.wait_limit_ns, &ctl.never);
       }
     }
@@ -436,11 +441,12 @@ cache_attend_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_const
       const uint32_t kaddr = smem_u32(smem), qaddr = kaddr + static_cast<uint32_t>(C::kQ);
       const uint32_t paddr = kaddr + static_cast<uint32_t>(C::kP);
       Block at = ctl.first;
-      const int n = x1 - x0;
-      int part = 0;
+      const uint32_t n = x1 - x0;
+      uint32_t part = 0;
       // S^T of tile `it`; it runs two tiles ahead of the probabilities
-      const auto scores = [&](int it) -> bool {
-        const int x = x0 + it, st = it % kKStages;
+      const auto scores = [&](uint32_t it) -> bool {
+        const int x = x0 + static_cast<int>(it);
+        const uint32_t st = it % kKStages;
         const bool fresh = x == at.first + at.tiles;
         if (fresh) {
           next_block(P, blocks, at);
@@ -462,8 +468,8 @@ cache_attend_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_const
         return true;
       };
       bool ok = scores(0) && (n == 1 || scores(1));
-      for (int it = 0; ok && it < n; ++it) {
-        const int st = it % kVStages;
+      for (uint32_t it = 0; ok && it < n; ++it) {
+        const uint32_t st = it % kVStages;
         if (!mbar_wait(&ctl.v_full[st], (it / kVStages) & 1, P.wait_limit_ns, &ctl.abort) ||
             !mbar_wait(&ctl.p_full, it & 1, P.wait_limit_ns, &ctl.abort)) {
           ok = false;
@@ -496,8 +502,8 @@ cache_attend_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_const
           for (int k = 0; k < 2; ++k) reinterpret_cast<uint32_t*>(qbuf + k * C::kQBytes + 2 * R * kHeadDim)[i] = 0;
       }
       Block at = ctl.first;
-      for (int part = 0;; ++part) {
-        const int parity = part & 1;
+      for (uint32_t part = 0;; ++part) {
+        const uint32_t parity = part & 1;
         if (part >= 2 && !warp_wait(&ctl.q_empty[parity], ((part >> 1) & 1) ^ 1, P.wait_limit_ns, &ctl.abort)) {
           if (lane == 0) fail();
           break;
@@ -577,14 +583,15 @@ cache_attend_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_const
       return warp_wait(&ctl.meet[half], met++ & 1u, P.wait_limit_ns, &ctl.abort);
     };
     Block at = ctl.first;
-    const int n = x1 - x0;
-    int part = 0, part0 = x0, splits = 0;
+    const uint32_t n = x1 - x0;
+    uint32_t part = 0;
+    int part0 = x0, splits = 0;
     bool ok = true;
     float m = -INFINITY;                 // lane i: row i's maximum so far
     float l[N], acc[N], keep[N];         // keep: exp(old maximum - new) of the last tile
     float back = 0.f;                    // the last tile's scale of O^T
     // adds tile `it`'s O^T
-    const auto take = [&](int it) -> bool {
+    const auto take = [&](uint32_t it) -> bool {
       if (!warp_wait(&ctl.o_full, it & 1, P.wait_limit_ns, &ctl.abort)) return false;
       tc_fence_after();
       float o[N == 4 ? 16 : 3 * N];
@@ -612,8 +619,9 @@ cache_attend_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_const
     };
     ok = begin();
     bool pending = false;   // the tile before is of this part and not added yet
-    for (int it = 0; ok && it < n; ++it) {
-      const int x = x0 + it, st = it % kVStages;
+    for (uint32_t it = 0; ok && it < n; ++it) {
+      const int x = x0 + static_cast<int>(it);
+      const uint32_t st = it % kVStages;
       const int pos = (x - at.first) * kTileKeys + tid;
       if (!warp_wait(&ctl.m_full[st], (it / kVStages) & 1, P.wait_limit_ns, &ctl.abort)) {
         ok = false;
@@ -623,11 +631,7 @@ cache_attend_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_const
       const uint32_t have = ctl.pages[st];
       const bool held = (have >> pg & 1u) && pos < at.len;
       const float ks = ctl.ks[st][pg];
-      float vtop = 0.f;
-#pragma unroll
-      for (int j = 0; j < kMostTilePages; ++j) vtop = fmaxf(vtop, ctl.vs[st][j]);
-      // the largest scale of the tile's values comes out of the sums; a token keeps the rest (at most 1)
-      const float vrest = held && vtop > 0.f ? ctl.vs[st][pg] * __frcp_rn(vtop) * 256.f : 0.f;
+      const float vrest = held ? ctl.vs[st][pg] : 0.f, vtop = ctl.vtop[st];
       if (!warp_wait(&ctl.s_full[it & 1], (it >> 1) & 1, P.wait_limit_ns, &ctl.abort)) {
         ok = false;
         break;
@@ -671,7 +675,7 @@ cache_attend_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_const
         ok = false;
         break;
       }
-      back = vtop * (1.f / 256.f);
+      back = vtop;
       if (lane < N) {   // lane i: row i's maximum
         const float top = fmaxf(fmaxf(ctl.red[it & 1][0][i0 + lane], ctl.red[it & 1][1][i0 + lane]),
                                 fmaxf(ctl.red[it & 1][2][i0 + lane], ctl.red[it & 1][3][i0 + lane]));
@@ -889,7 +893,7 @@ cache_attend_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_const
             top[i] = mn;
             sum[i] *= f0;
             a4[i].x *= f0, a4[i].y *= f0, a4[i].z *= f0, a4[i].w *= f0;
-#pragma unroll 4
+#pragma unroll 2
             for (int j = 0; j < count; ++j) {
               const float g = ex2(stats[j * kPartWords] - ref);
               const float4 o = reinterpret_cast<const float4*>(row + j * kPartWords)[lane];

@@ -379,16 +379,26 @@ def run_step(plan: Plan, bufs: Buffers, q_win, k, v, lambda1, lambda2, stream=No
 
 
 _Pair = ctypes.c_int64 * 2
+_bf16 = None   # torch.bfloat16, once torch is there
 
 
 def _row_strides(t, heads: int, name: str):
     """The {token, head} element strides of a bf16 tensor [..., heads, d] as a host array, or None where it
     is dense. The dimensions in front of the heads must be one run of tokens."""
-    shape, st = t.shape, t.stride()
-    if str(t.dtype) != "torch.bfloat16" or len(shape) < 3 or shape[-2] != heads or st[-1] != 1:
+    global _bf16
+    if _bf16 is None:
+        import torch
+        _bf16 = torch.bfloat16
+    shape = t.shape
+    if t.dtype is not _bf16 or len(shape) < 3 or shape[-2] != heads:
         raise ValueError(f"{name}: expected bf16 [..., {heads}, d] with contiguous rows")
     if t.is_contiguous():
         return None
+    st = t.stride()
+    if st[-1] != 1:
+        raise ValueError(f"{name}: expected bf16 [..., {heads}, d] with contiguous rows")
+    if len(shape) == 3:
+        return _Pair(st[0], st[1])
     token = span = None
     for i in range(len(shape) - 3, -1, -1):
         if shape[i] != 1:
