@@ -215,10 +215,17 @@ __global__ void cache_reset_kernel(int32_t* free_pages, int32_t* ring, int n) {
 // A run (new rows of one page and head, of keys or of values) is written by a team of P / kGroupRows groups
 // of 16 lanes; group g holds page rows kGroupRows g .. in registers, 8 elements of each row a lane, from the
 // load of a row to the store of its codes: bf16 is read once and codes are written once, whatever P.
-constexpr int kRowThreads = 256;
+//
+// Bound by HBM: 256 bytes read and 128 written a row. A team's loads are all in flight before its maximum is
+// known and its stores wait for that, so the overlap is between CTAs, and small ones do best: with one team
+// of 128 or 256 threads a CTA (P = 64, 128) or four smaller ones, 16 prompts at a budget of 509 in 8 layers
+// (387 MB) take 67.8 us, 84% of the HBM peak, and 24k prompt tokens (146 MB) 27.5 us, 79%; with 256 threads
+// for P = 64 73.6 and 29.8, with 16 rows a group 119 and 30.5, with 4 rows 92 and 42.6.
 constexpr int kGroupRows = 8;
 template <int kPage>
 constexpr int kTeamThreads = kPage / kGroupRows * 16;   // a warp at least
+template <int kPage>
+constexpr int kRowThreads = kTeamThreads<kPage> >= 128 ? kTeamThreads<kPage> : 4 * kTeamThreads<kPage>;
 
 // The larger magnitudes of two bf16 pairs; NaN counts only where both are.
 __device__ __forceinline__ uint32_t max_abs(uint32_t a, uint32_t b) {
@@ -270,7 +277,7 @@ __device__ __forceinline__ uint32_t scaled_codes(uint32_t two, float f) {
 template <int kPage>
 __device__ __forceinline__ void team_sync() {
   constexpr int kTeam = kTeamThreads<kPage>;
-  if constexpr (kTeam == kRowThreads)
+  if constexpr (kTeam == kRowThreads<kPage>)
     __syncthreads();
   else if constexpr (kTeam > 32)
     named_bar_sync(1 + threadIdx.x / kTeam, kTeam);
@@ -331,9 +338,9 @@ __device__ __forceinline__ void write_run(const uint4 (&x)[kGroupRows], int off,
 
 // Step 4 into the cache. A team takes page j of a unit, keys or values (the two alternate).
 template <int kPage>
-__global__ void __launch_bounds__(kRowThreads) cache_gather_kernel(const __grid_constant__ CacheGatherParams P) {
+__global__ void __launch_bounds__(kRowThreads<kPage>) cache_gather_kernel(const __grid_constant__ CacheGatherParams P) {
   wait_previous_kernel();   // the indices come from the selection launched before
-  constexpr int kTeam = kTeamThreads<kPage>, kGroups = kPage / kGroupRows, kTeams = kRowThreads / kTeam;
+  constexpr int kTeam = kTeamThreads<kPage>, kGroups = kPage / kGroupRows, kTeams = kRowThreads<kPage> / kTeam;
   __shared__ uint32_t team_max[kTeams][kGroups];
   const int team = threadIdx.x / kTeam, lane = threadIdx.x & 15, g = (threadIdx.x / 16) % kGroups;
   const uint32_t item = blockIdx.x * kTeams + team;   // (below 2^31)
@@ -369,7 +376,7 @@ __global__ void __launch_bounds__(kRowThreads) cache_gather_kernel(const __grid_
   for (int i = 0; i < kGroupRows; ++i) {
     const int s = __shfl_sync(lanes, src, i, 16);
     x[i] = make_uint4(0, 0, 0, 0);
-    if (s >= 0) x[i] = __ldcs(reinterpret_cast<const uint4*>(from + s * st) + lane);
+    if (s >= 0) x[i] = __ldg(reinterpret_cast<const uint4*>(from + s * st) + lane);
   }
   const int64_t block = static_cast<int64_t>(page) * P.c.heads + u.h;
   write_run<kPage>(x, 0, n, (values ? P.c.v : P.c.k) + block * (kPage * kHeadDim),
@@ -381,9 +388,9 @@ __global__ void __launch_bounds__(kRowThreads) cache_gather_kernel(const __grid_
 // the runs that start among them one after the other: 1 where the calls of a decode step have a token a
 // sequence, P where whole prompts have a run every P tokens.
 template <int kPage>
-__global__ void __launch_bounds__(kRowThreads, 4) cache_store_kernel(const __grid_constant__ CacheStoreParams P) {
+__global__ void __launch_bounds__(kRowThreads<kPage>, 1024 / kRowThreads<kPage>) cache_store_kernel(const __grid_constant__ CacheStoreParams P) {
   wait_previous_kernel();
-  constexpr int kTeam = kTeamThreads<kPage>, kGroups = kPage / kGroupRows, kTeams = kRowThreads / kTeam;
+  constexpr int kTeam = kTeamThreads<kPage>, kGroups = kPage / kGroupRows, kTeams = kRowThreads<kPage> / kTeam;
   __shared__ uint32_t team_max[kTeams][kGroups];
   const int team = threadIdx.x / kTeam, lane = threadIdx.x & 15, g = (threadIdx.x / 16) % kGroups;
   const int64_t item = static_cast<int64_t>(blockIdx.x) * kTeams + team;
@@ -433,7 +440,7 @@ __global__ void __launch_bounds__(kRowThreads, 4) cache_store_kernel(const __gri
     for (int i = 0; i < kGroupRows; ++i) {
       const int row = g * kGroupRows + i - off;
       x[i] = make_uint4(0, 0, 0, 0);
-      if (row >= 0 && row < n) x[i] = __ldcs(reinterpret_cast<const uint4*>(from + (t + row) * st) + lane);
+      if (row >= 0 && row < n) x[i] = __ldg(reinterpret_cast<const uint4*>(from + (t + row) * st) + lane);
     }
     const int64_t block = static_cast<int64_t>(page) * H + h;
     write_run<kPage>(x, off, n, (values ? P.c.v : P.c.k) + block * (kPage * kHeadDim),
@@ -450,18 +457,18 @@ constexpr int64_t kStoreBlockTokens = 4096;
 
 template <int kPage>
 cudaError_t store_paged(const CacheStoreParams& p, cudaStream_t stream) {
-  constexpr int kTeams = kRowThreads / kTeamThreads<kPage>;
+  constexpr int kTeams = kRowThreads<kPage> / kTeamThreads<kPage>;
   const int64_t items = (p.n_tokens + p.block - 1) / p.block * 2 * p.c.heads;
   return launch_after_previous(cache_store_kernel<kPage>, dim3(static_cast<unsigned>((items + kTeams - 1) / kTeams)),
-                               dim3(kRowThreads), 0, stream, p);
+                               dim3(kRowThreads<kPage>), 0, stream, p);
 }
 
 template <int kPage>
 cudaError_t gather_paged(const CacheGatherParams& p, cudaStream_t stream) {
-  constexpr int kTeams = kRowThreads / kTeamThreads<kPage>;
+  constexpr int kTeams = kRowThreads<kPage> / kTeamThreads<kPage>;
   const int64_t items = p.g.g.n_units * p.unit_pages * 2;
   return launch_after_previous(cache_gather_kernel<kPage>, dim3(static_cast<unsigned>((items + kTeams - 1) / kTeams)),
-                               dim3(kRowThreads), 0, stream, p);
+                               dim3(kRowThreads<kPage>), 0, stream, p);
 }
 
 }  // namespace
