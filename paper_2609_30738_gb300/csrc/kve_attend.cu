@@ -48,8 +48,9 @@ struct ACfg {
   static constexpr uint32_t kIdescO = idesc_e4m3_f32(128, kNp, true);
   static constexpr size_t kV = size_t(kKStages) * kTileBytes;
   static constexpr size_t kQ = kV + size_t(kVStages) * kTileBytes;
-  static constexpr size_t kQBytes = kNs * kHeadDim;  // by part parity
-  static constexpr size_t kP = kQ + 2 * kQBytes;
+  static constexpr uint32_t kQBufs = R > 8 ? 2 : 4;  // blocks whose query rows are held, by part
+  static constexpr size_t kQBytes = kNs * kHeadDim;
+  static constexpr size_t kP = kQ + kQBufs * kQBytes;
   static constexpr size_t kCtl = kP + kNp * kTileKeys;
 };
 
@@ -64,22 +65,23 @@ template <int R, int H>
 struct ACtl {
   uint64_t k_full[kKStages], k_empty[kKStages], v_full[kVStages], v_empty[kVStages];
   uint64_t m_full[kVStages];                   // the scales beside a V stage
-  uint64_t s_full[2], q_full[2], q_empty[2];   // by tile parity, by part parity
+  uint64_t s_full[2], q_full[ACfg<R, H>::kQBufs], q_empty[ACfg<R, H>::kQBufs];
   uint64_t p_full, o_full, meet[H], joined[H], drain;
   // of a tile's pages: the keys' scale, and the values' as 256 times a share of the tile's largest one
   float ks[kVStages][kMostTilePages], vs[kVStages][kMostTilePages];
   float vtop[kVStages];                        // that largest one / 256
   uint32_t pages[kVStages];                    // bit j: page j of the tile holds tokens
+  static constexpr uint32_t kQBufs = ACfg<R, H>::kQBufs;
   alignas(16) float red[2][4][R];              // row maxima of the warps, by tile parity
-  // of each warp's rows: the maximum, exp(old maximum - new); at the end of a part (x) the warp's row sums
-  alignas(16) float2 ref[4 * H][R / H];
-  // of a part's rows, by part parity: log2(e) / sqrt(d) / the power of two in the q pieces; tokens that the
-  // row sees; where its output goes (elements of out, of lse), -1 for no row
-  alignas(16) float qs[2][R];
-  alignas(16) int seen[2][R];
-  long long out_at[2][R];
-  int lse_at[2][R];
-  uint8_t nan_from[2][kHeadDim];               // by part parity: see there
+  alignas(16) float2 ref[4 * H][R / H];        // of each warp's rows: the maximum, exp(old maximum - new)
+  float sum[kQBufs > 2 ? 2 : 1][4][R];         // row sums of the warps, at the end of a part (by its parity)
+  // of the rows of a part in each query buffer: log2(e) / sqrt(d) / the power of two in the q pieces; tokens
+  // that the row sees; where its output goes (elements of out, of lse), -1 for no row
+  alignas(16) float qs[kQBufs][R];
+  alignas(16) int seen[kQBufs][R];
+  long long out_at[kQBufs][R];
+  int lse_at[kQBufs][R];
+  uint8_t nan_from[kQBufs][kHeadDim];          // see there
   Block split[2 * H];                          // parts left for the join, by half
   int last[2 * H], split_cta[2 * H];           // its parts, if they are all written; the CTA of the first
   Block first;                                 // the first part's block
@@ -230,8 +232,8 @@ cache_attend_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_const
       mbar_init(&ctl.v_empty[i], 1);
       mbar_init(&ctl.m_full[i], 1);
     }
-    for (int i = 0; i < 2; ++i) {
-      mbar_init(&ctl.s_full[i], 1);
+    for (int i = 0; i < 2; ++i) mbar_init(&ctl.s_full[i], 1);
+    for (int i = 0; i < C::kQBufs; ++i) {
       mbar_init(&ctl.q_full[i], 2);
       mbar_init(&ctl.q_empty[i], 4 * H + 1);   // the softmax warps, and the last scores
     }
@@ -453,18 +455,18 @@ cache_attend_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_const
           ++part;
         }
         if ((it == 0 || fresh) &&
-            !mbar_wait(&ctl.q_full[part & 1], (part >> 1) & 1, P.wait_limit_ns, &ctl.abort)) return false;
+            !mbar_wait(&ctl.q_full[part % C::kQBufs], (part / C::kQBufs) & 1, P.wait_limit_ns, &ctl.abort)) return false;
         if (!mbar_wait(&ctl.k_full[st], (it / kKStages) & 1, P.wait_limit_ns, &ctl.abort)) return false;
         tc_fence_after();
         const uint64_t a = sw128_desc(kaddr + st * kTileBytes);
-        const uint64_t b = sw128_desc(qaddr + (part & 1) * static_cast<uint32_t>(C::kQBytes));
+        const uint64_t b = sw128_desc(qaddr + part % C::kQBufs * static_cast<uint32_t>(C::kQBytes));
         const uint32_t d = tmem + (it & 1) * C::kNs;
 #pragma unroll
         for (int j = 0; j < kHeadDim / 32; ++j)   // 32 elements of d a step: 32 bytes of a row
           tc_mma_e4m3(d, a + 2 * j, b + 2 * j, C::kIdescS, j > 0);
         tc_commit(&ctl.k_empty[st]);
         tc_commit(&ctl.s_full[it & 1]);
-        if (x + 1 == x1 || x + 1 == at.first + at.tiles) tc_commit(&ctl.q_empty[part & 1]);
+        if (x + 1 == x1 || x + 1 == at.first + at.tiles) tc_commit(&ctl.q_empty[part % C::kQBufs]);
         return true;
       };
       bool ok = scores(0) && (n == 1 || scores(1));
@@ -499,12 +501,13 @@ cache_attend_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_const
       const int sub = lane & 15, first_row = (warp - 2) * 2 + (lane >> 4);
       if constexpr (2 * R < C::kNs) {   // columns behind the pieces: zeros, once
         for (int i = threadIdx.x - 64; i < (C::kNs - 2 * R) * kHeadDim / 4; i += 64)
-          for (int k = 0; k < 2; ++k) reinterpret_cast<uint32_t*>(qbuf + k * C::kQBytes + 2 * R * kHeadDim)[i] = 0;
+          for (int k = 0; k < C::kQBufs; ++k) reinterpret_cast<uint32_t*>(qbuf + k * C::kQBytes + 2 * R * kHeadDim)[i] = 0;
       }
       Block at = ctl.first;
       for (uint32_t part = 0;; ++part) {
-        const uint32_t parity = part & 1;
-        if (part >= 2 && !warp_wait(&ctl.q_empty[parity], ((part >> 1) & 1) ^ 1, P.wait_limit_ns, &ctl.abort)) {
+        const uint32_t qb = part % C::kQBufs;
+        if (part >= C::kQBufs &&
+            !warp_wait(&ctl.q_empty[qb], ((part / C::kQBufs) & 1) ^ 1, P.wait_limit_ns, &ctl.abort)) {
           if (lane == 0) fail();
           break;
         }
@@ -517,9 +520,9 @@ cache_attend_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_const
           x[k] = make_uint4(0, 0, 0, 0);
           if (row < rows) x[k] = __ldg(reinterpret_cast<const uint4*>(P.q + tok * P.q_st + hq * P.q_sh) + sub);
           if (sub == 0) {
-            ctl.seen[parity][i] = row < rows ? at.len - P.q_tokens + t + 1 : 0;
-            ctl.out_at[parity][i] = row < rows ? tok * P.o_st + hq * P.o_sh : -1;
-            ctl.lse_at[parity][i] = static_cast<int>(tok * P.c.hq) + hq;
+            ctl.seen[qb][i] = row < rows ? at.len - P.q_tokens + t + 1 : 0;
+            ctl.out_at[qb][i] = row < rows ? tok * P.o_st + hq * P.o_sh : -1;
+            ctl.lse_at[qb][i] = static_cast<int>(tok * P.c.hq) + hq;
           }
         }
 #pragma unroll
@@ -543,17 +546,17 @@ cache_attend_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_const
             lo[j / 2] |= e4m3x2((a - f.x) * 16.f, (b - f.y) * 16.f) << (16 * (j & 1));
           }
           const auto put = [&](int n, const uint32_t* v) {
-            *reinterpret_cast<uint2*>(qbuf + parity * C::kQBytes + n * kHeadDim + (((sub >> 1) ^ (n & 7)) << 4) +
+            *reinterpret_cast<uint2*>(qbuf + qb * C::kQBytes + n * kHeadDim + (((sub >> 1) ^ (n & 7)) << 4) +
                                       ((sub & 1) << 3)) = finite ? make_uint2(v[0], v[1]) : make_uint2(0, 0);
           };
           put(i, hi);
           put(R + i, lo);
           // a row with an infinity or a NaN: every logit NaN
-          if (sub == 0) ctl.qs[parity][i] = finite ? P.alpha * __frcp_rn(scale) : __uint_as_float(0x7fc00000u);
+          if (sub == 0) ctl.qs[qb][i] = finite ? P.alpha * __frcp_rn(scale) : __uint_as_float(0x7fc00000u);
         }
         fence_proxy_async_smem();
         __syncwarp();
-        if (lane == 0) mbar_arrive(&ctl.q_full[parity]);
+        if (lane == 0) mbar_arrive(&ctl.q_full[qb]);
         if (at.first + at.tiles >= x1) break;
         next_block(P, blocks, at);
       }
@@ -586,6 +589,11 @@ cache_attend_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_const
     const uint32_t n = x1 - x0;
     uint32_t part = 0;
     int part0 = x0, splits = 0;
+    struct End {
+      bool whole, first;   // the part is its whole block; its block's first part
+      int len;
+      uint32_t part;
+    };
     bool ok = true;
     float m = -INFINITY;                 // lane i: row i's maximum so far
     float l[N], acc[N], keep[N];         // keep: exp(old maximum - new) of the last tile
@@ -610,18 +618,87 @@ cache_attend_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_const
       }
       return true;
     };
-    const auto begin = [&]() -> bool {
+    const auto begin = [&]() {
 #pragma unroll
       for (int i = 0; i < N; ++i) l[i] = acc[i] = 0.f;
       m = -INFINITY;
-      if (half == 0) ctl.nan_from[part & 1][tid] = kNoNan;
-      return warp_wait(&ctl.q_full[part & 1], (part >> 1) & 1, P.wait_limit_ns, &ctl.abort);
     };
-    ok = begin();
+    const auto rows_ready = [&]() -> bool {   // of a new part
+      if (half == 0) ctl.nan_from[part % C::kQBufs][tid] = kNoNan;
+      return warp_wait(&ctl.q_full[part % C::kQBufs], (part / C::kQBufs) & 1, P.wait_limit_ns, &ctl.abort);
+    };
+    // The end of a part, first half: the row sums over the tokens' threads, each step halving the rows that a
+    // lane has, then the lanes. They are everybody's behind the next meeting.
+    const auto sum_rows = [&](uint32_t part) {
+      int row = 0;
+#pragma unroll
+      for (int o = 16, c = N / 2; o > 0; o >>= 1, c >>= 1) {
+        const bool up = lane & o;
+        if (c > 0) {
+#pragma unroll
+          for (int i = 0; i < c; ++i) {
+            const float other = __shfl_xor_sync(0xffffffffu, up ? l[i] : l[i + c], o);
+            l[i] = (up ? l[i + c] : l[i]) + other;
+          }
+          row += up ? c : 0;
+        } else {
+          l[0] += __shfl_xor_sync(0xffffffffu, l[0], o);
+        }
+      }
+      if (lane % (32 / N) == 0) ctl.sum[C::kQBufs > 2 ? part & 1 : 0][quad][i0 + row] = l[0];
+    };
+    // Second half, with the last tile's O^T added: the output, or the part for the join
+    const auto emit = [&](const End& end) {
+      const uint32_t qb = end.part % C::kQBufs;
+      if (P.q_tokens > 1) {
+        const int found = ctl.nan_from[qb][tid];
+        const int from = found == kNoNan ? INT32_MAX : end.len - P.q_tokens + 1 + found;
+#pragma unroll
+        for (int i = 0; i < N; ++i)
+          if (ctl.seen[qb][i0 + i] > from) acc[i] = __uint_as_float(0x7fc00000u);
+      }
+      float sum = 0.f;   // lane i: row i's
+      if (lane < N)
+      {
+        const float(*warps)[R] = ctl.sum[C::kQBufs > 2 ? end.part & 1 : 0];
+        sum = (warps[0][i0 + lane] + warps[1][i0 + lane]) + (warps[2][i0 + lane] + warps[3][i0 + lane]);
+      }
+      if (end.whole) {
+        const float inv = sum == 0.f ? 0.f : __frcp_rn(sum);
+#pragma unroll
+        for (int i = 0; i < N; ++i) {
+          const long long to = ctl.out_at[qb][i0 + i];
+          const float f = __shfl_sync(0xffffffffu, inv, i);
+          if (to >= 0) P.out[to + tid] = to_bf16(acc[i] * f);
+        }
+        if (P.lse && quad == 0 && lane < N && ctl.out_at[qb][i0 + lane] >= 0)
+          P.lse[ctl.lse_at[qb][i0 + lane]] = log_sum(m, sum);
+      } else {
+        // one of several parts of the block: left for the join. Slot 1 of the CTA is for a block's first part
+        // (its own last one), slot 0 for a later one (its own first)
+        float* dst = P.partial + (static_cast<int64_t>(blockIdx.x) * 2 + end.first) * kAttendPartWords +
+                     half * kPartWords;
+#pragma unroll
+        for (int i = 0; i < N; ++i) __stcg(dst + i * kHeadDim + tid, acc[i]);
+        if (quad == 0 && lane < N) {
+          __stcg(dst + N * kHeadDim + lane, m);
+          __stcg(dst + N * kHeadDim + N + lane, sum);
+        }
+      }
+      __syncwarp();
+      if (lane == 0) mbar_arrive(&ctl.q_empty[qb]);
+    };
+    // Where there are query rows for it the end of a part waits for its successor's first scores: the value
+    // product passes meanwhile, and that tile's meeting is the sums' too.
+    constexpr bool kLate = C::kQBufs > 2;
+    begin();
+    ok = rows_ready();
+    bool due = false;       // the tile before ended a part (end), whose end is still to come
+    End end = {};
     bool pending = false;   // the tile before is of this part and not added yet
     for (uint32_t it = 0; ok && it < n; ++it) {
       const int x = x0 + static_cast<int>(it);
-      const uint32_t st = it % kVStages;
+      const uint32_t st = it % kVStages, qb = part % C::kQBufs;
       const int pos = (x - at.first) * kTileKeys + tid;
       if (!warp_wait(&ctl.m_full[st], (it / kVStages) & 1, P.wait_limit_ns, &ctl.abort)) {
         ok = false;
@@ -649,7 +726,7 @@ cache_attend_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_const
         }
         tmem_wait_ld(s);
 #pragma unroll
-        for (int i = 0; i < N; ++i) w[i] = fmaf(s[N + i], 0.0625f, s[i]) * ctl.qs[part & 1][i0 + i] * ks;
+        for (int i = 0; i < N; ++i) w[i] = fmaf(s[N + i], 0.0625f, s[i]) * ctl.qs[qb][i0 + i] * ks;
       }
       const int tile0 = pos - tid, tile_end = tile0 + kTileKeys;
       const bool whole = have == (0xffu >> (kMostTilePages - (kTileKeys >> P.c.page_shift))) && tile_end <= at.len;
@@ -657,7 +734,7 @@ cache_attend_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_const
       if (!whole || some) {
 #pragma unroll
         for (int i = 0; i < N; ++i)
-          if (!held || pos >= ctl.seen[part & 1][i0 + i]) w[i] = -INFINITY;
+          if (!held || pos >= ctl.seen[qb][i0 + i]) w[i] = -INFINITY;
       }
       float* red = &ctl.red[it & 1][quad][i0];
 #pragma unroll
@@ -667,13 +744,20 @@ cache_attend_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_const
       }
       meet_arrive();
       // the tile before while the others arrive; its probabilities' buffer is free behind it
-      if (pending && !take(it - 1)) {
+      if ((pending || due) && !take(it - 1)) {
         ok = false;
         break;
       }
       if (!meet_wait()) {
         ok = false;
         break;
+      }
+      if constexpr (kLate) {
+        if (due) {
+          emit(end);
+          begin();
+          due = false;
+        }
       }
       back = vtop;
       if (lane < N) {   // lane i: row i's maximum
@@ -695,7 +779,7 @@ cache_attend_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_const
       if (!whole || some) {   // (a scale that is NaN, of tokens that a row does not see)
 #pragma unroll
         for (int i = 0; i < N; ++i)
-          if (!held || pos >= ctl.seen[part & 1][i0 + i]) w[i] = 0.f;
+          if (!held || pos >= ctl.seen[qb][i0 + i]) w[i] = 0.f;
       }
       // three e4m3 pieces of each probability: column k R + i of the token's row
       uint32_t out[up16(3 * N) / 4];
@@ -730,7 +814,8 @@ cache_attend_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_const
         if (!held) {
           // a probability of 0 does not undo a NaN: rows without a token are zeros
 #pragma unroll
-          for (int j = 0; j < kHeadDim / 16; ++j) reinterpret_cast<uint4*>(v + tid * kHeadDim)[j] = make_uint4(0, 0, 0, 0);
+          for (int j = 0; j < kHeadDim / 16; ++j)   // (each lane from another 16 bytes on: no bank twice)
+            reinterpret_cast<uint4*>(v + tid * kHeadDim)[(j + tid) % (kHeadDim / 16)] = make_uint4(0, 0, 0, 0);
         }
         if (some) {
           // nor may a NaN value that later rows see reach the earlier ones: it is taken out here, and given to
@@ -741,7 +826,7 @@ cache_attend_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_const
             uint8_t* at8 = v + t * kHeadDim + (((tid >> 4) ^ (t & 7)) << 4) + (tid & 15);
             if ((have >> (t >> P.c.page_shift) & 1u) && (*at8 & 0x7f) == 0x7f) {
               const int f = t - first;
-              if (f < ctl.nan_from[part & 1][tid]) ctl.nan_from[part & 1][tid] = static_cast<uint8_t>(f);
+              if (f < ctl.nan_from[qb][tid]) ctl.nan_from[qb][tid] = static_cast<uint8_t>(f);
               *at8 = 0;
             }
           }
@@ -755,77 +840,35 @@ cache_attend_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_const
       if (pending) continue;
 
       // ---------------------------------------------------------- the end of a part
-      if (!take(it)) {
-        ok = false;
-        break;
-      }
-      if (P.q_tokens > 1) {
-        const int found = ctl.nan_from[part & 1][tid];
-        const int from = found == kNoNan ? INT32_MAX : at.len - P.q_tokens + 1 + found;
-#pragma unroll
-        for (int i = 0; i < N; ++i)
-          if (ctl.seen[part & 1][i0 + i] > from) acc[i] = __uint_as_float(0x7fc00000u);
-      }
-      // row sums over the tokens' threads: each step halves the rows that a lane has, then the lanes
-      {
-        int row = 0;
-#pragma unroll
-        for (int o = 16, c = N / 2; o > 0; o >>= 1, c >>= 1) {
-          const bool up = lane & o;
-          if (c > 0) {
-#pragma unroll
-            for (int i = 0; i < c; ++i) {
-              const float other = __shfl_xor_sync(0xffffffffu, up ? l[i] : l[i + c], o);
-              l[i] = (up ? l[i + c] : l[i]) + other;
-            }
-            row += up ? c : 0;
-          } else {
-            l[0] += __shfl_xor_sync(0xffffffffu, l[0], o);
-          }
-        }
-        if (lane % (32 / N) == 0) ctl.ref[half * 4 + quad][row].x = l[0];
-      }
-      meet_arrive();
-      if (!meet_wait()) {
-        ok = false;
-        break;
-      }
-      float sum = 0.f;   // lane i: row i's
-      if (lane < N)
-        sum = (ctl.ref[half * 4][lane].x + ctl.ref[half * 4 + 1][lane].x) +
-              (ctl.ref[half * 4 + 2][lane].x + ctl.ref[half * 4 + 3][lane].x);
-      if (part0 == at.first && x + 1 == at.first + at.tiles) {
-        const float inv = sum == 0.f ? 0.f : __frcp_rn(sum);
-#pragma unroll
-        for (int i = 0; i < N; ++i) {
-          const long long to = ctl.out_at[part & 1][i0 + i];
-          const float f = __shfl_sync(0xffffffffu, inv, i);
-          if (to >= 0) P.out[to + tid] = to_bf16(acc[i] * f);
-        }
-        if (P.lse && quad == 0 && lane < N && ctl.out_at[part & 1][i0 + lane] >= 0)
-          P.lse[ctl.lse_at[part & 1][i0 + lane]] = log_sum(m, sum);
-      } else {
-        // one of several parts of the block: left for the join. Slot 1 of the CTA is for a block's first part
-        // (its own last one), slot 0 for a later one (its own first)
-        float* dst = P.partial + (static_cast<int64_t>(blockIdx.x) * 2 + (part0 == at.first)) * kAttendPartWords +
-                     half * kPartWords;
-#pragma unroll
-        for (int i = 0; i < N; ++i) __stcg(dst + i * kHeadDim + tid, acc[i]);
-        if (quad == 0 && lane < N) {
-          __stcg(dst + N * kHeadDim + lane, m);
-          __stcg(dst + N * kHeadDim + N + lane, sum);
-        }
+      const End now = {part0 == at.first && x + 1 == at.first + at.tiles, part0 == at.first, at.len, part};
+      if (!now.whole) {
         if (tid == 0) ctl.split[2 * half + splits] = at;
         ++splits;
       }
-      __syncwarp();
-      if (lane == 0) mbar_arrive(&ctl.q_empty[part & 1]);
+      sum_rows(part);
+      if constexpr (kLate) {
+        end = now;
+        due = true;
+      } else {
+        meet_arrive();
+        if (!take(it) || !meet_wait()) {
+          ok = false;
+          break;
+        }
+        emit(now);
+        begin();
+      }
       if (x + 1 < x1) {
         next_block(P, blocks, at);
         ++part;
         part0 = x + 1;
-        ok = begin();
+        ok = rows_ready();
       }
+    }
+    if (kLate && ok && due) {
+      meet_arrive();
+      ok = take(n - 1) && meet_wait();
+      if (ok) emit(end);
     }
 
     // ------------------------------------------------------------ the join of blocks that several CTAs had parts of
