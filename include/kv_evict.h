@@ -433,7 +433,8 @@ kve_status kv_evict_cache_store(const kve_cache* cache, const uint16_t* k_new,
  * own:  out = sum_i softmax(q . k_i / sqrt(d)) v_i.  A query that sees nothing (len < T - t, an
  * empty sequence) gets zeros and lse = -inf. Rows of sequences behind n_seq are left as
  * they were. q, out [n_seq * T][Hq][d] bf16, 16-byte aligned, element strides {token, head}
- * (multiples of 8, not negative; NULL is dense; out's rows must not overlap). lse (or NULL)
+ * (multiples of 8, not negative; NULL is dense; out's rows must not overlap; out may be q
+ * with the same strides). lse (or NULL)
  * [n_seq * T][Hq] fp32: ln sum_i exp(q . k_i / sqrt(d)). The table and lens of every layer
  * are passed; layer picks. What the pages hold behind a sequence, NaN codes included, has
  * no part in its rows. A query row with an infinity or a NaN gives NaN. */

@@ -155,6 +155,14 @@ __global__ void __launch_bounds__(kPagesThreads) cache_pages_kernel(const __grid
       if (!s.out) continue;
       const int base = page >= 0 && page < np ? page << shift : -1;
       const int end = min(s.b, (j0 + 32) << shift);
+      if ((j0 << shift) >= s.a && end == (j0 + 32) << shift && __all_sync(0xffffffffu, base >= 0)) {
+        // 32 whole pages: P times 32 slots, nothing to check
+        int32_t* to = s.out + ((j0 << shift) - s.a) + lane;
+#pragma unroll 8
+        for (int k = lane; k < 32 << shift; k += 32, to += 32)
+          *to = __shfl_sync(0xffffffffu, base, k >> shift) + (k & page_mask);
+        continue;
+      }
 #pragma unroll 4
       for (int pos = j0 << shift; pos < end; pos += 32) {
         const int mine = pos + lane;

@@ -427,6 +427,8 @@ class Cache8:
         self.k, self.v = (self._buffer(t, shape, torch.uint8, device) for t in (k, v))
         self.k_scale, self.v_scale = (self._buffer(t, shape[:2], torch.float32, device) for t in (k_scale, v_scale))
         self._h = None
+        if self.k.device.type != "cuda":
+            raise ValueError("Cache8: the pages are device memory")
         cfg = CacheConfig(self.num_layers, self.num_q_heads, self.heads, self.head_dim, page_tokens, num_pages,
                           max_pages, max_seqs)
         handle, size = ctypes.c_void_p(), ctypes.c_size_t()
@@ -436,6 +438,7 @@ class Cache8:
         self._h, self._lib = handle, _lib()
         self.ws = torch.empty(size.value, dtype=torch.uint8, device=self.k.device)
         self._ws = self.ws.data_ptr()
+        self._seqs, self._entries = self.num_layers * max_seqs, self.num_layers * max_seqs * max_pages
         dev = self.k.device
         raw = getattr(torch._C, "_cuda_getCurrentRawStream", None)   # (no Stream object made: 2 us less a call)
         if raw is not None and dev.type == "cuda":
@@ -444,6 +447,9 @@ class Cache8:
         else:
             self._current_stream = lambda: torch.cuda.current_stream(dev).cuda_stream
         self.reset()
+
+    def _is_table(self, t) -> bool:
+        return t.numel() == self._entries and t.is_contiguous()
 
     def _stream(self, stream):
         """The stream's address; None is the current stream of the cache's device."""
@@ -487,9 +493,9 @@ class Cache8:
             if len(shape) != 2 or shape[0] != self.num_layers or not slots.is_contiguous():
                 raise ValueError("slots: expected a contiguous [num_layers, n] tensor")
             stride = shape[1]
-        seqs = self.num_layers * self.max_seqs
+        seqs = self._seqs
         for name, t, n in (("lens_from", lens_from, seqs), ("lens_to", lens_to, seqs), ("lens_out", lens_out, seqs),
-                           ("table", table, seqs * self.max_pages), ("free_pages", free_pages, self.num_pages),
+                           ("table", table, self._entries), ("free_pages", free_pages, self.num_pages),
                            ("ring_in", ring_in, 2), ("ring_out", ring_out, 2)):
             if t.numel() != n or not t.is_contiguous():
                 raise ValueError(f"{name}: expected {n} contiguous values")
@@ -505,6 +511,8 @@ class Cache8:
             dev = getattr(t, "device", None)
             if dev is not None and getattr(dev, "type", None) == "cpu" and not t.is_pinned():
                 raise ValueError(f"gather: {name} is a pageable CPU tensor; pin it or move it to the GPU")
+        if indices.numel() != plan.n_units * plan.spec["budget"] or not self._is_table(table):
+            raise ValueError("gather: indices are the plan's [n_units, budget], table is [num_layers, max_seqs, max_pages]")
         _check(self._lib.kv_evict_cache_gather(self._h, plan._h, k.data_ptr(), v.data_ptr(), indices.data_ptr(),
                                                first_seq, table.data_ptr(), self._ws, self._stream(stream)),
                "kv_evict_cache_gather")
@@ -528,6 +536,8 @@ class Cache8:
         if len(shape) != 4 or out.shape != shape or (lse is not None and
                                                      (lse.shape != shape[:3] or not lse.is_contiguous())):
             raise ValueError("attend: q and out are [n_seq, q_tokens, Hq, d], lse [n_seq, q_tokens, Hq]")
+        if not self._is_table(table) or lens.numel() != self._seqs or not lens.is_contiguous():
+            raise ValueError("attend: table is [num_layers, max_seqs, max_pages], lens [num_layers, max_seqs]")
         _check(self._lib.kv_evict_cache_attend(
             self._h, layer, shape[0], shape[1], q.data_ptr(), _row_strides(q, self.num_q_heads, "q"),
             table.data_ptr(), lens.data_ptr(), out.data_ptr(), _row_strides(out, self.num_q_heads, "out"), _ptr(lse),

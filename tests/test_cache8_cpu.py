@@ -187,6 +187,11 @@ def test_binding_refuses():
     assert K._row_strides(q, 8, "q") is None
     wide = torch.zeros((3, 2, 12, 128), dtype=torch.bfloat16)[:, :, 2:10]
     assert list(K._row_strides(wide, 8, "q")) == [12 * 128, 128]
+    one = torch.zeros((3, 1, 12, 128), dtype=torch.bfloat16)[:, :, 2:10]      # a token in each: theirs is the stride
+    assert list(K._row_strides(one, 8, "q")) == [12 * 128, 128]
+    assert list(K._row_strides(wide[:, 0], 8, "q")) == [24 * 128, 128]
     for bad in (q.float(), q[..., ::2], q.transpose(0, 1), q[:, :, :4]):
         with pytest.raises(ValueError):
             K._row_strides(bad, 8, "q")
+    with pytest.raises(ValueError):                                           # pages in host memory
+        K.Cache8(dict(num_layers=1, num_q_heads=8, num_kv_heads=2, head_dim=128), 2, 8, 4, 16, device="cpu")

@@ -523,6 +523,37 @@ def test_calls_on_another_stream_and_captured(K):
                               qn[l], want[0], want[1], want[2], want[3], tab[l], f[l], G)
 
 
+def test_out_may_be_the_queries(K):
+    rng = np.random.default_rng(30)
+    for G, t in ((4, 1), (4, 5)):
+        c, q, k, ks, v, vs, table, lens = _attention_case(K, rng, 32, G, 2, t, [3000, 5, 0, 700])
+        x = T.to_torch(q)
+        c.attend(x, _dev(table), _dev(lens), 0, x)
+        T.check_attention(x.float().cpu().numpy().astype(np.float64), None, q, k, ks, v, vs, table, lens, G)
+
+
+def test_binding_checks_what_it_is_given(K):
+    c = _cache(K, 8, 2, 16, 8, 4, 3)
+    table, lens, free, ring = c.state()
+    q = torch.zeros((3, 1, 8, 128), dtype=torch.bfloat16, device=DEV)
+    rows = torch.zeros((5, 2, 128), dtype=torch.bfloat16, device=DEV)
+    slots = torch.full((5,), -1, dtype=torch.int32, device=DEV)
+    bad = [lambda: c.attend(q, table[:, :2], lens, 0, q.clone()), lambda: c.attend(q, table, lens[:, :2], 0, q.clone()),
+           lambda: c.attend(q, table, lens, 0, q[:2].clone()), lambda: c.attend(q[0], table, lens, 0, q[0].clone()),
+           lambda: c.attend(q, table, lens, 0, q.clone(), torch.zeros((3, 8), device=DEV)),
+           lambda: c.store(rows, rows[:4], slots), lambda: c.store(rows, rows, slots[:4]),
+           lambda: c.pages(lens, lens, table, free[:7], ring, ring, lens),
+           lambda: c.pages(lens[:, :2], lens, table, free, ring, ring, lens),
+           lambda: c.pages(lens, lens, table, free, ring, ring, lens, slots)]
+    for call in bad:
+        with pytest.raises(ValueError):
+            call()
+    with pytest.raises(K.KvEvictError):
+        c.attend(q, table, lens, 1, q.clone())
+    with pytest.raises(K.KvEvictError):
+        c.attend(torch.zeros((4, 1, 8, 128), dtype=torch.bfloat16, device=DEV), table, lens, 0, torch.zeros_like(q).repeat(2, 1, 1, 1)[:4])
+
+
 def test_two_caches_at_once(K):
     """Two caches, each with its own workspace, on two streams at once."""
     rng = np.random.default_rng(28)
