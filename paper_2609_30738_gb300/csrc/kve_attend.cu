@@ -61,59 +61,6 @@ struct Block {
   int index;   // its number among all blocks that have tiles
 };
 
-template <int R, int H>
-struct ACtl {
-  uint64_t k_full[kKStages], k_empty[kKStages], v_full[kVStages], v_empty[kVStages];
-  uint64_t m_full[kVStages];                   // the scales beside a V stage
-  uint64_t s_full[2], q_full[ACfg<R, H>::kQBufs], q_empty[ACfg<R, H>::kQBufs];
-  uint64_t p_full, o_full, meet[H], joined[H], drain;
-  // of a tile's pages: the keys' scale, and the values' as 256 times a share of the tile's largest one
-  float ks[kVStages][kMostTilePages], vs[kVStages][kMostTilePages];
-  float vtop[kVStages];                        // that largest one / 256
-  uint32_t pages[kVStages];                    // bit j: page j of the tile holds tokens
-  static constexpr uint32_t kQBufs = ACfg<R, H>::kQBufs;
-  alignas(16) float red[2][4][R];              // row maxima of the warps, by tile parity
-  alignas(16) float2 ref[4 * H][R / H];        // of each warp's rows: the maximum, exp(old maximum - new)
-  float sum[kQBufs > 2 ? 2 : 1][4][R];         // row sums of the warps, at the end of a part (by its parity)
-  // of the rows of a part in each query buffer: log2(e) / sqrt(d) / the power of two in the q pieces; tokens
-  // that the row sees; where its output goes (elements of out, of lse), -1 for no row
-  alignas(16) float qs[kQBufs][R];
-  alignas(16) int seen[kQBufs][R];
-  long long out_at[kQBufs][R];
-  int lse_at[kQBufs][R];
-  uint8_t nan_from[kQBufs][kHeadDim];          // see there
-  Block split[2 * H];                          // parts left for the join, by half
-  int last[2 * H], split_cta[2 * H];           // its parts, if they are all written; the CTA of the first
-  Block first;                                 // the first part's block
-  int ends[2];                                 // this CTA's tiles of the line
-  int2 sums[ACfg<R, H>::kThreads / 32];        // tiles, sequences that have some
-  uint32_t tmem_base;
-  int abort, never;                            // never: stays 0 (waits that a given-up call still has to make)
-};
-
-template <int R, int H>
-constexpr size_t attend_smem() {
-  return ACfg<R, H>::kCtl + sizeof(ACtl<R, H>);
-}
-
-__device__ __forceinline__ int seq_len(const AttendParams& P, int r) {
-  return min(max(__ldg(P.lens + r), 0), P.c.max_pages << P.c.page_shift);
-}
-
-// The block behind b in the line; a tile follows, so a sequence that is not empty does.
-__device__ __forceinline__ void next_block(const AttendParams& P, int blocks, Block& b) {
-  b.first += b.tiles;
-  ++b.index;
-  if (++b.rb < blocks) return;
-  b.rb = 0;
-  if (++b.h < P.c.heads) return;
-  b.h = 0;
-  do {
-    b.len = seq_len(P, ++b.r);
-    b.tiles = (b.len + kTileKeys - 1) / kTileKeys;
-  } while (b.tiles == 0);
-}
-
 // How the line is cut. A part costs about kPartTiles tiles besides its own (its query rows, the tensor
 // cores' latency at its two ends, its output), so a block counts as its tiles and kPartTiles more units, and
 // the units are dealt evenly: CTA w's raw cut is floor(units * w / ctas). A cut that would leave fewer than
@@ -151,6 +98,60 @@ struct Cuts {
     *w1 = from(a + b.tiles - least + 1) - 1;
   }
 };
+
+template <int R, int H>
+struct ACtl {
+  uint64_t k_full[kKStages], k_empty[kKStages], v_full[kVStages], v_empty[kVStages];
+  uint64_t m_full[kVStages];                   // the scales beside a V stage
+  uint64_t s_full[2], q_full[ACfg<R, H>::kQBufs], q_empty[ACfg<R, H>::kQBufs];
+  uint64_t p_full, o_full, meet[H], joined[H], drain;
+  // of a tile's pages: the keys' scale, and the values' as 256 times a share of the tile's largest one
+  float ks[kVStages][kMostTilePages], vs[kVStages][kMostTilePages];
+  float vtop[kVStages];                        // that largest one / 256
+  uint32_t pages[kVStages];                    // bit j: page j of the tile holds tokens
+  static constexpr uint32_t kQBufs = ACfg<R, H>::kQBufs;
+  alignas(16) float red[2][4][R];              // row maxima of the warps, by tile parity
+  alignas(16) float2 ref[4 * H][R / H];        // of each warp's rows: the maximum, exp(old maximum - new)
+  float sum[kQBufs > 2 ? 2 : 1][4][R];         // row sums of the warps, at the end of a part (by its parity)
+  // of the rows of a part in each query buffer: log2(e) / sqrt(d) / the power of two in the q pieces; tokens
+  // that the row sees; where its output goes (elements of out, of lse), -1 for no row
+  alignas(16) float qs[kQBufs][R];
+  alignas(16) int seen[kQBufs][R];
+  long long out_at[kQBufs][R];
+  int lse_at[kQBufs][R];
+  uint8_t nan_from[kQBufs][kHeadDim];          // see there
+  Block split[2];                              // parts left for the join (each half writes the same)
+  int last[2 * H], split_cta[2 * H];           // its parts, if they are all written; the CTA of the first
+  Block blocks[kQBufs];                        // of the part in each query buffer; [0] first of the first part
+  Cuts cuts;
+  int ends[2];                                 // this CTA's tiles of the line
+  int2 sums[ACfg<R, H>::kThreads / 32];        // tiles, sequences that have some
+  uint32_t tmem_base;
+  int abort, never;                            // never: stays 0 (waits that a given-up call still has to make)
+};
+
+template <int R, int H>
+constexpr size_t attend_smem() {
+  return ACfg<R, H>::kCtl + sizeof(ACtl<R, H>);
+}
+
+__device__ __forceinline__ int seq_len(const AttendParams& P, int r) {
+  return min(max(__ldg(P.lens + r), 0), P.c.max_pages << P.c.page_shift);
+}
+
+// The block behind b in the line; a tile follows, so a sequence that is not empty does.
+__device__ __forceinline__ void next_block(const AttendParams& P, int blocks, Block& b) {
+  b.first += b.tiles;
+  ++b.index;
+  if (++b.rb < blocks) return;
+  b.rb = 0;
+  if (++b.h < P.c.heads) return;
+  b.h = 0;
+  do {
+    b.len = seq_len(P, ++b.r);
+    b.tiles = (b.len + kTileKeys - 1) / kTileKeys;
+  } while (b.tiles == 0);
+}
 
 // The power of two that brings the largest magnitude (bf16 bits a, finite) into [128, 256), as fp32 bits.
 __device__ __forceinline__ uint32_t piece_scale(uint32_t a) {
@@ -297,9 +298,10 @@ cache_attend_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_const
   const long long all_units = (static_cast<long long>(all_tiles) + all_filled * kPartTiles) * per_seq;
   const bool too_long = all_tiles >= 1 << 30 || all_units >= 1 << 30;
   if ((bad || too_long) && blockIdx.x == 0) atomicOr(P.err, kErrCheck);
-  Cuts cuts;
+  Cuts cuts;   // (in shared memory for the join: no registers' business in between)
   const int units = too_long ? 0 : static_cast<int>(all_units);
   cuts.set(units, max(min(max(units / kLeastUnits, all_filled * per_seq), static_cast<int>(gridDim.x)), 1));
+  if (threadIdx.x == 0) ctl.cuts = cuts;
   if (cuts.units > 0 && static_cast<int>(blockIdx.x) < cuts.ctas) {
     // the thread that holds a cut's sequence says which tile of the line it is
     const int c0 = cuts.raw(blockIdx.x), c1 = cuts.raw(blockIdx.x + 1);
@@ -327,7 +329,7 @@ cache_attend_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_const
           if (b == per_seq) {   // behind the sequence: the next one that is not empty, if there is one
             f.r = -1 - r;
           }
-          ctl.first = f;
+          ctl.blocks[0] = f;
         }
       }
       at += tiles * per_seq;
@@ -339,17 +341,17 @@ cache_attend_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_const
   __syncthreads();
   const int x0 = ctl.ends[0], x1 = ctl.ends[1];
   const bool works = x0 < x1;
-  if (works && ctl.first.r < 0) {   // (for all threads)
+  if (works && ctl.blocks[0].r < 0) {   // (for all threads)
     __syncthreads();
     if (threadIdx.x == 0) {
-      Block f = ctl.first;
+      Block f = ctl.blocks[0];
       f.r = -1 - f.r;
       f.h = f.rb = 0;
       do {
         f.len = seq_len(P, ++f.r);
         f.tiles = (f.len + kTileKeys - 1) / kTileKeys;
       } while (f.tiles == 0);
-      ctl.first = f;
+      ctl.blocks[0] = f;
     }
     __syncthreads();
   }
@@ -388,7 +390,7 @@ cache_attend_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_const
         }
         return f;
       };
-      Ahead now = step({ctl.first, x0 - 1, -1, false});
+      Ahead now = step({ctl.blocks[0], x0 - 1, -1, false});
       Ahead then = step(now);
       float2 sc = scales(now);
       const uint32_t n = x1 - x0;
@@ -442,20 +444,18 @@ cache_attend_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_const
     if (works && lane == 0) {
       const uint32_t kaddr = smem_u32(smem), qaddr = kaddr + static_cast<uint32_t>(C::kQ);
       const uint32_t paddr = kaddr + static_cast<uint32_t>(C::kP);
-      Block at = ctl.first;
+      int end = x0;               // of the part's block
       const uint32_t n = x1 - x0;
-      uint32_t part = 0;
+      uint32_t part = 0xffffffffu;
       // S^T of tile `it`; it runs two tiles ahead of the probabilities
       const auto scores = [&](uint32_t it) -> bool {
         const int x = x0 + static_cast<int>(it);
         const uint32_t st = it % kKStages;
-        const bool fresh = x == at.first + at.tiles;
-        if (fresh) {
-          next_block(P, blocks, at);
+        if (x == end) {
           ++part;
+          if (!mbar_wait(&ctl.q_full[part % C::kQBufs], (part / C::kQBufs) & 1, P.wait_limit_ns, &ctl.abort)) return false;
+          end = ctl.blocks[part % C::kQBufs].first + ctl.blocks[part % C::kQBufs].tiles;
         }
-        if ((it == 0 || fresh) &&
-            !mbar_wait(&ctl.q_full[part % C::kQBufs], (part / C::kQBufs) & 1, P.wait_limit_ns, &ctl.abort)) return false;
         if (!mbar_wait(&ctl.k_full[st], (it / kKStages) & 1, P.wait_limit_ns, &ctl.abort)) return false;
         tc_fence_after();
         const uint64_t a = sw128_desc(kaddr + st * kTileBytes);
@@ -466,7 +466,7 @@ cache_attend_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_const
           tc_mma_e4m3(d, a + 2 * j, b + 2 * j, C::kIdescS, j > 0);
         tc_commit(&ctl.k_empty[st]);
         tc_commit(&ctl.s_full[it & 1]);
-        if (x + 1 == x1 || x + 1 == at.first + at.tiles) tc_commit(&ctl.q_empty[part % C::kQBufs]);
+        if (x + 1 == x1 || x + 1 == end) tc_commit(&ctl.q_empty[part % C::kQBufs]);
         return true;
       };
       bool ok = scores(0) && (n == 1 || scores(1));
@@ -503,7 +503,7 @@ cache_attend_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_const
         for (int i = threadIdx.x - 64; i < (C::kNs - 2 * R) * kHeadDim / 4; i += 64)
           for (int k = 0; k < C::kQBufs; ++k) reinterpret_cast<uint32_t*>(qbuf + k * C::kQBytes + 2 * R * kHeadDim)[i] = 0;
       }
-      Block at = ctl.first;
+      Block at = ctl.blocks[0];
       for (uint32_t part = 0;; ++part) {
         const uint32_t qb = part % C::kQBufs;
         if (part >= C::kQBufs &&
@@ -511,6 +511,7 @@ cache_attend_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_const
           if (lane == 0) fail();
           break;
         }
+        if (part > 0 && warp == 2 && lane == 0) ctl.blocks[qb] = at;
         uint4 x[R / 4];
 #pragma unroll
         for (int k = 0; k < R / 4; ++k) {
@@ -585,10 +586,10 @@ cache_attend_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_const
     const auto meet_wait = [&]() -> bool {
       return warp_wait(&ctl.meet[half], met++ & 1u, P.wait_limit_ns, &ctl.abort);
     };
-    Block at = ctl.first;
+    int len = 0, block0 = 0, block1 = 0;   // the part's sequence, its block's tiles of the line
     const uint32_t n = x1 - x0;
     uint32_t part = 0;
-    int part0 = x0, splits = 0;
+    int splits = 0;
     struct End {
       bool whole, first;   // the part is its whole block; its block's first part
       int len;
@@ -596,7 +597,7 @@ cache_attend_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_const
     };
     bool ok = true;
     float m = -INFINITY;                 // lane i: row i's maximum so far
-    float l[N], acc[N], keep[N];         // keep: exp(old maximum - new) of the last tile
+    float l[N], acc[N];
     float back = 0.f;                    // the last tile's scale of O^T
     // adds tile `it`'s O^T
     const auto take = [&](uint32_t it) -> bool {
@@ -614,7 +615,7 @@ cache_attend_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_const
 #pragma unroll
       for (int i = 0; i < N; ++i) {
         const float y = fmaf(fmaf(o[2 * N + i], 0.0625f, o[N + i]), 0.0625f, o[i]);
-        acc[i] = fmaf(y, back, acc[i] * keep[i]);
+        acc[i] = fmaf(y, back, acc[i]);
       }
       return true;
     };
@@ -625,7 +626,12 @@ cache_attend_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_const
     };
     const auto rows_ready = [&]() -> bool {   // of a new part
       if (half == 0) ctl.nan_from[part % C::kQBufs][tid] = kNoNan;
-      return warp_wait(&ctl.q_full[part % C::kQBufs], (part / C::kQBufs) & 1, P.wait_limit_ns, &ctl.abort);
+      if (!warp_wait(&ctl.q_full[part % C::kQBufs], (part / C::kQBufs) & 1, P.wait_limit_ns, &ctl.abort)) return false;
+      const Block& b = ctl.blocks[part % C::kQBufs];
+      len = b.len;
+      block0 = b.first;
+      block1 = b.first + b.tiles;
+      return true;
     };
     // The end of a part, first half: the row sums over the tokens' threads, each step halving the rows that a
     // lane has, then the lanes. They are everybody's behind the next meeting.
@@ -699,14 +705,14 @@ cache_attend_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_const
     for (uint32_t it = 0; ok && it < n; ++it) {
       const int x = x0 + static_cast<int>(it);
       const uint32_t st = it % kVStages, qb = part % C::kQBufs;
-      const int pos = (x - at.first) * kTileKeys + tid;
+      const int pos = (x - block0) * kTileKeys + tid;
       if (!warp_wait(&ctl.m_full[st], (it / kVStages) & 1, P.wait_limit_ns, &ctl.abort)) {
         ok = false;
         break;
       }
       const int pg = tid >> P.c.page_shift;
       const uint32_t have = ctl.pages[st];
-      const bool held = (have >> pg & 1u) && pos < at.len;
+      const bool held = (have >> pg & 1u) && pos < len;
       const float ks = ctl.ks[st][pg];
       const float vrest = held ? ctl.vs[st][pg] : 0.f, vtop = ctl.vtop[st];
       if (!warp_wait(&ctl.s_full[it & 1], (it >> 1) & 1, P.wait_limit_ns, &ctl.abort)) {
@@ -729,8 +735,8 @@ cache_attend_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_const
         for (int i = 0; i < N; ++i) w[i] = fmaf(s[N + i], 0.0625f, s[i]) * ctl.qs[qb][i0 + i] * ks;
       }
       const int tile0 = pos - tid, tile_end = tile0 + kTileKeys;
-      const bool whole = have == (0xffu >> (kMostTilePages - (kTileKeys >> P.c.page_shift))) && tile_end <= at.len;
-      const bool some = P.q_tokens > 1 && tile_end > at.len - P.q_tokens + 1;   // tokens that not all rows see
+      const bool whole = have == (0xffu >> (kMostTilePages - (kTileKeys >> P.c.page_shift))) && tile_end <= len;
+      const bool some = P.q_tokens > 1 && tile_end > len - P.q_tokens + 1;   // tokens that not all rows see
       if (!whole || some) {
 #pragma unroll
         for (int i = 0; i < N; ++i)
@@ -772,7 +778,7 @@ cache_attend_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_const
       for (int i = 0; i < N; ++i) {
         const float2 r = ctl.ref[half * 4 + quad][i];
         const float p = ex2(w[i] - r.x);
-        keep[i] = r.y;
+        acc[i] *= r.y;   // (the tile before is in it; this one's product comes later)
         l[i] = fmaf(l[i], r.y, p);
         w[i] = p * vrest;
       }
@@ -821,7 +827,7 @@ cache_attend_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_const
           // nor may a NaN value that later rows see reach the earlier ones: it is taken out here, and given to
           // the rows that see it when the part ends. nan_from: the first position with a NaN in this
           // column, counted from the first one that not every row sees
-          const int first = at.len - P.q_tokens + 1 - tile0, t0 = max(first, 0), t1 = min(at.len - tile0, kTileKeys);
+          const int first = len - P.q_tokens + 1 - tile0, t0 = max(first, 0), t1 = min(len - tile0, kTileKeys);
           for (int t = t0; t < t1; ++t) {
             uint8_t* at8 = v + t * kHeadDim + (((tid >> 4) ^ (t & 7)) << 4) + (tid & 15);
             if ((have >> (t >> P.c.page_shift) & 1u) && (*at8 & 0x7f) == 0x7f) {
@@ -836,13 +842,13 @@ cache_attend_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_const
       tc_fence_before();
       __syncwarp();
       if (lane == 0) mbar_arrive(&ctl.p_full);
-      pending = !(x + 1 == x1 || x + 1 == at.first + at.tiles);
+      pending = !(x + 1 == x1 || x + 1 == block1);
       if (pending) continue;
 
       // ---------------------------------------------------------- the end of a part
-      const End now = {part0 == at.first && x + 1 == at.first + at.tiles, part0 == at.first, at.len, part};
+      const End now = {block0 >= x0 && block1 <= x1, block0 >= x0, len, part};
       if (!now.whole) {
-        if (tid == 0) ctl.split[2 * half + splits] = at;
+        if (tid == 0) ctl.split[splits] = ctl.blocks[qb];
         ++splits;
       }
       sum_rows(part);
@@ -859,9 +865,7 @@ cache_attend_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_const
         begin();
       }
       if (x + 1 < x1) {
-        next_block(P, blocks, at);
         ++part;
-        part0 = x + 1;
         ok = rows_ready();
       }
     }
@@ -877,7 +881,7 @@ cache_attend_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_const
     allow_next_kernel();
     if (ok && splits > 0) {
       int w0 = 0, w1 = 0;
-      if (tid < splits) cuts.parts(ctl.split[2 * half + tid], &w0, &w1);
+      if (tid < splits) ctl.cuts.parts(ctl.split[tid], &w0, &w1);
       meet_arrive();
       ok = meet_wait();
       if (ok && tid < splits)
@@ -897,7 +901,7 @@ cache_attend_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_const
       for (int k = 0; ok && k < splits; ++k) {
         const int parts = ctl.last[2 * half + k];
         if (parts == 0) continue;
-        const Block b = ctl.split[2 * half + k];
+        const Block b = ctl.split[k];
         const int first = ctl.split_cta[2 * half + k];
         float top[N / 4], sum[N / 4];
         float4 a4[N / 4];
