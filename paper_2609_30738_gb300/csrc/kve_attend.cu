@@ -603,19 +603,33 @@ cache_attend_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_const
     const auto take = [&](uint32_t it) -> bool {
       if (!warp_wait(&ctl.o_full, it & 1, P.wait_limit_ns, &ctl.abort)) return false;
       tc_fence_after();
-      float o[N == 4 ? 16 : 3 * N];
-      if constexpr (H == 1 && N == 4) {
-        tmem_ld16(tmem + C::kOCol + my_lanes, o);
+      if constexpr (H == 1) {
+        float o[N == 4 ? 16 : 3 * N];
+        if constexpr (N == 4) {
+          tmem_ld16(tmem + C::kOCol + my_lanes, o);
+        } else {
+          static_assert(N == 8, "three loads of 8 columns");
+#pragma unroll
+          for (int k = 0; k < 3; ++k) tmem_ld8(tmem + C::kOCol + k * R + my_lanes, o + k * N);
+        }
+        tmem_wait_ld(o);
+#pragma unroll
+        for (int i = 0; i < N; ++i) {
+          const float y = fmaf(fmaf(o[2 * N + i], 0.0625f, o[N + i]), 0.0625f, o[i]);
+          acc[i] = fmaf(y, back, acc[i]);
+        }
       } else {
-        static_assert(N == 8, "three loads of 8 columns");
+        static_assert(N == 8, "a load of 8 columns a piece");
+        float f = back;
 #pragma unroll
-        for (int k = 0; k < 3; ++k) tmem_ld8(tmem + C::kOCol + k * R + i0 + my_lanes, o + k * N);
-      }
-      tmem_wait_ld(o);
+        for (int k = 0; k < 3; ++k) {   // (one after the other: 80 registers, and together they spill)
+          float o[N];
+          tmem_ld8(tmem + C::kOCol + k * R + i0 + my_lanes, o);
+          tmem_wait_ld(o);
 #pragma unroll
-      for (int i = 0; i < N; ++i) {
-        const float y = fmaf(fmaf(o[2 * N + i], 0.0625f, o[N + i]), 0.0625f, o[i]);
-        acc[i] = fmaf(y, back, acc[i]);
+          for (int i = 0; i < N; ++i) acc[i] = fmaf(o[i], f, acc[i]);
+          f *= 0.0625f;
+        }
       }
       return true;
     };
