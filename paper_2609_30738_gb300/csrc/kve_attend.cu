@@ -17,6 +17,16 @@
 // Statistics, sums and the output accumulate in fp32 registers: a tile's O^T is added to them scaled by
 // exp(old maximum - new), so TMEM holds one tile's products and is never rescaled.
 //
+// Warps: the TMA producer (pages two tiles and scales one tile ahead), the MMA issuer (scores two tiles ahead of
+// the value product), two that quantise the next block's query rows, and four softmax warps, eight for 16 rows
+// (a thread is a token and 4 or 8 rows, then a column of the output). Two CTAs an SM, 96 KB of tiles each: with
+// three V stages instead of four 16 rows take 73 us instead of 57 on 131072 tokens.
+//
+// Measured (device): 64 sequences of 512 to 16384 tokens, 446 MB, 74.9 us = 88% of the HBM peak; one of 131072,
+// 269 MB, 47.6 us = 83%, 8 us of them the start (lengths, cut, first tiles) and the join of 38 parts a head; 24 of
+// 500 to 8192 with 4 drafts each (16 rows), 125 MB, 33.0 us = 56%, bound by the softmax warps' instructions;
+// 16 of 96 to 700 8.4 us; one of 96 5.1 us, a chain of latencies.
+//
 // The work is cut over the tokens: all (sequence, head, row block)s' tiles in one line, an equal share of it
 // for each of two CTAs an SM, whatever the lengths (the lengths are read on the GPU: a captured call serves
 // every later length). A block that falls to several CTAs is joined by the one that finishes last, from
@@ -48,7 +58,9 @@ struct ACfg {
   static constexpr uint32_t kIdescO = idesc_e4m3_f32(128, kNp, true);
   static constexpr size_t kV = size_t(kKStages) * kTileBytes;
   static constexpr size_t kQ = kV + size_t(kVStages) * kTileBytes;
-  static constexpr uint32_t kQBufs = R > 8 ? 2 : 4;  // blocks whose query rows are held, by part
+  // blocks whose query rows are held, by part: four where they fit, so that batches of short sequences do not wait
+  // for them (1000 of 64 tokens: 57 us against 78 with two)
+  static constexpr uint32_t kQBufs = R > 8 ? 2 : 4;
   static constexpr size_t kQBytes = kNs * kHeadDim;
   static constexpr size_t kP = kQ + kQBufs * kQBytes;
   static constexpr size_t kCtl = kP + kNp * kTileKeys;
@@ -66,8 +78,10 @@ struct Block {
 // the units are dealt evenly: CTA w's raw cut is floor(units * w / ctas). A cut that would leave fewer than
 // `least` tiles of a block on one of its sides moves to that end of the block: a join costs more than those
 // tiles do. That is 4 tiles where a share is 8 units at most and 2 where it is longer and evenness counts
-// for more: 16 sequences of 96 to 700 tokens take 9.0 us with 4 against 10.0 with 2 and 11.3 with 1, 24 of
-// 500 to 8192 with 4 drafts each (share 16) 40.1 with 4 against 37.1 with 2 and with 1. No more CTAs take part than have kLeastUnits each, or a block.
+// for more: 16 sequences of 96 to 700 tokens take 8.4 us with 4 against 9.3 with 2 and 10.6 with 1, 24 of 500
+// to 8192 with 4 drafts each (a share of 16) 35.8 with 4 against 33.0 with 2. With kPartTiles = 0 they take
+// 10.5 and 35.5, and 64 sequences of 512 to 16384 79.9 instead of 75. No more CTAs take part than have
+// kLeastUnits each, or a block.
 constexpr int kPartTiles = 2, kLeastUnits = 4;
 
 struct Cuts {
