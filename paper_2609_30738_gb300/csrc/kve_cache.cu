@@ -20,6 +20,7 @@ namespace {
 // ---------------------------------------------------------------- tables and slots
 
 constexpr int kPagesThreads = 1024;
+constexpr int64_t kPagesCtas = 152;   // one an SM: pages and slots of 48 prompts in 32 layers 19.1 us, with 76 38.0, with 304 22.5
 constexpr int kPagesWarps = kPagesThreads / 32;
 static_assert(kPagesWarps == 32, "a lane a sequence of the CTA");
 
@@ -293,14 +294,8 @@ __device__ __forceinline__ void team_sync() {
     __syncwarp();
 }
 
-// Writes rows [off, off + n) of a page (codes and scale of one head); x[i] holds this lane's 8
-// elements of page row 16 g + i, zero outside the run. Every thread of the team comes here.
-template <int kPage>
-__device__ __forceinline__ void write_run(const uint4 (&x)[kGroupRows], int off, int n, uint8_t* codes, float* scale,
-                                          uint32_t* team_max) {
-  constexpr int kGroups = kPage / kGroupRows;
-  const int lane = threadIdx.x & 15, g = (threadIdx.x / 16) % kGroups;
-  const uint32_t lanes = threadIdx.x & 16 ? 0xffff0000u : 0x0000ffffu;
+// The largest finite magnitude of a group's rows (8 elements of each a lane), as bf16 bits, in all its lanes.
+__device__ __forceinline__ uint32_t group_max(const uint4 (&x)[kGroupRows], uint32_t lanes) {
   uint32_t m = 0;
 #pragma unroll
   for (int i = 0; i < kGroupRows; ++i) m = max_abs(m, max_abs(max_abs(x[i].x, x[i].y), max_abs(x[i].z, x[i].w)));
@@ -315,6 +310,37 @@ __device__ __forceinline__ void write_run(const uint4 (&x)[kGroupRows], int off,
   m = max(m & 0xffffu, m >> 16);
 #pragma unroll
   for (int o = 8; o > 0; o >>= 1) m = max(m, __shfl_xor_sync(lanes, m, o));
+  return m;
+}
+
+// Rows row0 .. end - 1 of a page to a scale that is 1 / f of theirs (their rounding again only where they become
+// subnormal), four in flight: beside the rows to be written there is no room for more.
+__device__ __forceinline__ void shrink_rows(uint8_t* codes, int row0, int end, float f, int lane) {
+  constexpr int kBatch = 4;
+#pragma unroll 1
+  for (; row0 < end; row0 += kBatch) {
+    uint2 c[kBatch];
+#pragma unroll
+    for (int i = 0; i < kBatch; ++i)
+      if (row0 + i < end) c[i] = reinterpret_cast<const uint2*>(codes + (row0 + i) * kHeadDim)[lane];
+#pragma unroll
+    for (int i = 0; i < kBatch; ++i)
+      if (row0 + i < end) {
+        c[i].x = scaled_codes(c[i].x & 0xffffu, f) | scaled_codes(c[i].x >> 16, f) << 16;
+        c[i].y = scaled_codes(c[i].y & 0xffffu, f) | scaled_codes(c[i].y >> 16, f) << 16;
+        reinterpret_cast<uint2*>(codes + (row0 + i) * kHeadDim)[lane] = c[i];
+      }
+  }
+}
+
+// Writes rows [off, off + n) of a page (codes and scale of one head); x[i] holds this lane's 8
+// elements of page row kGroupRows g + i, zero outside the run. Every thread of the team comes here.
+template <int kPage>
+__device__ __forceinline__ void write_run(const uint4 (&x)[kGroupRows], int off, int n, uint8_t* codes, float* scale,
+                                          uint32_t* team_max) {
+  constexpr int kGroups = kPage / kGroupRows;
+  const int lane = threadIdx.x & 15, g = (threadIdx.x / 16) % kGroups;
+  uint32_t m = group_max(x, threadIdx.x & 16 ? 0xffff0000u : 0x0000ffffu);
   // the page's scale is read before it is written: every group reads, then all meet
   const float held = off > 0 ? *scale : 0.f;
   if (lane == 0) team_max[g] = m;
@@ -323,25 +349,30 @@ __device__ __forceinline__ void write_run(const uint4 (&x)[kGroupRows], int off,
   for (int i = 0; i < kGroups; ++i) m = max(m, team_max[i]);
   const float s = fmaxf(held, __uint_as_float(need_bits(m)));
   const float inv = __frcp_rn(s);   // exact: a power of two
-  if (s > held && off > 0) {
-    // older rows to the larger scale (their rounding again only where they become subnormal)
-    const float f = held * inv;
-    for (int i = 0; i < kGroupRows; ++i) {
-      const int row = g * kGroupRows + i;
-      if (row >= off) break;
-      uint2* at = reinterpret_cast<uint2*>(codes + row * kHeadDim) + lane;
-      uint2 c = *at;
-      c.x = scaled_codes(c.x & 0xffffu, f) | scaled_codes(c.x >> 16, f) << 16;
-      c.y = scaled_codes(c.y & 0xffffu, f) | scaled_codes(c.y >> 16, f) << 16;
-      *at = c;
-    }
-  }
+  if (s > held && off > 0) shrink_rows(codes, g * kGroupRows, min((g + 1) * kGroupRows, off), held * inv, lane);
 #pragma unroll
   for (int i = 0; i < kGroupRows; ++i) {
     const int row = g * kGroupRows + i;
     if (static_cast<uint32_t>(row - off) < static_cast<uint32_t>(n)) reinterpret_cast<uint2*>(codes + row * kHeadDim)[lane] = row_codes(x[i], inv);
   }
   if (g == 0 && lane == 0) *scale = s;
+}
+
+// The same by one group, for a run of at most kGroupRows rows: x[i] is page row off + i, zero behind the run.
+__device__ __forceinline__ void write_short_run(const uint4 (&x)[kGroupRows], int off, int n, uint8_t* codes,
+                                                float* scale) {
+  const int lane = threadIdx.x & 15;
+  const uint32_t lanes = threadIdx.x & 16 ? 0xffff0000u : 0x0000ffffu;
+  const float held = off > 0 ? *scale : 0.f;
+  const uint32_t m = group_max(x, lanes);
+  __syncwarp(lanes);   // all have read the scale
+  const float s = fmaxf(held, __uint_as_float(need_bits(m)));
+  const float inv = __frcp_rn(s);
+  if (s > held) shrink_rows(codes, 0, off, held * inv, lane);
+#pragma unroll
+  for (int i = 0; i < kGroupRows; ++i)
+    if (i < n) reinterpret_cast<uint2*>(codes + (off + i) * kHeadDim)[lane] = row_codes(x[i], inv);
+  if (lane == 0) *scale = s;
 }
 
 // Step 4 into the cache. A team takes page j of a unit, keys or values (the two alternate).
@@ -392,15 +423,31 @@ __global__ void __launch_bounds__(kRowThreads<kPage>) cache_gather_kernel(const 
   allow_next_kernel();
 }
 
-// New tokens by slot. A team takes `block` consecutive tokens of one head, keys or values, and writes
-// the runs that start among them one after the other: 1 where the calls of a decode step have a token a
-// sequence, P where whole prompts have a run every P tokens.
+// New tokens by slot. A team takes `block` consecutive tokens (P, or P / 8) of one head, keys or values, and writes
+// the runs that start among them: one after the other by the whole team where they are long (a prompt's, a page
+// each), all at once by a group each where they are short (a decode step's tokens, drafts). Every warp lists the
+// runs by itself from the slots, a lane a token: a token continues a run where its slot is the one behind its
+// predecessor's on the same page. Runs of up to kGroupRows rows fit a group's registers and are short.
+//
+// A block of P / 8 tokens gives a small call more teams, one of P tokens a large one fewer scans (P = 64, P / 8
+// against P, us): 256 sequences x 1 token 3.3 and 11.1, 1000 x 1 7.3 and 11.5, 1000 x 2 9.3 and 8.2, 1000 x 8 29.1
+// and 12.6; one prompt of 512 3.4 and 2.9, of 1024 4.9 and 3.2, of 4096 11.8 and 5.3. P = 16: 3.5 and 13.4, 7.3 and
+// 13.9, 12.7 and 8.8, 28.4 and 13.3; 3.9 and 3.1, 5.3 and 3.4, 12.5 and 5.8. So P from 1024 tokens on. Decode steps
+// of 16 and 256 sequences (8 heads) take 2.6 and 3.4 us, mostly the launch and three loads in a row (slots, scale,
+// rows); a team a token with the runs found from 16 lanes took 2.9 and 4.15.
+constexpr int64_t kStoreBlockTokens = 1024;
+
 template <int kPage>
-__global__ void __launch_bounds__(kRowThreads<kPage>, 1024 / kRowThreads<kPage>) cache_store_kernel(const __grid_constant__ CacheStoreParams P) {
+__global__ void __launch_bounds__(kRowThreads<kPage>, 1024 / kRowThreads<kPage>)
+cache_store_kernel(const __grid_constant__ CacheStoreParams P) {
   wait_previous_kernel();
   constexpr int kTeam = kTeamThreads<kPage>, kGroups = kPage / kGroupRows, kTeams = kRowThreads<kPage> / kTeam;
+  constexpr int kWords = kPage / 16;   // of 32 tokens: a block of at most P and the run that leaves it
   __shared__ uint32_t team_max[kTeams][kGroups];
+  __shared__ uint32_t goes_on[kRowThreads<kPage> / 32][kWords];
+  __shared__ uint16_t runs[kRowThreads<kPage> / 32][kPage];   // first token << 8 | tokens: long, from the end short
   const int team = threadIdx.x / kTeam, lane = threadIdx.x & 15, g = (threadIdx.x / 16) % kGroups;
+  const int warp = threadIdx.x >> 5, lane32 = threadIdx.x & 31;
   const int64_t item = static_cast<int64_t>(blockIdx.x) * kTeams + team;
   const int H = P.c.heads;
   const int64_t first = item / (2 * H) * P.block;
@@ -409,59 +456,90 @@ __global__ void __launch_bounds__(kRowThreads<kPage>, 1024 / kRowThreads<kPage>)
   const bool values = hv & 1;
   const uint16_t* from = (values ? P.v + h * P.v_sh : P.k + h * P.k_sh);
   const int64_t st = values ? P.v_st : P.k_st;
-  const uint32_t lanes = threadIdx.x & 16 ? 0xffff0000u : 0x0000ffffu;
-  const int64_t limit = static_cast<int64_t>(P.c.num_pages) * kPage;
-  const int64_t last = min(first + P.block, P.n_tokens);
-  for (int64_t t = first; t < last;) {
-    // the next token that starts a run, 16 at a time
-    const int64_t i16 = t + lane;
-    const int here = i16 < last ? __ldg(P.slots + i16) : -1, prev = i16 > 0 && i16 < last ? __ldg(P.slots + i16 - 1) : -1;
-    const bool starts = here >= 0 && (prev < 0 || here != prev + 1 || here % kPage == 0);
-    const uint32_t found = (__ballot_sync(lanes, starts) >> (threadIdx.x & 16)) & 0xffffu;
-    if (!found) {
-      t += 16;
-      continue;
+  uint8_t* const codes = values ? P.c.v : P.c.k;
+  float* const scales = values ? P.c.v_scale : P.c.k_scale;
+  const int32_t* slots = P.slots + first;
+  const int64_t left = P.n_tokens - first;
+  // the slots of the block and of what a run can reach behind it
+  int longs = 0, shorts = 0;
+  {
+    int here[kWords];
+#pragma unroll
+    for (int c = 0; c < kWords; ++c) here[c] = 32 * c + lane32 < left ? __ldg(slots + 32 * c + lane32) : -1;
+    int before = first > 0 ? __ldg(slots - 1) : -1;
+    constexpr int kFirst = kPage > 32 ? kPage / 32 : 1;   // words of the block
+    uint32_t begins[kFirst];
+#pragma unroll
+    for (int c = 0; c < kWords; ++c) {
+      int prev = __shfl_up_sync(0xffffffffu, here[c], 1);
+      if (lane32 == 0) prev = before;
+      before = __shfl_sync(0xffffffffu, here[c], 31);
+      const bool on = here[c] >= 0 && prev >= 0 && here[c] - prev == 1 && (here[c] & (kPage - 1)) != 0;
+      const uint32_t word = __ballot_sync(0xffffffffu, on);
+      if (lane32 == 0) goes_on[warp][c] = word;
+      const uint32_t b = __ballot_sync(0xffffffffu, here[c] >= 0 && !on && 32 * c + lane32 < P.block);
+      if (c < kFirst) begins[c] = b;
     }
-    t += __ffs(found) - 1;
-    const int slot = __shfl_sync(lanes, here, __ffs(found) - 1, 16);
+    __syncwarp();
+#pragma unroll
+    for (int c = 0; c < kFirst; ++c) {
+      if (begins[c] == 0) continue;
+      const bool mine = begins[c] >> lane32 & 1u;
+      const int t = 32 * c + lane32;
+      int n = 1;   // tokens of the run that starts here: those that go on without a gap
+      if (mine)
+        for (int p = t + 1; p < 32 * kWords;) {
+          const uint32_t gap = ~(goes_on[warp][p >> 5] >> (p & 31));
+          const int ones = min(gap ? __ffs(gap) - 1 : 32, 32 - (p & 31));
+          n += ones;
+          p += ones;
+          if ((p & 31) != 0 || ones == 0) break;
+        }
+      const bool is_long = mine && n > kGroupRows;
+      const uint32_t l = __ballot_sync(0xffffffffu, is_long), b = begins[c] & ~l, below = (1u << lane32) - 1u;
+      if (is_long) runs[warp][longs + __popc(l & below)] = static_cast<uint16_t>(t << 8 | n);
+      if (mine && !is_long) runs[warp][kPage - 1 - shorts - __popc(b & below)] = static_cast<uint16_t>(t << 8 | n);
+      longs += __popc(l);
+      shorts += __popc(b);
+    }
+    __syncwarp();
+  }
+  const int limit = P.c.num_pages * kPage;   // (below 2^31)
+  for (int k = 0; k < longs + shorts;) {
+    const bool whole_team = k < longs;
+    const int at = whole_team ? k : kPage - 1 - (k - longs) - g;   // (short ones: this group's)
+    if (whole_team) {
+      ++k;
+    } else {
+      const bool none = k - longs + g >= shorts;
+      k += kGroups;
+      if (none) continue;
+    }
+    const int t = runs[warp][at] >> 8, n = runs[warp][at] & 255;
+    const int slot = __ldg(slots + t);
     if (slot >= limit) {
-      if (g == 0 && lane == 0) atomicOr(P.err, kErrCheck);
-      ++t;
+      if (lane == 0) atomicOr(P.err, kErrCheck);
       continue;
     }
-    // the run's length: the first token that is not the next slot of this page
-    const int page = slot / kPage, off = slot % kPage;
-    int n = kPage - off;
-    int next[kPage / 16];
-#pragma unroll
-    for (int c = 0; c < kPage / 16; ++c) {
-      const int i = c * 16 + lane;
-      next[c] = i < n && t + i < P.n_tokens ? __ldg(P.slots + t + i) : -1;
-    }
-#pragma unroll
-    for (int c = kPage / 16 - 1; c >= 0; --c) {   // (backwards: the first break counts)
-      const uint32_t who = (__ballot_sync(lanes, next[c] != slot + c * 16 + lane) >> (threadIdx.x & 16)) & 0xffffu;
-      if (who) n = min(kPage - off, c * 16 + __ffs(who) - 1);
-    }
+    const int off = slot & (kPage - 1);
+    const int64_t block = static_cast<int64_t>(slot / kPage) * H + h;
+    const int row0 = whole_team ? g * kGroupRows - off : 0;   // the run's row in x[0]
     uint4 x[kGroupRows];
 #pragma unroll
     for (int i = 0; i < kGroupRows; ++i) {
-      const int row = g * kGroupRows + i - off;
       x[i] = make_uint4(0, 0, 0, 0);
-      if (row >= 0 && row < n) x[i] = __ldg(reinterpret_cast<const uint4*>(from + (t + row) * st) + lane);
+      if (static_cast<uint32_t>(row0 + i) < static_cast<uint32_t>(n))
+        x[i] = __ldg(reinterpret_cast<const uint4*>(from + (first + t + row0 + i) * st) + lane);
     }
-    const int64_t block = static_cast<int64_t>(page) * H + h;
-    write_run<kPage>(x, off, n, (values ? P.c.v : P.c.k) + block * (kPage * kHeadDim),
-                     (values ? P.c.v_scale : P.c.k_scale) + block, team_max[team]);
-    team_sync<kPage>();   // team_max and the scale before the next run
-    t += n;
+    if (whole_team) {
+      write_run<kPage>(x, off, n, codes + block * (kPage * kHeadDim), scales + block, team_max[team]);
+      team_sync<kPage>();   // team_max and the scale before the next run
+    } else {
+      write_short_run(x, off, n, codes + block * (kPage * kHeadDim), scales + block);
+    }
   }
   allow_next_kernel();
 }
-
-constexpr int64_t kPagesCtas = 152;
-// Tokens of a call from which a team takes P tokens instead of one (measured at the kernel's launcher).
-constexpr int64_t kStoreBlockTokens = 4096;
 
 template <int kPage>
 cudaError_t store_paged(const CacheStoreParams& p, cudaStream_t stream) {
@@ -510,7 +588,7 @@ cudaError_t launch_cache_gather(const CacheGatherParams& p, cudaStream_t stream)
 
 cudaError_t launch_cache_store(const CacheStoreParams& params, cudaStream_t stream) {
   CacheStoreParams p = params;
-  p.block = p.n_tokens > kStoreBlockTokens ? p.c.page : 1;
+  p.block = p.n_tokens > kStoreBlockTokens ? p.c.page : p.c.page / kGroupRows;
   switch (p.c.page) {
     case 16: return store_paged<16>(p, stream);
     case 32: return store_paged<32>(p, stream);

@@ -159,6 +159,33 @@ def test_store(K, P, lens, new, heads):
     _same_pool(c, (k, ks, v, vs))
 
 
+@pytest.mark.parametrize("P", [16, 32, 64, 128])
+@pytest.mark.parametrize("times", [1, 12])
+def test_store_long_and_short_runs_in_one_call(K, P, times):
+    """Runs of 1 to 130 rows side by side, padded tokens between them, in calls of both block sizes."""
+    rng = np.random.default_rng(P * times)
+    new = [1, 9, 8, 1, 130, 7, 0, 2, 10, 1, 16, 17, 1, 33, 3, 65, 1, 1, 8, 9] * times
+    lens = [int(x) for x in rng.integers(0, 70, len(new))]
+    heads = 2
+    table, pages = T.table_for(rng, [a + b for a, b in zip(lens, new)], P)
+    k, ks = T.pool(rng, pages, heads, P)
+    v, vs = T.pool(rng, pages, heads, P)
+    slots = _store_slots(rng, lens, new, P, table)
+    n = len(slots)
+    assert (n > 1024) == (times > 1)
+    kn, vn = T.rows(rng, (n, heads, 128)), T.rows(rng, (n, heads, 128))
+    kn[rng.random(n) < 0.1] *= 64
+    vn[rng.random(n) < 0.1] *= 16
+    c = _cache(K, heads, heads, P, pages, table.shape[1], len(lens), pool=(k, ks, v, vs))
+    for _ in range(2):
+        c.store(T.to_torch(kn), T.to_torch(vn), _dev(slots))
+        assert c.status() == K.KVE_OK
+    ks, vs = ks.astype(np.float64), vs.astype(np.float64)
+    C.store(k, ks, kn, slots)
+    C.store(v, vs, vn, slots)
+    _same_pool(c, (k, ks, v, vs))
+
+
 def test_store_values_that_bf16_can_hold(K):
     rng = np.random.default_rng(9)
     for P in (16, 64):
