@@ -188,6 +188,7 @@ __global__ void __launch_bounds__(kPagesThreads) cache_pages_kernel(const __grid
     if (blockIdx.x == 0 && blockIdx.y == 0 && threadIdx.x == 0) {
       P.ring_out[0] = ok ? ring_at(head, taken, np) : head;
       P.ring_out[1] = ok ? static_cast<int>(count - taken + given) : count;
+      *P.refused = ok ? 0 : 1;
       if (!ok) atomicOr(P.err, bad ? kErrCheck : kErrPages);
     }
     allow_next_kernel();
@@ -206,6 +207,7 @@ __global__ void __launch_bounds__(kPagesThreads) cache_pages_kernel(const __grid
   if (threadIdx.x == 0) {
     P.ring_out[0] = ok ? ring_at(head, taken, np) : head;
     P.ring_out[1] = ok ? static_cast<int>(count - taken + given) : count;
+    *P.refused = ok ? 0 : 1;
     if (!ok) atomicOr(P.err, bad ? kErrCheck : kErrPages);
   }
 }
@@ -394,6 +396,7 @@ __global__ void __launch_bounds__(kRowThreads<kPage>) cache_gather_kernel(const 
   if (n <= 0) return;
   const int seq = u.layer * P.c.max_seqs + P.first_seq + u.r;
   const int page = __ldg(P.table + static_cast<int64_t>(seq) * P.c.max_pages + j);
+  const bool refused = __ldg(P.refused) != 0;   // the table's pages may be other sequences' by now
   // the positions of this group's rows: lane i looks row i's up
   const int row = j * kPage + g * kGroupRows + (lane & (kGroupRows - 1));
   int src = -1;
@@ -403,6 +406,7 @@ __global__ void __launch_bounds__(kRowThreads<kPage>) cache_gather_kernel(const 
   } else if (row < m + W) {
     src = Lc + (row - m);
   }
+  if (refused) return;
   if (page < 0 || page >= P.c.num_pages) {
     if (g == 0 && lane == 0) atomicOr(P.err, kErrCheck);
     return;
@@ -679,6 +683,7 @@ kve_status kv_evict_cache_create(const kve_cache_config* cfg, uint8_t* k, uint8_
   kve::CacheWsLayout& w = h->ws;
   w.err = 0;
   w.pages_done = 64;
+  w.refused = 128;
   w.arrive = 256;
   const size_t workers = static_cast<size_t>(kve::kAttendCtas) * sms;
   w.clear_end = align_up(w.arrive + sizeof(uint32_t) * 2 * workers, 256);
@@ -728,6 +733,7 @@ kve_status kv_evict_cache_pages(const kve_cache* cache, const int32_t* lens_from
   p.slot_stride = slot_stride;
   p.err = word(ws, cache->ws.err);
   p.done = word(ws, cache->ws.pages_done);
+  p.refused = word(ws, cache->ws.refused);
   p.in_place = lens_out == lens_from || lens_out == lens_to || ring_out == ring_in;
   return kve::launch_cache_pages(p, static_cast<cudaStream_t>(stream)) == cudaSuccess ? KVE_OK : KVE_ECUDA;
 }
@@ -764,6 +770,7 @@ kve_status kv_evict_cache_gather(const kve_cache* cache, const kve_plan* plan, c
   p.table = table;
   p.first_seq = first_seq;
   p.unit_pages = static_cast<int32_t>(pages);
+  p.refused = word(ws, cache->ws.refused);
   p.err = word(ws, cache->ws.err);
   return kve::launch_cache_gather(p, static_cast<cudaStream_t>(stream)) == cudaSuccess ? KVE_OK : KVE_ECUDA;
 }

@@ -246,6 +246,7 @@ struct CacheGeometry {
 struct CacheWsLayout {
   size_t err;        // uint32 error word
   size_t pages_done; // uint32 CTAs of a kv_evict_cache_pages call that have finished reading
+  size_t refused;    // uint32, 1 where the last kv_evict_cache_pages call moved no page
   size_t arrive;     // uint32 [kAttendCtas * SMs][2] parts of a split row block that are written
   size_t clear_end;  // bytes cleared by kv_evict_cache_reset
   size_t partial;    // fp32 [kAttendCtas * SMs][2][kAttendPartWords] partial rows of the attention
@@ -266,6 +267,7 @@ struct PagesParams {
   bool in_place;         // lens_out or ring_out is an input
   uint32_t* err;
   uint32_t* done;
+  uint32_t* refused;
 };
 
 struct CacheGatherParams {
@@ -274,6 +276,7 @@ struct CacheGatherParams {
   const int32_t* table;
   int32_t first_seq;
   int32_t unit_pages;    // pages of a unit of B + W rows
+  const uint32_t* refused;
   uint32_t* err;
 };
 

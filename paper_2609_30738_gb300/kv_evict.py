@@ -201,14 +201,19 @@ class Plan:
     def score_elems(self) -> int:
         return self.spec["num_layers"] * self.unit_heads * sum(self.seq_lens)
 
-    def kept_lens(self, lens, first_seq: int = 0):
+    def kept_lens(self, lens, first_seq: int = 0, stream=None):
         """lens (int32 [N_L, max_seqs]) with the sequences first_seq .. of this plan's requests at the rows that
-        the plan keeps, min(B_l, Lc_r) + W."""
+        the plan keeps, min(B_l, Lc_r) + W. lens is read, and the result written, on stream."""
         import torch
         w = self.spec["window"]
-        kept = [[min(b, n - w) + w for n in self.seq_lens] for b in self.layer_budgets]
-        out = lens.clone()
-        out[:, first_seq:first_seq + len(self.seq_lens)] = torch.tensor(kept, dtype=lens.dtype, device=lens.device)
+        if not 0 <= first_seq <= lens.shape[1] - len(self.seq_lens):
+            raise ValueError("kept_lens: the plan's requests do not fit behind first_seq")
+        kept = torch.tensor([[min(b, n - w) + w for n in self.seq_lens] for b in self.layer_budgets], dtype=lens.dtype)
+        if isinstance(stream, int):
+            stream = torch.cuda.ExternalStream(stream, device=lens.device)
+        with torch.cuda.stream(stream):   # (None changes nothing)
+            out = lens.clone()
+            out[:, first_seq:first_seq + len(self.seq_lens)] = kept.to(lens.device)
         return out
 
     def set_kv_strides(self, k_strides=None, v_strides=None):
@@ -439,7 +444,9 @@ class Cache8:
         self.ws = torch.empty(size.value, dtype=torch.uint8, device=self.k.device)
         self._ws = self.ws.data_ptr()
         self._seqs, self._entries = self.num_layers * max_seqs, self.num_layers * max_seqs * max_pages
+        self._i32, self._f32 = torch.int32, torch.float32
         dev = self.k.device
+        self._device = self.k.get_device()
         raw = getattr(torch._C, "_cuda_getCurrentRawStream", None)   # (no Stream object made: 2 us less a call)
         if raw is not None and dev.type == "cuda":
             index = torch.cuda.current_device() if dev.index is None else dev.index
@@ -448,8 +455,12 @@ class Cache8:
             self._current_stream = lambda: torch.cuda.current_stream(dev).cuda_stream
         self.reset()
 
-    def _is_table(self, t) -> bool:
-        return t.numel() == self._entries and t.is_contiguous()
+    def _here(self, t) -> bool:
+        """Whether kernels on the cache's device can read t."""
+        return t.get_device() == self._device or (t.device.type == "cpu" and t.is_pinned())
+
+    def _is_i32(self, t, n: int) -> bool:
+        return t.dtype is self._i32 and t.numel() == n and t.is_contiguous() and self._here(t)
 
     def _stream(self, stream):
         """The stream's address; None is the current stream of the cache's device."""
@@ -482,6 +493,9 @@ class Cache8:
 
     def reset(self, free_pages=None, ring=None, stream=None):
         """kv_evict_cache_reset: clear the workspace, and make every page free where the ring is given."""
+        for name, t, n in (("free_pages", free_pages, self.num_pages), ("ring", ring, 2)):
+            if t is not None and not self._is_i32(t, n):
+                raise ValueError(f"{name}: expected {n} contiguous int32 values on the cache's device")
         _check(self._lib.kv_evict_cache_reset(self._h, _ptr(free_pages), _ptr(ring), self._ws,
                                               self._stream(stream)), "kv_evict_cache_reset")
 
@@ -490,15 +504,15 @@ class Cache8:
         stride = 0
         if slots is not None:
             shape = slots.shape
-            if len(shape) != 2 or shape[0] != self.num_layers or not slots.is_contiguous():
-                raise ValueError("slots: expected a contiguous [num_layers, n] tensor")
+            if len(shape) != 2 or shape[0] != self.num_layers or not self._is_i32(slots, shape[0] * shape[1]):
+                raise ValueError("slots: expected a contiguous int32 [num_layers, n] tensor on the cache's device")
             stride = shape[1]
         seqs = self._seqs
         for name, t, n in (("lens_from", lens_from, seqs), ("lens_to", lens_to, seqs), ("lens_out", lens_out, seqs),
                            ("table", table, self._entries), ("free_pages", free_pages, self.num_pages),
                            ("ring_in", ring_in, 2), ("ring_out", ring_out, 2)):
-            if t.numel() != n or not t.is_contiguous():
-                raise ValueError(f"{name}: expected {n} contiguous values")
+            if not self._is_i32(t, n):
+                raise ValueError(f"{name}: expected {n} contiguous int32 values on the cache's device")
         _check(self._lib.kv_evict_cache_pages(
             self._h, lens_from.data_ptr(), lens_to.data_ptr(), table.data_ptr(), free_pages.data_ptr(),
             ring_in.data_ptr(), ring_out.data_ptr(), lens_out.data_ptr(), _ptr(slots), stride, self._ws,
@@ -511,8 +525,11 @@ class Cache8:
             dev = getattr(t, "device", None)
             if dev is not None and getattr(dev, "type", None) == "cpu" and not t.is_pinned():
                 raise ValueError(f"gather: {name} is a pageable CPU tensor; pin it or move it to the GPU")
-        if indices.numel() != plan.n_units * plan.spec["budget"] or not self._is_table(table):
-            raise ValueError("gather: indices are the plan's [n_units, budget], table is [num_layers, max_seqs, max_pages]")
+            if dev is not None and getattr(dev, "type", None) == "cuda" and t.get_device() != self._device:
+                raise ValueError(f"gather: {name} is on another device than the cache")
+        if not self._is_i32(indices, plan.n_units * plan.spec["budget"]) or not self._is_i32(table, self._entries):
+            raise ValueError("gather: indices are the plan's int32 [n_units, budget], table is int32 [num_layers, "
+                             "max_seqs, max_pages]")
         _check(self._lib.kv_evict_cache_gather(self._h, plan._h, k.data_ptr(), v.data_ptr(), indices.data_ptr(),
                                                first_seq, table.data_ptr(), self._ws, self._stream(stream)),
                "kv_evict_cache_gather")
@@ -522,8 +539,10 @@ class Cache8:
         int32 [tokens]."""
         n = slots.numel()
         rows = n * self.heads * self.head_dim
-        if k_new.numel() != rows or v_new.numel() != rows or not slots.is_contiguous():
-            raise ValueError("store: k_new and v_new hold a row of every head for each slot")
+        if k_new.numel() != rows or v_new.numel() != rows or not self._is_i32(slots, n):
+            raise ValueError("store: k_new and v_new hold a row of every head for each of the int32 slots")
+        if not self._here(k_new) or not self._here(v_new):
+            raise ValueError("store: k_new and v_new are on the cache's device")
         _check(self._lib.kv_evict_cache_store(
             self._h, k_new.data_ptr(), v_new.data_ptr(), _row_strides(k_new, self.heads, "k_new"),
             _row_strides(v_new, self.heads, "v_new"), slots.data_ptr(), n, self._ws, self._stream(stream)),
@@ -533,11 +552,13 @@ class Cache8:
         """kv_evict_cache_attend: q, out bf16 [n_seq, q_tokens, Hq, d], lse fp32 [n_seq, q_tokens, Hq] or
         None; table and lens of all layers."""
         shape = q.shape
-        if len(shape) != 4 or out.shape != shape or (lse is not None and
-                                                     (lse.shape != shape[:3] or not lse.is_contiguous())):
-            raise ValueError("attend: q and out are [n_seq, q_tokens, Hq, d], lse [n_seq, q_tokens, Hq]")
-        if not self._is_table(table) or lens.numel() != self._seqs or not lens.is_contiguous():
-            raise ValueError("attend: table is [num_layers, max_seqs, max_pages], lens [num_layers, max_seqs]")
+        if len(shape) != 4 or out.shape != shape or (lse is not None and (
+                lse.shape != shape[:3] or lse.dtype is not self._f32 or not lse.is_contiguous())):
+            raise ValueError("attend: q and out are [n_seq, q_tokens, Hq, d], lse is fp32 [n_seq, q_tokens, Hq]")
+        if not self._here(q) or not self._here(out) or (lse is not None and not self._here(lse)):
+            raise ValueError("attend: q, out and lse are on the cache's device")
+        if not self._is_i32(table, self._entries) or not self._is_i32(lens, self._seqs):
+            raise ValueError("attend: table is int32 [num_layers, max_seqs, max_pages], lens int32 [num_layers, max_seqs]")
         _check(self._lib.kv_evict_cache_attend(
             self._h, layer, shape[0], shape[1], q.data_ptr(), _row_strides(q, self.num_q_heads, "q"),
             table.data_ptr(), lens.data_ptr(), out.data_ptr(), _row_strides(out, self.num_q_heads, "out"), _ptr(lse),
@@ -552,8 +573,10 @@ def run_step_cache8(plan: Plan, bufs: Buffers, cache: Cache8, q_win, k, v, lambd
                     ring, first_seq: int = 0, stream=None):
     """The eviction step whose compact cache is the paged 8-bit one: score, select, pages for the plan's
     requests (their sequences first_seq .. must be empty), and the kept and window rows written into them.
-    lens and ring are advanced in place."""
+    lens and ring are advanced in place; where the free pages do not suffice, neither moves, no page is written
+    and cache.status() returns KVE_EPAGES."""
+    lens_to = plan.kept_lens(lens, first_seq, stream)
     plan.score(q_win, k, bufs.mu, bufs.sigma, bufs.ws, stream)
     plan.select(bufs.mu, bufs.sigma, k, lambda1, lambda2, bufs.indices, bufs.ws, bufs.order, bufs.margins, stream)
-    cache.pages(lens, plan.kept_lens(lens, first_seq), table, free_pages, ring, ring, lens, None, stream)
+    cache.pages(lens, lens_to, table, free_pages, ring, ring, lens, None, stream)
     cache.gather(plan, k, v, bufs.indices, table, first_seq, stream)

@@ -195,3 +195,18 @@ def test_binding_refuses():
             K._row_strides(bad, 8, "q")
     with pytest.raises(ValueError):                                           # pages in host memory
         K.Cache8(dict(num_layers=1, num_q_heads=8, num_kv_heads=2, head_dim=128), 2, 8, 4, 16, device="cpu")
+
+
+def test_kept_lens_of_a_plan():
+    torch = pytest.importorskip("torch")
+    from paper_2609_30738_gb300 import kv_evict as K
+    from paper_2609_30738_gb300.workloads import WORKLOADS, scaled
+    spec = scaled(WORKLOADS["mistral-1layer-L2048"], num_layers=2, seq_lens=[700, 90], budget=70)
+    plan = K.Plan(spec, [700, 90], layer_budgets=[70, 25])
+    W = spec["window"]
+    lens = torch.tensor([[1, 2, 3, 4], [5, 6, 7, 8]], dtype=torch.int32)
+    want = [[1, 70 + W, min(70, 90 - W) + W, 4], [5, 25 + W, 25 + W, 8]]
+    assert plan.kept_lens(lens, 1).tolist() == want and lens.tolist() == [[1, 2, 3, 4], [5, 6, 7, 8]]
+    for first in (-1, -2, 3):
+        with pytest.raises(ValueError):
+            plan.kept_lens(lens, first)

@@ -571,7 +571,16 @@ def test_binding_checks_what_it_is_given(K):
            lambda: c.store(rows, rows[:4], slots), lambda: c.store(rows, rows, slots[:4]),
            lambda: c.pages(lens, lens, table, free[:7], ring, ring, lens),
            lambda: c.pages(lens[:, :2], lens, table, free, ring, ring, lens),
-           lambda: c.pages(lens, lens, table, free, ring, ring, lens, slots)]
+           lambda: c.pages(lens, lens, table, free, ring, ring, lens, slots),
+           lambda: c.pages(lens, lens.long(), table, free, ring, ring, lens),
+           lambda: c.pages(lens, lens.cpu(), table, free, ring, ring, lens),
+           lambda: c.pages(lens, lens, table, free, ring, ring, lens, slots.reshape(1, 5).long()),
+           lambda: c.attend(q, table.long(), lens, 0, q.clone()), lambda: c.attend(q, table, lens.long(), 0, q.clone()),
+           lambda: c.attend(q, table, lens, 0, q.clone(), torch.zeros((3, 1, 8), dtype=torch.bfloat16, device=DEV)),
+           lambda: c.attend(q, table, lens, 0, q.clone(), torch.zeros((3, 1, 8))),
+           lambda: c.attend(q.cpu(), table, lens, 0, q.clone()), lambda: c.attend(q, table, lens, 0, q.cpu()),
+           lambda: c.store(rows, rows, slots.long()), lambda: c.store(rows.cpu(), rows, slots),
+           lambda: c.store(rows, rows, slots.cpu()), lambda: c.reset(free[:7], ring), lambda: c.reset(free, ring.long())]
     for call in bad:
         with pytest.raises(ValueError):
             call()
@@ -597,6 +606,38 @@ def test_two_caches_at_once(K):
     for (a, _), o, x in zip(alone, outs, cases):
         assert x[0].status() == K.KVE_OK
         assert np.array_equal(a, o.float().cpu().numpy().astype(np.float64))
+
+
+def test_eviction_that_finds_too_few_pages_writes_none(K):
+    """A sequence's old table entries name pages that others hold by now: where the new pages are refused, the rows
+    go nowhere; the next call that is served writes them. On a stream that is not the current one."""
+    spec = scaled(WORKLOADS["mistral-1layer-L2048"], num_layers=1, seq_lens=[200], num_kv_heads=2, num_q_heads=8,
+                  budget=40)
+    batch = synth.make_batch(spec, seed=3)
+    plan = K.Plan(spec, batch["seq_lens"])
+    bufs = K.Buffers(plan)
+    c = K.Cache8(spec, max_seqs=2, num_pages=6, max_pages=6, page_tokens=16)
+    table, lens, free, ring = c.state()
+    q, k, v = (batch[x].to(DEV) for x in ("q_win", "k", "v"))
+    lam = np.full(1, 0.5, np.float32)
+    for t in (c.k, c.v, c.k_scale, c.v_scale):
+        t.zero_()
+    for to in ([40, 0], [0, 0], [0, 60]):      # sequence 0 leaves its entries behind, sequence 1 takes pages
+        c.pages(lens, _dev(np.array([to], np.int32)), table, free, ring, ring, lens)
+    before = [t.cpu().numpy() for t in (c.k, c.k_scale, c.v, c.v_scale)], lens.tolist(), ring.tolist()
+    side = torch.cuda.Stream()
+    torch.cuda.synchronize()
+    for stream in (side, side.cuda_stream):
+        K.run_step_cache8(plan, bufs, c, q, k, v, lam, -lam, table, lens, free, ring, stream=stream)
+        assert plan.status(bufs.ws, stream) == K.KVE_OK and c.status(stream) == K.KVE_EPAGES
+        _same_pool(c, before[0])
+        assert lens.tolist() == before[1] and ring.tolist() == before[2]
+    # the same with the pages given back first
+    c.pages(lens, torch.zeros_like(lens), table, free, ring, ring, lens)
+    torch.cuda.synchronize()
+    K.run_step_cache8(plan, bufs, c, q, k, v, lam, -lam, table, lens, free, ring, stream=side)
+    assert c.status(side) == K.KVE_OK and lens.tolist() == [[40 + spec["window"], 0]]
+    assert all(bool((t != 0).any()) for t in (c.k, c.k_scale, c.v, c.v_scale))
 
 
 def test_eviction_into_the_cache_then_decode(K):
