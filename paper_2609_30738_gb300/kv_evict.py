@@ -460,7 +460,8 @@ class Cache8:
         return t.get_device() == self._device or (t.device.type == "cpu" and t.is_pinned())
 
     def _is_i32(self, t, n: int) -> bool:
-        return t.dtype is self._i32 and t.numel() == n and t.is_contiguous() and self._here(t)
+        return (t.dtype is self._i32 and t.numel() == n and t.is_contiguous() and
+                (t.get_device() == self._device or self._here(t)))
 
     def _stream(self, stream):
         """The stream's address; None is the current stream of the cache's device."""
@@ -507,11 +508,12 @@ class Cache8:
             if len(shape) != 2 or shape[0] != self.num_layers or not self._is_i32(slots, shape[0] * shape[1]):
                 raise ValueError("slots: expected a contiguous int32 [num_layers, n] tensor on the cache's device")
             stride = shape[1]
-        seqs = self._seqs
+        seqs, i32, dev = self._seqs, self._i32, self._device
         for name, t, n in (("lens_from", lens_from, seqs), ("lens_to", lens_to, seqs), ("lens_out", lens_out, seqs),
                            ("table", table, self._entries), ("free_pages", free_pages, self.num_pages),
                            ("ring_in", ring_in, 2), ("ring_out", ring_out, 2)):
-            if not self._is_i32(t, n):
+            if ((t.dtype is not i32 or t.numel() != n or t.get_device() != dev or not t.is_contiguous()) and
+                    not self._is_i32(t, n)):
                 raise ValueError(f"{name}: expected {n} contiguous int32 values on the cache's device")
         _check(self._lib.kv_evict_cache_pages(
             self._h, lens_from.data_ptr(), lens_to.data_ptr(), table.data_ptr(), free_pages.data_ptr(),
