@@ -20,7 +20,7 @@ namespace {
 // ---------------------------------------------------------------- tables and slots
 
 constexpr int kPagesThreads = 1024;
-constexpr int64_t kPagesCtas = 152;   // one an SM: pages and slots of 48 prompts in 32 layers 19.1 us, with 76 38.0, with 304 22.5
+constexpr int64_t kPagesCtas = 152;   // one an SM: twice as many took 3.5 us more on those prompts, half twice the time
 constexpr int kPagesWarps = kPagesThreads / 32;
 static_assert(kPagesWarps == 32, "a lane a sequence of the CTA");
 
@@ -48,14 +48,17 @@ __device__ __forceinline__ int ring_at(int head, long long i, int n) {
 
 // A CTA has 32 sequences, a warp each for their places in the ring and in their layer's slots; their pages, in
 // chunks of 32 (a lane a page), are one line that the warps share, so that one long sequence is no warp's
-// alone. A chunk's pages are read in one access and 32 slots at a time leave from registers: new pages cost
-// their 8 bytes and slots their 4. Before that every CTA sums the pages and tokens that each layer takes and
-// gives (a warp a layer), so that all agree whether the call can be done before one of them writes; these
-// sums are why there is one CTA an SM at most. Where the call changes its inputs in place (lens_out,
-// ring_out), the CTA that finishes reading last does that.
+// alone. A chunk's pages are read in one access, while the chunk before is written, and its slots leave from
+// registers, four at a time: new pages cost their 8 bytes and slots their 4. Before that every CTA sums the pages
+// and tokens that each layer takes and gives (a warp a layer), so that all agree whether the call can be done
+// before one of them writes; these sums are why there is one CTA an SM at most. Where the call changes its inputs in
+// place (lens_out, ring_out), the CTA that finishes reading last does that.
 //
-// A decode step (512 sequences, one new token each) is bound by latency: two reads of 8 bytes a sequence from
-// L2 and the chain length -> ring entry -> table.
+// A decode step (512 sequences, one new token each) is bound by latency: two reads of 8 bytes a sequence from L2
+// and the chain length -> ring entry -> table: 4.8 us. A wave of prompts is bound by the slots' write: 48 of 500 to
+// 32768 tokens in 32 layers (P = 16, 67 MB) 17.6 us, 56% of the HBM peak, of which 5.5 are the decode step's
+// latencies; 201 MB of slots at P = 64 40 us. Slots one at a time took 19.0 and 45.8, four without the read ahead 19.5
+// and 40.6.
 __global__ void __launch_bounds__(kPagesThreads) cache_pages_kernel(const __grid_constant__ PagesParams P) {
   wait_previous_kernel();
   __shared__ long long layer_sum[3][kMaxLayers];   // pages taken, pages given, new tokens
@@ -139,40 +142,78 @@ __global__ void __launch_bounds__(kPagesThreads) cache_pages_kernel(const __grid
     if (lane >= o) last += x;
   }
   const int all = __shfl_sync(0xffffffffu, last, 31);
-  for (int q = blockIdx.y * kPagesWarps + warp; q < all; q += kPagesWarps * gridDim.y) {
-    const int w = __popc(__ballot_sync(0xffffffffu, last <= q));   // the sequence whose chunk it is
-    const int c = q - (w > 0 ? __shfl_sync(0xffffffffu, last, max(w - 1, 0)) : 0);
-    const Grown s = grown[w];
+  // the page of a chunk's lane is read while the chunk before it is written
+  struct Chunk {
+    int w, c, page;   // its sequence, its number there, this lane's page (-1: none)
+  };
+  const auto read = [&](int q) {
+    Chunk k;
+    k.w = __popc(__ballot_sync(0xffffffffu, last <= q)) & 31;   // the sequence whose chunk it is
+    const int before = __shfl_sync(0xffffffffu, last, max(k.w - 1, 0));
+    k.c = q - (k.w > 0 ? before : 0);
+    k.page = -1;
+    if (q >= all) return k;
+    const Grown& s = grown[k.w];
+    const int have = (s.a + page_mask) >> shift, need = (s.b + page_mask) >> shift;
+    if (s.b > s.a) {
+      const int j = (s.a >> shift) + 32 * k.c + lane;
+      if (j < have)
+        k.page = s.row[j];
+      else if (j < need)
+        k.page = P.free_pages[ring_at(s.ring, j - have, np)];
+    } else {
+      const int j = need + 32 * k.c + lane;
+      if (j < have) k.page = s.row[j];
+    }
+    return k;
+  };
+  const int first = blockIdx.y * kPagesWarps + warp, step = kPagesWarps * gridDim.y;
+  Chunk next = read(first);
+  for (int q = first; q < all; q += step) {
+    const Chunk now = next;
+    if (q + step < all) next = read(q + step);
+    const Grown s = grown[now.w];
+    const int c = now.c, page = now.page;
     const int have = (s.a + page_mask) >> shift, need = (s.b + page_mask) >> shift;
     if (s.b > s.a) {
       const int j0 = (s.a >> shift) + 32 * c, j = j0 + lane;
-      int page = -1;
-      if (j < have) {
-        if (s.out) page = s.row[j];
-      } else if (j < need) {
-        page = P.free_pages[ring_at(s.ring, j - have, np)];
-        s.row[j] = page;
-      }
+      if (j >= have && j < need) s.row[j] = page;
       if (!s.out) continue;
       const int base = page >= 0 && page < np ? page << shift : -1;
-      const int end = min(s.b, (j0 + 32) << shift);
-      if ((j0 << shift) >= s.a && end == (j0 + 32) << shift && __all_sync(0xffffffffu, base >= 0)) {
-        // 32 whole pages: P times 32 slots, nothing to check
-        int32_t* to = s.out + ((j0 << shift) - s.a) + lane;
-#pragma unroll 8
-        for (int k = lane; k < 32 << shift; k += 32, to += 32)
-          *to = __shfl_sync(0xffffffffu, base, k >> shift) + (k & page_mask);
+      // slots [begin, end) of the chunk, counted from its first page
+      const int begin = max(s.a - (j0 << shift), 0), end = min(s.b - (j0 << shift), 32 << shift), len = end - begin;
+      int32_t* const to = s.out + ((j0 << shift) + begin - s.a);
+      if (__any_sync(0xffffffffu, j < need && base < 0)) {
+        // a table entry outside the pool: its tokens get no slot
+#pragma unroll 1
+        for (int i = 0; i < len; i += 32) {
+          const int k = begin + i + lane;
+          const int from = __shfl_sync(0xffffffffu, base, k >> shift);
+          if (i + lane < len) to[i + lane] = from < 0 ? -1 : from + (k & page_mask);
+        }
         continue;
       }
-#pragma unroll 4
-      for (int pos = j0 << shift; pos < end; pos += 32) {
-        const int mine = pos + lane;
-        const int from = __shfl_sync(0xffffffffu, base, (mine >> shift) - j0);
-        if (mine >= s.a && mine < end) s.out[mine - s.a] = from < 0 ? -1 : from + (mine & page_mask);
+      // up to the first multiple of 16 bytes and behind the last one by slot, in between four at a time
+      const int front = min(static_cast<int>(-(reinterpret_cast<uintptr_t>(to) >> 2) & 3), len);
+      const int quads = (len - front) >> 2, rest = (len - front) & 3;
+      {
+        const int i = lane < 16 ? lane : len - 32 + lane, k = begin + i;
+        const int from = __shfl_sync(0xffffffffu, base, k >> shift);
+        if (lane < front || lane >= 32 - rest) to[i] = from + (k & page_mask);
+      }
+#pragma unroll 2
+      for (int i = 0; i < quads; i += 32) {
+        const int q = front + 4 * (i + lane), k = begin + q, off = k & page_mask;
+        const int x = __shfl_sync(0xffffffffu, base, k >> shift) + off;
+        const int y = __shfl_sync(0xffffffffu, base, (k + 3) >> shift) + off - P.c.page;   // of those on the next page
+        if (i + lane < quads)
+          *reinterpret_cast<int4*>(to + q) =
+              make_int4(x, (off + 1 < P.c.page ? x : y) + 1, (off + 2 < P.c.page ? x : y) + 2,
+                        (off + 3 < P.c.page ? x : y) + 3);
       }
     } else {
       const int j = need + 32 * c + lane;
-      if (j < have) P.free_pages[ring_at(s.ring, j - need, np)] = s.row[j];
+      if (j < have) P.free_pages[ring_at(s.ring, j - need, np)] = page;
     }
   }
   if (seq < n) {

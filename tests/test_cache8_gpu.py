@@ -123,8 +123,10 @@ def test_pages_all_or_nothing(K):
 def _same_pool(c, want):
     for name, t, w in zip(("k", "k_scale", "v", "v_scale"), (c.k, c.k_scale, c.v, c.v_scale), want):
         got = t.cpu().numpy()
-        if not np.array_equal(got, w):
-            at = np.argwhere(got != w)
+        # (a scale that no call has set keeps what its memory held: NaN there is the same on both sides)
+        differs = (got != w) & ~(np.isnan(got) & np.isnan(w)) if got.shape == w.shape else got.shape != w.shape
+        if np.any(differs):
+            at = np.argwhere(differs)
             raise AssertionError(f"{name}: {len(at)} values differ, first at {at[0]}: {got[tuple(at[0])]} {w[tuple(at[0])]}")
 
 
