@@ -20,7 +20,7 @@ namespace {
 // ---------------------------------------------------------------- tables and slots
 
 constexpr int kPagesThreads = 1024;
-constexpr int64_t kPagesCtas = 152;   // one an SM: twice as many took 3.5 us more on those prompts, half twice the time
+constexpr int64_t kPagesCtas = 152;   // one an SM: twice as many took 3.2 us more on those prompts, half twice the time
 constexpr int kPagesWarps = kPagesThreads / 32;
 static_assert(kPagesWarps == 32, "a lane a sequence of the CTA");
 
@@ -178,13 +178,15 @@ __global__ void __launch_bounds__(kPagesThreads) cache_pages_kernel(const __grid
     if (s.b > s.a) {
       const int j0 = (s.a >> shift) + 32 * c, j = j0 + lane;
       if (j >= have && j < need) s.row[j] = page;
-      if (!s.out) continue;
       const int base = page >= 0 && page < np ? page << shift : -1;
+      const bool outside = __any_sync(0xffffffffu, j < need && base < 0);   // a page outside the pool
+      if (outside && lane == 0) atomicOr(P.err, kErrCheck);
+      if (!s.out) continue;
       // slots [begin, end) of the chunk, counted from its first page
       const int begin = max(s.a - (j0 << shift), 0), end = min(s.b - (j0 << shift), 32 << shift), len = end - begin;
       int32_t* const to = s.out + ((j0 << shift) + begin - s.a);
-      if (__any_sync(0xffffffffu, j < need && base < 0)) {
-        // a table entry outside the pool: its tokens get no slot
+      if (outside) {
+        // its tokens get no slot
 #pragma unroll 1
         for (int i = 0; i < len; i += 32) {
           const int k = begin + i + lane;

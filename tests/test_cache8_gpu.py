@@ -118,6 +118,37 @@ def test_pages_all_or_nothing(K):
             assert np.array_equal(x, y)
 
 
+@pytest.mark.parametrize("P", [16, 128])
+def test_pages_outside_the_pool_give_no_slots(K, P):
+    """A ring entry, and the table entry of a page that is filled further, outside the pool: their tokens have no
+    slot, the others theirs, the table and the ring move as ever, and the status tells."""
+    f = np.array([[P // 2 + 1, 0, 3]], np.int32)
+    t = np.array([[P + P // 2, 3 * P - 5, 40 * P]], np.int32)
+    n = 60
+    for row, entries in ((0, {}), (1, {}), (-7, {}), (0, {2: n}), (0, {0: -1, 30: 2 ** 31 - 1, 36: -2 ** 31})):
+        free = np.arange(n, dtype=np.int32)[::-1].copy()
+        for i, x in entries.items():
+            free[i] = x
+        table = np.full((1, 3, 50), -1, np.int32)
+        table[0, 0, 0], table[0, 2, 0] = 55 if row < 0 else row, n + 5 if row < 0 else 7
+        ring = np.array([0, 50], np.int32)
+        want = C.pages(f, t, table, free, ring, P)
+        new = [x[:] for x in want[0][0]]
+        slots, at = np.full((1, 45 * P), -1, np.int64), 0
+        for s in range(3):
+            for i in range(f[0, s], t[0, s]):
+                page = int(new[s][i // P])
+                slots[0, at] = page * P + i % P if 0 <= page < n else -1
+                at += 1
+        c = _cache(K, 1, 1, P, n, 50, 3)
+        for with_slots in (True, False):
+            got = _run_pages(c, f, t, table, free, ring, 45 * P if with_slots else None)
+            assert c.status() == (K.KVE_ECUDA if row < 0 or entries else K.KVE_OK) and c.status() == K.KVE_OK
+            for a, b in zip(got[:4], want[:4]):
+                assert np.array_equal(a, b)
+            assert got[4] is None or np.array_equal(got[4], slots)
+
+
 # ------------------------------------------------------------------------------------------------ writers
 
 def _same_pool(c, want):
