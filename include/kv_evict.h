@@ -423,7 +423,7 @@ kve_status kv_evict_cache_gather(const kve_cache* cache, const kve_plan* plan,
  * the call gets undefined codes. A run of tokens that starts at row 0 of a page sets its scale to
  * need of its rows; one that starts later keeps the larger of need and the page's scale,
  * and where that grows, the page's older rows are rounded to it once more. Making the same
- * call again changes nothing. n_tokens < 2^20. */
+ * call again changes nothing. n_tokens < 2^20; with 0 of them nothing is done. */
 kve_status kv_evict_cache_store(const kve_cache* cache, const uint16_t* k_new,
                                 const uint16_t* v_new, const int64_t* k_strides,
                                 const int64_t* v_strides, const int32_t* slots,

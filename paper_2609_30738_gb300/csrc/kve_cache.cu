@@ -823,7 +823,8 @@ kve_status kv_evict_cache_store(const kve_cache* cache, const uint16_t* k_new, c
                                 int64_t n_tokens, void* ws, void* stream) {
   if (!cache || n_tokens < 0 || n_tokens > INT32_MAX / (2 * kve::kMaxCacheHeads) || !ws || !aligned(ws, 256))
     return KVE_EINVAL;
-  if (!k_new || !v_new || !slots || !aligned(k_new, 16) || !aligned(v_new, 16) || !aligned(slots, 4)) return KVE_EINVAL;
+  if (n_tokens > 0 && (!k_new || !v_new || !slots)) return KVE_EINVAL;
+  if (!aligned(k_new, 16) || !aligned(v_new, 16) || !aligned(slots, 4)) return KVE_EINVAL;
   kve::CacheStoreParams p;
   std::memset(&p, 0, sizeof(p));
   p.c = cache->geo;
@@ -843,7 +844,7 @@ kve_status kv_evict_cache_attend(const kve_cache* cache, int32_t layer, int32_t 
                                  const uint16_t* q, const int64_t* q_strides, const int32_t* table,
                                  const int32_t* lens, uint16_t* out, const int64_t* out_strides, float* lse,
                                  void* ws, void* stream) {
-  if (!cache || !q || !table || !lens || !out || !ws || !aligned(ws, 256)) return KVE_EINVAL;
+  if (!cache || !table || !lens || !ws || !aligned(ws, 256) || (n_seq != 0 && (!q || !out))) return KVE_EINVAL;
   const kve::CacheGeometry& c = cache->geo;
   if (layer < 0 || layer >= c.num_layers || n_seq < 0 || n_seq > c.max_seqs || q_tokens < 1 ||
       static_cast<int64_t>(q_tokens) * c.group > kve::kMaxRows)
@@ -883,12 +884,19 @@ kve_status kv_evict_cache_attend(const kve_cache* cache, int32_t layer, int32_t 
 
 kve_status kv_evict_cache_status(const kve_cache* cache, void* ws, void* stream) {
   if (!cache || !ws || !aligned(ws, 256) || !on_device(cache)) return KVE_EINVAL;
-  if (cudaStreamSynchronize(static_cast<cudaStream_t>(stream)) != cudaSuccess) return KVE_ECUDA;
+  // all on the caller's stream, so that its next call finds the words cleared
+  const cudaStream_t st = static_cast<cudaStream_t>(stream);
+  const kve::CacheWsLayout& w = cache->ws;
   uint32_t err = 0;
-  if (cudaMemcpy(&err, word(ws, cache->ws.err), sizeof(err), cudaMemcpyDeviceToHost) != cudaSuccess) return KVE_ECUDA;
+  if (cudaMemcpyAsync(&err, word(ws, w.err), sizeof(err), cudaMemcpyDeviceToHost, st) != cudaSuccess ||
+      cudaStreamSynchronize(st) != cudaSuccess)
+    return KVE_ECUDA;
   if (err == 0) return KVE_OK;
-  // the arrival counters too: a call that gave up may not have counted all of its parts
-  if (cudaMemset(ws, 0, cache->ws.clear_end) != cudaSuccess) return KVE_ECUDA;
+  // the arrival counters too: a call that gave up may not have counted all of its parts; `refused` stays until
+  // the next kv_evict_cache_pages call
+  if (cudaMemsetAsync(ws, 0, w.refused, st) != cudaSuccess ||
+      cudaMemsetAsync(word(ws, w.arrive), 0, w.clear_end - w.arrive, st) != cudaSuccess)
+    return KVE_ECUDA;
   if (err & kve::kErrCheck) return KVE_ECUDA;
   return err & kve::kErrWait ? KVE_ETIMEOUT : KVE_EPAGES;
 }

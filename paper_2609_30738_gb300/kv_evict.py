@@ -517,7 +517,9 @@ class Cache8:
                 raise ValueError(f"{name}: expected {n} contiguous int32 values on the cache's device")
         _check(self._lib.kv_evict_cache_pages(
             self._h, lens_from.data_ptr(), lens_to.data_ptr(), table.data_ptr(), free_pages.data_ptr(),
-            ring_in.data_ptr(), ring_out.data_ptr(), lens_out.data_ptr(), _ptr(slots), stride, self._ws,
+            ring_in.data_ptr(), ring_out.data_ptr(), lens_out.data_ptr(),
+            # (an empty tensor has no address and room for no token: any address that is not NULL says so)
+            None if slots is None else slots.data_ptr() or self._ws, stride, self._ws,
             self._stream(stream)), "kv_evict_cache_pages")
 
     def gather(self, plan: Plan, k, v, indices, table, first_seq: int = 0, stream=None):
@@ -576,7 +578,8 @@ def run_step_cache8(plan: Plan, bufs: Buffers, cache: Cache8, q_win, k, v, lambd
     """The eviction step whose compact cache is the paged 8-bit one: score, select, pages for the plan's
     requests (their sequences first_seq .. must be empty), and the kept and window rows written into them.
     lens and ring are advanced in place; where the free pages do not suffice, neither moves, no page is written
-    and cache.status() returns KVE_EPAGES."""
+    and cache.status() returns KVE_EPAGES. Not for capture: the kept lengths come from the host (in a graph, call
+    kept_lens before and the four calls inside)."""
     lens_to = plan.kept_lens(lens, first_seq, stream)
     plan.score(q_win, k, bufs.mu, bufs.sigma, bufs.ws, stream)
     plan.select(bufs.mu, bufs.sigma, k, lambda1, lambda2, bufs.indices, bufs.ws, bufs.order, bufs.margins, stream)

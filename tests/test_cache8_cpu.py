@@ -148,12 +148,14 @@ def test_calls_refuse():
     # store: k, v, k_strides, v_strides, slots, n, ws
     good = [FAKE, FAKE, None, None, FAKE, 5, FAKE]
     assert lib.kv_evict_cache_store(h, *good[:5], 0, FAKE, None) == K.KVE_OK      # nothing to do
+    assert lib.kv_evict_cache_store(h, None, None, None, None, None, 0, FAKE, None) == K.KVE_OK
     for i, bad in [(0, None), (0, ODD), (1, None), (1, ODD), (2, pair(1024, 4)), (2, pair(-8, 128)), (3, pair(1 << 37, 8)),
                    (4, None), (4, SIDE), (5, -1), (5, 1 << 20), (6, None), (6, ODD)]:
         assert lib.kv_evict_cache_store(h, *[bad if j == i else x for j, x in enumerate(good)], None) == K.KVE_EINVAL, i
     # attend: layer, n_seq, q_tokens, q, q_strides, table, lens, out, out_strides, lse, ws
     good = [1, 4, 1, FAKE, None, FAKE, FAKE, FAKE, None, None, FAKE]
     assert lib.kv_evict_cache_attend(h, *[0 if j == 1 else x for j, x in enumerate(good)], None) == K.KVE_OK
+    assert lib.kv_evict_cache_attend(h, 1, 0, 1, None, None, FAKE, FAKE, None, None, None, FAKE, None) == K.KVE_OK
     for i, bad in [(0, -1), (0, 2), (1, -1), (1, 5), (2, 0), (2, 33), (3, None), (3, ODD), (4, pair(4096, 4)),
                    (5, None), (5, SIDE), (6, None), (6, SIDE), (7, None), (7, ODD), (8, pair(64, 128)), (8, pair(4096, 64)),
                    (8, pair(0, 128)), (8, pair(2048, 128)), (9, SIDE), (10, None), (10, ODD)]:

@@ -623,6 +623,37 @@ def test_binding_checks_what_it_is_given(K):
         c.attend(torch.zeros((4, 1, 8, 128), dtype=torch.bfloat16, device=DEV), table, lens, 0, torch.zeros_like(q).repeat(2, 1, 1, 1)[:4])
 
 
+@pytest.mark.parametrize("G,heads,t,lens", [(4, 2, 1, [5000, 0, 3, 129]), (4, 1, 9, [40, 0, 20000, 5]), (1, 3, 2, [700] * 9)])
+def test_attend_over_its_own_queries(K, G, heads, t, lens):
+    """out may be q: blocks that several CTAs share have read their queries before one of them writes."""
+    rng = np.random.default_rng(31)
+    c, q, k, ks, v, vs, table, lens = _attention_case(K, rng, 32, G, heads, t, lens)
+    alone = _attend(c, q, table, lens)
+    wide = torch.full((q.shape[0], t, G * heads + 3, 128), 7.0, dtype=torch.bfloat16, device=DEV)
+    for x in (T.to_torch(q), wide[:, :, 1:1 + G * heads]):
+        for _ in range(5):
+            x.copy_(T.to_torch(q))
+            lse = torch.zeros(q.shape[:3], device=DEV)
+            c.attend(x, _dev(table), _dev(lens), 0, x, lse)
+            assert c.status() == K.KVE_OK
+            assert np.array_equal(x.float().cpu().numpy(), alone[0]) and np.array_equal(lse.cpu().numpy(), alone[1])
+    assert bool((wide[:, :, :1] == 7).all()) and bool((wide[:, :, 1 + G * heads:] == 7).all())
+
+
+def test_empty_batches(K):
+    c = _cache(K, 8, 2, 16, 8, 4, 3)
+    table, lens, free, ring = c.state()
+    none = dict(dtype=torch.bfloat16, device=DEV)
+    c.store(torch.empty((0, 2, 128), **none), torch.empty((0, 2, 128), **none), lens[0, :0])
+    c.attend(torch.empty((0, 2, 8, 128), **none), table, lens, 0, torch.empty((0, 2, 8, 128), **none),
+             torch.empty((0, 2, 8), device=DEV))
+    no_slots = torch.empty((1, 0), dtype=torch.int32, device=DEV)
+    c.pages(lens, lens.clone(), table, free, ring, ring, lens, no_slots)
+    assert c.status() == K.KVE_OK and ring.tolist() == [0, 8]
+    c.pages(lens, lens + 1, table, free, ring, ring, lens, no_slots)      # tokens, and room for none
+    assert c.status() == K.KVE_ECUDA and ring.tolist() == [0, 8] and lens.tolist() == [[0, 0, 0]]
+
+
 def test_two_caches_at_once(K):
     """Two caches, each with its own workspace, on two streams at once."""
     rng = np.random.default_rng(28)
@@ -665,6 +696,9 @@ def test_eviction_that_finds_too_few_pages_writes_none(K):
         assert plan.status(bufs.ws, stream) == K.KVE_OK and c.status(stream) == K.KVE_EPAGES
         _same_pool(c, before[0])
         assert lens.tolist() == before[1] and ring.tolist() == before[2]
+        c.gather(plan, k, v, bufs.indices, table, 0, side)      # nor does one behind the status call
+        assert c.status(side) == K.KVE_OK
+        _same_pool(c, before[0])
     # the same with the pages given back first
     c.pages(lens, torch.zeros_like(lens), table, free, ring, ring, lens)
     torch.cuda.synchronize()
