@@ -278,6 +278,7 @@ cache_attend_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_const
     filled += len > 0;
   }
   if (warp == 1) {
+    __syncwarp();   // (the lanes leave the loop at different times)
     tmem_alloc(&ctl.tmem_base, C::kTmemCols);
     tmem_relinquish();
   }
@@ -1004,6 +1005,7 @@ cache_attend_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_const
   tc_fence_before();
   __syncthreads();
   if (warp == 1) {
+    __syncwarp();
     tc_fence_after();
     tmem_dealloc(tmem, C::kTmemCols);
   }
