@@ -22,9 +22,9 @@
 // (a thread is a token and 4 or 8 rows, then a column of the output). Two CTAs an SM, 96 KB of tiles each: with
 // three V stages instead of four 16 rows take 73 us instead of 57 on 131072 tokens.
 //
-// Measured (device): 64 sequences of 512 to 16384 tokens, 446 MB, 74.9 us = 88% of the HBM peak; one of 131072,
-// 269 MB, 47.6 us = 83%, 8 us of them the start (lengths, cut, first tiles) and the join of 38 parts a head; 24 of
-// 500 to 8192 with 4 drafts each (16 rows), 125 MB, 33.0 us = 56%, bound by the softmax warps' instructions;
+// Measured (device): 64 sequences of 512 to 16384 tokens, 446 MB, 72.8 us = 90% of the HBM peak; one of 131072,
+// 269 MB, 46.4 us = 85%, 8 us of them the start (lengths, cut, first tiles) and the join of 38 parts a head; 24 of
+// 500 to 8192 with 4 drafts each (16 rows), 125 MB, 31.8 us = 58%, bound by the softmax warps' instructions;
 // 16 of 96 to 700 8.4 us; one of 96 5.1 us, a chain of latencies.
 //
 // The work is cut over the tokens: all (sequence, head, row block)s' tiles in one line, an equal share of it
@@ -79,7 +79,7 @@ struct Block {
 // `least` tiles of a block on one of its sides moves to that end of the block: a join costs more than those
 // tiles do. That is 4 tiles where a share is 8 units at most and 2 where it is longer and evenness counts
 // for more: 16 sequences of 96 to 700 tokens take 8.4 us with 4 against 9.3 with 2 and 10.6 with 1, 24 of 500
-// to 8192 with 4 drafts each (a share of 16) 35.8 with 4 against 33.0 with 2. With kPartTiles = 0 they take
+// to 8192 with 4 drafts each (a share of 16) 34.2 with 4 against 31.8 with 2. With kPartTiles = 0 they take
 // 10.5 and 35.5, and 64 sequences of 512 to 16384 79.9 instead of 75. No more CTAs take part than have
 // kLeastUnits each, or a block.
 constexpr int kPartTiles = 2, kLeastUnits = 4;
@@ -410,6 +410,11 @@ cache_attend_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_const
       float2 sc = scales(now);
       const uint32_t n = x1 - x0;
       uint32_t it = 0;
+      // Pages of a call that reads more than L2 keeps anyway (8 tiles a share are 78 MB) leave it first: 64 ragged
+      // sequences 75.4 -> 72.8 us, 131072 tokens 47.9 -> 46.4, and row blocks that read a page several times are no
+      // slower (16 sequences of 8192 with 8 drafts 90.7 -> 90.0). Smaller caches may be there at the next call:
+      // 16 of 96 to 700 tokens would go from 8.36 to 8.5.
+      const uint64_t pol = n > 8 ? l2_policy_evict_first() : l2_policy_evict_normal();
       for (; it < n; ++it) {
         const uint32_t ks_at = it % kKStages, st = it % kVStages;
         const bool ok = valid(now.id);
@@ -430,8 +435,8 @@ cache_attend_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_const
         __syncwarp();
         if (ok) {
           const int row = (now.id * P.c.heads + now.b.h) << P.c.page_shift;
-          tma_load_2d(smem + ks_at * kTileBytes + lane * page_bytes, &tm_k, 0, row, &ctl.k_full[ks_at]);
-          tma_load_2d(smem + C::kV + st * kTileBytes + lane * page_bytes, &tm_v, 0, row, &ctl.v_full[st]);
+          tma_load_2d_hint(smem + ks_at * kTileBytes + lane * page_bytes, &tm_k, 0, row, &ctl.k_full[ks_at], pol);
+          tma_load_2d_hint(smem + C::kV + st * kTileBytes + lane * page_bytes, &tm_v, 0, row, &ctl.v_full[st], pol);
         }
         // the largest scale of the tile's values comes out of the sums; a token keeps the rest (at most 1)
         const float top = warp_max(sc.y);
