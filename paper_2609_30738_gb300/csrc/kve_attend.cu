@@ -12,10 +12,14 @@
 // exact enough as sums of e4m3 pieces, each piece a column of its own:
 //   q (8 significant bits) = hi + lo / 16, two pieces of 4 bits: exact but for elements below 2^-13 of
 //     the row's largest, which keep an absolute error of 2^-21 of it;
-//   p = hi + mid / 16 + lo / 256, three pieces: a relative 2^-12, below 2^-4 of the final bf16 rounding.
-//     Two pieces would be the 2^-8 that bf16 probabilities have.
-// Statistics, sums and the output accumulate in fp32 registers: a tile's O^T is added to them scaled by
-// exp(old maximum - new), so TMEM holds one tile's products and is never rescaled.
+//   p = hi + mid / 16 + lo / 256, three pieces of the probability against its own tile's maximum: a relative
+//     2^-12 (2^-4 of the final bf16 rounding) down to 2^-14 of that maximum, an absolute 2^-26 of it below. Two
+//     pieces would be the 2^-8 that bf16 probabilities have. Against the row's maximum every later tile of a
+//     row with one dominating token would lie in the absolute part: the output of 700 equal tokens beside
+//     one of probability 0.9993 and values 0 was off by 1.5e-2 (norm), and is by 5.6e-4 now. What a tile loses
+//     is 2^-19 of its largest value at most (128 tokens of 2^-26), half the step of its page's codes.
+// Statistics, sums and the output accumulate in fp32 registers: a tile's O^T is added to them, row by row,
+// times exp(tile's maximum - maximum so far), so TMEM holds one tile's products and is never rescaled.
 //
 // Warps: the TMA producer (pages two tiles and scales one tile ahead), the MMA issuer (scores two tiles ahead of
 // the value product), two that quantise the next block's query rows, and four softmax warps, eight for 16 rows
@@ -125,7 +129,9 @@ struct ACtl {
   uint32_t pages[kVStages];                    // bit j: page j of the tile holds tokens
   static constexpr uint32_t kQBufs = ACfg<R, H>::kQBufs;
   alignas(16) float red[2][4][R];              // row maxima of the warps, by tile parity
-  alignas(16) float2 ref[4 * H][R / H];        // of each warp's rows: the maximum, exp(old maximum - new)
+  // of a tile's rows: its maximum, exp(old maximum - new), exp(tile's maximum - new), and by the tile's parity that
+  // times vtop (each warp of the rows writes the same)
+  alignas(16) float top[R], kept[R], share[R], back[2][R];
   float sum[kQBufs > 2 ? 2 : 1][4][R];         // row sums of the warps, at the end of a part (by its parity)
   // of the rows of a part in each query buffer: log2(e) / sqrt(d) / the power of two in the q pieces; tokens
   // that the row sees; where its output goes (elements of out, of lse), -1 for no row
@@ -191,7 +197,8 @@ __device__ __forceinline__ float2 e4m3x2_values(uint32_t two) {
 
 // Three e4m3 pieces of two values of at most 256: x = hi + mid / 16 + lo / 256, each pair in 16 bits. The
 // values are rounded to f16 first (2^-12 of them; below 2^-14 an absolute 2^-25), whose 11 bits three
-// pieces of 4 hold, so that the rest is exact in packed f16.
+// pieces of 4 hold, so that the rest is exact in packed f16, down to 2^-6: below that a piece is subnormal, and
+// the sum of the three a multiple of 2^-17.
 __device__ __forceinline__ void e4m3_pieces(float lo, float hi, uint32_t (&piece)[3]) {
   uint32_t x;
   asm("cvt.rn.f16x2.f32 %0, %1, %2;" : "=r"(x) : "f"(hi), "f"(lo));
@@ -618,7 +625,6 @@ cache_attend_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_const
     bool ok = true;
     float m = -INFINITY;                 // lane i: row i's maximum so far
     float l[N], acc[N];
-    float back = 0.f;                    // the last tile's scale of O^T
     // adds tile `it`'s O^T
     const auto take = [&](uint32_t it) -> bool {
       if (!warp_wait(&ctl.o_full, it & 1, P.wait_limit_ns, &ctl.abort)) return false;
@@ -636,19 +642,21 @@ cache_attend_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_const
 #pragma unroll
         for (int i = 0; i < N; ++i) {
           const float y = fmaf(fmaf(o[2 * N + i], 0.0625f, o[N + i]), 0.0625f, o[i]);
-          acc[i] = fmaf(y, back, acc[i]);
+          acc[i] = fmaf(y, ctl.back[it & 1][i0 + i], acc[i]);
         }
       } else {
         static_assert(N == 8, "a load of 8 columns a piece");
-        float f = back;
 #pragma unroll
-        for (int k = 0; k < 3; ++k) {   // (one after the other: 80 registers, and together they spill)
-          float o[N];
-          tmem_ld8(tmem + C::kOCol + k * R + i0 + my_lanes, o);
+        for (int g = 0; g < N; g += 4) {   // (four rows at a time: 80 registers, and all together spill)
+          float o[12];
+#pragma unroll
+          for (int k = 0; k < 3; ++k) tmem_ld4(tmem + C::kOCol + k * R + i0 + g + my_lanes, o + 4 * k);
           tmem_wait_ld(o);
 #pragma unroll
-          for (int i = 0; i < N; ++i) acc[i] = fmaf(o[i], f, acc[i]);
-          f *= 0.0625f;
+          for (int i = 0; i < 4; ++i) {
+            const float y = fmaf(fmaf(o[8 + i], 0.0625f, o[4 + i]), 0.0625f, o[i]);
+            acc[g + i] = fmaf(y, ctl.back[it & 1][i0 + g + i], acc[g + i]);
+          }
         }
       }
       return true;
@@ -799,21 +807,22 @@ cache_attend_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_const
           due = false;
         }
       }
-      back = vtop;
       if (lane < N) {   // lane i: row i's maximum
         const float top = fmaxf(fmaxf(ctl.red[it & 1][0][i0 + lane], ctl.red[it & 1][1][i0 + lane]),
                                 fmaxf(ctl.red[it & 1][2][i0 + lane], ctl.red[it & 1][3][i0 + lane]));
-        const float mn = fmaxf(m, top), ref = mn == -INFINITY ? 0.f : mn;
-        ctl.ref[half * 4 + quad][lane] = make_float2(ref, ex2(m - ref));
+        const float mn = fmaxf(m, top), to = mn == -INFINITY ? 0.f : mn, share = ex2(top - to);
+        ctl.top[i0 + lane] = top == -INFINITY ? 0.f : top;
+        ctl.kept[i0 + lane] = ex2(m - to);
+        ctl.share[i0 + lane] = share;
+        ctl.back[it & 1][i0 + lane] = share * vtop;
         m = mn;
       }
       __syncwarp();
 #pragma unroll
       for (int i = 0; i < N; ++i) {
-        const float2 r = ctl.ref[half * 4 + quad][i];
-        const float p = ex2(w[i] - r.x);
-        acc[i] *= r.y;   // (the tile before is in it; this one's product comes later)
-        l[i] = fmaf(l[i], r.y, p);
+        const float p = ex2(w[i] - ctl.top[i0 + i]), kept = ctl.kept[i0 + i];
+        acc[i] *= kept;   // (the tile before is in it; this one's product comes later)
+        l[i] = fmaf(l[i], kept, p * ctl.share[i0 + i]);
         w[i] = p * vrest;
       }
       if (!whole || some) {   // (a scale that is NaN, of tokens that a row does not see)
