@@ -18,6 +18,9 @@
 //     row with one dominating token would lie in the absolute part: the output of 700 equal tokens beside
 //     one of probability 0.9993 and values 0 was off by 1.5e-2 (norm), and is by 5.6e-4 now. What a tile loses
 //     is 2^-19 of its largest value at most (128 tokens of 2^-26), half the step of its page's codes.
+//     Where a tile's pages have different value scales the pieces are of the probability times its page's, and
+//     "maximum" means the largest of these products that the row sees: a page of far larger values costs the
+//     others nothing where it is not seen (the newest drafts') or hardly counts.
 // Statistics, sums and the output accumulate in fp32 registers: a tile's O^T is added to them, row by row,
 // times exp(tile's maximum - maximum so far), so TMEM holds one tile's products and is never rescaled.
 //
@@ -46,6 +49,10 @@ constexpr int kTileBytes = kTileKeys * kHeadDim;
 constexpr int kMostTilePages = kTileKeys / 16;
 
 constexpr int kNoNan = 255;   // of positions 0 .. 126
+
+// The least log2 of a page's value scale over its tile's largest one that the reference of a row's probabilities
+// follows: beyond it they would leave fp32.
+constexpr float kLeastRatio = -112.f;
 
 constexpr int up16(int x) { return (x + 15) / 16 * 16; }
 
@@ -123,14 +130,15 @@ struct ACtl {
   uint64_t m_full[kVStages];                   // the scales beside a V stage
   uint64_t s_full[2], q_full[ACfg<R, H>::kQBufs], q_empty[ACfg<R, H>::kQBufs];
   uint64_t p_full, o_full, meet[H], joined[H], drain;
-  // of a tile's pages: the keys' scale, and the values' as 256 times a share of the tile's largest one
-  float ks[kVStages][kMostTilePages], vs[kVStages][kMostTilePages];
+  // of a tile's pages: the keys' scale, and the values' as 256 times a share of the tile's largest one, and that share's
+  // log2
+  float ks[kVStages][kMostTilePages], vs[kVStages][kMostTilePages], lvs[kVStages][kMostTilePages];
   float vtop[kVStages];                        // that largest one / 256
   uint32_t pages[kVStages];                    // bit j: page j of the tile holds tokens
   static constexpr uint32_t kQBufs = ACfg<R, H>::kQBufs;
   alignas(16) float red[2][4][R];              // row maxima of the warps, by tile parity
-  // of a tile's rows: its maximum, exp(old maximum - new), exp(tile's maximum - new), and by the tile's parity that
-  // times vtop (each warp of the rows writes the same)
+  // of a tile's rows: the maximum (logit and log2 of the value scale over the tile's largest), exp(old maximum - new),
+  // exp(tile's maximum - new), and by the tile's parity that times vtop (each warp of the rows writes the same)
   alignas(16) float top[R], kept[R], share[R], back[2][R];
   float sum[kQBufs > 2 ? 2 : 1][4][R];         // row sums of the warps, at the end of a part (by its parity)
   // of the rows of a part in each query buffer: log2(e) / sqrt(d) / the power of two in the q pieces; tokens
@@ -448,8 +456,10 @@ cache_attend_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_const
         // the largest scale of the tile's values comes out of the sums; a token keeps the rest (at most 1)
         const float top = warp_max(sc.y);
         if (lane < kMostTilePages) {
+          const float share = top > 0.f ? sc.y * rcp(top) : sc.y;
           ctl.ks[st][lane] = sc.x;
-          ctl.vs[st][lane] = top > 0.f ? sc.y * rcp(top) * 256.f : 0.f;
+          ctl.vs[st][lane] = share * 256.f;
+          ctl.lvs[st][lane] = fmaxf(lg2(share), kLeastRatio);
         }
         if (lane == 0) ctl.vtop[st] = top * (1.f / 256.f);
         __syncwarp();
@@ -755,7 +765,7 @@ cache_attend_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_const
       const int pg = tid >> P.c.page_shift;
       const uint32_t have = ctl.pages[st];
       const bool held = (have >> pg & 1u) && pos < len;
-      const float ks = ctl.ks[st][pg];
+      const float ks = ctl.ks[st][pg], lv = ctl.lvs[st][pg];
       const float vrest = held ? ctl.vs[st][pg] : 0.f, vtop = ctl.vtop[st];
       if (!warp_wait(&ctl.s_full[it & 1], (it >> 1) & 1, P.wait_limit_ns, &ctl.abort)) {
         ok = false;
@@ -787,7 +797,7 @@ cache_attend_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_const
       float* red = &ctl.red[it & 1][quad][i0];
 #pragma unroll
       for (int i = 0; i < N; ++i) {
-        const float top = warp_max(w[i]);
+        const float top = warp_max(w[i] + lv);
         if (lane == i) red[i] = top;
       }
       meet_arrive();

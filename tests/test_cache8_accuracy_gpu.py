@@ -97,3 +97,38 @@ def test_one_token_has_the_probability_and_no_value(K, P, G, t, n, share, flat):
     a = logit / (128 * 64.0 * 2.0 ** -6 / math.sqrt(128.0))
     q = T.bf16(a * sign * np.linspace(0.97, 1.0, t * G).reshape(1, t, G, 1))
     _check(K, q, k, ks, v, vs, table, [n], G)
+
+
+@pytest.mark.parametrize("P,G,t", [(16, 1, 4), (32, 2, 4), (64, 4, 4), (16, 4, 12), (64, 1, 2)])
+@pytest.mark.parametrize("up", [3, 20, 28, 36, 60, 100])
+def test_a_large_value_page_that_earlier_queries_do_not_see(K, P, G, t, up):
+    """The newest draft begins a page whose values are 2^up times the others'."""
+    rng = np.random.default_rng(P + up)
+    lens = [2 * P + 1, 128 + P + 1, 1025]
+    table, pages = T.table_for(rng, lens, P)
+    k, ks = T.pool(rng, pages, 1, P)
+    v, vs = T.pool(rng, pages, 1, P)
+    for r, n in enumerate(lens):
+        vs[table[r, n // P], 0] = 2.0 ** (up - 7)
+    q = T.rows(rng, (3, t, G, 128))
+    _check(K, q, k, ks, v, vs, table, lens, G)
+
+
+@pytest.mark.parametrize("P,G,t", [(16, 4, 1), (32, 4, 2), (64, 4, 4), (16, 1, 1)])
+@pytest.mark.parametrize("up,down", [(20, 10), (40, 40), (40, 60), (60, 30), (100, 110), (2, 30)])
+def test_a_large_value_page_with_small_probabilities(K, P, G, t, up, down):
+    """Pages whose values are 2^up times the others' and whose probabilities 2^-down of theirs."""
+    rng = np.random.default_rng(up + down)
+    n = 700
+    table, pages = T.table_for(rng, [n], P)
+    k, ks = T.pool(rng, pages, 1, P)
+    v, vs = T.pool(rng, pages, 1, P)
+    ks[:], vs[:] = 2.0 ** -6, 2.0 ** -7
+    sign = rng.choice([-1.0, 1.0], 128)
+    k[:] = C.encode(rng.standard_normal(k.shape))
+    a = down * math.log(2.0) / (128 * 64.0 * 2.0 ** -6 / math.sqrt(128.0))
+    for j in (1, 3, 700 // P - 1):
+        k[table[0, j], 0] = C.encode(-64.0 * sign)
+        vs[table[0, j], 0] = 2.0 ** (up - 7)
+    q = T.bf16(a * sign * np.linspace(0.97, 1.0, t * G).reshape(1, t, G, 1))
+    _check(K, q, k, ks, v, vs, table, [n], G)
