@@ -138,7 +138,8 @@ struct ACtl {
   static constexpr uint32_t kQBufs = ACfg<R, H>::kQBufs;
   alignas(16) float red[2][4][R];              // row maxima of the warps, by tile parity
   // of a tile's rows: the maximum (logit and log2 of the value scale over the tile's largest), exp(old maximum - new),
-  // exp(tile's maximum - new), and by the tile's parity that times vtop (each warp of the rows writes the same)
+  // exp(tile's maximum - new) in units of the row's sum, and by the tile's parity that times vtop
+  // (each warp of the rows writes the same)
   alignas(16) float top[R], kept[R], share[R], back[2][R];
   float sum[kQBufs > 2 ? 2 : 1][4][R];         // row sums of the warps, at the end of a part (by its parity)
   // of the rows of a part in each query buffer: log2(e) / sqrt(d) / the power of two in the q pieces; tokens
@@ -230,7 +231,14 @@ __device__ __forceinline__ uint16_t to_bf16(float x) {
   return d;
 }
 
-// ln of a row's sum given its maximum in log2 units (no token seen: -inf; a NaN sum is not 0, its row is NaN).
+// Probabilities are summed as 2^-len_bits(len) of themselves: then neither a row's sum passes 1 nor its unnormalised
+// output the largest value (values of 2e38 would, taken 100 times). In return an output keeps an absolute 2^-133 len,
+// the last bit of the factor of O^T.
+__device__ __forceinline__ float len_bits(int len) {
+  return static_cast<float>(32 - __clz(len - 1));   // (1: 0)
+}
+
+// ln of a row's sum given the log2 of its unit (no token seen: -inf; a NaN sum is not 0, its row is NaN).
 __device__ __forceinline__ float log_sum(float top, float sum) {
   return sum == 0.f ? -INFINITY : ((top == -INFINITY ? 0.f : top) + lg2(sum)) * 0.69314718056f;
 }
@@ -624,6 +632,7 @@ cache_attend_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_const
       return warp_wait(&ctl.meet[half], met++ & 1u, P.wait_limit_ns, &ctl.abort);
     };
     int len = 0, block0 = 0, block1 = 0;   // the part's sequence, its block's tiles of the line
+    float unit = 0.f;                      // len_bits(len)
     const uint32_t n = x1 - x0;
     uint32_t part = 0;
     int splits = 0;
@@ -681,6 +690,7 @@ cache_attend_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_const
       if (!warp_wait(&ctl.q_full[part % C::kQBufs], (part / C::kQBufs) & 1, P.wait_limit_ns, &ctl.abort)) return false;
       const Block& b = ctl.blocks[part % C::kQBufs];
       len = b.len;
+      unit = len_bits(len);
       block0 = b.first;
       block1 = b.first + b.tiles;
       return true;
@@ -730,7 +740,7 @@ cache_attend_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_const
           if (to >= 0) P.out[to + tid] = to_bf16(acc[i] * f);
         }
         if (P.lse && quad == 0 && lane < N && ctl.out_at[qb][i0 + lane] >= 0)
-          P.lse[ctl.lse_at[qb][i0 + lane]] = log_sum(m, sum);
+          P.lse[ctl.lse_at[qb][i0 + lane]] = log_sum(m + len_bits(end.len), sum);
       } else {
         // one of several parts of the block: left for the join. Slot 1 of the CTA is for a block's first part
         // (its own last one), slot 0 for a later one (its own first)
@@ -820,7 +830,7 @@ cache_attend_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_const
       if (lane < N) {   // lane i: row i's maximum
         const float top = fmaxf(fmaxf(ctl.red[it & 1][0][i0 + lane], ctl.red[it & 1][1][i0 + lane]),
                                 fmaxf(ctl.red[it & 1][2][i0 + lane], ctl.red[it & 1][3][i0 + lane]));
-        const float mn = fmaxf(m, top), to = mn == -INFINITY ? 0.f : mn, share = ex2(top - to);
+        const float mn = fmaxf(m, top), to = mn == -INFINITY ? 0.f : mn, share = ex2(top - (to + unit));
         ctl.top[i0 + lane] = top == -INFINITY ? 0.f : top;
         ctl.kept[i0 + lane] = ex2(m - to);
         ctl.share[i0 + lane] = share;
@@ -1019,7 +1029,7 @@ cache_attend_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_const
           v.x = to_bf16(a4[i].x * inv) | static_cast<uint32_t>(to_bf16(a4[i].y * inv)) << 16;
           v.y = to_bf16(a4[i].z * inv) | static_cast<uint32_t>(to_bf16(a4[i].w * inv)) << 16;
           reinterpret_cast<uint2*>(P.out + tok * P.o_st + hq * P.o_sh)[lane] = v;
-          if (P.lse && lane == 0) P.lse[tok * P.c.hq + hq] = log_sum(top[i], sum[i]);
+          if (P.lse && lane == 0) P.lse[tok * P.c.hq + hq] = log_sum(top[i] + len_bits(b.len), sum[i]);
         }
       }
     }

@@ -132,3 +132,19 @@ def test_a_large_value_page_with_small_probabilities(K, P, G, t, up, down):
         vs[table[0, j], 0] = 2.0 ** (up - 7)
     q = T.bf16(a * sign * np.linspace(0.97, 1.0, t * G).reshape(1, t, G, 1))
     _check(K, q, k, ks, v, vs, table, [n], G)
+
+
+@pytest.mark.parametrize("P,G,t", [(16, 4, 1), (64, 8, 1), (128, 4, 4)])
+@pytest.mark.parametrize("n", [1, 96, 3000, 20011])
+def test_values_near_the_largest_that_bf16_holds(K, P, G, t, n):
+    """An average of values of 2e38 and more is one of them, whatever its unnormalised sum would be."""
+    rng = np.random.default_rng(n + P)
+    table, pages = T.table_for(rng, [n], P)
+    k, ks = T.pool(rng, pages, 1, P)
+    v, vs = T.pool(rng, pages, 1, P)
+    v[:] = C.encode(rng.uniform(320, 416, v.shape))
+    vs[:] = 2.0 ** 119
+    q = T.rows(rng, (1, t, G, 128))
+    if t > 1 and n < t:
+        q = q[:, :1]
+    _check(K, q, k, ks, v, vs, table, [n], G)
