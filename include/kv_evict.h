@@ -367,8 +367,10 @@ typedef struct {
 
 typedef struct kve_cache kve_cache;
 
-/* A cache of cfg over device buffers that the caller owns (k and v 128-byte, the scales
- * 16-byte aligned; nothing is written). The handle owns host memory only.
+/* A cache of cfg over device buffers of one device that the caller owns (k and v 128-byte,
+ * the scales 16-byte aligned; nothing is written; KVE_EINVAL where one of them is host
+ * memory or another device's; where the CUDA runtime knows none of them, they are taken
+ * as they are). The handle owns host memory only.
  * *workspace_bytes receives the size of ws. */
 kve_status kv_evict_cache_create(const kve_cache_config* cfg, uint8_t* k, uint8_t* v,
                                  float* k_scale, float* v_scale, kve_cache** cache_out,

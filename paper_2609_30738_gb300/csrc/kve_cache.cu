@@ -666,6 +666,17 @@ bool row_strides(const int64_t* given, int64_t heads, int64_t* token, int64_t* h
   return true;
 }
 
+// The device that holds p; kHostMemory for pinned host memory, kUnknown where the runtime does not know the pointer.
+constexpr int kUnknown = -1, kHostMemory = -2;
+int place_of(const void* p) {
+  cudaPointerAttributes at;
+  if (cudaPointerGetAttributes(&at, p) != cudaSuccess) {
+    cudaGetLastError();
+    return kUnknown;
+  }
+  return at.type == cudaMemoryTypeDevice ? at.device : at.type == cudaMemoryTypeHost ? kHostMemory : kUnknown;
+}
+
 // The call's device is the buffers' device.
 bool on_device(const kve_cache* c) {
   if (c->device < 0) return true;
@@ -695,6 +706,11 @@ kve_status kv_evict_cache_create(const kve_cache_config* cfg, uint8_t* k, uint8_
   // rows of the pool are 32-bit TMA coordinates
   if (static_cast<int64_t>(c.num_pages) * c.page_tokens >= (int64_t(1) << 31) / c.num_kv_heads) return KVE_EINVAL;
   if (!aligned(k, 128) || !aligned(v, 128) || !aligned(k_scale, 16) || !aligned(v_scale, 16)) return KVE_EINVAL;
+  // the kernels follow all four: device memory of one device
+  const int device = place_of(k);
+  if (device == kHostMemory) return KVE_EINVAL;
+  for (const void* p : {static_cast<const void*>(v), static_cast<const void*>(k_scale), static_cast<const void*>(v_scale)})
+    if (place_of(p) != device) return KVE_EINVAL;
   kve_cache* h = new (std::nothrow) kve_cache;
   if (!h) return KVE_ENOMEM;
   std::memset(h, 0, sizeof(*h));
@@ -712,11 +728,8 @@ kve_status kv_evict_cache_create(const kve_cache_config* cfg, uint8_t* k, uint8_
   g.v = v;
   g.k_scale = k_scale;
   g.v_scale = v_scale;
-  cudaPointerAttributes at;
-  h->device = -1;
-  if (cudaPointerGetAttributes(&at, k) == cudaSuccess && at.type == cudaMemoryTypeDevice) h->device = at.device;
-  cudaGetLastError();
-  int dev = h->device, sms = 0;
+  h->device = device;
+  int dev = device, sms = 0;
   if ((dev < 0 && cudaGetDevice(&dev) != cudaSuccess) ||
       cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, dev) != cudaSuccess) {
     cudaGetLastError();

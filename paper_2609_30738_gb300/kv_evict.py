@@ -429,9 +429,10 @@ class Cache8:
         self.num_layers, self.num_q_heads, self.head_dim = spec["num_layers"], spec["num_q_heads"], spec["head_dim"]
         self.max_seqs, self.num_pages, self.max_pages, self.page_tokens = max_seqs, num_pages, max_pages, page_tokens
         shape = (num_pages, self.heads, page_tokens, self.head_dim)
+        self._h = None
+        device = self._one_device([t for t in (k, v, k_scale, v_scale) if t is not None], device)
         self.k, self.v = (self._buffer(t, shape, torch.uint8, device) for t in (k, v))
         self.k_scale, self.v_scale = (self._buffer(t, shape[:2], torch.float32, device) for t in (k_scale, v_scale))
-        self._h = None
         if self.k.device.type != "cuda":
             raise ValueError("Cache8: the pages are device memory")
         cfg = CacheConfig(self.num_layers, self.num_q_heads, self.heads, self.head_dim, page_tokens, num_pages,
@@ -466,6 +467,14 @@ class Cache8:
     def _stream(self, stream):
         """The stream's address; None is the current stream of the cache's device."""
         return self._current_stream() if stream is None else _stream_ptr(stream)
+
+    @staticmethod
+    def _one_device(given, device):
+        """The device of the given pages and scales, where the others are allocated too; `device` where none is
+        given."""
+        if any(t.device != given[0].device for t in given):
+            raise ValueError("Cache8: k, v and their scales are on one device")
+        return given[0].device if given else device
 
     @staticmethod
     def _buffer(t, shape, dtype, device):

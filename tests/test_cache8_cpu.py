@@ -199,6 +199,17 @@ def test_binding_refuses():
         K.Cache8(dict(num_layers=1, num_q_heads=8, num_kv_heads=2, head_dim=128), 2, 8, 4, 16, device="cpu")
 
 
+def test_pool_tensors_are_on_one_device():
+    torch = pytest.importorskip("torch")
+    K = _k()
+    here, there = torch.empty(2), torch.empty(2, device="meta")
+    assert K.Cache8._one_device([], "cuda") == "cuda"
+    assert K.Cache8._one_device([there, there], "cuda") == there.device
+    for given in ([here, there], [there, there, here]):
+        with pytest.raises(ValueError):
+            K.Cache8._one_device(given, "cuda")
+
+
 def test_kept_lens_of_a_plan():
     torch = pytest.importorskip("torch")
     from paper_2609_30738_gb300 import kv_evict as K

@@ -623,6 +623,37 @@ def test_binding_checks_what_it_is_given(K):
         c.attend(torch.zeros((4, 1, 8, 128), dtype=torch.bfloat16, device=DEV), table, lens, 0, torch.zeros_like(q).repeat(2, 1, 1, 1)[:4])
 
 
+def test_pool_in_host_memory_is_refused(K):
+    """Any of the four tensors on the host, pinned or not, through the binding and through the C call."""
+    import ctypes
+    spec = dict(num_layers=1, num_q_heads=8, num_kv_heads=2, head_dim=128)
+    make = lambda: dict(k=torch.zeros((8, 2, 16, 128), dtype=torch.uint8, device=DEV),  # noqa: E731
+                        v=torch.zeros((8, 2, 16, 128), dtype=torch.uint8, device=DEV),
+                        k_scale=torch.zeros((8, 2), device=DEV), v_scale=torch.zeros((8, 2), device=DEV))
+    cfg = K.CacheConfig(1, 8, 2, 128, 16, 8, 4, 3)
+
+    def create(bufs):
+        h, n = ctypes.c_void_p(), ctypes.c_size_t()
+        st = K.library().kv_evict_cache_create(ctypes.byref(cfg), *[bufs[x].data_ptr() for x in ("k", "v", "k_scale", "v_scale")],
+                                               ctypes.byref(h), ctypes.byref(n))
+        K.library().kv_evict_cache_destroy(h)
+        return st
+
+    assert create(make()) == K.KVE_OK
+    for name in make():
+        for pin in (False, True):
+            bufs = make()
+            host = bufs[name].cpu()
+            if pin:
+                host = host.pin_memory()
+            host = host if host.data_ptr() % 128 == 0 else None
+            if host is not None:
+                bufs[name] = host
+                assert create(bufs) == K.KVE_EINVAL
+                with pytest.raises(ValueError):
+                    K.Cache8(spec, 3, 8, 4, 16, **bufs)
+
+
 @pytest.mark.parametrize("G,heads,t,lens", [(4, 2, 1, [5000, 0, 3, 129]), (4, 1, 9, [40, 0, 20000, 5]), (1, 3, 2, [700] * 9)])
 def test_attend_over_its_own_queries(K, G, heads, t, lens):
     """out may be q: blocks that several CTAs share have read their queries before one of them writes."""
