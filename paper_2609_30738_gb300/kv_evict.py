@@ -178,6 +178,7 @@ class Plan:
                    "kv_evict_plan_layered")
         self._h = handle
         self.workspace_bytes = ws.value
+        self._kv_spans = (self._span(None),) * 2
         if k_strides is not None or v_strides is not None:
             self.set_kv_strides(k_strides, v_strides)
 
@@ -225,6 +226,29 @@ class Plan:
         _check(_lib().kv_evict_plan_set_kv_strides(self._h, None if ks is None else ks.ctypes.data,
                                                     None if vs is None else vs.ctypes.data),
                "kv_evict_plan_set_kv_strides")
+        self._kv_spans = tuple(self._span(s) for s in (ks, vs))
+
+    def _span(self, strides):
+        """(elements from the first to the last of the plan's keys or values, whether they are dense)."""
+        shape = (self.spec["num_layers"], self.spec["num_kv_heads"], sum(self.seq_lens))
+        if strides is None:
+            return shape[0] * shape[1] * shape[2] * self.spec["head_dim"], True
+        return sum((n - 1) * int(s) for n, s in zip(shape, strides)) + self.spec["head_dim"], False
+
+    def _check_source(self, name: str, t):
+        """Raises where the bf16 tensor t does not hold every row of the plan's k (name "k") or v at its strides."""
+        global _bf16
+        if _bf16 is None:
+            import torch
+            _bf16 = torch.bfloat16
+        span, dense = self._kv_spans[name == "v"]
+        bf16, whole = t.dtype is _bf16, t.is_contiguous()
+        if bf16 and whole and t.numel() >= span:
+            return
+        held = 1 + sum((n - 1) * s for n, s in zip(t.shape, t.stride())) if t.numel() else 0
+        if not bf16 or dense or held < span:
+            raise ValueError(f"{name}: expected bf16 [num_layers, num_kv_heads, {sum(self.seq_lens)}, d], dense or with "
+                             "the plan's strides")
 
     def set_debug(self, wait_limit_ns: int, fault: int = 0):
         _check(_lib().kv_evict_plan_set_debug(self._h, int(wait_limit_ns), int(fault)),
@@ -535,11 +559,10 @@ class Cache8:
         """kv_evict_cache_gather: the kept and the window rows of plan's requests as sequences first_seq ..;
         k and v as for Plan.gather."""
         for name, t in (("k", k), ("v", v)):
-            dev = getattr(t, "device", None)
-            if dev is not None and getattr(dev, "type", None) == "cpu" and not t.is_pinned():
-                raise ValueError(f"gather: {name} is a pageable CPU tensor; pin it or move it to the GPU")
-            if dev is not None and getattr(dev, "type", None) == "cuda" and t.get_device() != self._device:
-                raise ValueError(f"gather: {name} is on another device than the cache")
+            if not self._here(t):
+                raise ValueError(f"gather: {name} is on another device than the cache, or a pageable CPU tensor; move it "
+                                 "to the cache's device or pin it")
+            plan._check_source(name, t)
         if not self._is_i32(indices, plan.n_units * plan.spec["budget"]) or not self._is_i32(table, self._entries):
             raise ValueError("gather: indices are the plan's int32 [n_units, budget], table is int32 [num_layers, "
                              "max_seqs, max_pages]")

@@ -210,6 +210,33 @@ def test_pool_tensors_are_on_one_device():
             K.Cache8._one_device(given, "cuda")
 
 
+def test_sources_of_a_gather_hold_the_plans_rows():
+    torch = pytest.importorskip("torch")
+    K = _k()
+    spec = dict(num_layers=2, num_q_heads=8, num_kv_heads=2, head_dim=128, window=8, budget=16)
+    bf = dict(dtype=torch.bfloat16)
+    plan = K.Plan(spec, [40, 21])
+    for t in (torch.empty((2, 2, 61, 128), **bf), torch.empty(2 * 2 * 61 * 128 + 8, **bf)):
+        plan._check_source("k", t)
+    for t in (torch.empty((2, 2, 60, 128), **bf), torch.empty((2, 2, 61, 128)), torch.empty((2, 2, 61, 128), dtype=torch.float16),
+              torch.empty(0, **bf), torch.empty((2, 61, 2, 128), **bf).transpose(1, 2),
+              torch.empty((2, 2, 61, 256), **bf)[..., :128]):
+        with pytest.raises(ValueError):
+            plan._check_source("v", t)
+    # queries' heads own the units, the rows are the KV heads'
+    K.Plan(spec, [40, 21], per_query_head=True)._check_source("k", torch.empty((2, 2, 61, 128), **bf))
+    # token-major keys: the tensor as it lies, its view, and one token too few; the values are dense
+    plan.set_kv_strides((61 * 256, 128, 256), None)
+    whole = torch.empty((2, 61, 2, 128), **bf)
+    plan._check_source("k", whole)
+    plan._check_source("k", whole.transpose(1, 2))
+    for name, t in (("k", whole[:, :60].contiguous()), ("k", whole[:1]), ("v", whole.transpose(1, 2))):
+        with pytest.raises(ValueError):
+            plan._check_source(name, t)
+    plan.set_kv_strides(None, None)
+    plan._check_source("k", torch.empty((2, 2, 61, 128), **bf))
+
+
 def test_kept_lens_of_a_plan():
     torch = pytest.importorskip("torch")
     from paper_2609_30738_gb300 import kv_evict as K

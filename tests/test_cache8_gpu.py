@@ -623,6 +623,17 @@ def test_binding_checks_what_it_is_given(K):
         c.attend(torch.zeros((4, 1, 8, 128), dtype=torch.bfloat16, device=DEV), table, lens, 0, torch.zeros_like(q).repeat(2, 1, 1, 1)[:4])
 
 
+def test_gather_checks_its_sources(K):
+    spec = dict(num_layers=1, num_q_heads=8, num_kv_heads=2, head_dim=128, window=8, budget=16)
+    plan, c = K.Plan(spec, [61]), _cache(K, 8, 2, 16, 8, 4, 3)
+    table, idx = c.state()[0], torch.zeros((2, 16), dtype=torch.int32, device=DEV)
+    good = torch.zeros((1, 2, 61, 128), dtype=torch.bfloat16, device=DEV)
+    for bad in (good.float(), good[:, :, :60].contiguous(), good.cpu(), good.view(torch.int16)):
+        for k, v in ((bad, good), (good, bad)):
+            with pytest.raises(ValueError):
+                c.gather(plan, k, v, idx, table)
+
+
 def test_pool_in_host_memory_is_refused(K):
     """Any of the four tensors on the host, pinned or not, through the binding and through the C call."""
     import ctypes
