@@ -408,7 +408,9 @@ kve_status kv_evict_cache_pages(const kve_cache* cache, const int32_t* lens_from
  * in its order (kept candidates ascending, then the window rows), become positions 0 ..
  * m + W - 1 of sequence first_seq + r of every layer, in 8 bits. The table rows of those
  * sequences hold the pages (kv_evict_cache_pages with lens_to = m + W). Rows of the last
- * page behind the sequence are left as they were. Nothing is written where the last
+ * page behind the sequence are left as they were. A kept index outside 0 .. Lc_r - 1 (a
+ * selection that gave up leaves -1) becomes a row of zeros, and kv_evict_cache_status
+ * returns KVE_ECUDA. Nothing is written where the last
  * kv_evict_cache_pages call on ws moved no page: what the table then names can be another
  * sequence's. k, v and indices as for kv_evict_gather
  * (pinned host memory too); the plan and the cache have the same layers and heads. */

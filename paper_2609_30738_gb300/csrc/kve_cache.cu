@@ -443,13 +443,16 @@ __global__ void __launch_bounds__(kRowThreads<kPage>) cache_gather_kernel(const 
   // the positions of this group's rows: lane i looks row i's up
   const int row = j * kPage + g * kGroupRows + (lane & (kGroupRows - 1));
   int src = -1;
+  bool outside = false;
   if (row < m) {
     src = __ldg(P.g.indices + static_cast<int64_t>(unit) * P.g.budget + row);
-    if (src >= Lc) src = -1;   // never read outside the unit
+    outside = src < 0 || src >= Lc;   // never read outside the unit: a row of zeros, and the status tells
+    if (outside) src = -1;
   } else if (row < m + W) {
     src = Lc + (row - m);
   }
   if (refused) return;
+  if (outside) atomicOr(P.err, kErrCheck);
   if (page < 0 || page >= P.c.num_pages) {
     if (g == 0 && lane == 0) atomicOr(P.err, kErrCheck);
     return;

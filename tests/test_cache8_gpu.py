@@ -338,6 +338,36 @@ def test_gather_leaves_bad_pages_out(K):
         assert np.array_equal(c.k.cpu().numpy(), want) and np.array_equal(c.k_scale.cpu().numpy(), s)
 
 
+@pytest.mark.parametrize("P", [16, 64])
+@pytest.mark.parametrize("bad", [-1, 60, 61, 2 ** 31 - 1, -2 ** 31])
+def test_gather_reports_indices_outside_the_candidates(K, P, bad):
+    """A kept index outside the candidates is a row of zeros and an error; the others are written as ever."""
+    rng = np.random.default_rng(P)
+    spec = dict(num_layers=1, num_q_heads=2, num_kv_heads=2, head_dim=128, window=4, budget=20, pool_kernel=1,
+                candidate_factor=1, norm_eps=1e-12)
+    pages = -(-24 // P)
+    pool = T.pool(rng, pages, 2, P) + T.pool(rng, pages, 2, P)
+    c = _cache(K, 2, 2, P, pages, pages, 1, pool=pool)
+    k = T.rows(rng, (1, 2, 64, 128))
+    table = np.arange(pages, dtype=np.int32)
+    for at in ([], [7], [0, 19]):
+        idx = np.stack([np.sort(rng.permutation(60)[:20]) for _ in range(2)]).astype(np.int32)
+        idx[1, at] = bad
+        c.k.copy_(_dev(pool[0]))
+        c.k_scale.copy_(_dev(pool[1]))
+        c.gather(K.Plan(spec, [64]), T.to_torch(k), T.to_torch(k), _dev(idx), _dev(table))
+        assert c.status() == (K.KVE_ECUDA if at else K.KVE_OK) and c.status() == K.KVE_OK
+        want, s = pool[0].copy(), pool[1].astype(np.float64)
+        for h in range(2):
+            rows = np.concatenate([k[0, h, np.clip(idx[h], 0, 63)], k[0, h, 60:]])
+            if h == 1:
+                rows[at] = 0.0
+            one, sc = want[:, h].copy(), s[:, h].copy()
+            C.gather(one, sc, rows, table)
+            want[:, h], s[:, h] = one, sc
+        assert np.array_equal(c.k.cpu().numpy(), want) and np.array_equal(c.k_scale.cpu().numpy(), s)
+
+
 # ------------------------------------------------------------------------------------------------ attention
 
 def _attend(c, q, table, lens, layer=0, lse=True, fill=7.0, stream=None):
