@@ -51,14 +51,20 @@ __device__ __forceinline__ int ring_at(int head, long long i, int n) {
 // alone. A chunk's pages are read in one access, while the chunk before is written, and its slots leave from
 // registers, four at a time: new pages cost their 8 bytes and slots their 4. Before that every CTA sums the pages
 // and tokens that each layer takes and gives (a warp a layer), so that all agree whether the call can be done
-// before one of them writes; these sums are why there is one CTA an SM at most. Where the call changes its inputs in
-// place (lens_out, ring_out), the CTA that finishes reading last does that.
+// before one of them writes. Where the call changes its inputs in place (lens_out, ring_out), the CTA that finishes
+// reading last does that.
 //
 // A decode step (512 sequences, one new token each) is bound by latency: two reads of 8 bytes a sequence from L2
 // and the chain length -> ring entry -> table: 4.8 us. A wave of prompts is bound by the slots' write: 48 of 500 to
 // 32768 tokens in 32 layers (P = 16, 67 MB) 17.6 us, 56% of the HBM peak, of which 5.5 are the decode step's
 // latencies; 201 MB of slots at P = 64 40 us. Slots one at a time took 19.0 and 45.8, four without the read ahead 19.5
 // and 40.6.
+//
+// Every CTA reads all lengths, so there is never more than one an SM: with more than 32 sequences for each (kMany) a CTA
+// takes several groups of 32 after one sum. A sequence's place costs a sum over its layer's sequences in front, so the
+// step stays quadratic in those of one layer: decode steps of 32 layers x 256 sequences 10.8 us, 32 x 1024 45 (72 with a
+// CTA for each 32), 64 x 1024 94 (205).
+template <bool kMany>
 __global__ void __launch_bounds__(kPagesThreads) cache_pages_kernel(const __grid_constant__ PagesParams P) {
   wait_previous_kernel();
   __shared__ long long layer_sum[3][kMaxLayers];   // pages taken, pages given, new tokens
@@ -96,8 +102,8 @@ __global__ void __launch_bounds__(kPagesThreads) cache_pages_kernel(const __grid
   }
   if (bad) bad_word = 1;
   __syncthreads();
-  const int seq = blockIdx.x * kPagesWarps + warp;
-  const int layer = seq < n ? seq / S : layers - 1, r = seq - layer * S;
+  int seq = blockIdx.x * kPagesWarps + warp;
+  int layer = seq < n ? seq / S : layers - 1, r = seq - layer * S;
   long long taken = 0, given = 0, at = 0, back = 0;
   bool too_many = false;
   for (int l = lane; l < layers; l += 32) {
@@ -113,121 +119,134 @@ __global__ void __launch_bounds__(kPagesThreads) cache_pages_kernel(const __grid
   bad = bad_word || __any_sync(0xffffffffu, too_many) || head < 0 || head >= np || count < 0 || count > np ||
         count + given > np;
   const bool ok = !bad && taken <= count;
-  // this warp's sequence: its chunks of 32 pages, its place in the ring and in its layer's slots
-  int chunks = 0;
-  if (seq < n && ok) {
-    const int a = __ldg(P.from + seq), b = __ldg(P.to + seq);
-    const int have = (a + page_mask) >> shift, need = (b + page_mask) >> shift;
-    // from the page of the first new token on, or the released ones
-    chunks = b > a ? (need - (a >> shift) + 31) >> 5 : (have - need + 31) >> 5;
-    if (chunks > 0) {
-      long long before[3];
-      sum_of(P.from + layer * S, P.to + layer * S, r, before);
-      at = warp_sum(at) + before[0];
-      back = warp_sum(back) + before[1];
-      if (lane == 0) {
-        grown[warp] = {a, b, ring_at(head, b > a ? at : count + back, np),
-                       b > a && P.slots ? P.slots + layer * P.slot_stride + before[2] : nullptr,
-                       P.table + static_cast<int64_t>(seq) * P.c.max_pages};
-      }
-    }
-  }
-  if (lane == 0) chunks_of[warp] = chunks;
-  __syncthreads();
-  // all chunks of this CTA's sequences in one line, dealt to its warps (and those of the other blockIdx.y)
-  int last = chunks_of[lane];
-#pragma unroll
-  for (int o = 1; o < 32; o <<= 1) {
-    const int x = __shfl_up_sync(0xffffffffu, last, o);
-    if (lane >= o) last += x;
-  }
-  const int all = __shfl_sync(0xffffffffu, last, 31);
-  // the page of a chunk's lane is read while the chunk before it is written
-  struct Chunk {
-    int w, c, page;   // its sequence, its number there, this lane's page (-1: none)
-  };
-  const auto read = [&](int q) {
-    Chunk k;
-    k.w = __popc(__ballot_sync(0xffffffffu, last <= q)) & 31;   // the sequence whose chunk it is
-    const int before = __shfl_sync(0xffffffffu, last, max(k.w - 1, 0));
-    k.c = q - (k.w > 0 ? before : 0);
-    k.page = -1;
-    if (q >= all) return k;
-    const Grown& s = grown[k.w];
-    const int have = (s.a + page_mask) >> shift, need = (s.b + page_mask) >> shift;
-    if (s.b > s.a) {
-      const int j = (s.a >> shift) + 32 * k.c + lane;
-      if (j < have)
-        k.page = s.row[j];
-      else if (j < need)
-        k.page = P.free_pages[ring_at(s.ring, j - have, np)];
-    } else {
-      const int j = need + 32 * k.c + lane;
-      if (j < have) k.page = s.row[j];
-    }
-    return k;
-  };
-  const int first = blockIdx.y * kPagesWarps + warp, step = kPagesWarps * gridDim.y;
-  Chunk next = read(first);
-  for (int q = first; q < all; q += step) {
-    const Chunk now = next;
-    if (q + step < all) next = read(q + step);
-    const Grown s = grown[now.w];
-    const int c = now.c, page = now.page;
-    const int have = (s.a + page_mask) >> shift, need = (s.b + page_mask) >> shift;
-    if (s.b > s.a) {
-      const int j0 = (s.a >> shift) + 32 * c, j = j0 + lane;
-      if (j >= have && j < need) s.row[j] = page;
-      const int base = page >= 0 && page < np ? page << shift : -1;
-      const bool outside = __any_sync(0xffffffffu, j < need && base < 0);   // a page outside the pool
-      if (outside && lane == 0) atomicOr(P.err, kErrCheck);
-      if (!s.out) continue;
-      // slots [begin, end) of the chunk, counted from its first page
-      const int begin = max(s.a - (j0 << shift), 0), end = min(s.b - (j0 << shift), 32 << shift), len = end - begin;
-      int32_t* const to = s.out + ((j0 << shift) + begin - s.a);
-      if (outside) {
-        // its tokens get no slot
-#pragma unroll 1
-        for (int i = 0; i < len; i += 32) {
-          const int k = begin + i + lane;
-          const int from = __shfl_sync(0xffffffffu, base, k >> shift);
-          if (i + lane < len) to[i + lane] = from < 0 ? -1 : from + (k & page_mask);
+  for (;;) {
+    // this warp's sequence: its chunks of 32 pages, its place in the ring and in its layer's slots
+    int chunks = 0;
+    if (seq < n && ok) {
+      const int a = __ldg(P.from + seq), b = __ldg(P.to + seq);
+      const int have = (a + page_mask) >> shift, need = (b + page_mask) >> shift;
+      // from the page of the first new token on, or the released ones
+      chunks = b > a ? (need - (a >> shift) + 31) >> 5 : (have - need + 31) >> 5;
+      if (chunks > 0) {
+        long long before[3];
+        sum_of(P.from + layer * S, P.to + layer * S, r, before);
+        at = warp_sum(at) + before[0];
+        back = warp_sum(back) + before[1];
+        if (lane == 0) {
+          grown[warp] = {a, b, ring_at(head, b > a ? at : count + back, np),
+                         b > a && P.slots ? P.slots + layer * P.slot_stride + before[2] : nullptr,
+                         P.table + static_cast<int64_t>(seq) * P.c.max_pages};
         }
-        continue;
       }
-      // up to the first multiple of 16 bytes and behind the last one by slot, in between four at a time
-      const int front = min(static_cast<int>(-(reinterpret_cast<uintptr_t>(to) >> 2) & 3), len);
-      const int quads = (len - front) >> 2, rest = (len - front) & 3;
-      {
-        const int i = lane < 16 ? lane : len - 32 + lane, k = begin + i;
-        const int from = __shfl_sync(0xffffffffu, base, k >> shift);
-        if (lane < front || lane >= 32 - rest) to[i] = from + (k & page_mask);
-      }
-#pragma unroll 2
-      for (int i = 0; i < quads; i += 32) {
-        const int q = front + 4 * (i + lane), k = begin + q, off = k & page_mask;
-        const int x = __shfl_sync(0xffffffffu, base, k >> shift) + off;
-        const int y = __shfl_sync(0xffffffffu, base, (k + 3) >> shift) + off - P.c.page;   // of those on the next page
-        if (i + lane < quads)
-          *reinterpret_cast<int4*>(to + q) =
-              make_int4(x, (off + 1 < P.c.page ? x : y) + 1, (off + 2 < P.c.page ? x : y) + 2,
-                        (off + 3 < P.c.page ? x : y) + 3);
-      }
-    } else {
-      const int j = need + 32 * c + lane;
-      if (j < have) P.free_pages[ring_at(s.ring, j - need, np)] = page;
     }
-  }
-  if (seq < n) {
-    if (P.slots && r == S - 1) {
-      // behind the layer's new tokens (from its start where nothing was done)
-      int32_t* out = P.slots + layer * P.slot_stride;
-      for (int64_t i = (ok ? layer_sum[2][layer] : 0) + lane + 32 * blockIdx.y; i < P.slot_stride; i += 32 * gridDim.y)
-        out[i] = -1;
+    if (lane == 0) chunks_of[warp] = chunks;
+    __syncthreads();
+    // all chunks of this CTA's sequences in one line, dealt to its warps (and those of the other blockIdx.y)
+    int last = chunks_of[lane];
+  #pragma unroll
+    for (int o = 1; o < 32; o <<= 1) {
+      const int x = __shfl_up_sync(0xffffffffu, last, o);
+      if (lane >= o) last += x;
     }
+    const int all = __shfl_sync(0xffffffffu, last, 31);
+    // the page of a chunk's lane is read while the chunk before it is written
+    struct Chunk {
+      int w, c, page;   // its sequence, its number there, this lane's page (-1: none)
+    };
+    const auto read = [&](int q) {
+      Chunk k;
+      k.w = __popc(__ballot_sync(0xffffffffu, last <= q)) & 31;   // the sequence whose chunk it is
+      const int before = __shfl_sync(0xffffffffu, last, max(k.w - 1, 0));
+      k.c = q - (k.w > 0 ? before : 0);
+      k.page = -1;
+      if (q >= all) return k;
+      const Grown& s = grown[k.w];
+      const int have = (s.a + page_mask) >> shift, need = (s.b + page_mask) >> shift;
+      if (s.b > s.a) {
+        const int j = (s.a >> shift) + 32 * k.c + lane;
+        if (j < have)
+          k.page = s.row[j];
+        else if (j < need)
+          k.page = P.free_pages[ring_at(s.ring, j - have, np)];
+      } else {
+        const int j = need + 32 * k.c + lane;
+        if (j < have) k.page = s.row[j];
+      }
+      return k;
+    };
+    const int first = blockIdx.y * kPagesWarps + warp, step = kPagesWarps * gridDim.y;
+    Chunk next = read(first);
+    for (int q = first; q < all; q += step) {
+      const Chunk now = next;
+      if (q + step < all) next = read(q + step);
+      const Grown s = grown[now.w];
+      const int c = now.c, page = now.page;
+      const int have = (s.a + page_mask) >> shift, need = (s.b + page_mask) >> shift;
+      if (s.b > s.a) {
+        const int j0 = (s.a >> shift) + 32 * c, j = j0 + lane;
+        if (j >= have && j < need) s.row[j] = page;
+        const int base = page >= 0 && page < np ? page << shift : -1;
+        const bool outside = __any_sync(0xffffffffu, j < need && base < 0);   // a page outside the pool
+        if (outside && lane == 0) atomicOr(P.err, kErrCheck);
+        if (!s.out) continue;
+        // slots [begin, end) of the chunk, counted from its first page
+        const int begin = max(s.a - (j0 << shift), 0), end = min(s.b - (j0 << shift), 32 << shift), len = end - begin;
+        int32_t* const to = s.out + ((j0 << shift) + begin - s.a);
+        if (outside) {
+          // its tokens get no slot
+  #pragma unroll 1
+          for (int i = 0; i < len; i += 32) {
+            const int k = begin + i + lane;
+            const int from = __shfl_sync(0xffffffffu, base, k >> shift);
+            if (i + lane < len) to[i + lane] = from < 0 ? -1 : from + (k & page_mask);
+          }
+          continue;
+        }
+        // up to the first multiple of 16 bytes and behind the last one by slot, in between four at a time
+        const int front = min(static_cast<int>(-(reinterpret_cast<uintptr_t>(to) >> 2) & 3), len);
+        const int quads = (len - front) >> 2, rest = (len - front) & 3;
+        {
+          const int i = lane < 16 ? lane : len - 32 + lane, k = begin + i;
+          const int from = __shfl_sync(0xffffffffu, base, k >> shift);
+          if (lane < front || lane >= 32 - rest) to[i] = from + (k & page_mask);
+        }
+  #pragma unroll 2
+        for (int i = 0; i < quads; i += 32) {
+          const int q = front + 4 * (i + lane), k = begin + q, off = k & page_mask;
+          const int x = __shfl_sync(0xffffffffu, base, k >> shift) + off;
+          const int y = __shfl_sync(0xffffffffu, base, (k + 3) >> shift) + off - P.c.page;   // of those on the next page
+          if (i + lane < quads)
+            *reinterpret_cast<int4*>(to + q) =
+                make_int4(x, (off + 1 < P.c.page ? x : y) + 1, (off + 2 < P.c.page ? x : y) + 2,
+                          (off + 3 < P.c.page ? x : y) + 3);
+        }
+      } else {
+        const int j = need + 32 * c + lane;
+        if (j < have) P.free_pages[ring_at(s.ring, j - need, np)] = page;
+      }
+    }
+    if (seq < n) {
+      if (P.slots && r == S - 1) {
+        // behind the layer's new tokens (from its start where nothing was done)
+        int32_t* out = P.slots + layer * P.slot_stride;
+        for (int64_t i = (ok ? layer_sum[2][layer] : 0) + lane + 32 * blockIdx.y; i < P.slot_stride; i += 32 * gridDim.y)
+          out[i] = -1;
+      }
+    }
+    if (!P.in_place && seq < n && lane == 0 && blockIdx.y == 0) P.lens_out[seq] = ok ? P.to[seq] : P.from[seq];
+    if constexpr (!kMany) break;
+    seq += gridDim.x * kPagesWarps;
+    if (seq - warp >= n) break;
+    layer = seq < n ? seq / S : layers - 1;
+    r = seq - layer * S;
+    at = back = 0;
+    for (int l = lane; l < layer; l += 32) {
+      at += layer_sum[0][l];
+      back += layer_sum[1][l];
+    }
+    __syncthreads();   // (the group before is written)
   }
   if (!P.in_place) {
-    if (seq < n && lane == 0 && blockIdx.y == 0) P.lens_out[seq] = ok ? P.to[seq] : P.from[seq];
     if (blockIdx.x == 0 && blockIdx.y == 0 && threadIdx.x == 0) {
       P.ring_out[0] = ok ? ring_at(head, taken, np) : head;
       P.ring_out[1] = ok ? static_cast<int>(count - taken + given) : count;
@@ -611,13 +630,13 @@ cudaError_t gather_paged(const CacheGatherParams& p, cudaStream_t stream) {
 
 cudaError_t launch_cache_pages(const PagesParams& p, cudaStream_t stream) {
   const int n = p.c.num_layers * p.c.max_seqs;
-  const int64_t x = (n + kPagesWarps - 1) / kPagesWarps;
+  const int64_t groups = (n + kPagesWarps - 1) / kPagesWarps, x = std::min(groups, kPagesCtas);
   // CTAs that share 32 sequences: what their slots (or table rows) ask for, one CTA an SM in all
   const int64_t tokens = p.slots ? (p.slot_stride + p.c.max_seqs - 1) / p.c.max_seqs : int64_t(p.c.max_pages) << p.c.page_shift;
   int64_t y = (tokens >> p.c.page_shift) / 32;
   const int64_t most = x < kPagesCtas ? kPagesCtas / x : 1;
   y = y > most ? most : y;
-  return launch_after_previous(cache_pages_kernel, dim3(static_cast<unsigned>(x), static_cast<unsigned>(y < 1 ? 1 : y)),
+  return launch_after_previous(groups > x ? cache_pages_kernel<true> : cache_pages_kernel<false>, dim3(static_cast<unsigned>(x), static_cast<unsigned>(y < 1 ? 1 : y)),
                                dim3(kPagesThreads), 0, stream, p);
 }
 

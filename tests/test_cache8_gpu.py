@@ -93,6 +93,25 @@ def test_pages(K, layers, seqs, P, hi, kind, alias):
             assert a is None and b is None or np.array_equal(a, b)
 
 
+@pytest.mark.parametrize("layers,seqs,kind", [(256, 100, "decode"), (40, 1024, "any"), (200, 200, "fresh")])
+@pytest.mark.parametrize("alias", [False, True])
+def test_pages_of_more_sequences_than_one_round(K, layers, seqs, kind, alias):
+    """More (layer, sequence) pairs than the launch has warps: a CTA has several groups of them."""
+    rng = np.random.default_rng(layers + seqs)
+    f, t, table, free, ring = _pages_case(rng, layers, seqs, 16, 70, kind)
+    grow = int(np.maximum(t - f, 0).sum(axis=1).max())
+    c = _cache(K, 1, 1, 16, len(free), table.shape[2], seqs, layers)
+    for stride, short in ((grow + 9, 0), (None, 0), (grow, 1)):
+        r = ring.copy()
+        if short:
+            r[1] = max(0, int(np.maximum(-(-t // 16) - -(-f // 16), 0).sum()) - 1)
+        want = C.pages(f, t, table, free, r, 16, stride)
+        got = _run_pages(c, f, t, table, free, r, stride, alias)
+        assert c.status() == {"ok": K.KVE_OK, "pages": K.KVE_EPAGES}[want[5]] and want[5] == ("pages" if short else "ok")
+        for a, b in zip(got, want):
+            assert a is None and b is None or np.array_equal(a, b)
+
+
 def test_pages_all_or_nothing(K):
     rng = np.random.default_rng(5)
     f, t, table, free, ring = _pages_case(rng, 4, 6, 16, 300, "any")
