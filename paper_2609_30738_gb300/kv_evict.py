@@ -179,6 +179,7 @@ class Plan:
         self._h = handle
         self.workspace_bytes = ws.value
         self._kv_spans = (self._span(None),) * 2
+        self._kept = {}   # kept_lens' counts by device and type
         if k_strides is not None or v_strides is not None:
             self.set_kv_strides(k_strides, v_strides)
 
@@ -204,17 +205,25 @@ class Plan:
 
     def kept_lens(self, lens, first_seq: int = 0, stream=None):
         """lens (int32 [N_L, max_seqs]) with the sequences first_seq .. of this plan's requests at the rows that
-        the plan keeps, min(B_l, Lc_r) + W. lens is read, and the result written, on stream."""
+        the plan keeps, min(B_l, Lc_r) + W. lens is read, and the result written, on stream. The plan's first call for
+        a device copies its counts there and waits for that; later ones neither wait nor touch host memory and can
+        be captured (the plan then has to live as long as the graph)."""
         import torch
         w = self.spec["window"]
         if not 0 <= first_seq <= lens.shape[1] - len(self.seq_lens):
             raise ValueError("kept_lens: the plan's requests do not fit behind first_seq")
-        kept = torch.tensor([[min(b, n - w) + w for n in self.seq_lens] for b in self.layer_budgets], dtype=lens.dtype)
         if isinstance(stream, int):
             stream = torch.cuda.ExternalStream(stream, device=lens.device)
         with torch.cuda.stream(stream):   # (None changes nothing)
+            kept = self._kept.get((lens.device, lens.dtype))
+            if kept is None:
+                kept = torch.tensor([[min(b, n - w) + w for n in self.seq_lens] for b in self.layer_budgets],
+                                    dtype=lens.dtype).to(lens.device)
+                self._kept[lens.device, lens.dtype] = kept
             out = lens.clone()
-            out[:, first_seq:first_seq + len(self.seq_lens)] = kept.to(lens.device)
+            out[:, first_seq:first_seq + len(self.seq_lens)] = kept
+            if kept.is_cuda and not torch.cuda.is_current_stream_capturing():
+                kept.record_stream(torch.cuda.current_stream(kept.device))
         return out
 
     def set_kv_strides(self, k_strides=None, v_strides=None):
@@ -610,8 +619,8 @@ def run_step_cache8(plan: Plan, bufs: Buffers, cache: Cache8, q_win, k, v, lambd
     """The eviction step whose compact cache is the paged 8-bit one: score, select, pages for the plan's
     requests (their sequences first_seq .. must be empty), and the kept and window rows written into them.
     lens and ring are advanced in place; where the free pages do not suffice, neither moves, no page is written
-    and cache.status() returns KVE_EPAGES. Not for capture: the kept lengths come from the host (in a graph, call
-    kept_lens before and the four calls inside)."""
+    and cache.status() returns KVE_EPAGES. The plan's first step on a device waits for the copy of its kept lengths
+    (Plan.kept_lens); later ones do not wait and can be captured."""
     lens_to = plan.kept_lens(lens, first_seq, stream)
     plan.score(q_win, k, bufs.mu, bufs.sigma, bufs.ws, stream)
     plan.select(bufs.mu, bufs.sigma, k, lambda1, lambda2, bufs.indices, bufs.ws, bufs.order, bufs.margins, stream)

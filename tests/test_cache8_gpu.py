@@ -798,6 +798,65 @@ def test_eviction_that_finds_too_few_pages_writes_none(K):
     assert all(bool((t != 0).any()) for t in (c.k, c.k_scale, c.v, c.v_scale))
 
 
+def test_captured_eviction_into_the_cache(K):
+    """The step behind its first call: no wait for the device, and captured, replayed on other prompts, what it gives
+    eagerly."""
+    spec = scaled(WORKLOADS["mistral-1layer-L2048"], num_layers=2, seq_lens=[300, 133], num_kv_heads=2, num_q_heads=8,
+                  budget=40)
+    plan = K.Plan(spec, [300, 133], layer_budgets=[40, 25])
+    bufs = K.Buffers(plan)
+    c = K.Cache8(spec, max_seqs=3, num_pages=40, max_pages=6, page_tokens=16)
+    table, lens, free, ring = c.state()
+    start = [x.clone() for x in (table, lens, free, ring)]
+    data = [[synth.make_batch(spec, seed=s)[x].to(DEV) for x in ("q_win", "k", "v")] for s in (4, 5)]
+    q, k, v = (x.clone() for x in data[0])
+    lam = np.full(2, 0.5, np.float32)
+
+    def step(stream=None):
+        K.run_step_cache8(plan, bufs, c, q, k, v, lam, -lam, table, lens, free, ring, first_seq=1, stream=stream)
+
+    def fresh(i):
+        for x, y in zip((table, lens, free, ring, q, k, v), start + data[i]):
+            x.copy_(y)
+        for t in (c.k, c.v, c.k_scale, c.v_scale):
+            t.zero_()
+
+    def result():
+        assert plan.status(bufs.ws) == K.KVE_OK and c.status() == K.KVE_OK
+        return [x.clone() for x in (table, lens, free, ring, c.k, c.v, c.k_scale, c.v_scale)]
+
+    want = []
+    for i in (0, 1):
+        fresh(i)
+        step()
+        want.append(result())
+    assert want[0][1].tolist() == [[0, 40 + spec["window"], 40 + spec["window"]],
+                                   [0, 25 + spec["window"], 25 + spec["window"]]]
+    assert not torch.equal(want[0][4], want[1][4])
+    fresh(0)
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        step()
+    for i in (1, 0, 1):
+        fresh(i)
+        graph.replay()
+        for a, b in zip(result(), want[i]):
+            assert torch.equal(a, b)
+    # on a stream behind a long kernel the call returns before that has ended
+    side = torch.cuda.Stream()
+    fresh(0)
+    torch.cuda.synchronize()
+    with torch.cuda.stream(side):
+        torch.cuda._sleep(200_000_000)      # 0.1 s
+        ran = torch.cuda.Event()
+        ran.record()
+    step(side)
+    assert not ran.query()
+    side.synchronize()
+    for a, b in zip(result(), want[0]):
+        assert torch.equal(a, b)
+
+
 def test_eviction_into_the_cache_then_decode(K):
     """The whole path: score, select, pages and gather of a ragged batch into the cache, then answers that grow it,
     against the oracles of both."""
