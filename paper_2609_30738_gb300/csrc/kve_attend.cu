@@ -188,22 +188,6 @@ __device__ __forceinline__ uint32_t piece_scale(uint32_t a) {
   return static_cast<uint32_t>(min(e, 253)) << 23;
 }
 
-__device__ __forceinline__ uint32_t e4m3x2(float lo, float hi) {
-  uint16_t d;
-  asm("cvt.rn.satfinite.e4m3x2.f32 %0, %1, %2;" : "=h"(d) : "f"(hi), "f"(lo));
-  return d;
-}
-
-__device__ __forceinline__ float2 e4m3x2_values(uint32_t two) {
-  uint32_t h;
-  asm("cvt.rn.f16x2.e4m3x2 %0, %1;" : "=r"(h) : "h"(static_cast<uint16_t>(two)));
-  float2 f;
-  asm("{\n .reg .b16 a, b;\n mov.b32 {a, b}, %2;\n cvt.f32.f16 %0, a;\n cvt.f32.f16 %1, b;\n}"
-      : "=f"(f.x), "=f"(f.y)
-      : "r"(h));
-  return f;
-}
-
 // Three e4m3 pieces of two values of at most 256: x = hi + mid / 16 + lo / 256, each pair in 16 bits. The
 // values are rounded to f16 first (2^-12 of them; below 2^-14 an absolute 2^-25), whose 11 bits three
 // pieces of 4 hold, so that the rest is exact in packed f16, down to 2^-6: below that a piece is subnormal, and

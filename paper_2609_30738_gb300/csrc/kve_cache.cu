@@ -321,13 +321,6 @@ __device__ __forceinline__ uint32_t need_bits(uint32_t a) {
   return static_cast<uint32_t>(max(e, 1)) << 23;
 }
 
-// Two fp32 values as e4m3 codes (lo in the low byte), rounded to the nearest, ties to even.
-__device__ __forceinline__ uint32_t e4m3x2(float lo, float hi) {
-  uint16_t d;
-  asm("cvt.rn.satfinite.e4m3x2.f32 %0, %1, %2;" : "=h"(d) : "f"(hi), "f"(lo));
-  return d;
-}
-
 __device__ __forceinline__ uint2 row_codes(const uint4& x, float inv) {
   const auto two = [&](uint32_t p) {
     return e4m3x2(__uint_as_float(p << 16) * inv, __uint_as_float(p & 0xffff0000u) * inv);
@@ -337,13 +330,8 @@ __device__ __forceinline__ uint2 row_codes(const uint4& x, float inv) {
 
 // Two e4m3 codes times f, as e4m3 codes again.
 __device__ __forceinline__ uint32_t scaled_codes(uint32_t two, float f) {
-  uint32_t h;
-  asm("cvt.rn.f16x2.e4m3x2 %0, %1;" : "=r"(h) : "h"(static_cast<uint16_t>(two)));
-  float lo, hi;
-  asm("{\n .reg .b16 a, b;\n mov.b32 {a, b}, %2;\n cvt.f32.f16 %0, a;\n cvt.f32.f16 %1, b;\n}"
-      : "=f"(lo), "=f"(hi)
-      : "r"(h));
-  return e4m3x2(lo * f, hi * f);
+  const float2 x = e4m3x2_values(two);
+  return e4m3x2(x.x * f, x.y * f);
 }
 
 // Waits for the other groups of this thread's team.
