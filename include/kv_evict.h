@@ -443,7 +443,12 @@ kve_status kv_evict_cache_store(const kve_cache* cache, const uint16_t* k_new,
  * with the same strides). lse (or NULL)
  * [n_seq * T][Hq] fp32: ln sum_i exp(q . k_i / sqrt(d)). The table and lens of every layer
  * are passed; layer picks. What the pages hold behind a sequence, NaN codes included, has
- * no part in its rows. A query row with an infinity or a NaN gives NaN. */
+ * no part in its rows. A query row with an infinity or a NaN gives NaN.
+ * Statistics and sums are fp32. What is held in fewer bits: a query element below 2^-13 of
+ * its row's largest to 2^-21 of that; a probability times its page's value scale to 2^-12
+ * of itself, or to 2^-26 of the largest such product among the tokens of its tile
+ * (positions 128 j .. 128 j + 127) that the row sees, whichever is more; an output to
+ * len * 2^-133. */
 kve_status kv_evict_cache_attend(const kve_cache* cache, int32_t layer, int32_t n_seq,
                                  int32_t q_tokens, const uint16_t* q, const int64_t* q_strides,
                                  const int32_t* table, const int32_t* lens, uint16_t* out,

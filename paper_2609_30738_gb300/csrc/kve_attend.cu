@@ -27,12 +27,14 @@
 // Warps: the TMA producer (pages two tiles and scales one tile ahead), the MMA issuer (scores two tiles ahead of
 // the value product), two that quantise the next block's query rows, and four softmax warps, eight for 16 rows
 // (a thread is a token and 4 or 8 rows, then a column of the output). Two CTAs an SM, 96 KB of tiles each: with
-// three V stages instead of four 16 rows take 73 us instead of 57 on 131072 tokens.
+// three V stages instead of four 16 rows take 57.0 us instead of 56.0 on 131072 tokens.
 //
-// Measured (device): 64 sequences of 512 to 16384 tokens, 446 MB, 72.8 us = 90% of the HBM peak; one of 131072,
-// 269 MB, 46.4 us = 85%, 8 us of them the start (lengths, cut, first tiles) and the join of 38 parts a head; 24 of
-// 500 to 8192 with 4 drafts each (16 rows), 125 MB, 31.8 us = 58%, bound by the softmax warps' instructions;
-// 16 of 96 to 700 8.4 us; one of 96 5.1 us, a chain of latencies.
+// Measured (device; rates as shares of a copy's 6780 GB/s): 64 sequences of 512 to 16384 tokens, 446 MB, 73 us = 90%;
+// one of 131072, 269 MB, 46.4 us = 85%, 8 us of them the start (lengths, cut, first tiles) and the join of 38 parts a
+// head; 24 of 500 to 8192 with 4 drafts each (16 rows), 125 MB, 33.1 us = 55%, bound by the chain of a tile (scores,
+// maxima, meeting, exponentials, pieces, product: 2000 cycles a tile and SM, half of the issue slots empty); 16 of
+// 96 to 700 8.5 us; one of 96 5.2 us, a chain of latencies. With more than 16 rows every block of 16 reads the pages
+// again: 16 of 8192 with 8 drafts (32 rows), 271 MB, 93 us = 43%.
 //
 // The work is cut over the tokens: all (sequence, head, row block)s' tiles in one line, an equal share of it
 // for each of two CTAs an SM, whatever the lengths (the lengths are read on the GPU: a captured call serves
@@ -70,7 +72,7 @@ struct ACfg {
   static constexpr size_t kV = size_t(kKStages) * kTileBytes;
   static constexpr size_t kQ = kV + size_t(kVStages) * kTileBytes;
   // blocks whose query rows are held, by part: four where they fit, so that batches of short sequences do not wait
-  // for them (1000 of 64 tokens: 57 us against 78 with two)
+  // for them (1000 of 64 tokens: 58.9 us against 62.9 with two)
   static constexpr uint32_t kQBufs = R > 8 ? 2 : 4;
   static constexpr size_t kQBytes = kNs * kHeadDim;
   static constexpr size_t kP = kQ + kQBufs * kQBytes;
@@ -89,9 +91,9 @@ struct Block {
 // the units are dealt evenly: CTA w's raw cut is floor(units * w / ctas). A cut that would leave fewer than
 // `least` tiles of a block on one of its sides moves to that end of the block: a join costs more than those
 // tiles do. That is 4 tiles where a share is 8 units at most and 2 where it is longer and evenness counts
-// for more: 16 sequences of 96 to 700 tokens take 8.4 us with 4 against 9.3 with 2 and 10.6 with 1, 24 of 500
-// to 8192 with 4 drafts each (a share of 16) 34.2 with 4 against 31.8 with 2. With kPartTiles = 0 they take
-// 10.5 and 35.5, and 64 sequences of 512 to 16384 79.9 instead of 75. No more CTAs take part than have
+// for more: 16 sequences of 96 to 700 tokens take 8.5 us with 4 against 9.4 with 2 and 10.8 with 1, 24 of 500
+// to 8192 with 4 drafts each (a share of 16) 36.1 with 4 against 33.2 with 2 (32.6 with 1). With kPartTiles = 0 they
+// take 10.6 and 35.5, and 64 sequences of 512 to 16384 76.4 instead of 72.0. No more CTAs take part than have
 // kLeastUnits each, or a block.
 constexpr int kPartTiles = 2, kLeastUnits = 4;
 
@@ -418,9 +420,9 @@ cache_attend_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_const
       const uint32_t n = x1 - x0;
       uint32_t it = 0;
       // Pages of a call that reads more than L2 keeps anyway (8 tiles a share are 78 MB) leave it first: 64 ragged
-      // sequences 75.4 -> 72.8 us, 131072 tokens 47.9 -> 46.4, and row blocks that read a page several times are no
-      // slower (16 sequences of 8192 with 8 drafts 90.7 -> 90.0). Smaller caches may be there at the next call:
-      // 16 of 96 to 700 tokens would go from 8.36 to 8.5.
+      // sequences 74.9 -> 72.0 us, 131072 tokens 47.6 -> 46.0, and row blocks that read a page several times are no
+      // slower (16 sequences of 8192 with 8 drafts 94.6 -> 93.0). Smaller caches may be there at the next call:
+      // 16 of 96 to 700 tokens would go from 8.50 to 8.62.
       const uint64_t pol = n > 8 ? l2_policy_evict_first() : l2_policy_evict_normal();
       for (; it < n; ++it) {
         const uint32_t ks_at = it % kKStages, st = it % kVStages;

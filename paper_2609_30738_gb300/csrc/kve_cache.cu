@@ -56,7 +56,7 @@ __device__ __forceinline__ int ring_at(int head, long long i, int n) {
 //
 // A decode step (512 sequences, one new token each) is bound by latency: two reads of 8 bytes a sequence from L2
 // and the chain length -> ring entry -> table: 4.8 us. A wave of prompts is bound by the slots' write: 48 of 500 to
-// 32768 tokens in 32 layers (P = 16, 67 MB) 17.6 us, 56% of the HBM peak, of which 5.5 are the decode step's
+// 32768 tokens in 32 layers (P = 16, 67 MB) 17.6 us, 56% of a copy's 6780 GB/s, of which 5.5 are the decode step's
 // latencies; 201 MB of slots at P = 64 40 us. Slots one at a time took 19.0 and 45.8, four without the read ahead 19.5
 // and 40.6.
 //
@@ -292,7 +292,7 @@ __global__ void cache_reset_kernel(int32_t* free_pages, int32_t* ring, int n) {
 // Bound by HBM: 256 bytes read and 128 written a row. A team's loads are all in flight before its maximum is
 // known and its stores wait for that, so the overlap is between CTAs, and small ones do best: with one team
 // of 128 or 256 threads a CTA (P = 64, 128) or four smaller ones, 16 prompts at a budget of 509 in 8 layers
-// (387 MB) take 67.8 us, 84% of the HBM peak, and 24k prompt tokens (146 MB) 27.5 us, 79%; with 256 threads
+// (387 MB) take 68.5 us, 83% of a copy's 6780 GB/s, and 24k prompt tokens (146 MB) 27.6 us, 78%; with 256 threads
 // for P = 64 73.6 and 29.8, with 16 rows a group 119 and 30.5, with 4 rows 92 and 42.6.
 constexpr int kGroupRows = 8;
 template <int kPage>
@@ -489,9 +489,12 @@ __global__ void __launch_bounds__(kRowThreads<kPage>) cache_gather_kernel(const 
 // A block of P / 8 tokens gives a small call more teams, one of P tokens a large one fewer scans (P = 64, P / 8
 // against P, us): 256 sequences x 1 token 3.3 and 11.1, 1000 x 1 7.3 and 11.5, 1000 x 2 9.3 and 8.2, 1000 x 8 29.1
 // and 12.6; one prompt of 512 3.4 and 2.9, of 1024 4.9 and 3.2, of 4096 11.8 and 5.3. P = 16: 3.5 and 13.4, 7.3 and
-// 13.9, 12.7 and 8.8, 28.4 and 13.3; 3.9 and 3.1, 5.3 and 3.4, 12.5 and 5.8. So P from 1024 tokens on. Decode steps
-// of 16 and 256 sequences (8 heads) take 2.6 and 3.4 us, mostly the launch and three loads in a row (slots, scale,
-// rows); a team a token with the runs found from 16 lanes took 2.9 and 4.15.
+// 13.9, 12.7 and 8.8, 28.4 and 13.3; 3.9 and 3.1, 5.3 and 3.4, 12.5 and 5.8. So P for more than 1024 tokens: the
+// steps of up to 1024 sequences keep the small blocks, and prompts of 512 to 1024 tokens pay for it (what decides is
+// the length of the runs, which the host does not know). Decode steps of 16 and 256 sequences (8 heads) take
+// 2.6 and 3.4 us, mostly the launch and three loads in a row (slots, scale, rows); a team a token with the runs found
+// from 16 lanes took 2.9 and 4.15. Drafts, 1000 x 8 tokens at any offset, 49 MB, take 14.4 us where HBM would take
+// 7.3: 2000 teams of 8 runs, of which 1216 fit at once, are two rounds of that chain.
 constexpr int64_t kStoreBlockTokens = 1024;
 
 template <int kPage>
