@@ -33,7 +33,7 @@
 // one of 131072, 269 MB, 46.4 us = 85%, 8 us of them the start (lengths, cut, first tiles) and the join of 38 parts a
 // head; 24 of 500 to 8192 with 4 drafts each (16 rows), 125 MB, 33.1 us = 55%, bound by the chain of a tile (scores,
 // maxima, meeting, exponentials, pieces, product: 2000 cycles a tile and SM, half of the issue slots empty); 16 of
-// 96 to 700 8.5 us; one of 96 5.2 us, a chain of latencies. With more than 16 rows every block of 16 reads the pages
+// 96 to 700 8.6 us; one of 96 5.2 us, a chain of latencies. With more than 16 rows every block of 16 reads the pages
 // again: 16 of 8192 with 8 drafts (32 rows), 271 MB, 93 us = 43%.
 //
 // The work is cut over the tokens: all (sequence, head, row block)s' tiles in one line, an equal share of it
@@ -52,9 +52,10 @@ constexpr int kMostTilePages = kTileKeys / 16;
 
 constexpr int kNoNan = 255;   // of positions 0 .. 126
 
-// The least log2 of a page's value scale over its tile's largest one that the reference of a row's probabilities
-// follows: beyond it they would leave fp32.
-constexpr float kLeastRatio = -112.f;
+// The value scale that leaves the sums is a tile's largest one, or a smaller one where its pages are further apart than
+// this: a page's scale over it is then at least 2^-96 and, as long as they are not 2^192 apart, at most 2^96, so that
+// a row's probabilities, which count from the largest product with a scale that it sees, stay within fp32.
+constexpr float kMostLog = 96.f, kMostRatio = 7.92281625142643375935e28f;   // 2^96
 
 constexpr int up16(int x) { return (x + 15) / 16 * 16; }
 
@@ -91,7 +92,7 @@ struct Block {
 // the units are dealt evenly: CTA w's raw cut is floor(units * w / ctas). A cut that would leave fewer than
 // `least` tiles of a block on one of its sides moves to that end of the block: a join costs more than those
 // tiles do. That is 4 tiles where a share is 8 units at most and 2 where it is longer and evenness counts
-// for more: 16 sequences of 96 to 700 tokens take 8.5 us with 4 against 9.4 with 2 and 10.8 with 1, 24 of 500
+// for more: 16 sequences of 96 to 700 tokens take 8.6 us with 4 against 9.4 with 2 and 10.8 with 1, 24 of 500
 // to 8192 with 4 drafts each (a share of 16) 36.1 with 4 against 33.2 with 2 (32.6 with 1). With kPartTiles = 0 they
 // take 10.6 and 35.5, and 64 sequences of 512 to 16384 76.4 instead of 72.0. No more CTAs take part than have
 // kLeastUnits each, or a block.
@@ -132,14 +133,14 @@ struct ACtl {
   uint64_t m_full[kVStages];                   // the scales beside a V stage
   uint64_t s_full[2], q_full[ACfg<R, H>::kQBufs], q_empty[ACfg<R, H>::kQBufs];
   uint64_t p_full, o_full, meet[H], joined[H], drain;
-  // of a tile's pages: the keys' scale, and the values' as 256 times a share of the tile's largest one, and that share's
-  // log2
+  // of a tile's pages: the keys' scale, and the values' as 256 times a share of the one that leaves the sums, and that
+  // share's log2
   float ks[kVStages][kMostTilePages], vs[kVStages][kMostTilePages], lvs[kVStages][kMostTilePages];
-  float vtop[kVStages];                        // that largest one / 256
+  float vtop[kVStages];                        // the one that leaves / 256
   uint32_t pages[kVStages];                    // bit j: page j of the tile holds tokens
   static constexpr uint32_t kQBufs = ACfg<R, H>::kQBufs;
   alignas(16) float red[2][4][R];              // row maxima of the warps, by tile parity
-  // of a tile's rows: the maximum (logit and log2 of the value scale over the tile's largest), exp(old maximum - new),
+  // of a tile's rows: the maximum (logit and log2 of the value scale over the one that leaves), exp(old maximum - new),
   // exp(tile's maximum - new) in units of the row's sum, and by the tile's parity that times vtop
   // (each warp of the rows writes the same)
   alignas(16) float top[R], kept[R], share[R], back[2][R];
@@ -422,7 +423,7 @@ cache_attend_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_const
       // Pages of a call that reads more than L2 keeps anyway (8 tiles a share are 78 MB) leave it first: 64 ragged
       // sequences 74.9 -> 72.0 us, 131072 tokens 47.6 -> 46.0, and row blocks that read a page several times are no
       // slower (16 sequences of 8192 with 8 drafts 94.6 -> 93.0). Smaller caches may be there at the next call:
-      // 16 of 96 to 700 tokens would go from 8.50 to 8.62.
+      // 16 of 96 to 700 tokens would be 0.1 slower.
       const uint64_t pol = n > 8 ? l2_policy_evict_first() : l2_policy_evict_normal();
       for (; it < n; ++it) {
         const uint32_t ks_at = it % kKStages, st = it % kVStages;
@@ -447,13 +448,14 @@ cache_attend_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_const
           tma_load_2d_hint(smem + ks_at * kTileBytes + lane * page_bytes, &tm_k, 0, row, &ctl.k_full[ks_at], pol);
           tma_load_2d_hint(smem + C::kV + st * kTileBytes + lane * page_bytes, &tm_v, 0, row, &ctl.v_full[st], pol);
         }
-        // the largest scale of the tile's values comes out of the sums; a token keeps the rest (at most 1)
-        const float top = warp_max(sc.y);
+        // one scale of the tile's values comes out of the sums; a token keeps the rest
+        const float most = warp_max(sc.y), least = -warp_max(ok ? -sc.y : -INFINITY);
+        const float top = fmaxf(fminf(most, least * kMostRatio), most * (1.f / kMostRatio));
         if (lane < kMostTilePages) {
           const float share = top > 0.f ? sc.y * rcp(top) : sc.y;
           ctl.ks[st][lane] = sc.x;
           ctl.vs[st][lane] = share * 256.f;
-          ctl.lvs[st][lane] = fmaxf(lg2(share), kLeastRatio);
+          ctl.lvs[st][lane] = fmaxf(lg2(share), -kMostLog);
         }
         if (lane == 0) ctl.vtop[st] = top * (1.f / 256.f);
         __syncwarp();

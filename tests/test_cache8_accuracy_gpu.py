@@ -114,6 +114,22 @@ def test_a_large_value_page_that_earlier_queries_do_not_see(K, P, G, t, up):
     _check(K, q, k, ks, v, vs, table, lens, G)
 
 
+@pytest.mark.parametrize("P,G,t", [(16, 1, 4), (32, 2, 4), (64, 4, 4)])
+@pytest.mark.parametrize("low,high", [(-10, 119), (-30, 119), (-70, 119), (-126, 40), (-60, 0)])
+def test_values_at_both_ends_of_the_range_in_a_tile(K, P, G, t, low, high):
+    """Pages of scale 2^low that every query sees, and one of 2^high that only the newest does."""
+    rng = np.random.default_rng(P - low)
+    lens = [2 * P + 1, 128 + P + 1, 1025]
+    table, pages = T.table_for(rng, lens, P)
+    k, ks = T.pool(rng, pages, 1, P)
+    v, vs = T.pool(rng, pages, 1, P)
+    vs[:] = 2.0 ** low
+    for r, n in enumerate(lens):
+        vs[table[r, n // P], 0] = 2.0 ** high
+    q = T.rows(rng, (3, t, G, 128))
+    _check(K, q, k, ks, v, vs, table, lens, G)
+
+
 @pytest.mark.parametrize("P,G,t", [(16, 4, 1), (32, 4, 2), (64, 4, 4), (16, 1, 1)])
 @pytest.mark.parametrize("up,down", [(20, 10), (40, 40), (40, 60), (60, 30), (100, 110), (2, 30)])
 def test_a_large_value_page_with_small_probabilities(K, P, G, t, up, down):
