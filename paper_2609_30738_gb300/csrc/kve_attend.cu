@@ -218,9 +218,9 @@ __device__ __forceinline__ uint16_t to_bf16(float x) {
   return d;
 }
 
-// Probabilities are summed as 2^-len_bits(len) of themselves: then neither a row's sum passes 1 nor its unnormalised
-// output the largest value (values of 2e38 would, taken 100 times). In return an output keeps an absolute 2^-133 len,
-// the last bit of the factor of O^T.
+// Probabilities are summed as 2^-len_bits(len) of themselves: then a row's unnormalised output passes the largest value
+// as little as its sum passes 1 (values of 2e38 would leave fp32 from two of them on). In return an output keeps an
+// absolute 2^-133 len, the last bit of the factor of O^T.
 __device__ __forceinline__ float len_bits(int len) {
   return static_cast<float>(32 - __clz(len - 1));   // (1: 0)
 }
