@@ -455,6 +455,92 @@ kve_status kv_evict_cache_attend(const kve_cache* cache, int32_t layer, int32_t 
                                  const int64_t* out_strides, float* lse, void* ws,
                                  void* stream);
 
+/* ------------------------------------------------------------------------------------
+ * Rotary positions: the rotation that the queries and keys of this library have behind them ("after
+ * RoPE"), and that new ones still need. Behind an eviction a token's position is no longer its
+ * place in the cache, so positions are an input of every call.
+ *
+ *  * Pair j = 0 .. n/2 - 1 of the first n = rotary_dim elements of a row, (x_j, x_{j + n/2}), or
+ *    (x_2j, x_{2j+1}) where interleaved, becomes
+ *      A (a cos t - b sin t),  A (b cos t + a sin t),  t = position * frequencies[j];
+ *    the elements behind n stay as they are. Angles are exact to 2^-31 of a turn at every int32
+ *    position (negative ones too), cos and sin to 2^-20; results are rounded once to bf16.
+ *  * The transpose, A (a cos t + b sin t), A (b cos t - a sin t), is the gradient of that, and with
+ *    A = 1 takes it out again.
+ * ---------------------------------------------------------------------------------- */
+#define KVE_ROTARY_NONE 0     /* base^(-2j/n)                                                    */
+#define KVE_ROTARY_LINEAR 1   /* that over factor                                                */
+#define KVE_ROTARY_NTK 2      /* with base * factor^(n/(n-2)): the slowest pair factor times slower */
+#define KVE_ROTARY_PARTS 3    /* pairs of low_turns or fewer turns within original_length over factor,
+                                 those of high_turns or more as they are, linear in the turns between */
+#define KVE_ROTARY_YARN 4     /* the same, linear in j between the pairs that make high_turns (rounded
+                                 down) and low_turns (up); A = 1 + 0.1 ln factor                 */
+
+typedef struct kve_rotary kve_rotary;
+
+/* Frequencies [rotary_dim / 2] in radians a position, and A, of one of the forms above (host). base > 1;
+ * factor >= 1 (but for NONE); original_length >= 1 and 0 < low_turns < high_turns for PARTS and
+ * YARN, else not read. */
+kve_status kv_evict_rotary_frequencies(int32_t kind, int32_t rotary_dim, double base, double factor,
+                                       double original_length, double low_turns, double high_turns,
+                                       double* frequencies, double* amplitude);
+
+/* A rotation of rows of head_dim = 128 elements whose first rotary_dim (a multiple of 16, 16 .. 128)
+ * turn, by the given finite frequencies (host), A = amplitude (|A| <= 1e30). The handle owns host
+ * memory only, is immutable, and serves every device and stream; calls copy what they need of it. */
+kve_status kv_evict_rotary_create(int32_t head_dim, int32_t rotary_dim, int32_t interleaved,
+                                  const double* frequencies, double amplitude, kve_rotary** rotary_out);
+
+void kv_evict_rotary_destroy(kve_rotary* rotary);
+
+/* x, out [n_tokens][heads][d] bf16, 16-byte aligned, with element strides {token, head} (multiples of 8,
+ * not negative; NULL is dense; out's rows must not overlap): row (t, h) of out is that of x turned
+ * by positions[t] (int32, device memory). out may be x with the same strides, or shares nothing with
+ * it. transpose: 0 or 1. n_tokens * heads < 2^31; with 0 tokens nothing is done. KVE_EINVAL where
+ * out is host memory or another device's than the current one. */
+kve_status kv_evict_rotary_apply(const kve_rotary* rotary, const uint16_t* x, const int64_t* x_strides,
+                                 uint16_t* out, const int64_t* out_strides, int32_t heads,
+                                 const int32_t* positions, int64_t n_tokens, int32_t transpose,
+                                 void* stream);
+
+/* kv_evict_cache_store with the rotation on the way, in one launch: the keys are turned by
+ * positions [n_tokens] and rounded to bf16 before they are written, bit for bit as
+ * kv_evict_rotary_apply and kv_evict_cache_store would one after the other; the values are written as
+ * they are. With q and q_out (both or neither; [n_tokens][Hq][d], conditions as for
+ * kv_evict_rotary_apply) the tokens' queries are turned too, those of negative slots among them.
+ * q_out shares nothing with k_new and v_new. Works on 8-bit and 4-bit caches. */
+kve_status kv_evict_cache_append(const kve_cache* cache, const kve_rotary* rotary, const int32_t* positions,
+                                 const uint16_t* q, const int64_t* q_strides, uint16_t* q_out,
+                                 const int64_t* q_out_strides, const uint16_t* k_new,
+                                 const uint16_t* v_new, const int64_t* k_strides,
+                                 const int64_t* v_strides, const int32_t* slots, int64_t n_tokens,
+                                 void* ws, void* stream);
+
+/* ------------------------------------------------------------------------------------
+ * The paged cache in 4 bits: 68 bytes a row where the 8-bit cache has 128.
+ *
+ * A handle of kv_evict_cache4_create serves the calls of the 8-bit cache (kv_evict_cache_reset, _pages,
+ * _gather, _store, _append, _attend, _status, _destroy), with the same tables, lengths, slots and
+ * workspace, and these differences:
+ *
+ *  * Pages:  k, v [num_pages][H][P][d / 2] uint8: codes c in 0 .. 15, element 2i in the low and
+ *    2i + 1 in the high half of byte i; k_param, v_param [num_pages][H][P][2] bf16: s and z of each
+ *    row, an element being s c + z. (128-byte and 16-byte aligned.)
+ *  * A row x is written as z = min x, s = RN_bf16(fl((max x - min x) / 15)), fl in fp32, c = (x - z) / s
+ *    rounded to the nearest (ties to even); s = 0 and c = 0 where s would be below 2^-120. An element is off by
+ *    at most 0.53 of a step s. A row with an infinity or a NaN becomes s = z = NaN, c = 0, and so
+ *    NaN wherever it is seen.
+ *  * Rows share nothing: a page may be written in any order, and a slot that a call names twice gets
+ *    undefined codes (its row only).
+ *  * Attention: l = (s (q . c) + z sum q) / sqrt(d), out = sum p s c + sum p z, statistics and sums in
+ *    fp32. What is held in fewer bits: a query element below 2^-27 of its row's largest to 2^-38
+ *    of that; p s to 2^-12 of itself, or to 2^-39 of the largest p s so far, whichever is more; p z
+ *    to len * 2^-149. A query row with an infinity, a NaN or a magnitude of 2^112 or more
+ *    gives NaN.
+ * ---------------------------------------------------------------------------------- */
+kve_status kv_evict_cache4_create(const kve_cache_config* cfg, uint8_t* k, uint8_t* v, uint16_t* k_param,
+                                  uint16_t* v_param, kve_cache** cache_out, size_t* workspace_bytes);
+
 /* Synchronise the stream, read the error word of ws and clear it: KVE_OK, KVE_EPAGES (too
  * few free pages), KVE_ETIMEOUT (a bounded wait ran out) or KVE_ECUDA (a length, page, slot
  * or ring entry out of range, or a CUDA call failed). */

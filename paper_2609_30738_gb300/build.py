@@ -16,7 +16,7 @@ CSRC = os.path.join(HERE, "csrc")
 BUILD = os.path.join(HERE, "_build")
 LIB = os.path.join(HERE, "libkvevict.so")
 SOURCES = ["kve_host.cu", "kve_score.cu", "kve_select.cu", "kve_select_all.cu", "kve_gather.cu", "kve_cache.cu",
-           "kve_attend.cu"]
+           "kve_attend.cu", "kve_rotary.cu", "kve_cache4.cu", "kve_attend4.cu"]
 ARCH = ["-gencode", "arch=compute_103a,code=sm_103a"]
 FLAGS = ["-O3", "-lineinfo", "-std=c++17", "-Xcompiler", "-fPIC", "--expt-relaxed-constexpr",
          "-Xptxas", "-v"]

@@ -13,6 +13,7 @@
 
 #include "kve_internal.h"
 #include "kve_ptx.cuh"
+#include "kve_rotary.cuh"
 
 namespace kve {
 namespace {
@@ -497,10 +498,57 @@ __global__ void __launch_bounds__(kRowThreads<kPage>) cache_gather_kernel(const 
 // 7.3: 2000 teams of 8 runs, of which 1216 fit at once, are two rounds of that chain.
 constexpr int64_t kStoreBlockTokens = 1024;
 
-template <int kPage>
-__global__ void __launch_bounds__(kRowThreads<kPage>, 1024 / kRowThreads<kPage>)
-cache_store_kernel(const __grid_constant__ CacheStoreParams P) {
-  wait_previous_kernel();
+// The frequencies of the pairs that a lane's 8 elements belong to: 8 of them (partners are in another lane), or 4 side by
+// side.
+struct LaneTurns {
+  uint32_t hi[8], lo[8];
+  int partner;   // the lane with the other elements of the pairs; -1: not turned
+  bool second;   // this lane has the pairs' second elements
+  __device__ __forceinline__ void set(const RotaryTable& r, int lane) {
+    const int half = r.pairs >> 3;   // lanes with first elements (where partners are lanes apart)
+    const int from = r.interleaved ? lane : lane % half;
+    second = !r.interleaved && lane >= half;
+    partner = lane >= 2 * half ? -1 : r.interleaved ? lane : second ? lane - half : lane + half;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+      const int j = min(r.interleaved ? 4 * from + i : 8 * from + i, kMaxPairs - 1);
+      hi[i] = r.hi[j];
+      lo[i] = r.lo[j];
+    }
+  }
+};
+
+// Turns the rows x[i] of tokens token0 + i (those with row0 + i in 0 .. n - 1; 16 lanes have a row), rounded to bf16 as a
+// rotation by itself would leave them.
+__device__ __forceinline__ void turn_rows(uint4 (&x)[kGroupRows], const RotateParams& R, int64_t token0, int row0, int n,
+                                          const LaneTurns& turn) {
+  const uint32_t lanes = threadIdx.x & 16 ? 0xffff0000u : 0x0000ffffu;
+#pragma unroll
+  for (int i = 0; i < kGroupRows; ++i) {
+    if (static_cast<uint32_t>(row0 + i) >= static_cast<uint32_t>(n)) continue;   // (all 16 lanes)
+    const int pos = __ldg(R.positions + token0 + i);
+    uint32_t* w = &x[i].x;
+    if (R.r.interleaved) {
+#pragma unroll
+      for (int k = 0; k < 4; ++k) {
+        const float2 y = turned(bf16_low(w[k]), bf16_high(w[k]), turn_of(turn.hi[k], turn.lo[k], R.r.amplitude, pos));
+        if (turn.partner >= 0) w[k] = bf16_pair(y.x, y.y);
+      }
+      continue;
+    }
+#pragma unroll
+    for (int k = 0; k < 4; ++k) {
+      const uint32_t other = __shfl_sync(lanes, w[k], turn.partner & 15, 16);
+      const uint32_t a = turn.second ? other : w[k], b = turn.second ? w[k] : other;
+      const float2 u = turned(bf16_low(a), bf16_low(b), turn_of(turn.hi[2 * k], turn.lo[2 * k], R.r.amplitude, pos));
+      const float2 v = turned(bf16_high(a), bf16_high(b), turn_of(turn.hi[2 * k + 1], turn.lo[2 * k + 1], R.r.amplitude, pos));
+      if (turn.partner >= 0) w[k] = turn.second ? bf16_pair(u.y, v.y) : bf16_pair(u.x, v.x);
+    }
+  }
+}
+
+template <int kPage, bool kTurn>
+__device__ __forceinline__ void store_tile(const CacheStoreParams& P, const RotateParams* R, int64_t tile) {
   constexpr int kTeam = kTeamThreads<kPage>, kGroups = kPage / kGroupRows, kTeams = kRowThreads<kPage> / kTeam;
   constexpr int kWords = kPage / 16;   // of 32 tokens: a block of at most P and the run that leaves it
   __shared__ uint32_t team_max[kTeams][kGroups];
@@ -508,7 +556,7 @@ cache_store_kernel(const __grid_constant__ CacheStoreParams P) {
   __shared__ uint16_t runs[kRowThreads<kPage> / 32][kPage];   // first token << 8 | tokens: long, from the end short
   const int team = threadIdx.x / kTeam, lane = threadIdx.x & 15, g = (threadIdx.x / 16) % kGroups;
   const int warp = threadIdx.x >> 5, lane32 = threadIdx.x & 31;
-  const int64_t item = static_cast<int64_t>(blockIdx.x) * kTeams + team;
+  const int64_t item = tile * kTeams + team;
   const int H = P.c.heads;
   const int64_t first = item / (2 * H) * P.block;
   if (first >= P.n_tokens) return;   // the whole team
@@ -520,6 +568,10 @@ cache_store_kernel(const __grid_constant__ CacheStoreParams P) {
   float* const scales = values ? P.c.v_scale : P.c.k_scale;
   const int32_t* slots = P.slots + first;
   const int64_t left = P.n_tokens - first;
+  LaneTurns turn;
+  if constexpr (kTurn) {
+    if (!values) turn.set(R->r, lane);
+  }
   // the slots of the block and of what a run can reach behind it
   int longs = 0, shorts = 0;
   {
@@ -591,6 +643,9 @@ cache_store_kernel(const __grid_constant__ CacheStoreParams P) {
       if (static_cast<uint32_t>(row0 + i) < static_cast<uint32_t>(n))
         x[i] = __ldg(reinterpret_cast<const uint4*>(from + (first + t + row0 + i) * st) + lane);
     }
+    if constexpr (kTurn) {
+      if (!values) turn_rows(x, *R, first + t + row0, row0, n, turn);
+    }
     if (whole_team) {
       write_run<kPage>(x, off, n, codes + block * (kPage * kHeadDim), scales + block, team_max[team]);
       team_sync<kPage>();   // team_max and the scale before the next run
@@ -598,15 +653,48 @@ cache_store_kernel(const __grid_constant__ CacheStoreParams P) {
       write_short_run(x, off, n, codes + block * (kPage * kHeadDim), scales + block);
     }
   }
+}
+
+template <int kPage>
+__global__ void __launch_bounds__(kRowThreads<kPage>, 1024 / kRowThreads<kPage>)
+cache_store_kernel(const __grid_constant__ CacheStoreParams P) {
+  wait_previous_kernel();
+  store_tile<kPage, false>(P, nullptr, blockIdx.x);
+  allow_next_kernel();
+}
+
+// The rotating append: the first CTAs turn the queries, the others write the pages.
+template <int kPage>
+__global__ void __launch_bounds__(kRowThreads<kPage>, 768 / kRowThreads<kPage>)
+cache_append_kernel(const __grid_constant__ CacheAppendParams P, int64_t turn_tiles) {
+  wait_previous_kernel();
+  __shared__ __align__(16) float2 turns[kTurnTokens * kMaxPairs];
+  if (blockIdx.x < turn_tiles)
+    rotate_tile<kRowThreads<kPage>>(P.turn, blockIdx.x, turns);
+  else
+    store_tile<kPage, true>(P.s, &P.turn, blockIdx.x - turn_tiles);
   allow_next_kernel();
 }
 
 template <int kPage>
-cudaError_t store_paged(const CacheStoreParams& p, cudaStream_t stream) {
+int64_t store_ctas(const CacheStoreParams& p) {
   constexpr int kTeams = kRowThreads<kPage> / kTeamThreads<kPage>;
   const int64_t items = (p.n_tokens + p.block - 1) / p.block * 2 * p.c.heads;
-  return launch_after_previous(cache_store_kernel<kPage>, dim3(static_cast<unsigned>((items + kTeams - 1) / kTeams)),
+  return (items + kTeams - 1) / kTeams;
+}
+
+template <int kPage>
+cudaError_t store_paged(const CacheStoreParams& p, cudaStream_t stream) {
+  return launch_after_previous(cache_store_kernel<kPage>, dim3(static_cast<unsigned>(store_ctas<kPage>(p))),
                                dim3(kRowThreads<kPage>), 0, stream, p);
+}
+
+template <int kPage>
+cudaError_t append_paged(const CacheAppendParams& params, cudaStream_t stream) {
+  CacheAppendParams p = params;
+  const int64_t turn_tiles = p.turn.heads > 0 ? cut_rotate<kRowThreads<kPage>>(p.turn) : 0;
+  return launch_after_previous(cache_append_kernel<kPage>, dim3(static_cast<unsigned>(turn_tiles + store_ctas<kPage>(p.s))),
+                               dim3(kRowThreads<kPage>), 0, stream, p, turn_tiles);
 }
 
 template <int kPage>
@@ -646,9 +734,24 @@ cudaError_t launch_cache_gather(const CacheGatherParams& p, cudaStream_t stream)
   }
 }
 
+static int store_block(const CacheStoreParams& p) {
+  return p.n_tokens > kStoreBlockTokens ? p.c.page : p.c.page / kGroupRows;
+}
+
+cudaError_t launch_cache_append(const CacheAppendParams& params, cudaStream_t stream) {
+  CacheAppendParams p = params;
+  p.s.block = store_block(p.s);
+  switch (p.s.c.page) {
+    case 16: return append_paged<16>(p, stream);
+    case 32: return append_paged<32>(p, stream);
+    case 64: return append_paged<64>(p, stream);
+    default: return append_paged<128>(p, stream);
+  }
+}
+
 cudaError_t launch_cache_store(const CacheStoreParams& params, cudaStream_t stream) {
   CacheStoreParams p = params;
-  p.block = p.n_tokens > kStoreBlockTokens ? p.c.page : p.c.page / kGroupRows;
+  p.block = store_block(p);
   switch (p.c.page) {
     case 16: return store_paged<16>(p, stream);
     case 32: return store_paged<32>(p, stream);
@@ -657,20 +760,6 @@ cudaError_t launch_cache_store(const CacheStoreParams& params, cudaStream_t stre
   }
 }
 
-}  // namespace kve
-
-namespace {
-
-using kve::kHeadDim;
-
-constexpr uint64_t kWaitNs = 2000000000ull;   // every device-side wait, 2 s
-
-size_t align_up(size_t x, size_t a) { return (x + a - 1) / a * a; }
-
-bool aligned(const void* p, uintptr_t a) { return (reinterpret_cast<uintptr_t>(p) % a) == 0; }
-
-// {token, head} strides of a [tokens][heads][d] operand: the given ones, or dense. False if they
-// cannot be used (16-byte accesses; below 2^37 elements).
 bool row_strides(const int64_t* given, int64_t heads, int64_t* token, int64_t* head) {
   *token = given ? given[0] : heads * kHeadDim;
   *head = given ? given[1] : kHeadDim;
@@ -679,8 +768,15 @@ bool row_strides(const int64_t* given, int64_t heads, int64_t* token, int64_t* h
   return true;
 }
 
-// The device that holds p; kHostMemory for pinned host memory, kUnknown where the runtime does not know the pointer.
-constexpr int kUnknown = -1, kHostMemory = -2;
+// Tokens outside heads, or heads outside tokens.
+bool rows_apart(int64_t tokens, int64_t token, int64_t heads, int64_t head) {
+  const auto apart = [](int64_t inner, int64_t count, int64_t outer, int64_t outer_count) {
+    return (count <= 1 || inner >= kHeadDim) &&
+           (outer_count <= 1 || outer >= (count > 0 ? (count - 1) * inner : 0) + kHeadDim);
+  };
+  return apart(head, heads, token, tokens) || apart(token, tokens, head, heads);
+}
+
 int place_of(const void* p) {
   cudaPointerAttributes at;
   if (cudaPointerGetAttributes(&at, p) != cudaSuccess) {
@@ -690,6 +786,21 @@ int place_of(const void* p) {
   return at.type == cudaMemoryTypeDevice ? at.device : at.type == cudaMemoryTypeHost ? kHostMemory : kUnknown;
 }
 
+}  // namespace kve
+
+namespace {
+
+using kve::kHeadDim;
+using kve::kHostMemory;
+using kve::place_of;
+using kve::row_strides;
+
+constexpr uint64_t kWaitNs = 2000000000ull;   // every device-side wait, 2 s
+
+size_t align_up(size_t x, size_t a) { return (x + a - 1) / a * a; }
+
+bool aligned(const void* p, uintptr_t a) { return (reinterpret_cast<uintptr_t>(p) % a) == 0; }
+
 // The call's device is the buffers' device.
 bool on_device(const kve_cache* c) {
   if (c->device < 0) return true;
@@ -697,14 +808,9 @@ bool on_device(const kve_cache* c) {
   return cudaGetDevice(&dev) == cudaSuccess && dev == c->device;
 }
 
-uint32_t* word(void* ws, size_t at) { return reinterpret_cast<uint32_t*>(static_cast<uint8_t*>(ws) + at); }
-
-}  // namespace
-
-extern "C" {
-
-kve_status kv_evict_cache_create(const kve_cache_config* cfg, uint8_t* k, uint8_t* v, float* k_scale,
-                                 float* v_scale, kve_cache** cache_out, size_t* workspace_bytes) {
+// A cache of `bits`, with the given scales (8) or numbers of the rows (4).
+kve_status create_cache(const kve_cache_config* cfg, int bits, uint8_t* k, uint8_t* v, void* k_scale, void* v_scale,
+                        kve_cache** cache_out, size_t* workspace_bytes) {
   if (!cfg || !k || !v || !k_scale || !v_scale || !cache_out) return KVE_EINVAL;
   *cache_out = nullptr;
   const kve_cache_config& c = *cfg;
@@ -739,8 +845,14 @@ kve_status kv_evict_cache_create(const kve_cache_config* cfg, uint8_t* k, uint8_
   g.max_seqs = c.max_seqs;
   g.k = k;
   g.v = v;
-  g.k_scale = k_scale;
-  g.v_scale = v_scale;
+  h->bits = bits;
+  if (bits == 8) {
+    g.k_scale = static_cast<float*>(k_scale);
+    g.v_scale = static_cast<float*>(v_scale);
+  } else {
+    g.k_param = static_cast<uint32_t*>(k_scale);
+    g.v_param = static_cast<uint32_t*>(v_scale);
+  }
   h->device = device;
   int dev = device, sms = 0;
   if ((dev < 0 && cudaGetDevice(&dev) != cudaSuccess) ||
@@ -754,14 +866,52 @@ kve_status kv_evict_cache_create(const kve_cache_config* cfg, uint8_t* k, uint8_
   w.pages_done = 64;
   w.refused = 128;
   w.arrive = 256;
+  static_assert(kve::kAttend4Ctas <= kve::kAttendCtas && kve::kAttend4PartWords <= kve::kAttendPartWords, "one size for both");
   const size_t workers = static_cast<size_t>(kve::kAttendCtas) * sms;
   w.clear_end = align_up(w.arrive + sizeof(uint32_t) * 2 * workers, 256);
   w.partial = w.clear_end;
   w.total = align_up(w.partial + workers * 2 * kve::kAttendPartWords * sizeof(float), 256);
-  h->maps = kve::encode_pages(&h->tm_k, k, g) && kve::encode_pages(&h->tm_v, v, g);
+  h->maps = bits == 8 && kve::encode_pages(&h->tm_k, k, g) && kve::encode_pages(&h->tm_v, v, g);
   if (workspace_bytes) *workspace_bytes = w.total;
   *cache_out = h;
   return KVE_OK;
+}
+
+uint32_t* word(void* ws, size_t at) { return reinterpret_cast<uint32_t*>(static_cast<uint8_t*>(ws) + at); }
+
+// The checks and parameters of a store, with or without a rotation.
+kve_status store_params(const kve_cache* cache, const uint16_t* k_new, const uint16_t* v_new, const int64_t* k_strides,
+                        const int64_t* v_strides, const int32_t* slots, int64_t n_tokens, void* ws,
+                        kve::CacheStoreParams* p) {
+  if (!cache || n_tokens < 0 || n_tokens > INT32_MAX / (2 * kve::kMaxCacheHeads) || !ws || !aligned(ws, 256))
+    return KVE_EINVAL;
+  if (n_tokens > 0 && (!k_new || !v_new || !slots)) return KVE_EINVAL;
+  if (!aligned(k_new, 16) || !aligned(v_new, 16) || !aligned(slots, 4)) return KVE_EINVAL;
+  std::memset(p, 0, sizeof(*p));
+  p->c = cache->geo;
+  if (!row_strides(k_strides, p->c.heads, &p->k_st, &p->k_sh) || !row_strides(v_strides, p->c.heads, &p->v_st, &p->v_sh))
+    return KVE_EINVAL;
+  if (!on_device(cache)) return KVE_EINVAL;
+  p->k = k_new;
+  p->v = v_new;
+  p->slots = slots;
+  p->n_tokens = n_tokens;
+  p->err = word(ws, cache->ws.err);
+  return KVE_OK;
+}
+
+}  // namespace
+
+extern "C" {
+
+kve_status kv_evict_cache_create(const kve_cache_config* cfg, uint8_t* k, uint8_t* v, float* k_scale,
+                                 float* v_scale, kve_cache** cache_out, size_t* workspace_bytes) {
+  return create_cache(cfg, 8, k, v, k_scale, v_scale, cache_out, workspace_bytes);
+}
+
+kve_status kv_evict_cache4_create(const kve_cache_config* cfg, uint8_t* k, uint8_t* v, uint16_t* k_param,
+                                  uint16_t* v_param, kve_cache** cache_out, size_t* workspace_bytes) {
+  return create_cache(cfg, 4, k, v, k_param, v_param, cache_out, workspace_bytes);
 }
 
 void kv_evict_cache_destroy(kve_cache* cache) { delete cache; }
@@ -841,29 +991,51 @@ kve_status kv_evict_cache_gather(const kve_cache* cache, const kve_plan* plan, c
   p.unit_pages = static_cast<int32_t>(pages);
   p.refused = word(ws, cache->ws.refused);
   p.err = word(ws, cache->ws.err);
-  return kve::launch_cache_gather(p, static_cast<cudaStream_t>(stream)) == cudaSuccess ? KVE_OK : KVE_ECUDA;
+  const cudaStream_t st = static_cast<cudaStream_t>(stream);
+  const cudaError_t e = cache->bits == 4 ? kve::launch_cache4_gather(p, st) : kve::launch_cache_gather(p, st);
+  return e == cudaSuccess ? KVE_OK : KVE_ECUDA;
 }
 
 kve_status kv_evict_cache_store(const kve_cache* cache, const uint16_t* k_new, const uint16_t* v_new,
                                 const int64_t* k_strides, const int64_t* v_strides, const int32_t* slots,
                                 int64_t n_tokens, void* ws, void* stream) {
-  if (!cache || n_tokens < 0 || n_tokens > INT32_MAX / (2 * kve::kMaxCacheHeads) || !ws || !aligned(ws, 256))
-    return KVE_EINVAL;
-  if (n_tokens > 0 && (!k_new || !v_new || !slots)) return KVE_EINVAL;
-  if (!aligned(k_new, 16) || !aligned(v_new, 16) || !aligned(slots, 4)) return KVE_EINVAL;
   kve::CacheStoreParams p;
-  std::memset(&p, 0, sizeof(p));
-  p.c = cache->geo;
-  if (!row_strides(k_strides, p.c.heads, &p.k_st, &p.k_sh) || !row_strides(v_strides, p.c.heads, &p.v_st, &p.v_sh))
-    return KVE_EINVAL;
-  if (!on_device(cache)) return KVE_EINVAL;
+  const kve_status bad = store_params(cache, k_new, v_new, k_strides, v_strides, slots, n_tokens, ws, &p);
+  if (bad != KVE_OK || n_tokens == 0) return bad;
+  const cudaStream_t st = static_cast<cudaStream_t>(stream);
+  const cudaError_t e = cache->bits == 4 ? kve::launch_cache4_store(p, st) : kve::launch_cache_store(p, st);
+  return e == cudaSuccess ? KVE_OK : KVE_ECUDA;
+}
+
+kve_status kv_evict_cache_append(const kve_cache* cache, const kve_rotary* rotary, const int32_t* positions,
+                                 const uint16_t* q, const int64_t* q_strides, uint16_t* q_out,
+                                 const int64_t* q_out_strides, const uint16_t* k_new, const uint16_t* v_new,
+                                 const int64_t* k_strides, const int64_t* v_strides, const int32_t* slots,
+                                 int64_t n_tokens, void* ws, void* stream) {
+  kve::CacheAppendParams p;
+  if (!rotary || !q != !q_out || (n_tokens > 0 && !positions) || !aligned(positions, 4)) return KVE_EINVAL;
+  const kve_status bad = store_params(cache, k_new, v_new, k_strides, v_strides, slots, n_tokens, ws, &p.s);
+  if (bad != KVE_OK) return bad;
+  std::memset(&p.turn, 0, sizeof(p.turn));
+  if (q) {
+    const int32_t hq = cache->geo.hq;
+    if (!aligned(q, 16) || !aligned(q_out, 16) || n_tokens >= (int64_t(1) << 31) / hq) return KVE_EINVAL;
+    if (!row_strides(q_strides, hq, &p.turn.x_st, &p.turn.x_sh) ||
+        !row_strides(q_out_strides, hq, &p.turn.o_st, &p.turn.o_sh) ||
+        !kve::rows_apart(n_tokens, p.turn.o_st, hq, p.turn.o_sh))
+      return KVE_EINVAL;
+    if (q == q_out && (p.turn.x_st != p.turn.o_st || p.turn.x_sh != p.turn.o_sh)) return KVE_EINVAL;
+    p.turn.heads = hq;
+  }
   if (n_tokens == 0) return KVE_OK;
-  p.k = k_new;
-  p.v = v_new;
-  p.slots = slots;
-  p.n_tokens = n_tokens;
-  p.err = word(ws, cache->ws.err);
-  return kve::launch_cache_store(p, static_cast<cudaStream_t>(stream)) == cudaSuccess ? KVE_OK : KVE_ECUDA;
+  p.turn.r = rotary->table;
+  p.turn.x = q;
+  p.turn.out = q_out;
+  p.turn.positions = positions;
+  p.turn.n_tokens = n_tokens;
+  const cudaStream_t st = static_cast<cudaStream_t>(stream);
+  const cudaError_t e = cache->bits == 4 ? kve::launch_cache4_append(p, st) : kve::launch_cache_append(p, st);
+  return e == cudaSuccess ? KVE_OK : KVE_ECUDA;
 }
 
 kve_status kv_evict_cache_attend(const kve_cache* cache, int32_t layer, int32_t n_seq, int32_t q_tokens,
@@ -881,16 +1053,11 @@ kve_status kv_evict_cache_attend(const kve_cache* cache, int32_t layer, int32_t 
   std::memset(&p, 0, sizeof(p));
   if (!row_strides(q_strides, c.hq, &p.q_st, &p.q_sh) || !row_strides(out_strides, c.hq, &p.o_st, &p.o_sh))
     return KVE_EINVAL;
-  // rows of out lie apart: tokens outside heads, or heads outside tokens
   const int64_t tokens = static_cast<int64_t>(n_seq) * q_tokens;
-  const auto apart = [](int64_t inner, int64_t count, int64_t outer, int64_t outer_count) {
-    return (count <= 1 || inner >= kHeadDim) &&
-           (outer_count <= 1 || outer >= (count > 0 ? (count - 1) * inner : 0) + kHeadDim);
-  };
-  if (!apart(p.o_sh, c.hq, p.o_st, tokens) && !apart(p.o_st, tokens, p.o_sh, c.hq)) return KVE_EINVAL;
+  if (!kve::rows_apart(tokens, p.o_st, c.hq, p.o_sh)) return KVE_EINVAL;
   if (!on_device(cache)) return KVE_EINVAL;
   if (n_seq == 0) return KVE_OK;
-  if (!cache->maps) return KVE_ECUDA;
+  if (cache->bits == 8 && !cache->maps) return KVE_ECUDA;
   p.c = c;
   p.wait_limit_ns = kWaitNs;
   p.n_seq = n_seq;
@@ -905,7 +1072,9 @@ kve_status kv_evict_cache_attend(const kve_cache* cache, int32_t layer, int32_t 
   p.partial = reinterpret_cast<float*>(static_cast<uint8_t*>(ws) + cache->ws.partial);
   p.arrive = word(ws, cache->ws.arrive);
   p.err = word(ws, cache->ws.err);
-  return kve::launch_cache_attend(*cache, p, static_cast<cudaStream_t>(stream)) == cudaSuccess ? KVE_OK : KVE_ECUDA;
+  const cudaStream_t st = static_cast<cudaStream_t>(stream);
+  const cudaError_t e = cache->bits == 4 ? kve::launch_cache4_attend(*cache, p, st) : kve::launch_cache_attend(*cache, p, st);
+  return e == cudaSuccess ? KVE_OK : KVE_ECUDA;
 }
 
 kve_status kv_evict_cache_status(const kve_cache* cache, void* ws, void* stream) {

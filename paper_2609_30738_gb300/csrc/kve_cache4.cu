@@ -1,0 +1,244 @@
+// Rows of the paged 4-bit cache: the kept and the window rows of an eviction, and new tokens by slot, with or without the
+// rotation of their keys (and queries) on the way.
+//
+// A row x (128 elements, finite) becomes 128 codes and two bf16 numbers:
+//   z = min x,   s = RN_bf16((max x - min x) / 15),   c = RN((x - z) / s) in 0 .. 15
+// (s = 0, c = 0 where s would be below 2^-120; a row with an infinity or a NaN is a row of NaN: s = z = NaN, c = 0). No
+// row shares anything with another, so a page can be written row by row in any order, and a token that joins a page
+// touches no older one. s is rounded to 8 bits because c is chosen with the rounded s: it costs a 2^-9 of the range at
+// the far end, a 30th of a code's half step; z is an element and so exact.
+//
+// Bound by HBM: 256 bytes read and 68 written a row. Eight lanes have a row, 16 elements (32 bytes) each; the minimum
+// and maximum are packed bf16 operations and three shuffles.
+#include "kve_rotary.cuh"
+
+namespace kve {
+namespace {
+
+constexpr int kRowThreads4 = 256;
+constexpr int kGroups4 = kRowThreads4 / 8;
+constexpr int kRowCodes = kHeadDim / 2;   // bytes
+
+__device__ __forceinline__ uint32_t min2(uint32_t a, uint32_t b) {
+  uint32_t d;
+  asm("min.NaN.bf16x2 %0, %1, %2;" : "=r"(d) : "r"(a), "r"(b));
+  return d;
+}
+__device__ __forceinline__ uint32_t max2(uint32_t a, uint32_t b) {
+  uint32_t d;
+  asm("max.NaN.bf16x2 %0, %1, %2;" : "=r"(d) : "r"(a), "r"(b));
+  return d;
+}
+
+// d / unit to the nearest, ties to the even one, for 0 <= d / unit < 16. A quotient of two floats is never nearer than 2^-24
+// of itself to the middle between two integers without being there (unit has 8 bits, so d is no multiple of unit / 2
+// within 24 bits otherwise), and q below is within 2^-45 of it, exact where it is a float; so its rounding is the quotient's.
+__device__ __forceinline__ float code_of(float d, float unit, float inverse) {
+  const float q0 = d * inverse;
+  const float q = fmaf(fmaf(-q0, unit, d), inverse, q0);
+  return q + 12582912.f;   // 1.5 * 2^23: the integer in the low bits
+}
+
+// The codes of 8 elements, the first in the lowest four bits.
+__device__ __forceinline__ uint32_t codes_of(const uint4& x, float z16, float unit, float inverse) {
+  const uint32_t* w = &x.x;
+  uint32_t out = 0;
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    const float a = code_of(fmaf(bf16_low(w[i]), 0.0625f, -z16), unit, inverse);
+    const float b = code_of(fmaf(bf16_high(w[i]), 0.0625f, -z16), unit, inverse);
+    const uint32_t ia = min(__float_as_uint(a) & 31u, 15u), ib = min(__float_as_uint(b) & 31u, 15u);
+    out |= (ia | ib << 4) << (8 * i);
+  }
+  return out;
+}
+
+// Writes a row that 8 lanes hold in the chunks ca and cb: its codes, and in lane l = 0 its s and z.
+__device__ __forceinline__ void write_row4(const uint4& a, const uint4& b, int ca, int cb, uint8_t* codes, uint32_t* param,
+                                           int l, uint32_t lanes) {
+  uint32_t lo = min2(min2(min2(a.x, a.y), min2(a.z, a.w)), min2(min2(b.x, b.y), min2(b.z, b.w)));
+  uint32_t hi = max2(max2(max2(a.x, a.y), max2(a.z, a.w)), max2(max2(b.x, b.y), max2(b.z, b.w)));
+#pragma unroll
+  for (int o = 4; o > 0; o >>= 1) {
+    lo = min2(lo, __shfl_xor_sync(lanes, lo, o));
+    hi = max2(hi, __shfl_xor_sync(lanes, hi, o));
+  }
+  lo = min2(lo, lo >> 16 | lo << 16);
+  hi = max2(hi, hi >> 16 | hi << 16);
+  const bool finite = (lo & 0x7f80u) != 0x7f80u && (hi & 0x7f80u) != 0x7f80u;
+  // in units of 16, so that no difference overflows
+  const float z = bf16_low(lo) + 0.f, z16 = z * 0.0625f, top16 = bf16_low(hi) * 0.0625f;
+  uint32_t s = bf16_pair((top16 - z16) * 1.0666666667f, z);   // 16 / 15
+  if (bf16_low(s) < 7.52316384526264e-37f) s &= 0xffff0000u;   // 2^-120
+  const float unit = bf16_low(s) * 0.0625f;
+  const bool spread = finite && unit > 0.f;
+  const float inverse = spread ? __frcp_rn(unit) : 0.f;
+  uint32_t wa = 0, wb = 0;
+  if (spread) {
+    wa = codes_of(a, z16, unit, inverse);
+    wb = codes_of(b, z16, unit, inverse);
+  }
+  if (cb == ca + 1) {
+    reinterpret_cast<uint2*>(codes)[ca >> 1] = make_uint2(wa, wb);
+  } else {
+    reinterpret_cast<uint32_t*>(codes)[ca] = wa;
+    reinterpret_cast<uint32_t*>(codes)[cb] = wb;
+  }
+  if (l == 0) *param = finite ? s : 0x7fc07fc0u;
+}
+
+__device__ __forceinline__ uint32_t row_lanes() { return 0xffu << (threadIdx.x & 24); }
+
+// New tokens by slot, [tokens][2 H] rows (keys, then values) cut like a rotation's: a tile is up to 8 tokens by some
+// heads. With kTurn the first tiles turn the queries, and keys are turned (and rounded to bf16) before they are coded.
+template <bool kTurn>
+__global__ void __launch_bounds__(kRowThreads4) cache4_store_kernel(const __grid_constant__ CacheAppendParams A, int tile_tokens,
+                                                                    int tile_heads, int64_t turn_tiles) {
+  wait_previous_kernel();
+  __shared__ __align__(16) float2 turns[kTurn ? kTurnTokens * kMaxPairs : 1];
+  const CacheStoreParams& P = A.s;
+  int64_t tile = blockIdx.x;
+  if constexpr (kTurn) {
+    if (tile < turn_tiles) {
+      rotate_tile<kRowThreads4>(A.turn, tile, turns);
+      allow_next_kernel();
+      return;
+    }
+    tile -= turn_tiles;
+  }
+  const int H = P.c.heads, all = 2 * H;
+  const int head_tiles = (all + tile_heads - 1) / tile_heads;
+  const int64_t token0 = tile / head_tiles * tile_tokens;
+  const int head0 = static_cast<int>(tile % head_tiles) * tile_heads;
+  const int tokens = static_cast<int>(P.n_tokens - token0 < tile_tokens ? P.n_tokens - token0 : tile_tokens);
+  const int l = threadIdx.x & 7, group = threadIdx.x >> 3;
+  const int tok = group % tile_tokens, step = kGroups4 / tile_tokens;
+  const int slot = tok < tokens ? __ldg(P.slots + token0 + tok) : -1;
+  if constexpr (kTurn) {
+    if (head0 < H) turns_to_shared(turns, A.turn.r, A.turn.positions, token0, tokens, false);
+  }
+  const int limit = P.c.num_pages << P.c.page_shift;   // (below 2^31)
+  if (slot >= limit && l == 0 && group / tile_tokens == 0) atomicOr(P.err, kErrCheck);
+  if (slot < 0 || slot >= limit) return;
+  const int page = slot >> P.c.page_shift, off = slot & (P.c.page - 1);
+  const int64_t row0 = (static_cast<int64_t>(page) * H << P.c.page_shift) + off;
+  const uint32_t lanes = row_lanes();
+  RowChunks kc = {2 * l, 2 * l + 1, false};
+  float2 cs[8];
+  if constexpr (kTurn) {
+    kc = row_chunks(A.turn.r, l);
+    if (kc.turns && head0 < H) lane_turns(cs, turns + tok * kMaxPairs, l);
+  }
+  const int end = min(head0 + tile_heads, all);
+  constexpr int kInFlight = 2;
+  for (int h = head0 + group / tile_tokens; h < end; h += kInFlight * step) {
+    uint4 a[kInFlight], b[kInFlight];
+#pragma unroll
+    for (int i = 0; i < kInFlight; ++i) {
+      const int hh = h + i * step;
+      if (hh < end) {
+        const uint16_t* from = hh < H ? P.k + (token0 + tok) * P.k_st + hh * P.k_sh
+                                      : P.v + (token0 + tok) * P.v_st + (hh - H) * P.v_sh;
+        const uint4* v = reinterpret_cast<const uint4*>(from);
+        a[i] = v[hh < H ? kc.a : 2 * l];
+        b[i] = v[hh < H ? kc.b : 2 * l + 1];
+      }
+    }
+#pragma unroll
+    for (int i = 0; i < kInFlight; ++i) {
+      const int hh = h + i * step;
+      if (hh >= end) break;
+      const bool key = hh < H;
+      const int64_t row = row0 + (static_cast<int64_t>(key ? hh : hh - H) << P.c.page_shift);
+      if constexpr (kTurn) {
+        if (key && kc.turns) turn_chunks(a[i], b[i], cs, A.turn.r.interleaved);
+      }
+      write_row4(a[i], b[i], key ? kc.a : 2 * l, key ? kc.b : 2 * l + 1, (key ? P.c.k : P.c.v) + row * kRowCodes,
+                 (key ? P.c.k_param : P.c.v_param) + row, l, lanes);
+    }
+  }
+  allow_next_kernel();
+}
+
+// Step 4 into the cache: 8 lanes a row, kGatherRows rows of keys and of values each, all in flight.
+constexpr int kGatherRows = 2;
+__global__ void __launch_bounds__(kRowThreads4) cache4_gather_kernel(const __grid_constant__ CacheGatherParams P, int unit_tiles) {
+  wait_previous_kernel();   // the indices come from the selection launched before
+  const uint32_t unit = blockIdx.x / static_cast<uint32_t>(unit_tiles);
+  const int tile = static_cast<int>(blockIdx.x - unit * unit_tiles);
+  const UnitInfo u = unit_info(P.g.g, unit);
+  const int W = P.g.g.window, Lc = u.L - W;
+  const int m = min(P.g.layer_budget[u.layer], Lc), n = m + W;
+  const int l = threadIdx.x & 7, group = threadIdx.x >> 3;
+  const int first = tile * (kGroups4 * kGatherRows) + group;
+  const bool refused = __ldg(P.refused) != 0;   // the table's pages may be other sequences' by now
+  const int32_t* const table = P.table + (static_cast<int64_t>(u.layer) * P.c.max_seqs + P.first_seq + u.r) * P.c.max_pages;
+  const uint32_t lanes = row_lanes();
+  int src[kGatherRows], page[kGatherRows];
+  bool outside[kGatherRows];
+#pragma unroll
+  for (int i = 0; i < kGatherRows; ++i) {
+    const int row = first + i * kGroups4;
+    src[i] = page[i] = -1;
+    outside[i] = false;
+    if (row >= n) continue;
+    page[i] = __ldg(table + (row >> P.c.page_shift));
+    src[i] = row < m ? __ldg(P.g.indices + static_cast<int64_t>(unit) * P.g.budget + row) : Lc + (row - m);
+    outside[i] = row < m && (src[i] < 0 || src[i] >= Lc);   // never read outside the unit: a row of zeros, and the status tells
+  }
+  if (refused) return;
+  uint4 k[kGatherRows][2], v[kGatherRows][2];
+#pragma unroll
+  for (int i = 0; i < kGatherRows; ++i) {
+    k[i][0] = k[i][1] = v[i][0] = v[i][1] = make_uint4(0, 0, 0, 0);
+    if (first + i * kGroups4 >= n || outside[i]) continue;
+    const uint4* ks = reinterpret_cast<const uint4*>(P.g.k + u.k_off + src[i] * P.g.g.k_st) + 2 * l;
+    const uint4* vs = reinterpret_cast<const uint4*>(P.g.v + u.v_off + src[i] * P.g.g.v_st) + 2 * l;
+    k[i][0] = __ldg(ks);
+    k[i][1] = __ldg(ks + 1);
+    v[i][0] = __ldg(vs);
+    v[i][1] = __ldg(vs + 1);
+  }
+#pragma unroll
+  for (int i = 0; i < kGatherRows; ++i) {
+    const int row = first + i * kGroups4;
+    if (row >= n) break;
+    const bool good = page[i] >= 0 && page[i] < P.c.num_pages;
+    if ((outside[i] || !good) && l == 0) atomicOr(P.err, kErrCheck);
+    if (!good) continue;
+    const int64_t at = ((static_cast<int64_t>(page[i]) * P.c.heads + u.h) << P.c.page_shift) + (row & (P.c.page - 1));
+    write_row4(k[i][0], k[i][1], 2 * l, 2 * l + 1, P.c.k + at * kRowCodes, P.c.k_param + at, l, lanes);
+    write_row4(v[i][0], v[i][1], 2 * l, 2 * l + 1, P.c.v + at * kRowCodes, P.c.v_param + at, l, lanes);
+  }
+  allow_next_kernel();
+}
+
+template <bool kTurn>
+cudaError_t store4(CacheAppendParams p, cudaStream_t stream) {
+  const int64_t turn_tiles = kTurn && p.turn.heads > 0 ? cut_rotate<kRowThreads4>(p.turn) : 0;
+  RotateParams cut;   // keys and values as 2 H heads
+  cut.n_tokens = p.s.n_tokens;
+  cut.heads = 2 * p.s.c.heads;
+  const int64_t tiles = cut_rotate<kRowThreads4>(cut);
+  return launch_after_previous(cache4_store_kernel<kTurn>, dim3(static_cast<unsigned>(turn_tiles + tiles)), dim3(kRowThreads4), 0,
+                               stream, p, cut.tile_tokens, cut.tile_heads, turn_tiles);
+}
+
+}  // namespace
+
+cudaError_t launch_cache4_store(const CacheStoreParams& s, cudaStream_t stream) {
+  CacheAppendParams p = {};
+  p.s = s;
+  return store4<false>(p, stream);
+}
+
+cudaError_t launch_cache4_append(const CacheAppendParams& p, cudaStream_t stream) { return store4<true>(p, stream); }
+
+cudaError_t launch_cache4_gather(const CacheGatherParams& p, cudaStream_t stream) {
+  const int64_t rows = static_cast<int64_t>(p.unit_pages) << p.c.page_shift;
+  const int tiles = static_cast<int>((rows + kGroups4 * kGatherRows - 1) / (kGroups4 * kGatherRows));
+  return launch_after_previous(cache4_gather_kernel, dim3(static_cast<unsigned>(p.g.g.n_units * tiles)), dim3(kRowThreads4), 0,
+                               stream, p, tiles);
+}
+
+}  // namespace kve

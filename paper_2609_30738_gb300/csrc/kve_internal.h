@@ -31,6 +31,10 @@ constexpr int kMaxCacheHeads = 1024; // cache heads
 constexpr int kAttendCtas = 2;       // attention CTAs an SM
 constexpr int kAttendRows = 16;      // most query rows of one attention row block
 constexpr int kAttendPartWords = kAttendRows * (kHeadDim + 2);   // a part: rows, their maxima and sums
+// The paged 4-bit cache
+constexpr int kAttend4Ctas = 2;      // attention CTAs an SM (the workspace is sized like the 8-bit one's)
+constexpr int kAttend4PartWords = kAttendPartWords;
+constexpr int kAttend4PartTiles = 2; // what a part costs beside its own tiles
 
 // Request table and derived counts, identical on host and device.
 struct Geometry {
@@ -230,15 +234,40 @@ struct GatherParams {
   uint16_t* v_out;
 };
 
-// Sizes of a paged 8-bit cache and its buffers, identical on host and device.
+// Rotary positions: pair j turns by f_j radians a position. hi and lo are f_j / (2 pi) without its whole turns, in units
+// of 2^-64: position times that, modulo 2^64, is the angle of any 32-bit position without a rounding.
+constexpr int kMaxPairs = kHeadDim / 2;
+struct RotaryTable {
+  uint32_t hi[kMaxPairs], lo[kMaxPairs];
+  float amplitude;
+  int32_t pairs;         // rotary_dim / 2, a multiple of 8
+  int32_t interleaved;   // pairs (2j, 2j + 1), or (j, j + pairs)
+};
+
+struct RotateParams {
+  RotaryTable r;
+  const uint16_t* x;
+  int64_t x_st, x_sh;    // element strides of tokens and heads
+  uint16_t* out;
+  int64_t o_st, o_sh;
+  const int32_t* positions;
+  int64_t n_tokens;
+  int32_t heads;
+  int32_t transpose;
+  int32_t tile_tokens, tile_heads;   // of one CTA
+};
+
+// Sizes of a paged cache (8 or 4 bits) and its buffers, identical on host and device.
 struct CacheGeometry {
   int32_t num_layers, hq, heads, group;   // heads: those whose rows the cache holds
   int32_t page, page_shift;               // P = 1 << page_shift
   int32_t num_pages, max_pages, max_seqs;
   uint8_t* k;
   uint8_t* v;
-  float* k_scale;
+  float* k_scale;        // 8 bits
   float* v_scale;
+  uint32_t* k_param;     // 4 bits: s in the low, z in the high half, a word a row
+  uint32_t* v_param;
 };
 
 // Workspace of a cache (byte offsets): a header that kv_evict_cache_reset clears, then the
@@ -291,6 +320,13 @@ struct CacheStoreParams {
   uint32_t* err;
 };
 
+// The rotating append: q's rows are turned by `turn` (its heads are 0 where there is no q), the new keys by the same table
+// and positions on their way into the pages.
+struct CacheAppendParams {
+  CacheStoreParams s;
+  RotateParams turn;
+};
+
 struct AttendParams {
   CacheGeometry c;
   int32_t n_seq, q_tokens;
@@ -314,10 +350,15 @@ struct AttendParams {
 struct kve_cache {
   kve::CacheGeometry geo;
   kve::CacheWsLayout ws;
+  int32_t bits;          // 8 or 4
   int32_t device;        // of k, or -1 where the runtime does not know the pointer
   int32_t sms;           // SMs the workspace was sized for
   bool maps;             // the TMA maps are encoded (no driver, none)
   CUtensorMap tm_k, tm_v;
+};
+
+struct kve_rotary {
+  kve::RotaryTable table;
 };
 
 struct kve_plan {
@@ -387,6 +428,19 @@ cudaError_t launch_cache_gather(const CacheGatherParams& p, cudaStream_t stream)
 cudaError_t launch_cache_store(const CacheStoreParams& p, cudaStream_t stream);
 cudaError_t launch_cache_reset(const kve_cache& c, int32_t* free_pages, int32_t* ring, cudaStream_t stream);
 cudaError_t launch_cache_attend(const kve_cache& c, const AttendParams& p, cudaStream_t stream);
+cudaError_t launch_cache_append(const CacheAppendParams& p, cudaStream_t stream);
+cudaError_t launch_cache4_gather(const CacheGatherParams& p, cudaStream_t stream);
+cudaError_t launch_cache4_store(const CacheStoreParams& p, cudaStream_t stream);
+cudaError_t launch_cache4_append(const CacheAppendParams& p, cudaStream_t stream);
+cudaError_t launch_cache4_attend(const kve_cache& c, const AttendParams& p, cudaStream_t stream);
+cudaError_t launch_rotate(const RotateParams& p, cudaStream_t stream);
+// {token, head} strides of a [tokens][heads][d] operand: the given ones, or dense; false where they cannot be used (16-byte
+// accesses; below 2^37 elements). Whether rows at such strides lie apart. The device that holds p; kHostMemory for pinned
+// host memory, kUnknown where the runtime does not know the pointer (kve_cache.cu).
+bool row_strides(const int64_t* given, int64_t heads, int64_t* token, int64_t* head);
+bool rows_apart(int64_t tokens, int64_t token, int64_t heads, int64_t head);
+constexpr int kUnknown = -1, kHostMemory = -2;
+int place_of(const void* p);
 // The TMA map of a cache's codes, [pages * H * P][d] bytes in boxes of a page's rows with the 128-byte
 // swizzle; false without a driver (kve_host.cu).
 bool encode_pages(CUtensorMap* map, const void* base, const CacheGeometry& c);

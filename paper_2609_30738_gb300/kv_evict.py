@@ -25,7 +25,9 @@ EXPORTS = ("kv_evict_plan", "kv_evict_plan_layered", "kv_evict_plan_ex", "kv_evi
            "kv_evict_select_profiles_workspace", "kv_evict_gather", "kv_evict_select_gather",
            "kv_evict_status", "kv_evict_profile", "kv_evict_budget_pyramid", "kv_evict_strerror",
            "kv_evict_cache_create", "kv_evict_cache_destroy", "kv_evict_cache_reset", "kv_evict_cache_pages",
-           "kv_evict_cache_gather", "kv_evict_cache_store", "kv_evict_cache_attend", "kv_evict_cache_status")
+           "kv_evict_cache_gather", "kv_evict_cache_store", "kv_evict_cache_attend", "kv_evict_cache_status",
+           "kv_evict_cache_append", "kv_evict_cache4_create", "kv_evict_rotary_frequencies", "kv_evict_rotary_create",
+           "kv_evict_rotary_destroy", "kv_evict_rotary_apply")
 
 
 class KvEvictError(RuntimeError):
@@ -92,6 +94,14 @@ def _lib():
         lib.kv_evict_cache_store.argtypes = [vp] * 6 + [i64, vp, vp]
         lib.kv_evict_cache_attend.argtypes = [vp, i32, i32, i32] + [vp] * 9
         lib.kv_evict_cache_status.argtypes = [vp, vp, vp]
+        lib.kv_evict_cache_append.argtypes = [vp] * 12 + [i64, vp, vp]
+        lib.kv_evict_cache4_create.argtypes = [vp] * 7
+        f64 = ctypes.c_double
+        lib.kv_evict_rotary_frequencies.argtypes = [i32, i32] + [f64] * 5 + [vp, vp]
+        lib.kv_evict_rotary_create.argtypes = [i32, i32, i32, vp, f64, vp]
+        lib.kv_evict_rotary_destroy.argtypes = [vp]
+        lib.kv_evict_rotary_destroy.restype = None
+        lib.kv_evict_rotary_apply.argtypes = [vp] * 5 + [i32, vp, i64, i32, vp]
         lib.kv_evict_strerror.argtypes = [ctypes.c_int]
         lib.kv_evict_strerror.restype = ctypes.c_char_p
         for name in ("kv_evict_plan", "kv_evict_plan_layered", "kv_evict_plan_ex", "kv_evict_plan_set_debug",
@@ -102,7 +112,8 @@ def _lib():
                      "kv_evict_select_gather", "kv_evict_status", "kv_evict_profile",
                      "kv_evict_budget_pyramid", "kv_evict_cache_create", "kv_evict_cache_reset",
                      "kv_evict_cache_pages", "kv_evict_cache_gather", "kv_evict_cache_store",
-                     "kv_evict_cache_attend", "kv_evict_cache_status"):
+                     "kv_evict_cache_attend", "kv_evict_cache_status", "kv_evict_cache_append", "kv_evict_cache4_create",
+                     "kv_evict_rotary_frequencies", "kv_evict_rotary_create", "kv_evict_rotary_apply"):
             getattr(lib, name).restype = ctypes.c_int
         _LIB = lib
     return _LIB
@@ -448,6 +459,87 @@ def _row_strides(t, heads: int, name: str):
     return _Pair(heads * shape[-1] if token is None else token, st[-2])
 
 
+def _raw_stream(device):
+    """A function that returns the address of the current stream of a CUDA device (no Stream object made: 2 us less a
+    call)."""
+    import torch
+    raw = getattr(torch._C, "_cuda_getCurrentRawStream", None)
+    if raw is not None and device.type == "cuda":
+        index = torch.cuda.current_device() if device.index is None else device.index
+        return lambda: raw(index)
+    return lambda: torch.cuda.current_stream(device).cuda_stream
+
+
+ROTARY_KINDS = {"none": 0, "linear": 1, "ntk": 2, "parts": 3, "yarn": 4}
+
+
+class Rotary:
+    """kv_evict_rotary_create: rotary positions of the first rotary_dim elements (default: all) of rows of head_dim.
+    scaling names a form of kv_evict_rotary_frequencies (none, linear, ntk, parts, yarn) with its factor, original_length
+    and turns (low_turns, high_turns; by default 1 and 4 for parts, 1 and 32 for yarn); frequencies (radians a position,
+    rotary_dim / 2 of them) take its place where given. amplitude: what cos and sin are multiplied by (None: the
+    scaling's)."""
+
+    def __init__(self, head_dim: int = 128, rotary_dim: int | None = None, base: float = 10000.0, interleaved: bool = False,
+                 scaling: str = "none", factor: float = 1.0, original_length: float = 0.0, low_turns: float = 1.0,
+                 high_turns: float | None = None, frequencies=None, amplitude: float | None = None):
+        lib = _lib()
+        self._h = None
+        self.head_dim, self.rotary_dim = int(head_dim), int(head_dim if rotary_dim is None else rotary_dim)
+        self.interleaved = bool(interleaved)
+        if frequencies is None:
+            if scaling not in ROTARY_KINDS:
+                raise ValueError(f"scaling: one of {', '.join(ROTARY_KINDS)}")
+            f = np.zeros(max(self.rotary_dim // 2, 1), dtype=np.float64)
+            a = ctypes.c_double(1.0)
+            high = high_turns if high_turns is not None else 32.0 if scaling == "yarn" else 4.0
+            _check(lib.kv_evict_rotary_frequencies(ROTARY_KINDS[scaling], self.rotary_dim, float(base), float(factor),
+                                                   float(original_length), float(low_turns), float(high), f.ctypes.data,
+                                                   ctypes.byref(a)), "kv_evict_rotary_frequencies")
+            amplitude = a.value if amplitude is None else amplitude
+        else:
+            f = np.array(frequencies, dtype=np.float64)
+            if f.shape != (self.rotary_dim // 2,):
+                raise ValueError("frequencies: expected rotary_dim / 2 of them")
+        self.frequencies, self.amplitude = f, 1.0 if amplitude is None else float(amplitude)
+        handle = ctypes.c_void_p()
+        _check(lib.kv_evict_rotary_create(self.head_dim, self.rotary_dim, int(self.interleaved), f.ctypes.data,
+                                          self.amplitude, ctypes.byref(handle)), "kv_evict_rotary_create")
+        self._h, self._lib, self._streams = handle, lib, {}
+
+    def __del__(self):
+        h = getattr(self, "_h", None)
+        if h is not None and h.value and _LIB is not None:
+            _LIB.kv_evict_rotary_destroy(h)
+            self._h = None
+
+    def rotate(self, x, positions, out=None, transpose: bool = False, stream=None):
+        """kv_evict_rotary_apply: x bf16 [tokens, heads, d] (or [..., heads, d] whose tokens are one run), positions int32
+        [tokens]; out, of x's shape, is returned (None: x itself, in place). A [heads, tokens, d] tensor goes in as
+        x.transpose(0, 1). transpose: the gradient's rotation."""
+        out = x if out is None else out
+        shape = x.shape
+        if len(shape) < 3 or shape[-1] != self.head_dim or out.shape != shape:
+            raise ValueError(f"rotate: x and out are [tokens, heads, {self.head_dim}]")
+        heads, device = shape[-2], x.get_device()
+        tokens = x.numel() // (heads * self.head_dim) if heads else 0
+        if str(positions.dtype) != "torch.int32" or positions.numel() != tokens or not positions.is_contiguous():
+            raise ValueError("rotate: positions are one contiguous int32 value a token")
+        if device < 0 or out.get_device() != device or positions.get_device() != device:
+            raise ValueError("rotate: x, out and positions are on one CUDA device")
+        if stream is None:
+            current = self._streams.get(device)
+            if current is None:
+                current = self._streams[device] = _raw_stream(x.device)
+            stream = current()
+        else:
+            stream = _stream_ptr(stream)
+        _check(self._lib.kv_evict_rotary_apply(
+            self._h, x.data_ptr(), _row_strides(x, heads, "x"), out.data_ptr(), _row_strides(out, heads, "out"), heads,
+            positions.data_ptr(), tokens, 1 if transpose else 0, stream), "kv_evict_rotary_apply")
+        return out
+
+
 class Cache8:
     """kv_evict_cache_create: the paged 8-bit cache of a configuration (num_layers, num_q_heads,
     num_kv_heads, head_dim of spec; per_query_head: the query heads are the cache's heads). Its pages
@@ -455,25 +547,33 @@ class Cache8:
     tensors, or allocated here, with the workspace ws. Tables, lengths, the free ring and slots are the
     caller's int32 tensors (state() makes them)."""
 
+    _beside = "their scales"
+
     def __init__(self, spec: dict, max_seqs: int, num_pages: int, max_pages: int, page_tokens: int = 64,
                  device="cuda", per_query_head: bool = False, k=None, v=None, k_scale=None, v_scale=None):
         import torch
-        self.heads = spec["num_q_heads"] if per_query_head else spec["num_kv_heads"]
-        self.num_layers, self.num_q_heads, self.head_dim = spec["num_layers"], spec["num_q_heads"], spec["head_dim"]
-        self.max_seqs, self.num_pages, self.max_pages, self.page_tokens = max_seqs, num_pages, max_pages, page_tokens
-        shape = (num_pages, self.heads, page_tokens, self.head_dim)
-        self._h = None
+        heads = spec["num_q_heads"] if per_query_head else spec["num_kv_heads"]
         device = self._one_device([t for t in (k, v, k_scale, v_scale) if t is not None], device)
+        shape = (num_pages, heads, page_tokens, spec["head_dim"])
         self.k, self.v = (self._buffer(t, shape, torch.uint8, device) for t in (k, v))
         self.k_scale, self.v_scale = (self._buffer(t, shape[:2], torch.float32, device) for t in (k_scale, v_scale))
+        self._create("kv_evict_cache_create", spec, heads, max_seqs, num_pages, max_pages, page_tokens, self.k_scale,
+                     self.v_scale)
+
+    def _create(self, call, spec, heads, max_seqs, num_pages, max_pages, page_tokens, k_beside, v_beside):
+        """The handle of the cache over its pages and what stands beside them, and the workspace."""
+        import torch
+        self._h = None
+        self.heads = heads
+        self.num_layers, self.num_q_heads, self.head_dim = spec["num_layers"], spec["num_q_heads"], spec["head_dim"]
+        self.max_seqs, self.num_pages, self.max_pages, self.page_tokens = max_seqs, num_pages, max_pages, page_tokens
         if self.k.device.type != "cuda":
-            raise ValueError("Cache8: the pages are device memory")
+            raise ValueError(f"{type(self).__name__}: the pages are device memory")
         cfg = CacheConfig(self.num_layers, self.num_q_heads, self.heads, self.head_dim, page_tokens, num_pages,
                           max_pages, max_seqs)
         handle, size = ctypes.c_void_p(), ctypes.c_size_t()
-        _check(_lib().kv_evict_cache_create(ctypes.byref(cfg), _ptr(self.k), _ptr(self.v), _ptr(self.k_scale),
-                                            _ptr(self.v_scale), ctypes.byref(handle), ctypes.byref(size)),
-               "kv_evict_cache_create")
+        _check(getattr(_lib(), call)(ctypes.byref(cfg), _ptr(self.k), _ptr(self.v), _ptr(k_beside), _ptr(v_beside),
+                                     ctypes.byref(handle), ctypes.byref(size)), call)
         self._h, self._lib = handle, _lib()
         self.ws = torch.empty(size.value, dtype=torch.uint8, device=self.k.device)
         self._ws = self.ws.data_ptr()
@@ -481,12 +581,7 @@ class Cache8:
         self._i32, self._f32 = torch.int32, torch.float32
         dev = self.k.device
         self._device = self.k.get_device()
-        raw = getattr(torch._C, "_cuda_getCurrentRawStream", None)   # (no Stream object made: 2 us less a call)
-        if raw is not None and dev.type == "cuda":
-            index = torch.cuda.current_device() if dev.index is None else dev.index
-            self._current_stream = lambda: raw(index)
-        else:
-            self._current_stream = lambda: torch.cuda.current_stream(dev).cuda_stream
+        self._current_stream = _raw_stream(dev)
         self.reset()
 
     def _here(self, t) -> bool:
@@ -501,12 +596,12 @@ class Cache8:
         """The stream's address; None is the current stream of the cache's device."""
         return self._current_stream() if stream is None else _stream_ptr(stream)
 
-    @staticmethod
-    def _one_device(given, device):
-        """The device of the given pages and scales, where the others are allocated too; `device` where none is
-        given."""
+    @classmethod
+    def _one_device(cls, given, device):
+        """The device of the given pages and what stands beside them, where the others are allocated too; `device`
+        where none is given."""
         if any(t.device != given[0].device for t in given):
-            raise ValueError("Cache8: k, v and their scales are on one device")
+            raise ValueError(f"{cls.__name__}: k, v and {cls._beside} are on one device")
         return given[0].device if given else device
 
     @staticmethod
@@ -579,19 +674,49 @@ class Cache8:
                                                first_seq, table.data_ptr(), self._ws, self._stream(stream)),
                "kv_evict_cache_gather")
 
-    def store(self, k_new, v_new, slots, stream=None):
-        """kv_evict_cache_store: k_new, v_new bf16 [tokens, H, d] (slices of a projection's output too), slots
-        int32 [tokens]."""
+    def _check_rows(self, call, k_new, v_new, slots) -> int:
+        """The tokens of a store; raises where its tensors do not hold them."""
         n = slots.numel()
         rows = n * self.heads * self.head_dim
         if k_new.numel() != rows or v_new.numel() != rows or not self._is_i32(slots, n):
-            raise ValueError("store: k_new and v_new hold a row of every head for each of the int32 slots")
+            raise ValueError(f"{call}: k_new and v_new hold a row of every head for each of the int32 slots")
         if not self._here(k_new) or not self._here(v_new):
-            raise ValueError("store: k_new and v_new are on the cache's device")
+            raise ValueError(f"{call}: k_new and v_new are on the cache's device")
+        return n
+
+    def store(self, k_new, v_new, slots, stream=None):
+        """kv_evict_cache_store: k_new, v_new bf16 [tokens, H, d] (slices of a projection's output too), slots
+        int32 [tokens]."""
+        n = self._check_rows("store", k_new, v_new, slots)
         _check(self._lib.kv_evict_cache_store(
             self._h, k_new.data_ptr(), v_new.data_ptr(), _row_strides(k_new, self.heads, "k_new"),
             _row_strides(v_new, self.heads, "v_new"), slots.data_ptr(), n, self._ws, self._stream(stream)),
             "kv_evict_cache_store")
+
+    def append(self, rotary: Rotary, positions, k_new, v_new, slots, q=None, q_out=None, stream=None):
+        """kv_evict_cache_append: store with the keys turned by positions (int32 [tokens]) on the way, and with q bf16
+        [tokens, Hq, d] the queries too, into q_out (None: q itself, in place). Returns q_out."""
+        n = self._check_rows("append", k_new, v_new, slots)
+        if not self._is_i32(positions, n):
+            raise ValueError("append: positions are one int32 value a token, on the cache's device")
+        if rotary.head_dim != self.head_dim:
+            raise ValueError("append: the rotation is of another head_dim than the cache")
+        qs = outs = None
+        if q is not None:
+            q_out = q if q_out is None else q_out
+            if q.numel() != n * self.num_q_heads * self.head_dim or q_out.shape != q.shape:
+                raise ValueError("append: q and q_out hold a row of every query head for each token")
+            if not self._here(q) or not self._here(q_out):
+                raise ValueError("append: q and q_out are on the cache's device")
+            qs, outs = _row_strides(q, self.num_q_heads, "q"), _row_strides(q_out, self.num_q_heads, "q_out")
+        elif q_out is not None:
+            raise ValueError("append: q_out without q")
+        _check(self._lib.kv_evict_cache_append(
+            self._h, rotary._h, positions.data_ptr(), None if q is None else q.data_ptr(), qs,
+            None if q is None else q_out.data_ptr(), outs, k_new.data_ptr(), v_new.data_ptr(),
+            _row_strides(k_new, self.heads, "k_new"), _row_strides(v_new, self.heads, "v_new"), slots.data_ptr(), n,
+            self._ws, self._stream(stream)), "kv_evict_cache_append")
+        return q_out
 
     def attend(self, q, table, lens, layer: int, out, lse=None, stream=None):
         """kv_evict_cache_attend: q, out bf16 [n_seq, q_tokens, Hq, d], lse fp32 [n_seq, q_tokens, Hq] or
@@ -614,9 +739,28 @@ class Cache8:
         return int(self._lib.kv_evict_cache_status(self._h, self._ws, self._stream(stream)))
 
 
+class Cache4(Cache8):
+    """kv_evict_cache4_create: the paged cache in 4 bits, with the calls of Cache8. Its pages k, v [num_pages, H, P, d / 2]
+    uint8 (two codes a byte) and k_param, v_param [num_pages, H, P, 2] bf16 (s and z of each row) are the given
+    tensors, or allocated here."""
+
+    _beside = "their parameters"
+
+    def __init__(self, spec: dict, max_seqs: int, num_pages: int, max_pages: int, page_tokens: int = 64,
+                 device="cuda", per_query_head: bool = False, k=None, v=None, k_param=None, v_param=None):
+        import torch
+        heads = spec["num_q_heads"] if per_query_head else spec["num_kv_heads"]
+        device = self._one_device([t for t in (k, v, k_param, v_param) if t is not None], device)
+        shape = (num_pages, heads, page_tokens)
+        self.k, self.v = (self._buffer(t, shape + (spec["head_dim"] // 2,), torch.uint8, device) for t in (k, v))
+        self.k_param, self.v_param = (self._buffer(t, shape + (2,), torch.bfloat16, device) for t in (k_param, v_param))
+        self._create("kv_evict_cache4_create", spec, heads, max_seqs, num_pages, max_pages, page_tokens, self.k_param,
+                     self.v_param)
+
+
 def run_step_cache8(plan: Plan, bufs: Buffers, cache: Cache8, q_win, k, v, lambda1, lambda2, table, lens, free_pages,
                     ring, first_seq: int = 0, stream=None):
-    """The eviction step whose compact cache is the paged 8-bit one: score, select, pages for the plan's
+    """The eviction step whose compact cache is the paged one (a Cache8, or a Cache4): score, select, pages for the plan's
     requests (their sequences first_seq .. must be empty), and the kept and window rows written into them.
     lens and ring are advanced in place; where the free pages do not suffice, neither moves, no page is written
     and cache.status() returns KVE_EPAGES. The plan's first step on a device waits for the copy of its kept lengths
