@@ -8,12 +8,13 @@
 // Bound by the read of the cache, 136 bytes a token and head. A code becomes a matrix operand in registers, with
 // about 0.7 instructions an element and no conversion: the low four bits of an f16 are the subnormal c 2^-24 (and the
 // next four 16 c 2^-24), so a word of eight codes is four operand registers by one shift and four masks. The operands then
-// have to be in registers (mma.sync m16n8k16), where the loads put them:
-//   S [rows][tokens]   = Q K^T     A = the query rows (f16, kept in registers), B = codes of a token, 32 a lane
-//   O^T [d][rows]      = V^T W^T   A = codes of two tokens side by side, B = the weights where S left them
-// The sums over d and over tokens do not care for the order of d and of tokens, as long as both operands have the
-// same, so a lane's 16 bytes of K are eight k-steps as they lie, and a token's weight is already in the lane that
-// holds the token's V codes. What the sums see of fewer than 32 bits:
+// have to be in registers (mma.sync m16n8k16; in e4m3 that instruction is made of conversions and the f16 one here), where the
+// loads put them:
+//   S^T [tokens][rows] = K Q^T     A = codes of two tokens, 32 a lane and token, B = the query rows (f16, in registers)
+//   O^T [d][rows]      = V^T W^T   A = codes of two tokens side by side (transposing matrix loads), B = the weights,
+//                                  S^T's registers after an 8 x 8 transposition
+// so 8 rows fill the N side. The sums over d do not care for its order, as long as both operands have the same, so a lane's
+// 16 bytes of K are eight k-steps as they lie. What the sums see of fewer than 32 bits:
 //   q  bf16 times a power of two of its row, f16: exact down to 2^-31 of the row's largest (2^-27 in every second
 //      element, whose codes are 16 times larger), an absolute 2^-38 of it below;
 //   w  softmax(l)_i s_i over a reference within 2^8 of the row's largest such product so far, times 2^6, f16: 2^-12 of
@@ -48,11 +49,9 @@ template <int R>
 struct A4Cfg {
   static constexpr int kWarps = R == 8 ? 7 : 11;
   static constexpr int kThreads = 32 * (kWarps + 1);
-  static constexpr int kStages = 2;
+  static constexpr int kStages = R == 8 ? 3 : 4;
   static constexpr int kCtas = R == 8 ? kAttend4Ctas : 1;
-  static constexpr int kRowWords = kHeadDim + 4;           // a row of a warp's output in shared memory
-  static constexpr size_t kMerge = size_t(kWarps) * kStages * kStageBytes;
-  static constexpr size_t kCtl = kMerge + size_t(kWarps) * R * kRowWords * sizeof(float);
+  static constexpr size_t kCtl = size_t(kWarps) * kStages * kStageBytes;
 };
 
 // A part, tiles x .. end - 1 of block b, from token tok0 of its sequence on; steps first .. last - 1 of it are a warp's.
@@ -77,8 +76,12 @@ struct A4Ctl {
   uint64_t full[W][S], empty[W][S];
   uint32_t holes[W][S];                          // pages outside the pool: bit 0 of the first 16 tokens, bit 1 of the others
   LineCtl<W + 1> line;
-  Part part[W];                                  // (all lanes write the same)
-  float m[W][R], l[W][R];                        // of the warps' rows, at the end of a part
+  Part part[W], next[W];
+  int at[W];                                     // the stage (its bytes in the ring) with the warp's rows at a part's end
+  alignas(8) float m[W][8], l[W][8];             // of eight of the warps' rows, at the end of a part
+  bool has[W];                                   // the warp had steps in the part
+  float4 scale[W][R / 2];                        // of two rows: logits over products, sums of q in their units
+  int seen[W][R];                                // tokens that the row sees
   Block split[2];                                // parts left for the join
   int last[2];                                   // whether this CTA joins them
   int abort, never;                              // never: stays 0 (waits that a given-up call still has to make)
@@ -93,27 +96,44 @@ constexpr size_t attend4_smem() {
 }
 
 __device__ __forceinline__ void mma_f16(float (&d)[4], const uint32_t (&a)[4], uint32_t b0, uint32_t b1) {
-  asm volatile(
-      "mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
+  asm("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
       : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3])
       : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
 }
+
+// A warp's 8 x 8 matrix of 16-bit elements, transposed.
+__device__ __forceinline__ uint32_t transposed(uint32_t x) {
+  uint32_t d;
+  asm volatile("movmatrix.sync.aligned.m8n8.trans.b16 %0, %1;" : "=r"(d) : "r"(x));
+  return d;
+}
+
+// Four of them from shared memory, transposed: lane 8 m + i gives the address of row i of matrix m; register m of lane (g, t) has
+// the elements g of the rows 2 t (low) and 2 t + 1.
+__device__ __forceinline__ void load_transposed(uint32_t (&d)[4], uint32_t at) {
+  asm volatile("ldmatrix.sync.aligned.m8n8.x4.trans.shared.b16 {%0,%1,%2,%3}, [%4];"
+               : "=r"(d[0]), "=r"(d[1]), "=r"(d[2]), "=r"(d[3])
+               : "r"(at)
+               : "memory");
+}
+
+__device__ __forceinline__ float2 fmul2(float2 a, float2 b) {
+  uint64_t ra, rb, rd;
+  asm("mov.b64 %0, {%1,%2};" : "=l"(ra) : "f"(a.x), "f"(a.y));
+  asm("mov.b64 %0, {%1,%2};" : "=l"(rb) : "f"(b.x), "f"(b.y));
+  asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(rd) : "l"(ra), "l"(rb));
+  float2 d;
+  asm("mov.b64 {%0,%1}, %2;" : "=f"(d.x), "=f"(d.y) : "l"(rd));
+  return d;
+}
+
+__device__ __forceinline__ float2 both(float x) { return make_float2(x, x); }
+__device__ __forceinline__ float or_zero(float x) { return x == -INFINITY ? 0.f : x; }
 
 __device__ __forceinline__ uint32_t f16x2(float lo, float hi) {
   uint32_t d;
   asm("cvt.rn.f16x2.f32 %0, %1, %2;" : "=r"(d) : "f"(hi), "f"(lo));
   return d;
-}
-
-__device__ __forceinline__ uint4 lds128(uint32_t at) {
-  uint4 v;
-  asm volatile("ld.shared.v4.u32 {%0,%1,%2,%3}, [%4];" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "r"(at) : "memory");
-  return v;
-}
-__device__ __forceinline__ uint2 lds64(uint32_t at) {
-  uint2 v;
-  asm volatile("ld.shared.v2.u32 {%0,%1}, [%2];" : "=r"(v.x), "=r"(v.y) : "r"(at) : "memory");
-  return v;
 }
 
 __device__ __forceinline__ float low_bf16(uint32_t x) { return __uint_as_float(x << 16); }
@@ -268,25 +288,36 @@ cache_attend4_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_cons
     return P.group_inverse ? static_cast<int>(__umulhi(static_cast<uint32_t>(row), P.group_inverse)) : row;
   };
   int splits = 0;
-  const uint32_t ring = smem_u32(smem) + warp * (S * kStageBytes);
-  // K: column n of an 8-token block is token n ^ (n >> 1 & 1), so that the two tokens of a lane's column pair are
-  // neighbours of different parity: with the swizzle (a 16-byte chunk c of row r lies at c ^ (r >> 1 & 3)) neither K's reads nor
-  // V's meet on a bank
-  const int ktok = g ^ (g >> 1 & 1);
-  const uint32_t kget = ktok * kRowBytes + ((t ^ (ktok >> 1)) << 4);
-  // V: 8 bytes (g) of the tokens 2 t and 2 t + 1 of every 8, in the order of the columns
-  const int odd = t & 1;
-  const uint32_t vget = 2 * t * kRowBytes + (((g >> 1) ^ t) << 4) + ((g & 1) << 3);
-  const uint32_t vfirst = vget + odd * kRowBytes, vsecond = vget + (odd ^ 1) * kRowBytes;
-  const float4* const numbers = ctl.tokens[warp] + 2 * t;   // of token 2 t + (j ^ odd) of every 8
+  uint8_t* const ring = smem + warp * (S * kStageBytes);
+  // K: 16 bytes (t) of the tokens 8 i + g; V: row lane % 8, 16 bytes lane / 8 of eight tokens. A 16-byte chunk c of row r lies
+  // at c ^ (r >> 1 & 3): neither meets on a bank
+  const uint32_t kget = g * kRowBytes + ((t ^ (g >> 1)) << 4);
+  const uint32_t vget = (lane & 7) * kRowBytes + (((lane >> 3) ^ ((lane & 7) >> 1)) << 4);
   uint32_t used = 0;
   bool ok = true, failed = false;
+  // the raw query rows of a part: row 8 e + g of the block, elements 32 t .. 32 t + 31
+  uint4 raw[kHalves][4];
+  const auto load_rows = [&](const Block& b) {
+#pragma unroll
+    for (int e = 0; e < kHalves; ++e) {
+      const int row = b.rb * R + 8 * e + g;
+      const int qt = row_token(row), hq = b.h * P.c.group + row - qt * P.c.group;
+#pragma unroll
+      for (int i = 0; i < 4; ++i) raw[e][i] = make_uint4(0, 0, 0, 0);
+      if (row < rows) {
+        const uint16_t* from = P.q + (static_cast<int64_t>(b.r) * P.q_tokens + qt) * P.q_st + hq * P.q_sh + 32 * t;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) raw[e][i] = __ldg(reinterpret_cast<const uint4*>(from) + i);
+      }
+    }
+  };
   if (x0 < x1) {
     Part a;
     a.b = ctl.line.first;
     a.x = x0;
     a.template set<W>(x1, warp);
     ctl.part[warp] = a;
+    load_rows(a.b);
     __syncwarp();
   }
   for (int x = x0; x < x1;) {
@@ -294,23 +325,10 @@ cache_attend4_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_cons
     const Block& b = part.b;
     const float lb = len_bits(b.len);
     // ---------------------------------------------------------- the query rows
-    uint32_t q[8][4];            // k-step, operand register
-    float kq[kHalves], qb[kHalves];
-    int seen[kHalves];
+    uint32_t q[kHalves][8][2];   // k-step, operand register
 #pragma unroll
     for (int e = 0; e < kHalves; ++e) {
-      const int row = b.rb * R + 8 * e + g;
-      const int qt = row_token(row), hq = b.h * P.c.group + row - qt * P.c.group;
-      uint4 v[4];
-#pragma unroll
-      for (int i = 0; i < 4; ++i) v[i] = make_uint4(0, 0, 0, 0);
-      if (row < rows) {
-        const uint16_t* from = P.q + (static_cast<int64_t>(b.r) * P.q_tokens + qt) * P.q_st + hq * P.q_sh + 32 * t;
-#pragma unroll
-        for (int i = 0; i < 4; ++i) v[i] = __ldg(reinterpret_cast<const uint4*>(from) + i);
-      }
-      seen[e] = row < rows ? b.len - P.q_tokens + qt + 1 : 0;
-      const uint32_t* u = &v[0].x;
+      const uint32_t* u = &raw[e][0].x;
       uint32_t most = 0;
       float sum = 0.f;
 #pragma unroll
@@ -326,8 +344,13 @@ cache_attend4_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_cons
       const int ex = static_cast<int>(most >> 23);
       const int up = min(14 + 127 - ex, 126);
       const float scale = __uint_as_float(static_cast<uint32_t>(up + 127) << 23);
-      kq[e] = P.alpha * __uint_as_float(static_cast<uint32_t>(min(24 - up, 127) + 127) << 23);
-      qb[e] = ex >= 127 + 112 ? __uint_as_float(0x7fc00000u) : sum * scale * 5.9604644775390625e-8f;   // 2^-24
+      if (t == 0) {
+        float* const to = reinterpret_cast<float*>(&ctl.scale[warp][(8 * e + g) / 2]) + (g & 1);
+        to[0] = P.alpha * __uint_as_float(static_cast<uint32_t>(min(24 - up, 127) + 127) << 23);
+        to[2] = ex >= 127 + 112 ? __uint_as_float(0x7fc00000u) : sum * scale * 5.9604644775390625e-8f;   // 2^-24
+        const int row = b.rb * R + 8 * e + g;
+        ctl.seen[warp][8 * e + g] = row < rows ? b.len - P.q_tokens + row_token(row) + 1 : 0;
+      }
 #pragma unroll
       for (int w = 0; w < 4; ++w) {   // 8 elements: n and n + 4 go together
         float f[8];
@@ -338,17 +361,15 @@ cache_attend4_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_cons
         }
 #pragma unroll
         for (int h = 0; h < 2; ++h) {
-          q[2 * w + h][e] = f16x2(f[2 * h], f[2 * h + 4]);
-          q[2 * w + h][2 + e] = f16x2(f[2 * h + 1] * 0.0625f, f[2 * h + 5] * 0.0625f);
+          q[e][2 * w + h][0] = f16x2(f[2 * h], f[2 * h + 4]);
+          q[e][2 * w + h][1] = f16x2(f[2 * h + 1] * 0.0625f, f[2 * h + 5] * 0.0625f);
         }
       }
     }
-    if constexpr (kHalves == 1) {
-#pragma unroll
-      for (int k = 0; k < 8; ++k) q[k][1] = q[k][3] = 0;
-    }
+    __syncwarp();
 
     // ---------------------------------------------------------- the steps
+    // this lane's rows are 8 e + 2 t and 8 e + 2 t + 1, its tokens 8 i + g
     float o[8][kHalves][4];
 #pragma unroll
     for (int i = 0; i < 8; ++i)
@@ -356,103 +377,109 @@ cache_attend4_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_cons
       for (int e = 0; e < kHalves; ++e)
 #pragma unroll
         for (int k = 0; k < 4; ++k) o[i][e][k] = 0.f;
-    float m[kHalves], top[kHalves], l[kHalves], z[kHalves];   // the lane's maximum; the row's reference; the lane's sums of p, p z
+    float2 m[kHalves], top[kHalves], l[kHalves], z[kHalves];   // the lane's maxima; the rows' references; the lane's sums of p, p z
 #pragma unroll
     for (int e = 0; e < kHalves; ++e) {
-      m[e] = top[e] = -INFINITY;
-      l[e] = z[e] = 0.f;
+      m[e] = top[e] = both(-INFINITY);
+      l[e] = z[e] = both(0.f);
     }
-    const int last = part.last, tok0 = part.tok0, all_see = b.len - P.q_tokens + 1;
+    const int first = part.first, last = part.last, tok0 = part.tok0, all_see = b.len - P.q_tokens + 1;
+    uint32_t slot = 0;
 #pragma unroll 1
-    for (int step = part.first; step < last; ++step) {
-      const uint32_t slot = used % S;
+    for (int step = first; step < last; ++step) {
+      slot = used % S;
       if (!warp_wait(&ctl.full[warp][slot], (used / S) & 1, P.wait_limit_ns, &ctl.abort)) {
         ok = false;
         break;
       }
       ++used;
-      const uint32_t at = ring + slot * kStageBytes;
+      const uint8_t* const at = ring + slot * kStageBytes;
       {
         // a lane a token: its four numbers for every lane
         const uint32_t a = ctl.param[warp][slot][0][lane], c = ctl.param[warp][slot][1][lane];
         ctl.tokens[warp][lane] = make_float4(low_bf16(a), high_bf16(a), lg2(low_bf16(c)), high_bf16(c));
       }
-      float s[4][4];
+      float s[2][kHalves][4];
 #pragma unroll
-      for (int n = 0; n < 4; ++n) {
+      for (int k = 0; k < 2; ++k) {
 #pragma unroll
-        for (int k = 0; k < 4; ++k) s[n][k] = 0.f;
-        const uint4 v = lds128(at + n * (8 * kRowBytes) + kget);
-        const uint32_t u[4] = {v.x, v.y, v.z, v.w};
+        for (int e = 0; e < kHalves; ++e)
 #pragma unroll
-        for (int w = 0; w < 4; ++w) {
-          const uint32_t hi = u[w] >> 8;
-          mma_f16(s[n], q[2 * w], u[w] & 0x000f000fu, u[w] & 0x00f000f0u);
-          mma_f16(s[n], q[2 * w + 1], hi & 0x000f000fu, hi & 0x00f000f0u);
-        }
+          for (int r = 0; r < 4; ++r) s[k][e][r] = 0.f;
+        const uint4 va = *reinterpret_cast<const uint4*>(at + (2 * k) * (8 * kRowBytes) + kget);
+        const uint4 vb = *reinterpret_cast<const uint4*>(at + (2 * k + 1) * (8 * kRowBytes) + kget);
+#pragma unroll
+        for (int w = 0; w < 4; ++w)
+#pragma unroll
+          for (int h = 0; h < 2; ++h) {
+            const uint32_t ua = h ? (&va.x)[w] >> 8 : (&va.x)[w], ub = h ? (&vb.x)[w] >> 8 : (&vb.x)[w];
+            const uint32_t a[4] = {ua & 0x000f000fu, ub & 0x000f000fu, ua & 0x00f000f0u, ub & 0x00f000f0u};
+#pragma unroll
+            for (int e = 0; e < kHalves; ++e) mma_f16(s[k][e], a, q[e][2 * w + h][0], q[e][2 * w + h][1]);
+          }
       }
       __syncwarp();
       const int pos0 = tok0 + step * kStep;
       const uint32_t hole = ctl.holes[warp][slot];
       const bool some = hole != 0 || pos0 + kStep > all_see;   // tokens that not all rows see
-      // logits (over kq) in place of the products; beside them their sums with the log2 of V's s, or for two rows a lane
-      // that alone (registers)
-      float beside[4][2] = {};
-      const auto with_s = [&](int n, int j, int e) {
-        return kHalves == 1 ? beside[n][j] : fmaf(s[n][2 * e + j], kq[e], beside[n][j]);
-      };
+      // logits (over kq) in place of the products
+      float2 y[4][kHalves], kq[kHalves];
+      float ls[4];
 #pragma unroll
-      for (int n = 0; n < 4; ++n)
+      for (int e = 0; e < kHalves; ++e) {
+        const float4 c = ctl.scale[warp][4 * e + t];
+        kq[e] = make_float2(c.x, c.y);
 #pragma unroll
-        for (int j = 0; j < 2; ++j) {
-          const float4 f = numbers[8 * n + (j ^ odd)];
-#pragma unroll
-          for (int e = 0; e < kHalves; ++e) s[n][2 * e + j] = fmaf(f.x, s[n][2 * e + j], f.y * qb[e]);
-          beside[n][j] = kHalves == 1 ? fmaf(s[n][j], kq[0], f.z) : f.z;
+        for (int i = 0; i < 4; ++i) {
+          const float4 f = ctl.tokens[warp][8 * i + g];
+          ls[i] = f.z;
+          y[i][e] = ffma2(both(f.x), make_float2(s[i / 2][e][2 * (i & 1)], s[i / 2][e][2 * (i & 1) + 1]),
+                          fmul2(both(f.y), make_float2(c.z, c.w)));
         }
+      }
       if (some) {
 #pragma unroll
-        for (int n = 0; n < 4; ++n)
+        for (int e = 0; e < kHalves; ++e) {
+          const int s0 = ctl.seen[warp][8 * e + 2 * t], s1 = ctl.seen[warp][8 * e + 2 * t + 1];
 #pragma unroll
-          for (int j = 0; j < 2; ++j) {
-            const int pos = pos0 + 8 * n + 2 * t + (j ^ odd);
-            const bool gone = hole >> (n >> 1) & 1u;
-#pragma unroll
-            for (int e = 0; e < kHalves; ++e)
-              if (gone || pos >= seen[e]) {
-                s[n][2 * e + j] = -INFINITY;
-                if (kHalves == 1) beside[n][j] = -INFINITY;
-              }
+          for (int i = 0; i < 4; ++i) {
+            const int pos = pos0 + 8 * i + g;
+            const bool gone = hole >> (i >> 1) & 1u;
+            if (gone || pos >= s0) y[i][e].x = -INFINITY;
+            if (gone || pos >= s1) y[i][e].y = -INFINITY;
           }
+        }
       }
-      // the lane's own largest logits, and the row's references of the products within 2^kLazy of the largest so far
-      float tx[kHalves];
+      // the lane's own largest logits, and the rows' references of the products within 2^kLazy of the largest so far
+      float2 tx[kHalves];
       bool moved = false;
 #pragma unroll
       for (int e = 0; e < kHalves; ++e) {
-        float mx = -INFINITY;
-        tx[e] = -INFINITY;
+        float2 w[4];
 #pragma unroll
-        for (int n = 0; n < 4; ++n) {
-          mx = max3(mx, s[n][2 * e], s[n][2 * e + 1]);
-          tx[e] = max3(tx[e], with_s(n, 0, e), with_s(n, 1, e));
-        }
-        mx = fmaxf(mx * kq[e], m[e]);
-        const float kept = ex2(m[e] - (mx == -INFINITY ? 0.f : mx));
+        for (int i = 0; i < 4; ++i) w[i] = ffma2(y[i][e], kq[e], both(ls[i]));
+        tx[e] = make_float2(max3(fmaxf(w[0].x, w[1].x), w[2].x, w[3].x), max3(fmaxf(w[0].y, w[1].y), w[2].y, w[3].y));
+        float2 mx = make_float2(max3(fmaxf(y[0][e].x, y[1][e].x), y[2][e].x, y[3][e].x),
+                                max3(fmaxf(y[0][e].y, y[1][e].y), y[2][e].y, y[3][e].y));
+        mx = fmul2(mx, kq[e]);
+        mx = make_float2(fmaxf(mx.x, m[e].x), fmaxf(mx.y, m[e].y));
+        const float2 kept = make_float2(ex2(m[e].x - or_zero(mx.x)), ex2(m[e].y - or_zero(mx.y)));
         m[e] = mx;
-        l[e] *= kept;
-        z[e] *= kept;
-        moved |= tx[e] > top[e] + kLazy;
+        l[e] = fmul2(l[e], kept);
+        z[e] = fmul2(z[e], kept);
+        moved |= tx[e].x > top[e].x + kLazy || tx[e].y > top[e].y + kLazy;
       }
       if (__any_sync(0xffffffffu, moved)) {
 #pragma unroll
         for (int e = 0; e < kHalves; ++e) {
-          tx[e] = fmaxf(tx[e], __shfl_xor_sync(0xffffffffu, tx[e], 1));
-          tx[e] = fmaxf(fmaxf(tx[e], __shfl_xor_sync(0xffffffffu, tx[e], 2)), top[e]);
-          const float back = ex2(top[e] - (tx[e] == -INFINITY ? 0.f : tx[e]));
+#pragma unroll
+          for (int d = 4; d < 32; d <<= 1) {
+            tx[e].x = fmaxf(tx[e].x, __shfl_xor_sync(0xffffffffu, tx[e].x, d));
+            tx[e].y = fmaxf(tx[e].y, __shfl_xor_sync(0xffffffffu, tx[e].y, d));
+          }
+          tx[e] = make_float2(fmaxf(tx[e].x, top[e].x), fmaxf(tx[e].y, top[e].y));
+          const float f0 = ex2(top[e].x - or_zero(tx[e].x)), f1 = ex2(top[e].y - or_zero(tx[e].y));
           top[e] = tx[e];
-          // factors of the rows 2 t and 2 t + 1 (whose columns of O^T this lane has)
-          const float f0 = __shfl_sync(0xffffffffu, back, 8 * t), f1 = __shfl_sync(0xffffffffu, back, 8 * t + 4);
 #pragma unroll
           for (int i = 0; i < 8; ++i) {
             o[i][e][0] *= f0;
@@ -466,20 +493,23 @@ cache_attend4_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_cons
       const auto weigh = [&](auto kSome) {
 #pragma unroll
         for (int e = 0; e < kHalves; ++e) {
-          const float mr = (m[e] == -INFINITY ? 0.f : m[e]) + lb, tr = (top[e] == -INFINITY ? 0.f : top[e]) - (14.f - kLazy);
+          const float2 mr = make_float2(-(or_zero(m[e].x) + lb), -(or_zero(m[e].y) + lb));
+          const float2 tr = make_float2(14.f - kLazy - or_zero(top[e].x), 14.f - kLazy - or_zero(top[e].y));
 #pragma unroll
-          for (int n = 0; n < 4; ++n) {
-            float ww[2];
-#pragma unroll
-            for (int j = 0; j < 2; ++j) {
-              const float p = ex2(fmaf(s[n][2 * e + j], kq[e], -mr));
+          for (int i = 0; i < 4; ++i) {
+            const float vz = ctl.tokens[warp][8 * i + g].w;
+            const float2 a = ffma2(y[i][e], kq[e], mr);
+            const float2 p = make_float2(ex2(a.x), ex2(a.y));
+            const float2 c = fadd2(ffma2(y[i][e], kq[e], both(ls[i])), tr);
+            float2 ww = make_float2(ex2(c.x), ex2(c.y)), zz = both(vz);
+            if constexpr (kSome.value) {
               // (a NaN of a token that the row does not see stays out: some rows of the step may see it)
-              const bool out = kSome.value && s[n][2 * e + j] == -INFINITY;
-              l[e] += p;
-              z[e] = fmaf(p, out ? 0.f : numbers[8 * n + (j ^ odd)].w, z[e]);
-              ww[j] = out && kHalves > 1 ? 0.f : ex2(with_s(n, j, e) - tr);
+              if (y[i][e].x == -INFINITY) ww.x = zz.x = 0.f;
+              if (y[i][e].y == -INFINITY) ww.y = zz.y = 0.f;
             }
-            w[n][e] = f16x2(ww[0], ww[1]);
+            l[e] = fadd2(l[e], p);
+            z[e] = ffma2(p, zz, z[e]);
+            w[i][e] = f16x2(ww.x, ww.y);
           }
         }
       };
@@ -488,114 +518,130 @@ cache_attend4_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_cons
       else
         weigh(std::false_type{});
 #pragma unroll
-      for (int n = 0; n < 4; n += 2) {
-        const uint32_t va = at + kCodeBytes + n * (8 * kRowBytes);
-        const uint2 a0 = lds64(va + vfirst), a1 = lds64(va + vsecond);
-        const uint2 b0 = lds64(va + 8 * kRowBytes + vfirst), b1 = lds64(va + 8 * kRowBytes + vsecond);
+      for (int i = 0; i < 4; ++i)
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {   // four of a word's codes of both tokens side by side
-          const uint32_t sel = i & 1 ? 0x7632u : 0x5410u;
-          const uint32_t p0 = __byte_perm(i & 2 ? a0.y : a0.x, i & 2 ? a1.y : a1.x, sel);
-          const uint32_t p1 = __byte_perm(i & 2 ? b0.y : b0.x, i & 2 ? b1.y : b1.x, sel);
+        for (int e = 0; e < kHalves; ++e) w[i][e] = transposed(w[i][e]);
+#pragma unroll
+      for (int k = 0; k < 2; ++k) {
+        uint32_t c0[4], c1[4];   // four codes of two tokens each
+        const uint32_t va = smem_u32(at) + kCodeBytes + 2 * k * (8 * kRowBytes) + vget;
+        load_transposed(c0, va);
+        load_transposed(c1, va + 8 * kRowBytes);
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
 #pragma unroll
           for (int h = 0; h < 2; ++h) {
-            const uint32_t c0 = h ? p0 >> 8 : p0, c1 = h ? p1 >> 8 : p1;
-            const uint32_t a[4] = {c0 & 0x000f000fu, c0 & 0x00f000f0u, c1 & 0x000f000fu, c1 & 0x00f000f0u};
+            const uint32_t ua = h ? c0[i] >> 8 : c0[i], ub = h ? c1[i] >> 8 : c1[i];
+            const uint32_t a[4] = {ua & 0x000f000fu, ua & 0x00f000f0u, ub & 0x000f000fu, ub & 0x00f000f0u};
 #pragma unroll
-            for (int e = 0; e < kHalves; ++e) mma_f16(o[2 * i + h][e], a, w[n][e], w[n + 1][e]);
+            for (int e = 0; e < kHalves; ++e) mma_f16(o[2 * i + h][e], a, w[2 * k][e], w[2 * k + 1][e]);
           }
-        }
       }
       __syncwarp();   // the stage and the tokens' numbers have been read
-      if (lane == 0) mbar_arrive(&ctl.empty[warp][slot]);
+      // (the last stage of a part is where its sums are put together, then it is given back)
+      if (lane == 0 && step + 1 < last) mbar_arrive(&ctl.empty[warp][slot]);
     }
     if (!ok && lane == 0) fail();
 
-    // ---------------------------------------------------------- the end of a part: the warps' rows together
-#pragma unroll
-    for (int e = 0; e < kHalves; ++e) {
-      const float mine = m[e];
-      m[e] = fmaxf(m[e], __shfl_xor_sync(0xffffffffu, m[e], 1));
-      m[e] = fmaxf(m[e], __shfl_xor_sync(0xffffffffu, m[e], 2));
-      const float kept = ex2(mine - (m[e] == -INFINITY ? 0.f : m[e]));
-      l[e] *= kept;
-      z[e] *= kept;
-      l[e] += __shfl_xor_sync(0xffffffffu, l[e], 1);
-      z[e] += __shfl_xor_sync(0xffffffffu, z[e], 1);
-      l[e] += __shfl_xor_sync(0xffffffffu, l[e], 2);
-      z[e] += __shfl_xor_sync(0xffffffffu, z[e], 2);
-    }
-    meet_or<32 * W>(false);   // the sums of the part before are read
-    float* const merge = reinterpret_cast<float*>(smem + C::kMerge);
-    float* const mine = merge + warp * (R * C::kRowWords);
-#pragma unroll
-    for (int e = 0; e < kHalves; ++e) {
-      // quarters of sum p (s c + z), so that neither term alone passes the largest float
-      const float f = ex2((top[e] == -INFINITY ? 0.f : top[e]) - (m[e] == -INFINITY ? 0.f : m[e]) - lb);
-#pragma unroll
-      for (int j = 0; j < 2; ++j) {
-        const int from = 8 * t + 4 * j;
-        const float ff = __shfl_sync(0xffffffffu, f, from), zz = 0.25f * __shfl_sync(0xffffffffu, z[e], from);
-        float* to = mine + (8 * e + 2 * t + j) * C::kRowWords + 16 * g;
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-          float4 v;
-          // (c 2^-24 or 16 c 2^-24, weights times 2^(14 - kLazy), a quarter)
-          v.x = fmaf(o[2 * i][e][j] * 65536.f, ff, zz);
-          v.y = fmaf(o[2 * i][e][2 + j] * 4096.f, ff, zz);
-          v.z = fmaf(o[2 * i + 1][e][j] * 65536.f, ff, zz);
-          v.w = fmaf(o[2 * i + 1][e][2 + j] * 4096.f, ff, zz);
-          *reinterpret_cast<float4*>(to + 4 * i) = v;
-        }
-      }
-      if (t == 0) {
-        ctl.m[warp][8 * e + g] = m[e];
-        ctl.l[warp][8 * e + g] = l[e];
-      }
-    }
-    failed = meet_or<32 * W>(!ok);
-    if (failed) break;
-    const bool whole = x == b.first && part.end == b.first + b.tiles;
+    // ---------------------------------------------------------- the end of a part: the warps' rows together, eight by eight
+    const bool has = first < last, whole = x == b.first && part.end == b.first + b.tiles;
     float* const out = P.partial + (static_cast<int64_t>(blockIdx.x) * 2 + (x == b.first)) * kAttend4PartWords;
-    for (int row = warp; row < R; row += W) {
-      float mx = -INFINITY;
+    float* const mine = reinterpret_cast<float*>(ring + slot * kStageBytes);
+    if (lane == 0) {
+      ctl.has[warp] = has;
+      ctl.at[warp] = slot * kStageBytes;
+    }
+    const int next_x = part.end;
 #pragma unroll
-      for (int w = 0; w < W; ++w) mx = fmaxf(mx, ctl.m[w][row]);
-      const float mr = mx == -INFINITY ? 0.f : mx;
-      float4 a = make_float4(0.f, 0.f, 0.f, 0.f);
-      float sum = 0.f;
+    for (int e = 0; e < kHalves; ++e) {
+      if (has) {
+        float2 all = m[e];
 #pragma unroll
-      for (int w = 0; w < W; ++w) {
-        const float f = ex2(ctl.m[w][row] - mr);
-        const float4 v = reinterpret_cast<const float4*>(merge + (w * R + row) * C::kRowWords)[lane];
-        sum = fmaf(ctl.l[w][row], f, sum);
-        a.x = fmaf(v.x, f, a.x);
-        a.y = fmaf(v.y, f, a.y);
-        a.z = fmaf(v.z, f, a.z);
-        a.w = fmaf(v.w, f, a.w);
-      }
-      if (whole) {
-        emit_row(P, b, b.rb * R + row, rows, row_token, a, mx, sum, lb, lane);
-      } else {
-        reinterpret_cast<float4*>(out + row * kHeadDim)[lane] = a;
-        if (lane == 0) {
-          out[R * kHeadDim + row] = mx;
-          out[R * kHeadDim + R + row] = sum;
+        for (int d = 4; d < 32; d <<= 1) {
+          all.x = fmaxf(all.x, __shfl_xor_sync(0xffffffffu, all.x, d));
+          all.y = fmaxf(all.y, __shfl_xor_sync(0xffffffffu, all.y, d));
+        }
+        const float2 kept = make_float2(ex2(m[e].x - or_zero(all.x)), ex2(m[e].y - or_zero(all.y)));
+        float2 ll = fmul2(l[e], kept), zz = fmul2(z[e], kept);
+#pragma unroll
+        for (int d = 4; d < 32; d <<= 1) {
+          ll.x += __shfl_xor_sync(0xffffffffu, ll.x, d);
+          ll.y += __shfl_xor_sync(0xffffffffu, ll.y, d);
+          zz.x += __shfl_xor_sync(0xffffffffu, zz.x, d);
+          zz.y += __shfl_xor_sync(0xffffffffu, zz.y, d);
+        }
+        // quarters of sum p (s c + z), so that neither term alone passes the largest float: products of c 2^-24 or
+        // 16 c 2^-24 with weights times 2^(14 - kLazy)
+        const float f[2] = {ex2(or_zero(top[e].x) - or_zero(all.x) - lb), ex2(or_zero(top[e].y) - or_zero(all.y) - lb)};
+        const float zq[2] = {0.25f * zz.x, 0.25f * zz.y};
+#pragma unroll
+        for (int j = 0; j < 2; ++j)
+#pragma unroll
+          for (int i = 0; i < 4; ++i) {
+            float4 v;
+            v.x = fmaf(o[2 * i][e][j] * 65536.f, f[j], zq[j]);
+            v.y = fmaf(o[2 * i][e][2 + j] * 4096.f, f[j], zq[j]);
+            v.z = fmaf(o[2 * i + 1][e][j] * 65536.f, f[j], zq[j]);
+            v.w = fmaf(o[2 * i + 1][e][2 + j] * 4096.f, f[j], zq[j]);
+            // columns 32 i + 4 g of row 2 t + j; 16 bytes c of row r lie at c ^ (r & 6)
+            reinterpret_cast<float4*>(mine + (2 * t + j) * kHeadDim)[(8 * i + g) ^ (2 * t)] = v;
+          }
+        if (g == 0) {
+          *reinterpret_cast<float2*>(&ctl.m[warp][2 * t]) = all;
+          *reinterpret_cast<float2*>(&ctl.l[warp][2 * t]) = ll;
         }
       }
+      if (e + 1 == kHalves && next_x < x1) {   // the next part, and its rows on their way
+        Part a = part;
+        a.x = next_x;
+        next_block(P, blocks, kTileKeys, a.b);
+        a.template set<W>(x1, warp);
+        load_rows(a.b);
+        ctl.next[warp] = a;
+      }
+      failed = meet_or<32 * W>(!ok);
+      if (failed) break;
+      for (int row = warp; row < 8; row += W) {
+        float mx = -INFINITY;
+#pragma unroll
+        for (int w = 0; w < W; ++w)
+          if (ctl.has[w]) mx = fmaxf(mx, ctl.m[w][row]);
+        const float mr = or_zero(mx);
+        float4 a = make_float4(0.f, 0.f, 0.f, 0.f);
+        float sum = 0.f;
+#pragma unroll
+        for (int w = 0; w < W; ++w) {
+          if (!ctl.has[w]) continue;
+          const float f = ex2(ctl.m[w][row] - mr);
+          const float4 v = reinterpret_cast<const float4*>(smem + w * (S * kStageBytes) + ctl.at[w] + row * (kHeadDim * 4))[lane ^ (row & 6)];
+          sum = fmaf(ctl.l[w][row], f, sum);
+          a.x = fmaf(v.x, f, a.x);
+          a.y = fmaf(v.y, f, a.y);
+          a.z = fmaf(v.z, f, a.z);
+          a.w = fmaf(v.w, f, a.w);
+        }
+        const int r = 8 * e + row;
+        if (whole) {
+          emit_row(P, b, b.rb * R + r, rows, row_token, a, mx, sum, lb, lane);
+        } else {
+          reinterpret_cast<float4*>(out + r * kHeadDim)[lane] = a;
+          if (lane == 0) {
+            out[R * kHeadDim + r] = mx;
+            out[R * kHeadDim + R + r] = sum;
+          }
+        }
+      }
+      if (!whole && e == 0) {
+        if (threadIdx.x == 0) ctl.split[splits] = b;
+        ++splits;
+      }
+      meet_or<32 * W>(false);   // the sums have been read
     }
-    if (!whole) {
-      if (threadIdx.x == 0) ctl.split[splits] = b;
-      ++splits;
-    }
-    x = part.end;
+    if (failed) break;
+    if (has && lane == 0) mbar_arrive(&ctl.empty[warp][slot]);
+    x = next_x;
     if (x < x1) {
-      Part a = part;
-      a.x = x;
-      next_block(P, blocks, kTileKeys, a.b);
-      a.template set<W>(x1, warp);
-      __syncwarp();
-      ctl.part[warp] = a;
+      if (lane == 0) ctl.part[warp] = ctl.next[warp];
       __syncwarp();
     }
   }
