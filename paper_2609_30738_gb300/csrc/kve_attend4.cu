@@ -23,9 +23,11 @@
 // that a token of far larger values costs the others nothing where it hardly counts. References move only when a maximum
 // passes them by 2^8, which leaves the rescaling of the output to a few steps.
 //
-// A consumer warp takes 32 tokens a step from a ring of its own in shared memory (TMA boxes of 32 rows with the 64-byte
-// swizzle), and has maxima, sums and output of its own: no warp waits for another before a part ends. One warp fills all
-// rings, a lane for each, across the ends of parts.
+// A consumer warp takes 32 tokens a step from a ring of its own in shared memory, and has maxima, sums and output of its own:
+// no warp waits for another before a part ends. Its lanes fill the ring by asynchronous copies of 16 bytes, across the ends of
+// parts. (A warp that fills all rings was slower: a tensor copy takes about 110 cycles to issue and a step is four of them,
+// with pages of 16 eight, 131072 tokens 39.1 us; asynchronous copies with an arrival of each lane at the stage's barrier
+// take 340 cycles a step, 44.1 us.)
 //
 // The work is cut over the tokens like that of the 8-bit cache (kve_line.cuh): all tiles in one line, an even share
 // for each CTA, whatever the lengths; a block of rows that falls to several CTAs is joined by the one that finishes
@@ -44,11 +46,11 @@ constexpr int kRowBytes = kHeadDim / 2;                    // codes of a token
 constexpr int kCodeBytes = kStep * kRowBytes;
 constexpr int kStageBytes = 2 * kCodeBytes;                // K, then V
 
-// R rows of a block, on W consumer warps (and one that copies).
+// R rows of a block, on W warps.
 template <int R>
 struct A4Cfg {
-  static constexpr int kWarps = R == 8 ? 7 : 11;
-  static constexpr int kThreads = 32 * (kWarps + 1);
+  static constexpr int kWarps = R == 8 ? 8 : 12;
+  static constexpr int kThreads = 32 * kWarps;
   static constexpr int kStages = R == 8 ? 3 : 4;
   static constexpr int kCtas = R == 8 ? kAttend4Ctas : 1;
   static constexpr size_t kCtl = size_t(kWarps) * kStages * kStageBytes;
@@ -73,10 +75,8 @@ struct A4Ctl {
   static constexpr int W = A4Cfg<R>::kWarps, S = A4Cfg<R>::kStages;
   alignas(128) uint32_t param[W][S][2][kStep];   // K's, V's
   float4 tokens[W][kStep];                       // of a step's tokens: K's s and z, V's log2 s and z
-  uint64_t full[W][S], empty[W][S];
-  uint32_t holes[W][S];                          // pages outside the pool: bit 0 of the first 16 tokens, bit 1 of the others
-  LineCtl<W + 1> line;
-  Part part[W], next[W];
+  LineCtl<W> line;
+  Part part[W], next[W], ahead[W];               // of a warp's sums, and of its copies
   int at[W];                                     // the stage (its bytes in the ring) with the warp's rows at a part's end
   alignas(8) float m[W][8], l[W][8];             // of eight of the warps' rows, at the end of a part
   bool has[W];                                   // the warp had steps in the part
@@ -84,7 +84,6 @@ struct A4Ctl {
   int seen[W][R];                                // tokens that the row sees
   Block split[2];                                // parts left for the join
   int last[2];                                   // whether this CTA joins them
-  int abort, never;                              // never: stays 0 (waits that a given-up call still has to make)
 };
 
 // How far (log2) a row's largest product passes its reference before that moves. Weights count from 2^(14 - kLazy) there.
@@ -99,6 +98,16 @@ __device__ __forceinline__ void mma_f16(float (&d)[4], const uint32_t (&a)[4], u
   asm("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
       : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3])
       : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
+}
+
+// 16 bytes global -> shared; a lane's copies so far are a group, and all but the last N groups have landed.
+__device__ __forceinline__ void copy16(uint32_t dst, const void* src, uint64_t policy) {
+  asm volatile("cp.async.cg.shared.global.L2::cache_hint [%0], [%1], 16, %2;" ::"r"(dst), "l"(src), "l"(policy) : "memory");
+}
+__device__ __forceinline__ void copies_group() { asm volatile("cp.async.commit_group;" ::: "memory"); }
+template <int N>
+__device__ __forceinline__ void copies_wait() {
+  asm volatile("cp.async.wait_group %0;" ::"n"(N) : "memory");
 }
 
 // A warp's 8 x 8 matrix of 16-bit elements, transposed.
@@ -145,143 +154,22 @@ __device__ __forceinline__ float len_bits(int len) { return static_cast<float>(3
 
 static_assert(attend4_smem<8>() <= 113 * 1024 && attend4_smem<16>() <= 227 * 1024, "two CTAs an SM, or one");
 
-// A barrier of the consumer warps, and whether any of their threads says so.
-template <int kThreads>
-__device__ __forceinline__ bool meet_or(bool x) {
-  uint32_t any;
-  asm volatile("{\n .reg .pred p, q;\n setp.ne.u32 q, %1, 0;\n bar.red.or.pred p, 1, %2, q;\n selp.u32 %0, 1, 0, p;\n}"
-               : "=r"(any)
-               : "r"(x ? 1u : 0u), "n"(kThreads)
-               : "memory");
-  return any != 0;
-}
-
 template <int R>
 __global__ void __launch_bounds__(A4Cfg<R>::kThreads, A4Cfg<R>::kCtas)
-cache_attend4_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constant__ CUtensorMap tm_v,
-                     const __grid_constant__ AttendParams P) {
+cache_attend4_kernel(const __grid_constant__ AttendParams P) {
   using C = A4Cfg<R>;
   constexpr int W = C::kWarps, kHalves = R / 8;   // kHalves: rows of a lane
   constexpr int S = C::kStages;
-  extern __shared__ __align__(1024) uint8_t smem[];   // the swizzle counts from 512 bytes
+  extern __shared__ __align__(128) uint8_t smem[];
   A4Ctl<R>& ctl = *reinterpret_cast<A4Ctl<R>*>(smem + C::kCtl);
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
   const int rows = P.q_tokens * P.c.group;
   const int blocks = (rows + R - 1) / R;
-  if (warp < W && lane == 0) {
-    for (int i = 0; i < S; ++i) {
-      mbar_init(&ctl.full[warp][i], 1);
-      mbar_init(&ctl.empty[warp][i], 1);
-    }
-    fence_mbar_init();
-  }
-  if (threadIdx.x == 0) {
-    ctl.abort = ctl.never = 0;
-    prefetch_tensormap(&tm_k);
-    prefetch_tensormap(&tm_v);
-  }
   wait_previous_kernel();
   Cuts<kAttend4PartTiles> cuts;
-  line_share<W + 1>(P, blocks, kTileKeys, ctl.line, cuts);
+  line_share<W>(P, blocks, kTileKeys, ctl.line, cuts);
   const int x0 = ctl.line.ends[0], x1 = ctl.line.ends[1];
   const int shift = P.c.page_shift;
-  const auto fail = [&]() {
-    ctl.abort = 1;
-    atomicOr(P.err, kErrWait);
-  };
-
-  if (warp == W) {
-    // ------------------------------------------------------------ copies: lane w fills the ring of warp w
-    bool more = lane < W && x0 < x1;
-    Part a;
-    a.b = ctl.line.first;
-    a.x = x0;
-    int step = 0, at = 0, head = 0, id0 = -1, id1 = -1;   // the next copies: first token, first row of the head in a page, pages
-    const auto page = [&](int token) {
-      if (token >= a.b.len) return 0;   // (nobody sees what is there)
-      return __ldg(P.table + static_cast<int64_t>(a.b.r) * P.c.max_pages + (token >> shift));
-    };
-    const auto valid = [&](int id) { return id >= 0 && id < P.c.num_pages; };
-    const auto advance = [&]() {   // to the step behind `step - 1`, in this part or a later one
-      while (step >= a.last) {
-        a.x = a.end;
-        if (a.x >= x1) {
-          more = false;
-          return;
-        }
-        next_block(P, blocks, kTileKeys, a.b);
-        a.template set<W>(x1, lane);
-        step = a.first;
-      }
-      at = a.tok0 + step * kStep;
-      head = a.b.h << shift;
-      id0 = page(at);
-      if (P.c.page < kStep) id1 = page(at + 16);   // (looked at when the copies are made, a turn later)
-    };
-    if (more) {
-      a.template set<W>(x1, lane);
-      step = a.first;
-      advance();
-    }
-    // Pages of a call that reads more than L2 keeps leave it first.
-    const uint64_t policy = x1 - x0 > 8 ? l2_policy_evict_first() : l2_policy_evict_normal();
-    const int rows0 = min(P.c.page, kStep);   // boxes of 32 rows, or of a page's 16
-    uint32_t fetched = 0;
-    uint64_t since = global_timer_ns();
-    bool stuck = false;
-    while (__any_sync(0xffffffffu, more)) {
-      const uint32_t slot = fetched % S;
-      const bool go = more && (fetched < S || mbar_test_wait(&ctl.empty[lane][slot], (fetched / S & 1) ^ 1));
-      if (go) {
-        uint64_t* bar = &ctl.full[lane][slot];
-        const bool ok0 = valid(id0), ok1 = rows0 < kStep ? valid(id1) : ok0;
-        ctl.holes[lane][slot] = (ok0 ? 0u : 1u) | (ok1 ? 0u : 2u);
-        if (!ok0 || !ok1) atomicOr(P.err, kErrCheck);
-        mbar_arrive_expect_tx(bar, ((ok0 ? rows0 : 0) + (rows0 < kStep && ok1 ? rows0 : 0)) * (2 * (kRowBytes + 4)));
-        for (int i = 0; i < kStep; i += rows0) {
-          const int id = i == 0 ? id0 : id1;
-          if (!(i == 0 ? ok0 : ok1)) continue;
-          const int row = (id * P.c.heads << shift) + head + ((at + i) & (P.c.page - 1));
-          uint8_t* to = smem + (lane * S + slot) * kStageBytes + i * kRowBytes;
-          tma_load_2d_hint(to, &tm_k, 0, row, bar, policy);
-          tma_load_2d_hint(to + kCodeBytes, &tm_v, 0, row, bar, policy);
-          bulk_load(&ctl.param[lane][slot][0][i], P.c.k_param + row, rows0 * 4, bar);
-          bulk_load(&ctl.param[lane][slot][1][i], P.c.v_param + row, rows0 * 4, bar);
-        }
-        ++fetched;
-        ++step;
-        advance();
-      }
-      if (__any_sync(0xffffffffu, go)) {
-        since = global_timer_ns();
-      } else {
-        __nanosleep(32);
-        stuck = *static_cast<volatile int*>(&ctl.abort) != 0 || global_timer_ns() - since > P.wait_limit_ns;
-        if (__any_sync(0xffffffffu, stuck)) break;
-      }
-    }
-    if (__any_sync(0xffffffffu, stuck)) {
-      // a wait ran out: the copies in flight end before the shared memory does
-      if (lane == 0) fail();
-      for (int w = 0; w < W; ++w) {
-        const uint32_t n = __shfl_sync(0xffffffffu, fetched, w);
-        for (uint32_t k = n > S ? n - S : 0; k < n; ++k)
-          warp_wait(&ctl.full[w][k % S], (k / S) & 1, P.wait_limit_ns, &ctl.never);
-      }
-    }
-    // sequences without a token: their rows are zeros
-    for (int r = blockIdx.x; r < P.n_seq; r += gridDim.x)
-      if (seq_len(P, r) == 0)
-        for (int i = 0; i < P.q_tokens * P.c.hq; ++i) {
-          const int64_t tok = static_cast<int64_t>(r) * P.q_tokens + i / P.c.hq;
-          reinterpret_cast<uint2*>(P.out + tok * P.o_st + (i % P.c.hq) * P.o_sh)[lane] = make_uint2(0, 0);
-          if (P.lse && lane == 0) P.lse[tok * P.c.hq + i % P.c.hq] = -INFINITY;
-        }
-    allow_next_kernel();
-    return;
-  }
-
-  // -------------------------------------------------------------- the consumers
   const int g = lane >> 2, t = lane & 3;
   // row / group, for groups that are no power of two as for those that are
   const auto row_token = [&](int row) {
@@ -293,8 +181,87 @@ cache_attend4_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_cons
   // at c ^ (r >> 1 & 3): neither meets on a bank
   const uint32_t kget = g * kRowBytes + ((t ^ (g >> 1)) << 4);
   const uint32_t vget = (lane & 7) * kRowBytes + (((lane >> 3) ^ ((lane & 7) >> 1)) << 4);
-  uint32_t used = 0;
-  bool ok = true, failed = false;
+
+  // -------------------------------------------------------------- copies, S steps ahead
+  Part& ahead = ctl.ahead[warp];
+  int ahead_step = 0, ahead_last = -1, ahead_tok0 = 0, ahead_head = 0;   // (head: its first row in a page; last < 0: no more)
+  int window = 0, held = 0;      // entries window .. window + 31 of the sequence's table, a lane each
+  int fill = 0, slot = 0;        // the stages of the next copies and of the next step
+  uint32_t gaps = 0;             // two bits a stage: pages outside the pool, of its first and of its last 16 tokens
+  const auto read_table = [&]() {   // (looked at in the next fetch)
+    window = (ahead_tok0 + ahead_step * kStep) >> shift;
+    held = 0;                       // (behind the sequence: nobody sees what is there)
+    if (window + lane < (ahead.b.len + P.c.page - 1) >> shift)
+      held = __ldg(P.table + static_cast<int64_t>(ahead.b.r) * P.c.max_pages + window + lane);
+  };
+  const auto enter = [&]() {
+    ahead_step = ahead.first;
+    ahead_last = ahead.last;
+    ahead_tok0 = ahead.tok0;
+    ahead_head = ahead.b.h << shift;
+    if (ahead_step < ahead_last) read_table();
+  };
+  const auto settle = [&]() {   // on to a part with something to read
+    while (ahead_step >= ahead_last) {
+      Part a = ahead;
+      a.x = a.end;
+      if (a.x >= x1) {
+        ahead_last = -1;
+        return;
+      }
+      next_block(P, blocks, kTileKeys, a.b);
+      a.template set<W>(x1, warp);
+      __syncwarp();
+      ahead = a;
+      __syncwarp();
+      enter();
+    }
+  };
+  // 16 bytes a lane: eight tokens of K or V at once
+  const uint32_t put = smem_u32(ring) + g * kRowBytes + ((t ^ (g >> 1)) << 4);
+  // where the rows' numbers go: four lanes each for the halves of K's and of V's
+  const uint32_t put_number = smem_u32(ctl.param[warp][0][lane >> 3 & 1] + (lane & 7) * 4);
+  const auto fetch = [&]() {
+    if (ahead_last >= 0) {
+      const int at = ahead_tok0 + ahead_step * kStep;
+      int id0 = __shfl_sync(0xffffffffu, held, (at >> shift) - window);
+      int id1 = __shfl_sync(0xffffffffu, held, ((at + 16) >> shift) - window);
+      const bool ok0 = static_cast<uint32_t>(id0) < static_cast<uint32_t>(P.c.num_pages);
+      const bool ok1 = static_cast<uint32_t>(id1) < static_cast<uint32_t>(P.c.num_pages);
+      gaps = (gaps & ~(3u << 2 * fill)) | (ok0 ? 0u : 1u) << 2 * fill | (ok1 ? 0u : 2u) << 2 * fill;
+      if (!ok0 || !ok1) atomicOr(P.err, kErrCheck);
+      // Pages of a call that reads more than L2 keeps leave it first.
+      const uint64_t policy = x1 - x0 > 8 ? l2_policy_evict_first() : l2_policy_evict_normal();
+      const int row0 = (id0 * P.c.heads << shift) + ahead_head + (at & (P.c.page - 1));
+      const int row1 = (id1 * P.c.heads << shift) + ahead_head + ((at + 16) & (P.c.page - 1));
+      const uint32_t to = put + fill * kStageBytes;
+      if (ok0) {
+        const int64_t from = static_cast<int64_t>(row0) * kRowBytes + lane * 16;
+        copy16(to, P.c.k + from, policy);
+        copy16(to + 512, P.c.k + from + 512, policy);
+        copy16(to + kCodeBytes, P.c.v + from, policy);
+        copy16(to + kCodeBytes + 512, P.c.v + from + 512, policy);
+      }
+      if (ok1) {
+        const int64_t from = static_cast<int64_t>(row1) * kRowBytes + lane * 16;
+        copy16(to + 1024, P.c.k + from, policy);
+        copy16(to + 1536, P.c.k + from + 512, policy);
+        copy16(to + kCodeBytes + 1024, P.c.v + from, policy);
+        copy16(to + kCodeBytes + 1536, P.c.v + from + 512, policy);
+      }
+      if (lane < 16 && (lane & 4 ? ok1 : ok0))
+        copy16(put_number + fill * (2 * kStep * 4), (lane & 8 ? P.c.v_param : P.c.k_param) + (lane & 4 ? row1 : row0) + (lane & 3) * 4,
+               policy);
+      fill = fill + 1 == S ? 0 : fill + 1;
+      ++ahead_step;
+      if (ahead_step < ahead_last) {
+        if (((ahead_tok0 + ahead_step * kStep + 16) >> shift) >= window + 32) read_table();
+      } else {
+        settle();
+      }
+    }
+    copies_group();   // (an empty one too: groups are counted)
+  };
   // the raw query rows of a part: row 8 e + g of the block, elements 32 t .. 32 t + 31
   uint4 raw[kHalves][4];
   const auto load_rows = [&](const Block& b) {
@@ -316,9 +283,13 @@ cache_attend4_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_cons
     a.b = ctl.line.first;
     a.x = x0;
     a.template set<W>(x1, warp);
-    ctl.part[warp] = a;
-    load_rows(a.b);
+    ctl.part[warp] = ahead = a;
     __syncwarp();
+    enter();
+    load_rows(a.b);
+    settle();
+#pragma unroll 1
+    for (int i = 0; i < S; ++i) fetch();
   }
   for (int x = x0; x < x1;) {
     const Part& part = ctl.part[warp];
@@ -384,15 +355,10 @@ cache_attend4_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_cons
       l[e] = z[e] = both(0.f);
     }
     const int first = part.first, last = part.last, tok0 = part.tok0, all_see = b.len - P.q_tokens + 1;
-    uint32_t slot = 0;
 #pragma unroll 1
     for (int step = first; step < last; ++step) {
-      slot = used % S;
-      if (!warp_wait(&ctl.full[warp][slot], (used / S) & 1, P.wait_limit_ns, &ctl.abort)) {
-        ok = false;
-        break;
-      }
-      ++used;
+      copies_wait<S - 1>();
+      __syncwarp();   // every lane's copies of this step have landed
       const uint8_t* const at = ring + slot * kStageBytes;
       {
         // a lane a token: its four numbers for every lane
@@ -420,7 +386,7 @@ cache_attend4_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_cons
       }
       __syncwarp();
       const int pos0 = tok0 + step * kStep;
-      const uint32_t hole = ctl.holes[warp][slot];
+      const uint32_t hole = gaps >> 2 * slot & 3u;
       const bool some = hole != 0 || pos0 + kStep > all_see;   // tokens that not all rows see
       // logits (over kq) in place of the products
       float2 y[4][kHalves], kq[kHalves];
@@ -538,10 +504,11 @@ cache_attend4_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_cons
           }
       }
       __syncwarp();   // the stage and the tokens' numbers have been read
-      // (the last stage of a part is where its sums are put together, then it is given back)
-      if (lane == 0 && step + 1 < last) mbar_arrive(&ctl.empty[warp][slot]);
+      if (step + 1 < last) {   // (the last stage of a part is where its sums are put together)
+        fetch();
+        slot = slot + 1 == S ? 0 : slot + 1;
+      }
     }
-    if (!ok && lane == 0) fail();
 
     // ---------------------------------------------------------- the end of a part: the warps' rows together, eight by eight
     const bool has = first < last, whole = x == b.first && part.end == b.first + b.tiles;
@@ -599,8 +566,7 @@ cache_attend4_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_cons
         load_rows(a.b);
         ctl.next[warp] = a;
       }
-      failed = meet_or<32 * W>(!ok);
-      if (failed) break;
+      __syncthreads();
       for (int row = warp; row < 8; row += W) {
         float mx = -INFINITY;
 #pragma unroll
@@ -635,30 +601,40 @@ cache_attend4_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_cons
         if (threadIdx.x == 0) ctl.split[splits] = b;
         ++splits;
       }
-      meet_or<32 * W>(false);   // the sums have been read
+      __syncthreads();   // the sums have been read
     }
-    if (failed) break;
-    if (has && lane == 0) mbar_arrive(&ctl.empty[warp][slot]);
+    if (has) {
+      fetch();
+      slot = slot + 1 == S ? 0 : slot + 1;
+    }
     x = next_x;
     if (x < x1) {
       if (lane == 0) ctl.part[warp] = ctl.next[warp];
       __syncwarp();
     }
   }
-  if (failed) return;
+
+  // sequences without a token: their rows are zeros
+  for (int r = blockIdx.x * W + warp; r < P.n_seq; r += W * gridDim.x)
+    if (seq_len(P, r) == 0)
+      for (int i = 0; i < P.q_tokens * P.c.hq; ++i) {
+        const int64_t tok = static_cast<int64_t>(r) * P.q_tokens + i / P.c.hq;
+        reinterpret_cast<uint2*>(P.out + tok * P.o_st + (i % P.c.hq) * P.o_sh)[lane] = make_uint2(0, 0);
+        if (P.lse && lane == 0) P.lse[tok * P.c.hq + i % P.c.hq] = -INFINITY;
+      }
 
   // ------------------------------------------------------------ the join of blocks that several CTAs had parts of
   allow_next_kernel();
   if (splits == 0) return;
   __threadfence();
-  meet_or<32 * W>(false);   // every thread's part of the sums is out, and ctl.split is written
+  __syncthreads();   // every thread's part of the sums is out, and ctl.split is written
   for (int k = 0; k < splits; ++k) {
     const Block s = ctl.split[k];
     int w0, w1;
     cuts.parts(s, &w0, &w1);
     if (threadIdx.x == 0)
       ctl.last[k] = inc_acq_rel_gpu(P.arrive + w0, static_cast<unsigned>(w1 - w0)) == static_cast<unsigned>(w1 - w0);
-    meet_or<32 * W>(false);
+    __syncthreads();
     if (!ctl.last[k]) continue;
     __threadfence();
     const int parts = w1 - w0 + 1;
@@ -700,7 +676,7 @@ cudaError_t attend4_rows(const kve_cache& c, const AttendParams& p, cudaStream_t
   const int64_t most = static_cast<int64_t>(C::kCtas) * c.sms;
   const int64_t want = tiles >= most ? most : tiles * p.n_seq * p.c.heads * blocks;
   return launch_after_previous(fn, dim3(static_cast<unsigned>(want < most ? want : most)), dim3(C::kThreads),
-                               attend4_smem<R>(), stream, c.tm_k, c.tm_v, p);
+                               attend4_smem<R>(), stream, p);
 }
 
 }  // namespace

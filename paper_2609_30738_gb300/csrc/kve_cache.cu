@@ -871,7 +871,7 @@ kve_status create_cache(const kve_cache_config* cfg, int bits, uint8_t* k, uint8
   w.clear_end = align_up(w.arrive + sizeof(uint32_t) * 2 * workers, 256);
   w.partial = w.clear_end;
   w.total = align_up(w.partial + workers * 2 * kve::kAttendPartWords * sizeof(float), 256);
-  h->maps = kve::encode_pages(&h->tm_k, k, g, bits) && kve::encode_pages(&h->tm_v, v, g, bits);
+  h->maps = bits == 8 && kve::encode_pages(&h->tm_k, k, g) && kve::encode_pages(&h->tm_v, v, g);
   if (workspace_bytes) *workspace_bytes = w.total;
   *cache_out = h;
   return KVE_OK;
@@ -1057,7 +1057,7 @@ kve_status kv_evict_cache_attend(const kve_cache* cache, int32_t layer, int32_t 
   if (!kve::rows_apart(tokens, p.o_st, c.hq, p.o_sh)) return KVE_EINVAL;
   if (!on_device(cache)) return KVE_EINVAL;
   if (n_seq == 0) return KVE_OK;
-  if (!cache->maps) return KVE_ECUDA;
+  if (cache->bits == 8 && !cache->maps) return KVE_ECUDA;
   p.c = c;
   p.wait_limit_ns = kWaitNs;
   p.n_seq = n_seq;

@@ -353,7 +353,7 @@ struct kve_cache {
   int32_t bits;          // 8 or 4
   int32_t device;        // of k, or -1 where the runtime does not know the pointer
   int32_t sms;           // SMs the workspace was sized for
-  bool maps;             // the TMA maps are encoded (no driver, none)
+  bool maps;             // 8 bits: the TMA maps are encoded (no driver, none)
   CUtensorMap tm_k, tm_v;
 };
 
@@ -441,9 +441,9 @@ bool row_strides(const int64_t* given, int64_t heads, int64_t* token, int64_t* h
 bool rows_apart(int64_t tokens, int64_t token, int64_t heads, int64_t head);
 constexpr int kUnknown = -1, kHostMemory = -2;
 int place_of(const void* p);
-// The TMA map of a cache's codes, [pages * H * P] rows of 128 bytes in boxes of a page's rows with the 128-byte swizzle, or
-// rows of 64 bytes (4 bits) in boxes of up to 32 of them with the 64-byte swizzle; false without a driver (kve_host.cu).
-bool encode_pages(CUtensorMap* map, const void* base, const CacheGeometry& c, int bits);
+// The TMA map of a cache's codes, [pages * H * P][d] bytes in boxes of a page's rows with the 128-byte
+// swizzle; false without a driver (kve_host.cu).
+bool encode_pages(CUtensorMap* map, const void* base, const CacheGeometry& c);
 // Host memory the CUDA runtime does not know is refused as a row source (kve_host.cu).
 bool readable_source(const void* src);
 
