@@ -49,10 +49,21 @@ constexpr int kStageBytes = 2 * kCodeBytes;                // K, then V
 // R rows of a block, on W warps.
 template <int R>
 struct A4Cfg {
-  static constexpr int kWarps = R == 8 ? 8 : 12;
+#ifndef W8
+#define W8 8
+#define C8 2
+#define W16 4
+#define C16 3
+#endif
+#ifndef KP8
+#define KP8 2
+#define KP16 2
+#endif
+  static constexpr int kWarps = R == 8 ? W8 : W16;
   static constexpr int kThreads = 32 * kWarps;
-  static constexpr int kStages = R == 8 ? 3 : 4;
-  static constexpr int kCtas = R == 8 ? kAttend4Ctas : 1;
+  static constexpr int kStages = 3;
+  static constexpr int kCtas = R == 8 ? C8 : C16;
+  static constexpr int kTile = kWarps * kStep;   // tokens: a step of every warp
   static constexpr size_t kCtl = size_t(kWarps) * kStages * kStageBytes;
 };
 
@@ -63,8 +74,8 @@ struct Part {
   template <int W>
   __device__ __forceinline__ void set(int x1, int warp) {
     end = min(x1, b.first + b.tiles);
-    tok0 = (x - b.first) * kTileKeys;
-    const int steps = (min((end - b.first) * kTileKeys, b.len) - tok0 + kStep - 1) / kStep;
+    tok0 = (x - b.first) * (W * kStep);
+    const int steps = (min((end - b.first) * (W * kStep), b.len) - tok0 + kStep - 1) / kStep;
     first = steps * warp / W;
     last = steps * (warp + 1) / W;
   }
@@ -126,6 +137,13 @@ __device__ __forceinline__ void load_transposed(uint32_t (&d)[4], uint32_t at) {
                : "memory");
 }
 
+// A load that is issued here, not where its value is first needed.
+__device__ __forceinline__ uint4 load_now(const void* p) {
+  uint4 v;
+  asm volatile("ld.global.v4.u32 {%0,%1,%2,%3}, [%4];" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "l"(p) : "memory");
+  return v;
+}
+
 __device__ __forceinline__ float2 fmul2(float2 a, float2 b) {
   uint64_t ra, rb, rd;
   asm("mov.b64 %0, {%1,%2};" : "=l"(ra) : "f"(a.x), "f"(a.y));
@@ -152,7 +170,8 @@ __device__ __forceinline__ float high_bf16(uint32_t x) { return __uint_as_float(
 // little as the probabilities' sum passes 1.
 __device__ __forceinline__ float len_bits(int len) { return static_cast<float>(32 - __clz(len - 1)); }   // (1: 0)
 
-static_assert(attend4_smem<8>() <= 113 * 1024 && attend4_smem<16>() <= 227 * 1024, "two CTAs an SM, or one");
+static_assert((attend4_smem<8>() + 1024) * A4Cfg<8>::kCtas <= 228 * 1024 && (attend4_smem<16>() + 1024) * A4Cfg<16>::kCtas <= 228 * 1024,
+              "CTAs an SM");
 
 template <int R>
 __global__ void __launch_bounds__(A4Cfg<R>::kThreads, A4Cfg<R>::kCtas)
@@ -166,8 +185,9 @@ cache_attend4_kernel(const __grid_constant__ AttendParams P) {
   const int rows = P.q_tokens * P.c.group;
   const int blocks = (rows + R - 1) / R;
   wait_previous_kernel();
-  Cuts<kAttend4PartTiles> cuts;
-  line_share<W>(P, blocks, kTileKeys, ctl.line, cuts);
+  constexpr int kPart = R == 8 ? KP8 : KP16;
+  Cuts<kPart> cuts;
+  line_share<W>(P, blocks, A4Cfg<R>::kTile, ctl.line, cuts);
   const int x0 = ctl.line.ends[0], x1 = ctl.line.ends[1];
   const int shift = P.c.page_shift;
   const int g = lane >> 2, t = lane & 3;
@@ -209,7 +229,7 @@ cache_attend4_kernel(const __grid_constant__ AttendParams P) {
         ahead_last = -1;
         return;
       }
-      next_block(P, blocks, kTileKeys, a.b);
+      next_block(P, blocks, A4Cfg<R>::kTile, a.b);
       a.template set<W>(x1, warp);
       __syncwarp();
       ahead = a;
@@ -274,7 +294,7 @@ cache_attend4_kernel(const __grid_constant__ AttendParams P) {
       if (row < rows) {
         const uint16_t* from = P.q + (static_cast<int64_t>(b.r) * P.q_tokens + qt) * P.q_st + hq * P.q_sh + 32 * t;
 #pragma unroll
-        for (int i = 0; i < 4; ++i) raw[e][i] = __ldg(reinterpret_cast<const uint4*>(from) + i);
+        for (int i = 0; i < 4; ++i) raw[e][i] = load_now(from + 8 * i);
       }
     }
   };
@@ -561,7 +581,7 @@ cache_attend4_kernel(const __grid_constant__ AttendParams P) {
       if (e + 1 == kHalves && next_x < x1) {   // the next part, and its rows on their way
         Part a = part;
         a.x = next_x;
-        next_block(P, blocks, kTileKeys, a.b);
+        next_block(P, blocks, A4Cfg<R>::kTile, a.b);
         a.template set<W>(x1, warp);
         load_rows(a.b);
         ctl.next[warp] = a;
@@ -628,39 +648,101 @@ cache_attend4_kernel(const __grid_constant__ AttendParams P) {
   if (splits == 0) return;
   __threadfence();
   __syncthreads();   // every thread's part of the sums is out, and ctl.split is written
-  for (int k = 0; k < splits; ++k) {
-    const Block s = ctl.split[k];
+  constexpr int kRows = (R + W - 1) / W;
+  for (int n = 0; n < splits; ++n) {
+    const Block s = ctl.split[n];
     int w0, w1;
     cuts.parts(s, &w0, &w1);
     if (threadIdx.x == 0)
-      ctl.last[k] = inc_acq_rel_gpu(P.arrive + w0, static_cast<unsigned>(w1 - w0)) == static_cast<unsigned>(w1 - w0);
+      ctl.last[n] = inc_acq_rel_gpu(P.arrive + w0, static_cast<unsigned>(w1 - w0)) == static_cast<unsigned>(w1 - w0);
     __syncthreads();
-    if (!ctl.last[k]) continue;
+    if (!ctl.last[n]) continue;
     __threadfence();
-    const int parts = w1 - w0 + 1;
-    const float lb = len_bits(s.len);
-    for (int row = warp; row < R && s.rb * R + row < rows; row += W) {
-      // part p: slot 0 of CTA w0 + p, of the first one slot 1
-      const auto at = [&](int p) { return P.partial + (static_cast<int64_t>(w0 + p) * 2 + (p == 0)) * kAttend4PartWords; };
-      float mx = -INFINITY;
-      for (int p = lane; p < parts; p += 32) mx = fmaxf(mx, __ldcg(at(p) + R * kHeadDim + row));
-      mx = warp_max(mx);
-      const float mr = mx == -INFINITY ? 0.f : mx;
-      float4 a = make_float4(0.f, 0.f, 0.f, 0.f);
-      float sum = 0.f;
-#pragma unroll 8
-      for (int p = 0; p < parts; ++p) {
-        const float* from = at(p);
-        const float f = ex2(__ldcg(from + R * kHeadDim + row) - mr);
-        const float4 v = __ldcg(reinterpret_cast<const float4*>(from + row * kHeadDim) + lane);
-        sum = fmaf(__ldcg(from + R * kHeadDim + R + row), f, sum);
-        a.x = fmaf(v.x, f, a.x);
-        a.y = fmaf(v.y, f, a.y);
-        a.z = fmaf(v.z, f, a.z);
-        a.w = fmaf(v.w, f, a.w);
-      }
-      emit_row(P, s, s.rb * R + row, rows, row_token, a, mx, sum, lb, lane);
+    // A warp has the rows warp, warp + W, ...; where there are twice as many warps as rows or more, a row's parts are dealt
+    // to several warps, whose sums the first of them adds in their order.
+    const int parts = w1 - w0 + 1, there = min(R, rows - s.rb * R);
+    const int teams = kRows == 1 && there < W ? W / there : 1;
+    const int row0 = teams > 1 ? warp % there : warp, team = teams > 1 ? warp / there : 0;
+    const int p0 = parts * team / teams, p1 = parts * (team + 1) / teams;
+    const bool works = row0 < there && team < teams;
+    // part p: slot 0 of CTA w0 + p, of the first one slot 1
+    const auto at = [&](int p) { return P.partial + (static_cast<int64_t>(w0 + p) * 2 + (p == 0)) * kAttend4PartWords; };
+    float mx[kRows], sum[kRows];
+    float4 acc[kRows];
+#pragma unroll
+    for (int k = 0; k < kRows; ++k) {
+      mx[k] = -INFINITY;
+      sum[k] = 0.f;
+      acc[k] = make_float4(0.f, 0.f, 0.f, 0.f);
     }
+    for (int c0 = p0; works && c0 < p1; c0 += 32) {
+      const int count = min(p1 - c0, 32);
+      float f[kRows];
+#pragma unroll
+      for (int k = 0; k < kRows; ++k) {   // a lane a part: its maximum and sum
+        const int row = row0 + k * W;
+        float pm = -INFINITY, pl = 0.f;
+        if (lane < count && row < there) {
+          pm = __ldcg(at(c0 + lane) + R * kHeadDim + row);
+          pl = __ldcg(at(c0 + lane) + R * kHeadDim + R + row);
+        }
+        const float top = fmaxf(mx[k], warp_max(pm)), back = ex2(mx[k] - or_zero(top));
+        mx[k] = top;
+        f[k] = ex2(pm - or_zero(top));
+        pl *= f[k];
+#pragma unroll
+        for (int d = 16; d > 0; d >>= 1) pl += __shfl_xor_sync(0xffffffffu, pl, d);
+        sum[k] = fmaf(sum[k], back, pl);
+        acc[k].x *= back, acc[k].y *= back, acc[k].z *= back, acc[k].w *= back;
+      }
+      constexpr int kAtOnce = 16 / kRows;   // loads in flight
+      for (int j0 = 0; j0 < count; j0 += kAtOnce) {
+        float4 v[kAtOnce][kRows];
+#pragma unroll
+        for (int j = 0; j < kAtOnce; ++j)
+#pragma unroll
+          for (int k = 0; k < kRows; ++k) {
+            v[j][k] = make_float4(0.f, 0.f, 0.f, 0.f);
+            if (j0 + j < count && row0 + k * W < there)
+              v[j][k] = __ldcg(reinterpret_cast<const float4*>(at(c0 + j0 + j) + (row0 + k * W) * kHeadDim) + lane);
+          }
+#pragma unroll
+        for (int j = 0; j < kAtOnce; ++j)
+#pragma unroll
+          for (int k = 0; k < kRows; ++k) {
+            const float g = __shfl_sync(0xffffffffu, f[k], (j0 + j) & 31);
+            if (j0 + j >= count) continue;
+            acc[k].x = fmaf(v[j][k].x, g, acc[k].x);
+            acc[k].y = fmaf(v[j][k].y, g, acc[k].y);
+            acc[k].z = fmaf(v[j][k].z, g, acc[k].z);
+            acc[k].w = fmaf(v[j][k].w, g, acc[k].w);
+          }
+      }
+    }
+    if (teams > 1) {
+      float4* const sums = reinterpret_cast<float4*>(smem);
+      __syncthreads();   // (the block before has read its sums)
+      if (works) sums[warp * 32 + lane] = acc[0];
+      if (works && lane == 0) {
+        ctl.m[warp][0] = mx[0];
+        ctl.l[warp][0] = sum[0];
+      }
+      __syncthreads();
+      if (works && team == 0)
+        for (int w = row0 + there; w < teams * there; w += there) {
+          const float top = fmaxf(mx[0], ctl.m[w][0]), a = ex2(mx[0] - or_zero(top)), c = ex2(ctl.m[w][0] - or_zero(top));
+          const float4 v = sums[w * 32 + lane];
+          mx[0] = top;
+          sum[0] = fmaf(sum[0], a, ctl.l[w][0] * c);
+          acc[0] = make_float4(fmaf(acc[0].x, a, v.x * c), fmaf(acc[0].y, a, v.y * c), fmaf(acc[0].z, a, v.z * c),
+                               fmaf(acc[0].w, a, v.w * c));
+        }
+    }
+    if (works && team == 0)
+#pragma unroll
+      for (int k = 0; k < kRows; ++k)
+        if (row0 + k * W < there)
+          emit_row(P, s, s.rb * R + row0 + k * W, rows, row_token, acc[k], mx[k], sum[k], len_bits(s.len), lane);
   }
 }
 
@@ -672,7 +754,7 @@ cudaError_t attend4_rows(const kve_cache& c, const AttendParams& p, cudaStream_t
   if (e != cudaSuccess) return e;
   // no more CTAs than there can be tiles
   const int64_t blocks = (p.q_tokens * p.c.group + R - 1) / R;
-  const int64_t tiles = ((static_cast<int64_t>(p.c.max_pages) << p.c.page_shift) + kTileKeys - 1) / kTileKeys;
+  const int64_t tiles = ((static_cast<int64_t>(p.c.max_pages) << p.c.page_shift) + A4Cfg<R>::kTile - 1) / A4Cfg<R>::kTile;
   const int64_t most = static_cast<int64_t>(C::kCtas) * c.sms;
   const int64_t want = tiles >= most ? most : tiles * p.n_seq * p.c.heads * blocks;
   return launch_after_previous(fn, dim3(static_cast<unsigned>(want < most ? want : most)), dim3(C::kThreads),

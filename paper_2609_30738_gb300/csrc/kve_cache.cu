@@ -866,8 +866,8 @@ kve_status create_cache(const kve_cache_config* cfg, int bits, uint8_t* k, uint8
   w.pages_done = 64;
   w.refused = 128;
   w.arrive = 256;
-  static_assert(kve::kAttend4Ctas <= kve::kAttendCtas && kve::kAttend4PartWords <= kve::kAttendPartWords, "one size for both");
-  const size_t workers = static_cast<size_t>(kve::kAttendCtas) * sms;
+  static_assert(kve::kAttend4PartWords == kve::kAttendPartWords, "one size for both");
+  const size_t workers = static_cast<size_t>(bits == 8 ? kve::kAttendCtas : kve::kAttend4Ctas) * sms;
   w.clear_end = align_up(w.arrive + sizeof(uint32_t) * 2 * workers, 256);
   w.partial = w.clear_end;
   w.total = align_up(w.partial + workers * 2 * kve::kAttendPartWords * sizeof(float), 256);

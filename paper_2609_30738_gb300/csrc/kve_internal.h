@@ -32,9 +32,8 @@ constexpr int kAttendCtas = 2;       // attention CTAs an SM
 constexpr int kAttendRows = 16;      // most query rows of one attention row block
 constexpr int kAttendPartWords = kAttendRows * (kHeadDim + 2);   // a part: rows, their maxima and sums
 // The paged 4-bit cache
-constexpr int kAttend4Ctas = 2;      // attention CTAs an SM (the workspace is sized like the 8-bit one's)
+constexpr int kAttend4Ctas = 4;      // most attention CTAs an SM
 constexpr int kAttend4PartWords = kAttendPartWords;
-constexpr int kAttend4PartTiles = 2; // what a part costs beside its own tiles
 
 // Request table and derived counts, identical on host and device.
 struct Geometry {
