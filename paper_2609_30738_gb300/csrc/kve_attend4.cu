@@ -24,10 +24,9 @@
 // passes them by 2^8, which leaves the rescaling of the output to a few steps.
 //
 // A consumer warp takes 32 tokens a step from a ring of its own in shared memory, and has maxima, sums and output of its own:
-// no warp waits for another before a part ends. Its lanes fill the ring by asynchronous copies of 16 bytes, across the ends of
-// parts. (A warp that fills all rings was slower: a tensor copy takes about 110 cycles to issue and a step is four of them,
-// with pages of 16 eight, 131072 tokens 39.1 us; asynchronous copies with an arrival of each lane at the stage's barrier
-// take 340 cycles a step, 44.1 us.)
+// no warp waits for another before a part ends. It fills its ring itself, across the ends of parts, by
+// asynchronous copies that stand between its products. (A tensor copy holds its warp for more than 100 cycles, and a step is
+// four of them, with pages of 16 eight: 131072 tokens took 40.9 us with them, and one warp that fills all rings is too slow.)
 //
 // The work is cut over the tokens like that of the 8-bit cache (kve_line.cuh): all tiles in one line, an even share
 // for each CTA, whatever the lengths; a block of rows that falls to several CTAs is joined by the one that finishes
@@ -111,9 +110,13 @@ __device__ __forceinline__ void mma_f16(float (&d)[4], const uint32_t (&a)[4], u
       : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
 }
 
-// 16 bytes global -> shared; a lane's copies so far are a group, and all but the last N groups have landed.
-__device__ __forceinline__ void copy16(uint32_t dst, const void* src, uint64_t policy) {
-  asm volatile("cp.async.cg.shared.global.L2::cache_hint [%0], [%1], 16, %2;" ::"r"(dst), "l"(src), "l"(policy) : "memory");
+// 16 bytes global -> shared where `there`; a lane's copies so far are a group; all but the last N groups have landed.
+__device__ __forceinline__ void copy16(uint32_t dst, const void* src, uint64_t policy, bool there) {
+  asm volatile(
+      "{\n .reg .pred p;\n setp.ne.b32 p, %3, 0;\n"
+      " @p cp.async.cg.shared.global.L2::cache_hint [%0], [%1], 16, %2;\n}" ::"r"(dst),
+      "l"(src), "l"(policy), "r"(there ? 1 : 0)
+      : "memory");
 }
 __device__ __forceinline__ void copies_group() { asm volatile("cp.async.commit_group;" ::: "memory"); }
 template <int N>
@@ -197,16 +200,16 @@ cache_attend4_kernel(const __grid_constant__ AttendParams P) {
   };
   int splits = 0;
   uint8_t* const ring = smem + warp * (S * kStageBytes);
-  // K: 16 bytes (t) of the tokens 8 i + g; V: row lane % 8, 16 bytes lane / 8 of eight tokens. A 16-byte chunk c of row r lies
+  // K: 16 bytes (t) of the tokens 8 i + g; V: row lane % 8, 16 bytes lane / 8 of eight tokens. A 16-byte chunk c of token r lies
   // at c ^ (r >> 1 & 3): neither meets on a bank
-  const uint32_t kget = g * kRowBytes + ((t ^ (g >> 1)) << 4);
-  const uint32_t vget = (lane & 7) * kRowBytes + (((lane >> 3) ^ ((lane & 7) >> 1)) << 4);
+  const auto lies = [](int token, int chunk) { return token * kRowBytes + ((chunk ^ token >> 1) << 4); };
+  const uint32_t kget = lies(g, t), vget = lies(lane & 7, lane >> 3);
 
-  // -------------------------------------------------------------- copies, S steps ahead
+  // -------------------------------------------------------------- copies, S - 1 steps ahead
   Part& ahead = ctl.ahead[warp];
   int ahead_step = 0, ahead_last = -1, ahead_tok0 = 0, ahead_head = 0;   // (head: its first row in a page; last < 0: no more)
-  int window = 0, held = 0;      // entries window .. window + 31 of the sequence's table, a lane each
-  int fill = 0, slot = 0;        // the stages of the next copies and of the next step
+  int window = 0, held = 0;         // entries window .. window + 31 of the sequence's table, a lane each
+  int fill = 0, slot = 0;           // the stages of the next copies and of the next step
   uint32_t gaps = 0;             // two bits a stage: pages outside the pool, of its first and of its last 16 tokens
   const auto read_table = [&]() {   // (looked at in the next fetch)
     window = (ahead_tok0 + ahead_step * kStep) >> shift;
@@ -237,41 +240,43 @@ cache_attend4_kernel(const __grid_constant__ AttendParams P) {
       enter();
     }
   };
-  // 16 bytes a lane: eight tokens of K or V at once
-  const uint32_t put = smem_u32(ring) + g * kRowBytes + ((t ^ (g >> 1)) << 4);
-  // where the rows' numbers go: four lanes each for the halves of K's and of V's
+  // Pages of a call that reads more than L2 keeps leave it first.
+  const uint64_t policy = x1 - x0 > 8 ? l2_policy_evict_first() : l2_policy_evict_normal();
+  const uint32_t put = smem_u32(ring) + lies(g, t);   // eight tokens of K or V at once, 16 bytes a lane
+  // the rows' numbers: four lanes each for the halves of K's and of V's
   const uint32_t put_number = smem_u32(ctl.param[warp][0][lane >> 3 & 1] + (lane & 7) * 4);
-  const auto fetch = [&]() {
+  // The copies of the next step, in three pieces that stand between the products: where its rows are (of its two halves, in
+  // the pool), K, and the rest.
+  int row0 = 0, row1 = 0;
+  bool ok0 = false, ok1 = false;
+  const auto find = [&]() {
+    ok0 = ok1 = false;
+    if (ahead_last < 0) return;
+    const int at = ahead_tok0 + ahead_step * kStep;
+    const int id0 = __shfl_sync(0xffffffffu, held, (at >> shift) - window);
+    const int id1 = __shfl_sync(0xffffffffu, held, ((at + 16) >> shift) - window);
+    ok0 = static_cast<uint32_t>(id0) < static_cast<uint32_t>(P.c.num_pages);
+    ok1 = static_cast<uint32_t>(id1) < static_cast<uint32_t>(P.c.num_pages);
+    gaps = (gaps & ~(3u << 2 * fill)) | (ok0 ? 0u : 1u) << 2 * fill | (ok1 ? 0u : 2u) << 2 * fill;
+    if (!ok0 || !ok1) atomicOr(P.err, kErrCheck);
+    row0 = (id0 * P.c.heads << shift) + ahead_head + (at & (P.c.page - 1));
+    row1 = (id1 * P.c.heads << shift) + ahead_head + ((at + 16) & (P.c.page - 1));
+  };
+  const auto copy_codes = [&](const uint8_t* base, uint32_t to) {
+    const uint8_t* const from0 = base + static_cast<int64_t>(row0) * kRowBytes + lane * 16;
+    const uint8_t* const from1 = base + static_cast<int64_t>(row1) * kRowBytes + lane * 16;
+    copy16(to, from0, policy, ok0);
+    copy16(to + 512, from0 + 512, policy, ok0);
+    copy16(to + 1024, from1, policy, ok1);
+    copy16(to + 1536, from1 + 512, policy, ok1);
+  };
+  const auto copy_keys = [&]() { copy_codes(P.c.k, put + fill * kStageBytes); };
+  const auto copy_rest = [&]() {
+    copy_codes(P.c.v, put + fill * kStageBytes + kCodeBytes);
+    copy16(put_number + fill * (2 * kStep * 4), (lane & 8 ? P.c.v_param : P.c.k_param) + (lane & 4 ? row1 : row0) + (lane & 3) * 4,
+           policy, lane < 16 && (lane & 4 ? ok1 : ok0));
+    copies_group();   // (an empty one too: groups are counted)
     if (ahead_last >= 0) {
-      const int at = ahead_tok0 + ahead_step * kStep;
-      int id0 = __shfl_sync(0xffffffffu, held, (at >> shift) - window);
-      int id1 = __shfl_sync(0xffffffffu, held, ((at + 16) >> shift) - window);
-      const bool ok0 = static_cast<uint32_t>(id0) < static_cast<uint32_t>(P.c.num_pages);
-      const bool ok1 = static_cast<uint32_t>(id1) < static_cast<uint32_t>(P.c.num_pages);
-      gaps = (gaps & ~(3u << 2 * fill)) | (ok0 ? 0u : 1u) << 2 * fill | (ok1 ? 0u : 2u) << 2 * fill;
-      if (!ok0 || !ok1) atomicOr(P.err, kErrCheck);
-      // Pages of a call that reads more than L2 keeps leave it first.
-      const uint64_t policy = x1 - x0 > 8 ? l2_policy_evict_first() : l2_policy_evict_normal();
-      const int row0 = (id0 * P.c.heads << shift) + ahead_head + (at & (P.c.page - 1));
-      const int row1 = (id1 * P.c.heads << shift) + ahead_head + ((at + 16) & (P.c.page - 1));
-      const uint32_t to = put + fill * kStageBytes;
-      if (ok0) {
-        const int64_t from = static_cast<int64_t>(row0) * kRowBytes + lane * 16;
-        copy16(to, P.c.k + from, policy);
-        copy16(to + 512, P.c.k + from + 512, policy);
-        copy16(to + kCodeBytes, P.c.v + from, policy);
-        copy16(to + kCodeBytes + 512, P.c.v + from + 512, policy);
-      }
-      if (ok1) {
-        const int64_t from = static_cast<int64_t>(row1) * kRowBytes + lane * 16;
-        copy16(to + 1024, P.c.k + from, policy);
-        copy16(to + 1536, P.c.k + from + 512, policy);
-        copy16(to + kCodeBytes + 1024, P.c.v + from, policy);
-        copy16(to + kCodeBytes + 1536, P.c.v + from + 512, policy);
-      }
-      if (lane < 16 && (lane & 4 ? ok1 : ok0))
-        copy16(put_number + fill * (2 * kStep * 4), (lane & 8 ? P.c.v_param : P.c.k_param) + (lane & 4 ? row1 : row0) + (lane & 3) * 4,
-               policy);
       fill = fill + 1 == S ? 0 : fill + 1;
       ++ahead_step;
       if (ahead_step < ahead_last) {
@@ -280,7 +285,6 @@ cache_attend4_kernel(const __grid_constant__ AttendParams P) {
         settle();
       }
     }
-    copies_group();   // (an empty one too: groups are counted)
   };
   // the raw query rows of a part: row 8 e + g of the block, elements 32 t .. 32 t + 31
   uint4 raw[kHalves][4];
@@ -309,7 +313,11 @@ cache_attend4_kernel(const __grid_constant__ AttendParams P) {
     load_rows(a.b);
     settle();
 #pragma unroll 1
-    for (int i = 0; i < S; ++i) fetch();
+    for (int i = 0; i < S - 1; ++i) {
+      find();
+      copy_keys();
+      copy_rest();
+    }
   }
   for (int x = x0; x < x1;) {
     const Part& part = ctl.part[warp];
@@ -377,8 +385,10 @@ cache_attend4_kernel(const __grid_constant__ AttendParams P) {
     const int first = part.first, last = part.last, tok0 = part.tok0, all_see = b.len - P.q_tokens + 1;
 #pragma unroll 1
     for (int step = first; step < last; ++step) {
-      copies_wait<S - 1>();
-      __syncwarp();   // every lane's copies of this step have landed
+      copies_wait<S - 2>();
+      __syncwarp();   // every lane's copies of this step have landed, and the step before has been read
+      find();
+      copy_keys();
       const uint8_t* const at = ring + slot * kStageBytes;
       {
         // a lane a token: its four numbers for every lane
@@ -404,6 +414,7 @@ cache_attend4_kernel(const __grid_constant__ AttendParams P) {
             for (int e = 0; e < kHalves; ++e) mma_f16(s[k][e], a, q[e][2 * w + h][0], q[e][2 * w + h][1]);
           }
       }
+      copy_rest();
       __syncwarp();
       const int pos0 = tok0 + step * kStep;
       const uint32_t hole = gaps >> 2 * slot & 3u;
@@ -510,9 +521,9 @@ cache_attend4_kernel(const __grid_constant__ AttendParams P) {
 #pragma unroll
       for (int k = 0; k < 2; ++k) {
         uint32_t c0[4], c1[4];   // four codes of two tokens each
-        const uint32_t va = smem_u32(at) + kCodeBytes + 2 * k * (8 * kRowBytes) + vget;
-        load_transposed(c0, va);
-        load_transposed(c1, va + 8 * kRowBytes);
+        const uint32_t from = smem_u32(at) + kCodeBytes + 2 * k * (8 * kRowBytes) + vget;
+        load_transposed(c0, from);
+        load_transposed(c1, from + 8 * kRowBytes);
 #pragma unroll
         for (int i = 0; i < 4; ++i)
 #pragma unroll
@@ -523,20 +534,18 @@ cache_attend4_kernel(const __grid_constant__ AttendParams P) {
             for (int e = 0; e < kHalves; ++e) mma_f16(o[2 * i + h][e], a, w[2 * k][e], w[2 * k + 1][e]);
           }
       }
-      __syncwarp();   // the stage and the tokens' numbers have been read
-      if (step + 1 < last) {   // (the last stage of a part is where its sums are put together)
-        fetch();
-        slot = slot + 1 == S ? 0 : slot + 1;
-      }
+      slot = slot + 1 == S ? 0 : slot + 1;
     }
 
     // ---------------------------------------------------------- the end of a part: the warps' rows together, eight by eight
     const bool has = first < last, whole = x == b.first && part.end == b.first + b.tiles;
     float* const out = P.partial + (static_cast<int64_t>(blockIdx.x) * 2 + (x == b.first)) * kAttend4PartWords;
-    float* const mine = reinterpret_cast<float*>(ring + slot * kStageBytes);
+    // (in the stage of the last step, which the next one's copies will fill)
+    const int stage = slot == 0 ? S - 1 : slot - 1;
+    float* const mine = reinterpret_cast<float*>(ring + stage * kStageBytes);
     if (lane == 0) {
       ctl.has[warp] = has;
-      ctl.at[warp] = slot * kStageBytes;
+      ctl.at[warp] = stage * kStageBytes;
     }
     const int next_x = part.end;
 #pragma unroll
@@ -623,17 +632,12 @@ cache_attend4_kernel(const __grid_constant__ AttendParams P) {
       }
       __syncthreads();   // the sums have been read
     }
-    if (has) {
-      fetch();
-      slot = slot + 1 == S ? 0 : slot + 1;
-    }
     x = next_x;
     if (x < x1) {
       if (lane == 0) ctl.part[warp] = ctl.next[warp];
       __syncwarp();
     }
   }
-
   // sequences without a token: their rows are zeros
   for (int r = blockIdx.x * W + warp; r < P.n_seq; r += W * gridDim.x)
     if (seq_len(P, r) == 0)
@@ -646,7 +650,6 @@ cache_attend4_kernel(const __grid_constant__ AttendParams P) {
   // ------------------------------------------------------------ the join of blocks that several CTAs had parts of
   allow_next_kernel();
   if (splits == 0) return;
-  __threadfence();
   __syncthreads();   // every thread's part of the sums is out, and ctl.split is written
   constexpr int kRows = (R + W - 1) / W;
   for (int n = 0; n < splits; ++n) {
@@ -657,7 +660,6 @@ cache_attend4_kernel(const __grid_constant__ AttendParams P) {
       ctl.last[n] = inc_acq_rel_gpu(P.arrive + w0, static_cast<unsigned>(w1 - w0)) == static_cast<unsigned>(w1 - w0);
     __syncthreads();
     if (!ctl.last[n]) continue;
-    __threadfence();
     // A warp has the rows warp, warp + W, ...; where there are twice as many warps as rows or more, a row's parts are dealt
     // to several warps, whose sums the first of them adds in their order.
     const int parts = w1 - w0 + 1, there = min(R, rows - s.rb * R);
