@@ -498,57 +498,54 @@ __global__ void __launch_bounds__(kRowThreads<kPage>) cache_gather_kernel(const 
 // 7.3: 2000 teams of 8 runs, of which 1216 fit at once, are two rounds of that chain.
 constexpr int64_t kStoreBlockTokens = 1024;
 
-// The frequencies of the pairs that a lane's 8 elements belong to: 8 of them (partners are in another lane), or 4 side by
-// side.
+// The pairs that a lane turns: four side by side of its own elements, or where pairs are halves of the row, half of those that
+// it shares with its partner's lane. Then the two exchange the other halves, before and behind it, so that no turn is
+// computed twice in a row.
 struct LaneTurns {
-  uint32_t hi[8], lo[8];
-  int partner;   // the lane with the other elements of the pairs; -1: not turned
+  uint2 turn[4];
+  int partner;   // its lane; -1: nothing is turned
   bool second;   // this lane has the pairs' second elements
   __device__ __forceinline__ void set(const RotaryTable& r, int lane) {
     const int half = r.pairs >> 3;   // lanes with first elements (where partners are lanes apart)
-    const int from = r.interleaved ? lane : lane % half;
     second = !r.interleaved && lane >= half;
     partner = lane >= 2 * half ? -1 : r.interleaved ? lane : second ? lane - half : lane + half;
+    const int from = r.interleaved ? 4 * lane : second ? 8 * (lane - half) + 4 : 8 * lane;
 #pragma unroll
-    for (int i = 0; i < 8; ++i) {
-      const int j = min(r.interleaved ? 4 * from + i : 8 * from + i, kMaxPairs - 1);
-      hi[i] = r.hi[j];
-      lo[i] = r.lo[j];
-    }
+    for (int i = 0; i < 4; ++i) turn[i] = turn_at(r, min(from + i, kMaxPairs - 1));
   }
 };
 
 // Turns the rows x[i] of tokens token0 + i (those with row0 + i in 0 .. n - 1; 16 lanes have a row), rounded to bf16 as a
-// rotation by itself would leave them.
-__device__ __forceinline__ void turn_rows(uint4 (&x)[kGroupRows], const RotateParams& R, int64_t token0, int row0, int n,
+// rotation by itself would leave them. pos: in lane i, token i's position.
+__device__ __forceinline__ void turn_rows(uint4 (&x)[kGroupRows], const RotaryTable& r, int pos, int row0, int n,
                                           const LaneTurns& turn) {
   const uint32_t lanes = threadIdx.x & 16 ? 0xffff0000u : 0x0000ffffu;
 #pragma unroll
   for (int i = 0; i < kGroupRows; ++i) {
     if (static_cast<uint32_t>(row0 + i) >= static_cast<uint32_t>(n)) continue;   // (all 16 lanes)
-    const int pos = __ldg(R.positions + token0 + i);
-    uint32_t* w = &x[i].x;
-    if (R.r.interleaved) {
+    const int p = __shfl_sync(lanes, pos, i, 16);
+    float2 cs[4];
 #pragma unroll
-      for (int k = 0; k < 4; ++k) {
-        const float2 y = turned(bf16_low(w[k]), bf16_high(w[k]), turn_of(turn.hi[k], turn.lo[k], R.r.amplitude, pos));
-        if (turn.partner >= 0) w[k] = bf16_pair(y.x, y.y);
-      }
+    for (int k = 0; k < 4; ++k) cs[k] = turn_of(turn.turn[k], r.amplitude, p);
+    if (r.interleaved) {
+      if (turn.partner >= 0) turn_neighbours(x[i], cs);
       continue;
     }
-#pragma unroll
-    for (int k = 0; k < 4; ++k) {
-      const uint32_t other = __shfl_sync(lanes, w[k], turn.partner & 15, 16);
-      const uint32_t a = turn.second ? other : w[k], b = turn.second ? w[k] : other;
-      const float2 u = turned(bf16_low(a), bf16_low(b), turn_of(turn.hi[2 * k], turn.lo[2 * k], R.r.amplitude, pos));
-      const float2 v = turned(bf16_high(a), bf16_high(b), turn_of(turn.hi[2 * k + 1], turn.lo[2 * k + 1], R.r.amplitude, pos));
-      if (turn.partner >= 0) w[k] = turn.second ? bf16_pair(u.y, v.y) : bf16_pair(u.x, v.x);
-    }
+    // first elements a, second ones b: of 0 .. 3 in the first lane, of 4 .. 7 in the second
+    const int other = turn.partner & 15;
+    const uint32_t s0 = __shfl_sync(lanes, turn.second ? x[i].x : x[i].z, other, 16);
+    const uint32_t s1 = __shfl_sync(lanes, turn.second ? x[i].y : x[i].w, other, 16);
+    uint32_t a[2] = {turn.second ? s0 : x[i].x, turn.second ? s1 : x[i].y};
+    uint32_t b[2] = {turn.second ? x[i].z : s0, turn.second ? x[i].w : s1};
+    turn_halves(a, b, cs);
+    const uint32_t t0 = __shfl_sync(lanes, turn.second ? a[0] : b[0], other, 16);
+    const uint32_t t1 = __shfl_sync(lanes, turn.second ? a[1] : b[1], other, 16);
+    if (turn.partner >= 0) x[i] = turn.second ? make_uint4(t0, t1, b[0], b[1]) : make_uint4(a[0], a[1], t0, t1);
   }
 }
 
 template <int kPage, bool kTurn>
-__device__ __forceinline__ void store_tile(const CacheStoreParams& P, const RotateParams* R, int64_t tile) {
+__device__ __forceinline__ void store_tile(const CacheStoreParams& P, const RotateParams* R, uint32_t tile) {
   constexpr int kTeam = kTeamThreads<kPage>, kGroups = kPage / kGroupRows, kTeams = kRowThreads<kPage> / kTeam;
   constexpr int kWords = kPage / 16;   // of 32 tokens: a block of at most P and the run that leaves it
   __shared__ uint32_t team_max[kTeams][kGroups];
@@ -556,7 +553,7 @@ __device__ __forceinline__ void store_tile(const CacheStoreParams& P, const Rota
   __shared__ uint16_t runs[kRowThreads<kPage> / 32][kPage];   // first token << 8 | tokens: long, from the end short
   const int team = threadIdx.x / kTeam, lane = threadIdx.x & 15, g = (threadIdx.x / 16) % kGroups;
   const int warp = threadIdx.x >> 5, lane32 = threadIdx.x & 31;
-  const int64_t item = tile * kTeams + team;
+  const int64_t item = static_cast<int64_t>(tile) * kTeams + team;
   const int H = P.c.heads;
   const int64_t first = item / (2 * H) * P.block;
   if (first >= P.n_tokens) return;   // the whole team
@@ -637,6 +634,11 @@ __device__ __forceinline__ void store_tile(const CacheStoreParams& P, const Rota
     const int64_t block = static_cast<int64_t>(slot / kPage) * H + h;
     const int row0 = whole_team ? g * kGroupRows - off : 0;   // the run's row in x[0]
     uint4 x[kGroupRows];
+    int pos = 0;
+    if constexpr (kTurn) {
+      if (!values && static_cast<uint32_t>(row0 + lane) < static_cast<uint32_t>(n) && lane < kGroupRows)
+        pos = __ldg(R->positions + first + t + row0 + lane);
+    }
 #pragma unroll
     for (int i = 0; i < kGroupRows; ++i) {
       x[i] = make_uint4(0, 0, 0, 0);
@@ -644,7 +646,7 @@ __device__ __forceinline__ void store_tile(const CacheStoreParams& P, const Rota
         x[i] = __ldg(reinterpret_cast<const uint4*>(from + (first + t + row0 + i) * st) + lane);
     }
     if constexpr (kTurn) {
-      if (!values) turn_rows(x, *R, first + t + row0, row0, n, turn);
+      if (!values) turn_rows(x, R->r, pos, row0, n, turn);
     }
     if (whole_team) {
       write_run<kPage>(x, off, n, codes + block * (kPage * kHeadDim), scales + block, team_max[team]);
@@ -665,14 +667,14 @@ cache_store_kernel(const __grid_constant__ CacheStoreParams P) {
 
 // The rotating append: the first CTAs turn the queries, the others write the pages.
 template <int kPage>
-__global__ void __launch_bounds__(kRowThreads<kPage>, 768 / kRowThreads<kPage>)
+__global__ void __launch_bounds__(kRowThreads<kPage>, 640 / kRowThreads<kPage>)
 cache_append_kernel(const __grid_constant__ CacheAppendParams P, int64_t turn_tiles) {
   wait_previous_kernel();
   __shared__ __align__(16) float2 turns[kTurnTokens * kMaxPairs];
   if (blockIdx.x < turn_tiles)
     rotate_tile<kRowThreads<kPage>>(P.turn, blockIdx.x, turns);
   else
-    store_tile<kPage, true>(P.s, &P.turn, blockIdx.x - turn_tiles);
+    store_tile<kPage, true>(P.s, &P.turn, blockIdx.x - static_cast<uint32_t>(turn_tiles));
   allow_next_kernel();
 }
 

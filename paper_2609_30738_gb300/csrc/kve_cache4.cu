@@ -10,6 +10,7 @@
 //
 // Bound by HBM: 256 bytes read and 68 written a row. Eight lanes have a row, 16 elements (32 bytes) each; the minimum
 // and maximum are packed bf16 operations and three shuffles.
+#include "kve_ptx.cuh"
 #include "kve_rotary.cuh"
 
 namespace kve {
@@ -30,27 +31,28 @@ __device__ __forceinline__ uint32_t max2(uint32_t a, uint32_t b) {
   return d;
 }
 
-// d / unit to the nearest, ties to the even one, for 0 <= d / unit < 16. A quotient of two floats is never nearer than 2^-24
-// of itself to the middle between two integers without being there (unit has 8 bits, so d is no multiple of unit / 2
-// within 24 bits otherwise), and q below is within 2^-45 of it, exact where it is a float; so its rounding is the quotient's.
-__device__ __forceinline__ float code_of(float d, float unit, float inverse) {
-  const float q0 = d * inverse;
-  const float q = fmaf(fmaf(-q0, unit, d), inverse, q0);
-  return q + 12582912.f;   // 1.5 * 2^23: the integer in the low bits
-}
-
-// The codes of 8 elements, the first in the lowest four bits.
-__device__ __forceinline__ uint32_t codes_of(const uint4& x, float z16, float unit, float inverse) {
+// The codes of 8 elements, the first in the lowest four bits: (x - z) / s in 0 .. 15.06 (s is off by at most 2^-8) to the nearest,
+// ties to the even one. With inverse + rest = 1 / unit to 2^-47 of itself, q is the quotient rounded to fp32 as a division
+// rounds it: a quotient of a float by one of 8 bits is no nearer than 2^-33 of itself to the middle between two floats
+// without being a float.
+__device__ __forceinline__ uint32_t codes_of(const uint4& x, float z16, float inverse, float rest) {
   const uint32_t* w = &x.x;
-  uint32_t out = 0;
+  const float2 scale = make_float2(0.0625f, 0.0625f), z = make_float2(-z16, -z16);
+  const float2 hi = make_float2(inverse, inverse), lo = make_float2(rest, rest);
+  constexpr float kWhole = 12582912.f;   // 1.5 * 2^23: a sum with it has its integer in the low bits, 0x4b400000 above
+  uint32_t u[8];
 #pragma unroll
   for (int i = 0; i < 4; ++i) {
-    const float a = code_of(fmaf(bf16_low(w[i]), 0.0625f, -z16), unit, inverse);
-    const float b = code_of(fmaf(bf16_high(w[i]), 0.0625f, -z16), unit, inverse);
-    const uint32_t ia = min(__float_as_uint(a) & 31u, 15u), ib = min(__float_as_uint(b) & 31u, 15u);
-    out |= (ia | ib << 4) << (8 * i);
+    const float2 d = ffma2(make_float2(bf16_low(w[i]), bf16_high(w[i])), scale, z);
+    const float2 t = fadd2(ffma2(d, hi, fmul2(d, lo)), make_float2(kWhole, kWhole));
+    u[2 * i] = __float_as_uint(t.x);
+    u[2 * i + 1] = __float_as_uint(t.y);
   }
-  return out;
+  // sum of u_i 16^i, without 0x4b400000 * 0x11111111 (modulo 2^32)
+  uint32_t out = u[7];
+#pragma unroll
+  for (int i = 6; i >= 0; --i) out = out * 16u + u[i];
+  return out - 0x4b400000u * 0x11111111u;
 }
 
 // Writes a row that 8 lanes hold in the chunks ca and cb: its codes, and in lane l = 0 its s and z.
@@ -72,18 +74,9 @@ __device__ __forceinline__ void write_row4(const uint4& a, const uint4& b, int c
   if (bf16_low(s) < 7.52316384526264e-37f) s &= 0xffff0000u;   // 2^-120
   const float unit = bf16_low(s) * 0.0625f;
   const bool spread = finite && unit > 0.f;
-  const float inverse = spread ? __frcp_rn(unit) : 0.f;
-  uint32_t wa = 0, wb = 0;
-  if (spread) {
-    wa = codes_of(a, z16, unit, inverse);
-    wb = codes_of(b, z16, unit, inverse);
-  }
-  if (cb == ca + 1) {
-    reinterpret_cast<uint2*>(codes)[ca >> 1] = make_uint2(wa, wb);
-  } else {
-    reinterpret_cast<uint32_t*>(codes)[ca] = wa;
-    reinterpret_cast<uint32_t*>(codes)[cb] = wb;
-  }
+  const float inverse = spread ? __frcp_rn(unit) : 0.f, rest = fmaf(-unit, inverse, 1.f) * inverse;
+  reinterpret_cast<uint32_t*>(codes)[ca] = spread ? codes_of(a, z16, inverse, rest) : 0u;
+  reinterpret_cast<uint32_t*>(codes)[cb] = spread ? codes_of(b, z16, inverse, rest) : 0u;
   if (l == 0) *param = finite ? s : 0x7fc07fc0u;
 }
 
@@ -114,25 +107,12 @@ __global__ void __launch_bounds__(kRowThreads4) cache4_store_kernel(const __grid
   const int l = threadIdx.x & 7, group = threadIdx.x >> 3;
   const int tok = group % tile_tokens, step = kGroups4 / tile_tokens;
   const int slot = tok < tokens ? __ldg(P.slots + token0 + tok) : -1;
-  if constexpr (kTurn) {
-    if (head0 < H) turns_to_shared(turns, A.turn.r, A.turn.positions, token0, tokens, false);
-  }
-  const int limit = P.c.num_pages << P.c.page_shift;   // (below 2^31)
-  if (slot >= limit && l == 0 && group / tile_tokens == 0) atomicOr(P.err, kErrCheck);
-  if (slot < 0 || slot >= limit) return;
-  const int page = slot >> P.c.page_shift, off = slot & (P.c.page - 1);
-  const int64_t row0 = (static_cast<int64_t>(page) * H << P.c.page_shift) + off;
-  const uint32_t lanes = row_lanes();
-  RowChunks kc = {2 * l, 2 * l + 1, false};
-  float2 cs[8];
-  if constexpr (kTurn) {
-    kc = row_chunks(A.turn.r, l);
-    if (kc.turns && head0 < H) lane_turns(cs, turns + tok * kMaxPairs, l);
-  }
-  const int end = min(head0 + tile_heads, all);
-  constexpr int kInFlight = 2;
-  for (int h = head0 + group / tile_tokens; h < end; h += kInFlight * step) {
-    uint4 a[kInFlight], b[kInFlight];
+  RowChunks kc = {l, l + 8, false, false};
+  if constexpr (kTurn) kc = row_chunks(A.turn.r, l);
+  const int end = tok < tokens ? min(head0 + tile_heads, all) : 0;
+  constexpr int kInFlight = 4;
+  uint4 a[kInFlight], b[kInFlight];
+  const auto load = [&](int h) {
 #pragma unroll
     for (int i = 0; i < kInFlight; ++i) {
       const int hh = h + i * step;
@@ -140,10 +120,27 @@ __global__ void __launch_bounds__(kRowThreads4) cache4_store_kernel(const __grid
         const uint16_t* from = hh < H ? P.k + (token0 + tok) * P.k_st + hh * P.k_sh
                                       : P.v + (token0 + tok) * P.v_st + (hh - H) * P.v_sh;
         const uint4* v = reinterpret_cast<const uint4*>(from);
-        a[i] = v[hh < H ? kc.a : 2 * l];
-        b[i] = v[hh < H ? kc.b : 2 * l + 1];
+        a[i] = v[hh < H ? kc.a : l];
+        b[i] = v[hh < H ? kc.b : l + 8];
       }
     }
+  };
+  int h = head0 + group / tile_tokens;
+  load(h);
+  float2 cs[8];
+  if constexpr (kTurn) {
+    if (head0 < H) {
+      turns_to_shared<kRowThreads4>(turns, A.turn.r, A.turn.positions, token0, tokens, false);
+      if (tok < tokens && kc.turns_a) lane_turns(cs, turns + tok * kMaxPairs, A.turn.r, kc);
+    }
+  }
+  const int limit = P.c.num_pages << P.c.page_shift;   // (below 2^31)
+  if (slot >= limit && l == 0 && group / tile_tokens == 0) atomicOr(P.err, kErrCheck);
+  if (slot < 0 || slot >= limit) return;
+  const int page = slot >> P.c.page_shift, off = slot & (P.c.page - 1);
+  const int64_t row0 = (static_cast<int64_t>(page) * H << P.c.page_shift) + off;
+  const uint32_t lanes = row_lanes();
+  for (; h < end; h += kInFlight * step, load(h)) {
 #pragma unroll
     for (int i = 0; i < kInFlight; ++i) {
       const int hh = h + i * step;
@@ -151,9 +148,9 @@ __global__ void __launch_bounds__(kRowThreads4) cache4_store_kernel(const __grid
       const bool key = hh < H;
       const int64_t row = row0 + (static_cast<int64_t>(key ? hh : hh - H) << P.c.page_shift);
       if constexpr (kTurn) {
-        if (key && kc.turns) turn_chunks(a[i], b[i], cs, A.turn.r.interleaved);
+        if (key) turn_chunks(a[i], b[i], cs, kc, A.turn.r.interleaved);
       }
-      write_row4(a[i], b[i], key ? kc.a : 2 * l, key ? kc.b : 2 * l + 1, (key ? P.c.k : P.c.v) + row * kRowCodes,
+      write_row4(a[i], b[i], key ? kc.a : l, key ? kc.b : l + 8, (key ? P.c.k : P.c.v) + row * kRowCodes,
                  (key ? P.c.k_param : P.c.v_param) + row, l, lanes);
     }
   }
@@ -192,12 +189,12 @@ __global__ void __launch_bounds__(kRowThreads4) cache4_gather_kernel(const __gri
   for (int i = 0; i < kGatherRows; ++i) {
     k[i][0] = k[i][1] = v[i][0] = v[i][1] = make_uint4(0, 0, 0, 0);
     if (first + i * kGroups4 >= n || outside[i]) continue;
-    const uint4* ks = reinterpret_cast<const uint4*>(P.g.k + u.k_off + src[i] * P.g.g.k_st) + 2 * l;
-    const uint4* vs = reinterpret_cast<const uint4*>(P.g.v + u.v_off + src[i] * P.g.g.v_st) + 2 * l;
+    const uint4* ks = reinterpret_cast<const uint4*>(P.g.k + u.k_off + src[i] * P.g.g.k_st) + l;
+    const uint4* vs = reinterpret_cast<const uint4*>(P.g.v + u.v_off + src[i] * P.g.g.v_st) + l;
     k[i][0] = __ldg(ks);
-    k[i][1] = __ldg(ks + 1);
+    k[i][1] = __ldg(ks + 8);
     v[i][0] = __ldg(vs);
-    v[i][1] = __ldg(vs + 1);
+    v[i][1] = __ldg(vs + 8);
   }
 #pragma unroll
   for (int i = 0; i < kGatherRows; ++i) {
@@ -207,8 +204,8 @@ __global__ void __launch_bounds__(kRowThreads4) cache4_gather_kernel(const __gri
     if ((outside[i] || !good) && l == 0) atomicOr(P.err, kErrCheck);
     if (!good) continue;
     const int64_t at = ((static_cast<int64_t>(page[i]) * P.c.heads + u.h) << P.c.page_shift) + (row & (P.c.page - 1));
-    write_row4(k[i][0], k[i][1], 2 * l, 2 * l + 1, P.c.k + at * kRowCodes, P.c.k_param + at, l, lanes);
-    write_row4(v[i][0], v[i][1], 2 * l, 2 * l + 1, P.c.v + at * kRowCodes, P.c.v_param + at, l, lanes);
+    write_row4(k[i][0], k[i][1], l, l + 8, P.c.k + at * kRowCodes, P.c.k_param + at, l, lanes);
+    write_row4(v[i][0], v[i][1], l, l + 8, P.c.v + at * kRowCodes, P.c.v_param + at, l, lanes);
   }
   allow_next_kernel();
 }

@@ -233,11 +233,12 @@ struct GatherParams {
   uint16_t* v_out;
 };
 
-// Rotary positions: pair j turns by f_j radians a position. hi and lo are f_j / (2 pi) without its whole turns, in units
-// of 2^-64: position times that, modulo 2^64, is the angle of any 32-bit position without a rounding.
+// Rotary positions: pair j turns by f_j radians a position. turns[j] is f_j / (2 pi) without its whole turns, in units
+// of 2^-64 (x the low, y the high word): position times that, modulo 2^64, is the angle of any 32-bit position without a
+// rounding.
 constexpr int kMaxPairs = kHeadDim / 2;
 struct RotaryTable {
-  uint32_t hi[kMaxPairs], lo[kMaxPairs];
+  uint2 turns[kMaxPairs];
   float amplitude;
   int32_t pairs;         // rotary_dim / 2, a multiple of 8
   int32_t interleaved;   // pairs (2j, 2j + 1), or (j, j + pairs)

@@ -85,8 +85,8 @@ kve_status kv_evict_rotary_create(int32_t head_dim, int32_t rotary_dim, int32_t 
     const double part = turns - std::floor(turns);   // [0, 1]
     const double high = std::floor(part * 4294967296.0);
     const double low = std::floor((part * 4294967296.0 - high) * 4294967296.0);
-    h->table.hi[j] = static_cast<uint32_t>(static_cast<uint64_t>(high));   // (a whole turn is none)
-    h->table.lo[j] = static_cast<uint32_t>(static_cast<uint64_t>(low));
+    h->table.turns[j].y = static_cast<uint32_t>(static_cast<uint64_t>(high));   // (a whole turn is none)
+    h->table.turns[j].x = static_cast<uint32_t>(static_cast<uint64_t>(low));
   }
   h->table.amplitude = static_cast<float>(amplitude);
   h->table.pairs = rotary_dim / 2;

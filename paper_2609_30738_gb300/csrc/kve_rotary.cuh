@@ -5,16 +5,31 @@
 
 namespace kve {
 
-// {cos, sin} times the amplitude of the angle that pair j has at position pos. The angle is a fraction of a turn in 64-bit
-// integers (exact for every position, where an fp32 product is off by 2^-24 of the whole angle); its upper 32 bits
-// leave 1.5e-9 radians, and the approximate functions on [-pi, pi] an absolute 2^-20: 2^-11 of the bf16 rounding of what they
-// turn.
-__device__ __forceinline__ float2 turn_of(uint32_t hi, uint32_t lo, float amplitude, int pos) {
+// turns[j] of a kernel parameter. The lanes ask for different j, which a read of the constant bank would serve one after the
+// other: read as ordinary memory.
+__device__ __forceinline__ uint2 turn_at(const RotaryTable& r, int j) {
+  uint2 v;
+  asm("ld.v2.u32 {%0, %1}, [%2];" : "=r"(v.x), "=r"(v.y) : "l"(r.turns + j));
+  return v;
+}
+
+// {cos, sin} times the amplitude of the angle that a pair has at position pos. The angle is a fraction of a turn in 64-bit
+// integers (exact for every position, where an fp32 product is off by 2^-24 of the whole angle); its upper 32 bits are cut into
+// the nearest quarter turn and a rest x of at most pi / 4, whose sine and cosine are their Taylor polynomials up to x^9 and
+// x^8 (2^-29 and 2^-25 off at pi / 4): 2^-23 with the roundings.
+__device__ __forceinline__ float2 turn_of(uint2 turn, float amplitude, int pos) {
   const uint32_t p = static_cast<uint32_t>(pos);
-  uint32_t u = p * hi + __umulhi(p, lo);
-  if (pos < 0) u -= lo;   // (p is 2^32 too large)
-  const float x = static_cast<float>(static_cast<int32_t>(u)) * 1.46291807926715968e-9f;   // pi 2^-31
-  return make_float2(__cosf(x) * amplitude, __sinf(x) * amplitude);
+  uint32_t u = p * turn.y + __umulhi(p, turn.x);
+  if (pos < 0) u -= turn.x;   // (p is 2^32 too large)
+  const uint32_t quarter = u + 0x20000000u;   // (the quarter in its two upper bits)
+  const float x = static_cast<float>(static_cast<int32_t>(u - (quarter & 0xc0000000u))) * 1.46291807926715968e-9f;   // pi 2^-31
+  const float y = x * x;
+  const float s = fmaf(x * y, fmaf(y, fmaf(y, fmaf(y, 2.75573192e-6f, -1.98412698e-4f), 8.33333333e-3f), -1.66666667e-1f), x);
+  const float c = fmaf(y, fmaf(y, fmaf(y, fmaf(y, 2.48015873e-5f, -1.38888889e-3f), 4.16666667e-2f), -0.5f), 1.f);
+  const bool odd = quarter & 0x40000000u;
+  const uint32_t sign_s = quarter & 0x80000000u, sign_c = (quarter + 0x40000000u) & 0x80000000u;
+  return make_float2(__uint_as_float(__float_as_uint(odd ? s : c) ^ sign_c) * amplitude,
+                     __uint_as_float(__float_as_uint(odd ? c : s) ^ sign_s) * amplitude);
 }
 
 // (a, b) turned: (a c - b s, b c + a s), each rounded once behind its second product.
@@ -30,60 +45,77 @@ __device__ __forceinline__ uint32_t bf16_pair(float lo, float hi) {
 __device__ __forceinline__ float bf16_low(uint32_t x) { return __uint_as_float(x << 16); }
 __device__ __forceinline__ float bf16_high(uint32_t x) { return __uint_as_float(x & 0xffff0000u); }
 
-// 16 elements of a row, 8 pairs: a and b are 8 elements and their partners, or 16 elements whose neighbours are partners.
-__device__ __forceinline__ void turn_chunks(uint4& a, uint4& b, const float2 (&cs)[8], bool interleaved) {
-  uint32_t* x = &a.x;
-  uint32_t* y = &b.x;
-  if (interleaved) {
+// Four pairs, (a_i, b_i) by halves of x and y, or neighbours in x and y, with the turns cs[0 .. 3].
+__device__ __forceinline__ void turn_halves(uint32_t (&x)[2], uint32_t (&y)[2], const float2* cs) {
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      const float2 u = turned(bf16_low(x[i]), bf16_high(x[i]), cs[i]), v = turned(bf16_low(y[i]), bf16_high(y[i]), cs[4 + i]);
-      x[i] = bf16_pair(u.x, u.y);
-      y[i] = bf16_pair(v.x, v.y);
-    }
-  } else {
+  for (int i = 0; i < 2; ++i) {
+    const float2 u = turned(bf16_low(x[i]), bf16_low(y[i]), cs[2 * i]);
+    const float2 v = turned(bf16_high(x[i]), bf16_high(y[i]), cs[2 * i + 1]);
+    x[i] = bf16_pair(u.x, v.x);
+    y[i] = bf16_pair(u.y, v.y);
+  }
+}
+__device__ __forceinline__ void turn_neighbours(uint4& x, const float2* cs) {
+  uint32_t* w = &x.x;
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      const float2 u = turned(bf16_low(x[i]), bf16_low(y[i]), cs[2 * i]);
-      const float2 v = turned(bf16_high(x[i]), bf16_high(y[i]), cs[2 * i + 1]);
-      x[i] = bf16_pair(u.x, v.x);
-      y[i] = bf16_pair(u.y, v.y);
-    }
+  for (int i = 0; i < 4; ++i) {
+    const float2 u = turned(bf16_low(w[i]), bf16_high(w[i]), cs[i]);
+    w[i] = bf16_pair(u.x, u.y);
   }
 }
 
-// Which 8-element chunks lane l of the 8 that share a row has, and whether they are turned.
+// Which 8-element chunks lane l of the 8 that share a row has, and which of them are turned. Chunks of the 8 lanes stand side by
+// side (128 bytes of the row at once), but for parts of a row that turn by halves.
 struct RowChunks {
   int a, b;
-  bool turns;
+  bool turns_a, turns_b;
 };
 __device__ __forceinline__ RowChunks row_chunks(const RotaryTable& r, int l) {
-  const int half = r.pairs >> 3;   // lanes that turn: 8 pairs each
-  if (l >= half || r.interleaved) return {2 * l, 2 * l + 1, l < half};
-  return {l, l + half, true};
+  const int half = r.pairs >> 3;   // chunks of first elements
+  if (r.interleaved) return {l, l + 8, l < 2 * half, l + 8 < 2 * half};
+  return l < half ? RowChunks{l, l + half, true, true} : RowChunks{l + half, l + 8, false, false};
+}
+
+// The turns of those chunks: of the pairs of both, or of each one's.
+__device__ __forceinline__ void lane_turns(float2 (&cs)[8], const float2* token_turns, const RotaryTable& r, const RowChunks& c) {
+  const int j0 = r.interleaved ? 4 * c.a : 8 * c.a, j1 = r.interleaved ? 4 * c.b : j0 + 4;
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    const float4 v = reinterpret_cast<const float4*>(token_turns + (i < 2 ? j0 : j1))[i & 1];
+    cs[2 * i] = make_float2(v.x, v.y);
+    cs[2 * i + 1] = make_float2(v.z, v.w);
+  }
+}
+
+__device__ __forceinline__ void turn_chunks(uint4& a, uint4& b, const float2 (&cs)[8], const RowChunks& c, bool interleaved) {
+  if (interleaved) {
+    if (c.turns_a) turn_neighbours(a, cs);
+    if (c.turns_b) turn_neighbours(b, cs + 4);
+  } else if (c.turns_a) {
+    uint32_t x0[2] = {a.x, a.y}, x1[2] = {a.z, a.w}, y0[2] = {b.x, b.y}, y1[2] = {b.z, b.w};
+    turn_halves(x0, y0, cs);
+    turn_halves(x1, y1, cs + 4);
+    a = make_uint4(x0[0], x0[1], x1[0], x1[1]);
+    b = make_uint4(y0[0], y0[1], y1[0], y1[1]);
+  }
 }
 
 // The turns of `tokens` tokens from `token0` on into shared memory, [tokens][kMaxPairs]; every thread comes here and meets
 // the others behind it.
+template <int kThreads>
 __device__ __forceinline__ void turns_to_shared(float2* to, const RotaryTable& r, const int32_t* positions, int64_t token0,
                                                 int tokens, bool transpose) {
-  for (int i = threadIdx.x; i < tokens * kMaxPairs; i += blockDim.x) {
-    const int j = i % kMaxPairs;
-    if (j >= r.pairs) continue;
-    float2 cs = turn_of(r.hi[j], r.lo[j], r.amplitude, __ldg(positions + token0 + i / kMaxPairs));
-    if (transpose) cs.y = -cs.y;
-    to[i] = cs;
+  static_assert(kThreads % kMaxPairs == 0, "a thread has one pair");
+  const int j = threadIdx.x % kMaxPairs;
+  if (j < r.pairs) {
+    const uint2 turn = turn_at(r, j);
+    for (int i = threadIdx.x / kMaxPairs; i < tokens; i += kThreads / kMaxPairs) {
+      float2 cs = turn_of(turn, r.amplitude, __ldg(positions + token0 + i));
+      if (transpose) cs.y = -cs.y;
+      to[i * kMaxPairs + j] = cs;
+    }
   }
   __syncthreads();
-}
-
-__device__ __forceinline__ void lane_turns(float2 (&cs)[8], const float2* token_turns, int l) {
-#pragma unroll
-  for (int i = 0; i < 4; ++i) {
-    const float4 v = reinterpret_cast<const float4*>(token_turns + 8 * l)[i];
-    cs[2 * i] = make_float2(v.x, v.y);
-    cs[2 * i + 1] = make_float2(v.z, v.w);
-  }
 }
 
 // One CTA's tile of rows: 8 lanes a row, 32 bytes a lane; a lane keeps the turns of its token and goes through heads, four
@@ -96,34 +128,43 @@ __device__ __forceinline__ void rotate_tile(const RotateParams& P, int64_t tile,
   const int64_t token0 = tile / head_tiles * P.tile_tokens;
   const int head0 = static_cast<int>(tile % head_tiles) * P.tile_heads;
   const int tokens = static_cast<int>(P.n_tokens - token0 < P.tile_tokens ? P.n_tokens - token0 : P.tile_tokens);
-  turns_to_shared(turns, P.r, P.positions, token0, tokens, P.transpose);
   const int l = threadIdx.x & 7, group = threadIdx.x >> 3;
   const int tok = group % P.tile_tokens, step = kGroups / P.tile_tokens;
-  if (tok >= tokens) return;
   const RowChunks c = row_chunks(P.r, l);
-  if (!c.turns && P.out == P.x) return;
-  float2 cs[8];
-  if (c.turns) lane_turns(cs, turns + tok * kMaxPairs, l);
+  const bool in_place = P.out == P.x;
+  // what stays as it is needs no copy in place
+  const bool on_a = c.turns_a || !in_place, on_b = c.turns_b || !in_place;
   const uint16_t* x = P.x + (token0 + tok) * P.x_st;
   uint16_t* out = P.out + (token0 + tok) * P.o_st;
-  const int end = min(head0 + P.tile_heads, P.heads);
-  for (int h = head0 + group / P.tile_tokens; h < end; h += kInFlight * step) {
-    uint4 a[kInFlight], b[kInFlight];
+  const int end = tok < tokens ? min(head0 + P.tile_heads, P.heads) : 0;
+  uint4 a[kInFlight], b[kInFlight];
+  const auto load = [&](int h) {
 #pragma unroll
     for (int i = 0; i < kInFlight; ++i)
       if (h + i * step < end) {
         const uint4* from = reinterpret_cast<const uint4*>(x + (h + i * step) * P.x_sh);
-        a[i] = from[c.a];
-        b[i] = from[c.b];
+        if (on_a) a[i] = from[c.a];
+        if (on_b) b[i] = from[c.b];
       }
+  };
+  int h = head0 + group / P.tile_tokens;
+  load(h);   // (on their way while the turns are computed)
+  turns_to_shared<kThreads>(turns, P.r, P.positions, token0, tokens, P.transpose);
+  if (h >= end) return;
+  float2 cs[8];
+  if (c.turns_a) lane_turns(cs, turns + tok * kMaxPairs, P.r, c);
+  for (;;) {
 #pragma unroll
     for (int i = 0; i < kInFlight; ++i)
       if (h + i * step < end) {
-        if (c.turns) turn_chunks(a[i], b[i], cs, P.r.interleaved);
+        turn_chunks(a[i], b[i], cs, c, P.r.interleaved);
         uint4* to = reinterpret_cast<uint4*>(out + (h + i * step) * P.o_sh);
-        to[c.a] = a[i];
-        to[c.b] = b[i];
+        if (on_a) to[c.a] = a[i];
+        if (on_b) to[c.b] = b[i];
       }
+    h += kInFlight * step;
+    if (h >= end) return;
+    load(h);
   }
 }
 
