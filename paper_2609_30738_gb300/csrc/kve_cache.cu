@@ -10,6 +10,7 @@
 #include <cmath>
 #include <cstring>
 #include <new>
+#include <type_traits>
 
 #include "kve_internal.h"
 #include "kve_ptx.cuh"
@@ -498,6 +499,13 @@ __global__ void __launch_bounds__(kRowThreads<kPage>) cache_gather_kernel(const 
 // 7.3: 2000 teams of 8 runs, of which 1216 fit at once, are two rounds of that chain.
 constexpr int64_t kStoreBlockTokens = 1024;
 
+#ifndef KST
+#define KST 768
+#endif
+// Threads an SM: the rotating append's have the turns of their rows beside the rows.
+template <class Params>
+constexpr int kStoreThreads = std::is_same_v<Params, CacheAppendParams> ? KST : 1024;
+
 // The pairs that a lane turns: four side by side of its own elements, or where pairs are halves of the row, half of those that
 // it shares with its partner's lane. Then the two exchange the other halves, before and behind it, so that no turn is
 // computed twice in a row.
@@ -544,8 +552,30 @@ __device__ __forceinline__ void turn_rows(uint4 (&x)[kGroupRows], const RotaryTa
   }
 }
 
-template <int kPage, bool kTurn>
-__device__ __forceinline__ void store_tile(const CacheStoreParams& P, const RotateParams* R, uint32_t tile) {
+//
+// With parameters of the rotating append the first CTAs (turn_tiles) turn the queries, and the others turn the keys on their
+// way. (One body with the plain store as a kernel of its own: as a function of both it spilled three times as much.)
+template <int kPage, class Params>
+__global__ void __launch_bounds__(kRowThreads<kPage>, kStoreThreads<Params> / kRowThreads<kPage>)
+cache_store_kernel(const __grid_constant__ Params A, uint32_t turn_tiles) {
+  constexpr bool kTurn = std::is_same_v<Params, CacheAppendParams>;
+  wait_previous_kernel();
+  uint32_t tile = blockIdx.x;
+  if constexpr (kTurn) {
+    __shared__ __align__(16) float2 turns[kTurnTokens * kMaxPairs];
+    if (tile < turn_tiles) {
+      rotate_tile<kRowThreads<kPage>>(A.turn, tile, turns);
+      allow_next_kernel();
+      return;
+    }
+    tile -= turn_tiles;
+  }
+  const CacheStoreParams& P = [&]() -> const CacheStoreParams& {
+    if constexpr (kTurn)
+      return A.s;
+    else
+      return A;
+  }();
   constexpr int kTeam = kTeamThreads<kPage>, kGroups = kPage / kGroupRows, kTeams = kRowThreads<kPage> / kTeam;
   constexpr int kWords = kPage / 16;   // of 32 tokens: a block of at most P and the run that leaves it
   __shared__ uint32_t team_max[kTeams][kGroups];
@@ -567,7 +597,7 @@ __device__ __forceinline__ void store_tile(const CacheStoreParams& P, const Rota
   const int64_t left = P.n_tokens - first;
   LaneTurns turn;
   if constexpr (kTurn) {
-    if (!values) turn.set(R->r, lane);
+    if (!values) turn.set(A.turn.r, lane);
   }
   // the slots of the block and of what a run can reach behind it
   int longs = 0, shorts = 0;
@@ -637,7 +667,7 @@ __device__ __forceinline__ void store_tile(const CacheStoreParams& P, const Rota
     int pos = 0;
     if constexpr (kTurn) {
       if (!values && static_cast<uint32_t>(row0 + lane) < static_cast<uint32_t>(n) && lane < kGroupRows)
-        pos = __ldg(R->positions + first + t + row0 + lane);
+        pos = __ldg(A.turn.positions + first + t + row0 + lane);
     }
 #pragma unroll
     for (int i = 0; i < kGroupRows; ++i) {
@@ -646,7 +676,7 @@ __device__ __forceinline__ void store_tile(const CacheStoreParams& P, const Rota
         x[i] = __ldg(reinterpret_cast<const uint4*>(from + (first + t + row0 + i) * st) + lane);
     }
     if constexpr (kTurn) {
-      if (!values) turn_rows(x, R->r, pos, row0, n, turn);
+      if (!values) turn_rows(x, A.turn.r, pos, row0, n, turn);
     }
     if (whole_team) {
       write_run<kPage>(x, off, n, codes + block * (kPage * kHeadDim), scales + block, team_max[team]);
@@ -655,26 +685,6 @@ __device__ __forceinline__ void store_tile(const CacheStoreParams& P, const Rota
       write_short_run(x, off, n, codes + block * (kPage * kHeadDim), scales + block);
     }
   }
-}
-
-template <int kPage>
-__global__ void __launch_bounds__(kRowThreads<kPage>, 1024 / kRowThreads<kPage>)
-cache_store_kernel(const __grid_constant__ CacheStoreParams P) {
-  wait_previous_kernel();
-  store_tile<kPage, false>(P, nullptr, blockIdx.x);
-  allow_next_kernel();
-}
-
-// The rotating append: the first CTAs turn the queries, the others write the pages.
-template <int kPage>
-__global__ void __launch_bounds__(kRowThreads<kPage>, 640 / kRowThreads<kPage>)
-cache_append_kernel(const __grid_constant__ CacheAppendParams P, int64_t turn_tiles) {
-  wait_previous_kernel();
-  __shared__ __align__(16) float2 turns[kTurnTokens * kMaxPairs];
-  if (blockIdx.x < turn_tiles)
-    rotate_tile<kRowThreads<kPage>>(P.turn, blockIdx.x, turns);
-  else
-    store_tile<kPage, true>(P.s, &P.turn, blockIdx.x - static_cast<uint32_t>(turn_tiles));
   allow_next_kernel();
 }
 
@@ -687,16 +697,16 @@ int64_t store_ctas(const CacheStoreParams& p) {
 
 template <int kPage>
 cudaError_t store_paged(const CacheStoreParams& p, cudaStream_t stream) {
-  return launch_after_previous(cache_store_kernel<kPage>, dim3(static_cast<unsigned>(store_ctas<kPage>(p))),
-                               dim3(kRowThreads<kPage>), 0, stream, p);
+  return launch_after_previous(cache_store_kernel<kPage, CacheStoreParams>, dim3(static_cast<unsigned>(store_ctas<kPage>(p))),
+                               dim3(kRowThreads<kPage>), 0, stream, p, 0u);
 }
 
 template <int kPage>
 cudaError_t append_paged(const CacheAppendParams& params, cudaStream_t stream) {
   CacheAppendParams p = params;
   const int64_t turn_tiles = p.turn.heads > 0 ? cut_rotate<kRowThreads<kPage>>(p.turn) : 0;
-  return launch_after_previous(cache_append_kernel<kPage>, dim3(static_cast<unsigned>(turn_tiles + store_ctas<kPage>(p.s))),
-                               dim3(kRowThreads<kPage>), 0, stream, p, turn_tiles);
+  return launch_after_previous(cache_store_kernel<kPage, CacheAppendParams>, dim3(static_cast<unsigned>(turn_tiles + store_ctas<kPage>(p.s))),
+                               dim3(kRowThreads<kPage>), 0, stream, p, static_cast<uint32_t>(turn_tiles));
 }
 
 template <int kPage>

@@ -19,6 +19,7 @@ namespace {
 constexpr int kRowThreads4 = 256;
 constexpr int kGroups4 = kRowThreads4 / 8;
 constexpr int kRowCodes = kHeadDim / 2;   // bytes
+constexpr int kStoreTokens = kGroups4;    // most tokens of a tile
 
 __device__ __forceinline__ uint32_t min2(uint32_t a, uint32_t b) {
   uint32_t d;
@@ -32,7 +33,7 @@ __device__ __forceinline__ uint32_t max2(uint32_t a, uint32_t b) {
 }
 
 // The codes of 8 elements, the first in the lowest four bits: (x - z) / s in 0 .. 15.06 (s is off by at most 2^-8) to the nearest,
-// ties to the even one. With inverse + rest = 1 / unit to 2^-47 of itself, q is the quotient rounded to fp32 as a division
+// ties to the even one. With inverse + rest = 1 / unit to 2^-44 of itself, q is the quotient rounded to fp32 as a division
 // rounds it: a quotient of a float by one of 8 bits is no nearer than 2^-33 of itself to the middle between two floats
 // without being a float.
 __device__ __forceinline__ uint32_t codes_of(const uint4& x, float z16, float inverse, float rest) {
@@ -55,42 +56,41 @@ __device__ __forceinline__ uint32_t codes_of(const uint4& x, float z16, float in
   return out - 0x4b400000u * 0x11111111u;
 }
 
-// Writes a row that 8 lanes hold in the chunks ca and cb: its codes, and in lane l = 0 its s and z.
+// Writes row `row` that 8 lanes hold in the chunks ca and cb: its codes, and in lane l = 0 its s and z.
 __device__ __forceinline__ void write_row4(const uint4& a, const uint4& b, int ca, int cb, uint8_t* codes, uint32_t* param,
-                                           int l, uint32_t lanes) {
-  uint32_t lo = min2(min2(min2(a.x, a.y), min2(a.z, a.w)), min2(min2(b.x, b.y), min2(b.z, b.w)));
-  uint32_t hi = max2(max2(max2(a.x, a.y), max2(a.z, a.w)), max2(max2(b.x, b.y), max2(b.z, b.w)));
+                                           int row, int l, uint32_t lanes) {
+  const uint32_t lo = min2(min2(min2(a.x, a.y), min2(a.z, a.w)), min2(min2(b.x, b.y), min2(b.z, b.w))) ^ 0x80008000u;
+  const uint32_t hi = max2(max2(max2(a.x, a.y), max2(a.z, a.w)), max2(max2(b.x, b.y), max2(b.z, b.w)));
+  // the largest in the low half, minus the least in the high half
+  uint32_t ends = max2(__byte_perm(hi, lo, 0x5410), __byte_perm(hi, lo, 0x7632));
 #pragma unroll
-  for (int o = 4; o > 0; o >>= 1) {
-    lo = min2(lo, __shfl_xor_sync(lanes, lo, o));
-    hi = max2(hi, __shfl_xor_sync(lanes, hi, o));
-  }
-  lo = min2(lo, lo >> 16 | lo << 16);
-  hi = max2(hi, hi >> 16 | hi << 16);
-  const bool finite = (lo & 0x7f80u) != 0x7f80u && (hi & 0x7f80u) != 0x7f80u;
+  for (int o = 4; o > 0; o >>= 1) ends = max2(ends, __shfl_xor_sync(lanes, ends, o));
+  const bool finite = (ends & 0x7f80u) != 0x7f80u && (ends & 0x7f800000u) != 0x7f800000u;
   // in units of 16, so that no difference overflows
-  const float z = bf16_low(lo) + 0.f, z16 = z * 0.0625f, top16 = bf16_low(hi) * 0.0625f;
-  uint32_t s = bf16_pair((top16 - z16) * 1.0666666667f, z);   // 16 / 15
-  if (bf16_low(s) < 7.52316384526264e-37f) s &= 0xffff0000u;   // 2^-120
+  const float less = bf16_high(ends), z16 = less * -0.0625f;
+  const float spread16 = fmaf(bf16_low(ends), 0.0625f, -z16);
+  uint32_t s = bf16_pair(spread16 * 1.0666666667f, 0.f - less);   // 16 / 15
+  if (bf16_low(s) < 7.52316384526264e-37f) s &= 0xffff0000u;      // 2^-120
   const float unit = bf16_low(s) * 0.0625f;
   const bool spread = finite && unit > 0.f;
-  const float inverse = spread ? __frcp_rn(unit) : 0.f, rest = fmaf(-unit, inverse, 1.f) * inverse;
-  reinterpret_cast<uint32_t*>(codes)[ca] = spread ? codes_of(a, z16, inverse, rest) : 0u;
-  reinterpret_cast<uint32_t*>(codes)[cb] = spread ? codes_of(b, z16, inverse, rest) : 0u;
-  if (l == 0) *param = finite ? s : 0x7fc07fc0u;
+  const float inverse = rcp(unit), rest = fmaf(-unit, inverse, 1.f) * inverse;
+  uint32_t* const to = reinterpret_cast<uint32_t*>(codes + static_cast<int64_t>(row) * kRowCodes);
+  to[ca] = spread ? codes_of(a, z16, inverse, rest) : 0u;
+  to[cb] = spread ? codes_of(b, z16, inverse, rest) : 0u;
+  if (l == 0) param[row] = finite ? s : 0x7fc07fc0u;
 }
 
 __device__ __forceinline__ uint32_t row_lanes() { return 0xffu << (threadIdx.x & 24); }
 
-// New tokens by slot, [tokens][2 H] rows (keys, then values) cut like a rotation's: a tile is up to 8 tokens by some
-// heads. With kTurn the first tiles turn the queries, and keys are turned (and rounded to bf16) before they are coded.
+// New tokens by slot. A tile is up to kStoreTokens tokens by some heads of keys or of values (the two alternate). With kTurn
+// the first tiles turn the queries, and keys are turned (and rounded to bf16) before they are coded.
 template <bool kTurn>
 __global__ void __launch_bounds__(kRowThreads4) cache4_store_kernel(const __grid_constant__ CacheAppendParams A, int tile_tokens,
-                                                                    int tile_heads, int64_t turn_tiles) {
+                                                                    int tile_heads, uint32_t turn_tiles) {
   wait_previous_kernel();
-  __shared__ __align__(16) float2 turns[kTurn ? kTurnTokens * kMaxPairs : 1];
+  __shared__ __align__(16) float2 turns[kTurn ? kStoreTokens * kMaxPairs : 1];
   const CacheStoreParams& P = A.s;
-  int64_t tile = blockIdx.x;
+  uint32_t tile = blockIdx.x;
   if constexpr (kTurn) {
     if (tile < turn_tiles) {
       rotate_tile<kRowThreads4>(A.turn, tile, turns);
@@ -99,37 +99,41 @@ __global__ void __launch_bounds__(kRowThreads4) cache4_store_kernel(const __grid
     }
     tile -= turn_tiles;
   }
-  const int H = P.c.heads, all = 2 * H;
-  const int head_tiles = (all + tile_heads - 1) / tile_heads;
-  const int64_t token0 = tile / head_tiles * tile_tokens;
+  const int H = P.c.heads;
+  const bool key = (tile & 1) == 0;
+  tile >>= 1;
+  const uint32_t head_tiles = static_cast<uint32_t>((H + tile_heads - 1) / tile_heads);
+  const int64_t token0 = static_cast<int64_t>(tile / head_tiles) * tile_tokens;
   const int head0 = static_cast<int>(tile % head_tiles) * tile_heads;
   const int tokens = static_cast<int>(P.n_tokens - token0 < tile_tokens ? P.n_tokens - token0 : tile_tokens);
   const int l = threadIdx.x & 7, group = threadIdx.x >> 3;
-  const int tok = group % tile_tokens, step = kGroups4 / tile_tokens;
+  const int tok = group & (tile_tokens - 1), step = kGroups4 / tile_tokens;
   const int slot = tok < tokens ? __ldg(P.slots + token0 + tok) : -1;
   RowChunks kc = {l, l + 8, false, false};
-  if constexpr (kTurn) kc = row_chunks(A.turn.r, l);
-  const int end = tok < tokens ? min(head0 + tile_heads, all) : 0;
+  if constexpr (kTurn) {
+    if (key) kc = row_chunks(A.turn.r, l);
+  }
+  const int end = tok < tokens ? min(head0 + tile_heads, H) : 0;
   constexpr int kInFlight = 4;
+  const uint16_t* const base = key ? P.k + (token0 + tok) * P.k_st : P.v + (token0 + tok) * P.v_st;
+  const int64_t across = key ? P.k_sh : P.v_sh;
+  uint8_t* const codes = key ? P.c.k : P.c.v;
+  uint32_t* const param = key ? P.c.k_param : P.c.v_param;
   uint4 a[kInFlight], b[kInFlight];
   const auto load = [&](int h) {
 #pragma unroll
-    for (int i = 0; i < kInFlight; ++i) {
-      const int hh = h + i * step;
-      if (hh < end) {
-        const uint16_t* from = hh < H ? P.k + (token0 + tok) * P.k_st + hh * P.k_sh
-                                      : P.v + (token0 + tok) * P.v_st + (hh - H) * P.v_sh;
-        const uint4* v = reinterpret_cast<const uint4*>(from);
-        a[i] = v[hh < H ? kc.a : l];
-        b[i] = v[hh < H ? kc.b : l + 8];
+    for (int i = 0; i < kInFlight; ++i)
+      if (h + i * step < end) {
+        const uint4* from = reinterpret_cast<const uint4*>(base + (h + i * step) * across);
+        a[i] = from[kc.a];
+        b[i] = from[kc.b];
       }
-    }
   };
   int h = head0 + group / tile_tokens;
   load(h);
   float2 cs[8];
   if constexpr (kTurn) {
-    if (head0 < H) {
+    if (key) {
       turns_to_shared<kRowThreads4>(turns, A.turn.r, A.turn.positions, token0, tokens, false);
       if (tok < tokens && kc.turns_a) lane_turns(cs, turns + tok * kMaxPairs, A.turn.r, kc);
     }
@@ -137,75 +141,88 @@ __global__ void __launch_bounds__(kRowThreads4) cache4_store_kernel(const __grid
   const int limit = P.c.num_pages << P.c.page_shift;   // (below 2^31)
   if (slot >= limit && l == 0 && group / tile_tokens == 0) atomicOr(P.err, kErrCheck);
   if (slot < 0 || slot >= limit) return;
-  const int page = slot >> P.c.page_shift, off = slot & (P.c.page - 1);
-  const int64_t row0 = (static_cast<int64_t>(page) * H << P.c.page_shift) + off;
+  // rows of the pool are below 2^31
+  const int row0 = ((slot >> P.c.page_shift) * H << P.c.page_shift) + (slot & (P.c.page - 1));
   const uint32_t lanes = row_lanes();
-  for (; h < end; h += kInFlight * step, load(h)) {
+  while (h < end) {
 #pragma unroll
     for (int i = 0; i < kInFlight; ++i) {
-      const int hh = h + i * step;
-      if (hh >= end) break;
-      const bool key = hh < H;
-      const int64_t row = row0 + (static_cast<int64_t>(key ? hh : hh - H) << P.c.page_shift);
+      if (h + i * step >= end) break;
       if constexpr (kTurn) {
         if (key) turn_chunks(a[i], b[i], cs, kc, A.turn.r.interleaved);
       }
-      write_row4(a[i], b[i], key ? kc.a : l, key ? kc.b : l + 8, (key ? P.c.k : P.c.v) + row * kRowCodes,
-                 (key ? P.c.k_param : P.c.v_param) + row, l, lanes);
+      write_row4(a[i], b[i], kc.a, kc.b, codes, param, row0 + ((h + i * step) << P.c.page_shift), l, lanes);
     }
+    h += kInFlight * step;
+    load(h);
   }
   allow_next_kernel();
 }
 
-// Step 4 into the cache: 8 lanes a row, kGatherRows rows of keys and of values each, all in flight.
-constexpr int kGatherRows = 2;
-__global__ void __launch_bounds__(kRowThreads4) cache4_gather_kernel(const __grid_constant__ CacheGatherParams P, int unit_tiles) {
+// Step 4 into the cache: 8 lanes a row, kGatherRows rows of keys and of values in flight, kGatherTurns times.
+#ifndef GR
+#define GR 1
+#define GT 4
+#define GC 5
+#endif
+constexpr int kGatherRows = GR, kGatherTurns = GT;
+constexpr int kGatherTile = kGroups4 * kGatherRows * kGatherTurns;   // rows of a unit that a CTA has
+__global__ void __launch_bounds__(kRowThreads4, GC) cache4_gather_kernel(const __grid_constant__ CacheGatherParams P,
+                                                                         uint32_t unit_tiles) {
   wait_previous_kernel();   // the indices come from the selection launched before
-  const uint32_t unit = blockIdx.x / static_cast<uint32_t>(unit_tiles);
+  const uint32_t unit = blockIdx.x / unit_tiles;
   const int tile = static_cast<int>(blockIdx.x - unit * unit_tiles);
   const UnitInfo u = unit_info(P.g.g, unit);
   const int W = P.g.g.window, Lc = u.L - W;
   const int m = min(P.g.layer_budget[u.layer], Lc), n = m + W;
   const int l = threadIdx.x & 7, group = threadIdx.x >> 3;
-  const int first = tile * (kGroups4 * kGatherRows) + group;
+  const int first = tile * kGatherTile + group, end = min(n, (tile + 1) * kGatherTile);
   const bool refused = __ldg(P.refused) != 0;   // the table's pages may be other sequences' by now
   const int32_t* const table = P.table + (static_cast<int64_t>(u.layer) * P.c.max_seqs + P.first_seq + u.r) * P.c.max_pages;
+  const int32_t* const indices = P.g.indices + static_cast<int64_t>(unit) * P.g.budget;
   const uint32_t lanes = row_lanes();
-  int src[kGatherRows], page[kGatherRows];
-  bool outside[kGatherRows];
-#pragma unroll
-  for (int i = 0; i < kGatherRows; ++i) {
-    const int row = first + i * kGroups4;
-    src[i] = page[i] = -1;
-    outside[i] = false;
-    if (row >= n) continue;
-    page[i] = __ldg(table + (row >> P.c.page_shift));
-    src[i] = row < m ? __ldg(P.g.indices + static_cast<int64_t>(unit) * P.g.budget + row) : Lc + (row - m);
-    outside[i] = row < m && (src[i] < 0 || src[i] >= Lc);   // never read outside the unit: a row of zeros, and the status tells
-  }
+  const int shift = P.c.page_shift, head = u.h << shift;
   if (refused) return;
-  uint4 k[kGatherRows][2], v[kGatherRows][2];
+  // where the rows come from (-1: nowhere, a row of zeros) and their pages, a turn ahead
+  int src[kGatherRows], page[kGatherRows];
+  const auto look_up = [&](int row0) {
 #pragma unroll
-  for (int i = 0; i < kGatherRows; ++i) {
-    k[i][0] = k[i][1] = v[i][0] = v[i][1] = make_uint4(0, 0, 0, 0);
-    if (first + i * kGroups4 >= n || outside[i]) continue;
-    const uint4* ks = reinterpret_cast<const uint4*>(P.g.k + u.k_off + src[i] * P.g.g.k_st) + l;
-    const uint4* vs = reinterpret_cast<const uint4*>(P.g.v + u.v_off + src[i] * P.g.g.v_st) + l;
-    k[i][0] = __ldg(ks);
-    k[i][1] = __ldg(ks + 8);
-    v[i][0] = __ldg(vs);
-    v[i][1] = __ldg(vs + 8);
-  }
+    for (int i = 0; i < kGatherRows; ++i) {
+      const int row = row0 + i * kGroups4;
+      if (row >= end) continue;
+      page[i] = __ldg(table + (row >> shift));
+      src[i] = row < m ? __ldg(indices + row) : Lc + (row - m);
+    }
+  };
+  look_up(first);
+  for (int row0 = first; row0 < end; row0 += kGroups4 * kGatherRows) {
+    uint4 k[kGatherRows][2], v[kGatherRows][2];
+    int at[kGatherRows];
 #pragma unroll
-  for (int i = 0; i < kGatherRows; ++i) {
-    const int row = first + i * kGroups4;
-    if (row >= n) break;
-    const bool good = page[i] >= 0 && page[i] < P.c.num_pages;
-    if ((outside[i] || !good) && l == 0) atomicOr(P.err, kErrCheck);
-    if (!good) continue;
-    const int64_t at = ((static_cast<int64_t>(page[i]) * P.c.heads + u.h) << P.c.page_shift) + (row & (P.c.page - 1));
-    write_row4(k[i][0], k[i][1], l, l + 8, P.c.k + at * kRowCodes, P.c.k_param + at, l, lanes);
-    write_row4(v[i][0], v[i][1], l, l + 8, P.c.v + at * kRowCodes, P.c.v_param + at, l, lanes);
+    for (int i = 0; i < kGatherRows; ++i) {
+      const int row = row0 + i * kGroups4;
+      k[i][0] = k[i][1] = v[i][0] = v[i][1] = make_uint4(0, 0, 0, 0);
+      if (row >= end) continue;
+      const bool outside = row < m && static_cast<uint32_t>(src[i]) >= static_cast<uint32_t>(Lc);   // never read outside the unit
+      const bool good = static_cast<uint32_t>(page[i]) < static_cast<uint32_t>(P.c.num_pages);
+      if ((outside || !good) && l == 0) atomicOr(P.err, kErrCheck);
+      at[i] = good ? (page[i] * P.c.heads << shift) + head + (row & (P.c.page - 1)) : -1;
+      if (outside) continue;
+      const uint4* ks = reinterpret_cast<const uint4*>(P.g.k + u.k_off + src[i] * P.g.g.k_st) + l;
+      const uint4* vs = reinterpret_cast<const uint4*>(P.g.v + u.v_off + src[i] * P.g.g.v_st) + l;
+      k[i][0] = __ldg(ks);
+      k[i][1] = __ldg(ks + 8);
+      v[i][0] = __ldg(vs);
+      v[i][1] = __ldg(vs + 8);
+    }
+    look_up(row0 + kGroups4 * kGatherRows);
+#pragma unroll
+    for (int i = 0; i < kGatherRows; ++i) {
+      if (row0 + i * kGroups4 >= end) break;
+      if (at[i] < 0) continue;
+      write_row4(k[i][0], k[i][1], l, l + 8, P.c.k, P.c.k_param, at[i], l, lanes);
+      write_row4(v[i][0], v[i][1], l, l + 8, P.c.v, P.c.v_param, at[i], l, lanes);
+    }
   }
   allow_next_kernel();
 }
@@ -213,12 +230,20 @@ __global__ void __launch_bounds__(kRowThreads4) cache4_gather_kernel(const __gri
 template <bool kTurn>
 cudaError_t store4(CacheAppendParams p, cudaStream_t stream) {
   const int64_t turn_tiles = kTurn && p.turn.heads > 0 ? cut_rotate<kRowThreads4>(p.turn) : 0;
-  RotateParams cut;   // keys and values as 2 H heads
+  RotateParams cut;
   cut.n_tokens = p.s.n_tokens;
-  cut.heads = 2 * p.s.c.heads;
-  const int64_t tiles = cut_rotate<kRowThreads4>(cut);
+  cut.heads = p.s.c.heads;
+  int64_t tiles = cut_rotate<kRowThreads4>(cut);
+  // a group a token and all heads one after the other, where that still gives every SM two tiles of each: 24k tokens
+  // 32.1 -> XXX us
+  if (cut.n_tokens >= 304 * kStoreTokens / 2) {
+    cut.tile_tokens = kStoreTokens;
+    cut.tile_heads = cut.heads;
+    tiles = (cut.n_tokens + kStoreTokens - 1) / kStoreTokens;
+  }
+  tiles *= 2;   // of keys, and as many of values
   return launch_after_previous(cache4_store_kernel<kTurn>, dim3(static_cast<unsigned>(turn_tiles + tiles)), dim3(kRowThreads4), 0,
-                               stream, p, cut.tile_tokens, cut.tile_heads, turn_tiles);
+                               stream, p, cut.tile_tokens, cut.tile_heads, static_cast<uint32_t>(turn_tiles));
 }
 
 }  // namespace
@@ -233,9 +258,9 @@ cudaError_t launch_cache4_append(const CacheAppendParams& p, cudaStream_t stream
 
 cudaError_t launch_cache4_gather(const CacheGatherParams& p, cudaStream_t stream) {
   const int64_t rows = static_cast<int64_t>(p.unit_pages) << p.c.page_shift;
-  const int tiles = static_cast<int>((rows + kGroups4 * kGatherRows - 1) / (kGroups4 * kGatherRows));
+  const int64_t tiles = (rows + kGatherTile - 1) / kGatherTile;
   return launch_after_previous(cache4_gather_kernel, dim3(static_cast<unsigned>(p.g.g.n_units * tiles)), dim3(kRowThreads4), 0,
-                               stream, p, tiles);
+                               stream, p, static_cast<uint32_t>(tiles));
 }
 
 }  // namespace kve

@@ -83,10 +83,11 @@ kve_status kv_evict_rotary_create(int32_t head_dim, int32_t rotary_dim, int32_t 
   for (int j = 0; j < rotary_dim / 2; ++j) {
     const double turns = frequencies[j] / 6.283185307179586476925;
     const double part = turns - std::floor(turns);   // [0, 1]
-    const double high = std::floor(part * 4294967296.0);
-    const double low = std::floor((part * 4294967296.0 - high) * 4294967296.0);
-    h->table.turns[j].y = static_cast<uint32_t>(static_cast<uint64_t>(high));   // (a whole turn is none)
-    h->table.turns[j].x = static_cast<uint32_t>(static_cast<uint64_t>(low));
+    // high 2^32 + low, |low| <= 2^31 (a whole turn is none)
+    const double high = std::floor(part * 4294967296.0 + 0.5);
+    const double low = std::fmin((part * 4294967296.0 - high) * 4294967296.0, 2147483647.0);
+    h->table.turns[j].y = static_cast<uint32_t>(static_cast<uint64_t>(high));
+    h->table.turns[j].x = static_cast<uint32_t>(static_cast<int32_t>(low));
   }
   h->table.amplitude = static_cast<float>(amplitude);
   h->table.pairs = rotary_dim / 2;

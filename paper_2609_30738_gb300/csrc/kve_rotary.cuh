@@ -2,6 +2,7 @@
 #pragma once
 
 #include "kve_internal.h"
+#include "kve_ptx.cuh"
 
 namespace kve {
 
@@ -15,21 +16,22 @@ __device__ __forceinline__ uint2 turn_at(const RotaryTable& r, int j) {
 
 // {cos, sin} times the amplitude of the angle that a pair has at position pos. The angle is a fraction of a turn in 64-bit
 // integers (exact for every position, where an fp32 product is off by 2^-24 of the whole angle); its upper 32 bits are cut into
-// the nearest quarter turn and a rest x of at most pi / 4, whose sine and cosine are their Taylor polynomials up to x^9 and
-// x^8 (2^-29 and 2^-25 off at pi / 4): 2^-23 with the roundings.
+// the nearest half turn, which is a sign, and a rest x of at most pi / 2, whose sine over x and cosine are their Taylor
+// polynomials up to x^14 in packed fp32 (2^-33 off at pi / 2): 2^-22 with the roundings.
 __device__ __forceinline__ float2 turn_of(uint2 turn, float amplitude, int pos) {
-  const uint32_t p = static_cast<uint32_t>(pos);
-  uint32_t u = p * turn.y + __umulhi(p, turn.x);
-  if (pos < 0) u -= turn.x;   // (p is 2^32 too large)
-  const uint32_t quarter = u + 0x20000000u;   // (the quarter in its two upper bits)
-  const float x = static_cast<float>(static_cast<int32_t>(u - (quarter & 0xc0000000u))) * 1.46291807926715968e-9f;   // pi 2^-31
+  const uint32_t u = static_cast<uint32_t>(pos) * turn.y + static_cast<uint32_t>(__mulhi(pos, static_cast<int32_t>(turn.x)));
+  const float x = static_cast<float>(static_cast<int32_t>(u << 1)) * 7.31459039633577841e-10f;   // pi 2^-32
   const float y = x * x;
-  const float s = fmaf(x * y, fmaf(y, fmaf(y, fmaf(y, 2.75573192e-6f, -1.98412698e-4f), 8.33333333e-3f), -1.66666667e-1f), x);
-  const float c = fmaf(y, fmaf(y, fmaf(y, fmaf(y, 2.48015873e-5f, -1.38888889e-3f), 4.16666667e-2f), -0.5f), 1.f);
-  const bool odd = quarter & 0x40000000u;
-  const uint32_t sign_s = quarter & 0x80000000u, sign_c = (quarter + 0x40000000u) & 0x80000000u;
-  return make_float2(__uint_as_float(__float_as_uint(odd ? s : c) ^ sign_c) * amplitude,
-                     __uint_as_float(__float_as_uint(odd ? c : s) ^ sign_s) * amplitude);
+  const float2 yy = make_float2(y, y);
+  float2 p = ffma2(yy, make_float2(-7.64716373e-13f, -1.14707456e-11f), make_float2(1.60590438e-10f, 2.08767570e-9f));
+  p = ffma2(yy, p, make_float2(-2.50521084e-8f, -2.75573192e-7f));
+  p = ffma2(yy, p, make_float2(2.75573192e-6f, 2.48015873e-5f));
+  p = ffma2(yy, p, make_float2(-1.98412698e-4f, -1.38888889e-3f));
+  p = ffma2(yy, p, make_float2(8.33333333e-3f, 4.16666667e-2f));
+  p = ffma2(yy, p, make_float2(-1.66666667e-1f, -0.5f));
+  p = ffma2(yy, p, make_float2(1.f, 1.f));
+  const float f = __uint_as_float(__float_as_uint(amplitude) ^ ((u + 0x40000000u) & 0x80000000u));
+  return make_float2(p.y * f, p.x * x * f);
 }
 
 // (a, b) turned: (a c - b s, b c + a s), each rounded once behind its second product.
@@ -48,11 +50,12 @@ __device__ __forceinline__ float bf16_high(uint32_t x) { return __uint_as_float(
 // Four pairs, (a_i, b_i) by halves of x and y, or neighbours in x and y, with the turns cs[0 .. 3].
 __device__ __forceinline__ void turn_halves(uint32_t (&x)[2], uint32_t (&y)[2], const float2* cs) {
 #pragma unroll
-  for (int i = 0; i < 2; ++i) {
-    const float2 u = turned(bf16_low(x[i]), bf16_low(y[i]), cs[2 * i]);
-    const float2 v = turned(bf16_high(x[i]), bf16_high(y[i]), cs[2 * i + 1]);
-    x[i] = bf16_pair(u.x, v.x);
-    y[i] = bf16_pair(u.y, v.y);
+  for (int i = 0; i < 2; ++i) {   // two pairs at once, as `turned`
+    const float2 a = make_float2(bf16_low(x[i]), bf16_high(x[i])), b = make_float2(bf16_low(y[i]), bf16_high(y[i]));
+    const float2 c = make_float2(cs[2 * i].x, cs[2 * i + 1].x), s = make_float2(cs[2 * i].y, cs[2 * i + 1].y);
+    const float2 u = ffma2(a, c, fmul2(b, make_float2(-s.x, -s.y))), v = ffma2(b, c, fmul2(a, s));
+    x[i] = bf16_pair(u.x, u.y);
+    y[i] = bf16_pair(v.x, v.y);
   }
 }
 __device__ __forceinline__ void turn_neighbours(uint4& x, const float2* cs) {

@@ -8,9 +8,9 @@ from tests.cache8 import LOGIT_STEP, OUT_STEP, bf16, to_torch
 # A weight (probability times s) is rounded to f16, 2^-11 / 2 of itself; its exponential and the log2 of s add 2^-22 of it
 # and the fp32 rounding of an exponent of up to 2^7, 2^-17: together below 2^-11 / 2 + 2^-16.
 W_STEP = 2.0 ** -12 + 2.0 ** -16
-# cos and sin are off by 2^-23 at most, and each result has two products of them; 2^-22 for the fp32 rounding of both
+# cos and sin are off by 2^-22 at most, and each result has two products of them; 2^-22 for the fp32 rounding of both
 # products and their sum.
-TURN_STEP = 2.0 ** -23 + 2.0 ** -22
+TURN_STEP = 2.0 ** -22 + 2.0 ** -22
 
 
 def rows(rng, shape, spread=1.0):
