@@ -45,25 +45,17 @@ constexpr int kRowBytes = kHeadDim / 2;                    // codes of a token
 constexpr int kCodeBytes = kStep * kRowBytes;
 constexpr int kStageBytes = 2 * kCodeBytes;                // K, then V
 
-// R rows of a block, on W warps.
-template <int R>
+// R rows of a block on W warps of a CTA: 16 warps an SM for 8 rows, 12 for 16 (their registers). With fewer warps a CTA
+// the end of a part costs less, with more a block is cut into fewer parts: 8 warps where there are few blocks, else 4
+// (launch_cache4_attend).
+template <int R, int W>
 struct A4Cfg {
-#ifndef W8
-#define W8 8
-#define C8 2
-#define W16 4
-#define C16 3
-#endif
-#ifndef KP8
-#define KP8 2
-#define KP16 2
-#endif
-  static constexpr int kWarps = R == 8 ? W8 : W16;
-  static constexpr int kThreads = 32 * kWarps;
+  static constexpr int kThreads = 32 * W;
   static constexpr int kStages = 3;
-  static constexpr int kCtas = R == 8 ? C8 : C16;
-  static constexpr int kTile = kWarps * kStep;   // tokens: a step of every warp
-  static constexpr size_t kCtl = size_t(kWarps) * kStages * kStageBytes;
+  static constexpr int kCtas = (R == 8 ? 16 : 12) / W;
+  static constexpr int kTile = W * kStep;   // tokens: a step of every warp
+  static constexpr int kPart = 3;           // what a part costs beside its own tiles
+  static constexpr size_t kCtl = size_t(W) * kStages * kStageBytes;
 };
 
 // A part, tiles x .. end - 1 of block b, from token tok0 of its sequence on; steps first .. last - 1 of it are a warp's.
@@ -80,16 +72,15 @@ struct Part {
   }
 };
 
-template <int R>
+template <int R, int W>
 struct A4Ctl {
-  static constexpr int W = A4Cfg<R>::kWarps, S = A4Cfg<R>::kStages;
+  static constexpr int S = A4Cfg<R, W>::kStages;
   alignas(128) uint32_t param[W][S][2][kStep];   // K's, V's
   float4 tokens[W][kStep];                       // of a step's tokens: K's s and z, V's log2 s and z
   LineCtl<W> line;
   Part part[W], next[W], ahead[W];               // of a warp's sums, and of its copies
-  int at[W];                                     // the stage (its bytes in the ring) with the warp's rows at a part's end
+  int at[W];                                     // the stage (its bytes in the ring) with the warp's rows at a part's end, or -1
   alignas(8) float m[W][8], l[W][8];             // of eight of the warps' rows, at the end of a part
-  bool has[W];                                   // the warp had steps in the part
   float4 scale[W][R / 2];                        // of two rows: logits over products, sums of q in their units
   int seen[W][R];                                // tokens that the row sees
   Block split[2];                                // parts left for the join
@@ -99,9 +90,9 @@ struct A4Ctl {
 // How far (log2) a row's largest product passes its reference before that moves. Weights count from 2^(14 - kLazy) there.
 constexpr float kLazy = 8.f;
 
-template <int R>
+template <int R, int W>
 constexpr size_t attend4_smem() {
-  return A4Cfg<R>::kCtl + sizeof(A4Ctl<R>);
+  return A4Cfg<R, W>::kCtl + sizeof(A4Ctl<R, W>);
 }
 
 __device__ __forceinline__ void mma_f16(float (&d)[4], const uint32_t (&a)[4], uint32_t b0, uint32_t b1) {
@@ -140,6 +131,9 @@ __device__ __forceinline__ void load_transposed(uint32_t (&d)[4], uint32_t at) {
                : "memory");
 }
 
+// The 128 bytes around p towards L2 (which all SMs share: what is written there later is seen).
+__device__ __forceinline__ void prefetch_line(const void* p) { asm volatile("prefetch.global.L2 [%0];" ::"l"(p)); }
+
 // A load that is issued here, not where its value is first needed.
 __device__ __forceinline__ uint4 load_now(const void* p) {
   uint4 v;
@@ -163,24 +157,33 @@ __device__ __forceinline__ float high_bf16(uint32_t x) { return __uint_as_float(
 // little as the probabilities' sum passes 1.
 __device__ __forceinline__ float len_bits(int len) { return static_cast<float>(32 - __clz(len - 1)); }   // (1: 0)
 
-static_assert((attend4_smem<8>() + 1024) * A4Cfg<8>::kCtas <= 228 * 1024 && (attend4_smem<16>() + 1024) * A4Cfg<16>::kCtas <= 228 * 1024,
-              "CTAs an SM");
-
-template <int R>
-__global__ void __launch_bounds__(A4Cfg<R>::kThreads, A4Cfg<R>::kCtas)
+template <int R, int W>
+__global__ void __launch_bounds__(A4Cfg<R, W>::kThreads, A4Cfg<R, W>::kCtas)
 cache_attend4_kernel(const __grid_constant__ AttendParams P) {
-  using C = A4Cfg<R>;
-  constexpr int W = C::kWarps, kHalves = R / 8;   // kHalves: rows of a lane
+  using C = A4Cfg<R, W>;
+  constexpr int kHalves = R / 8;   // pairs of rows of a lane
   constexpr int S = C::kStages;
   extern __shared__ __align__(128) uint8_t smem[];
-  A4Ctl<R>& ctl = *reinterpret_cast<A4Ctl<R>*>(smem + C::kCtl);
+  static_assert((attend4_smem<R, W>() + 1024) * C::kCtas <= 228 * 1024, "CTAs an SM");
+  A4Ctl<R, W>& ctl = *reinterpret_cast<A4Ctl<R, W>*>(smem + C::kCtl);
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
   const int rows = P.q_tokens * P.c.group;
   const int blocks = (rows + R - 1) / R;
+  // what the first steps wait for, one after the other, is brought into L2 meanwhile: lengths, table and queries, a line a
+  // thread of the grid
+  {
+    const int64_t id = static_cast<int64_t>(blockIdx.x) * C::kThreads + threadIdx.x;
+    const int64_t table_lines = (static_cast<int64_t>(P.n_seq) * P.c.max_pages + 31) >> 5, q_rows = static_cast<int64_t>(P.n_seq) * P.q_tokens * P.c.hq;
+    if (id < table_lines) {
+      prefetch_line(P.table + id * 32);
+    } else if (id - table_lines < 2 * q_rows) {
+      const int row = static_cast<int>((id - table_lines) >> 1), tok = row / P.c.hq;
+      prefetch_line(P.q + tok * P.q_st + (row - tok * P.c.hq) * P.q_sh + (id - table_lines & 1) * 64);
+    }
+  }
   wait_previous_kernel();
-  constexpr int kPart = R == 8 ? KP8 : KP16;
-  Cuts<kPart> cuts;
-  line_share<W>(P, blocks, A4Cfg<R>::kTile, ctl.line, cuts);
+  Cuts<C::kPart> cuts;
+  line_share<W>(P, blocks, C::kTile, ctl.line, cuts);
   const int x0 = ctl.line.ends[0], x1 = ctl.line.ends[1];
   const int shift = P.c.page_shift;
   const int g = lane >> 2, t = lane & 3;
@@ -222,7 +225,7 @@ cache_attend4_kernel(const __grid_constant__ AttendParams P) {
         ahead_last = -1;
         return;
       }
-      next_block(P, blocks, A4Cfg<R>::kTile, a.b);
+      next_block(P, blocks, C::kTile, a.b);
       a.template set<W>(x1, warp);
       __syncwarp();
       ahead = a;
@@ -533,10 +536,7 @@ cache_attend4_kernel(const __grid_constant__ AttendParams P) {
     // (in the stage of the last step, which the next one's copies will fill)
     const int stage = slot == 0 ? S - 1 : slot - 1;
     float* const mine = reinterpret_cast<float*>(ring + stage * kStageBytes);
-    if (lane == 0) {
-      ctl.has[warp] = has;
-      ctl.at[warp] = stage * kStageBytes;
-    }
+    if (lane == 0) ctl.at[warp] = has ? stage * kStageBytes : -1;
     const int next_x = part.end;
 #pragma unroll
     for (int e = 0; e < kHalves; ++e) {
@@ -580,30 +580,32 @@ cache_attend4_kernel(const __grid_constant__ AttendParams P) {
       if (e + 1 == kHalves && next_x < x1) {   // the next part, and its rows on their way
         Part a = part;
         a.x = next_x;
-        next_block(P, blocks, A4Cfg<R>::kTile, a.b);
+        next_block(P, blocks, C::kTile, a.b);
         a.template set<W>(x1, warp);
         load_rows(a.b);
         ctl.next[warp] = a;
       }
       __syncthreads();
       for (int row = warp; row < 8; row += W) {
-        float mx = -INFINITY;
+        float f[W], mx = -INFINITY, sum = 0.f;
+        float4 v[W], a = make_float4(0.f, 0.f, 0.f, 0.f);
 #pragma unroll
-        for (int w = 0; w < W; ++w)
-          if (ctl.has[w]) mx = fmaxf(mx, ctl.m[w][row]);
-        const float mr = or_zero(mx);
-        float4 a = make_float4(0.f, 0.f, 0.f, 0.f);
-        float sum = 0.f;
+        for (int w = 0; w < W; ++w) {   // (a warp without steps has nothing there)
+          const int at = ctl.at[w];
+          f[w] = at >= 0 ? ctl.m[w][row] : -INFINITY;
+          v[w] = make_float4(0.f, 0.f, 0.f, 0.f);
+          if (at >= 0)
+            v[w] = reinterpret_cast<const float4*>(smem + w * (S * kStageBytes) + at + row * (kHeadDim * 4))[lane ^ (row & 6)];
+          mx = fmaxf(mx, f[w]);
+        }
 #pragma unroll
         for (int w = 0; w < W; ++w) {
-          if (!ctl.has[w]) continue;
-          const float f = ex2(ctl.m[w][row] - mr);
-          const float4 v = reinterpret_cast<const float4*>(smem + w * (S * kStageBytes) + ctl.at[w] + row * (kHeadDim * 4))[lane ^ (row & 6)];
-          sum = fmaf(ctl.l[w][row], f, sum);
-          a.x = fmaf(v.x, f, a.x);
-          a.y = fmaf(v.y, f, a.y);
-          a.z = fmaf(v.z, f, a.z);
-          a.w = fmaf(v.w, f, a.w);
+          f[w] = ex2(f[w] - or_zero(mx));
+          sum = fmaf(ctl.at[w] >= 0 ? ctl.l[w][row] : 0.f, f[w], sum);
+          a.x = fmaf(v[w].x, f[w], a.x);
+          a.y = fmaf(v[w].y, f[w], a.y);
+          a.z = fmaf(v[w].z, f[w], a.z);
+          a.w = fmaf(v[w].w, f[w], a.w);
         }
         const int r = 8 * e + row;
         if (whole) {
@@ -738,25 +740,29 @@ cache_attend4_kernel(const __grid_constant__ AttendParams P) {
   }
 }
 
-template <int R>
+template <int R, int W>
 cudaError_t attend4_rows(const kve_cache& c, const AttendParams& p, cudaStream_t stream) {
-  using C = A4Cfg<R>;
-  auto* fn = cache_attend4_kernel<R>;
-  cudaError_t e = cudaFuncSetAttribute(fn, cudaFuncAttributeMaxDynamicSharedMemorySize, static_cast<int>(attend4_smem<R>()));
+  using C = A4Cfg<R, W>;
+  constexpr size_t smem = attend4_smem<R, W>();
+  static_assert(C::kCtas <= kAttend4Ctas, "parts in the workspace");
+  auto* fn = cache_attend4_kernel<R, W>;
+  cudaError_t e = cudaFuncSetAttribute(fn, cudaFuncAttributeMaxDynamicSharedMemorySize, static_cast<int>(smem));
   if (e != cudaSuccess) return e;
   // no more CTAs than there can be tiles
   const int64_t blocks = (p.q_tokens * p.c.group + R - 1) / R;
-  const int64_t tiles = ((static_cast<int64_t>(p.c.max_pages) << p.c.page_shift) + A4Cfg<R>::kTile - 1) / A4Cfg<R>::kTile;
+  const int64_t tiles = ((static_cast<int64_t>(p.c.max_pages) << p.c.page_shift) + C::kTile - 1) / C::kTile;
   const int64_t most = static_cast<int64_t>(C::kCtas) * c.sms;
   const int64_t want = tiles >= most ? most : tiles * p.n_seq * p.c.heads * blocks;
-  return launch_after_previous(fn, dim3(static_cast<unsigned>(want < most ? want : most)), dim3(C::kThreads),
-                               attend4_smem<R>(), stream, p);
+  return launch_after_previous(fn, dim3(static_cast<unsigned>(want < most ? want : most)), dim3(C::kThreads), smem, stream, p);
 }
 
 }  // namespace
 
 cudaError_t launch_cache4_attend(const kve_cache& c, const AttendParams& p, cudaStream_t stream) {
-  return p.q_tokens * p.c.group <= 8 ? attend4_rows<8>(c, p, stream) : attend4_rows<16>(c, p, stream);
+  if (p.q_tokens * p.c.group > 8) return attend4_rows<16, 4>(c, p, stream);
+  // two CTAs an SM have a block each without cutting one
+  const bool many = static_cast<int64_t>(p.n_seq) * p.c.heads >= 2 * c.sms;
+  return many ? attend4_rows<8, 4>(c, p, stream) : attend4_rows<8, 8>(c, p, stream);
 }
 
 }  // namespace kve
