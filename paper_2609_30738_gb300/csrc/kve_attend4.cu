@@ -101,13 +101,11 @@ __device__ __forceinline__ void mma_f16(float (&d)[4], const uint32_t (&a)[4], u
       : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
 }
 
-// 16 bytes global -> shared where `there`; a lane's copies so far are a group; all but the last N groups have landed.
-__device__ __forceinline__ void copy16(uint32_t dst, const void* src, uint64_t policy, bool there) {
-  asm volatile(
-      "{\n .reg .pred p;\n setp.ne.b32 p, %3, 0;\n"
-      " @p cp.async.cg.shared.global.L2::cache_hint [%0], [%1], 16, %2;\n}" ::"r"(dst),
-      "l"(src), "l"(policy), "r"(there ? 1 : 0)
-      : "memory");
+// 16 bytes global -> shared, zeros where they are not `there` (src is not followed then); a lane's copies so far are a group; all
+// but the last N groups have landed.
+__device__ __forceinline__ void copy16(uint32_t dst, const void* src, uint64_t policy, uint32_t there) {
+  asm volatile("cp.async.cg.shared.global.L2::cache_hint [%0], [%1], 16, %3, %2;" ::"r"(dst), "l"(src), "l"(policy), "r"(there)
+               : "memory");
 }
 __device__ __forceinline__ void copies_group() { asm volatile("cp.async.commit_group;" ::: "memory"); }
 template <int N>
@@ -142,7 +140,7 @@ __device__ __forceinline__ uint4 load_now(const void* p) {
 }
 
 __device__ __forceinline__ float2 both(float x) { return make_float2(x, x); }
-__device__ __forceinline__ float or_zero(float x) { return x == -INFINITY ? 0.f : x; }
+constexpr float kNone = -3e38f;   // a maximum of nothing: finite, so that differences to it are no NaN
 
 __device__ __forceinline__ uint32_t f16x2(float lo, float hi) {
   uint32_t d;
@@ -241,17 +239,17 @@ cache_attend4_kernel(const __grid_constant__ AttendParams P) {
   // The copies of the next step, in three pieces that stand between the products: where its rows are (of its two halves, in
   // the pool), K, and the rest.
   int row0 = 0, row1 = 0;
-  bool ok0 = false, ok1 = false;
+  uint32_t ok0 = 0, ok1 = 0;   // bytes of each copy: 16, or 0 for a page outside the pool (or no step)
   const auto find = [&]() {
-    ok0 = ok1 = false;
+    ok0 = ok1 = 0;
     if (ahead_last < 0) return;
     const int at = ahead_tok0 + ahead_step * kStep;
     const int id0 = __shfl_sync(0xffffffffu, held, (at >> shift) - window);
     const int id1 = __shfl_sync(0xffffffffu, held, ((at + 16) >> shift) - window);
-    ok0 = static_cast<uint32_t>(id0) < static_cast<uint32_t>(P.c.num_pages);
-    ok1 = static_cast<uint32_t>(id1) < static_cast<uint32_t>(P.c.num_pages);
+    ok0 = static_cast<uint32_t>(id0) < static_cast<uint32_t>(P.c.num_pages) ? 16 : 0;
+    ok1 = static_cast<uint32_t>(id1) < static_cast<uint32_t>(P.c.num_pages) ? 16 : 0;
     gaps = (gaps & ~(3u << 2 * fill)) | (ok0 ? 0u : 1u) << 2 * fill | (ok1 ? 0u : 2u) << 2 * fill;
-    if (!ok0 || !ok1) atomicOr(P.err, kErrCheck);
+    if ((ok0 & ok1) == 0) atomicOr(P.err, kErrCheck);
     row0 = (id0 * P.c.heads << shift) + ahead_head + (at & (P.c.page - 1));
     row1 = (id1 * P.c.heads << shift) + ahead_head + ((at + 16) & (P.c.page - 1));
   };
@@ -266,8 +264,9 @@ cache_attend4_kernel(const __grid_constant__ AttendParams P) {
   const auto copy_keys = [&]() { copy_codes(P.c.k, put + fill * kStageBytes); };
   const auto copy_rest = [&]() {
     copy_codes(P.c.v, put + fill * kStageBytes + kCodeBytes);
-    copy16(put_number + fill * (2 * kStep * 4), (lane & 8 ? P.c.v_param : P.c.k_param) + (lane & 4 ? row1 : row0) + (lane & 3) * 4,
-           policy, lane < 16 && (lane & 4 ? ok1 : ok0));
+    if (lane < 16)
+      copy16(put_number + fill * (2 * kStep * 4), (lane & 8 ? P.c.v_param : P.c.k_param) + (lane & 4 ? row1 : row0) + (lane & 3) * 4,
+             policy, lane & 4 ? ok1 : ok0);
     copies_group();   // (an empty one too: groups are counted)
     if (ahead_last >= 0) {
       fill = fill + 1 == S ? 0 : fill + 1;
@@ -372,7 +371,7 @@ cache_attend4_kernel(const __grid_constant__ AttendParams P) {
     float2 m[kHalves], top[kHalves], l[kHalves], z[kHalves];   // the lane's maxima; the rows' references; the lane's sums of p, p z
 #pragma unroll
     for (int e = 0; e < kHalves; ++e) {
-      m[e] = top[e] = both(-INFINITY);
+      m[e] = top[e] = both(kNone);
       l[e] = z[e] = both(0.f);
     }
     const int first = part.first, last = part.last, tok0 = part.tok0, all_see = b.len - P.q_tokens + 1;
@@ -453,7 +452,7 @@ cache_attend4_kernel(const __grid_constant__ AttendParams P) {
                                 max3(fmaxf(y[0][e].y, y[1][e].y), y[2][e].y, y[3][e].y));
         mx = fmul2(mx, kq[e]);
         mx = make_float2(fmaxf(mx.x, m[e].x), fmaxf(mx.y, m[e].y));
-        const float2 kept = make_float2(ex2(m[e].x - or_zero(mx.x)), ex2(m[e].y - or_zero(mx.y)));
+        const float2 kept = make_float2(ex2(m[e].x - mx.x), ex2(m[e].y - mx.y));
         m[e] = mx;
         l[e] = fmul2(l[e], kept);
         z[e] = fmul2(z[e], kept);
@@ -468,7 +467,7 @@ cache_attend4_kernel(const __grid_constant__ AttendParams P) {
             tx[e].y = fmaxf(tx[e].y, __shfl_xor_sync(0xffffffffu, tx[e].y, d));
           }
           tx[e] = make_float2(fmaxf(tx[e].x, top[e].x), fmaxf(tx[e].y, top[e].y));
-          const float f0 = ex2(top[e].x - or_zero(tx[e].x)), f1 = ex2(top[e].y - or_zero(tx[e].y));
+          const float f0 = ex2(top[e].x - tx[e].x), f1 = ex2(top[e].y - tx[e].y);
           top[e] = tx[e];
 #pragma unroll
           for (int i = 0; i < 8; ++i) {
@@ -483,8 +482,8 @@ cache_attend4_kernel(const __grid_constant__ AttendParams P) {
       const auto weigh = [&](auto kSome) {
 #pragma unroll
         for (int e = 0; e < kHalves; ++e) {
-          const float2 mr = make_float2(-(or_zero(m[e].x) + lb), -(or_zero(m[e].y) + lb));
-          const float2 tr = make_float2(14.f - kLazy - or_zero(top[e].x), 14.f - kLazy - or_zero(top[e].y));
+          const float2 mr = make_float2(-(m[e].x + lb), -(m[e].y + lb));
+          const float2 tr = make_float2(14.f - kLazy - top[e].x, 14.f - kLazy - top[e].y);
 #pragma unroll
           for (int i = 0; i < 4; ++i) {
             const float vz = ctl.tokens[warp][8 * i + g].w;
@@ -547,7 +546,7 @@ cache_attend4_kernel(const __grid_constant__ AttendParams P) {
           all.x = fmaxf(all.x, __shfl_xor_sync(0xffffffffu, all.x, d));
           all.y = fmaxf(all.y, __shfl_xor_sync(0xffffffffu, all.y, d));
         }
-        const float2 kept = make_float2(ex2(m[e].x - or_zero(all.x)), ex2(m[e].y - or_zero(all.y)));
+        const float2 kept = make_float2(ex2(m[e].x - all.x), ex2(m[e].y - all.y));
         float2 ll = fmul2(l[e], kept), zz = fmul2(z[e], kept);
 #pragma unroll
         for (int d = 4; d < 32; d <<= 1) {
@@ -558,7 +557,7 @@ cache_attend4_kernel(const __grid_constant__ AttendParams P) {
         }
         // quarters of sum p (s c + z), so that neither term alone passes the largest float: products of c 2^-24 or
         // 16 c 2^-24 with weights times 2^(14 - kLazy)
-        const float f[2] = {ex2(or_zero(top[e].x) - or_zero(all.x) - lb), ex2(or_zero(top[e].y) - or_zero(all.y) - lb)};
+        const float f[2] = {ex2(top[e].x - all.x - lb), ex2(top[e].y - all.y - lb)};
         const float zq[2] = {0.25f * zz.x, 0.25f * zz.y};
 #pragma unroll
         for (int j = 0; j < 2; ++j)
@@ -587,12 +586,12 @@ cache_attend4_kernel(const __grid_constant__ AttendParams P) {
       }
       __syncthreads();
       for (int row = warp; row < 8; row += W) {
-        float f[W], mx = -INFINITY, sum = 0.f;
+        float f[W], mx = kNone, sum = 0.f;
         float4 v[W], a = make_float4(0.f, 0.f, 0.f, 0.f);
 #pragma unroll
         for (int w = 0; w < W; ++w) {   // (a warp without steps has nothing there)
           const int at = ctl.at[w];
-          f[w] = at >= 0 ? ctl.m[w][row] : -INFINITY;
+          f[w] = at >= 0 ? ctl.m[w][row] : kNone;
           v[w] = make_float4(0.f, 0.f, 0.f, 0.f);
           if (at >= 0)
             v[w] = reinterpret_cast<const float4*>(smem + w * (S * kStageBytes) + at + row * (kHeadDim * 4))[lane ^ (row & 6)];
@@ -600,7 +599,7 @@ cache_attend4_kernel(const __grid_constant__ AttendParams P) {
         }
 #pragma unroll
         for (int w = 0; w < W; ++w) {
-          f[w] = ex2(f[w] - or_zero(mx));
+          f[w] = ex2(f[w] - mx);
           sum = fmaf(ctl.at[w] >= 0 ? ctl.l[w][row] : 0.f, f[w], sum);
           a.x = fmaf(v[w].x, f[w], a.x);
           a.y = fmaf(v[w].y, f[w], a.y);
@@ -665,7 +664,7 @@ cache_attend4_kernel(const __grid_constant__ AttendParams P) {
     float4 acc[kRows];
 #pragma unroll
     for (int k = 0; k < kRows; ++k) {
-      mx[k] = -INFINITY;
+      mx[k] = kNone;
       sum[k] = 0.f;
       acc[k] = make_float4(0.f, 0.f, 0.f, 0.f);
     }
@@ -675,14 +674,14 @@ cache_attend4_kernel(const __grid_constant__ AttendParams P) {
 #pragma unroll
       for (int k = 0; k < kRows; ++k) {   // a lane a part: its maximum and sum
         const int row = row0 + k * W;
-        float pm = -INFINITY, pl = 0.f;
+        float pm = kNone, pl = 0.f;
         if (lane < count && row < there) {
           pm = __ldcg(at(c0 + lane) + R * kHeadDim + row);
           pl = __ldcg(at(c0 + lane) + R * kHeadDim + R + row);
         }
-        const float top = fmaxf(mx[k], warp_max(pm)), back = ex2(mx[k] - or_zero(top));
+        const float top = fmaxf(mx[k], warp_max(pm)), back = ex2(mx[k] - top);
         mx[k] = top;
-        f[k] = ex2(pm - or_zero(top));
+        f[k] = ex2(pm - top);
         pl *= f[k];
 #pragma unroll
         for (int d = 16; d > 0; d >>= 1) pl += __shfl_xor_sync(0xffffffffu, pl, d);
@@ -724,7 +723,7 @@ cache_attend4_kernel(const __grid_constant__ AttendParams P) {
       __syncthreads();
       if (works && team == 0)
         for (int w = row0 + there; w < teams * there; w += there) {
-          const float top = fmaxf(mx[0], ctl.m[w][0]), a = ex2(mx[0] - or_zero(top)), c = ex2(ctl.m[w][0] - or_zero(top));
+          const float top = fmaxf(mx[0], ctl.m[w][0]), a = ex2(mx[0] - top), c = ex2(ctl.m[w][0] - top);
           const float4 v = sums[w * 32 + lane];
           mx[0] = top;
           sum[0] = fmaf(sum[0], a, ctl.l[w][0] * c);

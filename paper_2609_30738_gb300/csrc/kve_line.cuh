@@ -189,7 +189,7 @@ __device__ __forceinline__ void emit_row(const AttendParams& P, const Block& b, 
   };
   reinterpret_cast<uint2*>(P.out + tok * P.o_st + hq * P.o_sh)[lane] = make_uint2(pair(a.x, a.y), pair(a.z, a.w));
   if (P.lse && lane == 0)
-    P.lse[tok * P.c.hq + hq] = sum == 0.f ? -INFINITY : ((top == -INFINITY ? 0.f : top) + lb + lg2(sum)) * 0.69314718056f;
+    P.lse[tok * P.c.hq + hq] = sum == 0.f ? -INFINITY : (top + lb + lg2(sum)) * 0.69314718056f;
 }
 
 }  // namespace kve
