@@ -304,12 +304,9 @@ cache_attend4_kernel(const __grid_constant__ AttendParams P) {
     enter();
     load_rows(a.b);
     settle();
-#pragma unroll 1
-    for (int i = 0; i < S - 1; ++i) {
-      find();
-      copy_keys();
-      copy_rest();
-    }
+    find();
+    copy_keys();
+    copy_rest();
   }
   for (int x = x0; x < x1;) {
     const Part& part = ctl.part[warp];
@@ -358,6 +355,14 @@ cache_attend4_kernel(const __grid_constant__ AttendParams P) {
       }
     }
     __syncwarp();
+    if (x == x0) {   // (not before: the queries' exchanges would wait behind these copies)
+#pragma unroll 1
+      for (int i = 1; i < S - 1; ++i) {
+        find();
+        copy_keys();
+        copy_rest();
+      }
+    }
 
     // ---------------------------------------------------------- the steps
     // this lane's rows are 8 e + 2 t and 8 e + 2 t + 1, its tokens 8 i + g
@@ -642,15 +647,18 @@ cache_attend4_kernel(const __grid_constant__ AttendParams P) {
   allow_next_kernel();
   if (splits == 0) return;
   __syncthreads();   // every thread's part of the sums is out, and ctl.split is written
+  if (threadIdx.x < splits) {
+    int w0, w1;
+    cuts.parts(ctl.split[threadIdx.x], &w0, &w1);
+    ctl.last[threadIdx.x] = inc_acq_rel_gpu(P.arrive + w0, static_cast<unsigned>(w1 - w0)) == static_cast<unsigned>(w1 - w0);
+  }
+  __syncthreads();
   constexpr int kRows = (R + W - 1) / W;
   for (int n = 0; n < splits; ++n) {
+    if (!ctl.last[n]) continue;
     const Block s = ctl.split[n];
     int w0, w1;
     cuts.parts(s, &w0, &w1);
-    if (threadIdx.x == 0)
-      ctl.last[n] = inc_acq_rel_gpu(P.arrive + w0, static_cast<unsigned>(w1 - w0)) == static_cast<unsigned>(w1 - w0);
-    __syncthreads();
-    if (!ctl.last[n]) continue;
     // A warp has the rows warp, warp + W, ...; where there are twice as many warps as rows or more, a row's parts are dealt
     // to several warps, whose sums the first of them adds in their order.
     const int parts = w1 - w0 + 1, there = min(R, rows - s.rb * R);
@@ -668,29 +676,11 @@ cache_attend4_kernel(const __grid_constant__ AttendParams P) {
       sum[k] = 0.f;
       acc[k] = make_float4(0.f, 0.f, 0.f, 0.f);
     }
+    constexpr int kAtOnce = kRows == 1 ? 20 : 16 / kRows;   // parts of each row whose loads are in flight
     for (int c0 = p0; works && c0 < p1; c0 += 32) {
       const int count = min(p1 - c0, 32);
-      float f[kRows];
-#pragma unroll
-      for (int k = 0; k < kRows; ++k) {   // a lane a part: its maximum and sum
-        const int row = row0 + k * W;
-        float pm = kNone, pl = 0.f;
-        if (lane < count && row < there) {
-          pm = __ldcg(at(c0 + lane) + R * kHeadDim + row);
-          pl = __ldcg(at(c0 + lane) + R * kHeadDim + R + row);
-        }
-        const float top = fmaxf(mx[k], warp_max(pm)), back = ex2(mx[k] - top);
-        mx[k] = top;
-        f[k] = ex2(pm - top);
-        pl *= f[k];
-#pragma unroll
-        for (int d = 16; d > 0; d >>= 1) pl += __shfl_xor_sync(0xffffffffu, pl, d);
-        sum[k] = fmaf(sum[k], back, pl);
-        acc[k].x *= back, acc[k].y *= back, acc[k].z *= back, acc[k].w *= back;
-      }
-      constexpr int kAtOnce = 16 / kRows;   // loads in flight
-      for (int j0 = 0; j0 < count; j0 += kAtOnce) {
-        float4 v[kAtOnce][kRows];
+      float4 v[kAtOnce][kRows];
+      const auto load = [&](int j0) {
 #pragma unroll
         for (int j = 0; j < kAtOnce; ++j)
 #pragma unroll
@@ -699,6 +689,32 @@ cache_attend4_kernel(const __grid_constant__ AttendParams P) {
             if (j0 + j < count && row0 + k * W < there)
               v[j][k] = __ldcg(reinterpret_cast<const float4*>(at(c0 + j0 + j) + (row0 + k * W) * kHeadDim) + lane);
           }
+      };
+      float pm[kRows], pl[kRows];   // a lane a part: its maximum and sum
+#pragma unroll
+      for (int k = 0; k < kRows; ++k) {
+        const int row = row0 + k * W;
+        pm[k] = kNone;
+        pl[k] = 0.f;
+        if (lane < count && row < there) {
+          pm[k] = __ldcg(at(c0 + lane) + R * kHeadDim + row);
+          pl[k] = __ldcg(at(c0 + lane) + R * kHeadDim + R + row);
+        }
+      }
+      load(0);
+      float f[kRows];
+#pragma unroll
+      for (int k = 0; k < kRows; ++k) {
+        const float top = fmaxf(mx[k], warp_max(pm[k])), back = ex2(mx[k] - top);
+        mx[k] = top;
+        f[k] = ex2(pm[k] - top);
+        pl[k] *= f[k];
+#pragma unroll
+        for (int d = 16; d > 0; d >>= 1) pl[k] += __shfl_xor_sync(0xffffffffu, pl[k], d);
+        sum[k] = fmaf(sum[k], back, pl[k]);
+        acc[k].x *= back, acc[k].y *= back, acc[k].z *= back, acc[k].w *= back;
+      }
+      for (int j0 = 0;;) {
 #pragma unroll
         for (int j = 0; j < kAtOnce; ++j)
 #pragma unroll
@@ -710,6 +726,9 @@ cache_attend4_kernel(const __grid_constant__ AttendParams P) {
             acc[k].z = fmaf(v[j][k].z, g, acc[k].z);
             acc[k].w = fmaf(v[j][k].w, g, acc[k].w);
           }
+        j0 += kAtOnce;
+        if (j0 >= count) break;
+        load(j0);
       }
     }
     if (teams > 1) {
