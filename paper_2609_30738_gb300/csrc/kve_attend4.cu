@@ -393,23 +393,28 @@ cache_attend4_kernel(const __grid_constant__ AttendParams P) {
         ctl.tokens[warp][lane] = make_float4(low_bf16(a), high_bf16(a), lg2(low_bf16(c)), high_bf16(c));
       }
       float s[2][kHalves][4];
+      {
+        uint4 u[4];
 #pragma unroll
-      for (int k = 0; k < 2; ++k) {
+        for (int i = 0; i < 4; ++i) u[i] = *reinterpret_cast<const uint4*>(at + i * (8 * kRowBytes) + kget);
 #pragma unroll
-        for (int e = 0; e < kHalves; ++e)
+        for (int k = 0; k < 2; ++k)
 #pragma unroll
-          for (int r = 0; r < 4; ++r) s[k][e][r] = 0.f;
-        const uint4 va = *reinterpret_cast<const uint4*>(at + (2 * k) * (8 * kRowBytes) + kget);
-        const uint4 vb = *reinterpret_cast<const uint4*>(at + (2 * k + 1) * (8 * kRowBytes) + kget);
+          for (int e = 0; e < kHalves; ++e)
+#pragma unroll
+            for (int r = 0; r < 4; ++r) s[k][e][r] = 0.f;
 #pragma unroll
         for (int w = 0; w < 4; ++w)
 #pragma unroll
-          for (int h = 0; h < 2; ++h) {
-            const uint32_t ua = h ? (&va.x)[w] >> 8 : (&va.x)[w], ub = h ? (&vb.x)[w] >> 8 : (&vb.x)[w];
-            const uint32_t a[4] = {ua & 0x000f000fu, ub & 0x000f000fu, ua & 0x00f000f0u, ub & 0x00f000f0u};
+          for (int h = 0; h < 2; ++h)
 #pragma unroll
-            for (int e = 0; e < kHalves; ++e) mma_f16(s[k][e], a, q[e][2 * w + h][0], q[e][2 * w + h][1]);
-          }
+            for (int k = 0; k < 2; ++k) {   // (the two halves' products one between the other: each waits for its own)
+              const uint32_t ua = h ? (&u[2 * k].x)[w] >> 8 : (&u[2 * k].x)[w];
+              const uint32_t ub = h ? (&u[2 * k + 1].x)[w] >> 8 : (&u[2 * k + 1].x)[w];
+              const uint32_t a[4] = {ua & 0x000f000fu, ub & 0x000f000fu, ua & 0x00f000f0u, ub & 0x00f000f0u};
+#pragma unroll
+              for (int e = 0; e < kHalves; ++e) mma_f16(s[k][e], a, q[e][2 * w + h][0], q[e][2 * w + h][1]);
+            }
       }
       copy_rest();
       __syncwarp();
