@@ -48,27 +48,33 @@ constexpr int kStageBytes = 2 * kCodeBytes;                // K, then V
 // R rows of a block on W warps of a CTA: 16 warps an SM for 8 rows, 12 for 16 (their registers). With fewer warps a CTA
 // the end of a part costs less, with more a block is cut into fewer parts: 8 warps where there are few blocks, else 4
 // (launch_cache4_attend).
+#ifndef WSM
+#define WSM 12
+#define W16 4
+#endif
 template <int R, int W>
 struct A4Cfg {
   static constexpr int kThreads = 32 * W;
   static constexpr int kStages = 3;
-  static constexpr int kCtas = (R == 8 ? 16 : 12) / W;
+  static constexpr int kCtas = (R == 8 ? 16 : WSM) / W;
   static constexpr int kTile = W * kStep;   // tokens: a step of every warp
   static constexpr int kPart = 3;           // what a part costs beside its own tiles
   static constexpr size_t kCtl = size_t(W) * kStages * kStageBytes;
 };
 
-// A part, tiles x .. end - 1 of block b, from token tok0 of its sequence on; steps first .. last - 1 of it are a warp's.
+// A part, tiles x .. end - 1 of block b, from token tok0 of its sequence on: `steps` steps, an even share of them a warp's.
 struct Part {
   Block b;
-  int x, end, tok0, first, last;
+  int x, end, tok0, steps;
   template <int W>
-  __device__ __forceinline__ void set(int x1, int warp) {
+  __device__ __forceinline__ void set(int x1) {
     end = min(x1, b.first + b.tiles);
     tok0 = (x - b.first) * (W * kStep);
-    const int steps = (min((end - b.first) * (W * kStep), b.len) - tok0 + kStep - 1) / kStep;
-    first = steps * warp / W;
-    last = steps * (warp + 1) / W;
+    steps = (min((end - b.first) * (W * kStep), b.len) - tok0 + kStep - 1) / kStep;
+  }
+  template <int W>
+  __device__ __forceinline__ int first(int warp) const {   // (of warp + 1: behind warp's last)
+    return steps * warp / W;
   }
 };
 
@@ -78,11 +84,13 @@ struct A4Ctl {
   alignas(128) uint32_t param[W][S][2][kStep];   // K's, V's
   float4 tokens[W][kStep];                       // of a step's tokens: K's s and z, V's log2 s and z
   LineCtl<W> line;
-  Part part[W], next[W], ahead[W];               // of a warp's sums, and of its copies
+  Part part[2];                                  // of the sums, by turns (all threads write the same)
+  Part ahead[W];                                 // of a warp's copies
   int at[W];                                     // the stage (its bytes in the ring) with the warp's rows at a part's end, or -1
   alignas(8) float m[W][8], l[W][8];             // of eight of the warps' rows, at the end of a part
-  float4 scale[W][R / 2];                        // of two rows: logits over products, sums of q in their units
-  int seen[W][R];                                // tokens that the row sees
+  uint4 q[R / 8][4][32];                         // the query rows of a part as operands: of eight rows, two k-steps, a lane
+  float4 scale[R / 2];                           // of two rows: logits over products, sums of q in their units
+  int seen[R];                                   // tokens that the row sees
   Block split[2];                                // parts left for the join
   int last[2];                                   // whether this CTA joins them
 };
@@ -189,7 +197,7 @@ cache_attend4_kernel(const __grid_constant__ AttendParams P) {
   const auto row_token = [&](int row) {
     return P.group_inverse ? static_cast<int>(__umulhi(static_cast<uint32_t>(row), P.group_inverse)) : row;
   };
-  int splits = 0;
+  int splits = 0, now = 0;
   uint8_t* const ring = smem + warp * (S * kStageBytes);
   // K: 16 bytes (t) of the tokens 8 i + g; V: row lane % 8, 16 bytes lane / 8 of eight tokens. A 16-byte chunk c of token r lies
   // at c ^ (r >> 1 & 3): neither meets on a bank
@@ -209,8 +217,8 @@ cache_attend4_kernel(const __grid_constant__ AttendParams P) {
       held = __ldg(P.table + static_cast<int64_t>(ahead.b.r) * P.c.max_pages + window + lane);
   };
   const auto enter = [&]() {
-    ahead_step = ahead.first;
-    ahead_last = ahead.last;
+    ahead_step = ahead.template first<W>(warp);
+    ahead_last = ahead.template first<W>(warp + 1);
     ahead_tok0 = ahead.tok0;
     ahead_head = ahead.b.h << shift;
     if (ahead_step < ahead_last) read_table();
@@ -224,7 +232,7 @@ cache_attend4_kernel(const __grid_constant__ AttendParams P) {
         return;
       }
       next_block(P, blocks, C::kTile, a.b);
-      a.template set<W>(x1, warp);
+      a.template set<W>(x1);
       __syncwarp();
       ahead = a;
       __syncwarp();
@@ -294,26 +302,9 @@ cache_attend4_kernel(const __grid_constant__ AttendParams P) {
       }
     }
   };
-  if (x0 < x1) {
-    Part a;
-    a.b = ctl.line.first;
-    a.x = x0;
-    a.template set<W>(x1, warp);
-    ctl.part[warp] = ahead = a;
-    __syncwarp();
-    enter();
-    load_rows(a.b);
-    settle();
-    find();
-    copy_keys();
-    copy_rest();
-  }
-  for (int x = x0; x < x1;) {
-    const Part& part = ctl.part[warp];
-    const Block& b = part.b;
-    const float lb = len_bits(b.len);
-    // ---------------------------------------------------------- the query rows
-    uint32_t q[kHalves][8][2];   // k-step, operand register
+  // A part's query rows as operands, in shared memory: every warp has them in `raw` and looks for their largest magnitudes; the
+  // conversion is dealt to the warps. (In registers they would be 32 of a thread's with 16 rows, and converted by all.)
+  const auto convert = [&](const Block& b) {
 #pragma unroll
     for (int e = 0; e < kHalves; ++e) {
       const uint32_t* u = &raw[e][0].x;
@@ -332,29 +323,47 @@ cache_attend4_kernel(const __grid_constant__ AttendParams P) {
       const int ex = static_cast<int>(most >> 23);
       const int up = min(14 + 127 - ex, 126);
       const float scale = __uint_as_float(static_cast<uint32_t>(up + 127) << 23);
-      if (t == 0) {
-        float* const to = reinterpret_cast<float*>(&ctl.scale[warp][(8 * e + g) / 2]) + (g & 1);
+      if (warp == W - 1 && t == 0) {
+        float* const to = reinterpret_cast<float*>(&ctl.scale[(8 * e + g) / 2]) + (g & 1);
         to[0] = P.alpha * __uint_as_float(static_cast<uint32_t>(min(24 - up, 127) + 127) << 23);
         to[2] = ex >= 127 + 112 ? __uint_as_float(0x7fc00000u) : sum * scale * 5.9604644775390625e-8f;   // 2^-24
         const int row = b.rb * R + 8 * e + g;
-        ctl.seen[warp][8 * e + g] = row < rows ? b.len - P.q_tokens + row_token(row) + 1 : 0;
+        ctl.seen[8 * e + g] = row < rows ? b.len - P.q_tokens + row_token(row) + 1 : 0;
       }
 #pragma unroll
       for (int w = 0; w < 4; ++w) {   // 8 elements: n and n + 4 go together
+        if (w % W != warp) continue;
         float f[8];
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
           f[2 * i] = low_bf16(u[4 * w + i]) * scale;
           f[2 * i + 1] = high_bf16(u[4 * w + i]) * scale;
         }
-#pragma unroll
-        for (int h = 0; h < 2; ++h) {
-          q[e][2 * w + h][0] = f16x2(f[2 * h], f[2 * h + 4]);
-          q[e][2 * w + h][1] = f16x2(f[2 * h + 1] * 0.0625f, f[2 * h + 5] * 0.0625f);
-        }
+        ctl.q[e][w][lane] = make_uint4(f16x2(f[0], f[4]), f16x2(f[1] * 0.0625f, f[5] * 0.0625f), f16x2(f[2], f[6]),
+                                       f16x2(f[3] * 0.0625f, f[7] * 0.0625f));
       }
     }
+  };
+  if (x0 < x1) {
+    Part a;
+    a.b = ctl.line.first;
+    a.x = x0;
+    a.template set<W>(x1);
+    ctl.part[0] = ahead = a;
     __syncwarp();
+    enter();
+    load_rows(a.b);
+    settle();
+    find();
+    copy_keys();
+    copy_rest();
+    convert(a.b);
+    __syncthreads();
+  }
+  for (int x = x0; x < x1;) {
+    const Part& part = ctl.part[now];
+    const Block& b = part.b;
+    const float lb = len_bits(b.len);
     if (x == x0) {   // (not before: the queries' exchanges would wait behind these copies)
 #pragma unroll 1
       for (int i = 1; i < S - 1; ++i) {
@@ -379,7 +388,7 @@ cache_attend4_kernel(const __grid_constant__ AttendParams P) {
       m[e] = top[e] = both(kNone);
       l[e] = z[e] = both(0.f);
     }
-    const int first = part.first, last = part.last, tok0 = part.tok0, all_see = b.len - P.q_tokens + 1;
+    const int first = part.template first<W>(warp), last = part.template first<W>(warp + 1), tok0 = part.tok0, all_see = b.len - P.q_tokens + 1;
 #pragma unroll 1
     for (int step = first; step < last; ++step) {
       copies_wait<S - 2>();
@@ -404,7 +413,10 @@ cache_attend4_kernel(const __grid_constant__ AttendParams P) {
 #pragma unroll
             for (int r = 0; r < 4; ++r) s[k][e][r] = 0.f;
 #pragma unroll
-        for (int w = 0; w < 4; ++w)
+        for (int w = 0; w < 4; ++w) {
+          uint4 q[kHalves];
+#pragma unroll
+          for (int e = 0; e < kHalves; ++e) q[e] = ctl.q[e][w][lane];
 #pragma unroll
           for (int h = 0; h < 2; ++h)
 #pragma unroll
@@ -413,8 +425,9 @@ cache_attend4_kernel(const __grid_constant__ AttendParams P) {
               const uint32_t ub = h ? (&u[2 * k + 1].x)[w] >> 8 : (&u[2 * k + 1].x)[w];
               const uint32_t a[4] = {ua & 0x000f000fu, ub & 0x000f000fu, ua & 0x00f000f0u, ub & 0x00f000f0u};
 #pragma unroll
-              for (int e = 0; e < kHalves; ++e) mma_f16(s[k][e], a, q[e][2 * w + h][0], q[e][2 * w + h][1]);
+              for (int e = 0; e < kHalves; ++e) mma_f16(s[k][e], a, h ? q[e].z : q[e].x, h ? q[e].w : q[e].y);
             }
+        }
       }
       copy_rest();
       __syncwarp();
@@ -426,7 +439,7 @@ cache_attend4_kernel(const __grid_constant__ AttendParams P) {
       float ls[4];
 #pragma unroll
       for (int e = 0; e < kHalves; ++e) {
-        const float4 c = ctl.scale[warp][4 * e + t];
+        const float4 c = ctl.scale[4 * e + t];
         kq[e] = make_float2(c.x, c.y);
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
@@ -439,7 +452,7 @@ cache_attend4_kernel(const __grid_constant__ AttendParams P) {
       if (some) {
 #pragma unroll
         for (int e = 0; e < kHalves; ++e) {
-          const int s0 = ctl.seen[warp][8 * e + 2 * t], s1 = ctl.seen[warp][8 * e + 2 * t + 1];
+          const int s0 = ctl.seen[8 * e + 2 * t], s1 = ctl.seen[8 * e + 2 * t + 1];
 #pragma unroll
           for (int i = 0; i < 4; ++i) {
             const int pos = pos0 + 8 * i + g;
@@ -590,9 +603,10 @@ cache_attend4_kernel(const __grid_constant__ AttendParams P) {
         Part a = part;
         a.x = next_x;
         next_block(P, blocks, C::kTile, a.b);
-        a.template set<W>(x1, warp);
+        a.template set<W>(x1);
         load_rows(a.b);
-        ctl.next[warp] = a;
+        ctl.part[now ^ 1] = a;
+        __syncwarp();
       }
       __syncthreads();
       for (int row = warp; row < 8; row += W) {
@@ -631,14 +645,13 @@ cache_attend4_kernel(const __grid_constant__ AttendParams P) {
         if (threadIdx.x == 0) ctl.split[splits] = b;
         ++splits;
       }
+      if (e + 1 == kHalves && next_x < x1) convert(ctl.part[now ^ 1].b);   // (no warp needs this part's rows any more)
       __syncthreads();   // the sums have been read
     }
     x = next_x;
-    if (x < x1) {
-      if (lane == 0) ctl.part[warp] = ctl.next[warp];
-      __syncwarp();
-    }
+    now ^= 1;
   }
+
   // sequences without a token: their rows are zeros
   for (int r = blockIdx.x * W + warp; r < P.n_seq; r += W * gridDim.x)
     if (seq_len(P, r) == 0)
@@ -782,7 +795,7 @@ cudaError_t attend4_rows(const kve_cache& c, const AttendParams& p, cudaStream_t
 }  // namespace
 
 cudaError_t launch_cache4_attend(const kve_cache& c, const AttendParams& p, cudaStream_t stream) {
-  if (p.q_tokens * p.c.group > 8) return attend4_rows<16, 4>(c, p, stream);
+  if (p.q_tokens * p.c.group > 8) return attend4_rows<16, W16>(c, p, stream);
   // two CTAs an SM have a block each without cutting one
   const bool many = static_cast<int64_t>(p.n_seq) * p.c.heads >= 2 * c.sms;
   return many ? attend4_rows<8, 4>(c, p, stream) : attend4_rows<8, 8>(c, p, stream);
