@@ -543,8 +543,10 @@ cache_attend4_kernel(const __grid_constant__ AttendParams P) {
         for (int i = 0; i < 4; ++i)
 #pragma unroll
           for (int h = 0; h < 2; ++h) {
-            const uint32_t ua = h ? c0[i] >> 8 : c0[i], ub = h ? c1[i] >> 8 : c1[i];
-            const uint32_t a[4] = {ua & 0x000f000fu, ua & 0x00f000f0u, ub & 0x000f000fu, ub & 0x00f000f0u};
+            // low codes, and low + 16 high ones: the end takes the former's sum out of the latter's
+            const uint32_t ua = h ? __byte_perm(c0[i], 0, 0x4341) : c0[i] & 0x00ff00ffu;
+            const uint32_t ub = h ? __byte_perm(c1[i], 0, 0x4341) : c1[i] & 0x00ff00ffu;
+            const uint32_t a[4] = {ua & 0x000f000fu, ua, ub & 0x000f000fu, ub};
 #pragma unroll
             for (int e = 0; e < kHalves; ++e) mma_f16(o[2 * i + h][e], a, w[2 * k][e], w[2 * k + 1][e]);
           }
@@ -588,9 +590,9 @@ cache_attend4_kernel(const __grid_constant__ AttendParams P) {
           for (int i = 0; i < 4; ++i) {
             float4 v;
             v.x = fmaf(o[2 * i][e][j] * 65536.f, f[j], zq[j]);
-            v.y = fmaf(o[2 * i][e][2 + j] * 4096.f, f[j], zq[j]);
+            v.y = fmaf((o[2 * i][e][2 + j] - o[2 * i][e][j]) * 4096.f, f[j], zq[j]);
             v.z = fmaf(o[2 * i + 1][e][j] * 65536.f, f[j], zq[j]);
-            v.w = fmaf(o[2 * i + 1][e][2 + j] * 4096.f, f[j], zq[j]);
+            v.w = fmaf((o[2 * i + 1][e][2 + j] - o[2 * i + 1][e][j]) * 4096.f, f[j], zq[j]);
             // columns 32 i + 4 g of row 2 t + j; 16 bytes c of row r lie at c ^ (r & 6)
             reinterpret_cast<float4*>(mine + (2 * t + j) * kHeadDim)[(8 * i + g) ^ (2 * t)] = v;
           }
