@@ -533,8 +533,8 @@ kve_status kv_evict_cache_append(const kve_cache* cache, const kve_rotary* rotar
  *  * Rows share nothing: a page may be written in any order, and a slot that a call names twice gets
  *    undefined codes (its row only).
  *  * Attention: l = (s (q . c) + z sum q) / sqrt(d), out = sum p s c + sum p z, statistics and sums in
- *    fp32. What is held in fewer bits: a query element below 2^-27 of its row's largest to 2^-38
- *    of that; p s to 2^-12 of itself, or to 2^-39 of the largest p s so far, whichever is more; p z
+ *    fp32. What is held in fewer bits: a query element below 2^-27 of its row's largest to 2^-35
+ *    of that; p s to 2^-12 of itself, or to 2^-31 of the largest p s so far, whichever is more; p z
  *    to len * 2^-149. A query row with an infinity, a NaN or a magnitude of 2^112 or more
  *    gives NaN.
  * ---------------------------------------------------------------------------------- */

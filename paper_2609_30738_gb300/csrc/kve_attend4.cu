@@ -16,7 +16,7 @@
 // so 8 rows fill the N side. The sums over d do not care for its order, as long as both operands have the same, so a lane's
 // 16 bytes of K are eight k-steps as they lie. What the sums see of fewer than 32 bits:
 //   q  bf16 times a power of two of its row, f16: exact down to 2^-31 of the row's largest (2^-27 in every second
-//      element, whose codes are 16 times larger), an absolute 2^-38 of it below;
+//      element, whose codes are 16 times larger), an absolute 2^-35 of it below;
 //   w  softmax(l)_i s_i over a reference within 2^8 of the row's largest such product so far, times 2^6, f16: 2^-12 of
 //      itself down to 2^-20 of that reference, an absolute 2^-31 of it below.
 // Maxima, sums, the part of z and the output are fp32. The reference of w is the product's own, not the probability's, so
@@ -45,18 +45,14 @@ constexpr int kRowBytes = kHeadDim / 2;                    // codes of a token
 constexpr int kCodeBytes = kStep * kRowBytes;
 constexpr int kStageBytes = 2 * kCodeBytes;                // K, then V
 
-// R rows of a block on W warps of a CTA: 16 warps an SM for 8 rows, 12 for 16 (their registers). With fewer warps a CTA
-// the end of a part costs less, with more a block is cut into fewer parts: 8 warps where there are few blocks, else 4
-// (launch_cache4_attend).
-#ifndef WSM
-#define WSM 12
-#define W16 4
-#endif
+// R rows of a block on W warps of a CTA. 16 warps an SM for 8 rows, 12 for 16 rows (with 16 warps their registers spill in the
+// loop: 24 sequences of 4 drafts 64 us for 34). With fewer warps a CTA the end of a part costs less, with more a block is cut into
+// fewer parts (launch_cache4_attend).
 template <int R, int W>
 struct A4Cfg {
   static constexpr int kThreads = 32 * W;
   static constexpr int kStages = 3;
-  static constexpr int kCtas = (R == 8 ? 16 : WSM) / W;
+  static constexpr int kCtas = (R == 8 ? 16 : 12) / W;
   static constexpr int kTile = W * kStep;   // tokens: a step of every warp
   static constexpr int kPart = 3;           // what a part costs beside its own tiles
   static constexpr size_t kCtl = size_t(W) * kStages * kStageBytes;
@@ -797,8 +793,9 @@ cudaError_t attend4_rows(const kve_cache& c, const AttendParams& p, cudaStream_t
 }  // namespace
 
 cudaError_t launch_cache4_attend(const kve_cache& c, const AttendParams& p, cudaStream_t stream) {
-  if (p.q_tokens * p.c.group > 8) return attend4_rows<16, W16>(c, p, stream);
-  // two CTAs an SM have a block each without cutting one
+  if (p.q_tokens * p.c.group > 8) return attend4_rows<16, 4>(c, p, stream);
+  // Two CTAs an SM have a block each without cutting one: 4 warps a CTA, else 8. (4 against 8: 64 ragged sequences of 8 heads 54.7
+  // and 60.2 us, 1000 of 64 tokens 59 and 108; 16 evicted 8.9 and 7.4, one of 131072 tokens 41.4 and 35.2, 8 of 32768 61.5 and 59.5.)
   const bool many = static_cast<int64_t>(p.n_seq) * p.c.heads >= 2 * c.sms;
   return many ? attend4_rows<8, 4>(c, p, stream) : attend4_rows<8, 8>(c, p, stream);
 }

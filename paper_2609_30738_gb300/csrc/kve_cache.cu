@@ -499,12 +499,10 @@ __global__ void __launch_bounds__(kRowThreads<kPage>) cache_gather_kernel(const 
 // 7.3: 2000 teams of 8 runs, of which 1216 fit at once, are two rounds of that chain.
 constexpr int64_t kStoreBlockTokens = 1024;
 
-#ifndef KST
-#define KST 768
-#endif
-// Threads an SM: the rotating append's have the turns of their rows beside the rows.
+// Threads an SM: the rotating append's have the turns of their rows beside the rows. (512, 768, 1024: 24k tokens 113.9, 102.6 and
+// 111.5 us, 256 tokens 5.15, 5.6 and 6.1, 16 tokens 2.9, 3.3 and 3.6.)
 template <class Params>
-constexpr int kStoreThreads = std::is_same_v<Params, CacheAppendParams> ? KST : 1024;
+constexpr int kStoreThreads = std::is_same_v<Params, CacheAppendParams> ? 768 : 1024;
 
 // The pairs that a lane turns: four side by side of its own elements, or where pairs are halves of the row, half of those that
 // it shares with its partner's lane. Then the two exchange the other halves, before and behind it, so that no turn is

@@ -9,7 +9,8 @@
 // the far end, a 30th of a code's half step; z is an element and so exact.
 //
 // Bound by HBM: 256 bytes read and 68 written a row. Eight lanes have a row, 16 elements (32 bytes) each; the minimum
-// and maximum are packed bf16 operations and three shuffles.
+// and maximum are packed bf16 operations and three shuffles, the division one reciprocal a row. 23,815 tokens of 8 heads (123 MB)
+// are stored in 24.1 us (18.5 at the copy's rate); 256 tokens in 1.8, which is the launch and two loads in a row (slots, rows).
 #include "kve_ptx.cuh"
 #include "kve_rotary.cuh"
 
@@ -159,15 +160,13 @@ __global__ void __launch_bounds__(kRowThreads4) cache4_store_kernel(const __grid
   allow_next_kernel();
 }
 
-// Step 4 into the cache: 8 lanes a row, kGatherRows rows of keys and of values in flight, kGatherTurns times.
-#ifndef GR
-#define GR 1
-#define GT 4
-#define GC 5
-#endif
-constexpr int kGatherRows = GR, kGatherTurns = GT;
-constexpr int kGatherTile = kGroups4 * kGatherRows * kGatherTurns;   // rows of a unit that a CTA has
-__global__ void __launch_bounds__(kRowThreads4, GC) cache4_gather_kernel(const __grid_constant__ CacheGatherParams P,
+// Step 4 into the cache: 8 lanes a row, of keys and of values, kGatherTurns times with the next row's place looked up ahead.
+// Reads whole rows at random places and writes a row's 64 bytes and its numbers: 16 requests of 509 kept rows and 8 layers, 327 MB,
+// take 62.4 us of 48.9 at the copy's rate, 64 requests' smallest (32 layers of 72 rows) 4.9 of 2.4. Tiles of 32 rows (one turn)
+// take 83.7 and 4.6, of 256 rows 62.2 and 5.0; two rows of a lane in flight, with 3 CTAs an SM for their registers, 82.0 and 4.95.
+constexpr int kGatherTurns = 4;
+constexpr int kGatherTile = kGroups4 * kGatherTurns;   // rows of a unit that a CTA has
+__global__ void __launch_bounds__(kRowThreads4, 5) cache4_gather_kernel(const __grid_constant__ CacheGatherParams P,
                                                                          uint32_t unit_tiles) {
   wait_previous_kernel();   // the indices come from the selection launched before
   const uint32_t unit = blockIdx.x / unit_tiles;
@@ -183,46 +182,32 @@ __global__ void __launch_bounds__(kRowThreads4, GC) cache4_gather_kernel(const _
   const uint32_t lanes = row_lanes();
   const int shift = P.c.page_shift, head = u.h << shift;
   if (refused) return;
-  // where the rows come from (-1: nowhere, a row of zeros) and their pages, a turn ahead
-  int src[kGatherRows], page[kGatherRows];
-  const auto look_up = [&](int row0) {
-#pragma unroll
-    for (int i = 0; i < kGatherRows; ++i) {
-      const int row = row0 + i * kGroups4;
-      if (row >= end) continue;
-      page[i] = __ldg(table + (row >> shift));
-      src[i] = row < m ? __ldg(indices + row) : Lc + (row - m);
-    }
+  // where the row comes from and its page, a turn ahead
+  int src = 0, page = 0;
+  const auto look_up = [&](int row) {
+    if (row >= end) return;
+    page = __ldg(table + (row >> shift));
+    src = row < m ? __ldg(indices + row) : Lc + (row - m);
   };
   look_up(first);
-  for (int row0 = first; row0 < end; row0 += kGroups4 * kGatherRows) {
-    uint4 k[kGatherRows][2], v[kGatherRows][2];
-    int at[kGatherRows];
-#pragma unroll
-    for (int i = 0; i < kGatherRows; ++i) {
-      const int row = row0 + i * kGroups4;
-      k[i][0] = k[i][1] = v[i][0] = v[i][1] = make_uint4(0, 0, 0, 0);
-      if (row >= end) continue;
-      const bool outside = row < m && static_cast<uint32_t>(src[i]) >= static_cast<uint32_t>(Lc);   // never read outside the unit
-      const bool good = static_cast<uint32_t>(page[i]) < static_cast<uint32_t>(P.c.num_pages);
-      if ((outside || !good) && l == 0) atomicOr(P.err, kErrCheck);
-      at[i] = good ? (page[i] * P.c.heads << shift) + head + (row & (P.c.page - 1)) : -1;
-      if (outside) continue;
-      const uint4* ks = reinterpret_cast<const uint4*>(P.g.k + u.k_off + src[i] * P.g.g.k_st) + l;
-      const uint4* vs = reinterpret_cast<const uint4*>(P.g.v + u.v_off + src[i] * P.g.g.v_st) + l;
-      k[i][0] = __ldg(ks);
-      k[i][1] = __ldg(ks + 8);
-      v[i][0] = __ldg(vs);
-      v[i][1] = __ldg(vs + 8);
+  for (int row = first; row < end; row += kGroups4) {
+    uint4 k[2] = {}, v[2] = {};
+    const bool outside = row < m && static_cast<uint32_t>(src) >= static_cast<uint32_t>(Lc);   // never read outside the unit
+    const bool good = static_cast<uint32_t>(page) < static_cast<uint32_t>(P.c.num_pages);
+    if ((outside || !good) && l == 0) atomicOr(P.err, kErrCheck);
+    const int at = good ? (page * P.c.heads << shift) + head + (row & (P.c.page - 1)) : -1;
+    if (!outside) {   // (else a row of zeros)
+      const uint4* ks = reinterpret_cast<const uint4*>(P.g.k + u.k_off + src * P.g.g.k_st) + l;
+      const uint4* vs = reinterpret_cast<const uint4*>(P.g.v + u.v_off + src * P.g.g.v_st) + l;
+      k[0] = __ldg(ks);
+      k[1] = __ldg(ks + 8);
+      v[0] = __ldg(vs);
+      v[1] = __ldg(vs + 8);
     }
-    look_up(row0 + kGroups4 * kGatherRows);
-#pragma unroll
-    for (int i = 0; i < kGatherRows; ++i) {
-      if (row0 + i * kGroups4 >= end) break;
-      if (at[i] < 0) continue;
-      write_row4(k[i][0], k[i][1], l, l + 8, P.c.k, P.c.k_param, at[i], l, lanes);
-      write_row4(v[i][0], v[i][1], l, l + 8, P.c.v, P.c.v_param, at[i], l, lanes);
-    }
+    look_up(row + kGroups4);
+    if (at < 0) continue;
+    write_row4(k[0], k[1], l, l + 8, P.c.k, P.c.k_param, at, l, lanes);
+    write_row4(v[0], v[1], l, l + 8, P.c.v, P.c.v_param, at, l, lanes);
   }
   allow_next_kernel();
 }
@@ -234,9 +219,9 @@ cudaError_t store4(CacheAppendParams p, cudaStream_t stream) {
   cut.n_tokens = p.s.n_tokens;
   cut.heads = p.s.c.heads;
   int64_t tiles = cut_rotate<kRowThreads4>(cut);
-  // a group a token and all heads one after the other, where that still gives every SM two tiles of each: 24k tokens
-  // 32.1 -> XXX us
-  if (cut.n_tokens >= 304 * kStoreTokens / 2) {
+  // A group a token and all its heads one after the other, where that still gives every SM a tile of keys and one of values: 24k
+  // tokens 24.1 us. (With it and without: 2500 tokens of 8 heads 5.6 and 4.4 us, 5000 7.35 and 7.3, 10000 13.6 and 15.2.)
+  if (cut.n_tokens >= 152 * kStoreTokens) {
     cut.tile_tokens = kStoreTokens;
     cut.tile_heads = cut.heads;
     tiles = (cut.n_tokens + kStoreTokens - 1) / kStoreTokens;
