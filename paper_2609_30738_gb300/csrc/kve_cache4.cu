@@ -57,15 +57,16 @@ __device__ __forceinline__ uint32_t codes_of(const uint4& x, float z16, float in
   return out - 0x4b400000u * 0x11111111u;
 }
 
-// Writes row `row` that 8 lanes hold in the chunks ca and cb: its codes, and in lane l = 0 its s and z.
+// Writes row `row` (negative: nothing) that 8 lanes hold in the chunks ca and cb: its codes, and in lane l = 0 its s and z. Whole
+// warps call it: shuffles under a mask of some lanes only cost more than the rows that are not there.
 __device__ __forceinline__ void write_row4(const uint4& a, const uint4& b, int ca, int cb, uint8_t* codes, uint32_t* param,
-                                           int row, int l, uint32_t lanes) {
+                                           int row, int l) {
   const uint32_t lo = min2(min2(min2(a.x, a.y), min2(a.z, a.w)), min2(min2(b.x, b.y), min2(b.z, b.w))) ^ 0x80008000u;
   const uint32_t hi = max2(max2(max2(a.x, a.y), max2(a.z, a.w)), max2(max2(b.x, b.y), max2(b.z, b.w)));
   // the largest in the low half, minus the least in the high half
   uint32_t ends = max2(__byte_perm(hi, lo, 0x5410), __byte_perm(hi, lo, 0x7632));
 #pragma unroll
-  for (int o = 4; o > 0; o >>= 1) ends = max2(ends, __shfl_xor_sync(lanes, ends, o));
+  for (int o = 4; o > 0; o >>= 1) ends = max2(ends, __shfl_xor_sync(0xffffffffu, ends, o));
   const bool finite = (ends & 0x7f80u) != 0x7f80u && (ends & 0x7f800000u) != 0x7f800000u;
   // in units of 16, so that no difference overflows
   const float less = bf16_high(ends), z16 = less * -0.0625f;
@@ -75,13 +76,13 @@ __device__ __forceinline__ void write_row4(const uint4& a, const uint4& b, int c
   const float unit = bf16_low(s) * 0.0625f;
   const bool spread = finite && unit > 0.f;
   const float inverse = rcp(unit), rest = fmaf(-unit, inverse, 1.f) * inverse;
+  const uint32_t first = spread ? codes_of(a, z16, inverse, rest) : 0u, second = spread ? codes_of(b, z16, inverse, rest) : 0u;
+  if (row < 0) return;
   uint32_t* const to = reinterpret_cast<uint32_t*>(codes + static_cast<int64_t>(row) * kRowCodes);
-  to[ca] = spread ? codes_of(a, z16, inverse, rest) : 0u;
-  to[cb] = spread ? codes_of(b, z16, inverse, rest) : 0u;
+  to[ca] = first;
+  to[cb] = second;
   if (l == 0) param[row] = finite ? s : 0x7fc07fc0u;
 }
-
-__device__ __forceinline__ uint32_t row_lanes() { return 0xffu << (threadIdx.x & 24); }
 
 // New tokens by slot. A tile is up to kStoreTokens tokens by some heads of keys or of values (the two alternate). With kTurn
 // the first tiles turn the queries, and keys are turned (and rounded to bf16) before they are coded.
@@ -141,18 +142,18 @@ __global__ void __launch_bounds__(kRowThreads4) cache4_store_kernel(const __grid
   }
   const int limit = P.c.num_pages << P.c.page_shift;   // (below 2^31)
   if (slot >= limit && l == 0 && group / tile_tokens == 0) atomicOr(P.err, kErrCheck);
-  if (slot < 0 || slot >= limit) return;
+  const bool kept = slot >= 0 && slot < limit;
   // rows of the pool are below 2^31
   const int row0 = ((slot >> P.c.page_shift) * H << P.c.page_shift) + (slot & (P.c.page - 1));
-  const uint32_t lanes = row_lanes();
-  while (h < end) {
+  while (__any_sync(0xffffffffu, kept && h < end)) {
 #pragma unroll
     for (int i = 0; i < kInFlight; ++i) {
-      if (h + i * step >= end) break;
+      const bool there = kept && h + i * step < end;
+      if (!__any_sync(0xffffffffu, there)) break;
       if constexpr (kTurn) {
         if (key) turn_chunks(a[i], b[i], cs, kc, A.turn.r.interleaved);
       }
-      write_row4(a[i], b[i], kc.a, kc.b, codes, param, row0 + ((h + i * step) << P.c.page_shift), l, lanes);
+      write_row4(a[i], b[i], kc.a, kc.b, codes, param, there ? row0 + ((h + i * step) << P.c.page_shift) : -1, l);
     }
     h += kInFlight * step;
     load(h);
@@ -179,7 +180,6 @@ __global__ void __launch_bounds__(kRowThreads4, 5) cache4_gather_kernel(const __
   const bool refused = __ldg(P.refused) != 0;   // the table's pages may be other sequences' by now
   const int32_t* const table = P.table + (static_cast<int64_t>(u.layer) * P.c.max_seqs + P.first_seq + u.r) * P.c.max_pages;
   const int32_t* const indices = P.g.indices + static_cast<int64_t>(unit) * P.g.budget;
-  const uint32_t lanes = row_lanes();
   const int shift = P.c.page_shift, head = u.h << shift;
   if (refused) return;
   // where the row comes from and its page, a turn ahead
@@ -190,13 +190,14 @@ __global__ void __launch_bounds__(kRowThreads4, 5) cache4_gather_kernel(const __
     src = row < m ? __ldg(indices + row) : Lc + (row - m);
   };
   look_up(first);
-  for (int row = first; row < end; row += kGroups4) {
+  for (int row = first; row - (group & 3) < end; row += kGroups4) {   // (the warp's first row)
     uint4 k[2] = {}, v[2] = {};
+    const bool there = row < end;
     const bool outside = row < m && static_cast<uint32_t>(src) >= static_cast<uint32_t>(Lc);   // never read outside the unit
     const bool good = static_cast<uint32_t>(page) < static_cast<uint32_t>(P.c.num_pages);
-    if ((outside || !good) && l == 0) atomicOr(P.err, kErrCheck);
-    const int at = good ? (page * P.c.heads << shift) + head + (row & (P.c.page - 1)) : -1;
-    if (!outside) {   // (else a row of zeros)
+    if (there && (outside || !good) && l == 0) atomicOr(P.err, kErrCheck);
+    const int at = there && good ? (page * P.c.heads << shift) + head + (row & (P.c.page - 1)) : -1;
+    if (there && !outside) {   // (else a row of zeros)
       const uint4* ks = reinterpret_cast<const uint4*>(P.g.k + u.k_off + src * P.g.g.k_st) + l;
       const uint4* vs = reinterpret_cast<const uint4*>(P.g.v + u.v_off + src * P.g.g.v_st) + l;
       k[0] = __ldg(ks);
@@ -205,9 +206,8 @@ __global__ void __launch_bounds__(kRowThreads4, 5) cache4_gather_kernel(const __
       v[1] = __ldg(vs + 8);
     }
     look_up(row + kGroups4);
-    if (at < 0) continue;
-    write_row4(k[0], k[1], l, l + 8, P.c.k, P.c.k_param, at, l, lanes);
-    write_row4(v[0], v[1], l, l + 8, P.c.v, P.c.v_param, at, l, lanes);
+    write_row4(k[0], k[1], l, l + 8, P.c.k, P.c.k_param, at, l);
+    write_row4(v[0], v[1], l, l + 8, P.c.v, P.c.v_param, at, l);
   }
   allow_next_kernel();
 }
