@@ -551,22 +551,21 @@ __device__ __forceinline__ void turn_rows(uint4 (&x)[kGroupRows], const RotaryTa
 }
 
 //
-// With parameters of the rotating append the first CTAs (turn_tiles) turn the queries, and the others turn the keys on their
-// way. (One body with the plain store as a kernel of its own: as a function of both it spilled three times as much.)
+// With parameters of the rotating append the CTAs behind the first row_ctas turn the queries, and those turn the keys on their
+// way: they start first because they take longer (as the last: 2000 tokens 14.8 us for 11.7, 1000 x 8 23.1 for 20.1, 24k 102.6
+// for 101.9; evenly between the others 13.6, 24.5 and 112). (One body with the plain store as a kernel of its own: as a function of both it spilled three times as much.)
 template <int kPage, class Params>
 __global__ void __launch_bounds__(kRowThreads<kPage>, kStoreThreads<Params> / kRowThreads<kPage>)
-cache_store_kernel(const __grid_constant__ Params A, uint32_t turn_tiles) {
+cache_store_kernel(const __grid_constant__ Params A, uint32_t row_ctas) {
   constexpr bool kTurn = std::is_same_v<Params, CacheAppendParams>;
   wait_previous_kernel();
-  uint32_t tile = blockIdx.x;
   if constexpr (kTurn) {
     __shared__ __align__(16) float2 turns[kTurnTokens * kMaxPairs];
-    if (tile < turn_tiles) {
-      rotate_tile<kRowThreads<kPage>>(A.turn, tile, turns);
+    if (blockIdx.x >= row_ctas) {
+      rotate_tile<kRowThreads<kPage>>(A.turn, blockIdx.x - row_ctas, turns);
       allow_next_kernel();
       return;
     }
-    tile -= turn_tiles;
   }
   const CacheStoreParams& P = [&]() -> const CacheStoreParams& {
     if constexpr (kTurn)
@@ -581,7 +580,7 @@ cache_store_kernel(const __grid_constant__ Params A, uint32_t turn_tiles) {
   __shared__ uint16_t runs[kRowThreads<kPage> / 32][kPage];   // first token << 8 | tokens: long, from the end short
   const int team = threadIdx.x / kTeam, lane = threadIdx.x & 15, g = (threadIdx.x / 16) % kGroups;
   const int warp = threadIdx.x >> 5, lane32 = threadIdx.x & 31;
-  const int64_t item = static_cast<int64_t>(tile) * kTeams + team;
+  const int64_t item = static_cast<int64_t>(blockIdx.x) * kTeams + team;
   const int H = P.c.heads;
   const int64_t first = item / (2 * H) * P.block;
   if (first >= P.n_tokens) return;   // the whole team
@@ -702,9 +701,9 @@ cudaError_t store_paged(const CacheStoreParams& p, cudaStream_t stream) {
 template <int kPage>
 cudaError_t append_paged(const CacheAppendParams& params, cudaStream_t stream) {
   CacheAppendParams p = params;
-  const int64_t turn_tiles = p.turn.heads > 0 ? cut_rotate<kRowThreads<kPage>>(p.turn) : 0;
-  return launch_after_previous(cache_store_kernel<kPage, CacheAppendParams>, dim3(static_cast<unsigned>(turn_tiles + store_ctas<kPage>(p.s))),
-                               dim3(kRowThreads<kPage>), 0, stream, p, static_cast<uint32_t>(turn_tiles));
+  const int64_t turn_tiles = p.turn.heads > 0 ? cut_rotate<kRowThreads<kPage>>(p.turn) : 0, row_ctas = store_ctas<kPage>(p.s);
+  return launch_after_previous(cache_store_kernel<kPage, CacheAppendParams>, dim3(static_cast<unsigned>(row_ctas + turn_tiles)),
+                               dim3(kRowThreads<kPage>), 0, stream, p, static_cast<uint32_t>(row_ctas));
 }
 
 template <int kPage>

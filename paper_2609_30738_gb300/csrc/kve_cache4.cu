@@ -85,21 +85,20 @@ __device__ __forceinline__ void write_row4(const uint4& a, const uint4& b, int c
 }
 
 // New tokens by slot. A tile is up to kStoreTokens tokens by some heads of keys or of values (the two alternate). With kTurn
-// the first tiles turn the queries, and keys are turned (and rounded to bf16) before they are coded.
+// the last tiles turn the queries, and keys are turned (and rounded to bf16) before they are coded.
 template <bool kTurn>
 __global__ void __launch_bounds__(kRowThreads4) cache4_store_kernel(const __grid_constant__ CacheAppendParams A, int tile_tokens,
-                                                                    int tile_heads, uint32_t turn_tiles) {
+                                                                    int tile_heads, uint32_t row_tiles) {
   wait_previous_kernel();
   __shared__ __align__(16) float2 turns[kTurn ? kStoreTokens * kMaxPairs : 1];
   const CacheStoreParams& P = A.s;
   uint32_t tile = blockIdx.x;
   if constexpr (kTurn) {
-    if (tile < turn_tiles) {
-      rotate_tile<kRowThreads4>(A.turn, tile, turns);
+    if (tile >= row_tiles) {
+      rotate_tile<kRowThreads4>(A.turn, tile - row_tiles, turns);
       allow_next_kernel();
       return;
     }
-    tile -= turn_tiles;
   }
   const int H = P.c.heads;
   const bool key = (tile & 1) == 0;
@@ -228,7 +227,7 @@ cudaError_t store4(CacheAppendParams p, cudaStream_t stream) {
   }
   tiles *= 2;   // of keys, and as many of values
   return launch_after_previous(cache4_store_kernel<kTurn>, dim3(static_cast<unsigned>(turn_tiles + tiles)), dim3(kRowThreads4), 0,
-                               stream, p, cut.tile_tokens, cut.tile_heads, static_cast<uint32_t>(turn_tiles));
+                               stream, p, cut.tile_tokens, cut.tile_heads, static_cast<uint32_t>(tiles));
 }
 
 }  // namespace
