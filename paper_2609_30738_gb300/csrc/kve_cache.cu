@@ -1037,6 +1037,10 @@ kve_status kv_evict_cache_append(const kve_cache* cache, const kve_rotary* rotar
     p.turn.heads = hq;
   }
   if (n_tokens == 0) return KVE_OK;
+  if (q) {   // the cache's device, or an address that the driver does not know
+    const int device = place_of(q_out);
+    if (device == kHostMemory || (device >= 0 && cache->device >= 0 && device != cache->device)) return KVE_EINVAL;
+  }
   p.turn.r = rotary->table;
   p.turn.x = q;
   p.turn.out = q_out;

@@ -706,7 +706,7 @@ class Cache8:
             q_out = q if q_out is None else q_out
             if q.numel() != n * self.num_q_heads * self.head_dim or q_out.shape != q.shape:
                 raise ValueError("append: q and q_out hold a row of every query head for each token")
-            if not self._here(q) or not self._here(q_out):
+            if not self._here(q) or q_out.get_device() != self._device:
                 raise ValueError("append: q and q_out are on the cache's device")
             qs, outs = _row_strides(q, self.num_q_heads, "q"), _row_strides(q_out, self.num_q_heads, "q_out")
         elif q_out is not None:

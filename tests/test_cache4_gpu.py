@@ -179,7 +179,7 @@ def test_append_checks_its_tensors():
     s = p = _i32([0, 1, 2])
     for bad in (dict(positions=p[:2]), dict(positions=p.long()), dict(positions=p.cpu()), dict(q=q[:2]),
                 dict(q=q.float()), dict(q_out=q), dict(q=q, q_out=q[:, :4]), dict(k_new=k[:2]), dict(v_new=k.float()),
-                dict(k_new=k.cpu()), dict(slots=s.long()), dict(q=q.cpu())):
+                dict(k_new=k.cpu()), dict(slots=s.long()), dict(q=q.cpu()), dict(q=q, q_out=q.cpu().pin_memory())):
         a = dict(positions=p, k_new=k, v_new=k, slots=s)
         a.update(bad)
         with pytest.raises(ValueError):
