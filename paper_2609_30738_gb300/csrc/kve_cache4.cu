@@ -8,9 +8,9 @@
 // touches no older one. s is rounded to 8 bits because c is chosen with the rounded s: it costs a 2^-9 of the range at
 // the far end, a 30th of a code's half step; z is an element and so exact.
 //
-// Bound by HBM: 256 bytes read and 68 written a row. Eight lanes have a row, 16 elements (32 bytes) each; the minimum
-// and maximum are packed bf16 operations and three shuffles, the division one reciprocal a row. 23,815 tokens of 8 heads (123 MB)
-// are stored in 24.1 us (18.5 at the copy's rate); 256 tokens in 1.8, which is the launch and two loads in a row (slots, rows).
+// Bound by HBM: 256 bytes read and 68 written a row. Four lanes have a row, 64 bytes each as two pieces of 32 (with turns eight, as
+// the pairs lie); the minimum and maximum are packed bf16 operations and two shuffles, the division one reciprocal a row. What a row
+// costs beside its elements is half of the instructions, so few lanes a row and many rows an SM.
 #include "kve_ptx.cuh"
 #include "kve_rotary.cuh"
 
@@ -18,9 +18,8 @@ namespace kve {
 namespace {
 
 constexpr int kRowThreads4 = 256;
-constexpr int kGroups4 = kRowThreads4 / 8;
 constexpr int kRowCodes = kHeadDim / 2;   // bytes
-constexpr int kStoreTokens = kGroups4;    // most tokens of a tile
+constexpr int kStoreTokens = 32;          // most tokens of a tile
 
 __device__ __forceinline__ uint32_t min2(uint32_t a, uint32_t b) {
   uint32_t d;
@@ -57,16 +56,22 @@ __device__ __forceinline__ uint32_t codes_of(const uint4& x, float z16, float in
   return out - 0x4b400000u * 0x11111111u;
 }
 
-// Writes row `row` (negative: nothing) that 8 lanes hold in the chunks ca and cb: its codes, and in lane l = 0 its s and z. Whole
-// warps call it: shuffles under a mask of some lanes only cost more than the rows that are not there.
-__device__ __forceinline__ void write_row4(const uint4& a, const uint4& b, int ca, int cb, uint8_t* codes, uint32_t* param,
-                                           int row, int l) {
-  const uint32_t lo = min2(min2(min2(a.x, a.y), min2(a.z, a.w)), min2(min2(b.x, b.y), min2(b.z, b.w))) ^ 0x80008000u;
-  const uint32_t hi = max2(max2(max2(a.x, a.y), max2(a.z, a.w)), max2(max2(b.x, b.y), max2(b.z, b.w)));
+// The codes of row `row` (negative: nothing) that 16 / N lanes hold, N chunks of 8 elements each, and in lane l = 0 its s and z.
+// Whole warps come here: shuffles under a mask of some lanes only cost more than the rows that are not there.
+template <int N>
+__device__ __forceinline__ void row_codes4(const uint4 (&x)[N], uint32_t (&c)[N], uint32_t* param, int row, int l) {
+  uint32_t lo = 0, hi = 0;
+#pragma unroll
+  for (int i = 0; i < N; ++i) {
+    const uint32_t a = min2(min2(x[i].x, x[i].y), min2(x[i].z, x[i].w)), b = max2(max2(x[i].x, x[i].y), max2(x[i].z, x[i].w));
+    lo = i ? min2(lo, a) : a;
+    hi = i ? max2(hi, b) : b;
+  }
+  lo ^= 0x80008000u;
   // the largest in the low half, minus the least in the high half
   uint32_t ends = max2(__byte_perm(hi, lo, 0x5410), __byte_perm(hi, lo, 0x7632));
 #pragma unroll
-  for (int o = 4; o > 0; o >>= 1) ends = max2(ends, __shfl_xor_sync(0xffffffffu, ends, o));
+  for (int o = 8 / N; o > 0; o >>= 1) ends = max2(ends, __shfl_xor_sync(0xffffffffu, ends, o));
   const bool finite = (ends & 0x7f80u) != 0x7f80u && (ends & 0x7f800000u) != 0x7f800000u;
   // in units of 16, so that no difference overflows
   const float less = bf16_high(ends), z16 = less * -0.0625f;
@@ -76,18 +81,30 @@ __device__ __forceinline__ void write_row4(const uint4& a, const uint4& b, int c
   const float unit = bf16_low(s) * 0.0625f;
   const bool spread = finite && unit > 0.f;
   const float inverse = rcp(unit), rest = fmaf(-unit, inverse, 1.f) * inverse;
-  const uint32_t first = spread ? codes_of(a, z16, inverse, rest) : 0u, second = spread ? codes_of(b, z16, inverse, rest) : 0u;
-  if (row < 0) return;
+#pragma unroll
+  for (int i = 0; i < N; ++i) c[i] = spread ? codes_of(x[i], z16, inverse, rest) : 0u;
+  if (row >= 0 && l == 0) param[row] = finite ? s : 0x7fc07fc0u;
+}
+
+__device__ __forceinline__ void write_codes4(const uint32_t (&c)[2], uint8_t* codes, int row, int, const RowChunks& at) {
   uint32_t* const to = reinterpret_cast<uint32_t*>(codes + static_cast<int64_t>(row) * kRowCodes);
-  to[ca] = first;
-  to[cb] = second;
-  if (l == 0) param[row] = finite ? s : 0x7fc07fc0u;
+  to[at.a] = c[0];
+  to[at.b] = c[1];
+}
+__device__ __forceinline__ void write_codes4(const uint32_t (&c)[4], uint8_t* codes, int row, int l, const RowChunks& = {}) {
+  uint2* const to = reinterpret_cast<uint2*>(codes + static_cast<int64_t>(row) * kRowCodes);
+  to[l] = make_uint2(c[0], c[1]);
+  to[l + 4] = make_uint2(c[2], c[3]);
 }
 
 // New tokens by slot. A tile is up to kStoreTokens tokens by some heads of keys or of values (the two alternate). With kTurn
 // the last tiles turn the queries, and keys are turned (and rounded to bf16) before they are coded.
+//
+// Without turns a lane has one row in flight and an SM 56 warps: 23,815 tokens of 8 heads (123 MB) 22.9 us of 18.5, 10,000 10.8,
+// 1000 2.3; two rows and 40 warps took 26.4, 12.8 and 2.4, with 8 lanes a row 23.5, 13.1 and 2.9. With turns four rows and 32 warps:
+// those tokens with 32 query heads (514 MB) 81.5 us of 76.9; two rows and 40 warps spill (158), four and 24 warps 95.
 template <bool kTurn>
-__global__ void __launch_bounds__(kRowThreads4) cache4_store_kernel(const __grid_constant__ CacheAppendParams A, int tile_tokens,
+__global__ void __launch_bounds__(kRowThreads4, kTurn ? 4 : 7) cache4_store_kernel(const __grid_constant__ CacheAppendParams A, int tile_tokens,
                                                                     int tile_heads, uint32_t row_tiles) {
   wait_previous_kernel();
   __shared__ __align__(16) float2 turns[kTurn ? kStoreTokens * kMaxPairs : 1];
@@ -107,27 +124,29 @@ __global__ void __launch_bounds__(kRowThreads4) cache4_store_kernel(const __grid
   const int64_t token0 = static_cast<int64_t>(tile / head_tiles) * tile_tokens;
   const int head0 = static_cast<int>(tile % head_tiles) * tile_heads;
   const int tokens = static_cast<int>(P.n_tokens - token0 < tile_tokens ? P.n_tokens - token0 : tile_tokens);
-  const int l = threadIdx.x & 7, group = threadIdx.x >> 3;
-  const int tok = group & (tile_tokens - 1), step = kGroups4 / tile_tokens;
+  constexpr int N = kTurn ? 2 : 4, kLanes = 16 / N;   // chunks of 8 elements a lane, lanes a row
+  const int l = threadIdx.x % kLanes, group = threadIdx.x / kLanes;
+  const int tok = group & (tile_tokens - 1), step = kRowThreads4 / kLanes / tile_tokens;
   const int slot = tok < tokens ? __ldg(P.slots + token0 + tok) : -1;
-  RowChunks kc = {l, l + 8, false, false};
+  RowChunks kc = {l, l + 8, false, false};   // (kTurn; else the chunks 2 l, 2 l + 1 and those 8 further on)
   if constexpr (kTurn) {
     if (key) kc = row_chunks(A.turn.r, l);
   }
+  const auto chunk = [&](int c) { return kTurn ? (c ? kc.b : kc.a) : 2 * l + (c & 1) + 8 * (c >> 1); };
   const int end = tok < tokens ? min(head0 + tile_heads, H) : 0;
-  constexpr int kInFlight = 4;
+  constexpr int kInFlight = kTurn ? 4 : 1;   // rows of a lane
   const uint16_t* const base = key ? P.k + (token0 + tok) * P.k_st : P.v + (token0 + tok) * P.v_st;
   const int64_t across = key ? P.k_sh : P.v_sh;
   uint8_t* const codes = key ? P.c.k : P.c.v;
   uint32_t* const param = key ? P.c.k_param : P.c.v_param;
-  uint4 a[kInFlight], b[kInFlight];
+  uint4 x[kInFlight][N];
   const auto load = [&](int h) {
 #pragma unroll
     for (int i = 0; i < kInFlight; ++i)
       if (h + i * step < end) {
         const uint4* from = reinterpret_cast<const uint4*>(base + (h + i * step) * across);
-        a[i] = from[kc.a];
-        b[i] = from[kc.b];
+#pragma unroll
+        for (int c = 0; c < N; ++c) x[i][c] = from[chunk(c)];
       }
   };
   int h = head0 + group / tile_tokens;
@@ -150,9 +169,12 @@ __global__ void __launch_bounds__(kRowThreads4) cache4_store_kernel(const __grid
       const bool there = kept && h + i * step < end;
       if (!__any_sync(0xffffffffu, there)) break;
       if constexpr (kTurn) {
-        if (key) turn_chunks(a[i], b[i], cs, kc, A.turn.r.interleaved);
+        if (key) turn_chunks(x[i][0], x[i][1], cs, kc, A.turn.r.interleaved);
       }
-      write_row4(a[i], b[i], kc.a, kc.b, codes, param, there ? row0 + ((h + i * step) << P.c.page_shift) : -1, l);
+      const int row = there ? row0 + ((h + i * step) << P.c.page_shift) : -1;
+      uint32_t c[N];
+      row_codes4<N>(x[i], c, param, row, l);
+      if (there) write_codes4(c, codes, row, l, kc);
     }
     h += kInFlight * step;
     load(h);
@@ -160,21 +182,22 @@ __global__ void __launch_bounds__(kRowThreads4) cache4_store_kernel(const __grid
   allow_next_kernel();
 }
 
-// Step 4 into the cache: 8 lanes a row, of keys and of values, kGatherTurns times with the next row's place looked up ahead.
-// Reads whole rows at random places and writes a row's 64 bytes and its numbers: 16 requests of 509 kept rows and 8 layers, 327 MB,
-// take 62.4 us of 48.9 at the copy's rate, 64 requests' smallest (32 layers of 72 rows) 4.9 of 2.4. Tiles of 32 rows (one turn)
-// take 83.7 and 4.6, of 256 rows 62.2 and 5.0; two rows of a lane in flight, with 3 CTAs an SM for their registers, 82.0 and 4.95.
-constexpr int kGatherTurns = 4;
-constexpr int kGatherTile = kGroups4 * kGatherTurns;   // rows of a unit that a CTA has
-__global__ void __launch_bounds__(kRowThreads4, 5) cache4_gather_kernel(const __grid_constant__ CacheGatherParams P,
+// Step 4 into the cache: a CTA has keys or values of a unit, 4 lanes a row, kGatherTurns rows one after the other with the next
+// one's place looked up ahead. Whole rows at random places: 16 requests of 509 + 8 rows in 8 layers (327 MB) take 54.4 us of 48.9 at
+// a copy's rate, 32 layers of one request's 96 rows 4.5 of 2.4. With 8 lanes a row and keys and values in one CTA 61.5 and 4.9; with
+// 2 rows a CTA 66 and 4.4, with 8 57.1 and 4.6; with 6 CTAs an SM 56.1, with 5 60.5.
+constexpr int kGatherTurns = 4, kGatherGroups = kRowThreads4 / 4;
+constexpr int kGatherTile = kGatherGroups * kGatherTurns;   // rows of a unit that a CTA has
+__global__ void __launch_bounds__(kRowThreads4, 7) cache4_gather_kernel(const __grid_constant__ CacheGatherParams P,
                                                                          uint32_t unit_tiles) {
   wait_previous_kernel();   // the indices come from the selection launched before
-  const uint32_t unit = blockIdx.x / unit_tiles;
-  const int tile = static_cast<int>(blockIdx.x - unit * unit_tiles);
+  const bool key = (blockIdx.x & 1) == 0;
+  const uint32_t unit = (blockIdx.x >> 1) / unit_tiles;
+  const int tile = static_cast<int>((blockIdx.x >> 1) - unit * unit_tiles);
   const UnitInfo u = unit_info(P.g.g, unit);
   const int W = P.g.g.window, Lc = u.L - W;
   const int m = min(P.g.layer_budget[u.layer], Lc), n = m + W;
-  const int l = threadIdx.x & 7, group = threadIdx.x >> 3;
+  const int l = threadIdx.x & 3, group = threadIdx.x >> 2;
   const int first = tile * kGatherTile + group, end = min(n, (tile + 1) * kGatherTile);
   const bool refused = __ldg(P.refused) != 0;   // the table's pages may be other sequences' by now
   const int32_t* const table = P.table + (static_cast<int64_t>(u.layer) * P.c.max_seqs + P.first_seq + u.r) * P.c.max_pages;
@@ -189,24 +212,28 @@ __global__ void __launch_bounds__(kRowThreads4, 5) cache4_gather_kernel(const __
     src = row < m ? __ldg(indices + row) : Lc + (row - m);
   };
   look_up(first);
-  for (int row = first; row - (group & 3) < end; row += kGroups4) {   // (the warp's first row)
-    uint4 k[2] = {}, v[2] = {};
+  const uint16_t* const from = key ? P.g.k + u.k_off : P.g.v + u.v_off;
+  const int64_t st = key ? P.g.g.k_st : P.g.g.v_st;
+  uint8_t* const codes = key ? P.c.k : P.c.v;
+  uint32_t* const param = key ? P.c.k_param : P.c.v_param;
+  for (int row = first; row - (group & 7) < end; row += kGatherGroups) {   // (the warp's first row)
+    uint4 x[4] = {};
     const bool there = row < end;
     const bool outside = row < m && static_cast<uint32_t>(src) >= static_cast<uint32_t>(Lc);   // never read outside the unit
     const bool good = static_cast<uint32_t>(page) < static_cast<uint32_t>(P.c.num_pages);
     if (there && (outside || !good) && l == 0) atomicOr(P.err, kErrCheck);
     const int at = there && good ? (page * P.c.heads << shift) + head + (row & (P.c.page - 1)) : -1;
     if (there && !outside) {   // (else a row of zeros)
-      const uint4* ks = reinterpret_cast<const uint4*>(P.g.k + u.k_off + src * P.g.g.k_st) + l;
-      const uint4* vs = reinterpret_cast<const uint4*>(P.g.v + u.v_off + src * P.g.g.v_st) + l;
-      k[0] = __ldg(ks);
-      k[1] = __ldg(ks + 8);
-      v[0] = __ldg(vs);
-      v[1] = __ldg(vs + 8);
+      const uint4* const xs = reinterpret_cast<const uint4*>(from + src * st) + 2 * l;
+      x[0] = __ldg(xs);
+      x[1] = __ldg(xs + 1);
+      x[2] = __ldg(xs + 8);
+      x[3] = __ldg(xs + 9);
     }
-    look_up(row + kGroups4);
-    write_row4(k[0], k[1], l, l + 8, P.c.k, P.c.k_param, at, l);
-    write_row4(v[0], v[1], l, l + 8, P.c.v, P.c.v_param, at, l);
+    look_up(row + kGatherGroups);
+    uint32_t c[4];
+    row_codes4<4>(x, c, param, at, l);
+    if (at >= 0) write_codes4(c, codes, at, l);
   }
   allow_next_kernel();
 }
@@ -217,10 +244,11 @@ cudaError_t store4(CacheAppendParams p, cudaStream_t stream) {
   RotateParams cut;
   cut.n_tokens = p.s.n_tokens;
   cut.heads = p.s.c.heads;
-  int64_t tiles = cut_rotate<kRowThreads4>(cut);
-  // A group a token and all its heads one after the other, where that still gives every SM a tile of keys and one of values: 24k
-  // tokens 24.1 us. (With it and without: 2500 tokens of 8 heads 5.6 and 4.4 us, 5000 7.35 and 7.3, 10000 13.6 and 15.2.)
-  if (cut.n_tokens >= 152 * kStoreTokens) {
+  constexpr int kWide = kTurn ? kRowThreads4 : 2 * kRowThreads4;   // (8 lanes a row there)
+  int64_t tiles = cut_rotate<kWide>(cut);
+  // With turns, a group a token and all its heads one after the other, where that still gives every SM a tile of keys and one of
+  // values: 6000 tokens 26.2 us for 31.3, 24k 95 for 117.
+  if (kTurn && cut.n_tokens >= 152 * kStoreTokens) {
     cut.tile_tokens = kStoreTokens;
     cut.tile_heads = cut.heads;
     tiles = (cut.n_tokens + kStoreTokens - 1) / kStoreTokens;
@@ -243,7 +271,7 @@ cudaError_t launch_cache4_append(const CacheAppendParams& p, cudaStream_t stream
 cudaError_t launch_cache4_gather(const CacheGatherParams& p, cudaStream_t stream) {
   const int64_t rows = static_cast<int64_t>(p.unit_pages) << p.c.page_shift;
   const int64_t tiles = (rows + kGatherTile - 1) / kGatherTile;
-  return launch_after_previous(cache4_gather_kernel, dim3(static_cast<unsigned>(p.g.g.n_units * tiles)), dim3(kRowThreads4), 0,
+  return launch_after_previous(cache4_gather_kernel, dim3(static_cast<unsigned>(p.g.g.n_units * tiles * 2)), dim3(kRowThreads4), 0,
                                stream, p, static_cast<uint32_t>(tiles));
 }
 
