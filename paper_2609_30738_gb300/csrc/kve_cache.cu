@@ -562,7 +562,7 @@ cache_store_kernel(const __grid_constant__ Params A, uint32_t row_ctas) {
   if constexpr (kTurn) {
     __shared__ __align__(16) float2 turns[kTurnTokens * kMaxPairs];
     if (blockIdx.x >= row_ctas) {
-      rotate_tile<kRowThreads<kPage>>(A.turn, blockIdx.x - row_ctas, turns);
+      rotate_tile<kRowThreads<kPage>, 4>(A.turn, blockIdx.x - row_ctas, turns);
       allow_next_kernel();
       return;
     }

@@ -112,7 +112,7 @@ __global__ void __launch_bounds__(kRowThreads4, kTurn ? 4 : 7) cache4_store_kern
   uint32_t tile = blockIdx.x;
   if constexpr (kTurn) {
     if (tile >= row_tiles) {
-      rotate_tile<kRowThreads4>(A.turn, tile - row_tiles, turns);
+      rotate_tile<kRowThreads4, 4>(A.turn, tile - row_tiles, turns);
       allow_next_kernel();
       return;
     }

@@ -121,12 +121,12 @@ __device__ __forceinline__ void turns_to_shared(float2* to, const RotaryTable& r
   __syncthreads();
 }
 
-// One CTA's tile of rows: 8 lanes a row, 32 bytes a lane; a lane keeps the turns of its token and goes through heads, four
-// rows in flight. turns: kTileTokens * kMaxPairs of shared memory, 16-byte aligned.
+// One CTA's tile of rows: 8 lanes a row, 32 bytes a lane; a lane keeps the turns of its token and goes through heads,
+// kInFlight rows in flight. turns: kTileTokens * kMaxPairs of shared memory, 16-byte aligned.
 constexpr int kTurnTokens = 8;
-template <int kThreads>
+template <int kThreads, int kInFlight>
 __device__ __forceinline__ void rotate_tile(const RotateParams& P, int64_t tile, float2* turns) {
-  constexpr int kGroups = kThreads / 8, kInFlight = 4;
+  constexpr int kGroups = kThreads / 8;
   const int head_tiles = (P.heads + P.tile_heads - 1) / P.tile_heads;
   const int64_t token0 = tile / head_tiles * P.tile_tokens;
   const int head0 = static_cast<int>(tile % head_tiles) * P.tile_heads;
