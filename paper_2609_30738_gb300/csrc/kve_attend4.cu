@@ -31,6 +31,7 @@
 // The work is cut over the tokens like that of the 8-bit cache (kve_line.cuh): all tiles in one line, an even share
 // for each CTA, whatever the lengths; a block of rows that falls to several CTAs is joined by the one that finishes
 // last, from fp32 parts in token order.
+#include <climits>
 #include <type_traits>
 
 #include "kve_internal.h"
@@ -105,10 +106,15 @@ __device__ __forceinline__ void mma_f16(float (&d)[4], const uint32_t (&a)[4], u
       : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
 }
 
-// 16 bytes global -> shared, zeros where they are not `there` (src is not followed then); a lane's copies so far are a group; all
+// 16 bytes global -> shared (where `here`), zeros where they are not `there` (src is not followed then); a lane's copies so far are a group; all
 // but the last N groups have landed.
 __device__ __forceinline__ void copy16(uint32_t dst, const void* src, uint64_t policy, uint32_t there) {
   asm volatile("cp.async.cg.shared.global.L2::cache_hint [%0], [%1], 16, %3, %2;" ::"r"(dst), "l"(src), "l"(policy), "r"(there)
+               : "memory");
+}
+__device__ __forceinline__ void copy16_if(bool here, uint32_t dst, const void* src, uint64_t policy, uint32_t there) {
+  asm volatile("{\n .reg .pred p;\n setp.ne.s32 p, %4, 0;\n @p cp.async.cg.shared.global.L2::cache_hint [%0], [%1], 16, %3, %2;\n}" ::"r"(dst),
+               "l"(src), "l"(policy), "r"(there), "r"(static_cast<int>(here))
                : "memory");
 }
 __device__ __forceinline__ void copies_group() { asm volatile("cp.async.commit_group;" ::: "memory"); }
@@ -202,12 +208,16 @@ cache_attend4_kernel(const __grid_constant__ AttendParams P) {
 
   // -------------------------------------------------------------- copies, S - 1 steps ahead
   Part& ahead = ctl.ahead[warp];
-  int ahead_step = 0, ahead_last = -1, ahead_tok0 = 0, ahead_head = 0;   // (head: its first row in a page; last < 0: no more)
+  int ahead_step = 0, ahead_until = 0, ahead_last = -1, ahead_tok0 = 0, ahead_head = 0;   // (until: the end, or that of `held`)
+  bool lost = false;                // a page outside the pool
   int window = 0, held = 0;         // entries window .. window + 31 of the sequence's table, a lane each
   int fill = 0, slot = 0;           // the stages of the next copies and of the next step
   uint32_t gaps = 0;             // two bits a stage: pages outside the pool, of its first and of its last 16 tokens
   const auto read_table = [&]() {   // (looked at in the next fetch)
-    window = (ahead_tok0 + ahead_step * kStep) >> shift;
+    const int at = ahead_tok0 + ahead_step * kStep;
+    window = at >> shift;
+    // (the first step that asks for an entry behind those: its second half may be on the next page)
+    ahead_until = min(ahead_last, ahead_step + (((32 << shift) - (at & (P.c.page - 1)) - 16 + kStep - 1) / kStep));
     held = 0;                       // (behind the sequence: nobody sees what is there)
     if (window + lane < (ahead.b.len + P.c.page - 1) >> shift)
       held = __ldg(P.table + static_cast<int64_t>(ahead.b.r) * P.c.max_pages + window + lane);
@@ -223,8 +233,10 @@ cache_attend4_kernel(const __grid_constant__ AttendParams P) {
     while (ahead_step >= ahead_last) {
       Part a = ahead;
       a.x = a.end;
-      if (a.x >= x1) {
+      if (a.x >= x1) {   // no more: pages that are not there, and no error
         ahead_last = -1;
+        ahead_until = INT_MAX;
+        held = -1;
         return;
       }
       next_block(P, blocks, C::kTile, a.b);
@@ -245,15 +257,13 @@ cache_attend4_kernel(const __grid_constant__ AttendParams P) {
   int row0 = 0, row1 = 0;
   uint32_t ok0 = 0, ok1 = 0;   // bytes of each copy: 16, or 0 for a page outside the pool (or no step)
   const auto find = [&]() {
-    ok0 = ok1 = 0;
-    if (ahead_last < 0) return;
     const int at = ahead_tok0 + ahead_step * kStep;
     const int id0 = __shfl_sync(0xffffffffu, held, (at >> shift) - window);
     const int id1 = __shfl_sync(0xffffffffu, held, ((at + 16) >> shift) - window);
     ok0 = static_cast<uint32_t>(id0) < static_cast<uint32_t>(P.c.num_pages) ? 16 : 0;
     ok1 = static_cast<uint32_t>(id1) < static_cast<uint32_t>(P.c.num_pages) ? 16 : 0;
     gaps = (gaps & ~(3u << 2 * fill)) | (ok0 ? 0u : 1u) << 2 * fill | (ok1 ? 0u : 2u) << 2 * fill;
-    if ((ok0 & ok1) == 0) atomicOr(P.err, kErrCheck);
+    lost |= (ok0 & ok1) == 0 && ahead_last >= 0;
     row0 = (id0 * P.c.heads << shift) + ahead_head + (at & (P.c.page - 1));
     row1 = (id1 * P.c.heads << shift) + ahead_head + ((at + 16) & (P.c.page - 1));
   };
@@ -268,18 +278,15 @@ cache_attend4_kernel(const __grid_constant__ AttendParams P) {
   const auto copy_keys = [&]() { copy_codes(P.c.k, put + fill * kStageBytes); };
   const auto copy_rest = [&]() {
     copy_codes(P.c.v, put + fill * kStageBytes + kCodeBytes);
-    if (lane < 16)
-      copy16(put_number + fill * (2 * kStep * 4), (lane & 8 ? P.c.v_param : P.c.k_param) + (lane & 4 ? row1 : row0) + (lane & 3) * 4,
-             policy, lane & 4 ? ok1 : ok0);
+    copy16_if(lane < 16, put_number + fill * (2 * kStep * 4), (lane & 8 ? P.c.v_param : P.c.k_param) + (lane & 4 ? row1 : row0) + (lane & 3) * 4,
+              policy, lane & 4 ? ok1 : ok0);
     copies_group();   // (an empty one too: groups are counted)
-    if (ahead_last >= 0) {
-      fill = fill + 1 == S ? 0 : fill + 1;
-      ++ahead_step;
-      if (ahead_step < ahead_last) {
-        if (((ahead_tok0 + ahead_step * kStep + 16) >> shift) >= window + 32) read_table();
-      } else {
+    fill = fill + 1 == S ? 0 : fill + 1;
+    if (++ahead_step >= ahead_until) {
+      if (ahead_step < ahead_last)
+        read_table();
+      else
         settle();
-      }
     }
   };
   // the raw query rows of a part: row 8 e + g of the block, elements 32 t .. 32 t + 31
@@ -650,6 +657,8 @@ cache_attend4_kernel(const __grid_constant__ AttendParams P) {
     now ^= 1;
   }
 
+  if (lost && lane == 0) atomicOr(P.err, kErrCheck);
+
   // sequences without a token: their rows are zeros
   for (int r = blockIdx.x * W + warp; r < P.n_seq; r += W * gridDim.x)
     if (seq_len(P, r) == 0)
@@ -662,6 +671,7 @@ cache_attend4_kernel(const __grid_constant__ AttendParams P) {
   // ------------------------------------------------------------ the join of blocks that several CTAs had parts of
   allow_next_kernel();
   if (splits == 0) return;
+  copies_wait<0>();  // (the empty ones behind the last step write zeros into the ring)
   __syncthreads();   // every thread's part of the sums is out, and ctl.split is written
   if (threadIdx.x < splits) {
     int w0, w1;
