@@ -44,7 +44,8 @@ namespace {
 constexpr int kStep = 32;                                  // tokens of a warp's step
 constexpr int kRowBytes = kHeadDim / 2;                    // codes of a token
 constexpr int kCodeBytes = kStep * kRowBytes;
-constexpr int kStageBytes = 2 * kCodeBytes;                // K, then V
+constexpr int kNumbers = 2 * kCodeBytes;                   // K, V, then the numbers of K's rows and of V's
+constexpr int kStageBytes = kNumbers + 2 * kStep * 4;
 
 // R rows of a block on W warps of a CTA. 16 warps an SM for 8 rows, 12 for 16 rows (with 16 warps their registers spill in the
 // loop: 24 sequences of 4 drafts 64 us for 34). With fewer warps a CTA the end of a part costs less, with more a block is cut into
@@ -77,9 +78,7 @@ struct Part {
 
 template <int R, int W>
 struct A4Ctl {
-  static constexpr int S = A4Cfg<R, W>::kStages;
-  alignas(128) uint32_t param[W][S][2][kStep];   // K's, V's
-  float4 tokens[W][kStep];                       // of a step's tokens: K's s and z, V's log2 s and z
+  alignas(128) float4 tokens[W][kStep];                       // of a step's tokens: K's s and z, V's log2 s and z
   LineCtl<W> line;
   Part part[2];                                  // of the sums, by turns (all threads write the same)
   Part ahead[W];                                 // of a warp's copies
@@ -208,34 +207,39 @@ cache_attend4_kernel(const __grid_constant__ AttendParams P) {
 
   // -------------------------------------------------------------- copies, S - 1 steps ahead
   Part& ahead = ctl.ahead[warp];
-  int ahead_step = 0, ahead_until = 0, ahead_last = -1, ahead_tok0 = 0, ahead_head = 0;   // (until: the end, or that of `held`)
-  bool lost = false;                // a page outside the pool
-  int window = 0, held = 0;         // entries window .. window + 31 of the sequence's table, a lane each
-  int fill = 0, slot = 0;           // the stages of the next copies and of the next step
-  uint32_t gaps = 0;             // two bits a stage: pages outside the pool, of its first and of its last 16 tokens
-  const auto read_table = [&]() {   // (looked at in the next fetch)
-    const int at = ahead_tok0 + ahead_step * kStep;
-    window = at >> shift;
+  const int page_mask = P.c.page - 1;
+  const uint32_t page_rows = P.c.heads << shift;
+  int held = 0;                       // 32 entries of the sequence's table, a lane each
+  int rel = 0, rel_until = INT_MIN;   // the next step's first token in those pages; the end of them or of the warp's steps
+  int ahead_pos = 0, ahead_last = 0;  // the part's tokens that those pages begin at, and that the warp's steps end at
+  int ahead_head = 0;                 // the head's first row in a page
+  const uint32_t ring0 = smem_u32(ring), ring1 = ring0 + S * kStageBytes;
+  uint32_t fill = ring0, slot = ring0;   // the stages of the next copies and of the next step
+  uint32_t gaps = 0, lost = 0;        // two bits a step, the next one's lowest: pages outside the pool, of its halves; any
+  const auto read_table = [&](int at) {   // from token `at` on (looked at in the next fetch)
+    const int window = at >> shift;
+    ahead_pos = window << shift;
+    rel = at - ahead_pos;
     // (the first step that asks for an entry behind those: its second half may be on the next page)
-    ahead_until = min(ahead_last, ahead_step + (((32 << shift) - (at & (P.c.page - 1)) - 16 + kStep - 1) / kStep));
-    held = 0;                       // (behind the sequence: nobody sees what is there)
-    if (window + lane < (ahead.b.len + P.c.page - 1) >> shift)
+    rel_until = min(ahead_last - ahead_pos, (32 << shift) - 16);
+    held = 0;                         // (behind the sequence: nobody sees what is there)
+    if (window + lane < (ahead.b.len + page_mask) >> shift)
       held = __ldg(P.table + static_cast<int64_t>(ahead.b.r) * P.c.max_pages + window + lane);
   };
   const auto enter = [&]() {
-    ahead_step = ahead.template first<W>(warp);
-    ahead_last = ahead.template first<W>(warp + 1);
-    ahead_tok0 = ahead.tok0;
+    const int at = ahead.tok0 + ahead.template first<W>(warp) * kStep;
+    ahead_last = ahead.tok0 + ahead.template first<W>(warp + 1) * kStep;
     ahead_head = ahead.b.h << shift;
-    if (ahead_step < ahead_last) read_table();
+    ahead_pos = at;
+    rel = rel_until = 0;
+    if (at < ahead_last) read_table(at);
   };
   const auto settle = [&]() {   // on to a part with something to read
-    while (ahead_step >= ahead_last) {
+    while (ahead_pos + rel >= ahead_last) {
       Part a = ahead;
       a.x = a.end;
-      if (a.x >= x1) {   // no more: pages that are not there, and no error
-        ahead_last = -1;
-        ahead_until = INT_MAX;
+      if (a.x >= x1) {   // no more: pages that are not there
+        rel_until = INT_MAX;
         held = -1;
         return;
       }
@@ -249,42 +253,43 @@ cache_attend4_kernel(const __grid_constant__ AttendParams P) {
   };
   // Pages of a call that reads more than L2 keeps leave it first.
   const uint64_t policy = x1 - x0 > 8 ? l2_policy_evict_first() : l2_policy_evict_normal();
-  const uint32_t put = smem_u32(ring) + lies(g, t);   // eight tokens of K or V at once, 16 bytes a lane
+  const uint32_t put = lies(g, t);   // eight tokens of K or V at once, 16 bytes a lane
+  const uint8_t* const k_base = P.c.k + lane * 16;
+  const uint8_t* const v_base = P.c.v + lane * 16;
   // the rows' numbers: four lanes each for the halves of K's and of V's
-  const uint32_t put_number = smem_u32(ctl.param[warp][0][lane >> 3 & 1] + (lane & 7) * 4);
+  const uint32_t* const numbers = (lane & 8 ? P.c.v_param : P.c.k_param) + (lane & 3) * 4;
   // The copies of the next step, in three pieces that stand between the products: where its rows are (of its two halves, in
   // the pool), K, and the rest.
-  int row0 = 0, row1 = 0;
+  uint32_t row0 = 0, row1 = 0;
   uint32_t ok0 = 0, ok1 = 0;   // bytes of each copy: 16, or 0 for a page outside the pool (or no step)
   const auto find = [&]() {
-    const int at = ahead_tok0 + ahead_step * kStep;
-    const int id0 = __shfl_sync(0xffffffffu, held, (at >> shift) - window);
-    const int id1 = __shfl_sync(0xffffffffu, held, ((at + 16) >> shift) - window);
+    const int id0 = __shfl_sync(0xffffffffu, held, rel >> shift);
+    const int id1 = __shfl_sync(0xffffffffu, held, (rel + 16) >> shift);
     ok0 = static_cast<uint32_t>(id0) < static_cast<uint32_t>(P.c.num_pages) ? 16 : 0;
     ok1 = static_cast<uint32_t>(id1) < static_cast<uint32_t>(P.c.num_pages) ? 16 : 0;
-    gaps = (gaps & ~(3u << 2 * fill)) | (ok0 ? 0u : 1u) << 2 * fill | (ok1 ? 0u : 2u) << 2 * fill;
-    lost |= (ok0 & ok1) == 0 && ahead_last >= 0;
-    row0 = (id0 * P.c.heads << shift) + ahead_head + (at & (P.c.page - 1));
-    row1 = (id1 * P.c.heads << shift) + ahead_head + ((at + 16) & (P.c.page - 1));
+    gaps = gaps >> 2 | (ok0 ^ 16) << 2 * (S - 3) | (ok1 ^ 16) << (2 * (S - 3) + 1);   // (bits 2 (S - 1) and the next)
+    row0 = static_cast<uint32_t>(id0) * page_rows + ahead_head + (rel & page_mask);
+    row1 = static_cast<uint32_t>(id1) * page_rows + ahead_head + (rel + 16 & page_mask);
   };
   const auto copy_codes = [&](const uint8_t* base, uint32_t to) {
-    const uint8_t* const from0 = base + static_cast<int64_t>(row0) * kRowBytes + lane * 16;
-    const uint8_t* const from1 = base + static_cast<int64_t>(row1) * kRowBytes + lane * 16;
+    const uint8_t* const from0 = base + static_cast<uint64_t>(row0) * kRowBytes;
+    const uint8_t* const from1 = base + static_cast<uint64_t>(row1) * kRowBytes;
     copy16(to, from0, policy, ok0);
     copy16(to + 512, from0 + 512, policy, ok0);
     copy16(to + 1024, from1, policy, ok1);
     copy16(to + 1536, from1 + 512, policy, ok1);
   };
-  const auto copy_keys = [&]() { copy_codes(P.c.k, put + fill * kStageBytes); };
+  const auto copy_keys = [&]() { copy_codes(k_base, fill + put); };
   const auto copy_rest = [&]() {
-    copy_codes(P.c.v, put + fill * kStageBytes + kCodeBytes);
-    copy16_if(lane < 16, put_number + fill * (2 * kStep * 4), (lane & 8 ? P.c.v_param : P.c.k_param) + (lane & 4 ? row1 : row0) + (lane & 3) * 4,
-              policy, lane & 4 ? ok1 : ok0);
+    copy_codes(v_base, fill + put + kCodeBytes);
+    copy16_if(lane < 16, fill + kNumbers + lane * 16, numbers + (lane & 4 ? row1 : row0), policy, lane & 4 ? ok1 : ok0);
     copies_group();   // (an empty one too: groups are counted)
-    fill = fill + 1 == S ? 0 : fill + 1;
-    if (++ahead_step >= ahead_until) {
-      if (ahead_step < ahead_last)
-        read_table();
+    fill += kStageBytes;
+    if (fill == ring1) fill = ring0;
+    rel += kStep;
+    if (rel >= rel_until) {
+      if (ahead_pos + rel < ahead_last)
+        read_table(ahead_pos + rel);
       else
         settle();
     }
@@ -398,10 +403,11 @@ cache_attend4_kernel(const __grid_constant__ AttendParams P) {
       __syncwarp();   // every lane's copies of this step have landed, and the step before has been read
       find();
       copy_keys();
-      const uint8_t* const at = ring + slot * kStageBytes;
+      const uint8_t* const at = ring + (slot - ring0);
       {
         // a lane a token: its four numbers for every lane
-        const uint32_t a = ctl.param[warp][slot][0][lane], c = ctl.param[warp][slot][1][lane];
+        const uint32_t* const n = reinterpret_cast<const uint32_t*>(at + kNumbers);
+        const uint32_t a = n[lane], c = n[kStep + lane];
         ctl.tokens[warp][lane] = make_float4(low_bf16(a), high_bf16(a), lg2(low_bf16(c)), high_bf16(c));
       }
       float s[2][kHalves][4];
@@ -435,7 +441,8 @@ cache_attend4_kernel(const __grid_constant__ AttendParams P) {
       copy_rest();
       __syncwarp();
       const int pos0 = tok0 + step * kStep;
-      const uint32_t hole = gaps >> 2 * slot & 3u;
+      const uint32_t hole = gaps & 3u;
+      lost |= hole;
       const bool some = hole != 0 || pos0 + kStep > all_see;   // tokens that not all rows see
       // logits (over kq) in place of the products
       float2 y[4][kHalves], kq[kHalves];
@@ -539,7 +546,7 @@ cache_attend4_kernel(const __grid_constant__ AttendParams P) {
 #pragma unroll
       for (int k = 0; k < 2; ++k) {
         uint32_t c0[4], c1[4];   // four codes of two tokens each
-        const uint32_t from = smem_u32(at) + kCodeBytes + 2 * k * (8 * kRowBytes) + vget;
+        const uint32_t from = slot + kCodeBytes + 2 * k * (8 * kRowBytes) + vget;
         load_transposed(c0, from);
         load_transposed(c1, from + 8 * kRowBytes);
 #pragma unroll
@@ -554,16 +561,17 @@ cache_attend4_kernel(const __grid_constant__ AttendParams P) {
             for (int e = 0; e < kHalves; ++e) mma_f16(o[2 * i + h][e], a, w[2 * k][e], w[2 * k + 1][e]);
           }
       }
-      slot = slot + 1 == S ? 0 : slot + 1;
+      slot += kStageBytes;
+      if (slot == ring1) slot = ring0;
     }
 
     // ---------------------------------------------------------- the end of a part: the warps' rows together, eight by eight
     const bool has = first < last, whole = x == b.first && part.end == b.first + b.tiles;
     float* const out = P.partial + (static_cast<int64_t>(blockIdx.x) * 2 + (x == b.first)) * kAttend4PartWords;
     // (in the stage of the last step, which the next one's copies will fill)
-    const int stage = slot == 0 ? S - 1 : slot - 1;
-    float* const mine = reinterpret_cast<float*>(ring + stage * kStageBytes);
-    if (lane == 0) ctl.at[warp] = has ? stage * kStageBytes : -1;
+    const int stage = (slot == ring0 ? ring1 : slot) - kStageBytes - ring0;
+    float* const mine = reinterpret_cast<float*>(ring + stage);
+    if (lane == 0) ctl.at[warp] = has ? stage : -1;
     const int next_x = part.end;
 #pragma unroll
     for (int e = 0; e < kHalves; ++e) {
