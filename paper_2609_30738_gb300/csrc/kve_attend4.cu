@@ -811,10 +811,13 @@ cudaError_t attend4_rows(const kve_cache& c, const AttendParams& p, cudaStream_t
 }  // namespace
 
 cudaError_t launch_cache4_attend(const kve_cache& c, const AttendParams& p, cudaStream_t stream) {
-  if (p.q_tokens * p.c.group > 8) return attend4_rows<16, 4>(c, p, stream);
-  // Two CTAs an SM have a block each without cutting one: 4 warps a CTA, else 8. (4 against 8: 64 ragged sequences of 8 heads 54.7
-  // and 60.2 us, 1000 of 64 tokens 59 and 108; 16 evicted 8.9 and 7.4, one of 131072 tokens 41.4 and 35.2, 8 of 32768 61.5 and 59.5.)
-  const bool many = static_cast<int64_t>(p.n_seq) * p.c.heads >= 2 * c.sms;
+  const int64_t rows = static_cast<int64_t>(p.q_tokens) * p.c.group, blocks = static_cast<int64_t>(p.n_seq) * p.c.heads * ((rows + 15) / 16);
+  // Two CTAs an SM have a block each without cutting one: 4 warps a CTA, else 8, of 16 rows 6. (4 against 8: 64 ragged sequences of 8
+  // heads 50.6 and 60.2 us, 1000 of 64 tokens 59 and 108; 16 evicted 8.9 and 6.9, one of 131072 tokens 39 and 33, 8 of 32768 57 and
+  // 55. 16 rows, 4 against 6: 100 ragged ones 45 and 51, 16 of 8192 with 32 rows 80.1 and 80.4, 24 of 500 to 8192 33.5 both, one of
+  // 131072 54.7 and 49.3; 12 there 46.5, but 37.6 for the 24.)
+  const bool many = blocks >= 2 * c.sms;
+  if (rows > 8) return many ? attend4_rows<16, 4>(c, p, stream) : attend4_rows<16, 6>(c, p, stream);
   return many ? attend4_rows<8, 4>(c, p, stream) : attend4_rows<8, 8>(c, p, stream);
 }
 
