@@ -54,7 +54,7 @@ template <int R, int W>
 struct A4Cfg {
   static constexpr int kThreads = 32 * W;
   static constexpr int kStages = 3;
-  static constexpr int kCtas = (R == 8 ? 16 : 12) / W;
+  static constexpr int kCtas = W == 2 ? 7 : (R == 8 ? 16 : 12) / W;   // (eight of two warps do not fit into the shared memory)
   static constexpr int kTile = W * kStep;   // tokens: a step of every warp
   static constexpr int kPart = 3;           // what a part costs beside its own tiles
   static constexpr size_t kCtl = size_t(W) * kStages * kStageBytes;
@@ -813,11 +813,14 @@ cudaError_t attend4_rows(const kve_cache& c, const AttendParams& p, cudaStream_t
 cudaError_t launch_cache4_attend(const kve_cache& c, const AttendParams& p, cudaStream_t stream) {
   const int64_t rows = static_cast<int64_t>(p.q_tokens) * p.c.group, blocks = static_cast<int64_t>(p.n_seq) * p.c.heads * ((rows + 15) / 16);
   // Two CTAs an SM have a block each without cutting one: 4 warps a CTA, else 8, of 16 rows 6. (4 against 8: 64 ragged sequences of 8
-  // heads 50.6 and 60.2 us, 1000 of 64 tokens 59 and 108; 16 evicted 8.9 and 6.9, one of 131072 tokens 39 and 33, 8 of 32768 57 and
-  // 55. 16 rows, 4 against 6: 100 ragged ones 45 and 51, 16 of 8192 with 32 rows 80.1 and 80.4, 24 of 500 to 8192 33.5 both, one of
-  // 131072 54.7 and 49.3; 12 there 46.5, but 37.6 for the 24.)
+  // heads 50.6 and 56.1 us, 16 evicted 8.1 and 7.0, one of 131072 tokens 38.3 and 33.2, 8 of 32768 57.1 and 55.1. 16 rows, 4 against
+  // 6: 100 ragged ones 44.9 and 50.9, 16 of 8192 with 32 rows 79.9 and 80.3, 24 of 500 to 8192 33.5 both, one of 131072 55.0 and
+  // 49.2; 12 there 46.5, but 37.6 for the 24.)
   const bool many = blocks >= 2 * c.sms;
   if (rows > 8) return many ? attend4_rows<16, 4>(c, p, stream) : attend4_rows<16, 6>(c, p, stream);
+  // Many short ones, as a table says that holds no long ones: 2 warps (against 4: 1000 of 64 tokens 46.5 and 58.8, 400 of 20 to 800
+  // 39.1 and 43.5, of 50 to 4000 95.8 and 96.5; but of 100 to 8000 154 and 148, 200 of 50 to 800 28.8 both, 100 18.7 and 15.5).
+  if (blocks >= 16 * c.sms && static_cast<int64_t>(p.c.max_pages) << p.c.page_shift <= 4096) return attend4_rows<8, 2>(c, p, stream);
   return many ? attend4_rows<8, 4>(c, p, stream) : attend4_rows<8, 8>(c, p, stream);
 }
 

@@ -322,6 +322,17 @@ def test_attention_of_many_sequences_and_of_one_long():
     _attend(K, rng, [40000], 32, 16, 1, 1)
 
 
+@pytest.mark.parametrize("n,longest,P,hq,hkv,t,last", [
+    (40, 300, 32, 8, 8, 1, 9000), (40, 300, 16, 32, 8, 2, 4500), (310, 90, 16, 16, 8, 1, 700), (620, 40, 32, 4, 4, 2, 3000),
+    (700, 3, 16, 32, 4, 1, 4096)])
+def test_attention_of_many_blocks(n, longest, P, hq, hkv, t, last):
+    torch, K = _k()
+    rng = np.random.default_rng(n + P)
+    lens = [int(x) for x in rng.integers(0, longest, n - 1)] + [last]
+    cache = _attend(K, rng, lens, P, hq, hkv, t, fused=True)[0]
+    assert cache.status() == K.KVE_OK
+
+
 def test_rows_behind_n_seq_stay_and_empty_batches_are_served():
     torch, K = _k()
     cache, out, _, args, _ = _attend(K, np.random.default_rng(21), [40, 50, 60], 16, 8, 2, 2, n_seq=2)
