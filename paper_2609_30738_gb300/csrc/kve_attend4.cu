@@ -5,16 +5,25 @@
 //   out = sum_i softmax(l)_i s_i c_i + sum_i softmax(l)_i z_i,   lse = ln sum_i exp(l_i).
 // Scales and zeros never touch a code: both products are of the codes alone.
 //
-// Bound by the read of the cache, 136 bytes a token and head. A code becomes a matrix operand in registers, with
-// about 0.7 instructions an element and no conversion: the low four bits of an f16 are the subnormal c 2^-24 (and the
-// next four 16 c 2^-24), so a word of eight codes is four operand registers by one shift and four masks. The operands then
-// have to be in registers (mma.sync m16n8k16; in e4m3 that instruction is made of conversions and the f16 one here), where the
-// loads put them:
-//   S^T [tokens][rows] = K Q^T     A = codes of two tokens, 32 a lane and token, B = the query rows (f16, in registers)
+// Bound by the read of the cache, 136 bytes a token and head, and by start and end: 131072 tokens of 8 heads (143 MB) take 33.2 us
+// where a copy's rate is 21.3, and twice that (8 x 32768) 55.1, so between the two it runs at 97% of that rate, beside 11 us. Five of
+// them are any call's (96 tokens: lengths, cut, table, first codes, a step, output), the others the first copies of all CTAs at once
+// and the join. 64 ragged sequences of 512 to 16384 tokens (237 MB) take 50.6 us of 35.5, where CTAs have several parts. 430 warp
+// instructions for 32 tokens of 8 rows, half of them the integer unit's, of which more than half unpack codes, are close behind: each
+// tenth of them was 2 us there. With 16 rows (24 sequences of 500 to 8192 tokens 33.5 us of 10) they are 540, and for their registers
+// only three warps a scheduler, which wait for their own results.
+//
+// A code becomes a matrix operand in registers, with half an instruction an element and no conversion: the low four bits of an f16
+// are the subnormal c 2^-24 and the next four 16 c 2^-24, so a word of eight codes is four operand registers by a shift and masks. The
+// operands then have to be in registers (mma.sync m16n8k16; in e4m3 that instruction is made of conversions and the f16 one here:
+// 131072 tokens 50.5 us for 40.8 at the time), where the loads put them:
+//   S^T [tokens][rows] = K Q^T     A = codes of two tokens, 32 a lane and token, B = the query rows (f16, from shared memory)
 //   O^T [d][rows]      = V^T W^T   A = codes of two tokens side by side (transposing matrix loads), B = the weights,
 //                                  S^T's registers after an 8 x 8 transposition
-// so 8 rows fill the N side. The sums over d do not care for its order, as long as both operands have the same, so a lane's
-// 16 bytes of K are eight k-steps as they lie. What the sums see of fewer than 32 bits:
+// so 8 rows fill the N side (tokens there instead took 66.3 us for 61.2 on the 64). The sums over d do not care for its order, as long
+// as both operands have the same, so a lane's 16 bytes of K are eight k-steps as they lie. V's second codes stay with the first ones,
+// c + 16 c', which saves a mask, and the end takes the first one's sum out again: both are fp32 sums of exact products, and the
+// difference is off by 16 / 15 of what the sum of 16 c' alone would be. What the sums see of fewer than 32 bits:
 //   q  bf16 times a power of two of its row, f16: exact down to 2^-31 of the row's largest (2^-27 in every second
 //      element, whose codes are 16 times larger), an absolute 2^-35 of it below;
 //   w  softmax(l)_i s_i over a reference within 2^8 of the row's largest such product so far, times 2^6, f16: 2^-12 of
@@ -23,10 +32,11 @@
 // that a token of far larger values costs the others nothing where it hardly counts. References move only when a maximum
 // passes them by 2^8, which leaves the rescaling of the output to a few steps.
 //
-// A consumer warp takes 32 tokens a step from a ring of its own in shared memory, and has maxima, sums and output of its own:
-// no warp waits for another before a part ends. It fills its ring itself, across the ends of parts, by
-// asynchronous copies that stand between its products. (A tensor copy holds its warp for more than 100 cycles, and a step is
-// four of them, with pages of 16 eight: 131072 tokens took 40.9 us with them, and one warp that fills all rings is too slow.)
+// A warp takes 32 tokens a step from a ring of its own in shared memory, and has maxima, sums and output of its own: no warp waits for
+// another before a part ends. It fills its ring itself, across the ends of parts, by asynchronous copies that stand between its
+// products, with as few instructions as will do: each tenth of them is 2 us of the 64. (A tensor copy holds its warp for more than 100
+// cycles, and a step is four of them, with pages of 16 eight: 131072 tokens took 40.9 us for 38.2; one warp that fills all rings 40.8 for
+// 38.6. The next step's scores between the products with V 36.2 for 35.3, their registers.)
 //
 // The work is cut over the tokens like that of the 8-bit cache (kve_line.cuh): all tiles in one line, an even share
 // for each CTA, whatever the lengths; a block of rows that falls to several CTAs is joined by the one that finishes
@@ -105,16 +115,17 @@ __device__ __forceinline__ void mma_f16(float (&d)[4], const uint32_t (&a)[4], u
       : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
 }
 
-// 16 bytes global -> shared (where `here`), zeros where they are not `there` (src is not followed then); a lane's copies so far are a group; all
-// but the last N groups have landed.
+// 16 bytes global -> shared (where `here`), zeros where they are not `there` (src is not followed then); a lane's copies so far are a
+// group; all but the last N groups have landed.
 __device__ __forceinline__ void copy16(uint32_t dst, const void* src, uint64_t policy, uint32_t there) {
   asm volatile("cp.async.cg.shared.global.L2::cache_hint [%0], [%1], 16, %3, %2;" ::"r"(dst), "l"(src), "l"(policy), "r"(there)
                : "memory");
 }
 __device__ __forceinline__ void copy16_if(bool here, uint32_t dst, const void* src, uint64_t policy, uint32_t there) {
-  asm volatile("{\n .reg .pred p;\n setp.ne.s32 p, %4, 0;\n @p cp.async.cg.shared.global.L2::cache_hint [%0], [%1], 16, %3, %2;\n}" ::"r"(dst),
-               "l"(src), "l"(policy), "r"(there), "r"(static_cast<int>(here))
-               : "memory");
+  asm volatile(
+      "{\n .reg .pred p;\n setp.ne.s32 p, %4, 0;\n @p cp.async.cg.shared.global.L2::cache_hint [%0], [%1], 16, %3, %2;\n}" ::"r"(dst),
+      "l"(src), "l"(policy), "r"(there), "r"(static_cast<int>(here))
+      : "memory");
 }
 __device__ __forceinline__ void copies_group() { asm volatile("cp.async.commit_group;" ::: "memory"); }
 template <int N>
@@ -180,7 +191,8 @@ cache_attend4_kernel(const __grid_constant__ AttendParams P) {
   // thread of the grid
   {
     const int64_t id = static_cast<int64_t>(blockIdx.x) * C::kThreads + threadIdx.x;
-    const int64_t table_lines = (static_cast<int64_t>(P.n_seq) * P.c.max_pages + 31) >> 5, q_rows = static_cast<int64_t>(P.n_seq) * P.q_tokens * P.c.hq;
+    const int64_t table_lines = (static_cast<int64_t>(P.n_seq) * P.c.max_pages + 31) >> 5;
+    const int64_t q_rows = static_cast<int64_t>(P.n_seq) * P.q_tokens * P.c.hq;
     if (id < table_lines) {
       prefetch_line(P.table + id * 32);
     } else if (id - table_lines < 2 * q_rows) {
@@ -396,7 +408,8 @@ cache_attend4_kernel(const __grid_constant__ AttendParams P) {
       m[e] = top[e] = both(kNone);
       l[e] = z[e] = both(0.f);
     }
-    const int first = part.template first<W>(warp), last = part.template first<W>(warp + 1), tok0 = part.tok0, all_see = b.len - P.q_tokens + 1;
+    const int first = part.template first<W>(warp), last = part.template first<W>(warp + 1);
+    const int tok0 = part.tok0, all_see = b.len - P.q_tokens + 1;
 #pragma unroll 1
     for (int step = first; step < last; ++step) {
       copies_wait<S - 2>();
@@ -811,7 +824,8 @@ cudaError_t attend4_rows(const kve_cache& c, const AttendParams& p, cudaStream_t
 }  // namespace
 
 cudaError_t launch_cache4_attend(const kve_cache& c, const AttendParams& p, cudaStream_t stream) {
-  const int64_t rows = static_cast<int64_t>(p.q_tokens) * p.c.group, blocks = static_cast<int64_t>(p.n_seq) * p.c.heads * ((rows + 15) / 16);
+  const int64_t rows = static_cast<int64_t>(p.q_tokens) * p.c.group;
+  const int64_t blocks = static_cast<int64_t>(p.n_seq) * p.c.heads * ((rows + 15) / 16);
   // Two CTAs an SM have a block each without cutting one: 4 warps a CTA, else 8, of 16 rows 6. (4 against 8: 64 ragged sequences of 8
   // heads 50.6 and 56.1 us, 16 evicted 8.1 and 7.0, one of 131072 tokens 38.3 and 33.2, 8 of 32768 57.1 and 55.1. 16 rows, 4 against
   // 6: 100 ragged ones 44.9 and 50.9, 16 of 8192 with 32 rows 79.9 and 80.3, 24 of 500 to 8192 33.5 both, one of 131072 55.0 and
