@@ -57,14 +57,15 @@ constexpr int kCodeBytes = kStep * kRowBytes;
 constexpr int kNumbers = 2 * kCodeBytes;                   // K, V, then the numbers of K's rows and of V's
 constexpr int kStageBytes = kNumbers + 2 * kStep * 4;
 
-// R rows of a block on W warps of a CTA. 16 warps an SM for 8 rows, 12 for 16 rows (with 16 warps their registers spill in the
-// loop: 24 sequences of 4 drafts 64 us for 34). With fewer warps a CTA the end of a part costs less, with more a block is cut into
-// fewer parts (launch_cache4_attend).
+// R rows of a block on W warps of a CTA (attend4_rows). 12 warps an SM for 8 rows, or one CTA of 8, and 8 for 16: registers that let
+// a warp's own instructions overlap are worth more than warps. (16 warps of 128 registers: 64 ragged sequences 50.6 us for 46.9, 8 warps
+// and 4 stages 60.5. 16 rows with 12 warps, 168 registers and spills: 24 sequences of 4 drafts 33.5 for 29.0, with 16 warps 64.) A ring of 4 stages
+// instead of 3 took 48.2 and 29.9.
 template <int R, int W>
 struct A4Cfg {
   static constexpr int kThreads = 32 * W;
   static constexpr int kStages = 3;
-  static constexpr int kCtas = W == 2 ? 7 : (R == 8 ? 16 : 12) / W;   // (eight of two warps do not fit into the shared memory)
+  static constexpr int kCtas = R == 16 ? 8 / W : W == 8 ? 1 : 12 / W;
   static constexpr int kTile = W * kStep;   // tokens: a step of every warp
   static constexpr int kPart = 3;           // what a part costs beside its own tiles
   static constexpr size_t kCtl = size_t(W) * kStages * kStageBytes;
@@ -821,21 +822,28 @@ cudaError_t attend4_rows(const kve_cache& c, const AttendParams& p, cudaStream_t
   return launch_after_previous(fn, dim3(static_cast<unsigned>(want < most ? want : most)), dim3(C::kThreads), smem, stream, p);
 }
 
+template <int W>
+cudaError_t attend4_warps(const kve_cache& c, const AttendParams& p, cudaStream_t stream) {
+  return p.q_tokens * p.c.group > 8 ? attend4_rows<16, W>(c, p, stream) : attend4_rows<8, W>(c, p, stream);
+}
+
 }  // namespace
 
 cudaError_t launch_cache4_attend(const kve_cache& c, const AttendParams& p, cudaStream_t stream) {
   const int64_t rows = static_cast<int64_t>(p.q_tokens) * p.c.group;
-  const int64_t blocks = static_cast<int64_t>(p.n_seq) * p.c.heads * ((rows + 15) / 16);
-  // Two CTAs an SM have a block each without cutting one: 4 warps a CTA, else 8, of 16 rows 6. (4 against 8: 64 ragged sequences of 8
-  // heads 50.6 and 56.1 us, 16 evicted 8.1 and 7.0, one of 131072 tokens 38.3 and 33.2, 8 of 32768 57.1 and 55.1. 16 rows, 4 against
-  // 6: 100 ragged ones 44.9 and 50.9, 16 of 8192 with 32 rows 79.9 and 80.3, 24 of 500 to 8192 33.5 both, one of 131072 55.0 and
-  // 49.2; 12 there 46.5, but 37.6 for the 24.)
-  const bool many = blocks >= 2 * c.sms;
-  if (rows > 8) return many ? attend4_rows<16, 4>(c, p, stream) : attend4_rows<16, 6>(c, p, stream);
-  // Many short ones, as a table says that holds no long ones: 2 warps (against 4: 1000 of 64 tokens 46.5 and 58.8, 400 of 20 to 800
-  // 39.1 and 43.5, of 50 to 4000 95.8 and 96.5; but of 100 to 8000 154 and 148, 200 of 50 to 800 28.8 both, 100 18.7 and 15.5).
-  if (blocks >= 16 * c.sms && static_cast<int64_t>(p.c.max_pages) << p.c.page_shift <= 4096) return attend4_rows<8, 2>(c, p, stream);
-  return many ? attend4_rows<8, 4>(c, p, stream) : attend4_rows<8, 8>(c, p, stream);
+  const int64_t blocks = static_cast<int64_t>(p.n_seq) * p.c.heads * (rows > 8 ? (rows + 15) / 16 : 1);
+  const int64_t longest = static_cast<int64_t>(p.c.max_pages) << p.c.page_shift;
+  // Few warps a CTA make the end of a part cheap, many cut a block into fewer parts and its steps among more.
+  // Three blocks an SM or more: 2 warps a CTA. (8 heads; 2 against 4 warps: 64 ragged sequences 46.2 and 46.9 us, 400 of 100 to 8000
+  // tokens 129 and 136, 400 of 20 to 800 34.7 and 41.7, 1000 of 64 42.2 and 63.3; 50 of 200 to 800, 400 blocks, 15.8 and 13.0. 16
+  // rows: 100 of 100 to 3000 39.5 and 41.9, 400 of 20 to 800 64 and 78.)
+  if (blocks >= 3 * c.sms) return attend4_warps<2>(c, p, stream);
+  // No more than one block an SM and a table that holds short ones only: 8 warps. (8 against 4: 16 of 96 to 700 6.6 and 7.6, 8 of 100 to
+  // 800 7.4 and 8.1, 8 of 500 to 2000 11.5 and 12.0, 19 of 50 to 1000 8.6 and 10.4; 24, 192 blocks, 10.5 and 8.8, 4 of 200 to 3000
+  // 13.3 and 11.0, 8 of 32768 56.3 and 51.0, one of 131072 32.0 and 32.8. 16 rows: 16 of 100 to 700 12.1 and 12.6, 19 of 100 to 2000
+  // 16.4 and 17.4.)
+  if (blocks <= c.sms && longest <= 2048) return attend4_warps<8>(c, p, stream);
+  return attend4_warps<4>(c, p, stream);
 }
 
 }  // namespace kve

@@ -32,7 +32,7 @@ constexpr int kAttendCtas = 2;       // attention CTAs an SM
 constexpr int kAttendRows = 16;      // most query rows of one attention row block
 constexpr int kAttendPartWords = kAttendRows * (kHeadDim + 2);   // a part: rows, their maxima and sums
 // The paged 4-bit cache
-constexpr int kAttend4Ctas = 7;      // most attention CTAs an SM
+constexpr int kAttend4Ctas = 6;      // most attention CTAs an SM
 constexpr int kAttend4PartWords = kAttendPartWords;
 
 // Request table and derived counts, identical on host and device.
