@@ -5,13 +5,13 @@
 //   out = sum_i softmax(l)_i s_i c_i + sum_i softmax(l)_i z_i,   lse = ln sum_i exp(l_i).
 // Scales and zeros never touch a code: both products are of the codes alone.
 //
-// Bound by the read of the cache, 136 bytes a token and head, and by start and end: 131072 tokens of 8 heads (143 MB) take 33.2 us
-// where a copy's rate is 21.3, and twice that (8 x 32768) 55.1, so between the two it runs at 97% of that rate, beside 11 us. Five of
-// them are any call's (96 tokens: lengths, cut, table, first codes, a step, output), the others the first copies of all CTAs at once
-// and the join. 64 ragged sequences of 512 to 16384 tokens (237 MB) take 50.6 us of 35.5, where CTAs have several parts. 430 warp
-// instructions for 32 tokens of 8 rows, half of them the integer unit's, of which more than half unpack codes, are close behind: each
-// tenth of them was 2 us there. With 16 rows (24 sequences of 500 to 8192 tokens 33.5 us of 10) they are 540, and for their registers
-// only three warps a scheduler, which wait for their own results.
+// Bound by the read of the cache, 136 bytes a token and head, and by start and end: 64 ragged sequences of 512 to 16384 tokens and 8
+// heads (237 MB) take 46.5 us where a copy's rate is 35.5, and 400 of 100 to 8000 (759 MB) 129, so between the two it runs at 94% of
+// that rate, beside 9 us. 5 of them are any call's (96 tokens: lengths, cut, table, first codes, a step, output); then the first copies
+// of all CTAs at once, the ends of parts, the join, which is longest for few heads of long sequences (one of 131072 tokens, 143 MB, 33.0
+// of 21.3). A step of a warp, 32 tokens and 8 rows, is 368 instructions, half of them the integer unit's, most of which unpack codes.
+// 16 rows are 489, of them 64 matrix products, and two warps a scheduler that wait for their own results: 24 sequences of 500 to 8192
+// tokens 29.1 us of 10, 16 of 8192 with 32 rows 74.5 of 21.7.
 //
 // A code becomes a matrix operand in registers, with half an instruction an element and no conversion: the low four bits of an f16
 // are the subnormal c 2^-24 and the next four 16 c 2^-24, so a word of eight codes is four operand registers by a shift and masks. The
@@ -34,7 +34,7 @@
 //
 // A warp takes 32 tokens a step from a ring of its own in shared memory, and has maxima, sums and output of its own: no warp waits for
 // another before a part ends. It fills its ring itself, across the ends of parts, by asynchronous copies that stand between its
-// products, with as few instructions as will do: each tenth of them is 2 us of the 64. (A tensor copy holds its warp for more than 100
+// products, with as few instructions as will do: a tenth of them was 2 us of the 64. (A tensor copy holds its warp for more than 100
 // cycles, and a step is four of them, with pages of 16 eight: 131072 tokens took 40.9 us for 38.2; one warp that fills all rings 40.8 for
 // 38.6. The next step's scores between the products with V 36.2 for 35.3, their registers.)
 //
