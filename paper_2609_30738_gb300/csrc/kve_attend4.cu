@@ -679,6 +679,7 @@ cache_attend4_kernel(const __grid_constant__ AttendParams P) {
     now ^= 1;
   }
 
+  copies_wait<0>();   // (the empty ones behind the last step write zeros into the ring)
   if (lost && lane == 0) atomicOr(P.err, kErrCheck);
 
   // sequences without a token: their rows are zeros
@@ -693,7 +694,6 @@ cache_attend4_kernel(const __grid_constant__ AttendParams P) {
   // ------------------------------------------------------------ the join of blocks that several CTAs had parts of
   allow_next_kernel();
   if (splits == 0) return;
-  copies_wait<0>();  // (the empty ones behind the last step write zeros into the ring)
   __syncthreads();   // every thread's part of the sums is out, and ctl.split is written
   if (threadIdx.x < splits) {
     int w0, w1;
