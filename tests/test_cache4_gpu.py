@@ -324,7 +324,7 @@ def test_attention_of_many_sequences_and_of_one_long():
 
 @pytest.mark.parametrize("n,longest,P,hq,hkv,t,last", [
     (40, 300, 32, 8, 8, 1, 9000), (40, 300, 16, 32, 8, 2, 4500), (310, 90, 16, 16, 8, 1, 700), (620, 40, 32, 4, 4, 2, 3000),
-    (700, 3, 16, 32, 4, 1, 4096), (40, 200, 16, 32, 8, 4, 2500), (62, 200, 64, 32, 8, 4, 3000), (470, 70, 32, 16, 1, 1, 900)])
+    (700, 3, 16, 32, 4, 1, 4096), (40, 200, 16, 32, 8, 4, 2500), (62, 200, 64, 32, 8, 4, 3000), (470, 70, 32, 16, 1, 1, 900), (1024, 30, 16, 4, 4, 1, 500)])
 def test_attention_of_many_blocks(n, longest, P, hq, hkv, t, last):
     torch, K = _k()
     rng = np.random.default_rng(n + P)
