@@ -41,6 +41,7 @@
 // every later length). A block that falls to several CTAs is joined by the one that finishes last, from
 // their fp32 parts in token order, so the sum does not depend on who that is.
 #include "kve_internal.h"
+#include "kve_line.cuh"
 #include "kve_ptx.cuh"
 
 namespace kve {
@@ -80,52 +81,14 @@ struct ACfg {
   static constexpr size_t kCtl = kP + kNp * kTileKeys;
 };
 
-// A (sequence, head, row block): the rows of one row block over one sequence's tiles, `first` their first in
-// the line of all tiles.
-struct Block {
-  int r, h, rb, len, tiles, first;
-  int index;   // its number among all blocks that have tiles
-};
-
-// How the line is cut. A part costs about kPartTiles tiles besides its own (its query rows, the tensor
-// cores' latency at its two ends, its output), so a block counts as its tiles and kPartTiles more units, and
-// the units are dealt evenly: CTA w's raw cut is floor(units * w / ctas). A cut that would leave fewer than
-// `least` tiles of a block on one of its sides moves to that end of the block: a join costs more than those
-// tiles do. That is 4 tiles where a share is 8 units at most and 2 where it is longer and evenness counts
+// How the line is cut (kve_line.cuh): a part costs about kPartTiles tiles besides its own (its query rows, the tensor
+// cores' latency at its two ends, its output), and cuts that would leave fewer than `least` tiles of a block move to its
+// end. That is 4 tiles where a share is 8 units at most and 2 where it is longer and evenness counts
 // for more: 16 sequences of 96 to 700 tokens take 8.6 us with 4 against 9.4 with 2 and 10.8 with 1, 24 of 500
 // to 8192 with 4 drafts each (a share of 16) 36.1 with 4 against 33.2 with 2 (32.6 with 1). With kPartTiles = 0 they
 // take 10.6 and 35.5, and 64 sequences of 512 to 16384 76.4 instead of 72.0. No more CTAs take part than have
 // kLeastUnits each, or a block.
-constexpr int kPartTiles = 2, kLeastUnits = 4;
-
-struct Cuts {
-  int each, rest, ctas, units, least;
-  uint32_t inverse;   // of ctas, 2^32 / ctas rounded up: exact for the products below ctas^2 that it divides
-  __device__ __forceinline__ void set(int n, int w) {
-    units = n;
-    ctas = w;
-    each = n / w;
-    rest = n - each * w;
-    least = each <= 8 ? 4 : 2;
-    inverse = 0xffffffffu / static_cast<uint32_t>(w) + 1u;   // (for one CTA 0, and rest is 0)
-  }
-  __device__ __forceinline__ int raw(int w) const {
-    return each * w + static_cast<int>(__umulhi(static_cast<uint32_t>(rest * w), inverse));
-  }
-  // the first w with raw(w) >= u
-  __device__ __forceinline__ int from(int u) const {
-    int w = min(max(static_cast<int>(static_cast<float>(u) * static_cast<float>(ctas) / static_cast<float>(units)), 0), ctas);
-    while (w > 0 && raw(w - 1) >= u) --w;
-    while (w < ctas && raw(w) < u) ++w;
-    return w;
-  }
-  // CTAs [*w0, *w1] have the parts of block b
-  __device__ __forceinline__ void parts(const Block& b, int* w0, int* w1) const {
-    const int a = b.first + (b.index + 1) * kPartTiles;   // its tile 0 in units
-    *w0 = from(a + least) - 1;
-    *w1 = from(a + b.tiles - least + 1) - 1;
-  }
-};
+constexpr int kPartTiles = 2;
 
 template <int R, int H>
 struct ACtl {
@@ -155,7 +118,7 @@ struct ACtl {
   Block split[2];                              // parts left for the join (each half writes the same)
   int last[2 * H], split_cta[2 * H];           // its parts, if they are all written; the CTA of the first
   Block blocks[kQBufs];                        // of the part in each query buffer; [0] first of the first part
-  Cuts cuts;
+  Cuts<kPartTiles> cuts;
   int ends[2];                                 // this CTA's tiles of the line
   int2 sums[ACfg<R, H>::kThreads / 32];        // tiles, sequences that have some
   uint32_t tmem_base;
@@ -165,24 +128,6 @@ struct ACtl {
 template <int R, int H>
 constexpr size_t attend_smem() {
   return ACfg<R, H>::kCtl + sizeof(ACtl<R, H>);
-}
-
-__device__ __forceinline__ int seq_len(const AttendParams& P, int r) {
-  return min(max(__ldg(P.lens + r), 0), P.c.max_pages << P.c.page_shift);
-}
-
-// The block behind b in the line; a tile follows, so a sequence that is not empty does.
-__device__ __forceinline__ void next_block(const AttendParams& P, int blocks, Block& b) {
-  b.first += b.tiles;
-  ++b.index;
-  if (++b.rb < blocks) return;
-  b.rb = 0;
-  if (++b.h < P.c.heads) return;
-  b.h = 0;
-  do {
-    b.len = seq_len(P, ++b.r);
-    b.tiles = (b.len + kTileKeys - 1) / kTileKeys;
-  } while (b.tiles == 0);
 }
 
 // The power of two that brings the largest magnitude (bf16 bits a, finite) into [128, 256), as fp32 bits.
@@ -216,13 +161,6 @@ __device__ __forceinline__ uint16_t to_bf16(float x) {
   uint16_t d;
   asm("cvt.rn.bf16.f32 %0, %1;" : "=h"(d) : "f"(x));
   return d;
-}
-
-// Probabilities are summed as 2^-len_bits(len) of themselves: then a row's unnormalised output passes the largest value
-// as little as its sum passes 1 (values of 2e38 would leave fp32 from two of them on). In return an output keeps an
-// absolute 2^-133 len, the last bit of the factor of O^T.
-__device__ __forceinline__ float len_bits(int len) {
-  return static_cast<float>(32 - __clz(len - 1));   // (1: 0)
 }
 
 // ln of a row's sum given the log2 of its unit (no token seen: -inf; a NaN sum is not 0, its row is NaN).
@@ -323,7 +261,7 @@ cache_attend_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_const
   const long long all_units = (static_cast<long long>(all_tiles) + all_filled * kPartTiles) * per_seq;
   const bool too_long = all_tiles >= 1 << 30 || all_units >= 1 << 30;
   if ((bad || too_long) && blockIdx.x == 0) atomicOr(P.err, kErrCheck);
-  Cuts cuts;   // (in shared memory for the join: no registers' business in between)
+  Cuts<kPartTiles> cuts;   // (in shared memory for the join: no registers' business in between)
   const int units = too_long ? 0 : static_cast<int>(all_units);
   cuts.set(units, max(min(max(units / kLeastUnits, all_filled * per_seq), static_cast<int>(gridDim.x)), 1));
   if (threadIdx.x == 0) ctl.cuts = cuts;
@@ -398,7 +336,7 @@ cache_attend_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_const
       };
       const auto step = [&](Ahead a) {
         ++a.x;
-        if (a.x < x1 && a.x == a.b.first + a.b.tiles) next_block(P, blocks, a.b);
+        if (a.x < x1 && a.x == a.b.first + a.b.tiles) next_block(P, blocks, kTileKeys, a.b);
         const int j = (a.x - a.b.first) * tile_pages + lane;
         a.id = -1;
         a.has = a.x < x1 && lane < tile_pages && (j << P.c.page_shift) < a.b.len;
@@ -592,7 +530,7 @@ cache_attend_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_const
         __syncwarp();
         if (lane == 0) mbar_arrive(&ctl.q_full[qb]);
         if (at.first + at.tiles >= x1) break;
-        next_block(P, blocks, at);
+        next_block(P, blocks, kTileKeys, at);
       }
     }
     // sequences without a token: their rows are zeros

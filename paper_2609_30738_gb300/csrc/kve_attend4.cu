@@ -172,10 +172,6 @@ __device__ __forceinline__ uint32_t f16x2(float lo, float hi) {
 __device__ __forceinline__ float low_bf16(uint32_t x) { return __uint_as_float(x << 16); }
 __device__ __forceinline__ float high_bf16(uint32_t x) { return __uint_as_float(x & 0xffff0000u); }
 
-// log2 of the unit in which a row's probabilities are summed: then a sum of values near bf16's largest passes that as
-// little as the probabilities' sum passes 1.
-__device__ __forceinline__ float len_bits(int len) { return static_cast<float>(32 - __clz(len - 1)); }   // (1: 0)
-
 template <int R, int W>
 __global__ void __launch_bounds__(A4Cfg<R, W>::kThreads, A4Cfg<R, W>::kCtas)
 cache_attend4_kernel(const __grid_constant__ AttendParams P) {

@@ -69,6 +69,10 @@ __device__ __forceinline__ void next_block(const AttendParams& P, int blocks, in
   } while (b.tiles == 0);
 }
 
+// log2 of the unit in which a row's probabilities are summed, 2^-len_bits(len) of themselves: then a row's unnormalised output passes
+// the largest value as little as its sum passes 1 (values of 2e38 would leave fp32 from two of them on).
+__device__ __forceinline__ float len_bits(int len) { return static_cast<float>(32 - __clz(len - 1)); }   // (1: 0)
+
 template <int kWarps>
 struct LineCtl {
   int2 sums[kWarps];   // tiles, sequences that have some
