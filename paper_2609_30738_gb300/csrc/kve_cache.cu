@@ -387,11 +387,29 @@ __device__ __forceinline__ void shrink_rows(uint8_t* codes, int row0, int end, f
   }
 }
 
+// Where a lane's 8 elements lie in a row: side by side, or as two pieces of 4, a and b.
+struct SideBySide {
+  int lane;
+  __device__ __forceinline__ uint4 load(const uint16_t* row) const { return __ldg(reinterpret_cast<const uint4*>(row) + lane); }
+  __device__ __forceinline__ void store(uint8_t* row, uint2 codes) const { reinterpret_cast<uint2*>(row)[lane] = codes; }
+};
+struct TwoPieces {
+  int a, b;
+  __device__ __forceinline__ uint4 load(const uint16_t* row) const {
+    const uint2 x = __ldg(reinterpret_cast<const uint2*>(row) + a), y = __ldg(reinterpret_cast<const uint2*>(row) + b);
+    return make_uint4(x.x, x.y, y.x, y.y);
+  }
+  __device__ __forceinline__ void store(uint8_t* row, uint2 codes) const {
+    reinterpret_cast<uint32_t*>(row)[a] = codes.x;
+    reinterpret_cast<uint32_t*>(row)[b] = codes.y;
+  }
+};
+
 // Writes rows [off, off + n) of a page (codes and scale of one head); x[i] holds this lane's 8
 // elements of page row kGroupRows g + i, zero outside the run. Every thread of the team comes here.
-template <int kPage>
+template <int kPage, class Where>
 __device__ __forceinline__ void write_run(const uint4 (&x)[kGroupRows], int off, int n, uint8_t* codes, float* scale,
-                                          uint32_t* team_max) {
+                                          uint32_t* team_max, const Where& where) {
   constexpr int kGroups = kPage / kGroupRows;
   const int lane = threadIdx.x & 15, g = (threadIdx.x / 16) % kGroups;
   uint32_t m = group_max(x, threadIdx.x & 16 ? 0xffff0000u : 0x0000ffffu);
@@ -407,14 +425,15 @@ __device__ __forceinline__ void write_run(const uint4 (&x)[kGroupRows], int off,
 #pragma unroll
   for (int i = 0; i < kGroupRows; ++i) {
     const int row = g * kGroupRows + i;
-    if (static_cast<uint32_t>(row - off) < static_cast<uint32_t>(n)) reinterpret_cast<uint2*>(codes + row * kHeadDim)[lane] = row_codes(x[i], inv);
+    if (static_cast<uint32_t>(row - off) < static_cast<uint32_t>(n)) where.store(codes + row * kHeadDim, row_codes(x[i], inv));
   }
   if (g == 0 && lane == 0) *scale = s;
 }
 
 // The same by one group, for a run of at most kGroupRows rows: x[i] is page row off + i, zero behind the run.
+template <class Where>
 __device__ __forceinline__ void write_short_run(const uint4 (&x)[kGroupRows], int off, int n, uint8_t* codes,
-                                                float* scale) {
+                                                float* scale, const Where& where) {
   const int lane = threadIdx.x & 15;
   const uint32_t lanes = threadIdx.x & 16 ? 0xffff0000u : 0x0000ffffu;
   const float held = off > 0 ? *scale : 0.f;
@@ -425,7 +444,7 @@ __device__ __forceinline__ void write_short_run(const uint4 (&x)[kGroupRows], in
   if (s > held) shrink_rows(codes, 0, off, held * inv, lane);
 #pragma unroll
   for (int i = 0; i < kGroupRows; ++i)
-    if (i < n) reinterpret_cast<uint2*>(codes + (off + i) * kHeadDim)[lane] = row_codes(x[i], inv);
+    if (i < n) where.store(codes + (off + i) * kHeadDim, row_codes(x[i], inv));
   if (lane == 0) *scale = s;
 }
 
@@ -478,7 +497,7 @@ __global__ void __launch_bounds__(kRowThreads<kPage>) cache_gather_kernel(const 
   }
   const int64_t block = static_cast<int64_t>(page) * P.c.heads + u.h;
   write_run<kPage>(x, 0, n, (values ? P.c.v : P.c.k) + block * (kPage * kHeadDim),
-                   (values ? P.c.v_scale : P.c.k_scale) + block, team_max[team]);
+                   (values ? P.c.v_scale : P.c.k_scale) + block, team_max[team], SideBySide{lane});
   allow_next_kernel();
 }
 
@@ -504,20 +523,17 @@ constexpr int64_t kStoreBlockTokens = 1024;
 template <class Params>
 constexpr int kStoreThreads = std::is_same_v<Params, CacheAppendParams> ? 768 : 1024;
 
-// The pairs that a lane turns: four side by side of its own elements, or where pairs are halves of the row, half of those that
-// it shares with its partner's lane. Then the two exchange the other halves, before and behind it, so that no turn is
-// computed twice in a row.
+// Of a row that turns, each of 16 lanes has both elements of four pairs, as its two pieces: no lane waits for another's, and no
+// turn is computed twice in a row.
 struct LaneTurns {
   uint2 turn[4];
-  int partner;   // its lane; -1: nothing is turned
-  bool second;   // this lane has the pairs' second elements
-  __device__ __forceinline__ void set(const RotaryTable& r, int lane) {
-    const int half = r.pairs >> 3;   // lanes with first elements (where partners are lanes apart)
-    second = !r.interleaved && lane >= half;
-    partner = lane >= 2 * half ? -1 : r.interleaved ? lane : second ? lane - half : lane + half;
-    const int from = r.interleaved ? 4 * lane : second ? 8 * (lane - half) + 4 : 8 * lane;
+  bool turns;
+  __device__ __forceinline__ TwoPieces set(const RotaryTable& r, int lane) {
+    turns = 4 * lane < r.pairs;
 #pragma unroll
-    for (int i = 0; i < 4; ++i) turn[i] = turn_at(r, min(from + i, kMaxPairs - 1));
+    for (int i = 0; i < 4; ++i) turn[i] = turn_at(r, 4 * lane + i);   // (of 64)
+    if (!r.interleaved && turns) return {lane, lane + (r.pairs >> 2)};
+    return {2 * lane, 2 * lane + 1};
   }
 };
 
@@ -530,23 +546,17 @@ __device__ __forceinline__ void turn_rows(uint4 (&x)[kGroupRows], const RotaryTa
   for (int i = 0; i < kGroupRows; ++i) {
     if (static_cast<uint32_t>(row0 + i) >= static_cast<uint32_t>(n)) continue;   // (all 16 lanes)
     const int p = __shfl_sync(lanes, pos, i, 16);
+    if (!turn.turns) continue;
     float2 cs[4];
 #pragma unroll
     for (int k = 0; k < 4; ++k) cs[k] = turn_of(turn.turn[k], r.amplitude, p);
     if (r.interleaved) {
-      if (turn.partner >= 0) turn_neighbours(x[i], cs);
-      continue;
+      turn_neighbours(x[i], cs);
+    } else {
+      uint32_t a[2] = {x[i].x, x[i].y}, b[2] = {x[i].z, x[i].w};
+      turn_halves(a, b, cs);
+      x[i] = make_uint4(a[0], a[1], b[0], b[1]);
     }
-    // first elements a, second ones b: of 0 .. 3 in the first lane, of 4 .. 7 in the second
-    const int other = turn.partner & 15;
-    const uint32_t s0 = __shfl_sync(lanes, turn.second ? x[i].x : x[i].z, other, 16);
-    const uint32_t s1 = __shfl_sync(lanes, turn.second ? x[i].y : x[i].w, other, 16);
-    uint32_t a[2] = {turn.second ? s0 : x[i].x, turn.second ? s1 : x[i].y};
-    uint32_t b[2] = {turn.second ? x[i].z : s0, turn.second ? x[i].w : s1};
-    turn_halves(a, b, cs);
-    const uint32_t t0 = __shfl_sync(lanes, turn.second ? a[0] : b[0], other, 16);
-    const uint32_t t1 = __shfl_sync(lanes, turn.second ? a[1] : b[1], other, 16);
-    if (turn.partner >= 0) x[i] = turn.second ? make_uint4(t0, t1, b[0], b[1]) : make_uint4(a[0], a[1], t0, t1);
   }
 }
 
@@ -595,8 +605,12 @@ cache_store_kernel(const __grid_constant__ Params A, uint32_t row_ctas) {
   const int32_t* slots = P.slots + first;
   const int64_t left = P.n_tokens - first;
   LaneTurns turn;
+  std::conditional_t<kTurn, TwoPieces, SideBySide> where = {};
   if constexpr (kTurn) {
-    if (!values) turn.set(A.turn.r, lane);
+    where = {2 * lane, 2 * lane + 1};
+    if (!values) where = turn.set(A.turn.r, lane);
+  } else {
+    where = {lane};
   }
   // the slots of the block and of what a run can reach behind it
   int longs = 0, shorts = 0;
@@ -672,16 +686,16 @@ cache_store_kernel(const __grid_constant__ Params A, uint32_t row_ctas) {
     for (int i = 0; i < kGroupRows; ++i) {
       x[i] = make_uint4(0, 0, 0, 0);
       if (static_cast<uint32_t>(row0 + i) < static_cast<uint32_t>(n))
-        x[i] = __ldg(reinterpret_cast<const uint4*>(from + (first + t + row0 + i) * st) + lane);
+        x[i] = where.load(from + (first + t + row0 + i) * st);
     }
     if constexpr (kTurn) {
       if (!values) turn_rows(x, A.turn.r, pos, row0, n, turn);
     }
     if (whole_team) {
-      write_run<kPage>(x, off, n, codes + block * (kPage * kHeadDim), scales + block, team_max[team]);
+      write_run<kPage>(x, off, n, codes + block * (kPage * kHeadDim), scales + block, team_max[team], where);
       team_sync<kPage>();   // team_max and the scale before the next run
     } else {
-      write_short_run(x, off, n, codes + block * (kPage * kHeadDim), scales + block);
+      write_short_run(x, off, n, codes + block * (kPage * kHeadDim), scales + block, where);
     }
   }
   allow_next_kernel();
