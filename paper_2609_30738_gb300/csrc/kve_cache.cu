@@ -518,8 +518,8 @@ __global__ void __launch_bounds__(kRowThreads<kPage>) cache_gather_kernel(const 
 // 7.3: 2000 teams of 8 runs, of which 1216 fit at once, are two rounds of that chain.
 constexpr int64_t kStoreBlockTokens = 1024;
 
-// Threads an SM: the rotating append's have the turns of their rows beside the rows. (512, 640, 768, 896, 1024: 24k tokens 111.5, 102.6,
-// 100.9, 101.9 and 108.1 us, 2000 tokens 12.0, 11.0, 11.3, 12.4 and 14.1, 16 tokens 2.8, 2.9, 3.2, 3.4 and 3.5.)
+// Threads an SM: the rotating append's have the turns of their rows beside the rows. (512, 640, 768, 896, 1024: 24k tokens 107.4, 99.2,
+// 96.5, 97.8 and 102.6 us, 2000 tokens 11.6, 11.0, 10.4, 11.7 and 12.7, 16 tokens 2.6, 2.8, 2.8, 3.0 and 3.2.)
 template <class Params>
 constexpr int kStoreThreads = std::is_same_v<Params, CacheAppendParams> ? 768 : 1024;
 
@@ -562,10 +562,10 @@ __device__ __forceinline__ void turn_rows(uint4 (&x)[kGroupRows], const RotaryTa
 
 // With parameters of the rotating append the CTAs behind the first row_ctas turn the queries, and those turn the keys on their
 // way: they start first because they take longer (as the last: 2000 tokens 14.8 us for 11.7, 1000 x 8 23.1 for 20.1, 24k 102.6
-// for 101.9; evenly between the others 13.6, 24.5 and 112). 24k tokens with 32 query heads (537 MB) take 100.9 us of 80.3 at a copy's
-// rate, without the queries 48.5 where the plain store has 28: every head's rows compute their turns. (Kept in shared memory for four
-// heads one after the other 114.9, for two 120.) One body with the plain store as a kernel of its own: as a function of both it
-// spilled three times as much.
+// for 101.9; evenly between the others 13.6, 24.5 and 112, all at the time). 24k tokens with 32 query heads (537 MB) take 96.5 us of
+// 80.3 at a copy's rate, 6000 without their queries 16.8 of 9.2: every head's rows compute their turns. (With elements side by side, the
+// pairs' halves exchanged by shuffles, 100.9 and 18.9; turns kept in shared memory for four heads one after the other 114.9, for two
+// 120.) One body with the plain store as a kernel of its own: as a function of both it spilled three times as much.
 template <int kPage, class Params>
 __global__ void __launch_bounds__(kRowThreads<kPage>, kStoreThreads<Params> / kRowThreads<kPage>)
 cache_store_kernel(const __grid_constant__ Params A, uint32_t row_ctas) {
