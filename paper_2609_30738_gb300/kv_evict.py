@@ -483,8 +483,9 @@ class Rotary:
     def __init__(self, head_dim: int = 128, rotary_dim: int | None = None, base: float = 10000.0, interleaved: bool = False,
                  scaling: str = "none", factor: float = 1.0, original_length: float = 0.0, low_turns: float = 1.0,
                  high_turns: float | None = None, frequencies=None, amplitude: float | None = None):
+        import torch
         lib = _lib()
-        self._h = None
+        self._h, self._i32 = None, torch.int32
         self.head_dim, self.rotary_dim = int(head_dim), int(head_dim if rotary_dim is None else rotary_dim)
         self.interleaved = bool(interleaved)
         if frequencies is None:
@@ -523,7 +524,7 @@ class Rotary:
             raise ValueError(f"rotate: x and out are [tokens, heads, {self.head_dim}]")
         heads, device = shape[-2], x.get_device()
         tokens = x.numel() // (heads * self.head_dim) if heads else 0
-        if str(positions.dtype) != "torch.int32" or positions.numel() != tokens or not positions.is_contiguous():
+        if positions.dtype is not self._i32 or positions.numel() != tokens or not positions.is_contiguous():
             raise ValueError("rotate: positions are one contiguous int32 value a token")
         if device < 0 or out.get_device() != device or positions.get_device() != device:
             raise ValueError("rotate: x, out and positions are on one CUDA device")
