@@ -534,9 +534,9 @@ kve_status kv_evict_cache_append(const kve_cache* cache, const kve_rotary* rotar
  *    undefined codes (its row only).
  *  * Attention: l = (s (q . c) + z sum q) / sqrt(d), out = sum p s c + sum p z, statistics and sums in
  *    fp32. What is held in fewer bits: a query element below 2^-27 of its row's largest to 2^-35
- *    of that; p s to 2^-12 of itself, or to 2^-31 of the largest p s so far, whichever is more; p z
- *    to len * 2^-149. A query row with an infinity, a NaN or a magnitude of 2^112 or more
- *    gives NaN.
+ *    of that; p s to 2^-12 of itself, or to 2^-31 of the largest p s so far, whichever is more; the sum
+ *    of p z to len * 2^-149. A p below 2^-126 of its row's largest may count as 0. A query row with an
+ *    infinity, a NaN or a magnitude of 2^112 or more gives NaN.
  * ---------------------------------------------------------------------------------- */
 kve_status kv_evict_cache4_create(const kve_cache_config* cfg, uint8_t* k, uint8_t* v, uint16_t* k_param,
                                   uint16_t* v_param, kve_cache** cache_out, size_t* workspace_bytes);

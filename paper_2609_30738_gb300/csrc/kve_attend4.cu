@@ -30,7 +30,9 @@
 //      itself down to 2^-20 of that reference, an absolute 2^-31 of it below.
 // Maxima, sums, the part of z and the output are fp32. The reference of w is the product's own, not the probability's, so
 // that a token of far larger values costs the others nothing where it hardly counts. References move only when a maximum
-// passes them by 2^8, which leaves the rescaling of the output to a few steps.
+// passes them by 2^8, which leaves the rescaling of the output to a few steps. What a warp leaves at the end of a part, and a CTA for the join, is
+// the average over its tokens beside their maximum and sum, so values at either end of fp32 keep their bits whatever the length; the sum
+// of p z before that is scaled down by the length only once a |z| of 2^96 comes.
 //
 // A warp takes 32 tokens a step from a ring of its own in shared memory, and has maxima, sums and output of its own: no warp waits for
 // another before a part ends. It fills its ring itself, across the ends of parts, by asynchronous copies that stand between its
@@ -161,6 +163,7 @@ __device__ __forceinline__ uint4 load_now(const void* p) {
 }
 
 __device__ __forceinline__ float2 both(float x) { return make_float2(x, x); }
+constexpr uint32_t kLargeZ = (127u + 96u) << 23;   // 2^96: sums of up to 2^30 tokens below it stay in fp32
 constexpr float kNone = -3e38f;   // a maximum of nothing: finite, so that differences to it are no NaN
 
 __device__ __forceinline__ uint32_t f16x2(float lo, float hi) {
@@ -168,6 +171,16 @@ __device__ __forceinline__ uint32_t f16x2(float lo, float hi) {
   asm("cvt.rn.f16x2.f32 %0, %1, %2;" : "=r"(d) : "f"(hi), "f"(lo));
   return d;
 }
+
+// 2^x down to fp32's last bit (ex2 gives 0 below 2^-126).
+__device__ __forceinline__ float ex2_small(float x) {
+  float y;
+  asm("ex2.approx.f32 %0, %1;" : "=f"(y) : "f"(x));
+  return y;
+}
+
+// What a row's sums are divided by; 0 for a row that saw nothing (its sums are 0).
+__device__ __forceinline__ float over(float sum) { return sum == 0.f ? 0.f : rcp(sum); }
 
 __device__ __forceinline__ float low_bf16(uint32_t x) { return __uint_as_float(x << 16); }
 __device__ __forceinline__ float high_bf16(uint32_t x) { return __uint_as_float(x & 0xffff0000u); }
@@ -380,7 +393,6 @@ cache_attend4_kernel(const __grid_constant__ AttendParams P) {
   for (int x = x0; x < x1;) {
     const Part& part = ctl.part[now];
     const Block& b = part.b;
-    const float lb = len_bits(b.len);
     if (x == x0) {   // (not before: the queries' exchanges would wait behind these copies)
 #pragma unroll 1
       for (int i = 1; i < S - 1; ++i) {
@@ -405,6 +417,7 @@ cache_attend4_kernel(const __grid_constant__ AttendParams P) {
       m[e] = top[e] = both(kNone);
       l[e] = z[e] = both(0.f);
     }
+    float unit = 1.f;   // of z
     const int first = part.template first<W>(warp), last = part.template first<W>(warp + 1);
     const int tok0 = part.tok0, all_see = b.len - P.q_tokens + 1;
 #pragma unroll 1
@@ -418,7 +431,12 @@ cache_attend4_kernel(const __grid_constant__ AttendParams P) {
         // a lane a token: its four numbers for every lane
         const uint32_t* const n = reinterpret_cast<const uint32_t*>(at + kNumbers);
         const uint32_t a = n[lane], c = n[kStep + lane];
-        ctl.tokens[warp][lane] = make_float4(low_bf16(a), high_bf16(a), lg2(low_bf16(c)), high_bf16(c));
+        if (__any_sync(0xffffffffu, (c & 0x7f800000u) >= kLargeZ) && unit == 1.f) {   // (as the sum so far)
+          unit = ex2(-len_bits(b.len));
+#pragma unroll
+          for (int e = 0; e < kHalves; ++e) z[e] = fmul2(z[e], both(unit));
+        }
+        ctl.tokens[warp][lane] = make_float4(low_bf16(a), high_bf16(a), lg2(low_bf16(c)), high_bf16(c) * unit);
       }
       float s[2][kHalves][4];
       {
@@ -525,7 +543,7 @@ cache_attend4_kernel(const __grid_constant__ AttendParams P) {
       const auto weigh = [&](auto kSome) {
 #pragma unroll
         for (int e = 0; e < kHalves; ++e) {
-          const float2 mr = make_float2(-(m[e].x + lb), -(m[e].y + lb));
+          const float2 mr = make_float2(-m[e].x, -m[e].y);
           const float2 tr = make_float2(14.f - kLazy - top[e].x, 14.f - kLazy - top[e].y);
 #pragma unroll
           for (int i = 0; i < 4; ++i) {
@@ -601,19 +619,21 @@ cache_attend4_kernel(const __grid_constant__ AttendParams P) {
           zz.x += __shfl_xor_sync(0xffffffffu, zz.x, d);
           zz.y += __shfl_xor_sync(0xffffffffu, zz.y, d);
         }
-        // quarters of sum p (s c + z), so that neither term alone passes the largest float: products of c 2^-24 or
-        // 16 c 2^-24 with weights times 2^(14 - kLazy)
-        const float f[2] = {ex2(top[e].x - all.x - lb), ex2(top[e].y - all.y - lb)};
-        const float zq[2] = {0.25f * zz.x, 0.25f * zz.y};
+        // The warp's averages, as quarters, so that neither sum p s c nor sum p z alone passes the largest float: products of c 2^-24
+        // or 16 c 2^-24 with weights times 2^(14 - kLazy). Averages keep the bits of values near either end of fp32, which sums of
+        // fractions of them would lose.
+        const float ov[2] = {over(ll.x), over(ll.y)}, back = 0.25f / unit;
+        const float f[2] = {ex2_small(top[e].x - all.x), ex2_small(top[e].y - all.y)};
+        const float zq[2] = {zz.x * ov[0] * back, zz.y * ov[1] * back};
 #pragma unroll
         for (int j = 0; j < 2; ++j)
 #pragma unroll
           for (int i = 0; i < 4; ++i) {
             float4 v;
-            v.x = fmaf(o[2 * i][e][j] * 65536.f, f[j], zq[j]);
-            v.y = fmaf((o[2 * i][e][2 + j] - o[2 * i][e][j]) * 4096.f, f[j], zq[j]);
-            v.z = fmaf(o[2 * i + 1][e][j] * 65536.f, f[j], zq[j]);
-            v.w = fmaf((o[2 * i + 1][e][2 + j] - o[2 * i + 1][e][j]) * 4096.f, f[j], zq[j]);
+            v.x = fmaf(o[2 * i][e][j] * (65536.f * ov[j]), f[j], zq[j]);
+            v.y = fmaf((o[2 * i][e][2 + j] - o[2 * i][e][j]) * (4096.f * ov[j]), f[j], zq[j]);
+            v.z = fmaf(o[2 * i + 1][e][j] * (65536.f * ov[j]), f[j], zq[j]);
+            v.w = fmaf((o[2 * i + 1][e][2 + j] - o[2 * i + 1][e][j]) * (4096.f * ov[j]), f[j], zq[j]);
             // columns 32 i + 4 g of row 2 t + j; 16 bytes c of row r lie at c ^ (r & 6)
             reinterpret_cast<float4*>(mine + (2 * t + j) * kHeadDim)[(8 * i + g) ^ (2 * t)] = v;
           }
@@ -645,9 +665,14 @@ cache_attend4_kernel(const __grid_constant__ AttendParams P) {
           mx = fmaxf(mx, f[w]);
         }
 #pragma unroll
+        for (int w = 0; w < W; ++w) {   // (shares of the sum)
+          f[w] = ctl.at[w] >= 0 ? ctl.l[w][row] * ex2(f[w] - mx) : 0.f;
+          sum += f[w];
+        }
+        const float ov = over(sum);
+#pragma unroll
         for (int w = 0; w < W; ++w) {
-          f[w] = ex2(f[w] - mx);
-          sum = fmaf(ctl.at[w] >= 0 ? ctl.l[w][row] : 0.f, f[w], sum);
+          f[w] *= ov;
           a.x = fmaf(v[w].x, f[w], a.x);
           a.y = fmaf(v[w].y, f[w], a.y);
           a.z = fmaf(v[w].z, f[w], a.z);
@@ -655,7 +680,7 @@ cache_attend4_kernel(const __grid_constant__ AttendParams P) {
         }
         const int r = 8 * e + row;
         if (whole) {
-          emit_row(P, b, b.rb * R + r, rows, row_token, a, mx, sum, lb, lane);
+          emit_row(P, b, b.rb * R + r, rows, row_token, a, mx, sum, lane);
         } else {
           reinterpret_cast<float4*>(out + r * kHeadDim)[lane] = a;
           if (lane == 0) {
@@ -749,13 +774,15 @@ cache_attend4_kernel(const __grid_constant__ AttendParams P) {
       float f[kRows];
 #pragma unroll
       for (int k = 0; k < kRows; ++k) {
-        const float top = fmaxf(mx[k], warp_max(pm[k])), back = ex2(mx[k] - top);
+        const float top = fmaxf(mx[k], warp_max(pm[k])), kept = sum[k] * ex2(mx[k] - top);
         mx[k] = top;
-        f[k] = ex2(pm[k] - top);
-        pl[k] *= f[k];
+        pl[k] *= ex2(pm[k] - top);
+        f[k] = pl[k];
 #pragma unroll
         for (int d = 16; d > 0; d >>= 1) pl[k] += __shfl_xor_sync(0xffffffffu, pl[k], d);
-        sum[k] = fmaf(sum[k], back, pl[k]);
+        sum[k] = kept + pl[k];
+        const float ov = over(sum[k]), back = kept * ov;
+        f[k] *= ov;
         acc[k].x *= back, acc[k].y *= back, acc[k].z *= back, acc[k].w *= back;
       }
       for (int j0 = 0;;) {
@@ -786,10 +813,12 @@ cache_attend4_kernel(const __grid_constant__ AttendParams P) {
       __syncthreads();
       if (works && team == 0)
         for (int w = row0 + there; w < teams * there; w += there) {
-          const float top = fmaxf(mx[0], ctl.m[w][0]), a = ex2(mx[0] - top), c = ex2(ctl.m[w][0] - top);
+          const float top = fmaxf(mx[0], ctl.m[w][0]);
+          const float mine = sum[0] * ex2(mx[0] - top), other = ctl.l[w][0] * ex2(ctl.m[w][0] - top);
           const float4 v = sums[w * 32 + lane];
           mx[0] = top;
-          sum[0] = fmaf(sum[0], a, ctl.l[w][0] * c);
+          sum[0] = mine + other;
+          const float ov = over(sum[0]), a = mine * ov, c = other * ov;
           acc[0] = make_float4(fmaf(acc[0].x, a, v.x * c), fmaf(acc[0].y, a, v.y * c), fmaf(acc[0].z, a, v.z * c),
                                fmaf(acc[0].w, a, v.w * c));
         }
@@ -798,7 +827,7 @@ cache_attend4_kernel(const __grid_constant__ AttendParams P) {
 #pragma unroll
       for (int k = 0; k < kRows; ++k)
         if (row0 + k * W < there)
-          emit_row(P, s, s.rb * R + row0 + k * W, rows, row_token, acc[k], mx[k], sum[k], len_bits(s.len), lane);
+          emit_row(P, s, s.rb * R + row0 + k * W, rows, row_token, acc[k], mx[k], sum[k], lane);
   }
 }
 

@@ -69,8 +69,8 @@ __device__ __forceinline__ void next_block(const AttendParams& P, int blocks, in
   } while (b.tiles == 0);
 }
 
-// log2 of the unit in which a row's probabilities are summed, 2^-len_bits(len) of themselves: then a row's unnormalised output passes
-// the largest value as little as its sum passes 1 (values of 2e38 would leave fp32 from two of them on).
+// log2 of the unit in which a row's sums over tokens are held where they could leave fp32, 2^-len_bits(len) of themselves: then a
+// sum passes the largest value as little as the average does (values of 2e38 would leave fp32 from two of them on).
 __device__ __forceinline__ float len_bits(int len) { return static_cast<float>(32 - __clz(len - 1)); }   // (1: 0)
 
 template <int kWarps>
@@ -178,22 +178,21 @@ __device__ __forceinline__ void line_share(const AttendParams& P, int blocks, in
   }
 }
 
-// One output row: quarters of sum p v (four columns a lane), the log2 of the largest p, sum p in units of 2^-lb.
+// One output row: a quarter of the average of v (four columns a lane), the log2 of the largest p, sum p in units of that.
 template <class RowToken>
 __device__ __forceinline__ void emit_row(const AttendParams& P, const Block& b, int row, int rows, RowToken row_token,
-                                         const float4& a, float top, float sum, float lb, int lane) {
+                                         const float4& a, float top, float sum, int lane) {
   if (row >= rows) return;
   const int t = row_token(row), hq = b.h * P.c.group + row - t * P.c.group;
   const int64_t tok = static_cast<int64_t>(b.r) * P.q_tokens + t;
-  const float inv = sum == 0.f ? 0.f : __frcp_rn(sum);
   const auto pair = [&](float x, float y) {
     uint32_t d;
-    asm("cvt.rn.bf16x2.f32 %0, %1, %2;" : "=r"(d) : "f"(y * inv * 4.f), "f"(x * inv * 4.f));
+    asm("cvt.rn.bf16x2.f32 %0, %1, %2;" : "=r"(d) : "f"(y * 4.f), "f"(x * 4.f));
     return d;
   };
   reinterpret_cast<uint2*>(P.out + tok * P.o_st + hq * P.o_sh)[lane] = make_uint2(pair(a.x, a.y), pair(a.z, a.w));
   if (P.lse && lane == 0)
-    P.lse[tok * P.c.hq + hq] = sum == 0.f ? -INFINITY : (top + lb + lg2(sum)) * 0.69314718056f;
+    P.lse[tok * P.c.hq + hq] = sum == 0.f ? -INFINITY : (top + lg2(sum)) * 0.69314718056f;
 }
 
 }  // namespace kve

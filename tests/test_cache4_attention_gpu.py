@@ -1,0 +1,64 @@
+"""Attention over the paged 4-bit cache where its sums come near the ends of fp32."""
+
+import numpy as np
+import pytest
+
+from oracle import cache4_oracle as Q
+from tests import cache8 as T
+from tests.test_cache4_gpu import _attend, _k
+
+pytestmark = pytest.mark.gpu
+
+
+@pytest.mark.parametrize("lens,hq,hkv,t", [([5000, 9000, 300], 4, 1, 1), ([70001], 8, 1, 2), ([3000] * 40, 8, 8, 1)])
+def test_small_values_of_long_sequences(lens, hq, hkv, t):
+    # s of about 2^-119, the least that a row is written with: none of its bits may go with the length
+    torch, K = _k()
+
+    def small(k, kp, v, vp, tables, q):
+        vp[:] = T.bf16(vp * 2.0 ** -118)
+    cache = _attend(K, np.random.default_rng(sum(lens)), lens, 32, hq, hkv, t, shake=small)[0]
+    assert cache.status() == K.KVE_OK
+
+
+def _one_far(z, codes, size, rest):
+    """q = 1/2 everywhere and keys of zeros but one, whose logit is 64 z / sqrt(d): a token of given probability, with values
+    of `size`, among some of size `rest`."""
+    def shake(k, kp, v, vp, tables, q):
+        q[:] = 0.5
+        kp[...] = 0.0
+        page, off = tables[0, 0, 5], 7
+        kp[page, :, off, 1] = z
+        vp[:] = T.bf16(vp * rest)
+        v[page, :, off] = codes
+        vp[page, :, off] = [size, -8 * size]
+    return shake
+
+
+@pytest.mark.parametrize("P,lens,hq,hkv,t", [(128, [9000], 4, 1, 1), (16, [2000], 8, 1, 2)])
+@pytest.mark.parametrize("size", [2.0 ** 90, 2.0 ** 100])
+def test_far_values_that_hardly_count(P, lens, hq, hkv, t, size):
+    # 64 z / sqrt(128) = -83.44: a probability of 2^-120.4 of the others', by values that much larger than theirs. Both parts of
+    # such a token's values count, s c and z, which nearly cancel where c is 8.
+    torch, K = _k()
+    rng = np.random.default_rng(5)
+    for codes in (0x88, rng.integers(0, 256, 64)):
+        shake = _one_far(-14.75, codes, size, size * 2.0 ** -138)
+        cache = _attend(K, np.random.default_rng(lens[0]), lens, P, hq, hkv, t, shake=shake)[0]
+        assert cache.status() == K.KVE_OK
+
+
+def test_the_largest_values_among_small_ones():
+    # rows of bf16's largest values behind thousands of small ones and in front of them, at every length's unit
+    torch, K = _k()
+    rng = np.random.default_rng(6)
+
+    def large(k, kp, v, vp, tables, q):
+        c, f = Q.encode(T.bf16(np.where(rng.random((len(lens), v.shape[1], 128)) < 0.5, 3.3e38, -3.3e38)))
+        for s, n in enumerate(lens):
+            for i in {0, n // 2, n - 1}:
+                page, off = tables[0, s, i // 64], i % 64
+                v[page, :, off], vp[page, :, off] = Q.pack(c[s]), f[s]
+    lens = [5000, 1, 3, 700, 2500]
+    _, out, _, _, _ = _attend(K, rng, lens, 64, 8, 2, 1, shake=large)
+    assert torch.isfinite(out).all()
