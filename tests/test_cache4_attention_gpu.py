@@ -1,4 +1,4 @@
-"""Attention over the paged 4-bit cache where its sums come near the ends of fp32."""
+"""Attention over the paged 4-bit cache where its sums come near the ends of fp32, and where its blocks are cut."""
 
 import numpy as np
 import pytest
@@ -62,3 +62,37 @@ def test_the_largest_values_among_small_ones():
     lens = [5000, 1, 3, 700, 2500]
     _, out, _, _, _ = _attend(K, rng, lens, 64, 8, 2, 1, shake=large)
     assert torch.isfinite(out).all()
+
+
+def _split_blocks(lens, heads, row_blocks, tile, ctas, part=3):
+    """How many blocks of rows fall to two CTAs or more, by the rule of the line: a block counts as its tiles and `part`
+    more, all is dealt evenly, and no cut leaves fewer than `least` tiles of a block on one of its sides."""
+    blocks = [-(-n // tile) for n in lens if n > 0 for _ in range(heads * row_blocks)]
+    units = sum(blocks) + part * len(blocks)
+    ctas = max(min(max(units // 4, len(blocks)), ctas), 1)
+    least = 4 if units // ctas <= 8 else 2
+    cuts = np.array([units * w // ctas for w in range(1, ctas)])
+    first = np.cumsum([0] + [n + part for n in blocks])[:-1] + part
+    return sum(bool(((cuts - a >= least) & (cuts - a <= n - least)).any()) for a, n in zip(first, blocks))
+
+
+# a table of at most 2048 tokens and no more blocks than SMs: 8 warps a CTA, tiles of 256 tokens. The rows of a block are dealt
+# to 8, 4, 2 (with and without idle warps) or one team of warps at the join, and 9 rows or more take the 16-row kernel
+@pytest.mark.parametrize("n,length,P,hq,hkv,t", [
+    (16, 2000, 32, 8, 8, 1), (16, 2000, 16, 24, 8, 1), (16, 2000, 64, 32, 8, 1), (16, 2000, 128, 64, 8, 1), (8, 1900, 64, 8, 8, 2),
+    (8, 1900, 32, 24, 8, 1), (8, 1900, 16, 40, 8, 1), (8, 1900, 128, 8, 8, 7), (16, 2000, 32, 128, 8, 1), (8, 1900, 64, 24, 8, 4),
+    (5, 2000, 32, 32, 8, 4), (4, 2000, 64, 64, 8, 3)])
+def test_blocks_of_eight_warps_are_joined(n, length, P, hq, hkv, t):
+    torch, K = _k()
+    lens = [length - i % 3 for i in range(n)]
+    rows, sms = t * hq // hkv, torch.cuda.get_device_properties(0).multi_processor_count
+    row_blocks = -(-rows // 16) if rows > 8 else 1
+    assert n * hkv * row_blocks <= sms and -(-length // P) * P <= 2048
+    if sms == 152:
+        assert _split_blocks(lens, hkv, row_blocks, 256, sms) > 0
+    cache, out, lse, args, _ = _attend(K, np.random.default_rng(n + hq + t), lens, P, hq, hkv, t, fused=True)
+    assert cache.status() == K.KVE_OK
+    for _ in range(3):
+        again, l2 = torch.empty_like(out), torch.empty_like(lse)
+        cache.attend(*args, again, l2)
+        assert torch.equal(again, out) and torch.equal(l2, lse)
