@@ -526,9 +526,9 @@ kve_status kv_evict_cache_append(const kve_cache* cache, const kve_rotary* rotar
  *  * Pages:  k, v [num_pages][H][P][d / 2] uint8: codes c in 0 .. 15, element 2i in the low and
  *    2i + 1 in the high half of byte i; k_param, v_param [num_pages][H][P][2] bf16: s and z of each
  *    row, an element being s c + z. (128-byte and 16-byte aligned.)
- *  * A row x is written as z = min x, s = RN_bf16(fl((max x - min x) / 15)), fl in fp32, c = (x - z) / s
- *    rounded to the nearest (ties to even); s = 0 and c = 0 where s would be below 2^-120. An element is off by
- *    at most 0.53 of a step s. A row with an infinity or a NaN becomes s = z = NaN, c = 0, and so
+ *  * A row x is written as z = min x, s = RN_bf16(fl(fl((max x - min x) / 16) * fl(16 / 15))),
+ *    c = fl(fl((x - z) / 16) / (s / 16)) rounded to the nearest integer (ties to even), fl to fp32;
+ *    s = 0 and c = 0 where s would be below 2^-120. An element is off by at most 0.53 of a step s. A row with an infinity or a NaN becomes s = z = NaN, c = 0, and so
  *    NaN wherever it is seen.
  *  * Rows share nothing: a page may be written in any order, and a slot that a call names twice gets
  *    undefined codes (its row only).

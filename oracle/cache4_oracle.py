@@ -69,8 +69,8 @@ def encode(rows):
     lo, hi = x.min(-1) + 0.0, x.max(-1)
     s = _bf16(np.float32(np.float32(hi / 16 - lo / 16) * np.float32(16 / 15)))
     s = np.where(s >= 2.0 ** -120, s, 0.0)
-    # (hi - lo may pass fp32, not float64)
-    c = np.minimum(np.rint((x - lo[..., None]) / np.where(s > 0, s, 1.0)[..., None]), 15)
+    unit = np.float32(np.where(s > 0, s, 1.0) / 16)[..., None]
+    c = np.minimum(np.rint(np.float32(x / 16 - lo[..., None] / 16) / unit), 15)
     c = np.where((s > 0)[..., None], c, 0).astype(np.uint8)
     param = np.stack([s, lo], -1)
     return c, np.where(good[..., None], param, np.nan)

