@@ -234,8 +234,8 @@ struct GatherParams {
 };
 
 // Rotary positions: pair j turns by f_j radians a position. turns[j] is f_j / (2 pi) without its whole turns, in units
-// of 2^-64, y 2^32 + x with x signed: position times that, modulo 2^64, is the angle of any 32-bit position without a
-// rounding.
+// of 2^-64 to the nearest, y 2^32 + x with x signed: position times that, modulo 2^64, is the angle of any 32-bit position
+// to 2^-33 of a turn.
 constexpr int kMaxPairs = kHeadDim / 2;
 struct RotaryTable {
   uint2 turns[kMaxPairs];

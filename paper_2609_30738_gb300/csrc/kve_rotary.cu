@@ -26,6 +26,30 @@ __global__ void __launch_bounds__(kRotateThreads, 4) rotate_kernel(const __grid_
   allow_next_kernel();
 }
 
+// f / (2 pi) without its whole turns, in units of 2^-64 to the nearest (|f| < 2^62: within an eighth of a unit more). f = m 2^e with
+// an integer m of 53 bits, times 1 / (2 pi) in 128 bits; a division in 64-bit floating point would be off by 2^-56 of a turn, which a
+// position of 2^31 makes 2^-25.
+uint64_t units_of_turn(double f) {
+  constexpr uint64_t kHigh = 0x28be60db9391054aull, kLow = 0x7f09d5f47d4d3770ull;   // 2^128 / (2 pi)
+  int e = 0;
+  const uint64_t m = static_cast<uint64_t>(std::ldexp(std::frexp(std::fabs(f), &e), 53));
+  using Wide = unsigned __int128;
+  const Wide low = static_cast<Wide>(m) * kLow, high = static_cast<Wide>(m) * kHigh + (low >> 64);
+  const uint64_t w[4] = {static_cast<uint64_t>(low), static_cast<uint64_t>(high), static_cast<uint64_t>(high >> 64), 0};
+  // the product's bits from 2^shift on
+  const int shift = 117 - e;
+  uint64_t units = 0;
+  if (shift <= 0) {
+    units = shift > -64 ? w[0] << -shift : 0;
+  } else if (shift < 192) {
+    const int i = shift / 64, by = shift % 64;
+    units = by == 0 ? w[i] : w[i] >> by | w[i + 1] << (64 - by);
+    const int half = shift - 1;
+    units += w[half / 64] >> half % 64 & 1u;
+  }
+  return f < 0.0 ? 0 - units : units;
+}
+
 }  // namespace
 
 cudaError_t launch_rotate(const RotateParams& params, cudaStream_t stream) {
@@ -84,13 +108,10 @@ kve_status kv_evict_rotary_create(int32_t head_dim, int32_t rotary_dim, int32_t 
   if (!h) return KVE_ENOMEM;
   std::memset(h, 0, sizeof(*h));
   for (int j = 0; j < rotary_dim / 2; ++j) {
-    const double turns = frequencies[j] / 6.283185307179586476925;
-    const double part = turns - std::floor(turns);   // [0, 1]
-    // high 2^32 + low, |low| <= 2^31 (a whole turn is none)
-    const double high = std::floor(part * 4294967296.0 + 0.5);
-    const double low = std::fmin((part * 4294967296.0 - high) * 4294967296.0, 2147483647.0);
-    h->table.turns[j].y = static_cast<uint32_t>(static_cast<uint64_t>(high));
-    h->table.turns[j].x = static_cast<uint32_t>(static_cast<int32_t>(low));
+    // high 2^32 + low, with low signed
+    const uint64_t units = kve::units_of_turn(frequencies[j]);
+    h->table.turns[j].x = static_cast<uint32_t>(units);
+    h->table.turns[j].y = static_cast<uint32_t>((units >> 32) + (units >> 31 & 1u));
   }
   h->table.amplitude = static_cast<float>(amplitude);
   h->table.pairs = rotary_dim / 2;
