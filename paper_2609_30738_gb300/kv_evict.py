@@ -470,6 +470,14 @@ def _raw_stream(device):
     return lambda: torch.cuda.current_stream(device).cuda_stream
 
 
+def _no_gradient(call: str):
+    """For a call on tensors that require a gradient: raises where autograd would have to see it."""
+    import torch
+    if torch.is_grad_enabled():
+        raise ValueError(f"{call}: records no gradient; call it under torch.no_grad(), or from an autograd.Function whose backward "
+                         "pass is rotate(..., transpose=True)")
+
+
 ROTARY_KINDS = {"none": 0, "linear": 1, "ntk": 2, "parts": 3, "yarn": 4}
 
 
@@ -517,11 +525,14 @@ class Rotary:
     def rotate(self, x, positions, out=None, transpose: bool = False, stream=None):
         """kv_evict_rotary_apply: x bf16 [tokens, heads, d] (or [..., heads, d] whose tokens are one run), positions int32
         [tokens]; out, of x's shape, is returned (None: x itself, in place). A [heads, tokens, d] tensor goes in as
-        x.transpose(0, 1). transpose: the gradient's rotation."""
+        x.transpose(0, 1). transpose: the gradient's rotation; none is recorded, and tensors that require one are refused
+        where it would have to be."""
         out = x if out is None else out
         shape = x.shape
         if len(shape) < 3 or shape[-1] != self.head_dim or out.shape != shape:
             raise ValueError(f"rotate: x and out are [tokens, heads, {self.head_dim}]")
+        if x.requires_grad or out.requires_grad:
+            _no_gradient("rotate")
         heads, device = shape[-2], x.get_device()
         tokens = x.numel() // (heads * self.head_dim) if heads else 0
         if positions.dtype is not self._i32 or positions.numel() != tokens or not positions.is_contiguous():
@@ -709,6 +720,8 @@ class Cache8:
                 raise ValueError("append: q and q_out hold a row of every query head for each token")
             if not self._here(q) or q_out.get_device() != self._device:
                 raise ValueError("append: q and q_out are on the cache's device")
+            if q.requires_grad or q_out.requires_grad:
+                _no_gradient("append")
             qs, outs = _row_strides(q, self.num_q_heads, "q"), _row_strides(q_out, self.num_q_heads, "q_out")
         elif q_out is not None:
             raise ValueError("append: q_out without q")
