@@ -496,7 +496,7 @@ void kv_evict_rotary_destroy(kve_rotary* rotary);
 
 /* x, out [n_tokens][heads][d] bf16, 16-byte aligned, with element strides {token, head} (multiples of 8,
  * not negative; NULL is dense; out's rows must not overlap): row (t, h) of out is that of x turned
- * by positions[t] (int32, device memory). out may be x with the same strides, or shares nothing with
+ * by positions[t] (int32). x and positions may be pinned host memory. out may be x with the same strides, or shares nothing with
  * it. transpose: 0 or 1. n_tokens * heads < 2^31; with 0 tokens nothing is done. KVE_EINVAL where
  * out is host memory or another device's than the current one. */
 kve_status kv_evict_rotary_apply(const kve_rotary* rotary, const uint16_t* x, const int64_t* x_strides,

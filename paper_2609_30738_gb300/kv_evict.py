@@ -470,6 +470,11 @@ def _raw_stream(device):
     return lambda: torch.cuda.current_stream(device).cuda_stream
 
 
+def _reads(t, device: int) -> bool:
+    """Whether kernels on CUDA device `device` can read t."""
+    return t.get_device() == device or (t.device.type == "cpu" and t.is_pinned())
+
+
 def _no_gradient(call: str):
     """For a call on tensors that require a gradient: raises where autograd would have to see it."""
     import torch
@@ -525,7 +530,7 @@ class Rotary:
     def rotate(self, x, positions, out=None, transpose: bool = False, stream=None):
         """kv_evict_rotary_apply: x bf16 [tokens, heads, d] (or [..., heads, d] whose tokens are one run), positions int32
         [tokens]; out, of x's shape, is returned (None: x itself, in place). A [heads, tokens, d] tensor goes in as
-        x.transpose(0, 1). transpose: the gradient's rotation; none is recorded, and tensors that require one are refused
+        x.transpose(0, 1). x and positions may lie in pinned memory. transpose: the gradient's rotation; none is recorded, and tensors that require one are refused
         where it would have to be."""
         out = x if out is None else out
         shape = x.shape
@@ -533,16 +538,17 @@ class Rotary:
             raise ValueError(f"rotate: x and out are [tokens, heads, {self.head_dim}]")
         if x.requires_grad or out.requires_grad:
             _no_gradient("rotate")
-        heads, device = shape[-2], x.get_device()
+        heads, device = shape[-2], out.get_device()
         tokens = x.numel() // (heads * self.head_dim) if heads else 0
         if positions.dtype is not self._i32 or positions.numel() != tokens or not positions.is_contiguous():
             raise ValueError("rotate: positions are one contiguous int32 value a token")
-        if device < 0 or out.get_device() != device or positions.get_device() != device:
-            raise ValueError("rotate: x, out and positions are on one CUDA device")
+        if device < 0 or not (x.get_device() == device or _reads(x, device)) or not (
+                positions.get_device() == device or _reads(positions, device)):
+            raise ValueError("rotate: x, out and positions are on one CUDA device, x and positions there or in pinned memory")
         if stream is None:
             current = self._streams.get(device)
             if current is None:
-                current = self._streams[device] = _raw_stream(x.device)
+                current = self._streams[device] = _raw_stream(out.device)
             stream = current()
         else:
             stream = _stream_ptr(stream)
@@ -598,7 +604,7 @@ class Cache8:
 
     def _here(self, t) -> bool:
         """Whether kernels on the cache's device can read t."""
-        return t.get_device() == self._device or (t.device.type == "cpu" and t.is_pinned())
+        return _reads(t, self._device)
 
     def _is_i32(self, t, n: int) -> bool:
         return (t.dtype is self._i32 and t.numel() == n and t.is_contiguous() and

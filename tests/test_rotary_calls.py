@@ -73,3 +73,33 @@ def test_gradients_through_a_function_of_the_callers():
         with torch.no_grad():
             assert torch.equal(cache.append(r, pos, k, k, slots, q=leaf, q_out=torch.empty_like(x)), want)
         assert cache.status() == K.KVE_OK
+
+
+@pytest.mark.gpu
+def test_what_is_read_may_lie_in_pinned_memory():
+    # as in append: what is turned and the positions, but not what is written
+    torch, K = _k(True)
+    rng = np.random.default_rng(2)
+    r = K.Rotary(interleaved=True)
+    x = to_torch(F.rows(rng, (37, 8, 128)))
+    pos = torch.from_numpy(rng.integers(0, 100000, 37).astype(np.int32)).cuda()
+    want = r.rotate(x, pos, torch.empty_like(x))
+    near, at = x.cpu().pin_memory(), pos.cpu().pin_memory()
+    for a, p in ((x, at), (near, pos), (near, at)):
+        assert torch.equal(r.rotate(a, p, torch.empty_like(x)), want)
+    for bad in ((near, pos), (x, pos, near), (x.cpu(), pos, torch.empty_like(x)), (x, pos.cpu())):
+        with pytest.raises(ValueError, match="CUDA device"):
+            r.rotate(*bad)
+    assert torch.equal(near, x.cpu())
+    k = x[:, :2].contiguous()
+    slots = torch.arange(37, dtype=torch.int32, device="cuda")
+    for Cache in (K.Cache8, K.Cache4):
+        made = []
+        for p in (pos, at):
+            cache = Cache(dict(num_layers=1, num_q_heads=8, num_kv_heads=2, head_dim=128), max_seqs=1, num_pages=3, max_pages=3,
+                          page_tokens=16)
+            cache.k.zero_()
+            q = cache.append(r, p, k, k, slots, q=x if p is pos else near, q_out=torch.empty_like(x))
+            assert torch.equal(q, want) and cache.status() == K.KVE_OK
+            made.append(cache.k)
+        assert torch.equal(*made)
