@@ -4,8 +4,9 @@ import numpy as np
 import pytest
 
 from oracle import cache4_oracle as Q
+from tests import cache4 as F
 from tests import cache8 as T
-from tests.test_cache4_gpu import _attend, _k
+from tests.test_cache4_gpu import _attend, _k, _np, _spec
 
 pytestmark = pytest.mark.gpu
 
@@ -96,3 +97,25 @@ def test_blocks_of_eight_warps_are_joined(n, length, P, hq, hkv, t):
         again, l2 = torch.empty_like(out), torch.empty_like(lse)
         cache.attend(*args, again, l2)
         assert torch.equal(again, out) and torch.equal(l2, lse)
+
+
+@pytest.mark.parametrize("lens,P,hq,hkv,t", [([96 + 40 * i for i in range(16)], 32, 32, 8, 1), ([300, 0, 5, 2000], 128, 8, 2, 4),
+                                             ([700] * 9, 16, 8, 1, 1)])
+def test_a_table_wider_than_its_sequences(lens, P, hq, hkv, t):
+    # the width of a table chooses between kernels, not between results
+    torch, K = _k()
+    rng = np.random.default_rng(sum(lens))
+    cache, _, _, (q, table, lens_t, layer), _ = _attend(K, rng, lens, P, hq, hkv, t, check=False)
+    spare = max(0, 2049 // P + 1 - cache.num_pages)   # (a table is no wider than the pool)
+    grown = [torch.cat([x, x[:1].expand(spare, *x.shape[1:])]) for x in (cache.k, cache.k_param, cache.v, cache.v_param)]
+    pages = len(grown[0])
+    wide = K.Cache4(_spec(1, hq, hkv), max_seqs=len(lens), num_pages=pages, max_pages=pages, page_tokens=P, k=grown[0],
+                    k_param=grown[1], v=grown[2], v_param=grown[3])
+    assert pages * P > 2048
+    to = torch.full((1, len(lens), pages), -1, dtype=torch.int32, device="cuda")
+    to[:, :, :table.shape[2]] = table
+    out, lse = torch.empty_like(q), torch.empty(q.shape[:3], device="cuda")
+    wide.attend(q, to, lens_t, layer, out, lse)
+    F.check_attention(_np(out), lse.cpu().numpy().astype(np.float64), _np(q), cache.k.cpu().numpy(), _np(cache.k_param),
+                      cache.v.cpu().numpy(), _np(cache.v_param), table[0].cpu().numpy(), np.array(lens), hq // hkv)
+    assert wide.status() == K.KVE_OK
