@@ -523,6 +523,9 @@ constexpr int64_t kStoreBlockTokens = 1024;
 template <class Params>
 constexpr int kStoreThreads = std::is_same_v<Params, CacheAppendParams> ? 768 : 1024;
 
+__device__ __forceinline__ const CacheStoreParams& rows_of(const CacheStoreParams& p) { return p; }
+__device__ __forceinline__ const CacheStoreParams& rows_of(const CacheAppendParams& p) { return p.s; }
+
 // Of a row that turns, each of 16 lanes has both elements of four pairs, as its two pieces: no lane waits for another's, and no
 // turn is computed twice in a row.
 struct LaneTurns {
@@ -579,12 +582,7 @@ cache_store_kernel(const __grid_constant__ Params A, uint32_t row_ctas) {
       return;
     }
   }
-  const CacheStoreParams& P = [&]() -> const CacheStoreParams& {
-    if constexpr (kTurn)
-      return A.s;
-    else
-      return A;
-  }();
+  const CacheStoreParams& P = rows_of(A);
   constexpr int kTeam = kTeamThreads<kPage>, kGroups = kPage / kGroupRows, kTeams = kRowThreads<kPage> / kTeam;
   constexpr int kWords = kPage / 16;   // of 32 tokens: a block of at most P and the run that leaves it
   __shared__ uint32_t team_max[kTeams][kGroups];
