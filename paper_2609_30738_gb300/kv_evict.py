@@ -470,9 +470,8 @@ def _raw_stream(device):
     return lambda: torch.cuda.current_stream(device).cuda_stream
 
 
-def _reads(t, device: int) -> bool:
-    """Whether kernels on CUDA device `device` can read t."""
-    return t.get_device() == device or (t.device.type == "cpu" and t.is_pinned())
+def _pinned(t) -> bool:
+    return t.device.type == "cpu" and t.is_pinned()
 
 
 def _no_gradient(call: str):
@@ -542,8 +541,8 @@ class Rotary:
         tokens = x.numel() // (heads * self.head_dim) if heads else 0
         if positions.dtype is not self._i32 or positions.numel() != tokens or not positions.is_contiguous():
             raise ValueError("rotate: positions are one contiguous int32 value a token")
-        if device < 0 or not (x.get_device() == device or _reads(x, device)) or not (
-                positions.get_device() == device or _reads(positions, device)):
+        if (device < 0 or (x.get_device() != device and not _pinned(x)) or
+                (positions.get_device() != device and not _pinned(positions))):
             raise ValueError("rotate: x, out and positions are on one CUDA device, x and positions there or in pinned memory")
         if stream is None:
             current = self._streams.get(device)
@@ -604,7 +603,7 @@ class Cache8:
 
     def _here(self, t) -> bool:
         """Whether kernels on the cache's device can read t."""
-        return _reads(t, self._device)
+        return t.get_device() == self._device or _pinned(t)
 
     def _is_i32(self, t, n: int) -> bool:
         return (t.dtype is self._i32 and t.numel() == n and t.is_contiguous() and
