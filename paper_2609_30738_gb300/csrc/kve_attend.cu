@@ -213,7 +213,7 @@ cache_attend_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_const
     prefetch_tensormap(&tm_v);
   }
   wait_previous_kernel();
-  // The line's length, and the block in which this CTA's share starts: a run of sequences a thread
+  // The line's length, and the block in which this CTA's share starts: a run of sequences a thread (as line_share of kve_line.cuh)
   const int cap = P.c.max_pages << P.c.page_shift;
   const int per = (P.n_seq + kThreads - 1) / kThreads;
   const int s0 = min(static_cast<int>(threadIdx.x) * per, P.n_seq), s1 = min(s0 + per, P.n_seq);

@@ -6,12 +6,12 @@
 // Scales and zeros never touch a code: both products are of the codes alone.
 //
 // Bound by the read of the cache, 136 bytes a token and head, and by start and end: 64 ragged sequences of 512 to 16384 tokens and 8
-// heads (237 MB) take 46.5 us where a copy's rate is 35.5, and 400 of 100 to 8000 (759 MB) 129, so between the two it runs at 94% of
+// heads (237 MB) take 47.2 us where a copy's rate is 35.5, and 400 of 100 to 8000 (759 MB) 131, so between the two it runs at 93% of
 // that rate, beside 9 us. 5 of them are any call's (96 tokens: lengths, cut, table, first codes, a step, output); then the first copies
-// of all CTAs at once, the ends of parts, the join, which is longest for few heads of long sequences (one of 131072 tokens, 143 MB, 33.0
-// of 21.3). A step of a warp, 32 tokens and 8 rows, is 368 instructions, half of them the integer unit's, most of which unpack codes.
-// 16 rows are 489, of them 64 matrix products, and two warps a scheduler that wait for their own results: 24 sequences of 500 to 8192
-// tokens 29.1 us of 10, 16 of 8192 with 32 rows 74.5 of 21.7.
+// of all CTAs at once, the ends of parts, the join, which is longest for few heads of long sequences (one of 131072 tokens, 143 MB, 33.3
+// of 21.3). A step of a warp, 32 tokens and 8 rows, is 375 instructions, half of them the integer unit's, most of which unpack codes.
+// 16 rows are 494, of them 64 matrix products, and two warps a scheduler that wait for their own results: 24 sequences of 500 to 8192
+// tokens 29.2 us of 10, 16 of 8192 with 32 rows 76 of 21.7.
 //
 // A code becomes a matrix operand in registers, with half an instruction an element and no conversion: the low four bits of an f16
 // are the subnormal c 2^-24 and the next four 16 c 2^-24, so a word of eight codes is four operand registers by a shift and masks. The
@@ -32,7 +32,8 @@
 // that a token of far larger values costs the others nothing where it hardly counts. References move only when a maximum
 // passes them by 2^8, which leaves the rescaling of the output to a few steps. What a warp leaves at the end of a part, and a CTA for the join, is
 // the average over its tokens beside their maximum and sum, so values at either end of fp32 keep their bits whatever the length; the sum
-// of p z before that is scaled down by the length only once a |z| of 2^96 comes.
+// of p z before that is scaled down by the length only once a |z| of 2^96 comes. (Sums in a unit of the length throughout lose s near
+// 2^-119 behind some thousand tokens; they took 46.9 us for 47.2 on the 64, 33.0 for 33.3 and 74.6 for 76.)
 //
 // A warp takes 32 tokens a step from a ring of its own in shared memory, and has maxima, sums and output of its own: no warp waits for
 // another before a part ends. It fills its ring itself, across the ends of parts, by asynchronous copies that stand between its
@@ -858,12 +859,14 @@ cudaError_t launch_cache4_attend(const kve_cache& c, const AttendParams& p, cuda
   const int64_t rows = static_cast<int64_t>(p.q_tokens) * p.c.group;
   const int64_t blocks = static_cast<int64_t>(p.n_seq) * p.c.heads * (rows > 8 ? (rows + 15) / 16 : 1);
   const int64_t longest = static_cast<int64_t>(p.c.max_pages) << p.c.page_shift;
-  // Few warps a CTA make the end of a part cheap, many cut a block into fewer parts and its steps among more.
+  // Few warps a CTA make the end of a part cheap, many cut a block into fewer parts and its steps among more. (Figures of both sides from
+  // the same day, with tables as wide as the longest sequence; today's are up to 2% more.)
   // Three blocks an SM or more: 2 warps a CTA. (8 heads; 2 against 4 warps: 64 ragged sequences 46.2 and 46.9 us, 400 of 100 to 8000
   // tokens 129 and 136, 400 of 20 to 800 34.7 and 41.7, 1000 of 64 42.2 and 63.3; 50 of 200 to 800, 400 blocks, 15.8 and 13.0. 16
   // rows: 100 of 100 to 3000 39.5 and 41.9, 400 of 20 to 800 64 and 78.)
   if (blocks >= 3 * c.sms) return attend4_warps<2>(c, p, stream);
-  // No more than one block an SM and a table that holds short ones only: 8 warps. (8 against 4: 16 of 96 to 700 6.6 and 7.6, 8 of 100 to
+  // No more than one block an SM and a table that holds short ones only (lengths are not known here, so a wider table takes 4 warps for
+  // short ones too: 16 of 96 to 700 with a table of 16384 tokens 7.7 for 6.6): 8 warps. (8 against 4: 16 of 96 to 700 6.6 and 7.6, 8 of 100 to
   // 800 7.4 and 8.1, 8 of 500 to 2000 11.5 and 12.0, 19 of 50 to 1000 8.6 and 10.4; 24, 192 blocks, 10.5 and 8.8, 4 of 200 to 3000
   // 13.3 and 11.0, 8 of 32768 56.3 and 51.0, one of 131072 32.0 and 32.8. 16 rows: 16 of 100 to 700 12.1 and 12.6, 19 of 100 to 2000
   // 16.4 and 17.4.)

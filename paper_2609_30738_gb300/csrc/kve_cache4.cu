@@ -103,8 +103,10 @@ __device__ __forceinline__ void write_codes4(const uint32_t (&c)[4], uint8_t* co
 // the last tiles turn the queries, and keys are turned (and rounded to bf16) before they are coded.
 //
 // Without turns a lane has one row in flight and an SM 56 warps: 23,815 tokens of 8 heads (123 MB) 22.9 us of 18.5, 10,000 10.8,
-// 1000 2.3; two rows and 40 warps took 26.4, 12.8 and 2.4, with 8 lanes a row 23.5, 13.1 and 2.9. With turns four rows and 32 warps:
-// those tokens with 32 query heads (514 MB) 81.5 us of 76.9; two rows and 40 warps spill (158), four and 24 warps 95.
+// 1000 2.3; two rows and 40 warps took 26.4, 12.8 and 2.4, with 8 lanes a row 23.5, 13.1 and 2.9. Its 32 registers spill 44 bytes: with 48
+// warps and 12 bytes 23.9, 11.5 and 2.25, with 40 and none 25.0, 12.1 and 2.2. With turns four rows and 32 warps: those tokens with 32
+// query heads (514 MB) 84.2 us of 76.9, 1000 x 8 tokens 31.2, 256 3.7, 16 2.7, whatever the page. 64 registers spill 96 bytes; 24 warps
+// and no spills take 84.2, 30.6, 3.4 and 2.45; two rows and 40 warps spill more (158).
 template <bool kTurn>
 __global__ void __launch_bounds__(kRowThreads4, kTurn ? 4 : 7) cache4_store_kernel(const __grid_constant__ CacheAppendParams A, int tile_tokens,
                                                                     int tile_heads, uint32_t row_tiles) {
@@ -185,9 +187,9 @@ __global__ void __launch_bounds__(kRowThreads4, kTurn ? 4 : 7) cache4_store_kern
 }
 
 // Step 4 into the cache: a CTA has keys or values of a unit, 4 lanes a row, kGatherTurns rows one after the other with the next
-// one's place looked up ahead. Whole rows at random places: 16 requests of 509 + 8 rows in 8 layers (327 MB) take 54.4 us of 48.9 at
-// a copy's rate, 32 layers of one request's 96 rows 4.5 of 2.4. With 8 lanes a row and keys and values in one CTA 61.5 and 4.9; with
-// 2 rows a CTA 66 and 4.4, with 8 57.1 and 4.6; with 6 CTAs an SM 56.1, with 5 60.5.
+// one's place looked up ahead. Whole rows at random places: 16 requests of 509 + 8 rows in 8 layers (327 MB) take 54.1 us of 48.9 at
+// a copy's rate, 32 layers of one request's 96 rows 4.5 of 2.4 (12 bytes of spills; without, at 6 CTAs an SM, 56.1 and 4.5). With 8 lanes a row and keys and values in one CTA 61.5 and 4.9; with
+// 2 rows a CTA 66 and 4.4, with 8 57.1 and 4.6; with 5 CTAs an SM 60.5.
 constexpr int kGatherTurns = 4, kGatherGroups = kRowThreads4 / 4;
 constexpr int kGatherTile = kGatherGroups * kGatherTurns;   // rows of a unit that a CTA has
 __global__ void __launch_bounds__(kRowThreads4, 7) cache4_gather_kernel(const __grid_constant__ CacheGatherParams P,
@@ -249,7 +251,7 @@ cudaError_t store4(CacheAppendParams p, cudaStream_t stream) {
   constexpr int kWide = kTurn ? kRowThreads4 : 2 * kRowThreads4;   // (8 lanes a row there)
   int64_t tiles = cut_rotate<kWide>(cut);
   // With turns, a group a token and all its heads one after the other, where that still gives every SM a tile of keys and one of
-  // values: 6000 tokens 26.2 us for 31.3, 24k 95 for 117.
+  // values: 6000 tokens 26.2 us for 31.3, 24k 95 for 117 at the time (24.7 and 84.2 now).
   if (kTurn && cut.n_tokens >= 152 * kStoreTokens) {
     cut.tile_tokens = kStoreTokens;
     cut.tile_heads = cut.heads;

@@ -1,5 +1,7 @@
 // How the attention over a paged cache is cut: the tiles of all (sequence, head, row block)s in one line, an even
-// share of it for every CTA, whatever the lengths, which are read on the GPU.
+// share of it for every CTA, whatever the lengths, which are read on the GPU. Blocks, cuts and the walk over them are those of the 8-bit
+// cache's attention too; that has line_share's steps in a body of its own, around its tensor memory's allocation (kve_attend.cu), and
+// what Cuts::parts says has to hold for both.
 #pragma once
 
 #include "kve_internal.h"

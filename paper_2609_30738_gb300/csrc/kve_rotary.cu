@@ -17,7 +17,7 @@ namespace {
 constexpr int kRotateThreads = 256;
 
 // 16,411 tokens of 40 heads (336 MB, half of each head turns) take 51.4 us of 50.3 at a copy's rate, the window rows of 32 layers
-// (17 MB) 5.2 of 2.5, which is the launch, positions, rows. Two rows a lane in flight and 32 warps an SM; four rows and 24 warps took
+// (17 MB) 5.1 of 2.5, which is the launch, positions, rows. Two rows a lane in flight and 32 warps an SM; four rows and 24 warps took
 // 52.1 and 5.8, two and 40 52.1 and 5.3, two and 48 (spills) 58.3 and 6.6.
 __global__ void __launch_bounds__(kRotateThreads, 4) rotate_kernel(const __grid_constant__ RotateParams P) {
   wait_previous_kernel();
