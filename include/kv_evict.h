@@ -464,7 +464,7 @@ kve_status kv_evict_cache_attend(const kve_cache* cache, int32_t layer, int32_t 
  *    (x_2j, x_{2j+1}) where interleaved, becomes
  *      A (a cos t - b sin t),  A (b cos t + a sin t),  t = position * frequencies[j];
  *    the elements behind n stay as they are. For frequencies below 2^62 in magnitude angles are exact
- *    to 2^-31 of a turn at every int32 position (negative ones too); cos and sin to 2^-22 beside that;
+ *    to 2^-31 of a turn at every int32 position (negative ones too); cos and sin to 2^-23 beside that;
  *    results are rounded once to bf16.
  *  * The transpose, A (a cos t + b sin t), A (b cos t - a sin t), is the gradient of that, and with
  *    A = 1 takes it out again.

@@ -16,22 +16,27 @@ __device__ __forceinline__ uint2 turn_at(const RotaryTable& r, int j) {
 
 // {cos, sin} times the amplitude of the angle that a pair has at position pos. The angle is a fraction of a turn in 64-bit
 // integers (exact for every position, where an fp32 product is off by 2^-24 of the whole angle); its upper 32 bits are cut into
-// the nearest half turn, which is a sign, and a rest x of at most pi / 2, whose sine over x and cosine are their Taylor
-// polynomials up to x^14 in packed fp32 (2^-33 off at pi / 2): 2^-22 with the roundings.
+// the nearest quarter turn, which says which of the two is which and their signs, and a rest x of at most pi / 4, whose sine over x and
+// cosine are their Taylor polynomials up to x^10 in packed fp32 (2^-32 off at pi / 4): 2^-23 with the roundings, half of it those of x.
+// (Half turns, with polynomials up to x^14, were off by 2^-22.1: of 2M turned elements 95 went to another bf16 number than the exact result does,
+// now 68, and 61 where cos and sin are rounded from 64 bits and each product by itself.)
 __device__ __forceinline__ float2 turn_of(uint2 turn, float amplitude, int pos) {
   const uint32_t u = static_cast<uint32_t>(pos) * turn.y + static_cast<uint32_t>(__mulhi(pos, static_cast<int32_t>(turn.x)));
-  const float x = static_cast<float>(static_cast<int32_t>(u << 1)) * 7.31459039633577841e-10f;   // pi 2^-32
+  const float x = static_cast<float>(static_cast<int32_t>(u << 2)) * 3.65729519816788900e-10f;   // pi 2^-33
   const float y = x * x;
   const float2 yy = make_float2(y, y);
-  float2 p = ffma2(yy, make_float2(-7.64716373e-13f, -1.14707456e-11f), make_float2(1.60590438e-10f, 2.08767570e-9f));
-  p = ffma2(yy, p, make_float2(-2.50521084e-8f, -2.75573192e-7f));
-  p = ffma2(yy, p, make_float2(2.75573192e-6f, 2.48015873e-5f));
+  float2 p = ffma2(yy, make_float2(-2.50521084e-8f, -2.75573192e-7f), make_float2(2.75573192e-6f, 2.48015873e-5f));
   p = ffma2(yy, p, make_float2(-1.98412698e-4f, -1.38888889e-3f));
   p = ffma2(yy, p, make_float2(8.33333333e-3f, 4.16666667e-2f));
   p = ffma2(yy, p, make_float2(-1.66666667e-1f, -0.5f));
   p = ffma2(yy, p, make_float2(1.f, 1.f));
-  const float f = __uint_as_float(__float_as_uint(amplitude) ^ ((u + 0x40000000u) & 0x80000000u));
-  return make_float2(p.y * f, p.x * x * f);
+  const float s = p.x * x;
+  // quarters 1 and 3 change places; the cosine is negative in 1 and 2, the sine in 2 and 3
+  const uint32_t w = u + 0x20000000u;
+  const bool odd = (w & 0x40000000u) != 0;
+  const float a = __uint_as_float(__float_as_uint(amplitude) ^ ((w + 0x40000000u) & 0x80000000u));
+  const float b = __uint_as_float(__float_as_uint(amplitude) ^ (w & 0x80000000u));
+  return make_float2((odd ? s : p.y) * a, (odd ? p.y : s) * b);
 }
 
 // (a, b) turned: (a c - b s, b c + a s), each rounded once behind its second product.

@@ -102,3 +102,37 @@ def test_far_appends_are_rotate_then_store(bits, n, inter, P):
     for name in names:
         assert torch.equal(getattr(a, name), getattr(b, name)), name
     assert a.status() == b.status() == K.KVE_OK
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("inter", [False, True])
+def test_cosines_and_sines_to_2_to_the_minus_23(inter):
+    # Pairs (a, b) of bf16 numbers at an angle t that turns them to (nearly) (0, b'): a cos t - b sin t is so small there that bf16 rounds
+    # it by 2^-28 at most, and the errors of the two products show. With a cosine and a sine off by E each and the product that
+    # is rounded by half an fp32 step, 2^-24 |b sin t|, the result is off by (|a| + |b|) E + 2^-24 |b sin t|; the angle's 2^-31 of a turn
+    # move it by 2^-28.3 hypot(a, b) more, and its own roundings are relative to it.
+    import torch
+    if not torch.cuda.is_available():
+        pytest.skip("needs a GPU")
+    K = _k()
+    rng = np.random.default_rng(11)
+    n = 64 * 256
+    small = rng.integers(128, 257, n) * np.exp2(-rng.integers(8, 17, n).astype(float))   # bf16 numbers in [2^-9, 1]
+    flip = rng.random(n) < 0.5
+    a, b = np.where(flip, small, 1.0) * rng.choice([-1, 1], n), np.where(flip, 1.0, small) * rng.choice([-1, 1], n)
+    t = np.arctan2(a, b) + rng.uniform(-2.0 ** -20, 2.0 ** -20, n)
+    t += np.pi * rng.integers(-1, 2, n)
+    first, second = (slice(0, None, 2), slice(1, None, 2)) if inter else (slice(0, 64), slice(64, None))
+    x = torch.zeros(n // 64, 1, 128, dtype=torch.bfloat16)
+    x[:, 0, first], x[:, 0, second] = (torch.from_numpy(v.reshape(-1, 64)).to(torch.bfloat16) for v in (a, b))
+    assert np.array_equal(x[:, 0, first].double().numpy().reshape(-1), a) and np.array_equal(x[:, 0, second].double().numpy().reshape(-1), b)
+    x, one = x.cuda(), torch.ones(1, dtype=torch.int32, device="cuda")
+    for i in range(n // 64):
+        K.Rotary(frequencies=t[64 * i:64 * i + 64], interleaved=inter).rotate(x[i:i + 1], one)
+    got = x[:, 0, first].double().cpu().numpy().reshape(-1)
+    want = a * np.cos(t) - b * np.sin(t)
+    assert np.abs(want).max() < 2.0 ** -19
+    bound = ((np.abs(a) + np.abs(b)) * 2.0 ** -23 + 2.0 ** -24 * np.abs(b * np.sin(t)) + 2.0 ** -28.3 * np.hypot(a, b) +
+             2.0 ** -8 * np.abs(want) + 2.0 ** -30)
+    err = np.abs(got - want)
+    assert (err <= bound).all(), float((err / bound).max())
