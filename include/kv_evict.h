@@ -496,9 +496,9 @@ void kv_evict_rotary_destroy(kve_rotary* rotary);
 
 /* x, out [n_tokens][heads][d] bf16, 16-byte aligned, with element strides {token, head} (multiples of 8,
  * not negative; NULL is dense; out's rows must not overlap): row (t, h) of out is that of x turned
- * by positions[t] (int32). x and positions may be pinned host memory. out may be x with the same strides, or shares nothing with
- * it. transpose: 0 or 1. n_tokens * heads < 2^31; with 0 tokens nothing is done. KVE_EINVAL where
- * out is host memory or another device's than the current one. */
+ * by positions[t] (int32). x and positions may be pinned host memory. out may be x with the same
+ * strides, or shares nothing with it. transpose: 0 or 1. n_tokens * heads < 2^31; with 0 tokens
+ * nothing is done. KVE_EINVAL where out is host memory or another device's than the current one. */
 kve_status kv_evict_rotary_apply(const kve_rotary* rotary, const uint16_t* x, const int64_t* x_strides,
                                  uint16_t* out, const int64_t* out_strides, int32_t heads,
                                  const int32_t* positions, int64_t n_tokens, int32_t transpose,
@@ -529,8 +529,8 @@ kve_status kv_evict_cache_append(const kve_cache* cache, const kve_rotary* rotar
  *    row, an element being s c + z. (128-byte and 16-byte aligned.)
  *  * A row x is written as z = min x, s = RN_bf16(fl(fl((max x - min x) / 16) * fl(16 / 15))),
  *    c = fl(fl((x - z) / 16) / (s / 16)) rounded to the nearest integer (ties to even), fl to fp32;
- *    s = 0 and c = 0 where s would be below 2^-120. An element is off by at most 0.53 of a step s. A row with an infinity or a NaN becomes s = z = NaN, c = 0, and so
- *    NaN wherever it is seen.
+ *    s = 0 and c = 0 where s would be below 2^-120. An element is off by at most 0.53 of a step s. A
+ *    row with an infinity or a NaN becomes s = z = NaN, c = 0, and so NaN wherever it is seen.
  *  * Rows share nothing: a page may be written in any order, and a slot that a call names twice gets
  *    undefined codes (its row only).
  *  * Attention: l = (s (q . c) + z sum q) / sqrt(d), out = sum p s c + sum p z, statistics and sums in

@@ -30,9 +30,9 @@
 //      itself down to 2^-20 of that reference, an absolute 2^-31 of it below.
 // Maxima, sums, the part of z and the output are fp32. The reference of w is the product's own, not the probability's, so
 // that a token of far larger values costs the others nothing where it hardly counts. References move only when a maximum
-// passes them by 2^8, which leaves the rescaling of the output to a few steps. What a warp leaves at the end of a part, and a CTA for the join, is
-// the average over its tokens beside their maximum and sum, so values at either end of fp32 keep their bits whatever the length; the sum
-// of p z before that is scaled down by the length only once a |z| of 2^96 comes. (Sums in a unit of the length throughout lose s near
+// passes them by 2^8, which leaves the rescaling of the output to a few steps. What a warp leaves at the end of a
+// part, and a CTA for the join, is the average over its tokens beside their maximum and sum, so values at either end of fp32 keep their
+// bits whatever the length; the sum of p z before that is scaled down by the length only once a |z| of 2^96 comes. (Sums in a unit of the length throughout lose s near
 // 2^-119 behind some thousand tokens; they took 46.9 us for 47.2 on the 64, 33.0 for 33.3 and 74.6 for 76.)
 //
 // A warp takes 32 tokens a step from a ring of its own in shared memory, and has maxima, sums and output of its own: no warp waits for

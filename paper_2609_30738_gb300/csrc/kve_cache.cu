@@ -567,7 +567,7 @@ __device__ __forceinline__ void turn_rows(uint4 (&x)[kGroupRows], const RotaryTa
 // way: they start first because they take longer (as the last: 2000 tokens 14.8 us for 11.7, 400 x 8 23.1 for 20.1, 24k 102.6
 // for 101.9; evenly between the others 13.6, 24.5 and 112, all at the time). 24k tokens with 32 query heads (537 MB) take 96.5 us of
 // 80.3 at a copy's rate, 6000 without their queries 16.8 of 9.2: every head's rows compute their turns. Pages of 16 and 32 spill 76
-// bytes: 24k tokens 103 us, 1000 x 8 40.0 for 36.5, 16 3.1 for 2.8. (With elements side by side, the
+// bytes: 24k tokens 103 us, 1000 x 8 40.4 for 36.7, 16 3.3 for 2.9. (With elements side by side, the
 // pairs' halves exchanged by shuffles, 100.9 and 18.9; turns kept in shared memory for four heads one after the other 114.9, for two
 // 120.) One body with the plain store as a kernel of its own: as a function of both it spilled three times as much.
 template <int kPage, class Params>
